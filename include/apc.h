@@ -117,7 +117,7 @@ typedef struct apc_tensor {
   uint64_t global_offset;
 } apc_tensor;
 
-typedef enum apc_dtype { APC_F32 = 0, APC_BF16 = 1 } apc_dtype;
+typedef enum apc_dtype { APC_F32 = 0, APC_BF16 = 1, APC_F16 = 2 } apc_dtype;  /* APC_F16: the operators below only */
 
 /* One buffer for apc_digest: n elements of `dtype` at `data` (device), whose
  * element 0 has index global_offset in the flat model, summed into digest
@@ -217,6 +217,123 @@ apc_status apc_digest(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slot
 apc_status apc_count_nonzero(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots, apc_stream_t stream,
                              uint64_t *out_counts);
 
+/* ---- The operators around a training step's output head -----------------
+ *
+ * What makes the gradient that apc_commit_step consumes, for a model whose
+ * head is distilled in 8 bits: quantization with a scale per block of 128, the
+ * matrix product of such operands, and the distillation loss with its
+ * gradient.  Every sum has a fixed order and no result depends on the order of
+ * atomics, so replicas that run the same step commit identical bits and their
+ * digests agree.
+ *
+ * Matrices are row-major: element (i, j) of a matrix with pitch P sits at
+ * i*P + j, and columns behind the last are neither read nor written.  A matrix
+ * without rows or columns is valid and its pointers may be NULL.  Sizes are at
+ * most 2^31 - 1 rows and columns.  Outputs must not overlap each other or any
+ * input, but for the one aliasing that apc_distill_grad allows.  The
+ * conventions at the head of this file hold (device memory of the caller, no
+ * synchronization, statuses); APC_GRID_LIMIT and apc_set_reserved_sms apply. */
+
+/* 8-bit formats: E4M3 (largest value 448, no infinities) and E5M2 (57,344). */
+typedef enum apc_fp8 { APC_E4M3 = 0, APC_E5M2 = 1 } apc_fp8;
+
+/* A matrix of R rows and C columns in 8 bits with a scale per block.  The value
+ * of element (i, j) is data[i*pitch + j] * scale[(j/128)*scale_pitch + i/block_rows].
+ *   data        16-byte aligned, as is the pitch (bytes between rows)
+ *   scale       fp32: one line of ceil(R/block_rows) scales for each 128 columns
+ *   block_rows  1 (a scale for every 128 values of a row) or 128 (square blocks) */
+typedef struct apc_fp8_matrix {
+  void *data;
+  float *scale;
+  int64_t pitch;
+  int64_t scale_pitch;
+  uint32_t format; /* apc_fp8 */
+  uint32_t block_rows;
+} apc_fp8_matrix;
+
+/* Quantize x (rows x cols, apc_dtype, pitch in elements) into q and, unless qt
+ * is NULL, x transposed (cols x rows) into qt, from one reading of x.
+ *   scale   of a block: the smallest power of two 2^e, e >= -126, with
+ *           largest finite |x| of the block <= 2^e * the format's largest
+ *           value; 1 for a block whose finite values are all zero
+ *   data    x / scale rounded to the nearest 8-bit value, ties to even.  The
+ *           division is exact, so q is the same on every machine
+ * Non-finite values do not enter the scale: a NaN becomes a NaN, an infinity a
+ * NaN in E4M3 (which has no infinities) and an infinity in E5M2.
+ * q and qt take the same block_rows; their formats may differ.
+ * Returns APC_EINVAL (null or overlapping buffers, unknown types, a pitch below
+ * the width, memory of another device), APC_EALIGN (x not aligned to its
+ * element; data or its pitch not to 16 bytes; scale not to 4), APC_ERANGE
+ * (sizes), APC_ECUDA or APC_OK. */
+apc_status apc_quantize_fp8(const void *x, int64_t rows, int64_t cols, int64_t pitch, uint32_t dtype,
+                            const apc_fp8_matrix *q, const apc_fp8_matrix *qt, apc_stream_t stream);
+
+/* out = a b^T: out[i, j] = sum over k of a[i, k] b[j, k], for a (m x k) and b
+ * (n x k) in 8 bits and out (m x n, apc_dtype, out_pitch in elements).
+ * The products of each 128 values of k are summed by the tensor cores in fp32,
+ * the sums are multiplied by both blocks' scales and added in fp32 in a fixed
+ * order, and the total is rounded once to out's type.  k = 0 writes zeros.
+ * The two formats and the two block sizes may differ.
+ * Errors as apc_quantize_fp8; APC_ETIMEOUT is reported by apc_device_status
+ * if a bounded wait of the kernel gave up (out is then incomplete and the call
+ * can be repeated). */
+apc_status apc_matmul_fp8(const apc_fp8_matrix *a, const apc_fp8_matrix *b, int64_t m, int64_t n, int64_t k, void *out,
+                          int64_t out_pitch, uint32_t out_dtype, apc_stream_t stream);
+
+typedef enum apc_index { APC_I32 = 0, APC_I64 = 1 } apc_index;
+
+#define APC_DISTILL_MAX_K 1024
+
+/* Distillation of a student from the k largest logits of a teacher in each row.
+ *
+ * Row t has the student's logits z, the teacher's logits u_i at the vocabulary's
+ * places ids_i, and optionally a label y.  With tau the temperature,
+ *   p_i  = exp(u_i/tau) / sum of exp(u_j/tau) over the row's entries or, with
+ *          teacher_lse, exp(u_i/tau - teacher_lse): the teacher's probabilities
+ *          in its whole vocabulary, whose sum P is below 1
+ *   q    = softmax(z/tau)
+ *   loss = kd_weight * tau^2 * sum of p_i (log p_i - log q[ids_i])
+ *          + label_weight * (log sum exp(z) - z[y])
+ *   d loss / dz = kd_weight * tau * (P q - p) + label_weight * (softmax(z) - onehot(y))
+ * An entry counts only where its id lies in [0, vocab) and its logit is not
+ * -infinity, whatever else stands there; so does a label.  Entries with the
+ * same id add up.  A row without entries has no teacher's part.  A row whose
+ * logits are all -infinity has loss 0, lse -infinity and gradient 0.  Masked
+ * logits (-infinity) have q = 0; an entry or label there makes the loss +infinity.
+ *   logits        rows x vocab, apc_dtype, pitch in elements
+ *   ids, teacher  rows x k (k <= APC_DISTILL_MAX_K; 0: no teacher), apc_index and apc_dtype
+ *   teacher_lse   fp32, one per row: log sum exp(u/tau) over the whole vocabulary, or NULL
+ *   labels        apc_index, one per row, or NULL
+ *   temperature   > 0; kd_weight, label_weight >= 0; all finite */
+typedef struct apc_distill {
+  const void *logits;
+  const void *ids;
+  const void *teacher;
+  const float *teacher_lse;
+  const void *labels;
+  int64_t rows, vocab, k;
+  int64_t pitch, ids_pitch, teacher_pitch;
+  uint32_t dtype, ids_dtype, teacher_dtype, labels_dtype;
+  double temperature, kd_weight, label_weight;
+} apc_distill;
+
+/* loss: fp32, one per row.  lse: the statistics for the gradient, fp32, the
+ * rows' log sum exp(z/tau) and, with labels, behind them the rows' log sum
+ * exp(z).  Reads the logits once.  Errors as apc_quantize_fp8. */
+apc_status apc_distill_loss(const apc_distill *d, float *loss, float *lse, apc_stream_t stream);
+
+/* dlogits (rows x vocab, the logits' type): grad_loss[t] times the gradient of
+ * row t's loss, from lse as apc_distill_loss left it.  A row whose grad_loss is
+ * 0 gets zeros, whatever its logits hold.  dlogits may be the logits' own
+ * memory with the same pitch: the gradient then takes their place. */
+apc_status apc_distill_grad(const apc_distill *d, const float *lse, const float *grad_loss, void *dlogits,
+                            int64_t dlogits_pitch, apc_stream_t stream);
+
+/* Both in one pass over the logits, for a grad_loss that is known before the
+ * loss (a mean's weights, a loss scale). */
+apc_status apc_distill_loss_grad(const apc_distill *d, const float *grad_loss, float *loss, float *lse, void *dlogits,
+                                 int64_t dlogits_pitch, apc_stream_t stream);
+
 /* The eight binary32 scalars that apc_commit_step passes to the device for
  * step t, in the order b1, 1-b1, b2, 1-b2, eps, 1-lr*wd, lr/(1-b1^t),
  * 1/sqrt(1-b2^t).  t is the optimizer step tau_opt of the preserved state
@@ -295,7 +412,7 @@ const char *apc_status_string(apc_status s);
  * pointer stays valid until that thread's next apc_* call. */
 const char *apc_last_error(void);
 
-/* ABI version of this header: 3. */
+/* ABI version of this header: 3 (functions were added since; none changed). */
 int32_t apc_version(void);
 
 #ifdef __cplusplus

@@ -18,6 +18,10 @@ Entry points mirror the C names:
 * :func:`upload` -> ``apc_upload``: host-to-device upload executed by a
   bounded number of CTAs, and :func:`set_reserved_sms` ->
   ``apc_set_reserved_sms``: SMs the persistent kernels leave free for it.
+* :mod:`.operators`: 8-bit quantization, the block-scaled 8-bit product and
+  distillation, around the output head of the step that makes the gradient
+  (``quantize_fp8``, ``matmul_fp8``, ``distill_loss``, ``distill_grad``,
+  ``distill_loss_grad``, here too).
 
 A table or buffer list that is used every step can be marshalled once with
 :func:`prepare_table` / :func:`prepare_buffers` and passed in its place.
@@ -111,6 +115,17 @@ def library():
         lib.apc_upload.restype = ctypes.c_int
         lib.apc_set_reserved_sms.argtypes = [i32]
         lib.apc_set_reserved_sms.restype = ctypes.c_int
+        u32 = ctypes.c_uint32
+        lib.apc_quantize_fp8.argtypes = [vp, i64, i64, i64, u32, vp, vp, vp]
+        lib.apc_quantize_fp8.restype = ctypes.c_int
+        lib.apc_matmul_fp8.argtypes = [vp, vp, i64, i64, i64, vp, i64, u32, vp]
+        lib.apc_matmul_fp8.restype = ctypes.c_int
+        lib.apc_distill_loss.argtypes = [vp, vp, vp, vp]
+        lib.apc_distill_loss.restype = ctypes.c_int
+        lib.apc_distill_grad.argtypes = [vp, vp, vp, vp, i64, vp]
+        lib.apc_distill_grad.restype = ctypes.c_int
+        lib.apc_distill_loss_grad.argtypes = [vp, vp, vp, vp, vp, i64, vp]
+        lib.apc_distill_loss_grad.restype = ctypes.c_int
         _lib = lib
     return _lib
 
@@ -453,3 +468,16 @@ def state_buffers_bf16(p, m, v, global_offset: int = 0) -> list[BufferEntry]:
 
 __all__ += ["digests_to_host", "state_buffers", "device_status", "selftest_wait_timeout", "count_nonzero",
             "COMMIT_ZERO_GRAD", "TensorEntryBF16", "commit_step_bf16", "state_buffers_bf16"]
+
+_OPERATORS = ("quantize_fp8", "matmul_fp8", "distill_loss", "distill_grad", "distill_loss_grad")
+__all__ += list(_OPERATORS)
+
+
+def __getattr__(name: str):
+    """The operators need torch, which the rest of this module imports only
+    where it is used: they are loaded when they are first asked for."""
+    if name in _OPERATORS:
+        from . import operators
+        globals().update((n, getattr(operators, n)) for n in _OPERATORS)
+        return globals()[name]
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))

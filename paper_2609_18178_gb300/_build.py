@@ -32,7 +32,8 @@ LIB = os.path.join(LIB_DIR, "libapc.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 # exact IEEE binary32: no contraction into FMA, IEEE divide and sqrt, denormals kept
 NUMERIC = ["-fmad=false", "-prec-div=true", "-prec-sqrt=true", "-ftz=false"]
-UNITS = ["apc_commit.cu", "apc_digest.cu", "apc_guard.cu", "apc_upload.cu", "apc_host.cpp"]
+UNITS = ["apc_commit.cu", "apc_digest.cu", "apc_guard.cu", "apc_upload.cu", "apc_quantize.cu", "apc_matmul.cu",
+         "apc_distill.cu", "apc_host.cpp", "apc_ops_host.cpp"]
 # The integer-pipe probe is a library of its own: the benchmark's
 # measurement tool for the verification pass's roofline, not the hot path.
 PROBE_LIB = os.path.join(BUILD, "libapc_probe.so")
@@ -41,7 +42,8 @@ PROBE_SRC = os.path.join(CSRC, "apc_probe.cu")
 
 def sources() -> list[str]:
     out = [os.path.join(CSRC, u) for u in UNITS]
-    out += [os.path.join(CSRC, h) for h in ("apc_internal.h", "apc_device.cuh", "apc_tma.cuh", "apc_launch.cuh")]
+    out += [os.path.join(CSRC, h) for h in ("apc_internal.h", "apc_device.cuh", "apc_tma.cuh", "apc_launch.cuh",
+                                             "apc_ops.h", "apc_ops.cuh")]
     out.append(os.path.join(INCLUDE, "apc.h"))
     return out
 

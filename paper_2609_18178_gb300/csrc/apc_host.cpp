@@ -26,6 +26,7 @@
 
 #include "../../include/apc.h"
 #include "apc_internal.h"
+#include "apc_ops.h"
 
 #define APC_EXPORT extern "C" __attribute__((visibility("default")))
 
@@ -811,6 +812,50 @@ APC_EXPORT apc_status apc_selftest_wait_timeout(uint64_t limit_ns, apc_stream_t 
   if (e) return cuda_fail(e, "self-test kernel launch");
   return APC_OK;
 }
+
+// What the operators' host side (apc_ops_host.cpp) shares with this file.
+namespace apc {
+
+void op_begin() { g_last_error[0] = 0; }
+
+apc_status op_fail(apc_status s, const char *fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
+  va_end(ap);
+  return s;
+}
+
+apc_status op_cuda_fail(int err, const char *what) { return cuda_fail(err, what); }
+
+// A call's few ranges: written ones are apart from all others, and each begins
+// in the current device's memory.
+apc_status op_ranges(const OpRange *r, int n) {
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < i; ++j)
+      if ((r[i].written || r[j].written) && r[i].lo < r[j].hi && r[j].lo < r[i].hi)
+        return fail(APC_EINVAL, "%s overlaps %s", r[i].name, r[j].name);
+  int dev = 0;
+  int e = (int)cudaGetDevice(&dev);
+  if (e) return cuda_fail(e, "cudaGetDevice");
+  for (int i = 0; i < n; ++i) {
+    cudaPointerAttributes a;
+    if ((e = (int)cudaPointerGetAttributes(&a, (const void *)r[i].lo))) return cuda_fail(e, "cudaPointerGetAttributes");
+    if (!((a.type == cudaMemoryTypeDevice && a.device == dev) || a.type == cudaMemoryTypeManaged))
+      return fail(APC_EINVAL, "%s is not memory of the current device %d (memory type %d, device %d)", r[i].name, dev,
+                  (int)a.type, a.device);
+  }
+  return APC_OK;
+}
+
+apc_status op_grid(int per_sm, unsigned *cap) {
+  Device d;
+  const apc_status st = device_info(&d);
+  if (st == APC_OK) *cap = grid_for(d.sms, per_sm).cap;
+  return st;
+}
+
+}  // namespace apc
 
 APC_EXPORT const char *apc_status_string(apc_status s) {
   switch (s) {

@@ -1,0 +1,255 @@
+"""The operators around a training step's output head (include/apc.h): 8-bit
+quantization with block scales, the product of such operands, and distillation
+from a teacher's top logits.  Argument marshalling only, as in the package's
+other entry points:
+
+* :func:`quantize_fp8` -> ``apc_quantize_fp8``
+* :func:`matmul_fp8` -> ``apc_matmul_fp8``
+* :func:`distill_loss`, :func:`distill_grad`, :func:`distill_loss_grad` ->
+  ``apc_distill_loss``, ``apc_distill_grad``, ``apc_distill_loss_grad``
+
+An 8-bit matrix is a pair of tensors: the data, ``[rows, cols]`` of
+``torch.float8_e4m3fn`` or ``torch.float8_e5m2`` whose rows start at multiples
+of 16 bytes, and the scales, fp32 ``[ceil(cols/128), rows]`` (one for every 128
+values of a row) or ``[ceil(cols/128), ceil(rows/128)]`` (square blocks).
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+__all__ = ["quantize_fp8", "matmul_fp8", "distill_loss", "distill_grad", "distill_loss_grad"]
+
+BLOCK = 128
+_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_FORMAT = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
+_INDEX = {torch.int32: 0, torch.int64: 1}
+
+
+class _Fp8Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("pitch", ctypes.c_int64),
+                ("scale_pitch", ctypes.c_int64), ("format", ctypes.c_uint32), ("block_rows", ctypes.c_uint32)]
+
+
+class _Distill(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("logits", "ids", "teacher", "teacher_lse", "labels")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "vocab", "k", "pitch", "ids_pitch", "teacher_pitch")] + \
+               [(n, ctypes.c_uint32) for n in ("dtype", "ids_dtype", "teacher_dtype", "labels_dtype")] + \
+               [(n, ctypes.c_double) for n in ("temperature", "kd_weight", "label_weight")]
+
+
+def _here(x, name: str, device: int) -> None:
+    if not x.is_cuda:
+        raise ValueError("%s is not on a CUDA device" % name)
+    if x.get_device() != device:
+        raise ValueError("%s is on cuda:%d but the current device is cuda:%d (use torch.cuda.device(...))"
+                         % (name, x.get_device(), device))
+
+
+def _matrix(x, name: str, kinds, device: int, shape=None) -> int:
+    """The pitch of a two-dimensional tensor on the current device, of one of
+    the types and of the shape given."""
+    _here(x, name, device)
+    if x.dtype not in kinds:
+        raise ValueError("%s has type %s" % (name, x.dtype))
+    if x.dim() != 2:
+        raise ValueError("%s has %d dimensions, expected 2" % (name, x.dim()))
+    r, c = x.shape
+    if shape is not None and (r, c) != shape:
+        raise ValueError("%s is %d x %d, expected %d x %d" % (name, r, c, *shape))
+    pitch, step = x.stride()
+    if step != 1 and c > 1:
+        raise ValueError("%s: neighbours in a row are %d elements apart, expected 1" % (name, step))
+    return pitch if r > 1 else c
+
+
+def _vector(x, name: str, kinds, device: int, n: int) -> int:
+    _here(x, name, device)
+    if x.dtype not in kinds:
+        raise ValueError("%s has type %s" % (name, x.dtype))
+    if x.numel() != n or not x.is_contiguous():
+        raise ValueError("%s: expected %d contiguous elements, got %s" % (name, n, tuple(x.shape)))
+    return x.data_ptr()
+
+
+_F32 = {torch.float32: 0}
+
+
+def _blocks(n: int) -> int:
+    return (n + BLOCK - 1) // BLOCK
+
+
+def _fp8(data, scale, name: str, device: int, block=None) -> _Fp8Matrix:
+    """The C structure of an 8-bit matrix; block: its rows per scale, found from
+    the scale's shape if not given."""
+    pitch = _matrix(data, name, _FORMAT, device)
+    r, c = data.shape
+    scale_pitch = _matrix(scale, name + "_scale", _F32, device)
+    if block is None:
+        block = 1 if scale.shape[1] == r else BLOCK
+    if tuple(scale.shape) != (_blocks(c), -(-r // block)):
+        raise ValueError("%s_scale is %d x %d: expected %d x %d, or %d columns for square blocks"
+                         % (name, *scale.shape, _blocks(c), r, _blocks(r)))
+    return _Fp8Matrix(data.data_ptr(), scale.data_ptr(), pitch, scale_pitch, _FORMAT[data.dtype], block)
+
+
+def _fp8_empty(rows: int, cols: int, block: int, dtype, like):
+    return (torch.empty(rows, (cols + 15) // 16 * 16, dtype=dtype, device=like.device)[:, :cols],
+            torch.empty(_blocks(cols), -(-rows // block), dtype=torch.float32, device=like.device))
+
+
+def _call(f, *args) -> None:
+    status = f(*args)
+    if status:
+        from . import _check
+        _check(status)
+
+
+def _library():
+    from . import library
+    return library()
+
+
+def _stream(stream):
+    from . import _stream as handle
+    return handle(stream)
+
+
+def quantize_fp8(x, block_rows: int = 1, dtype=torch.float8_e4m3fn, transposed: bool = False, out=None, stream=None):
+    """Enqueue the quantization of ``x`` (``[rows, cols]``, fp32, bf16 or fp16,
+    any row pitch) to 8 bits with a power-of-two scale for every 128 values of
+    a row (``block_rows=1``) or every 128 x 128 block (``block_rows=128``).
+
+    Returns ``(data, scale)`` or, with ``transposed``, ``(data, scale, data_t,
+    scale_t)`` with the transpose quantized from the same reading of ``x``,
+    its blocks along its own rows.  ``out`` takes tensors of those shapes."""
+    lib = _library()
+    device = torch.cuda.current_device()
+    pitch = _matrix(x, "x", _DTYPE, device)
+    if dtype not in _FORMAT:
+        raise ValueError("dtype %s is not an 8-bit floating type" % dtype)
+    if block_rows not in (1, BLOCK):
+        raise ValueError("block_rows %r is neither 1 nor %d" % (block_rows, BLOCK))
+    r, c = x.shape
+    if out is None:
+        out = _fp8_empty(r, c, block_rows, dtype, x)
+        if transposed:
+            out += _fp8_empty(c, r, block_rows, dtype, x)
+    elif len(out) != (4 if transposed else 2):
+        raise ValueError("out has %d tensors, expected %d" % (len(out), 4 if transposed else 2))
+    for i, (shape, name) in enumerate((((r, c), "q"), ((c, r), "qt"))[:len(out) // 2]):
+        if tuple(out[2 * i].shape) != shape or out[2 * i].dtype != dtype:
+            raise ValueError("out: %s is %s of %s, expected %s of %s"
+                             % (name, tuple(out[2 * i].shape), out[2 * i].dtype, shape, dtype))
+    q = _fp8(out[0], out[1], "q", device, block_rows)
+    qt = _fp8(out[2], out[3], "qt", device, block_rows) if transposed else None
+    _call(lib.apc_quantize_fp8, x.data_ptr(), r, c, pitch, _DTYPE[x.dtype], ctypes.addressof(q),
+          ctypes.addressof(qt) if transposed else None, _stream(stream))
+    return tuple(out)
+
+
+def matmul_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, stream=None):
+    """Enqueue ``out = a b^T`` for 8-bit ``a`` (``[m, k]``) and ``b`` (``[n,
+    k]``) with their scales.  Returns ``out`` (``[m, n]`` of ``out_dtype``:
+    fp32, bf16 or fp16), or fills the one given, of any row pitch."""
+    lib = _library()
+    device = torch.cuda.current_device()
+    p, q = _fp8(a, a_scale, "a", device), _fp8(b, b_scale, "b", device)
+    m, k = a.shape
+    n = b.shape[0]
+    if b.shape[1] != k:
+        raise ValueError("a has %d columns and b has %d" % (k, b.shape[1]))
+    if out is None:
+        out = torch.empty(m, n, dtype=out_dtype, device=a.device)
+    pitch = _matrix(out, "out", _DTYPE, device, (m, n))
+    _call(lib.apc_matmul_fp8, ctypes.addressof(p), ctypes.addressof(q), m, n, k, out.data_ptr(), pitch,
+          _DTYPE[out.dtype], _stream(stream))
+    return out
+
+
+def _distill(logits, ids, teacher, temperature, kd_weight, teacher_lse, labels, label_weight, device) -> _Distill:
+    pitch = _matrix(logits, "logits", _DTYPE, device)
+    rows, vocab = logits.shape
+    ids_pitch = _matrix(ids, "ids", _INDEX, device)
+    k = ids.shape[1]
+    teacher_pitch = _matrix(teacher, "teacher", _DTYPE, device, (rows, k))
+    if ids.shape[0] != rows:
+        raise ValueError("ids has %d rows and the logits %d" % (ids.shape[0], rows))
+    return _Distill(
+        logits.data_ptr(), ids.data_ptr(), teacher.data_ptr(),
+        None if teacher_lse is None else _vector(teacher_lse, "teacher_lse", _F32, device, rows),
+        None if labels is None else _vector(labels, "labels", _INDEX, device, rows),
+        rows, vocab, k, pitch, ids_pitch, teacher_pitch, _DTYPE[logits.dtype], _INDEX[ids.dtype],
+        _DTYPE[teacher.dtype], 0 if labels is None else _INDEX[labels.dtype], temperature, kd_weight, label_weight)
+
+
+def _lse_room(lse, logits, labels, device):
+    n = 1 if labels is None else 2
+    if lse is None:
+        lse = torch.empty(n, logits.shape[0], dtype=torch.float32, device=logits.device)
+    return lse, _vector(lse, "lse", _F32, device, n * logits.shape[0])
+
+
+def _dlogits_room(out, logits, device):
+    if out is None:
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+    return out, _matrix(out, "out", {logits.dtype: 0}, device, tuple(logits.shape))
+
+
+def distill_loss(logits, ids, teacher, *, temperature=1.0, kd_weight=1.0, teacher_lse=None, labels=None,
+                 label_weight=0.0, loss=None, lse=None, stream=None):
+    """Enqueue each row's distillation loss: ``kd_weight * temperature^2`` times
+    the divergence from the teacher's ``k`` largest logits (``teacher``, fp32,
+    bf16 or fp16, at the vocabulary's places ``ids``, int32 or int64; ``[rows,
+    k]``) to the student's softmax of ``logits`` (``[rows, vocab]``), plus
+    ``label_weight`` times the cross entropy of ``labels`` (``[rows]``).
+
+    The teacher is normalised over the row's entries or, with ``teacher_lse``
+    (fp32 ``[rows]``: logsumexp of all its logits over the temperature), over
+    its whole vocabulary.  Entries whose id lies outside the vocabulary or whose
+    logit is -inf do not count, nor do labels outside it.
+
+    Returns ``(loss, lse)``: fp32 ``[rows]``, and the statistics that
+    :func:`distill_grad` takes, fp32 ``[1 or, with labels, 2, rows]``."""
+    lib = _library()
+    device = torch.cuda.current_device()
+    d = _distill(logits, ids, teacher, temperature, kd_weight, teacher_lse, labels, label_weight, device)
+    if loss is None:
+        loss = torch.empty(d.rows, dtype=torch.float32, device=logits.device)
+    lse, at = _lse_room(lse, logits, labels, device)
+    _call(lib.apc_distill_loss, ctypes.addressof(d), _vector(loss, "loss", _F32, device, d.rows), at, _stream(stream))
+    return loss, lse
+
+
+def distill_grad(logits, ids, teacher, lse, grad_loss, *, temperature=1.0, kd_weight=1.0, teacher_lse=None, labels=None,
+                 label_weight=0.0, out=None, stream=None):
+    """Enqueue the gradient of the logits: ``grad_loss[t]`` (fp32 ``[rows]``)
+    times the gradient of row t's :func:`distill_loss`, whose ``lse`` is given.
+    Rows with a ``grad_loss`` of 0 get zeros.  Returns it in the logits' type,
+    or in ``out``, which may be ``logits`` itself."""
+    lib = _library()
+    device = torch.cuda.current_device()
+    d = _distill(logits, ids, teacher, temperature, kd_weight, teacher_lse, labels, label_weight, device)
+    out, pitch = _dlogits_room(out, logits, device)
+    lse, at = _lse_room(lse, logits, labels, device)
+    _call(lib.apc_distill_grad, ctypes.addressof(d), at, _vector(grad_loss, "grad_loss", _F32, device, d.rows),
+          out.data_ptr(), pitch, _stream(stream))
+    return out
+
+
+def distill_loss_grad(logits, ids, teacher, grad_loss, *, temperature=1.0, kd_weight=1.0, teacher_lse=None, labels=None,
+                      label_weight=0.0, loss=None, lse=None, out=None, stream=None):
+    """Enqueue :func:`distill_loss` and :func:`distill_grad` in one pass over
+    the logits, for a ``grad_loss`` known before the loss (a mean's weights, a
+    loss scale).  Returns ``(loss, lse, dlogits)``."""
+    lib = _library()
+    device = torch.cuda.current_device()
+    d = _distill(logits, ids, teacher, temperature, kd_weight, teacher_lse, labels, label_weight, device)
+    if loss is None:
+        loss = torch.empty(d.rows, dtype=torch.float32, device=logits.device)
+    lse, at = _lse_room(lse, logits, labels, device)
+    out, pitch = _dlogits_room(out, logits, device)
+    _call(lib.apc_distill_loss_grad, ctypes.addressof(d), _vector(grad_loss, "grad_loss", _F32, device, d.rows),
+          _vector(loss, "loss", _F32, device, d.rows), at, out.data_ptr(), pitch, _stream(stream))
+    return loss, lse, out

@@ -1,0 +1,134 @@
+"""The operators' C ABI without a GPU: bad arguments are refused before
+anything asks for a device."""
+import ctypes
+
+import pytest
+
+import paper_2609_18178_gb300 as apc
+from paper_2609_18178_gb300.operators import _Distill, _Fp8Matrix
+
+EINVAL, EALIGN, ERANGE = 1, 2, 3
+AT = 1 << 40  # an address that nothing dereferences
+
+
+def fp8(data=AT, scale=AT + (1 << 30), pitch=256, scale_pitch=64, fmt=0, block=1):
+    return _Fp8Matrix(data, scale, pitch, scale_pitch, fmt, block)
+
+
+def ref(x):
+    return None if x is None else ctypes.addressof(x)
+
+
+def quantize(x=AT + (1 << 32), rows=64, cols=256, pitch=256, dtype=1, q=None, qt=None):
+    q = q or fp8()
+    return apc.library().apc_quantize_fp8(x, rows, cols, pitch, dtype, ref(q), ref(qt), None)
+
+
+def matmul(a=None, b=None, m=64, n=64, k=256, out=AT + (1 << 32), pitch=64, dtype=1):
+    a, b = a or fp8(), b or fp8(AT + (1 << 33), AT + (1 << 34))
+    return apc.library().apc_matmul_fp8(ref(a), ref(b), m, n, k, out, pitch, dtype, None)
+
+
+def distill(what="loss_grad", loss=AT + (5 << 32), lse=AT + (6 << 32), g=AT + (7 << 32), d=AT + (8 << 32), dpitch=1000, **kw):
+    f = dict(logits=AT, ids=AT + (1 << 32), teacher=AT + (2 << 32), teacher_lse=None, labels=None, rows=16, vocab=1000, k=8,
+             pitch=1000, ids_pitch=8, teacher_pitch=8, dtype=1, ids_dtype=1, teacher_dtype=0, labels_dtype=0,
+             temperature=1.0, kd_weight=1.0, label_weight=0.0)
+    f.update(kw)
+    s = _Distill(**f)
+    lib = apc.library()
+    if what == "loss":
+        return lib.apc_distill_loss(ref(s), loss, lse, None)
+    if what == "grad":
+        return lib.apc_distill_grad(ref(s), lse, g, d, dpitch, None)
+    return lib.apc_distill_loss_grad(ref(s), g, loss, lse, d, dpitch, None)
+
+
+@pytest.mark.parametrize("want,kw", [
+    (EINVAL, dict(x=None)),
+    (EINVAL, dict(rows=-1)),
+    (ERANGE, dict(cols=1 << 31)),
+    (EINVAL, dict(dtype=3)),
+    (EINVAL, dict(pitch=255)),
+    (EALIGN, dict(x=AT + 1)),
+    (ERANGE, dict(rows=1 << 30, pitch=1 << 40)),
+    (EINVAL, dict(q=fp8(data=None))),
+    (EINVAL, dict(q=fp8(scale=None))),
+    (EALIGN, dict(q=fp8(data=AT + 8))),
+    (EALIGN, dict(q=fp8(pitch=260))),
+    (EALIGN, dict(q=fp8(scale=AT + 2))),
+    (EINVAL, dict(q=fp8(scale_pitch=63))),
+    (EINVAL, dict(q=fp8(fmt=2))),
+    (EINVAL, dict(q=fp8(block=64))),
+    (EINVAL, dict(q=fp8(), qt=fp8(AT + (1 << 33), AT + (1 << 34), block=128))),
+    (EINVAL, dict(q=fp8(), qt=fp8(AT + 4096, AT + (1 << 34)))),       # the two outputs overlap
+    (EINVAL, dict(x=AT)),                                               # an output over the input
+])
+def test_quantize_refuses(want, kw):
+    assert quantize(**kw) == want
+    assert apc.library().apc_last_error()
+
+
+@pytest.mark.parametrize("want,kw", [
+    (EINVAL, dict(out=None)),
+    (EINVAL, dict(m=-1)),
+    (ERANGE, dict(n=1 << 31)),
+    (EINVAL, dict(dtype=7)),
+    (EINVAL, dict(pitch=63)),
+    (EALIGN, dict(out=AT + (1 << 32) + 1)),
+    (EALIGN, dict(dtype=0, out=AT + (1 << 32) + 2)),
+    (EINVAL, dict(a=fp8(data=None))),
+    (EALIGN, dict(b=fp8(AT + (1 << 33) + 4, AT + (1 << 34)))),
+    (EALIGN, dict(b=fp8(AT + (1 << 33), AT + (1 << 34), pitch=264))),
+    (EINVAL, dict(a=fp8(scale_pitch=10))),
+    (EINVAL, dict(out=AT)),
+])
+def test_matmul_refuses(want, kw):
+    assert matmul(**kw) == want
+
+
+@pytest.mark.parametrize("want,kw", [
+    (EINVAL, dict(logits=None)),
+    (EINVAL, dict(ids=None)),
+    (EINVAL, dict(loss=None)),
+    (EINVAL, dict(lse=None)),
+    (EINVAL, dict(g=None)),
+    (EINVAL, dict(d=None)),
+    (EINVAL, dict(vocab=0)),
+    (EINVAL, dict(k=1025, ids_pitch=2000, teacher_pitch=2000)),
+    (EINVAL, dict(k=-1)),
+    (EINVAL, dict(dtype=3)),
+    (EINVAL, dict(ids_dtype=2)),
+    (EINVAL, dict(teacher_dtype=3)),
+    (EINVAL, dict(labels=AT + (9 << 32), labels_dtype=2)),
+    (EINVAL, dict(temperature=0.0)),
+    (EINVAL, dict(temperature=-1.0)),
+    (EINVAL, dict(temperature=float("nan"))),
+    (EINVAL, dict(temperature=1e-39)),
+    (EINVAL, dict(kd_weight=-1.0)),
+    (EINVAL, dict(label_weight=float("inf"))),
+    (EINVAL, dict(pitch=999)),
+    (EINVAL, dict(dpitch=999)),
+    (EALIGN, dict(ids=AT + (1 << 32) + 4)),
+    (EALIGN, dict(lse=AT + (6 << 32) + 2)),
+    (EINVAL, dict(d=AT + 64)),                    # the gradient over the logits, but not in their place
+    (EINVAL, dict(d=AT, dpitch=1008)),
+    (EINVAL, dict(loss=AT + (6 << 32) + 32)),     # over the statistics
+    (EINVAL, dict(what="loss", loss=None)),
+    (EINVAL, dict(what="grad", d=None)),
+    (EINVAL, dict(what="grad", lse=None)),
+])
+def test_distill_refuses(want, kw):
+    assert distill(**kw) == want
+
+
+def test_empty_calls_need_no_device():
+    none = fp8(data=None, scale=None)
+    assert quantize(x=None, rows=0, q=none) == 0
+    assert quantize(x=None, cols=0, q=none, qt=none) == 0
+    assert matmul(a=none, m=0, out=None) == 0
+    assert distill(logits=None, ids=None, teacher=None, loss=None, lse=None, g=None, d=None, rows=0) == 0
+
+
+def test_struct_layout():
+    assert ctypes.sizeof(_Fp8Matrix) == 40
+    assert ctypes.sizeof(_Distill) == 5 * 8 + 6 * 8 + 4 * 4 + 3 * 8
