@@ -748,6 +748,22 @@ int launch_wait_timeout(uint64_t limit_ns, void *stream) {
   return (int)cudaGetLastError();
 }
 
+// For kernels of other translation units that share the word: its address, asked
+// for once per device.
+int commit_status_word(unsigned **out) {
+  constexpr int kDevices = 64;
+  static std::atomic<unsigned *> words[kDevices];
+  int dev = 0;
+  int e = (int)cudaGetDevice(&dev);
+  if (e) return e;
+  if (dev >= 0 && dev < kDevices && (*out = words[dev].load(std::memory_order_acquire))) return 0;
+  void *p = nullptr;
+  if ((e = (int)cudaGetSymbolAddress(&p, g_commit_status))) return e;
+  *out = static_cast<unsigned *>(p);
+  if (dev >= 0 && dev < kDevices) words[dev].store(*out, std::memory_order_release);
+  return 0;
+}
+
 int read_commit_status(unsigned *out) {
   cudaError_t e = cudaMemcpyFromSymbol(out, g_commit_status, sizeof(unsigned));
   if (e != cudaSuccess) return (int)e;

@@ -848,10 +848,12 @@ apc_status op_ranges(const OpRange *r, int n) {
   return APC_OK;
 }
 
-apc_status op_grid(int per_sm, unsigned *cap) {
+apc_status op_grid(int per_sm, unsigned *cap, unsigned *sms) {
   Device d;
   const apc_status st = device_info(&d);
-  if (st == APC_OK) *cap = grid_for(d.sms, per_sm).cap;
+  if (st != APC_OK) return st;
+  *cap = grid_for(d.sms, per_sm).cap;
+  if (sms) *sms = (unsigned)d.sms;
   return st;
 }
 

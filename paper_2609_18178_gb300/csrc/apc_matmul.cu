@@ -1,71 +1,564 @@
-// The product of two block-scaled 8-bit matrices (apc_matmul_fp8).
+// The product of two block-scaled 8-bit matrices (apc_matmul_fp8) on the
+// 5th-generation tensor cores.
 //
-// One CTA computes a 64 x 64 tile of out: operands are widened into shared
-// memory, a block of 128 k at a time, its products summed in fp32, and the
-// sums added with both scales.
-#include <cuda_fp8.h>
+//   out[i, j] = sum over blocks c of 128 k:
+//                 sa[c, i] sb[c, j] * (sum over k in c of a[i, k] b[j, k])
+//
+// The inner sum is four tcgen05.mma (K = 32 each) into tensor memory, in fp32.
+// Its accumulator is then read back, multiplied by the scales and added into
+// fp32 registers while the tensor core fills the other of two accumulators:
+// the scales are arbitrary fp32 numbers, and no sum of more than 128 products
+// is left to the tensor core's own rounding.
+//
+// Two kernels, warp-specialized alike: one warp issues TMA loads into a ring of
+// shared-memory stages (128 bytes of k a row, 128-byte swizzle, zeros beyond
+// the edges), one thread issues the products, the others add up.
+#include <cuda.h>
+#include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 
 #include "apc_ops.cuh"
+#include "apc_tcgen05.cuh"
 
 namespace apc {
 
 namespace {
 
-constexpr int kTile = 64, kStep = 32;
+// What both kernels take.  "r" is the operand on the accumulator's lanes, "c"
+// the one on its columns.
+struct ProductPlan {
+  const float *r_scale, *c_scale;
+  int64_t r_scale_pitch, c_scale_pitch;
+  uint32_t r_shift, c_shift;
+  uint32_t rows, cols;      // of the product's lanes and columns
+  uint32_t row_tiles, col_tiles;
+  uint32_t blocks;          // of 128 k
+  uint32_t instruction;
+  void *out;
+  int64_t row_step, col_step;  // elements of out
+  unsigned *status;
+};
 
-__device__ __forceinline__ float widen(uint8_t v, bool e5m2) {
-  const __half_raw h = __nv_cvt_fp8_to_halfraw(v, e5m2 ? __NV_E5M2 : __NV_E4M3);
-  return __half2float(__half(h));
+__device__ __forceinline__ void give_up(unsigned *status) { atomicOr(status, (unsigned)APC_ETIMEOUT); }
+
+// ---------------------------------------------------------------------------
+// The kernel for few columns: 128 rows of the wide operand (a weight's outputs)
+// on the lanes, BN columns (tokens) beside them.
+//
+// The k blocks of a tile are split evenly over a cluster's CTAs, so that few
+// tiles still keep all SMs loading: each CTA sums its share in registers, then
+// sends every CTA the columns that it owns (st.async into its shared memory,
+// counted by an mbarrier), and the owner adds the shares in the order of their
+// ranks and stores.  The loads of the next tile run meanwhile.
+constexpr int kMidThreads = 192;
+
+template <int BN>
+struct MidShape {
+  static constexpr int kRowBytes = 128 * kBlock, kColBytes = BN * kBlock;
+  static constexpr int kStageBytes = kRowBytes + kColBytes;
+  static constexpr int kRecvBytes = BN * 128 * 4;
+  static constexpr int kStages = (200 * 1024 - kRecvBytes) / kStageBytes > 12 ? 12 : (200 * 1024 - kRecvBytes) / kStageBytes;
+  static constexpr int kScaleBytes = 4 * 2 * BN * 4;
+  static constexpr int kBytes = 1024 + kStages * kStageBytes + kRecvBytes + kScaleBytes;
+  static constexpr int kTmem = 2 * BN < 32 ? 32 : 2 * BN;
+};
+
+template <int BN, typename T>
+__global__ void __launch_bounds__(kMidThreads, 1)
+    mid_kernel(const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c,
+               const __grid_constant__ ProductPlan p, const uint32_t split_log2) {
+  using S = MidShape<BN>;
+  constexpr int kLog2Bn = BN == 16 ? 4 : BN == 32 ? 5 : BN == 64 ? 6 : 7;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full[S::kStages], empty[S::kStages], acc_full[2], acc_empty[2], recv_full, recv_free;
+  __shared__ uint32_t tmem_at;
+  uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  float *recv = reinterpret_cast<float *>(smem + S::kStages * S::kStageBytes);
+  float *scales = recv + S::kRecvBytes / 4;
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t split = 1u << split_log2;
+  const uint32_t rank = split > 1 ? cluster_rank() : 0;
+  const uint32_t first = blockIdx.x / split, step = gridDim.x / split;
+  const uint32_t tiles = p.row_tiles * p.col_tiles;
+  const uint32_t b0 = (uint32_t)((uint64_t)p.blocks * rank / split), b1 = (uint32_t)((uint64_t)p.blocks * (rank + 1) / split);
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S::kStages; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
+    for (int i = 0; i < 2; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 4);
+    mbar_init(&recv_full, 1);
+    mbar_init(&recv_free, 4 * split);
+    mbar_init_fence();
+  }
+  if (warp == 1) tmem_alloc<1>(&tmem_at, S::kTmem);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (split > 1) cluster_arrive(), cluster_wait();  // the barriers are there before anyone sends
+  const uint32_t tmem = tmem_at;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      prefetch_map(&map_r);
+      prefetch_map(&map_c);
+      uint32_t use = 0;
+      bool ok = true;
+      for (uint32_t t = first; t < tiles && ok; t += step) {
+        const int32_t r0 = (int32_t)(t % p.row_tiles) * 128, c0 = (int32_t)(t / p.row_tiles) * BN;
+        for (uint32_t b = b0; b < b1; ++b, ++use) {
+          const uint32_t st = use % S::kStages;
+          if (use >= S::kStages && !mbar_wait(&empty[st], (use / S::kStages + 1) & 1)) {
+            ok = false;
+            break;
+          }
+          const uint32_t at = smem_addr(smem + st * S::kStageBytes), bar = smem_addr(&full[st]);
+          mbar_arrive_expect_tx(&full[st], S::kStageBytes);
+          load_box(at, &map_r, (int32_t)(b * kBlock), r0, bar);
+          load_box(at + S::kRowBytes, &map_c, (int32_t)(b * kBlock), c0, bar);
+        }
+      }
+      if (!ok) {  // let the copies in flight land
+        give_up(p.status);
+        for (uint32_t u = use > S::kStages ? use - S::kStages : 0; u < use; ++u) mbar_wait(&full[u % S::kStages], u / S::kStages & 1);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      uint32_t use = 0;
+      bool ok = true;
+      for (uint32_t t = first; t < tiles && ok; t += step)
+        for (uint32_t b = b0; b < b1; ++b, ++use) {
+          const uint32_t st = use % S::kStages, buf = use & 1;
+          if ((use >= 2 && !mbar_wait(&acc_empty[buf], (use / 2 + 1) & 1)) || !mbar_wait(&full[st], use / S::kStages & 1)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint64_t dr = operand_desc(smem_addr(smem + st * S::kStageBytes));
+          const uint64_t dc = operand_desc(smem_addr(smem + st * S::kStageBytes + S::kRowBytes));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) mma_fp8<1>(tmem + buf * BN, dr + 2 * k, dc + 2 * k, p.instruction, k > 0);
+          mma_commit(&empty[st]);
+          mma_commit(&acc_full[buf]);
+        }
+      if (!ok) {  // let the products in flight end
+        give_up(p.status);
+        for (uint32_t u = use > 2 ? use - 2 : 0; u < use; ++u) mbar_wait(&acc_full[u & 1], u / 2 & 1);
+      }
+    }
+  } else {
+    const uint32_t quad = warp & 3, row = quad * 32 + lane;
+    float *sc = scales + (warp - 2) * 2 * BN;
+    uint32_t use = 0, done = 0;
+    bool ok = true;
+    if (split > 1 && threadIdx.x == 64) mbar_arrive_expect_tx(&recv_full, S::kRecvBytes);
+    for (uint32_t t = first; t < tiles && ok; t += step, ++done) {
+      const uint32_t r0 = t % p.row_tiles * 128, c0 = t / p.row_tiles * BN;
+      const uint32_t r = r0 + row < p.rows ? r0 + row : p.rows - 1;
+      constexpr int kPer = (BN + 31) / 32;
+      float next_c[kPer], next_r;
+      auto fetch = [&](uint32_t b) {
+        next_r = __ldg(p.r_scale + b * p.r_scale_pitch + (r >> p.r_shift));
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          const uint32_t c = c0 + i * 32 + lane;
+          next_c[i] = (BN >= 32 || lane < BN) && c < p.cols ? __ldg(p.c_scale + b * p.c_scale_pitch + (c >> p.c_shift)) : 0.0f;
+        }
+      };
+      uint64_t acc[BN / 2];
+#pragma unroll
+      for (int i = 0; i < BN / 2; ++i) acc[i] = 0;
+      fetch(b0);
+      for (uint32_t b = b0; b < b1; ++b, ++use) {
+        const uint32_t buf = use & 1;
+        float *s = sc + buf * BN;
+        const uint64_t sr = pack2(next_r, next_r);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (BN >= 32 || lane < BN) s[i * 32 + lane] = next_c[i];
+        __syncwarp();
+        if (b + 1 < b1) fetch(b + 1);
+        ok = __all_sync(~0u, mbar_wait(&acc_full[buf], use / 2 & 1));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t at = tmem + buf * BN + (quad << 21);  // lane 32 * quad in bits 16 up
+        constexpr int kChunk = BN < 32 ? 16 : 32;
+#pragma unroll
+        for (int c = 0; c < BN; c += kChunk) {
+          uint32_t d[kChunk];
+          if constexpr (kChunk == 32) tmem_load32(d, at + c);
+          else tmem_load16(d, at + c);
+          tmem_landed(d);
+          if (c + kChunk == BN) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&acc_empty[buf]);
+          }
+#pragma unroll
+          for (int i = 0; i < kChunk; i += 4) {
+            const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(s + c + i);
+            acc[(c + i) / 2] = fma2(pack2(d[i], d[i + 1]), mul2(sr, v.x), acc[(c + i) / 2]);
+            acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), mul2(sr, v.y), acc[(c + i) / 2 + 1]);
+          }
+        }
+      }
+      if (!ok) break;
+      T *out = static_cast<T *>(p.out) + (int64_t)(r0 + row) * p.row_step;
+      const bool in = r0 + row < p.rows;
+      if (split == 1) {
+#pragma unroll
+        for (int i = 0; i < BN / 2; ++i) {
+          const float2 v = unpack2(acc[i]);
+          if (in && c0 + 2 * i < p.cols) out[(int64_t)(c0 + 2 * i) * p.col_step] = from_float<T>(v.x);
+          if (in && c0 + 2 * i + 1 < p.cols) out[(int64_t)(c0 + 2 * i + 1) * p.col_step] = from_float<T>(v.y);
+        }
+        continue;
+      }
+      // a share to each CTA of the cluster, once it has read the tile before
+      if (done) ok = __all_sync(~0u, mbar_wait_cluster(&recv_free, (done + 1) & 1));
+      if (!ok) break;
+      const uint32_t per_log2 = kLog2Bn - split_log2, per = 1u << per_log2;  // columns that a CTA owns
+      const uint32_t mine = smem_addr(recv) + (rank * per * 128 + row) * 4, bar = smem_addr(&recv_full);
+#pragma unroll
+      for (int i = 0; i < BN; ++i) {
+        const float2 v = unpack2(acc[i / 2]);
+        const uint32_t owner = (uint32_t)i >> per_log2;
+        store_async(map_rank(mine + (i & (per - 1)) * 512, owner), i % 2 ? v.y : v.x, map_rank(bar, owner));
+      }
+      ok = __all_sync(~0u, mbar_wait_cluster(&recv_full, done & 1));
+      if (!ok) break;
+      if (threadIdx.x == 64) mbar_arrive_expect_tx(&recv_full, S::kRecvBytes);
+      for (uint32_t c = 0; c < per; ++c) {
+        float sum = recv[c * 128 + row];
+        for (uint32_t k = 1; k < split; ++k) sum += recv[(k * per + c) * 128 + row];
+        const uint32_t col = c0 + rank * per + c;
+        if (in && col < p.cols) out[(int64_t)col * p.col_step] = from_float<T>(sum);
+      }
+      __syncwarp();
+      if (lane < split) arrive_remote(map_rank(smem_addr(&recv_free), lane));
+    }
+    if (!ok) {
+      give_up(p.status);
+      if (split > 1) mbar_wait_cluster(&recv_full, done & 1);  // let the shares in flight land
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (split > 1) cluster_arrive(), cluster_wait();  // nobody sends to a CTA that has left
+  tc_fence_after();
+  if (warp == 1) tmem_free<1>(tmem, S::kTmem);
+}
+
+// ---------------------------------------------------------------------------
+// The kernel for large products: a pair of CTAs computes 256 x 256 of out, each
+// CTA 128 rows of a on its lanes and all 256 rows of b on its columns, of which
+// it holds half in shared memory (tcgen05.mma.cta_group::2 reads both halves).
+// The first CTA's thread issues for both.  Persistent: the pair's next tile is
+// loaded and multiplied while the epilogue stores.
+constexpr int kBigThreads = 320, kBigStages = 6;
+constexpr int kBigHalf = 128 * kBlock, kBigStageBytes = 2 * kBigHalf;
+constexpr int kBigScaleBytes = 8 * 2 * 128 * 4;
+constexpr int kBigBytes = 1024 + kBigStages * kBigStageBytes + kBigScaleBytes;
+constexpr uint32_t kBigGroup = 16;  // row tiles that are walked together
+
+// Tile t of the walk: groups of row tiles, in each the row tile first, so that
+// the tiles in flight share few rows of both operands in L2.
+__device__ __forceinline__ void big_tile(const ProductPlan &p, uint32_t t, uint32_t *r, uint32_t *c) {
+  const uint32_t group = t / (kBigGroup * p.col_tiles), first = group * kBigGroup;
+  const uint32_t height = min(kBigGroup, p.row_tiles - first), i = t - first * p.col_tiles;
+  *r = first + i % height;
+  *c = i / height;
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) matmul_kernel(const __grid_constant__ MatmulArgs p) {
-  __shared__ float sa[kStep][kTile + 1], sb[kStep][kTile + 1];
-  const uint32_t tm = (p.m + kTile - 1) / kTile, tn = (p.n + kTile - 1) / kTile;
-  const uint32_t tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (uint64_t tile = blockIdx.x; tile < (uint64_t)tm * tn; tile += gridDim.x) {
-    const uint32_t m0 = (uint32_t)(tile / tn) * kTile, n0 = (uint32_t)(tile % tn) * kTile;
-    float acc[4][4] = {};
-    for (uint32_t kb = 0; kb * kBlock < p.k; ++kb) {
-      float part[4][4] = {};
-      for (uint32_t k0 = kb * kBlock; k0 < min(p.k, (kb + 1) * kBlock); k0 += kStep) {
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < kTile * kStep; i += 256) {
-          const uint32_t r = i / kStep, c = i % kStep;
-          const bool in = k0 + c < p.k;
-          sa[c][r] = in && m0 + r < p.m ? widen(p.a[(m0 + r) * p.a_pitch + k0 + c], p.a_e5m2) : 0.0f;
-          sb[c][r] = in && n0 + r < p.n ? widen(p.b[(n0 + r) * p.b_pitch + k0 + c], p.b_e5m2) : 0.0f;
-        }
-        __syncthreads();
-        for (int c = 0; c < kStep; ++c)
-          for (int i = 0; i < 4; ++i)
-            for (int j = 0; j < 4; ++j) part[i][j] = __fmaf_rn(sa[c][ty * 4 + i], sb[c][tx + 16 * j], part[i][j]);
+__device__ __forceinline__ void store_row(T *out, const uint64_t (&acc)[64], uint32_t count) {
+  constexpr int kPer = 16 / sizeof(T);
+  if (count == 128 && (uintptr_t)out % 16 == 0) {
+#pragma unroll
+    for (int i = 0; i < 128; i += kPer) {
+      union {
+        T v[kPer];
+        uint4 q;
+      } u;
+#pragma unroll
+      for (int j = 0; j < kPer; j += 2) {
+        const float2 v = unpack2(acc[(i + j) / 2]);
+        u.v[j] = from_float<T>(v.x);
+        u.v[j + 1] = from_float<T>(v.y);
       }
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t m = m0 + ty * 4 + i, n = n0 + tx + 16 * j;
-          if (m < p.m && n < p.n)
-            acc[i][j] = __fmaf_rn(part[i][j], p.a_scale[kb * p.a_scale_pitch + (m >> p.a_shift)] *
-                                                  p.b_scale[kb * p.b_scale_pitch + (n >> p.b_shift)], acc[i][j]);
-        }
+      *reinterpret_cast<uint4 *>(out + i) = u.q;
     }
-    for (int i = 0; i < 4; ++i)
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t m = m0 + ty * 4 + i, n = n0 + tx + 16 * j;
-        if (m < p.m && n < p.n) static_cast<T *>(p.out)[m * p.out_pitch + n] = from_float<T>(acc[i][j]);
-      }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 64; ++i) {
+      const float2 v = unpack2(acc[i]);
+      if (2 * i < count) out[2 * i] = from_float<T>(v.x);
+      if (2 * i + 1 < count) out[2 * i + 1] = from_float<T>(v.y);
+    }
   }
+}
+
+// ROWS: the scales of b change from column to column.
+template <typename T, bool ROWS>
+__global__ void __launch_bounds__(kBigThreads, 1)
+    big_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+               const __grid_constant__ ProductPlan p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full[kBigStages], empty[kBigStages], acc_full[2], acc_empty[2];
+  __shared__ uint32_t tmem_at;
+  uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  float *scales = reinterpret_cast<float *>(smem + kBigStages * kBigStageBytes);
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, rank = cluster_rank();
+  const uint32_t first = blockIdx.x / 2, step = gridDim.x / 2, tiles = p.row_tiles * p.col_tiles;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kBigStages; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
+    for (int i = 0; i < 2; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 16);
+    mbar_init_fence();
+  }
+  if (warp == 1) tmem_alloc<2>(&tmem_at, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  cluster_arrive(), cluster_wait();
+  const uint32_t tmem = tmem_at;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      prefetch_map(&map_a);
+      prefetch_map(&map_b);
+      uint32_t use = 0;
+      bool ok = true;
+      for (uint32_t t = first; t < tiles && ok; t += step) {
+        uint32_t tr, tc;
+        big_tile(p, t, &tr, &tc);
+        const int32_t r0 = (int32_t)(tr * 256 + rank * 128), c0 = (int32_t)(tc * 256 + rank * 128);
+        for (uint32_t b = 0; b < p.blocks; ++b, ++use) {
+          const uint32_t st = use % kBigStages;
+          if (use >= kBigStages && !mbar_wait_cluster(&empty[st], (use / kBigStages + 1) & 1)) {
+            ok = false;
+            break;
+          }
+          const uint32_t at = smem_addr(smem + st * kBigStageBytes), bar = map_rank(smem_addr(&full[st]), 0);
+          if (rank == 0) mbar_arrive_expect_tx(&full[st], 2 * kBigStageBytes);
+          load_box_pair(at, &map_a, (int32_t)(b * kBlock), r0, bar);
+          load_box_pair(at + kBigHalf, &map_b, (int32_t)(b * kBlock), c0, bar);
+        }
+      }
+      if (!ok) {  // let the copies in flight land, the other CTA's too
+        give_up(p.status);
+        if (rank == 0)
+          for (uint32_t u = use > kBigStages ? use - kBigStages : 0; u < use; ++u) mbar_wait_cluster(&full[u % kBigStages], u / kBigStages & 1);
+        const uint64_t t0 = global_ns();
+        for (uint32_t i = 0; i < kWaitIterations && global_ns() - t0 < 1000000; ++i) __nanosleep(1000);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      uint32_t use = 0;
+      bool ok = true;
+      for (uint32_t t = first; t < tiles && ok; t += step)
+        for (uint32_t b = 0; b < p.blocks; ++b, ++use) {
+          const uint32_t st = use % kBigStages, buf = use & 1;
+          if ((use >= 2 && !mbar_wait_cluster(&acc_empty[buf], (use / 2 + 1) & 1)) ||
+              !mbar_wait_cluster(&full[st], use / kBigStages & 1)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint64_t da = operand_desc(smem_addr(smem + st * kBigStageBytes));
+          const uint64_t db = operand_desc(smem_addr(smem + st * kBigStageBytes + kBigHalf));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) mma_fp8<2>(tmem + buf * 256, da + 2 * k, db + 2 * k, p.instruction, k > 0);
+          mma_commit_pair(&empty[st]);
+          mma_commit_pair(&acc_full[buf]);
+        }
+      if (!ok) {  // let the products in flight end
+        give_up(p.status);
+        for (uint32_t u = use > 2 ? use - 2 : 0; u < use; ++u) mbar_wait_cluster(&acc_full[u & 1], u / 2 & 1);
+      }
+    }
+  } else {
+    const uint32_t quad = warp & 3, half = (warp - 2) / 4, row = quad * 32 + lane;
+    float *sc = scales + (warp - 2) * 2 * 128;
+    uint32_t use = 0;
+    bool ok = true;
+    for (uint32_t t = first; t < tiles && ok; t += step) {
+      uint32_t tr, tc;
+      big_tile(p, t, &tr, &tc);
+      const uint32_t r0 = tr * 256 + rank * 128, c0 = tc * 256 + half * 128;
+      const uint32_t r = min(r0 + row, p.rows - 1);
+      const float *rs = p.r_scale + (r >> p.r_shift);
+      float next_r, next_c[ROWS ? 4 : 1];
+      auto fetch = [&](uint32_t b) {
+        next_r = __ldg(rs + b * p.r_scale_pitch);
+        if (ROWS) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            next_c[i] = __ldg(p.c_scale + b * p.c_scale_pitch + min(c0 + i * 32 + lane, p.cols - 1));
+        } else {
+          next_c[0] = __ldg(p.c_scale + b * p.c_scale_pitch + (min(c0, p.cols - 1) >> 7));
+        }
+      };
+      uint64_t acc[64];
+#pragma unroll
+      for (int i = 0; i < 64; ++i) acc[i] = 0;
+      fetch(0);
+      for (uint32_t b = 0; b < p.blocks; ++b, ++use) {
+        const uint32_t buf = use & 1;
+        float *s = sc + buf * 128;
+        const float one = ROWS ? next_r : next_r * next_c[0];
+        const uint64_t sr = pack2(one, one);
+        if (ROWS) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[i * 32 + lane] = next_c[i];
+          __syncwarp();
+        }
+        if (b + 1 < p.blocks) fetch(b + 1);
+        ok = __all_sync(~0u, mbar_wait_cluster(&acc_full[buf], use / 2 & 1));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t at = tmem + buf * 256 + half * 128 + (quad << 21);
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) {
+          uint32_t d[32];
+          tmem_load32(d, at + c);
+          tmem_landed(d);
+          if (c == 96) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_remote(map_rank(smem_addr(&acc_empty[buf]), 0));
+          }
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            if (ROWS) {
+              const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(s + c + i);
+              acc[(c + i) / 2] = fma2(pack2(d[i], d[i + 1]), mul2(sr, v.x), acc[(c + i) / 2]);
+              acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), mul2(sr, v.y), acc[(c + i) / 2 + 1]);
+            } else {
+              acc[(c + i) / 2] = fma2(pack2(d[i], d[i + 1]), sr, acc[(c + i) / 2]);
+              acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), sr, acc[(c + i) / 2 + 1]);
+            }
+          }
+        }
+      }
+      if (!ok) break;
+      if (r0 + row < p.rows && c0 < p.cols)
+        store_row(static_cast<T *>(p.out) + (int64_t)(r0 + row) * p.row_step + c0, acc, min(128u, p.cols - c0));
+    }
+    if (!ok) give_up(p.status);
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive(), cluster_wait();
+  tc_fence_after();
+  if (warp == 1) tmem_free<2>(tmem, 512);
+}
+
+// ---------------------------------------------------------------------------
+
+int encode(CUtensorMap *map, const uint8_t *data, uint32_t rows, uint32_t cols, int64_t pitch, uint32_t box_rows) {
+  static const PFN_cuTensorMapEncodeTiled_v12000 tiled = [] {
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult st = cudaDriverEntryPointSymbolNotFound;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &st) != cudaSuccess) cudaGetLastError();
+    return st == cudaDriverEntryPointSuccess ? (PFN_cuTensorMapEncodeTiled_v12000)fn : nullptr;
+  }();
+  if (!tiled) return (int)cudaErrorNotSupported;
+  const cuuint64_t dims[2] = {cols, rows};
+  const cuuint64_t strides[1] = {rows > 1 ? (cuuint64_t)pitch : ((cuuint64_t)cols + 15) / 16 * 16};
+  const cuuint32_t box[2] = {kBlock, box_rows}, steps[2] = {1, 1};
+  const CUresult r = tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(data), dims, strides, box, steps,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? 0 : (int)cudaErrorInvalidValue;
+}
+
+template <typename K, typename... A>
+int launch_cluster(K kernel, unsigned grid, unsigned threads, unsigned smem, unsigned cluster, void *stream, A... args) {
+  int e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e) return e;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim = {cluster, 1, 1};
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = (cudaStream_t)stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = cluster > 1 ? 1 : 0;
+  return (int)cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
+
+template <int BN, typename T>
+int launch_mid(const MatmulArgs &a, ProductPlan p, unsigned cap, unsigned sms, void *stream) {
+  p.r_scale = a.b_scale, p.c_scale = a.a_scale;
+  p.r_scale_pitch = a.b_scale_pitch, p.c_scale_pitch = a.a_scale_pitch;
+  p.r_shift = a.b_shift, p.c_shift = a.a_shift;
+  p.rows = a.n, p.cols = a.m;
+  p.row_tiles = ceil_div(a.n, 128), p.col_tiles = ceil_div(a.m, BN);
+  p.instruction = 1u << 4 | a.b_e5m2 << 7 | a.a_e5m2 << 10 | (uint32_t)(BN >> 3) << 17 | 8u << 24;
+  p.row_step = 1, p.col_step = a.out_pitch;
+  CUtensorMap r, c;
+  int e = encode(&r, a.b, a.n, a.k, a.b_pitch, 128);
+  if (!e) e = encode(&c, a.a, a.m, a.k, a.a_pitch, BN);
+  if (e) return e;
+  const uint64_t tiles = (uint64_t)p.row_tiles * p.col_tiles;
+  // the split that leaves the least to the CTA with the most to do, a cluster's
+  // exchange counting as three blocks; it follows the sizes and the GPU, not the cap
+  uint32_t best = 0;
+  uint64_t best_cost = UINT64_MAX;
+  for (uint32_t s = 0; s <= 3 && (1u << s) <= p.blocks && (1u << s) <= BN / 2; ++s) {
+    const uint64_t cost = (uint64_t)ceil_div(tiles, sms >> s) * (ceil_div(p.blocks, 1u << s) + (s ? 3 : 1));
+    if (cost < best_cost) best = s, best_cost = cost;
+  }
+  const uint64_t clusters = tiles < (cap >> best) ? tiles : (cap >> best);
+  const unsigned grid = (unsigned)(clusters ? clusters : 1) << best;
+  return launch_cluster(mid_kernel<BN, T>, grid, kMidThreads, MidShape<BN>::kBytes, 1u << best, stream, r, c, p, best);
+}
+
+template <typename T>
+int launch_big(const MatmulArgs &a, ProductPlan p, unsigned cap, void *stream) {
+  p.r_scale = a.a_scale, p.c_scale = a.b_scale;
+  p.r_scale_pitch = a.a_scale_pitch, p.c_scale_pitch = a.b_scale_pitch;
+  p.r_shift = a.a_shift, p.c_shift = a.b_shift;
+  p.rows = a.m, p.cols = a.n;
+  p.row_tiles = ceil_div(a.m, 256), p.col_tiles = ceil_div(a.n, 256);
+  p.instruction = 1u << 4 | a.a_e5m2 << 7 | a.b_e5m2 << 10 | (256u >> 3) << 17 | (256u >> 4) << 24;
+  p.row_step = a.out_pitch, p.col_step = 1;
+  CUtensorMap ma, mb;
+  int e = encode(&ma, a.a, a.m, a.k, a.a_pitch, 128);
+  if (!e) e = encode(&mb, a.b, a.n, a.k, a.b_pitch, 128);
+  if (e) return e;
+  const uint64_t tiles = (uint64_t)p.row_tiles * p.col_tiles, pairs = cap >= 2 ? cap / 2 : 1;
+  const unsigned grid = (unsigned)(tiles < pairs ? tiles : pairs) * 2;
+  return a.b_shift ? launch_cluster(big_kernel<T, false>, grid, kBigThreads, kBigBytes, 2, stream, ma, mb, p)
+                   : launch_cluster(big_kernel<T, true>, grid, kBigThreads, kBigBytes, 2, stream, ma, mb, p);
 }
 
 }  // namespace
 
-int launch_matmul(const MatmulArgs &a, unsigned cap, void *stream) {
-  const uint64_t tiles = (uint64_t)((a.m + kTile - 1) / kTile) * ((a.n + kTile - 1) / kTile);
+int launch_matmul(const MatmulArgs &a, unsigned cap, unsigned sms, void *stream) {
+  if (a.k == 0) {
+    const size_t size = a.out_dtype == APC_F32 ? 4 : 2;
+    return (int)cudaMemset2DAsync(a.out, (size_t)a.out_pitch * size, 0, a.n * size, a.m, (cudaStream_t)stream);
+  }
+  ProductPlan p = {};
+  p.blocks = ceil_div(a.k, kBlock);
+  p.out = a.out;
+  int e = commit_status_word(&p.status);
+  if (e) return e;
   return with_dtype(a.out_dtype, [&](auto t) {
-    const uint64_t most = (uint64_t)cap * 4;
-    matmul_kernel<decltype(t)><<<(unsigned)(tiles < most ? tiles : most), 256, 0, (cudaStream_t)stream>>>(a);
-    return (int)cudaGetLastError();
+    using T = decltype(t);
+    if (a.m > 128 && (uint64_t)ceil_div(a.m, 256) * ceil_div(a.n, 256) >= sms / 4) return launch_big<T>(a, p, cap, stream);
+    if (a.m <= 16) return launch_mid<16, T>(a, p, cap, sms, stream);
+    if (a.m <= 32) return launch_mid<32, T>(a, p, cap, sms, stream);
+    if (a.m <= 64) return launch_mid<64, T>(a, p, cap, sms, stream);
+    return launch_mid<128, T>(a, p, cap, sms, stream);
   });
 }
 

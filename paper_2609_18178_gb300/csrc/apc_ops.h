@@ -22,7 +22,7 @@ apc_status op_cuda_fail(int err, const char *what);
 apc_status op_ranges(const OpRange *r, int n);
 // CTAs of a persistent grid with so many resident per SM, after
 // apc_set_reserved_sms and APC_GRID_LIMIT.
-apc_status op_grid(int per_sm, unsigned *cap);
+apc_status op_grid(int per_sm, unsigned *cap, unsigned *sms = nullptr);
 
 constexpr int kBlock = 128;  // columns (and, in square blocks, rows) that share a scale
 
@@ -59,7 +59,11 @@ struct MatmulArgs {
   uint32_t out_dtype;
 };
 
-int launch_matmul(const MatmulArgs &a, unsigned cap, void *stream);
+// cap: CTAs of the persistent grid; sms: the device's SMs, by which sizes alone choose
+// a kernel and a split.  Returns a cudaError_t value, as the others do.
+int launch_matmul(const MatmulArgs &a, unsigned cap, unsigned sms, void *stream);
+// The device status word of apc_device_status (apc_commit.cu) on the current device.
+int commit_status_word(unsigned **out);
 
 // ---- distillation
 struct DistillArgs {

@@ -140,8 +140,9 @@ APC_EXPORT apc_status apc_matmul_fp8(const apc_fp8_matrix *a, const apc_fp8_matr
   p.out_pitch = pitch_of(m, n, out_pitch);
   p.out_dtype = out_dtype;
   unsigned cap = 0;
-  if ((st = apc::op_grid(1, &cap)) != APC_OK) return st;
-  const int e = apc::launch_matmul(p, cap, stream);
+  unsigned sms = 0;
+  if ((st = apc::op_grid(1, &cap, &sms)) != APC_OK) return st;
+  const int e = apc::launch_matmul(p, cap, sms, stream);
   return e ? apc::op_cuda_fail(e, "product kernel launch") : APC_OK;
 }
 

@@ -208,7 +208,8 @@ def check_matmul(out, ref, size, k):
 @pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 16, 128), (1, 4096, 4096), (2, 129, 100), (7, 1000, 300), (16, 256, 2048),
                                    (17, 130, 129), (31, 65, 127), (33, 257, 640), (64, 4097, 256), (65, 500, 1111),
                                    (100, 128, 5000), (128, 128, 128), (129, 255, 384), (200, 700, 90), (256, 256, 1024),
-                                   (300, 513, 777), (513, 300, 257), (1000, 1, 1000), (1025, 513, 130), (2100, 2050, 16)])
+                                   (300, 513, 777), (513, 300, 257), (1000, 1, 1000), (1025, 513, 130), (2100, 2050, 16),
+                                   (2100, 2050, 1111), (5000, 600, 640)])
 @pytest.mark.parametrize("ba,bb", [(1, 128), (1, 1), (128, 128)])
 def test_matmul(m, n, k, ba, bb):
     a, sa = operand(m, k, ba, E4M3, m + k)
