@@ -39,6 +39,9 @@ struct ProductPlan {
   unsigned *status;
 };
 
+// A whole warp's wait: its lanes give up together.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity) { return __all_sync(~0u, mbar_wait(bar, parity)); }
+
 __device__ __forceinline__ void give_up(unsigned *status) { atomicOr(status, (unsigned)APC_ETIMEOUT); }
 
 // ---------------------------------------------------------------------------
@@ -97,23 +100,24 @@ __global__ void __launch_bounds__(kMidThreads, 1)
   const uint32_t tmem = tmem_at;
 
   if (warp == 0) {
-    if (lane == 0) {
-      prefetch_map(&map_r);
-      prefetch_map(&map_c);
+    {
       uint32_t use = 0;
       bool ok = true;
       for (uint32_t t = first; t < tiles && ok; t += step) {
         const int32_t r0 = (int32_t)(t % p.row_tiles) * 128, c0 = (int32_t)(t / p.row_tiles) * BN;
         for (uint32_t b = b0; b < b1; ++b, ++use) {
           const uint32_t st = use % S::kStages;
-          if (use >= S::kStages && !mbar_wait(&empty[st], (use / S::kStages + 1) & 1)) {
+          if (use >= S::kStages && !warp_wait(&empty[st], (use / S::kStages + 1) & 1)) {
             ok = false;
             break;
           }
           const uint32_t at = smem_addr(smem + st * S::kStageBytes), bar = smem_addr(&full[st]);
-          mbar_arrive_expect_tx(&full[st], S::kStageBytes);
-          load_box(at, &map_r, (int32_t)(b * kBlock), r0, bar);
-          load_box(at + S::kRowBytes, &map_c, (int32_t)(b * kBlock), c0, bar);
+          if (elect_one()) {
+            mbar_arrive_expect_tx(&full[st], S::kStageBytes);
+            load_box(at, &map_r, (int32_t)(b * kBlock), r0, bar);
+            load_box(at + S::kRowBytes, &map_c, (int32_t)(b * kBlock), c0, bar);
+          }
+          __syncwarp();
         }
       }
       if (!ok) {  // let the copies in flight land
@@ -122,23 +126,26 @@ __global__ void __launch_bounds__(kMidThreads, 1)
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    {
       uint32_t use = 0;
       bool ok = true;
       for (uint32_t t = first; t < tiles && ok; t += step)
         for (uint32_t b = b0; b < b1; ++b, ++use) {
           const uint32_t st = use % S::kStages, buf = use & 1;
-          if ((use >= 2 && !mbar_wait(&acc_empty[buf], (use / 2 + 1) & 1)) || !mbar_wait(&full[st], use / S::kStages & 1)) {
+          if ((use >= 2 && !warp_wait(&acc_empty[buf], (use / 2 + 1) & 1)) || !warp_wait(&full[st], use / S::kStages & 1)) {
             ok = false;
             break;
           }
           tc_fence_after();
           const uint64_t dr = operand_desc(smem_addr(smem + st * S::kStageBytes));
           const uint64_t dc = operand_desc(smem_addr(smem + st * S::kStageBytes + S::kRowBytes));
+          if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) mma_fp8<1>(tmem + buf * BN, dr + 2 * k, dc + 2 * k, p.instruction, k > 0);
-          mma_commit(&empty[st]);
-          mma_commit(&acc_full[buf]);
+            for (int k = 0; k < 4; ++k) mma_fp8<1>(tmem + buf * BN, dr + 2 * k, dc + 2 * k, p.instruction, k > 0);
+            mma_commit(&empty[st]);
+            mma_commit(&acc_full[buf]);
+          }
+          __syncwarp();
         }
       if (!ok) {  // let the products in flight end
         give_up(p.status);
@@ -177,7 +184,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
           if (BN >= 32 || lane < BN) s[i * 32 + lane] = next_c[i];
         __syncwarp();
         if (b + 1 < b1) fetch(b + 1);
-        ok = __all_sync(~0u, mbar_wait(&acc_full[buf], use / 2 & 1));
+        ok = warp_wait(&acc_full[buf], use / 2 & 1);
         if (!ok) break;
         tc_fence_after();
         const uint32_t at = tmem + buf * BN + (quad << 21);  // lane 32 * quad in bits 16 up
@@ -185,8 +192,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
 #pragma unroll
         for (int c = 0; c < BN; c += kChunk) {
           uint32_t d[kChunk];
-          if constexpr (kChunk == 32) tmem_load32(d, at + c);
-          else tmem_load16(d, at + c);
+          tmem_load(d, at + c);
           tmem_landed(d);
           if (c + kChunk == BN) {
             tc_fence_before();
@@ -255,9 +261,24 @@ __global__ void __launch_bounds__(kMidThreads, 1)
 // it holds half in shared memory (tcgen05.mma.cta_group::2 reads both halves).
 // The first CTA's thread issues for both.  Persistent: the pair's next tile is
 // loaded and multiplied while the epilogue stores.
-constexpr int kBigThreads = 320, kBigStages = 6;
+#ifndef APC_BIG_WARPS
+#define APC_BIG_WARPS 8
+#endif
+#ifndef APC_BIG_UNITS
+#define APC_BIG_UNITS 1
+#endif
+#ifndef APC_BIG_LOAD
+#define APC_BIG_LOAD 16
+#endif
+#ifndef APC_BIG_STAGES
+#define APC_BIG_STAGES 6
+#endif
+constexpr int kBigWarps = APC_BIG_WARPS, kBigUnits = APC_BIG_UNITS, kBigLoad = APC_BIG_LOAD;
+constexpr int kBigThreads = 128 + 32 * kBigWarps, kBigStages = APC_BIG_STAGES;
+constexpr int kBigCols = 1024 / kBigWarps;  // columns that a warp adds up
+constexpr int kUnitCols = 256 / kBigUnits;
 constexpr int kBigHalf = 128 * kBlock, kBigStageBytes = 2 * kBigHalf;
-constexpr int kBigScaleBytes = 8 * 2 * 128 * 4;
+constexpr int kBigScaleBytes = kBigWarps * 2 * kBigCols * 4;
 constexpr int kBigBytes = 1024 + kBigStages * kBigStageBytes + kBigScaleBytes;
 constexpr uint32_t kBigGroup = 16;  // row tiles that are walked together
 
@@ -271,11 +292,11 @@ __device__ __forceinline__ void big_tile(const ProductPlan &p, uint32_t t, uint3
 }
 
 template <typename T>
-__device__ __forceinline__ void store_row(T *out, const uint64_t (&acc)[64], uint32_t count) {
+__device__ __forceinline__ void store_row(T *out, const uint64_t (&acc)[kBigCols / 2], uint32_t count) {
   constexpr int kPer = 16 / sizeof(T);
-  if (count == 128 && (uintptr_t)out % 16 == 0) {
+  if (count == kBigCols && (uintptr_t)out % 16 == 0) {
 #pragma unroll
-    for (int i = 0; i < 128; i += kPer) {
+    for (int i = 0; i < kBigCols; i += kPer) {
       union {
         T v[kPer];
         uint4 q;
@@ -290,7 +311,7 @@ __device__ __forceinline__ void store_row(T *out, const uint64_t (&acc)[64], uin
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 64; ++i) {
+    for (int i = 0; i < kBigCols / 2; ++i) {
       const float2 v = unpack2(acc[i]);
       if (2 * i < count) out[2 * i] = from_float<T>(v.x);
       if (2 * i + 1 < count) out[2 * i + 1] = from_float<T>(v.y);
@@ -304,7 +325,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
     big_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ ProductPlan p) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[kBigStages], empty[kBigStages], acc_full[2], acc_empty[2];
+  __shared__ uint64_t full[kBigStages], empty[kBigStages], acc_full[2 * kBigUnits], acc_empty[2 * kBigUnits];
   __shared__ uint32_t tmem_at;
   uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   float *scales = reinterpret_cast<float *>(smem + kBigStages * kBigStageBytes);
@@ -313,7 +334,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kBigStages; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
-    for (int i = 0; i < 2; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 16);
+    for (int i = 0; i < 2 * kBigUnits; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 2 * kBigWarps / kBigUnits);
     mbar_init_fence();
   }
   if (warp == 1) tmem_alloc<2>(&tmem_at, 512);
@@ -323,128 +344,140 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   cluster_arrive(), cluster_wait();
   const uint32_t tmem = tmem_at;
 
-  if (warp == 0) {
-    if (lane == 0) {
-      prefetch_map(&map_a);
-      prefetch_map(&map_b);
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBigWarps == 8 ? 56 : 32));
+    if (warp == 0) {
       uint32_t use = 0;
       bool ok = true;
       for (uint32_t t = first; t < tiles && ok; t += step) {
         uint32_t tr, tc;
         big_tile(p, t, &tr, &tc);
-        const int32_t r0 = (int32_t)(tr * 256 + rank * 128), c0 = (int32_t)(tc * 256 + rank * 128);
+        const int32_t r0 = (int32_t)(tr * 256 + rank * 128), c0 = (int32_t)(tc * 256 + rank * (kUnitCols / 2));
         for (uint32_t b = 0; b < p.blocks; ++b, ++use) {
           const uint32_t st = use % kBigStages;
-          if (use >= kBigStages && !mbar_wait_cluster(&empty[st], (use / kBigStages + 1) & 1)) {
+          if (use >= kBigStages && !warp_wait(&empty[st], (use / kBigStages + 1) & 1)) {
             ok = false;
             break;
           }
           const uint32_t at = smem_addr(smem + st * kBigStageBytes), bar = map_rank(smem_addr(&full[st]), 0);
-          if (rank == 0) mbar_arrive_expect_tx(&full[st], 2 * kBigStageBytes);
-          load_box_pair(at, &map_a, (int32_t)(b * kBlock), r0, bar);
-          load_box_pair(at + kBigHalf, &map_b, (int32_t)(b * kBlock), c0, bar);
+          if (elect_one()) {
+            if (rank == 0) mbar_arrive_expect_tx(&full[st], 2 * kBigStageBytes);
+            load_box_pair(at, &map_a, (int32_t)(b * kBlock), r0, bar);
+            load_box_pair(at + kBigHalf, &map_b, (int32_t)(b * kBlock), c0, bar);
+            if (kBigUnits == 2) load_box_pair(at + kBigHalf + kBigHalf / 2, &map_b, (int32_t)(b * kBlock), c0 + 128, bar);
+          }
+          __syncwarp();
         }
       }
       if (!ok) {  // let the copies in flight land, the other CTA's too
         give_up(p.status);
         if (rank == 0)
-          for (uint32_t u = use > kBigStages ? use - kBigStages : 0; u < use; ++u) mbar_wait_cluster(&full[u % kBigStages], u / kBigStages & 1);
+          for (uint32_t u = use > kBigStages ? use - kBigStages : 0; u < use; ++u) mbar_wait(&full[u % kBigStages], u / kBigStages & 1);
         const uint64_t t0 = global_ns();
         for (uint32_t i = 0; i < kWaitIterations && global_ns() - t0 < 1000000; ++i) __nanosleep(1000);
       }
     }
-  } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    if (warp == 1 && rank == 0) {
       uint32_t use = 0;
       bool ok = true;
       for (uint32_t t = first; t < tiles && ok; t += step)
         for (uint32_t b = 0; b < p.blocks; ++b, ++use) {
           const uint32_t st = use % kBigStages, buf = use & 1;
-          if ((use >= 2 && !mbar_wait_cluster(&acc_empty[buf], (use / 2 + 1) & 1)) ||
-              !mbar_wait_cluster(&full[st], use / kBigStages & 1)) {
-            ok = false;
-            break;
-          }
-          tc_fence_after();
+          if (!(ok = warp_wait(&full[st], use / kBigStages & 1))) break;
           const uint64_t da = operand_desc(smem_addr(smem + st * kBigStageBytes));
           const uint64_t db = operand_desc(smem_addr(smem + st * kBigStageBytes + kBigHalf));
 #pragma unroll
-          for (int k = 0; k < 4; ++k) mma_fp8<2>(tmem + buf * 256, da + 2 * k, db + 2 * k, p.instruction, k > 0);
-          mma_commit_pair(&empty[st]);
-          mma_commit_pair(&acc_full[buf]);
+          for (int h = 0; h < kBigUnits; ++h) {
+            if (use >= 2 && !(ok = warp_wait(&acc_empty[2 * h + buf], (use / 2 + 1) & 1))) break;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                mma_fp8<2>(tmem + (2 * h + buf) * kUnitCols, da + 2 * k, db + h * (kBigHalf / 2 >> 4) + 2 * k, p.instruction, k > 0);
+              mma_commit_pair(&acc_full[2 * h + buf]);
+              if (h == kBigUnits - 1) mma_commit_pair(&empty[st]);
+            }
+            __syncwarp();
+          }
+          if (!ok) break;
         }
       if (!ok) {  // let the products in flight end
         give_up(p.status);
-        for (uint32_t u = use > 2 ? use - 2 : 0; u < use; ++u) mbar_wait_cluster(&acc_full[u & 1], u / 2 & 1);
+        for (uint32_t u = use > 2 ? use - 2 : 0; u < use; ++u)
+          for (int h = 0; h < kBigUnits; ++h) mbar_wait(&acc_full[2 * h + (u & 1)], u / 2 & 1);
       }
     }
   } else {
-    const uint32_t quad = warp & 3, half = (warp - 2) / 4, row = quad * 32 + lane;
-    float *sc = scales + (warp - 2) * 2 * 128;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kBigWarps == 8 ? 224 : 112));
+    const uint32_t quad = warp & 3, part = (warp - 4) / 4, half = part * kBigCols / kUnitCols, row = quad * 32 + lane;
+    float *sc = scales + (warp - 4) * 2 * kBigCols;
     uint32_t use = 0;
     bool ok = true;
     for (uint32_t t = first; t < tiles && ok; t += step) {
       uint32_t tr, tc;
       big_tile(p, t, &tr, &tc);
-      const uint32_t r0 = tr * 256 + rank * 128, c0 = tc * 256 + half * 128;
+      const uint32_t r0 = tr * 256 + rank * 128, c0 = tc * 256 + part * kBigCols;
       const uint32_t r = min(r0 + row, p.rows - 1);
       const float *rs = p.r_scale + (r >> p.r_shift);
-      float next_r, next_c[ROWS ? 4 : 1];
+      float next_r, next_c[ROWS ? kBigCols / 32 : 1];
       auto fetch = [&](uint32_t b) {
         next_r = __ldg(rs + b * p.r_scale_pitch);
         if (ROWS) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < kBigCols / 32; ++i)
             next_c[i] = __ldg(p.c_scale + b * p.c_scale_pitch + min(c0 + i * 32 + lane, p.cols - 1));
         } else {
           next_c[0] = __ldg(p.c_scale + b * p.c_scale_pitch + (min(c0, p.cols - 1) >> 7));
         }
       };
-      uint64_t acc[64];
+      uint64_t acc[kBigCols / 2];
 #pragma unroll
-      for (int i = 0; i < 64; ++i) acc[i] = 0;
+      for (int i = 0; i < kBigCols / 2; ++i) acc[i] = 0;
+      // adds some columns of a sum of 128 products, scaled; c: the first, within the warp's
+      auto add = [&](const uint32_t (&d)[kBigLoad], int c, uint64_t sr, const float *s) {
+#pragma unroll
+        for (int i = 0; i < kBigLoad; i += 4) {
+          uint64_t x = sr, y = sr;
+          if (ROWS) {
+            const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(s + c + i);
+            x = mul2(sr, v.x), y = mul2(sr, v.y);
+          }
+          acc[(c + i) / 2] = fma2(pack2(d[i], d[i + 1]), x, acc[(c + i) / 2]);
+          acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), y, acc[(c + i) / 2 + 1]);
+        }
+      };
       fetch(0);
       for (uint32_t b = 0; b < p.blocks; ++b, ++use) {
         const uint32_t buf = use & 1;
-        float *s = sc + buf * 128;
+        float *s = sc + buf * kBigCols;
         const float one = ROWS ? next_r : next_r * next_c[0];
         const uint64_t sr = pack2(one, one);
         if (ROWS) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[i * 32 + lane] = next_c[i];
+          for (int i = 0; i < kBigCols / 32; ++i) s[i * 32 + lane] = next_c[i];
           __syncwarp();
         }
         if (b + 1 < p.blocks) fetch(b + 1);
-        ok = __all_sync(~0u, mbar_wait_cluster(&acc_full[buf], use / 2 & 1));
+        ok = warp_wait(&acc_full[2 * half + buf], use / 2 & 1);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t at = tmem + buf * 256 + half * 128 + (quad << 21);
+        const uint32_t at = tmem + (2 * half + buf) * kUnitCols + part * kBigCols % kUnitCols + (quad << 21);
 #pragma unroll
-        for (int c = 0; c < 128; c += 32) {
-          uint32_t d[32];
-          tmem_load32(d, at + c);
+        for (int c = 0; c < kBigCols; c += kBigLoad) {
+          uint32_t d[kBigLoad];
+          tmem_load(d, at + c);
           tmem_landed(d);
-          if (c == 96) {
+          if (c + kBigLoad == kBigCols) {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) arrive_remote(map_rank(smem_addr(&acc_empty[buf]), 0));
+            if (lane == 0) arrive_remote_relaxed(map_rank(smem_addr(&acc_empty[2 * half + buf]), 0));
           }
-#pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            if (ROWS) {
-              const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(s + c + i);
-              acc[(c + i) / 2] = fma2(pack2(d[i], d[i + 1]), mul2(sr, v.x), acc[(c + i) / 2]);
-              acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), mul2(sr, v.y), acc[(c + i) / 2 + 1]);
-            } else {
-              acc[(c + i) / 2] = fma2(pack2(d[i], d[i + 1]), sr, acc[(c + i) / 2]);
-              acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), sr, acc[(c + i) / 2 + 1]);
-            }
-          }
+          add(d, c, sr, s);
         }
       }
       if (!ok) break;
       if (r0 + row < p.rows && c0 < p.cols)
-        store_row(static_cast<T *>(p.out) + (int64_t)(r0 + row) * p.row_step + c0, acc, min(128u, p.cols - c0));
+        store_row(static_cast<T *>(p.out) + (int64_t)(r0 + row) * p.row_step + c0, acc, min((uint32_t)kBigCols, p.cols - c0));
     }
     if (!ok) give_up(p.status);
   }
@@ -528,11 +561,11 @@ int launch_big(const MatmulArgs &a, ProductPlan p, unsigned cap, void *stream) {
   p.r_shift = a.a_shift, p.c_shift = a.b_shift;
   p.rows = a.m, p.cols = a.n;
   p.row_tiles = ceil_div(a.m, 256), p.col_tiles = ceil_div(a.n, 256);
-  p.instruction = 1u << 4 | a.a_e5m2 << 7 | a.b_e5m2 << 10 | (256u >> 3) << 17 | (256u >> 4) << 24;
+  p.instruction = 1u << 4 | a.a_e5m2 << 7 | a.b_e5m2 << 10 | (uint32_t)(kUnitCols >> 3) << 17 | (256u >> 4) << 24;
   p.row_step = a.out_pitch, p.col_step = 1;
   CUtensorMap ma, mb;
   int e = encode(&ma, a.a, a.m, a.k, a.a_pitch, 128);
-  if (!e) e = encode(&mb, a.b, a.n, a.k, a.b_pitch, 128);
+  if (!e) e = encode(&mb, a.b, a.n, a.k, a.b_pitch, kUnitCols / 2);
   if (e) return e;
   const uint64_t tiles = (uint64_t)p.row_tiles * p.col_tiles, pairs = cap >= 2 ? cap / 2 : 1;
   const unsigned grid = (unsigned)(tiles < pairs ? tiles : pairs) * 2;

@@ -9,6 +9,21 @@
 
 namespace apc {
 
+// One lane of a converged warp, in a form that the compiler knows to be one.
+// The loops around tcgen05 and TMA run in the whole warp, so that barriers,
+// coordinates and descriptors stay in uniform registers, and only the
+// instructions themselves are elected: with a loop in one lane the issue of
+// four products took 600 cycles, more than the products.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(p));
+  return p != 0;
+}
+
 // ---- clusters
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -28,6 +43,13 @@ __device__ __forceinline__ uint32_t map_rank(uint32_t a, uint32_t rank) {
 
 __device__ __forceinline__ void arrive_remote(uint32_t mapped) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mapped) : "memory");
+}
+
+// The same where nothing but tensor memory was read, which tcgen05.fence orders: a
+// release at cluster scope waits for the thread's memory operations, 1,000
+// cycles and more, and would bound the product kernel (1,136 TFLOP/s with it).
+__device__ __forceinline__ void arrive_remote_relaxed(uint32_t mapped) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(mapped) : "memory");
 }
 
 // Stores a word into another CTA's shared memory and counts its 4 bytes there.
@@ -103,7 +125,7 @@ __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
 // 32 columns of this thread's lane.
-__device__ __forceinline__ void tmem_load32(uint32_t (&r)[32], uint32_t at) {
+__device__ __forceinline__ void tmem_load(uint32_t (&r)[32], uint32_t at) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
       "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
@@ -114,7 +136,7 @@ __device__ __forceinline__ void tmem_load32(uint32_t (&r)[32], uint32_t at) {
       : "r"(at));
 }
 
-__device__ __forceinline__ void tmem_load16(uint32_t (&r)[16], uint32_t at) {
+__device__ __forceinline__ void tmem_load(uint32_t (&r)[16], uint32_t at) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
