@@ -83,7 +83,7 @@ struct DistillArgs {
   float grad_kd;             // kd_weight*tau
 };
 
-int launch_distill(const DistillArgs &a, unsigned cap, void *stream);
+int launch_distill(const DistillArgs &a, unsigned cap, unsigned sms, void *stream);
 int distill_per_sm(const DistillArgs &a);
 
 }  // namespace apc

@@ -228,8 +228,9 @@ apc_status distill(const apc_distill *d, const float *grad_loss, float *loss, fl
   a.grad_kd = (float)(d->kd_weight * tau);
   a.loss_label = (float)d->label_weight;
   unsigned cap = 0;
-  if ((st = apc::op_grid(apc::distill_per_sm(a), &cap)) != APC_OK) return st;
-  const int e = apc::launch_distill(a, cap, stream);
+  unsigned sms = 0;
+  if ((st = apc::op_grid(apc::distill_per_sm(a), &cap, &sms)) != APC_OK) return st;
+  const int e = apc::launch_distill(a, cap, sms, stream);
   return e ? apc::op_cuda_fail(e, "distillation kernel launch") : APC_OK;
 }
 
