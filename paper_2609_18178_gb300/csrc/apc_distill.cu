@@ -9,11 +9,17 @@
 // go through in pairs, two fp32 lanes an instruction.
 //
 // A row belongs to one CTA or, where rows are few or long, to a cluster whose
-// CTAs exchange maxima and sums.  Its logits are read once: they stay in
-// registers between the normaliser and the gradient where they fit (kVectors of
-// 16 bytes a thread), else the second sweep reads them again.  One extra warp
-// works on the teacher's few entries, a row ahead.
+// CTAs exchange maxima and sums.  Its logits come once, by bulk copies into a
+// ring of shared-memory chunks that runs ahead of the arithmetic into the next
+// row, and stay there between the normaliser and the gradient; a part that the
+// ring does not hold is loaded a second time.  One warp copies, a few work on the
+// teacher's entries some rows ahead, the others on the logits.
+//
+// Every wait on a barrier is bounded; one that gives up sets the device status
+// word, and the CTA goes through its rows without waiting or copying further.
 #include <cuda_runtime.h>
+
+#include <algorithm>
 
 #include "apc_ops.cuh"
 #include "apc_tcgen05.cuh"
@@ -22,24 +28,24 @@ namespace apc {
 
 namespace {
 
-#ifndef APC_DISTILL_WORKERS
-#define APC_DISTILL_WORKERS 256
+#ifndef APC_DISTILL_WARPS
+#define APC_DISTILL_WARPS 8
 #endif
-#ifndef APC_DISTILL_KEEP
-#define APC_DISTILL_KEEP 16
+#ifndef APC_DISTILL_CTAS
+#define APC_DISTILL_CTAS 2
 #endif
-#ifndef APC_DISTILL_STREAM
-#define APC_DISTILL_STREAM 8
+#ifndef APC_DISTILL_TEACHERS
+#define APC_DISTILL_TEACHERS 4
 #endif
-#ifndef APC_DISTILL_STREAM_CTAS
-#define APC_DISTILL_STREAM_CTAS 4
+#ifndef APC_DISTILL_VECTORS
+#define APC_DISTILL_VECTORS 8
 #endif
-constexpr int kWorkers = APC_DISTILL_WORKERS, kThreads = kWorkers + 32, kWarps = kWorkers / 32;
-// Vectors of 16 bytes that a thread holds, and CTAs on an SM: the rows that stay
-// in registers, and the forms that pass over the logits once.
-constexpr int kKeep = APC_DISTILL_KEEP, kStream = APC_DISTILL_STREAM;
-constexpr int residents(int form) { return form == 3 ? 2 : APC_DISTILL_STREAM_CTAS; }
-constexpr int kSlots = 2048;  // of the table that finds equal ids
+// Warps on the logits and on the teacher's entries, vectors of 16 bytes that each
+// of the former's threads takes of a chunk, CTAs on an SM.
+constexpr int kWarps = APC_DISTILL_WARPS, kWorkers = 32 * kWarps, kTeachers = APC_DISTILL_TEACHERS;
+constexpr int kThreads = kWorkers + 32 * kTeachers + 32;
+constexpr int kVectors = APC_DISTILL_VECTORS, kChunk = kWorkers * kVectors, kMaxChunks = 16;
+constexpr int kCtas = APC_DISTILL_CTAS;
 constexpr int kMaxSplit = 8;
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -80,21 +86,50 @@ __device__ __forceinline__ Sum joined(Sum a, float scale, int lanes = 32) {
   return a;
 }
 
-// What the teacher's warp leaves of a row's entries; the label is entry k.
+// What a teacher's warp leaves of a row's entries; the label is entry k.
 struct Entries {
-  int32_t id[APC_DISTILL_MAX_K + 1];  // -1: does not count
-  float p[APC_DISTILL_MAX_K + 1];     // the probability; the label's is 1
-  float z[APC_DISTILL_MAX_K + 1];     // the student's logit there
-  float p_sum, entropy;               // sum of p and of p log p
-  int32_t same;                       // some place occurs twice
+  int32_t *id;           // -1: does not count
+  float *p;              // the probability; the label's is 1
+  float *z;              // the student's logit there
+  float p_sum, entropy;  // sum of p and of p log p
+  int32_t same;          // some place occurs twice
 };
 
 struct Shared {
-  Entries e[2];
-  __align__(16) int32_t slot[kSlots];
-  Sum part[2][kWarps];
-  Sum peer[2][kMaxSplit];
+  Entries e[kTeachers + 1];
+  Sum part[kTeachers + 1][kWarps];
+  Sum peer[kTeachers + 1][kMaxSplit];
+  uint64_t full[kMaxChunks], empty[kMaxChunks], peer_full[kTeachers + 1];
+  int32_t dead;
+  int32_t pad_;
 };
+
+// How the rest of shared memory is shared out: the ring, the entries of one row
+// more than there are teachers, each teacher's table of ids.
+struct Layout {
+  uint32_t chunks, teachers, room, slots_log2;  // room: entries of a row, the label's among them
+  __host__ __device__ uint32_t bytes() const {
+    return (uint32_t)sizeof(Shared) + 16 + chunks * kChunk * 16 + (teachers + 1) * room * 12 + (teachers * 4 << slots_log2);
+  }
+};
+
+// wait_for, at once if another wait of this CTA has given up.
+__device__ __noinline__ void wait_alive(uint32_t bar, uint32_t parity, volatile int32_t *dead, unsigned *status) {
+  uint64_t t0 = 0;
+  for (uint32_t it = 1; !*dead; ++it) {
+    if (mbar_try_wait(bar, parity)) return;
+    if (it == 1024) t0 = global_ns();
+    if (it >= kWaitIterations && (it & 1023u) == 0 && global_ns() - t0 > kWaitNanoseconds) {
+      *dead = 1;
+      atomicOr(status, (unsigned)APC_ETIMEOUT);
+    }
+  }
+}
+
+__device__ __forceinline__ void wait(uint64_t *bar, uint32_t parity, Shared &sh, unsigned *status) {
+  const uint32_t a = smem_addr(bar);
+  if (!mbar_try_wait(a, parity) && !mbar_try_wait(a, parity)) wait_alive(a, parity, &sh.dead, status);
+}
 
 __device__ __forceinline__ int64_t index_at(const void *p, bool wide, int64_t i) {
   return wide ? static_cast<const int64_t *>(p)[i] : static_cast<const int32_t *>(p)[i];
@@ -109,24 +144,43 @@ __device__ __forceinline__ float number_at(const void *p, uint32_t dtype, int64_
 // One warp: the entries of a row.  Equal ids are looked for with a table of the
 // ids by hash.
 template <typename T>
-__device__ void teacher_entries(const DistillArgs &a, uint32_t row, Entries &e, int32_t *slot, uint32_t lane) {
+__device__ __noinline__ void teacher_entries(const DistillArgs &a, uint32_t row, Entries &e, int32_t *slot, uint32_t slots_log2,
+                                             uint32_t lane) {
   const T *z = static_cast<const T *>(a.logits) + (int64_t)row * a.pitch;
+  const int64_t at_id = (int64_t)row * a.ids_pitch, at_u = (int64_t)row * a.teacher_pitch;
+  int32_t *ids = e.id;
+  float *ps = e.p, *zs = e.z;
   float top = -kInf;
-  for (uint32_t i = lane; i < a.k; i += 32) {
-    const int64_t id = index_at(a.ids, a.ids64, (int64_t)row * a.ids_pitch + i);
-    const float u = number_at(a.teacher, a.teacher_dtype, (int64_t)row * a.teacher_pitch + i);
-    const bool counts = id >= 0 && id < (int64_t)a.vocab && u != -kInf;
-    e.id[i] = counts ? (int32_t)id : -1;
-    e.p[i] = counts ? u : -kInf;
-    e.z[i] = counts ? to_float(z[id]) : 0.0f;
-    if (counts) top = fmaxf(top, u);
+  constexpr int kBatch = 4;  // loads in flight
+  for (uint32_t i0 = lane; i0 < a.k; i0 += 32 * kBatch) {
+    int64_t id[kBatch];
+    float u[kBatch], x[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const uint32_t i = i0 + 32 * b;
+      id[b] = i < a.k ? index_at(a.ids, a.ids64, at_id + i) : -1;
+      u[b] = i < a.k ? number_at(a.teacher, a.teacher_dtype, at_u + i) : -kInf;
+      if (id[b] < 0 || id[b] >= (int64_t)a.vocab || u[b] == -kInf) id[b] = -1, u[b] = -kInf;
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) x[b] = id[b] >= 0 ? to_float(z[id[b]]) : 0.0f;
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const uint32_t i = i0 + 32 * b;
+      if (i < a.k) ids[i] = (int32_t)id[b], ps[i] = u[b], zs[i] = x[b];
+      top = fmaxf(top, u[b]);
+    }
   }
   if (lane == 0) {
     int64_t y = a.labels ? index_at(a.labels, a.labels64, row) : -1;
     if (y >= (int64_t)a.vocab || y < 0) y = -1;
-    e.id[a.k] = (int32_t)y;
-    e.p[a.k] = 1.0f;
-    e.z[a.k] = y >= 0 ? to_float(z[y]) : 0.0f;
+    ids[a.k] = (int32_t)y;
+    ps[a.k] = 1.0f;
+    zs[a.k] = y >= 0 ? to_float(z[y]) : 0.0f;
+  }
+  if (a.dlogits) {  // an empty table
+    int4 *t = reinterpret_cast<int4 *>(slot);
+    for (uint32_t i = lane; i < 1u << slots_log2 >> 2; i += 32) t[i] = make_int4(-1, -1, -1, -1);
   }
   for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
   float norm = 0.0f;
@@ -136,37 +190,34 @@ __device__ void teacher_entries(const DistillArgs &a, uint32_t row, Entries &e, 
   } else {
     if (top == -kInf) top = 0.0f;
     float s = 0.0f;
-    for (uint32_t i = lane; i < a.k; i += 32) s += exp2f((e.p[i] - top) * a.scale2);
+    for (uint32_t i = lane; i < a.k; i += 32) s += exp2f((ps[i] - top) * a.scale2);
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
     norm = logf(s);
   }
   float p_sum = 0.0f, entropy = 0.0f;
-  for (uint32_t i = lane; i < a.k; i += 32) {
-    const float lp = e.id[i] >= 0 ? __fmaf_rn(e.p[i] - top, a.inv_tau, -norm) : -kInf, p = expf(lp);
-    e.p[i] = p;
-    p_sum += p;
-    if (p != 0.0f) entropy = __fmaf_rn(p, lp, entropy);
+  bool same = false;
+  __syncwarp();
+  for (uint32_t i = lane; i <= a.k; i += 32) {
+    const int32_t id = ids[i];
+    if (i < a.k) {
+      const float lp = id >= 0 ? __fmaf_rn(ps[i] - top, a.inv_tau, -norm) : -kInf, p = expf(lp);
+      ps[i] = p;
+      p_sum += p;
+      if (p != 0.0f) entropy = __fmaf_rn(p, lp, entropy);
+    }
+    if (a.dlogits && id >= 0)
+      for (uint32_t h = (uint32_t)id * 2654435761u >> (32 - slots_log2);; h = (h + 1) & ((1u << slots_log2) - 1)) {  // at most half full
+        const int32_t was = atomicCAS(&slot[h], -1, id);
+        same |= was == id;
+        if (was == -1 || was == id) break;
+      }
   }
   for (int o = 16; o; o >>= 1) {
     p_sum += __shfl_xor_sync(~0u, p_sum, o);
     entropy += __shfl_xor_sync(~0u, entropy, o);
   }
-  if (lane == 0) e.p_sum = p_sum, e.entropy = entropy;
-  if (!a.dlogits) return;
-  for (uint32_t i = lane; i < kSlots / 4; i += 32) reinterpret_cast<int4 *>(slot)[i] = make_int4(-1, -1, -1, -1);
-  __syncwarp();
-  bool same = false;
-  for (uint32_t i = lane; i <= a.k; i += 32) {
-    const int32_t id = e.id[i];
-    if (id < 0) continue;
-    for (uint32_t h = (uint32_t)id * 2654435761u >> 21;; h = (h + 1) % kSlots) {  // at most half full
-      const int32_t was = atomicCAS(&slot[h], -1, id);
-      same |= was == id;
-      if (was == -1 || was == id) break;
-    }
-  }
   same = __any_sync(~0u, same);
-  if (lane == 0) e.same = same;
+  if (lane == 0) e.p_sum = p_sum, e.entropy = entropy, e.same = same;
 }
 
 // Words of T: a pair of 16 bits or one of 32.
@@ -260,236 +311,304 @@ __device__ __forceinline__ float largest(const uint4 (&x)[N]) {
   }
 }
 
-// Nothing known of the words beyond this point: they are widened anew, not kept wide.
-template <int N>
-__device__ __forceinline__ void forget(uint4 (&x)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(x[i].x), "+r"(x[i].y), "+r"(x[i].z), "+r"(x[i].w));
-}
-
 // A vector of elements that leave every maximum and sum alone.
 template <typename T>
 __device__ __forceinline__ uint4 nothing() {
-  const uint32_t w = sizeof(T) == 4 ? 0xff800000u : sizeof(T) == 2 && __is_same(T, __half) ? 0xfc00fc00u : 0xff80ff80u;
+  const uint32_t w = sizeof(T) == 4 ? 0xff800000u : __is_same(T, __half) ? 0xfc00fc00u : 0xff80ff80u;
   return {w, w, w, w};
 }
 
 // FORM: 1 loss, 2 gradient, 3 both.  TWO: the labels need the sums at tau = 1
-// beside those at tau.
+// beside those at tau.  alike: the gradient's rows are aligned as the logits' are.
 template <typename T, int FORM, bool TWO>
-__global__ void __launch_bounds__(kThreads, FORM == 3 ? 2 : APC_DISTILL_STREAM_CTAS)
-    distill_kernel(const __grid_constant__ DistillArgs a, const uint32_t split, const bool alike) {
+__global__ void __launch_bounds__(kThreads, kCtas)
+    distill_kernel(const __grid_constant__ DistillArgs a, const __grid_constant__ Layout layout, const uint32_t split,
+                   const bool alike) {
   extern __shared__ __align__(16) uint8_t raw[];
   Shared &sh = *reinterpret_cast<Shared *>(raw);
-  constexpr int kPer = 16 / sizeof(T);
+  uint4 *ring = reinterpret_cast<uint4 *>(raw + (sizeof(Shared) + 15) / 16 * 16);
+  int32_t *tables = reinterpret_cast<int32_t *>(ring + layout.chunks * kChunk);
+  const uint32_t kChunks = layout.chunks;
+  constexpr int kPer = 16 / sizeof(T), kPairs = kPer / 2;
   constexpr bool kLoss = FORM & 1, kGrad = FORM & 2;
-  constexpr int kVectors = FORM == 3 ? kKeep : kStream;
   const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const uint32_t rank = split > 1 ? blockIdx.x % split : 0, first = blockIdx.x / split, step = gridDim.x / split;
   const bool together = kLoss && split > 1;  // the CTAs of a row are a cluster
-  const bool worker = warp < kWarps;
-  if (!worker && first < a.rows) teacher_entries<T>(a, first, sh.e[0], sh.slot, lane);
-  uint32_t turn = 0;
-  for (uint32_t row = first; row < a.rows; row += step, turn ^= 1) {
-    const T *z = static_cast<const T *>(a.logits) + (int64_t)row * a.pitch;
-    // vectors [v0, v1) of the 16-byte aligned body are this CTA's; the elements
-    // outside the body are the first CTA's, one a thread
-    const uint32_t head = min(a.vocab, (uint32_t)((16 - (uintptr_t)z % 16) % 16 / sizeof(T)));
-    const uint32_t body = (a.vocab - head) / kPer, odd = a.vocab - body * kPer;
-    const uint32_t v0 = (uint32_t)((uint64_t)body * rank / split), v1 = (uint32_t)((uint64_t)body * (rank + 1) / split);
-    const uint4 *zv = reinterpret_cast<const uint4 *>(z + head);
-    const bool has_odd = worker && rank == 0 && tid < odd;
-    const uint32_t odd_at = tid < head ? tid : body * kPer + tid;
-    const bool keeps = v1 - v0 <= kWorkers * kVectors;  // the row stays in registers
-    uint4 x[kVectors];
-    float x_odd = -kInf;
-    auto load = [&](uint32_t at) {
-#pragma unroll
-      for (int i = 0; i < kVectors; ++i) {
-        const uint32_t v = at + i * kWorkers + tid;
-        x[i] = v < v1 ? __ldcs(zv + v) : nothing<T>();
-      }
-    };
-    if (worker) {
-      load(v0);
-      if (has_odd) x_odd = to_float(z[odd_at]);
+  if (tid == 0) {
+    for (uint32_t i = 0; i < kChunks; ++i) mbar_init(&sh.full[i], 1), mbar_init(&sh.empty[i], kWarps);
+    for (int i = 0; i <= kTeachers; ++i) mbar_init(&sh.peer_full[i], 1);
+    sh.dead = 0;
+    uint8_t *entries = reinterpret_cast<uint8_t *>(tables + (layout.teachers << layout.slots_log2));
+    for (uint32_t i = 0; i <= layout.teachers; ++i, entries += layout.room * 12) {
+      sh.e[i].id = reinterpret_cast<int32_t *>(entries);
+      sh.e[i].p = reinterpret_cast<float *>(entries + layout.room * 4);
+      sh.e[i].z = reinterpret_cast<float *>(entries + layout.room * 8);
     }
-    Sum sum = {-kInf, 0.0f, 0.0f};
-    if (kLoss) {
-      if (worker) {
-        sum.m = x_odd;
-        for (uint32_t at = v0;;) {
-          const float m = fmaxf(sum.m, largest<T>(x));
-          if (at != v0) {
-            sum.s = moved(sum.s, sum.m, m, a.scale2);
-            if (TWO) sum.s1 = moved(sum.s1, sum.m, m, kLog2e);
+    mbar_init_fence();
+    if (together)
+      for (uint32_t i = 0; i <= layout.teachers; ++i) mbar_arrive_expect_tx(&sh.peer_full[i], split * 12);
+  }
+  __syncthreads();
+  if (together) cluster_arrive(), cluster_wait();  // the barriers are there before anyone sends
+
+  // Vectors [v0, v1) of a row's 16-byte aligned body are this CTA's; the elements
+  // outside the body are the first CTA's.
+  struct Part {
+    const T *z;
+    uint32_t head, body, v0, v1, chunks;
+    bool keeps;  // the ring holds the part: loss and gradient share one copy
+  };
+  auto part_of = [&](uint32_t row) {
+    Part p;
+    p.z = static_cast<const T *>(a.logits) + (int64_t)row * a.pitch;
+    p.head = min(a.vocab, (uint32_t)((16 - (uintptr_t)p.z % 16) % 16 / sizeof(T)));
+    p.body = (a.vocab - p.head) / kPer;
+    p.v0 = (uint32_t)((uint64_t)p.body * rank / split), p.v1 = (uint32_t)((uint64_t)p.body * (rank + 1) / split);
+    p.chunks = (p.v1 - p.v0 + kChunk - 1) / kChunk;
+    p.keeps = p.chunks <= kChunks;
+    return p;
+  };
+
+  if (warp == kWarps + kTeachers) {
+    // copies
+    if (lane == 0) {
+      const uint64_t policy = l2_evict_first();
+      uint32_t use = 0;
+      for (uint32_t row = first; row < a.rows; row += step) {
+        const Part p = part_of(row);
+        for (int sweep = 0; sweep < (FORM == 3 && !p.keeps ? 2 : 1); ++sweep)
+          for (uint32_t c = 0; c < p.chunks; ++c, ++use) {
+            const uint32_t s = use % kChunks, from = p.v0 + c * kChunk, bytes = min((uint32_t)kChunk, p.v1 - from) * 16;
+            if (use >= kChunks) wait(&sh.empty[s], (use / kChunks + 1) & 1, sh, a.status);
+            if (*(volatile int32_t *)&sh.dead) goto drain;
+            mbar_arrive_expect_tx(&sh.full[s], bytes);
+            bulk_g2s(ring + s * kChunk, reinterpret_cast<const uint4 *>(p.z + p.head) + from, bytes, &sh.full[s], policy);
           }
-          sum.m = m;
-          const float from = reference(m);
-          const uint64_t minus = pack2(-from, -from), scale = pack2(a.scale2, a.scale2), scale1 = pack2(kLog2e, kLog2e);
-          if (at == v0 && has_odd) {
-            sum.s += exp2_approx((x_odd - from) * a.scale2);
-            if (TWO) sum.s1 += exp2_approx((x_odd - from) * kLog2e);
+      }
+    drain:
+      if (*(volatile int32_t *)&sh.dead)
+        for (uint32_t u = use > kChunks ? use - kChunks : 0; u < use; ++u) wait_for(&sh.full[u % kChunks], u / kChunks & 1);
+    }
+  } else if (warp < kWarps + layout.teachers) {
+    // Row i is teacher i's (modulo their number).  It meets the workers at a barrier
+    // of its own when its entries are there and their sums are, and then goes on to
+    // the entries of row i + teachers.  Entries, sums and the cluster's sums have one
+    // place more than there are teachers: at row i's barrier everyone is through
+    // with row i - 1 but its own teacher, who is with row i - 1 + teachers.
+    const bool worker = warp < kWarps;
+    const uint32_t teachers = layout.teachers, own = worker ? 0 : warp - kWarps;
+    int32_t *table = tables + (own << layout.slots_log2);
+    uint32_t use = 0, done = own;
+    if (!worker && first + (uint64_t)own * step < a.rows)
+      teacher_entries<T>(a, first + own * step, sh.e[own], table, layout.slots_log2, lane);
+    for (uint64_t row = first + (uint64_t)own * step; row < a.rows; row += worker ? step : (uint64_t)step * teachers, done += worker ? 1 : teachers) {
+      const uint32_t turn = done % (teachers + 1), round = done / (teachers + 1), barrier = 2 + done % teachers;
+      const Part p = part_of(row);
+      const uint32_t odd = a.vocab - p.body * kPer;
+      const bool has_odd = worker && rank == 0 && tid < odd;
+      const uint32_t odd_at = tid < p.head ? tid : p.body * kPer + tid;
+      const float x_odd = has_odd ? to_float(p.z[odd_at]) : -kInf;
+      Sum sum = {x_odd, 0.0f, 0.0f};
+      if (kLoss) {
+        if (worker) {
+          if (has_odd) {
+            sum.s = exp2_approx((x_odd - reference(x_odd)) * a.scale2);
+            if (TWO) sum.s1 = exp2_approx((x_odd - reference(x_odd)) * kLog2e);
           }
-          uint64_t part = 0, part1 = 0;
+          const uint64_t scale = pack2(a.scale2, a.scale2), scale1 = pack2(kLog2e, kLog2e);
+          uint64_t parts = pack2(sum.s, 0.0f), parts1 = pack2(sum.s1, 0.0f);
+          for (uint32_t c = 0; c < p.chunks; ++c) {
+            const uint32_t s = (use + c) % kChunks, n = p.v1 - p.v0 - c * kChunk;
+            wait(&sh.full[s], (use + c) / kChunks & 1, sh, a.status);
+            uint4 x[kVectors];
+            const uint4 *from = ring + s * kChunk + tid;
+            if (n >= kChunk) {
 #pragma unroll
-          for (int i = 0; i < kVectors; ++i) {
+              for (int i = 0; i < kVectors; ++i) x[i] = from[i * kWorkers];
+            } else {
 #pragma unroll
-            for (int j = 0; j < 8 / (int)sizeof(T); ++j) {
-              const uint64_t y = add2(pair<T>(x[i], j), minus);
-              part = add2(part, exp2_pair(mul2(y, scale)));
-              if (TWO) part1 = add2(part1, exp2_pair(mul2(y, scale1)));
+              for (int i = 0; i < kVectors; ++i) x[i] = i * kWorkers + tid < n ? from[i * kWorkers] : nothing<T>();
+            }
+            const float m = largest<T>(x);
+            if (m > sum.m) {  // the sums move to the new maximum
+              const uint64_t f = pack2(moved(1.0f, sum.m, m, a.scale2), moved(1.0f, sum.m, m, a.scale2));
+              parts = mul2(parts, f);
+              if (TWO) parts1 = mul2(parts1, pack2(moved(1.0f, sum.m, m, kLog2e), moved(1.0f, sum.m, m, kLog2e)));
+              sum.m = m;
+            }
+            const uint64_t minus = pack2(-reference(sum.m), -reference(sum.m));
+#pragma unroll
+            for (int i = 0; i < kVectors; ++i) {
+#pragma unroll
+              for (int j = 0; j < kPairs; ++j) {
+                const uint64_t y = add2(pair<T>(x[i], j), minus);
+                parts = add2(parts, exp2_pair(mul2(y, scale)));
+                if (TWO) parts1 = add2(parts1, exp2_pair(mul2(y, scale1)));
+              }
+            }
+            if (FORM == 1 || !p.keeps) {
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&sh.empty[s]);
             }
           }
-          const float2 u = unpack2(part), u1 = unpack2(part1);
-          sum.s += u.x + u.y;
-          if (TWO) sum.s1 += u1.x + u1.y;
-          at += kWorkers * kVectors;
-          if (at >= v1) break;
-          load(at);
+          if (FORM == 1 || !p.keeps) use += p.chunks;
+          const float2 u = unpack2(parts), u1 = unpack2(parts1);
+          sum.s = u.x + u.y;
+          if (TWO) sum.s1 = u1.x + u1.y;
+          sum = joined<TWO>(sum, a.scale2);
+          if (lane == 0) sh.part[turn][warp] = sum;
         }
+        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(kWorkers + 32) : "memory");
+        sum = lane < kWarps ? sh.part[turn][lane] : Sum{-kInf, 0.0f, 0.0f};
         sum = joined<TWO>(sum, a.scale2);
-        if (lane == 0) sh.part[turn][warp] = sum;
-      }
-      __syncthreads();
-      sum = joined<TWO>(sh.part[turn][lane % kWarps], a.scale2, kWarps);
-      if (together) {
-        if (tid < split) {
-          const uint32_t at = map_rank(smem_addr(&sh.peer[turn][rank]), tid);
-          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(sum.m) : "memory");
-          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(sum.s) : "memory");
-          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 8), "f"(sum.s1) : "memory");
-        }
-        cluster_arrive(), cluster_wait();
-        sum = sh.peer[turn][0];
-        for (uint32_t k = 1; k < split; ++k) join<TWO>(sum, sh.peer[turn][k], a.scale2);
-      }
-    } else {
-      __syncthreads();
-    }
-    const Entries &en = sh.e[turn];
-    const float from = reference(sum.m);
-    const float log_s = kLoss ? log2f(sum.s) : 0.0f, log_s1 = kLoss ? (TWO ? log2f(sum.s1) : log_s) : 0.0f;
-    if (!worker) {
-      // the row's loss, then the next row's entries
-      if (kLoss && rank == 0) {
-        const bool some = sum.m != -kInf || sum.s != 0.0f;
-        float cross = 0.0f;
-        for (uint32_t i = lane; i < a.k; i += 32)
-          if (en.p[i] != 0.0f) cross = __fmaf_rn(en.p[i], (en.z[i] - from) * a.scale2 - log_s, cross);
-        for (int o = 16; o; o >>= 1) cross += __shfl_xor_sync(~0u, cross, o);
-        if (lane == 0) {
-          float loss = a.loss_kd * __fmaf_rn(-kLn2, cross, en.entropy);
-          if (en.id[a.k] >= 0 && a.loss_label != 0.0f) loss -= a.loss_label * kLn2 * ((en.z[a.k] - from) * kLog2e - log_s1);
-          a.loss[row] = some ? loss : 0.0f;
-          a.lse[row] = some ? __fmaf_rn(from, a.inv_tau, log_s * kLn2) : -kInf;
-          if (a.labels) a.lse[(int64_t)a.rows + row] = some ? __fmaf_rn(log_s1, kLn2, from) : -kInf;
-        }
-      }
-      if (row + step < a.rows) teacher_entries<T>(a, row + step, sh.e[turn ^ 1], sh.slot, lane);
-      continue;
-    }
-    if (!kGrad) continue;
-    const float g = a.grad_loss[row];
-    const bool label = en.id[a.k] >= 0;
-    float c0 = g * a.grad_kd * en.p_sum, c1 = label ? g * a.loss_label : 0.0f, l = 0.0f, l1 = 0.0f;
-    bool live = g != 0.0f;
-    if (kLoss) {
-      live = live && (sum.m != -kInf || sum.s != 0.0f);
-      c0 /= sum.s, c1 /= TWO ? sum.s1 : sum.s;
-    } else {
-      l = a.lse[row];
-      if (a.labels) l1 = a.lse[(int64_t)a.rows + row];
-      live = live && l != -kInf;
-    }
-    if (!TWO) c0 += c1;  // one temperature for both
-    // Both temperatures' parts, without the entries': c 2^((z times + plus) scale),
-    // from the row's own maximum and sums or from the given logarithms.
-    const float times = kLoss ? 1.0f : a.inv_tau, plus = kLoss ? -from : -l, plus1 = kLoss ? -from : -l1;
-    const float scale = kLoss ? a.scale2 : kLog2e;
-    const uint64_t times2 = pack2(times, times), plus2 = pack2(plus, plus), plus12 = pack2(plus1, plus1);
-    const uint64_t scale2 = pack2(scale, scale), scale12 = pack2(kLog2e, kLog2e), c02 = pack2(c0, c0), c12 = pack2(c1, c1);
-    auto whole2 = [&](uint64_t y) {
-      const uint64_t t = kLoss ? add2(y, plus2) : fma2(y, times2, plus2);
-      const uint64_t q = mul2(c02, exp2_pair(mul2(t, scale2)));
-      return TWO ? fma2(c12, exp2_pair(mul2(kLoss ? t : add2(y, plus12), scale12)), q) : q;
-    };
-    auto whole = [&](float y) { return unpack2(whole2(pack2(y, y))).x; };
-    T *d = static_cast<T *>(a.dlogits) + (int64_t)row * a.dpitch;
-    auto put = [&](uint32_t at, uint32_t i, uint4 v) {
-      const uint32_t k = at + i * kWorkers + tid;
-      if (k >= v1) return;
-      if (alike) {
-        __stcs(reinterpret_cast<uint4 *>(d + head) + k, v);
-      } else {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        for (int j = 0; j < kPer; ++j) {
-          if constexpr (sizeof(T) == 4) d[head + k * kPer + j] = __uint_as_float(w[j]);
-          else reinterpret_cast<uint16_t *>(d)[head + k * kPer + j] = (uint16_t)(w[j / 2] >> (j % 2 * 16));
-        }
-      }
-    };
-    if (!live) {
-      for (uint32_t at = v0; at < v1; at += kWorkers * kVectors)
-        for (int i = 0; i < kVectors; ++i) put(at, i, make_uint4(0, 0, 0, 0));
-      if (has_odd) d[odd_at] = from_float<T>(0.0f);
-    } else {
-      if (kLoss && !keeps) load(v0);
-      if (kLoss) forget(x);
-      for (uint32_t at = v0;;) {
-#pragma unroll
-        for (int i = 0; i < kVectors; ++i) put(at, i, map<T>(x[i], whole2));
-        at += kWorkers * kVectors;
-        if (at >= v1) break;
-        load(at);
-      }
-      if (has_odd) d[odd_at] = from_float<T>(whole(x_odd));
-    }
-    asm volatile("bar.sync 1, %0;" ::"n"(kWorkers) : "memory");  // the row is written but for its entries
-    if (!live) continue;
-    for (uint32_t i = tid; i <= a.k; i += kWorkers) {
-      const int32_t id = en.id[i];
-      if (id < 0) continue;
-      // whoever wrote the place writes it again
-      const uint32_t v = ((uint32_t)id - head) / kPer;
-      const bool mine = (uint32_t)id < head || v >= body ? rank == 0 : v >= v0 && v < v1;
-      if (!mine) continue;
-      float take = i == a.k ? a.loss_label : a.grad_kd * en.p[i];
-      bool first_one = true;
-      if (en.same) {
-        take = 0.0f;
-        for (uint32_t j = 0; j <= a.k; ++j)
-          if (en.id[j] == id) {
-            first_one = first_one && j >= i;
-            take += j == a.k ? a.loss_label : a.grad_kd * en.p[j];
+        if (together) {
+          if (tid < split) {
+            const uint32_t at = map_rank(smem_addr(&sh.peer[turn][rank]), tid), bar = map_rank(smem_addr(&sh.peer_full[turn]), tid);
+            store_async(at, sum.m, bar), store_async(at + 4, sum.s, bar), store_async(at + 8, sum.s1, bar);
           }
+          wait(&sh.peer_full[turn], round & 1, sh, a.status);
+          asm volatile("fence.acq_rel.cluster;" ::: "memory");
+          if (tid == 0) mbar_arrive_expect_tx(&sh.peer_full[turn], split * 12);  // for the next round
+          sum = sh.peer[turn][0];
+          for (uint32_t k = 1; k < split; ++k) join<TWO>(sum, sh.peer[turn][k], a.scale2);
+        }
+      } else {
+        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(kWorkers + 32) : "memory");
       }
-      if (first_one) d[id] = from_float<T>(__fmaf_rn(-g, take, whole(en.z[i])));
+      const Entries &en = sh.e[turn];
+      const float from = reference(sum.m);
+      if (!worker) {
+        // the row's loss, then the next row's entries
+        if (kLoss && rank == 0) {
+          const float log_s = log2f(sum.s), log_s1 = TWO ? log2f(sum.s1) : log_s;
+          const bool some = sum.m != -kInf || sum.s != 0.0f;
+          float cross = 0.0f;
+          for (uint32_t i = lane; i < a.k; i += 32)
+            if (en.p[i] != 0.0f) cross = __fmaf_rn(en.p[i], (en.z[i] - from) * a.scale2 - log_s, cross);
+          for (int o = 16; o; o >>= 1) cross += __shfl_xor_sync(~0u, cross, o);
+          if (lane == 0) {
+            float loss = a.loss_kd * __fmaf_rn(-kLn2, cross, en.entropy);
+            if (en.id[a.k] >= 0 && a.loss_label != 0.0f) loss -= a.loss_label * kLn2 * ((en.z[a.k] - from) * kLog2e - log_s1);
+            a.loss[row] = some ? loss : 0.0f;
+            a.lse[row] = some ? __fmaf_rn(from, a.inv_tau, log_s * kLn2) : -kInf;
+            if (a.labels) a.lse[(int64_t)a.rows + row] = some ? __fmaf_rn(log_s1, kLn2, from) : -kInf;
+          }
+        }
+        if (row + (uint64_t)step * teachers < a.rows)
+          teacher_entries<T>(a, (uint32_t)(row + (uint64_t)step * teachers), sh.e[(done + teachers) % (teachers + 1)], table, layout.slots_log2, lane);
+        continue;
+      }
+      if (!kGrad) continue;
+      const float g = a.grad_loss[row];
+      float c0 = g * a.grad_kd * en.p_sum, c1 = en.id[a.k] >= 0 ? g * a.loss_label : 0.0f, l = 0.0f, l1 = 0.0f;
+      bool live = g != 0.0f;
+      if (kLoss) {
+        live = live && (sum.m != -kInf || sum.s != 0.0f);
+        c0 /= sum.s, c1 /= TWO ? sum.s1 : sum.s;
+      } else {
+        l = a.lse[row];
+        if (a.labels) l1 = a.lse[(int64_t)a.rows + row];
+        live = live && l != -kInf;
+      }
+      if (!TWO) c0 += c1;  // one temperature for both
+      // Both temperatures' parts, without the entries': c 2^((z times + plus) scale),
+      // from the row's own maximum and sums or from the given logarithms.
+      const float times = kLoss ? 1.0f : a.inv_tau, plus = kLoss ? -from : -l, plus1 = kLoss ? -from : -l1;
+      const float scale = kLoss ? a.scale2 : kLog2e;
+      const uint64_t times2 = pack2(times, times), plus2 = pack2(plus, plus), plus12 = pack2(plus1, plus1);
+      const uint64_t scale2 = pack2(scale, scale), scale12 = pack2(kLog2e, kLog2e), c02 = pack2(c0, c0), c12 = pack2(c1, c1);
+      auto whole2 = [&](uint64_t y) {
+        const uint64_t t = kLoss ? add2(y, plus2) : fma2(y, times2, plus2);
+        const uint64_t q = mul2(c02, exp2_pair(mul2(t, scale2)));
+        return TWO ? fma2(c12, exp2_pair(mul2(kLoss ? t : add2(y, plus12), scale12)), q) : q;
+      };
+      auto whole = [&](float y) { return unpack2(whole2(pack2(y, y))).x; };
+      T *d = static_cast<T *>(a.dlogits) + (int64_t)row * a.dpitch;
+      for (uint32_t c = 0; c < p.chunks; ++c, ++use) {
+        const uint32_t s = use % kChunks, at = p.v0 + c * kChunk;
+        wait(&sh.full[s], use / kChunks & 1, sh, a.status);
+        const uint4 *x = ring + s * kChunk + tid;
+        if (alike && live && p.v1 - at >= kChunk) {
+          uint4 *to = reinterpret_cast<uint4 *>(d + p.head) + at + tid;
+#pragma unroll
+          for (int i = 0; i < kVectors; ++i) __stcs(to + i * kWorkers, map<T>(x[i * kWorkers], whole2));
+        } else {
+          for (int i = 0; i < kVectors; ++i) {
+            const uint32_t k = at + i * kWorkers + tid;
+            if (k >= p.v1) break;
+            const uint4 v = live ? map<T>(x[i * kWorkers], whole2) : make_uint4(0, 0, 0, 0);
+            if (alike) {
+              __stcs(reinterpret_cast<uint4 *>(d + p.head) + k, v);
+            } else {
+              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int j = 0; j < kPer; ++j) {
+                if constexpr (sizeof(T) == 4) d[p.head + (int64_t)k * kPer + j] = __uint_as_float(w[j]);
+                else reinterpret_cast<uint16_t *>(d)[p.head + (int64_t)k * kPer + j] = (uint16_t)(w[j / 2] >> (j % 2 * 16));
+              }
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.empty[s]);
+      }
+      if (has_odd) d[odd_at] = from_float<T>(live ? whole(x_odd) : 0.0f);
+      asm volatile("bar.sync 1, %0;" ::"n"(kWorkers) : "memory");  // the row is written but for its entries
+      if (!live) continue;
+      for (uint32_t i = tid; i <= a.k; i += kWorkers) {
+        const int32_t id = en.id[i];
+        if (id < 0) continue;
+        // whoever wrote the place writes it again
+        const uint32_t v = ((uint32_t)id - p.head) / kPer;
+        if (!((uint32_t)id < p.head || v >= p.body ? rank == 0 : v >= p.v0 && v < p.v1)) continue;
+        float take = i == a.k ? a.loss_label : a.grad_kd * en.p[i];
+        bool first_one = true;
+        if (en.same) {
+          take = 0.0f;
+          for (uint32_t j = 0; j <= a.k; ++j)
+            if (en.id[j] == id) {
+              first_one = first_one && j >= i;
+              take += j == a.k ? a.loss_label : a.grad_kd * en.p[j];
+            }
+        }
+        if (first_one) d[id] = from_float<T>(__fmaf_rn(-g, take, whole(en.z[i])));
+      }
     }
   }
+  __syncwarp();
   if (together) cluster_arrive(), cluster_wait();  // nobody writes to a CTA that has left
 }
 
 }  // namespace
 
-int distill_per_sm(const DistillArgs &a) { return residents((a.loss ? 1 : 0) | (a.dlogits ? 2 : 0)); }
+int distill_per_sm(const DistillArgs &) { return kCtas; }
 
-int launch_distill(const DistillArgs &a, unsigned cap, unsigned sms, void *stream) {
+int launch_distill(const DistillArgs &args, unsigned cap, unsigned sms, void *stream) {
+  DistillArgs a = args;
+  const int e = commit_status_word(&a.status);
+  if (e) return e;
   return with_dtype(a.dtype, [&](auto t) {
     using T = decltype(t);
     const uint32_t size = sizeof(T), body = a.vocab / (16 / size);
+    Layout l = {};
+    l.teachers = a.k <= 256 ? kTeachers : a.k <= 512 ? (kTeachers + 1) / 2 : 1;
+    l.room = (a.k + 1 + 3) / 4 * 4;
+    l.slots_log2 = 6;
+    while ((1u << l.slots_log2) < 2 * (a.k + 1)) ++l.slots_log2;
+    constexpr uint32_t kRoom = 227 * 1024 / kCtas - 1024;
+    l.chunks = std::min((uint32_t)kMaxChunks, (kRoom - l.bytes()) / (kChunk * 16));
     // a row over more CTAs while they would not fill the GPU, or while its parts do
-    // not fit the registers, but not into parts of less than two vectors a thread
+    // not fit the ring, but not into parts of less than two chunks
     uint32_t split = 1;
-    while (split < (uint32_t)kMaxSplit && body / (2 * split) >= 2 * kWorkers &&
-           ((uint64_t)a.rows * split <= sms || (a.loss && a.dlogits && body > split * kWorkers * kKeep)))
+    while (split < (uint32_t)kMaxSplit && body / (2 * split) >= 2 * kChunk &&
+           ((uint64_t)a.rows * split <= sms || (a.loss && a.dlogits && body > split * l.chunks * kChunk)))
       split *= 2;
     const uint64_t most = cap >= split ? cap / split : 1;
     const unsigned grid = (unsigned)(a.rows < most ? a.rows : most) * split;
     const bool alike = a.dlogits && ((uintptr_t)a.dlogits - (uintptr_t)a.logits) % 16 == 0 && (a.dpitch - a.pitch) * size % 16 == 0;
     const bool two = a.labels && a.inv_tau != 1.0f;
     auto go = [&](auto kernel, bool cluster) {
-      int e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared));
+      int e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)l.bytes());
       if (e) return e;
       cudaLaunchAttribute attr = {};
       attr.id = cudaLaunchAttributeClusterDimension;
@@ -497,11 +616,11 @@ int launch_distill(const DistillArgs &a, unsigned cap, unsigned sms, void *strea
       cudaLaunchConfig_t cfg = {};
       cfg.gridDim = dim3(grid);
       cfg.blockDim = dim3(kThreads);
-      cfg.dynamicSmemBytes = sizeof(Shared);
+      cfg.dynamicSmemBytes = l.bytes();
       cfg.stream = (cudaStream_t)stream;
       cfg.attrs = &attr;
       cfg.numAttrs = cluster && split > 1 ? 1 : 0;
-      return (int)cudaLaunchKernelEx(&cfg, kernel, a, split, alike);
+      return (int)cudaLaunchKernelEx(&cfg, kernel, a, l, split, alike);
     };
     if (!a.dlogits) return two ? go(distill_kernel<T, 1, true>, true) : go(distill_kernel<T, 1, false>, true);
     if (!a.loss) return two ? go(distill_kernel<T, 2, true>, false) : go(distill_kernel<T, 2, false>, false);

@@ -40,7 +40,7 @@ struct ProductPlan {
 };
 
 // A whole warp's wait: its lanes give up together.
-__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity) { return __all_sync(~0u, mbar_wait(bar, parity)); }
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity) { return __all_sync(~0u, wait_for(bar, parity)); }
 
 __device__ __forceinline__ void give_up(unsigned *status) { atomicOr(status, (unsigned)APC_ETIMEOUT); }
 
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
       }
       if (!ok) {  // let the copies in flight land
         give_up(p.status);
-        for (uint32_t u = use > S::kStages ? use - S::kStages : 0; u < use; ++u) mbar_wait(&full[u % S::kStages], u / S::kStages & 1);
+        for (uint32_t u = use > S::kStages ? use - S::kStages : 0; u < use; ++u) wait_for(&full[u % S::kStages], u / S::kStages & 1);
       }
     }
   } else if (warp == 1) {
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
         }
       if (!ok) {  // let the products in flight end
         give_up(p.status);
-        for (uint32_t u = use > 2 ? use - 2 : 0; u < use; ++u) mbar_wait(&acc_full[u & 1], u / 2 & 1);
+        for (uint32_t u = use > 2 ? use - 2 : 0; u < use; ++u) wait_for(&acc_full[u & 1], u / 2 & 1);
       }
     }
   } else {
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
         continue;
       }
       // a share to each CTA of the cluster, once it has read the tile before
-      if (done) ok = __all_sync(~0u, mbar_wait_cluster(&recv_free, (done + 1) & 1));
+      if (done) ok = __all_sync(~0u, wait_for_cluster(&recv_free, (done + 1) & 1));
       if (!ok) break;
       const uint32_t per_log2 = kLog2Bn - split_log2, per = 1u << per_log2;  // columns that a CTA owns
       const uint32_t mine = smem_addr(recv) + (rank * per * 128 + row) * 4, bar = smem_addr(&recv_full);
@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
         const uint32_t owner = (uint32_t)i >> per_log2;
         store_async(map_rank(mine + (i & (per - 1)) * 512, owner), i % 2 ? v.y : v.x, map_rank(bar, owner));
       }
-      ok = __all_sync(~0u, mbar_wait_cluster(&recv_full, done & 1));
+      ok = __all_sync(~0u, wait_for_cluster(&recv_full, done & 1));
       if (!ok) break;
       if (threadIdx.x == 64) mbar_arrive_expect_tx(&recv_full, S::kRecvBytes);
       for (uint32_t c = 0; c < per; ++c) {
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
     }
     if (!ok) {
       give_up(p.status);
-      if (split > 1) mbar_wait_cluster(&recv_full, done & 1);  // let the shares in flight land
+      if (split > 1) wait_for_cluster(&recv_full, done & 1);  // let the shares in flight land
     }
   }
   __syncwarp();
@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
       if (!ok) {  // let the copies in flight land, the other CTA's too
         give_up(p.status);
         if (rank == 0)
-          for (uint32_t u = use > kBigStages ? use - kBigStages : 0; u < use; ++u) mbar_wait(&full[u % kBigStages], u / kBigStages & 1);
+          for (uint32_t u = use > kBigStages ? use - kBigStages : 0; u < use; ++u) wait_for(&full[u % kBigStages], u / kBigStages & 1);
         const uint64_t t0 = global_ns();
         for (uint32_t i = 0; i < kWaitIterations && global_ns() - t0 < 1000000; ++i) __nanosleep(1000);
       }
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
       if (!ok) {  // let the products in flight end
         give_up(p.status);
         for (uint32_t u = use > 2 ? use - 2 : 0; u < use; ++u)
-          for (int h = 0; h < kBigUnits; ++h) mbar_wait(&acc_full[2 * h + (u & 1)], u / 2 & 1);
+          for (int h = 0; h < kBigUnits; ++h) wait_for(&acc_full[2 * h + (u & 1)], u / 2 & 1);
       }
     }
   } else {

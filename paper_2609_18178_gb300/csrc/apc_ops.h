@@ -81,6 +81,7 @@ struct DistillArgs {
   float scale2;              // log2(e)/tau
   float loss_kd, loss_label; // kd_weight*tau^2, label_weight
   float grad_kd;             // kd_weight*tau
+  unsigned *status;          // the device status word
 };
 
 int launch_distill(const DistillArgs &a, unsigned cap, unsigned sms, void *stream);

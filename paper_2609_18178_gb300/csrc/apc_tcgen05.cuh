@@ -59,27 +59,28 @@ __device__ __forceinline__ void store_async(uint32_t mapped, float v, uint32_t m
                : "memory");
 }
 
-__device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-
-// mbar_wait for a barrier on which other CTAs of the cluster arrive.
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t *bar, uint32_t parity) {
-  const uint32_t a = smem_addr(bar);
-  if (try_wait_cluster(a, parity)) return true;
-  const uint64_t t0 = global_ns();
+// mbar_wait with the clock read only once a wait is a long one: the loops here
+// wait for a few hundred cycles again and again, and reading %globaltimer takes
+// longer than that.
+__device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity) {
+  uint64_t t0 = 0;
   for (uint32_t it = 1;; ++it) {
-    if (try_wait_cluster(a, parity)) return true;
+    if (mbar_try_wait(bar, parity)) return true;
+    if (it == 1024) t0 = global_ns();
     if (it >= kWaitIterations && (it & 1023u) == 0 && global_ns() - t0 > kWaitNanoseconds) return false;
   }
+}
+
+__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity) {
+  const uint32_t a = smem_addr(bar);
+  return mbar_try_wait(a, parity) || mbar_try_wait(a, parity) || wait_long(a, parity);
+}
+
+// wait_for what other CTAs of the cluster stored.
+__device__ __forceinline__ bool wait_for_cluster(uint64_t *bar, uint32_t parity) {
+  const bool ok = wait_for(bar, parity);
+  asm volatile("fence.acq_rel.cluster;" ::: "memory");
+  return ok;
 }
 
 // ---- TMA: a box of a matrix of bytes at column x (a multiple of 16), row y.
