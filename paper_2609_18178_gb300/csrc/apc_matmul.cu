@@ -12,7 +12,10 @@
 //
 // Two kernels, warp-specialized alike: one warp issues TMA loads into a ring of
 // shared-memory stages (128 bytes of k a row, 128-byte swizzle, zeros beyond
-// the edges), one thread issues the products, the others add up.
+// the edges), one copies the blocks' scales into a ring of their own, one thread
+// issues the products, the others add up.  (With the scales loaded by the adding
+// warps a block ahead, each block took a trip to memory: 1,600 cycles for
+// few columns, 900 for large products.)
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
@@ -44,148 +47,160 @@ __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity) { retu
 
 __device__ __forceinline__ void give_up(unsigned *status) { atomicOr(status, (unsigned)APC_ETIMEOUT); }
 
+constexpr int kScaleSlots = 8;  // blocks whose scales are on their way or in use
+
 // ---------------------------------------------------------------------------
 // The kernel for few columns: 128 rows of the wide operand (a weight's outputs)
 // on the lanes, BN columns (tokens) beside them.
 //
 // The k blocks of a tile are split evenly over a cluster's CTAs, so that few
-// tiles still keep all SMs loading: each CTA sums its share in registers, then
-// sends every CTA the columns that it owns (st.async into its shared memory,
-// counted by an mbarrier), and the owner adds the shares in the order of their
+// tiles still keep all SMs loading: each CTA sums its share in registers, leaves it
+// in shared memory and sends every CTA the columns that it owns (one bulk copy
+// each, counted by an mbarrier); the owner adds the shares in the order of their
 // ranks and stores.  The loads of the next tile run meanwhile.
-constexpr int kMidThreads = 192;
+//
+// A wait that gives up marks the CTA dead: it stops loading and issuing, waits for
+// what is in flight, and its sums go on without waiting, so that every barrier is
+// reached.
+constexpr int kMidThreads = 224;
 
-template <int BN>
+template <int BN, bool SPLIT>
 struct MidShape {
   static constexpr int kRowBytes = 128 * kBlock, kColBytes = BN * kBlock;
   static constexpr int kStageBytes = kRowBytes + kColBytes;
-  static constexpr int kRecvBytes = BN * 128 * 4;
-  static constexpr int kStages = (200 * 1024 - kRecvBytes) / kStageBytes > 12 ? 12 : (200 * 1024 - kRecvBytes) / kStageBytes;
-  static constexpr int kScaleBytes = 4 * 2 * BN * 4;
-  static constexpr int kBytes = 1024 + kStages * kStageBytes + kRecvBytes + kScaleBytes;
-  static constexpr int kTmem = 2 * BN < 32 ? 32 : 2 * BN;
+  static constexpr int kShareBytes = SPLIT ? BN * 128 * 4 : 0;
+  static constexpr int kScaleBytes = kScaleSlots * (128 + BN) * 4;
+  static constexpr int kRoom = 224 * 1024 - 2 * kShareBytes - kScaleBytes;
+  static constexpr int kStages = kRoom / kStageBytes > 12 ? 12 : kRoom / kStageBytes;
+  static constexpr int kBytes = 1024 + kStages * kStageBytes + 2 * kShareBytes + kScaleBytes;
+  // accumulators: a block's way from its products through the sums and back takes
+  // many times as long as either
+  static constexpr int kAcc = 512 / BN < 8 ? 512 / BN : 8;
+  static constexpr int kTmem = kAcc * BN;
 };
 
-template <int BN, typename T>
+template <int BN, bool SPLIT, typename T>
 __global__ void __launch_bounds__(kMidThreads, 1)
     mid_kernel(const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_c,
                const __grid_constant__ ProductPlan p, const uint32_t split_log2) {
-  using S = MidShape<BN>;
+  using S = MidShape<BN, SPLIT>;
   constexpr int kLog2Bn = BN == 16 ? 4 : BN == 32 ? 5 : BN == 64 ? 6 : 7;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[S::kStages], empty[S::kStages], acc_full[2], acc_empty[2], recv_full, recv_free;
+  __shared__ uint64_t full[S::kStages], empty[S::kStages], acc_full[S::kAcc], acc_empty[S::kAcc], recv_full, recv_free;
+  __shared__ uint64_t scale_full[kScaleSlots], scale_empty[kScaleSlots];
   __shared__ uint32_t tmem_at;
+  __shared__ volatile int32_t dead;
   uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  float *recv = reinterpret_cast<float *>(smem + S::kStages * S::kStageBytes);
-  float *scales = recv + S::kRecvBytes / 4;
+  float *share = reinterpret_cast<float *>(smem + S::kStages * S::kStageBytes);  // [column][row]
+  float *recv = share + S::kShareBytes / 4;                                       // [rank][own column][row]
+  float *scales = recv + S::kShareBytes / 4;                                     // [slot][128 rows, BN columns]
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const uint32_t split = 1u << split_log2;
-  const uint32_t rank = split > 1 ? cluster_rank() : 0;
+  const uint32_t split = SPLIT ? 1u << split_log2 : 1, rank = SPLIT ? cluster_rank() : 0;
   const uint32_t first = blockIdx.x / split, step = gridDim.x / split;
   const uint32_t tiles = p.row_tiles * p.col_tiles;
   const uint32_t b0 = (uint32_t)((uint64_t)p.blocks * rank / split), b1 = (uint32_t)((uint64_t)p.blocks * (rank + 1) / split);
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kStages; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
-    for (int i = 0; i < 2; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 4);
+    for (int i = 0; i < S::kAcc; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 4);
+    for (int i = 0; i < kScaleSlots; ++i) mbar_init(&scale_full[i], 32), mbar_init(&scale_empty[i], 4);
     mbar_init(&recv_full, 1);
     mbar_init(&recv_free, 4 * split);
+    dead = 0;
     mbar_init_fence();
   }
   if (warp == 1) tmem_alloc<1>(&tmem_at, S::kTmem);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (split > 1) cluster_arrive(), cluster_wait();  // the barriers are there before anyone sends
+  if (SPLIT) cluster_arrive(), cluster_wait();  // the barriers are there before anyone sends
   const uint32_t tmem = tmem_at;
+  // A whole warp's wait.
+  auto alive = [&](uint64_t *bar, uint32_t parity) {
+    bool ok = wait_for(bar, parity, &dead);
+    ok = __all_sync(~0u, ok);
+    if (!ok && !dead) {
+      dead = 1;
+      give_up(p.status);
+    }
+    return ok;
+  };
 
   if (warp == 0) {
-    {
-      uint32_t use = 0;
-      bool ok = true;
-      for (uint32_t t = first; t < tiles && ok; t += step) {
-        const int32_t r0 = (int32_t)(t % p.row_tiles) * 128, c0 = (int32_t)(t / p.row_tiles) * BN;
-        for (uint32_t b = b0; b < b1; ++b, ++use) {
-          const uint32_t st = use % S::kStages;
-          if (use >= S::kStages && !warp_wait(&empty[st], (use / S::kStages + 1) & 1)) {
-            ok = false;
-            break;
-          }
-          const uint32_t at = smem_addr(smem + st * S::kStageBytes), bar = smem_addr(&full[st]);
-          if (elect_one()) {
-            mbar_arrive_expect_tx(&full[st], S::kStageBytes);
-            load_box(at, &map_r, (int32_t)(b * kBlock), r0, bar);
-            load_box(at + S::kRowBytes, &map_c, (int32_t)(b * kBlock), c0, bar);
-          }
-          __syncwarp();
+    uint32_t use = 0;
+    bool ok = true;
+    for (uint32_t t = first; t < tiles && ok; t += step) {
+      const int32_t r0 = (int32_t)(t % p.row_tiles) * 128, c0 = (int32_t)(t / p.row_tiles) * BN;
+      for (uint32_t b = b0; b < b1; ++b, ++use) {
+        const uint32_t st = use % S::kStages;
+        if (use >= S::kStages && !(ok = alive(&empty[st], (use / S::kStages + 1) & 1))) break;
+        const uint32_t at = smem_addr(smem + st * S::kStageBytes), bar = smem_addr(&full[st]);
+        if (elect_one()) {
+          mbar_arrive_expect_tx(&full[st], S::kStageBytes);
+          load_box(at, &map_r, (int32_t)(b * kBlock), r0, bar);
+          load_box(at + S::kRowBytes, &map_c, (int32_t)(b * kBlock), c0, bar);
         }
-      }
-      if (!ok) {  // let the copies in flight land
-        give_up(p.status);
-        for (uint32_t u = use > S::kStages ? use - S::kStages : 0; u < use; ++u) wait_for(&full[u % S::kStages], u / S::kStages & 1);
+        __syncwarp();
       }
     }
+    if (!ok)  // let the copies in flight land
+      for (uint32_t u = use > S::kStages ? use - S::kStages : 0; u < use; ++u) wait_for(&full[u % S::kStages], u / S::kStages & 1);
   } else if (warp == 1) {
-    {
-      uint32_t use = 0;
-      bool ok = true;
-      for (uint32_t t = first; t < tiles && ok; t += step)
-        for (uint32_t b = b0; b < b1; ++b, ++use) {
-          const uint32_t st = use % S::kStages, buf = use & 1;
-          if ((use >= 2 && !warp_wait(&acc_empty[buf], (use / 2 + 1) & 1)) || !warp_wait(&full[st], use / S::kStages & 1)) {
-            ok = false;
-            break;
-          }
-          tc_fence_after();
-          const uint64_t dr = operand_desc(smem_addr(smem + st * S::kStageBytes));
-          const uint64_t dc = operand_desc(smem_addr(smem + st * S::kStageBytes + S::kRowBytes));
-          if (elect_one()) {
+    uint32_t use = 0;
+    bool ok = true;
+    for (uint32_t t = first; t < tiles && ok; t += step)
+      for (uint32_t b = b0; b < b1; ++b, ++use) {
+        const uint32_t st = use % S::kStages, buf = use % S::kAcc;
+        ok = (use < S::kAcc || alive(&acc_empty[buf], (use / S::kAcc + 1) & 1)) && alive(&full[st], use / S::kStages & 1);
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t dr = operand_desc(smem_addr(smem + st * S::kStageBytes));
+        const uint64_t dc = operand_desc(smem_addr(smem + st * S::kStageBytes + S::kRowBytes));
+        if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) mma_fp8<1>(tmem + buf * BN, dr + 2 * k, dc + 2 * k, p.instruction, k > 0);
-            mma_commit(&empty[st]);
-            mma_commit(&acc_full[buf]);
-          }
-          __syncwarp();
+          for (int k = 0; k < 4; ++k) mma_fp8<1>(tmem + buf * BN, dr + 2 * k, dc + 2 * k, p.instruction, k > 0);
+          mma_commit(&acc_full[buf]);
+          mma_commit(&empty[st]);
         }
-      if (!ok) {  // let the products in flight end
-        give_up(p.status);
-        for (uint32_t u = use > 2 ? use - 2 : 0; u < use; ++u) wait_for(&acc_full[u & 1], u / 2 & 1);
+        __syncwarp();
       }
+    if (!ok)  // let the products in flight end
+      for (uint32_t u = use > S::kAcc ? use - S::kAcc : 0; u < use; ++u) wait_for(&acc_full[u % S::kAcc], u / S::kAcc & 1);
+  } else if (warp == 6) {
+    uint32_t use = 0;
+    for (uint32_t t = first; t < tiles; t += step) {
+      const uint32_t r0 = t % p.row_tiles * 128 + lane, c0 = t / p.row_tiles * BN + lane;
+      for (uint32_t b = b0; b < b1; ++b, ++use) {
+        const uint32_t slot = use % kScaleSlots, at = smem_addr(scales + slot * (128 + BN) + lane);
+        if (use >= kScaleSlots && !alive(&scale_empty[slot], (use / kScaleSlots + 1) & 1)) break;
+        const float *rs = p.r_scale + b * p.r_scale_pitch, *cs = p.c_scale + b * p.c_scale_pitch;
+#pragma unroll
+        for (int i = 0; i < 128; i += 32) copy_word(at + i * 4, rs + (min(r0 + i, p.rows - 1) >> p.r_shift));
+#pragma unroll
+        for (int i = 0; i < BN; i += 32)
+          if (BN >= 32 || lane < BN) copy_word(at + (128 + i) * 4, cs + (min(c0 + i, p.cols - 1) >> p.c_shift));
+        arrive_with_words(&scale_full[slot]);
+      }
+      if (dead) break;
     }
+    words_landed();
   } else {
     const uint32_t quad = warp & 3, row = quad * 32 + lane;
-    float *sc = scales + (warp - 2) * 2 * BN;
     uint32_t use = 0, done = 0;
-    bool ok = true;
-    if (split > 1 && threadIdx.x == 64) mbar_arrive_expect_tx(&recv_full, S::kRecvBytes);
-    for (uint32_t t = first; t < tiles && ok; t += step, ++done) {
+    if (SPLIT && threadIdx.x == 64) mbar_arrive_expect_tx(&recv_full, S::kShareBytes);
+    for (uint32_t t = first; t < tiles; t += step, ++done) {
       const uint32_t r0 = t % p.row_tiles * 128, c0 = t / p.row_tiles * BN;
-      const uint32_t r = r0 + row < p.rows ? r0 + row : p.rows - 1;
-      constexpr int kPer = (BN + 31) / 32;
-      float next_c[kPer], next_r;
-      auto fetch = [&](uint32_t b) {
-        next_r = __ldg(p.r_scale + b * p.r_scale_pitch + (r >> p.r_shift));
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const uint32_t c = c0 + i * 32 + lane;
-          next_c[i] = (BN >= 32 || lane < BN) && c < p.cols ? __ldg(p.c_scale + b * p.c_scale_pitch + (c >> p.c_shift)) : 0.0f;
-        }
-      };
       uint64_t acc[BN / 2];
 #pragma unroll
       for (int i = 0; i < BN / 2; ++i) acc[i] = 0;
-      fetch(b0);
       for (uint32_t b = b0; b < b1; ++b, ++use) {
-        const uint32_t buf = use & 1;
-        float *s = sc + buf * BN;
-        const uint64_t sr = pack2(next_r, next_r);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-          if (BN >= 32 || lane < BN) s[i * 32 + lane] = next_c[i];
-        __syncwarp();
-        if (b + 1 < b1) fetch(b + 1);
-        ok = warp_wait(&acc_full[buf], use / 2 & 1);
-        if (!ok) break;
+        const uint32_t buf = use % S::kAcc;
+        const uint32_t slot = use % kScaleSlots;
+        const float *s = scales + slot * (128 + BN) + 128;
+        alive(&scale_full[slot], use / kScaleSlots & 1);
+        const float one = s[(int)row - 128];
+        const uint64_t sr = pack2(one, one);
+        alive(&acc_full[buf], use / S::kAcc & 1);
         tc_fence_after();
         const uint32_t at = tmem + buf * BN + (quad << 21);  // lane 32 * quad in bits 16 up
         constexpr int kChunk = BN < 32 ? 16 : 32;
@@ -206,33 +221,36 @@ __global__ void __launch_bounds__(kMidThreads, 1)
             acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), mul2(sr, v.y), acc[(c + i) / 2 + 1]);
           }
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&scale_empty[slot]);
       }
-      if (!ok) break;
       T *out = static_cast<T *>(p.out) + (int64_t)(r0 + row) * p.row_step;
       const bool in = r0 + row < p.rows;
-      if (split == 1) {
+      if (!SPLIT) {
 #pragma unroll
-        for (int i = 0; i < BN / 2; ++i) {
-          const float2 v = unpack2(acc[i]);
-          if (in && c0 + 2 * i < p.cols) out[(int64_t)(c0 + 2 * i) * p.col_step] = from_float<T>(v.x);
-          if (in && c0 + 2 * i + 1 < p.cols) out[(int64_t)(c0 + 2 * i + 1) * p.col_step] = from_float<T>(v.y);
+        for (int i = 0; i < BN; ++i) {
+          const float2 v = unpack2(acc[i / 2]);
+          if (in && c0 + i < p.cols) out[(int64_t)(c0 + i) * p.col_step] = from_float<T>(i % 2 ? v.y : v.x);
         }
         continue;
       }
-      // a share to each CTA of the cluster, once it has read the tile before
-      if (done) ok = __all_sync(~0u, wait_for_cluster(&recv_free, (done + 1) & 1));
-      if (!ok) break;
-      const uint32_t per_log2 = kLog2Bn - split_log2, per = 1u << per_log2;  // columns that a CTA owns
-      const uint32_t mine = smem_addr(recv) + (rank * per * 128 + row) * 4, bar = smem_addr(&recv_full);
+      // a share to each CTA of the cluster, once all have read the tile before
+      if (done) alive(&recv_free, (done + 1) & 1);
 #pragma unroll
       for (int i = 0; i < BN; ++i) {
         const float2 v = unpack2(acc[i / 2]);
-        const uint32_t owner = (uint32_t)i >> per_log2;
-        store_async(map_rank(mine + (i & (per - 1)) * 512, owner), i % 2 ? v.y : v.x, map_rank(bar, owner));
+        share[i * 128 + row] = i % 2 ? v.y : v.x;
       }
-      ok = __all_sync(~0u, wait_for_cluster(&recv_full, done & 1));
-      if (!ok) break;
-      if (threadIdx.x == 64) mbar_arrive_expect_tx(&recv_full, S::kRecvBytes);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      const uint32_t per = 1u << (kLog2Bn - split_log2);  // columns that a CTA owns
+      if (threadIdx.x - 64 < split) {
+        const uint32_t owner = threadIdx.x - 64;
+        bulk_s2s(map_rank(smem_addr(recv + rank * per * 128), owner), smem_addr(share + owner * per * 128), per * 512,
+                 map_rank(smem_addr(&recv_full), owner));
+      }
+      alive(&recv_full, done & 1);
+      if (threadIdx.x == 64) mbar_arrive_expect_tx(&recv_full, S::kShareBytes);
       for (uint32_t c = 0; c < per; ++c) {
         float sum = recv[c * 128 + row];
         for (uint32_t k = 1; k < split; ++k) sum += recv[(k * per + c) * 128 + row];
@@ -242,15 +260,12 @@ __global__ void __launch_bounds__(kMidThreads, 1)
       __syncwarp();
       if (lane < split) arrive_remote(map_rank(smem_addr(&recv_free), lane));
     }
-    if (!ok) {
-      give_up(p.status);
-      if (split > 1) wait_for_cluster(&recv_full, done & 1);  // let the shares in flight land
-    }
+    if (SPLIT && dead && done) wait_for(&recv_full, (done - 1) & 1);  // let the shares in flight land
   }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (split > 1) cluster_arrive(), cluster_wait();  // nobody sends to a CTA that has left
+  if (SPLIT) cluster_arrive(), cluster_wait();  // nobody sends to a CTA that has left
   tc_fence_after();
   if (warp == 1) tmem_free<1>(tmem, S::kTmem);
 }
@@ -278,7 +293,7 @@ constexpr int kBigThreads = 128 + 32 * kBigWarps, kBigStages = APC_BIG_STAGES;
 constexpr int kBigCols = 1024 / kBigWarps;  // columns that a warp adds up
 constexpr int kUnitCols = 256 / kBigUnits;
 constexpr int kBigHalf = 128 * kBlock, kBigStageBytes = 2 * kBigHalf;
-constexpr int kBigScaleBytes = kBigWarps * 2 * kBigCols * 4;
+constexpr int kBigScaleBytes = kScaleSlots * (128 + 256) * 4;
 constexpr int kBigBytes = 1024 + kBigStages * kBigStageBytes + kBigScaleBytes;
 constexpr uint32_t kBigGroup = 16;  // row tiles that are walked together
 
@@ -326,15 +341,17 @@ __global__ void __launch_bounds__(kBigThreads, 1)
                const __grid_constant__ ProductPlan p) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kBigStages], empty[kBigStages], acc_full[2 * kBigUnits], acc_empty[2 * kBigUnits];
+  __shared__ uint64_t scale_full[kScaleSlots], scale_empty[kScaleSlots];
   __shared__ uint32_t tmem_at;
   uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  float *scales = reinterpret_cast<float *>(smem + kBigStages * kBigStageBytes);
+  float *scales = reinterpret_cast<float *>(smem + kBigStages * kBigStageBytes);  // [slot][128 rows, 256 columns]
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, rank = cluster_rank();
   const uint32_t first = blockIdx.x / 2, step = gridDim.x / 2, tiles = p.row_tiles * p.col_tiles;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kBigStages; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
     for (int i = 0; i < 2 * kBigUnits; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 2 * kBigWarps / kBigUnits);
+    for (int i = 0; i < kScaleSlots; ++i) mbar_init(&scale_full[i], 32), mbar_init(&scale_empty[i], kBigWarps);
     mbar_init_fence();
   }
   if (warp == 1) tmem_alloc<2>(&tmem_at, 512);
@@ -377,6 +394,31 @@ __global__ void __launch_bounds__(kBigThreads, 1)
         for (uint32_t i = 0; i < kWaitIterations && global_ns() - t0 < 1000000; ++i) __nanosleep(1000);
       }
     }
+    if (warp == 2) {
+      uint32_t use = 0;
+      bool ok = true;
+      for (uint32_t t = first; t < tiles && ok; t += step) {
+        uint32_t tr, tc;
+        big_tile(p, t, &tr, &tc);
+        const uint32_t r0 = tr * 256 + rank * 128 + lane, c0 = tc * 256 + lane;
+        for (uint32_t b = 0; b < p.blocks; ++b, ++use) {
+          const uint32_t slot = use % kScaleSlots, at = smem_addr(scales + slot * 384 + lane);
+          if (use >= kScaleSlots && !(ok = warp_wait(&scale_empty[slot], (use / kScaleSlots + 1) & 1))) break;
+          const float *rs = p.r_scale + b * p.r_scale_pitch, *cs = p.c_scale + b * p.c_scale_pitch;
+#pragma unroll
+          for (int i = 0; i < 128; i += 32) copy_word(at + i * 4, rs + (min(r0 + i, p.rows - 1) >> p.r_shift));
+          if (ROWS) {
+#pragma unroll
+            for (int i = 0; i < 256; i += 32) copy_word(at + (128 + i) * 4, cs + min(c0 + i, p.cols - 1));
+          } else if (lane < 2) {  // one for each 128 columns
+            copy_word(at + 128 * 4, cs + (min(tc * 256 + lane * 128, p.cols - 1) >> 7));
+          }
+          arrive_with_words(&scale_full[slot]);
+        }
+      }
+      words_landed();
+      if (!ok) give_up(p.status);
+    }
     if (warp == 1 && rank == 0) {
       uint32_t use = 0;
       bool ok = true;
@@ -410,26 +452,12 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kBigWarps == 8 ? 224 : 112));
     const uint32_t quad = warp & 3, part = (warp - 4) / 4, half = part * kBigCols / kUnitCols, row = quad * 32 + lane;
-    float *sc = scales + (warp - 4) * 2 * kBigCols;
     uint32_t use = 0;
     bool ok = true;
     for (uint32_t t = first; t < tiles && ok; t += step) {
       uint32_t tr, tc;
       big_tile(p, t, &tr, &tc);
       const uint32_t r0 = tr * 256 + rank * 128, c0 = tc * 256 + part * kBigCols;
-      const uint32_t r = min(r0 + row, p.rows - 1);
-      const float *rs = p.r_scale + (r >> p.r_shift);
-      float next_r, next_c[ROWS ? kBigCols / 32 : 1];
-      auto fetch = [&](uint32_t b) {
-        next_r = __ldg(rs + b * p.r_scale_pitch);
-        if (ROWS) {
-#pragma unroll
-          for (int i = 0; i < kBigCols / 32; ++i)
-            next_c[i] = __ldg(p.c_scale + b * p.c_scale_pitch + min(c0 + i * 32 + lane, p.cols - 1));
-        } else {
-          next_c[0] = __ldg(p.c_scale + b * p.c_scale_pitch + (min(c0, p.cols - 1) >> 7));
-        }
-      };
       uint64_t acc[kBigCols / 2];
 #pragma unroll
       for (int i = 0; i < kBigCols / 2; ++i) acc[i] = 0;
@@ -446,18 +474,14 @@ __global__ void __launch_bounds__(kBigThreads, 1)
           acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), y, acc[(c + i) / 2 + 1]);
         }
       };
-      fetch(0);
       for (uint32_t b = 0; b < p.blocks; ++b, ++use) {
         const uint32_t buf = use & 1;
-        float *s = sc + buf * kBigCols;
-        const float one = ROWS ? next_r : next_r * next_c[0];
+        const uint32_t slot = use % kScaleSlots;
+        const float *s = scales + slot * 384 + 128 + (ROWS ? part * kBigCols : part * kBigCols / 128);
+        ok = warp_wait(&scale_full[slot], use / kScaleSlots & 1);
+        if (!ok) break;
+        const float mine = scales[slot * 384 + row], one = ROWS ? mine : mine * s[0];
         const uint64_t sr = pack2(one, one);
-        if (ROWS) {
-#pragma unroll
-          for (int i = 0; i < kBigCols / 32; ++i) s[i * 32 + lane] = next_c[i];
-          __syncwarp();
-        }
-        if (b + 1 < p.blocks) fetch(b + 1);
         ok = warp_wait(&acc_full[2 * half + buf], use / 2 & 1);
         if (!ok) break;
         tc_fence_after();
@@ -474,6 +498,8 @@ __global__ void __launch_bounds__(kBigThreads, 1)
           }
           add(d, c, sr, s);
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&scale_empty[slot]);
       }
       if (!ok) break;
       if (r0 + row < p.rows && c0 < p.cols)
@@ -545,13 +571,15 @@ int launch_mid(const MatmulArgs &a, ProductPlan p, unsigned cap, unsigned sms, v
   // exchange counting as three blocks; it follows the sizes and the GPU, not the cap
   uint32_t best = 0;
   uint64_t best_cost = UINT64_MAX;
-  for (uint32_t s = 0; s <= 3 && (1u << s) <= p.blocks && (1u << s) <= BN / 2; ++s) {
+  for (uint32_t s = 0; s <= (BN == 128 ? 0 : 3) && (1u << s) <= p.blocks; ++s) {
     const uint64_t cost = (uint64_t)ceil_div(tiles, sms >> s) * (ceil_div(p.blocks, 1u << s) + (s ? 3 : 1));
     if (cost < best_cost) best = s, best_cost = cost;
   }
   const uint64_t clusters = tiles < (cap >> best) ? tiles : (cap >> best);
   const unsigned grid = (unsigned)(clusters ? clusters : 1) << best;
-  return launch_cluster(mid_kernel<BN, T>, grid, kMidThreads, MidShape<BN>::kBytes, 1u << best, stream, r, c, p, best);
+  if (BN < 128 && best)
+    return launch_cluster(mid_kernel<BN, BN < 128, T>, grid, kMidThreads, MidShape<BN, BN < 128>::kBytes, 1u << best, stream, r, c, p, best);
+  return launch_cluster(mid_kernel<BN, false, T>, grid, kMidThreads, MidShape<BN, false>::kBytes, 1, stream, r, c, p, 0u);
 }
 
 template <typename T>
@@ -590,7 +618,8 @@ int launch_matmul(const MatmulArgs &a, unsigned cap, unsigned sms, void *stream)
     if (a.m > 128 && (uint64_t)ceil_div(a.m, 256) * ceil_div(a.n, 256) >= sms / 4) return launch_big<T>(a, p, cap, stream);
     if (a.m <= 16) return launch_mid<16, T>(a, p, cap, sms, stream);
     if (a.m <= 32) return launch_mid<32, T>(a, p, cap, sms, stream);
-    if (a.m <= 64) return launch_mid<64, T>(a, p, cap, sms, stream);
+    // 64 columns a tile until tiles of 128 fill the GPU
+    if (a.m <= 64 || (uint64_t)ceil_div(a.n, 128) * ceil_div(a.m, 128) < sms) return launch_mid<64, T>(a, p, cap, sms, stream);
     return launch_mid<128, T>(a, p, cap, sms, stream);
   });
 }

@@ -42,10 +42,10 @@ __device__ __forceinline__ uint32_t map_rank(uint32_t a, uint32_t rank) {
 }
 
 __device__ __forceinline__ void arrive_remote(uint32_t mapped) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mapped) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(mapped) : "memory");
 }
 
-// The same where nothing but tensor memory was read, which tcgen05.fence orders: a
+// The same where nothing but tensor memory was read, which tcgen05.fence orders.  A
 // release at cluster scope waits for the thread's memory operations, 1,000
 // cycles and more, and would bound the product kernel (1,136 TFLOP/s with it).
 __device__ __forceinline__ void arrive_remote_relaxed(uint32_t mapped) {
@@ -59,21 +59,29 @@ __device__ __forceinline__ void store_async(uint32_t mapped, float v, uint32_t m
                : "memory");
 }
 
+// Copies `bytes` (a multiple of 16) of this CTA's shared memory into another CTA's
+// and counts them there.  One barrier update for the whole copy: 4-byte st.async
+// updates one a word, and 16,384 of them took 10 us.
+__device__ __forceinline__ void bulk_s2s(uint32_t mapped, uint32_t from, uint32_t bytes, uint32_t mapped_bar) {
+  asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(mapped),
+               "r"(from), "r"(bytes), "r"(mapped_bar)
+               : "memory");
+}
+
 // mbar_wait with the clock read only once a wait is a long one: the loops here
 // wait for a few hundred cycles again and again, and reading %globaltimer takes
 // longer than that.
-__device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity) {
+// dead: given up by another wait of this CTA, which ends this one too.
+__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, const volatile int32_t *dead = nullptr) {
+  const uint32_t a = smem_addr(bar);
+  if (mbar_try_wait(a, parity) || mbar_try_wait(a, parity)) return true;
   uint64_t t0 = 0;
   for (uint32_t it = 1;; ++it) {
-    if (mbar_try_wait(bar, parity)) return true;
+    if (mbar_try_wait(a, parity)) return true;
+    if (dead && *dead) return false;
     if (it == 1024) t0 = global_ns();
     if (it >= kWaitIterations && (it & 1023u) == 0 && global_ns() - t0 > kWaitNanoseconds) return false;
   }
-}
-
-__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity) {
-  const uint32_t a = smem_addr(bar);
-  return mbar_try_wait(a, parity) || mbar_try_wait(a, parity) || wait_long(a, parity);
 }
 
 // wait_for what other CTAs of the cluster stored.
@@ -204,6 +212,18 @@ __device__ __forceinline__ void mma_commit_pair(uint64_t *bar) {
       "h"((uint16_t)3)
       : "memory");
 }
+
+// ---- a word from global to shared memory without a register, and the arrival of
+// the calling thread's words so far
+__device__ __forceinline__ void copy_word(uint32_t dst, const float *src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+__device__ __forceinline__ void arrive_with_words(uint64_t *bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+
+__device__ __forceinline__ void words_landed() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // ---- two fp32 lanes in one instruction
 __device__ __forceinline__ uint64_t pack2(float lo, float hi) {
