@@ -43,7 +43,9 @@ struct ProductPlan {
 };
 
 // A whole warp's wait: its lanes give up together.
-__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity) { return __all_sync(~0u, wait_for(bar, parity)); }
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity) {
+  return __all_sync(~0u, mbar_try_wait(smem_addr(bar), parity)) || __all_sync(~0u, wait_for(bar, parity));
+}
 
 __device__ __forceinline__ void give_up(unsigned *status) { atomicOr(status, (unsigned)APC_ETIMEOUT); }
 
@@ -117,8 +119,8 @@ __global__ void __launch_bounds__(kMidThreads, 1)
   const uint32_t tmem = tmem_at;
   // A whole warp's wait.
   auto alive = [&](uint64_t *bar, uint32_t parity) {
-    bool ok = wait_for(bar, parity, &dead);
-    ok = __all_sync(~0u, ok);
+    if (__all_sync(~0u, mbar_try_wait(smem_addr(bar), parity))) return true;
+    const bool ok = __all_sync(~0u, wait_for(bar, parity, &dead));
     if (!ok && !dead) {
       dead = 1;
       give_up(p.status);
@@ -127,82 +129,70 @@ __global__ void __launch_bounds__(kMidThreads, 1)
   };
 
   if (warp == 0) {
-    uint32_t use = 0;
+    Turn<S::kStages> st;
+    uint32_t issued = 0;
     bool ok = true;
     for (uint32_t t = first; t < tiles && ok; t += step) {
       const int32_t r0 = (int32_t)(t % p.row_tiles) * 128, c0 = (int32_t)(t / p.row_tiles) * BN;
-      for (uint32_t b = b0; b < b1; ++b, ++use) {
-        const uint32_t st = use % S::kStages;
-        if (use >= S::kStages && !(ok = alive(&empty[st], (use / S::kStages + 1) & 1))) break;
-        const uint32_t at = smem_addr(smem + st * S::kStageBytes), bar = smem_addr(&full[st]);
-        if (elect_one()) {
-          mbar_arrive_expect_tx(&full[st], S::kStageBytes);
-          load_box(at, &map_r, (int32_t)(b * kBlock), r0, bar);
-          load_box(at + S::kRowBytes, &map_c, (int32_t)(b * kBlock), c0, bar);
-        }
-        __syncwarp();
+      for (uint32_t b = b0; b < b1; ++b, st.next(), ++issued) {
+        if (!(ok = alive(&empty[st.at], st.phase ^ 1))) break;
+        const uint32_t at = smem_addr(smem) + st.at * S::kStageBytes;
+        load_block(at, &map_r, r0, at + S::kRowBytes, &map_c, c0, (int32_t)(b * kBlock), smem_addr(&full[st.at]), S::kStageBytes);
       }
     }
     if (!ok)  // let the copies in flight land
-      for (uint32_t u = use > S::kStages ? use - S::kStages : 0; u < use; ++u) wait_for(&full[u % S::kStages], u / S::kStages & 1);
+      for (uint32_t i = min(issued, (uint32_t)S::kStages); i; --i) st.back(), wait_for(&full[st.at], st.phase);
   } else if (warp == 1) {
-    uint32_t use = 0;
+    Turn<S::kStages> st;
+    Turn<S::kAcc> acc;
+    uint32_t issued = 0;
     bool ok = true;
+    const uint64_t r_desc = operand_desc(smem_addr(smem)), c_desc = operand_desc(smem_addr(smem) + S::kRowBytes);
     for (uint32_t t = first; t < tiles && ok; t += step)
-      for (uint32_t b = b0; b < b1; ++b, ++use) {
-        const uint32_t st = use % S::kStages, buf = use % S::kAcc;
-        ok = (use < S::kAcc || alive(&acc_empty[buf], (use / S::kAcc + 1) & 1)) && alive(&full[st], use / S::kStages & 1);
-        if (!ok) break;
+      for (uint32_t b = b0; b < b1; ++b, st.next(), acc.next(), ++issued) {
+        if (!(ok = alive(&acc_empty[acc.at], acc.phase ^ 1) && alive(&full[st.at], st.phase))) break;
         tc_fence_after();
-        const uint64_t dr = operand_desc(smem_addr(smem + st * S::kStageBytes));
-        const uint64_t dc = operand_desc(smem_addr(smem + st * S::kStageBytes + S::kRowBytes));
-        if (elect_one()) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) mma_fp8<1>(tmem + buf * BN, dr + 2 * k, dc + 2 * k, p.instruction, k > 0);
-          mma_commit(&acc_full[buf]);
-          mma_commit(&empty[st]);
-        }
-        __syncwarp();
+        const uint64_t off = st.at * (S::kStageBytes >> 4);
+        mma_block<1>(tmem + acc.at * BN, r_desc + off, c_desc + off, p.instruction, smem_addr(&acc_full[acc.at]), smem_addr(&empty[st.at]));
       }
     if (!ok)  // let the products in flight end
-      for (uint32_t u = use > S::kAcc ? use - S::kAcc : 0; u < use; ++u) wait_for(&acc_full[u % S::kAcc], u / S::kAcc & 1);
+      for (uint32_t i = min(issued, (uint32_t)S::kAcc); i; --i) acc.back(), wait_for(&acc_full[acc.at], acc.phase);
   } else if (warp == 6) {
-    uint32_t use = 0;
-    for (uint32_t t = first; t < tiles; t += step) {
+    Turn<kScaleSlots> slot;
+    for (uint32_t t = first; t < tiles && !dead; t += step) {
       const uint32_t r0 = t % p.row_tiles * 128 + lane, c0 = t / p.row_tiles * BN + lane;
-      for (uint32_t b = b0; b < b1; ++b, ++use) {
-        const uint32_t slot = use % kScaleSlots, at = smem_addr(scales + slot * (128 + BN) + lane);
-        if (use >= kScaleSlots && !alive(&scale_empty[slot], (use / kScaleSlots + 1) & 1)) break;
+      for (uint32_t b = b0; b < b1; ++b, slot.next()) {
+        const uint32_t at = smem_addr(scales + slot.at * (128 + BN) + lane);
+        if (!alive(&scale_empty[slot.at], slot.phase ^ 1)) break;
         const float *rs = p.r_scale + b * p.r_scale_pitch, *cs = p.c_scale + b * p.c_scale_pitch;
 #pragma unroll
         for (int i = 0; i < 128; i += 32) copy_word(at + i * 4, rs + (min(r0 + i, p.rows - 1) >> p.r_shift));
 #pragma unroll
         for (int i = 0; i < BN; i += 32)
           if (BN >= 32 || lane < BN) copy_word(at + (128 + i) * 4, cs + (min(c0 + i, p.cols - 1) >> p.c_shift));
-        arrive_with_words(&scale_full[slot]);
+        arrive_with_words(&scale_full[slot.at]);
       }
-      if (dead) break;
     }
     words_landed();
   } else {
     const uint32_t quad = warp & 3, row = quad * 32 + lane;
-    uint32_t use = 0, done = 0;
+    Turn<S::kAcc> buf;
+    Turn<kScaleSlots> slot;
+    uint32_t done = 0;
     if (SPLIT && threadIdx.x == 64) mbar_arrive_expect_tx(&recv_full, S::kShareBytes);
     for (uint32_t t = first; t < tiles; t += step, ++done) {
       const uint32_t r0 = t % p.row_tiles * 128, c0 = t / p.row_tiles * BN;
       uint64_t acc[BN / 2];
 #pragma unroll
       for (int i = 0; i < BN / 2; ++i) acc[i] = 0;
-      for (uint32_t b = b0; b < b1; ++b, ++use) {
-        const uint32_t buf = use % S::kAcc;
-        const uint32_t slot = use % kScaleSlots;
-        const float *s = scales + slot * (128 + BN) + 128;
-        alive(&scale_full[slot], use / kScaleSlots & 1);
+      for (uint32_t b = b0; b < b1; ++b, buf.next(), slot.next()) {
+        const float *s = scales + slot.at * (128 + BN) + 128;
+        alive(&scale_full[slot.at], slot.phase);
         const float one = s[(int)row - 128];
         const uint64_t sr = pack2(one, one);
-        alive(&acc_full[buf], use / S::kAcc & 1);
+        alive(&acc_full[buf.at], buf.phase);
         tc_fence_after();
-        const uint32_t at = tmem + buf * BN + (quad << 21);  // lane 32 * quad in bits 16 up
+        const uint32_t at = tmem + buf.at * BN + (quad << 21);  // lane 32 * quad in bits 16 up
         constexpr int kChunk = BN < 32 ? 16 : 32;
 #pragma unroll
         for (int c = 0; c < BN; c += kChunk) {
@@ -212,7 +202,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
           if (c + kChunk == BN) {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&acc_empty[buf]);
+            if (lane == 0) mbar_arrive(&acc_empty[buf.at]);
           }
 #pragma unroll
           for (int i = 0; i < kChunk; i += 4) {
@@ -222,7 +212,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
           }
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(&scale_empty[slot]);
+        if (lane == 0) mbar_arrive(&scale_empty[slot.at]);
       }
       T *out = static_cast<T *>(p.out) + (int64_t)(r0 + row) * p.row_step;
       const bool in = r0 + row < p.rows;
@@ -279,19 +269,15 @@ __global__ void __launch_bounds__(kMidThreads, 1)
 #ifndef APC_BIG_WARPS
 #define APC_BIG_WARPS 8
 #endif
-#ifndef APC_BIG_UNITS
-#define APC_BIG_UNITS 1
-#endif
 #ifndef APC_BIG_LOAD
 #define APC_BIG_LOAD 16
 #endif
 #ifndef APC_BIG_STAGES
 #define APC_BIG_STAGES 6
 #endif
-constexpr int kBigWarps = APC_BIG_WARPS, kBigUnits = APC_BIG_UNITS, kBigLoad = APC_BIG_LOAD;
+constexpr int kBigWarps = APC_BIG_WARPS, kBigLoad = APC_BIG_LOAD;
 constexpr int kBigThreads = 128 + 32 * kBigWarps, kBigStages = APC_BIG_STAGES;
 constexpr int kBigCols = 1024 / kBigWarps;  // columns that a warp adds up
-constexpr int kUnitCols = 256 / kBigUnits;
 constexpr int kBigHalf = 128 * kBlock, kBigStageBytes = 2 * kBigHalf;
 constexpr int kBigScaleBytes = kScaleSlots * (128 + 256) * 4;
 constexpr int kBigBytes = 1024 + kBigStages * kBigStageBytes + kBigScaleBytes;
@@ -340,7 +326,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
     big_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ ProductPlan p) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[kBigStages], empty[kBigStages], acc_full[2 * kBigUnits], acc_empty[2 * kBigUnits];
+  __shared__ uint64_t full[kBigStages], empty[kBigStages], acc_full[2], acc_empty[2];
   __shared__ uint64_t scale_full[kScaleSlots], scale_empty[kScaleSlots];
   __shared__ uint32_t tmem_at;
   uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -350,7 +336,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kBigStages; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
-    for (int i = 0; i < 2 * kBigUnits; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 2 * kBigWarps / kBigUnits);
+    for (int i = 0; i < 2; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 2 * kBigWarps);
     for (int i = 0; i < kScaleSlots; ++i) mbar_init(&scale_full[i], 32), mbar_init(&scale_empty[i], kBigWarps);
     mbar_init_fence();
   }
@@ -364,46 +350,39 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBigWarps == 8 ? 56 : 32));
     if (warp == 0) {
-      uint32_t use = 0;
+      Turn<kBigStages> st;
+      uint32_t issued = 0;
       bool ok = true;
+      const uint32_t bars = map_rank(smem_addr(full), 0);
       for (uint32_t t = first; t < tiles && ok; t += step) {
         uint32_t tr, tc;
         big_tile(p, t, &tr, &tc);
-        const int32_t r0 = (int32_t)(tr * 256 + rank * 128), c0 = (int32_t)(tc * 256 + rank * (kUnitCols / 2));
-        for (uint32_t b = 0; b < p.blocks; ++b, ++use) {
-          const uint32_t st = use % kBigStages;
-          if (use >= kBigStages && !warp_wait(&empty[st], (use / kBigStages + 1) & 1)) {
-            ok = false;
-            break;
-          }
-          const uint32_t at = smem_addr(smem + st * kBigStageBytes), bar = map_rank(smem_addr(&full[st]), 0);
-          if (elect_one()) {
-            if (rank == 0) mbar_arrive_expect_tx(&full[st], 2 * kBigStageBytes);
-            load_box_pair(at, &map_a, (int32_t)(b * kBlock), r0, bar);
-            load_box_pair(at + kBigHalf, &map_b, (int32_t)(b * kBlock), c0, bar);
-            if (kBigUnits == 2) load_box_pair(at + kBigHalf + kBigHalf / 2, &map_b, (int32_t)(b * kBlock), c0 + 128, bar);
-          }
-          __syncwarp();
+        const int32_t r0 = (int32_t)(tr * 256 + rank * 128), c0 = (int32_t)(tc * 256 + rank * 128);
+        for (uint32_t b = 0; b < p.blocks; ++b, st.next(), ++issued) {
+          if (!(ok = warp_wait(&empty[st.at], st.phase ^ 1))) break;
+          const uint32_t at = smem_addr(smem) + st.at * kBigStageBytes;
+          load_block_pair(at, &map_a, r0, at + kBigHalf, &map_b, c0, (int32_t)(b * kBlock), bars + st.at * 8, smem_addr(&full[st.at]),
+                          rank == 0 ? 2 * kBigStageBytes : 0);
         }
       }
       if (!ok) {  // let the copies in flight land, the other CTA's too
         give_up(p.status);
         if (rank == 0)
-          for (uint32_t u = use > kBigStages ? use - kBigStages : 0; u < use; ++u) wait_for(&full[u % kBigStages], u / kBigStages & 1);
+          for (uint32_t i = min(issued, (uint32_t)kBigStages); i; --i) st.back(), wait_for(&full[st.at], st.phase);
         const uint64_t t0 = global_ns();
         for (uint32_t i = 0; i < kWaitIterations && global_ns() - t0 < 1000000; ++i) __nanosleep(1000);
       }
     }
     if (warp == 2) {
-      uint32_t use = 0;
+      Turn<kScaleSlots> slot;
       bool ok = true;
       for (uint32_t t = first; t < tiles && ok; t += step) {
         uint32_t tr, tc;
         big_tile(p, t, &tr, &tc);
         const uint32_t r0 = tr * 256 + rank * 128 + lane, c0 = tc * 256 + lane;
-        for (uint32_t b = 0; b < p.blocks; ++b, ++use) {
-          const uint32_t slot = use % kScaleSlots, at = smem_addr(scales + slot * 384 + lane);
-          if (use >= kScaleSlots && !(ok = warp_wait(&scale_empty[slot], (use / kScaleSlots + 1) & 1))) break;
+        for (uint32_t b = 0; b < p.blocks; ++b, slot.next()) {
+          const uint32_t at = smem_addr(scales + slot.at * 384 + lane);
+          if (!(ok = warp_wait(&scale_empty[slot.at], slot.phase ^ 1))) break;
           const float *rs = p.r_scale + b * p.r_scale_pitch, *cs = p.c_scale + b * p.c_scale_pitch;
 #pragma unroll
           for (int i = 0; i < 128; i += 32) copy_word(at + i * 4, rs + (min(r0 + i, p.rows - 1) >> p.r_shift));
@@ -413,46 +392,36 @@ __global__ void __launch_bounds__(kBigThreads, 1)
           } else if (lane < 2) {  // one for each 128 columns
             copy_word(at + 128 * 4, cs + (min(tc * 256 + lane * 128, p.cols - 1) >> 7));
           }
-          arrive_with_words(&scale_full[slot]);
+          arrive_with_words(&scale_full[slot.at]);
         }
       }
       words_landed();
       if (!ok) give_up(p.status);
     }
     if (warp == 1 && rank == 0) {
-      uint32_t use = 0;
+      Turn<kBigStages> st;
+      Turn<2> acc;
+      uint32_t issued = 0;
       bool ok = true;
+      const uint64_t da = operand_desc(smem_addr(smem)), db = operand_desc(smem_addr(smem) + kBigHalf);
       for (uint32_t t = first; t < tiles && ok; t += step)
-        for (uint32_t b = 0; b < p.blocks; ++b, ++use) {
-          const uint32_t st = use % kBigStages, buf = use & 1;
-          if (!(ok = warp_wait(&full[st], use / kBigStages & 1))) break;
-          const uint64_t da = operand_desc(smem_addr(smem + st * kBigStageBytes));
-          const uint64_t db = operand_desc(smem_addr(smem + st * kBigStageBytes + kBigHalf));
-#pragma unroll
-          for (int h = 0; h < kBigUnits; ++h) {
-            if (use >= 2 && !(ok = warp_wait(&acc_empty[2 * h + buf], (use / 2 + 1) & 1))) break;
-            tc_fence_after();
-            if (elect_one()) {
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-                mma_fp8<2>(tmem + (2 * h + buf) * kUnitCols, da + 2 * k, db + h * (kBigHalf / 2 >> 4) + 2 * k, p.instruction, k > 0);
-              mma_commit_pair(&acc_full[2 * h + buf]);
-              if (h == kBigUnits - 1) mma_commit_pair(&empty[st]);
-            }
-            __syncwarp();
-          }
-          if (!ok) break;
+        for (uint32_t b = 0; b < p.blocks; ++b, st.next(), acc.next(), ++issued) {
+          if (!(ok = warp_wait(&full[st.at], st.phase) && warp_wait(&acc_empty[acc.at], acc.phase ^ 1))) break;
+          tc_fence_after();
+          const uint64_t off = st.at * (kBigStageBytes >> 4);
+          mma_block<2>(tmem + acc.at * 256, da + off, db + off, p.instruction, smem_addr(&acc_full[acc.at]), smem_addr(&empty[st.at]));
         }
       if (!ok) {  // let the products in flight end
         give_up(p.status);
-        for (uint32_t u = use > 2 ? use - 2 : 0; u < use; ++u)
-          for (int h = 0; h < kBigUnits; ++h) wait_for(&acc_full[2 * h + (u & 1)], u / 2 & 1);
+        for (uint32_t i = min(issued, 2u); i; --i) acc.back(), wait_for(&acc_full[acc.at], acc.phase);
       }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kBigWarps == 8 ? 224 : 112));
-    const uint32_t quad = warp & 3, part = (warp - 4) / 4, half = part * kBigCols / kUnitCols, row = quad * 32 + lane;
-    uint32_t use = 0;
+    const uint32_t quad = warp & 3, part = (warp - 4) / 4, row = quad * 32 + lane;
+    const uint32_t empty_bars = map_rank(smem_addr(acc_empty), 0);
+    Turn<2> buf;
+    Turn<kScaleSlots> slot;
     bool ok = true;
     for (uint32_t t = first; t < tiles && ok; t += step) {
       uint32_t tr, tc;
@@ -474,18 +443,14 @@ __global__ void __launch_bounds__(kBigThreads, 1)
           acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), y, acc[(c + i) / 2 + 1]);
         }
       };
-      for (uint32_t b = 0; b < p.blocks; ++b, ++use) {
-        const uint32_t buf = use & 1;
-        const uint32_t slot = use % kScaleSlots;
-        const float *s = scales + slot * 384 + 128 + (ROWS ? part * kBigCols : part * kBigCols / 128);
-        ok = warp_wait(&scale_full[slot], use / kScaleSlots & 1);
-        if (!ok) break;
-        const float mine = scales[slot * 384 + row], one = ROWS ? mine : mine * s[0];
+      for (uint32_t b = 0; b < p.blocks; ++b, buf.next(), slot.next()) {
+        const float *s = scales + slot.at * 384 + 128 + (ROWS ? part * kBigCols : part * kBigCols / 128);
+        if (!(ok = warp_wait(&scale_full[slot.at], slot.phase))) break;
+        const float mine = scales[slot.at * 384 + row], one = ROWS ? mine : mine * s[0];
         const uint64_t sr = pack2(one, one);
-        ok = warp_wait(&acc_full[2 * half + buf], use / 2 & 1);
-        if (!ok) break;
+        if (!(ok = warp_wait(&acc_full[buf.at], buf.phase))) break;
         tc_fence_after();
-        const uint32_t at = tmem + (2 * half + buf) * kUnitCols + part * kBigCols % kUnitCols + (quad << 21);
+        const uint32_t at = tmem + buf.at * 256 + part * kBigCols + (quad << 21);
 #pragma unroll
         for (int c = 0; c < kBigCols; c += kBigLoad) {
           uint32_t d[kBigLoad];
@@ -494,12 +459,12 @@ __global__ void __launch_bounds__(kBigThreads, 1)
           if (c + kBigLoad == kBigCols) {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) arrive_remote_relaxed(map_rank(smem_addr(&acc_empty[2 * half + buf]), 0));
+            if (lane == 0) arrive_remote_relaxed(empty_bars + buf.at * 8);
           }
           add(d, c, sr, s);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(&scale_empty[slot]);
+        if (lane == 0) mbar_arrive(&scale_empty[slot.at]);
       }
       if (!ok) break;
       if (r0 + row < p.rows && c0 < p.cols)
@@ -589,11 +554,11 @@ int launch_big(const MatmulArgs &a, ProductPlan p, unsigned cap, void *stream) {
   p.r_shift = a.a_shift, p.c_shift = a.b_shift;
   p.rows = a.m, p.cols = a.n;
   p.row_tiles = ceil_div(a.m, 256), p.col_tiles = ceil_div(a.n, 256);
-  p.instruction = 1u << 4 | a.a_e5m2 << 7 | a.b_e5m2 << 10 | (uint32_t)(kUnitCols >> 3) << 17 | (256u >> 4) << 24;
+  p.instruction = 1u << 4 | a.a_e5m2 << 7 | a.b_e5m2 << 10 | (256u >> 3) << 17 | (256u >> 4) << 24;
   p.row_step = a.out_pitch, p.col_step = 1;
   CUtensorMap ma, mb;
   int e = encode(&ma, a.a, a.m, a.k, a.a_pitch, 128);
-  if (!e) e = encode(&mb, a.b, a.n, a.k, a.b_pitch, kUnitCols / 2);
+  if (!e) e = encode(&mb, a.b, a.n, a.k, a.b_pitch, 128);
   if (e) return e;
   const uint64_t tiles = (uint64_t)p.row_tiles * p.col_tiles, pairs = cap >= 2 ? cap / 2 : 1;
   const unsigned grid = (unsigned)(tiles < pairs ? tiles : pairs) * 2;

@@ -9,20 +9,10 @@
 
 namespace apc {
 
-// One lane of a converged warp, in a form that the compiler knows to be one.
-// The loops around tcgen05 and TMA run in the whole warp, so that barriers,
-// coordinates and descriptors stay in uniform registers, and only the
-// instructions themselves are elected: with a loop in one lane the issue of
+// The loops around tcgen05 and TMA run in a whole warp, so that barriers,
+// coordinates and descriptors stay in uniform registers, and the instructions
+// themselves are elected (elect.sync): with a loop in one lane the issue of
 // four products took 600 cycles, more than the products.
-__device__ __forceinline__ bool elect_one() {
-  uint32_t p;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "elect.sync _|p, 0xffffffff;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(p));
-  return p != 0;
-}
 
 // ---- clusters
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -89,27 +79,6 @@ __device__ __forceinline__ bool wait_for_cluster(uint64_t *bar, uint32_t parity)
   const bool ok = wait_for(bar, parity);
   asm volatile("fence.acq_rel.cluster;" ::: "memory");
   return ok;
-}
-
-// ---- TMA: a box of a matrix of bytes at column x (a multiple of 16), row y.
-__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
-  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
-}
-
-__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-      "l"(map), "r"(x), "r"(y), "r"(bar)
-      : "memory");
-}
-
-// The same for a pair of CTAs: `bar` may be a barrier of either.
-__device__ __forceinline__ void load_box_pair(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
-      "[%4];" ::"r"(dst),
-      "l"(map), "r"(x), "r"(y), "r"(bar)
-      : "memory");
 }
 
 // ---- tensor memory
@@ -184,34 +153,83 @@ __device__ __forceinline__ uint32_t fp8_instruction(uint32_t a_format, uint32_t 
   return 1u << 4 | a_format << 7 | b_format << 10 | (n >> 3) << 17 | (m >> 4) << 24;
 }
 
+// One thread of a converged warp issues the four products of a block of 128 k
+// (overwriting the accumulator first) and both commits: `done` is arrived on once
+// they are complete, `read` too.  Predicated as a whole: a branch around them and
+// the warp's return from it cost as much as the products' issue.
 template <int PAIR>
-__device__ __forceinline__ void mma_fp8(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, bool add) {
+__device__ __forceinline__ void mma_block(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, uint32_t done, uint32_t read) {
   if (PAIR == 2)
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(instruction), "r"((uint32_t)add)
+        "{\n\t.reg .pred q, no, yes;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t.reg .b16 both;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "setp.ne.b32 no, 0, 0;\n\tsetp.eq.b32 yes, 0, 0;\n\tmov.b16 both, 3;\n\t"
+        "add.s64 a1, %1, 2;\n\tadd.s64 a2, %1, 4;\n\tadd.s64 a3, %1, 6;\n\t"
+        "add.s64 b1, %2, 2;\n\tadd.s64 b2, %2, 4;\n\tadd.s64 b3, %2, 6;\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, no;\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a1, b1, %3, yes;\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a2, b2, %3, yes;\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a3, b3, %3, yes;\n\t"
+        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%4], both;\n\t"
+        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%5], both;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(instruction), "r"(done), "r"(read)
         : "memory");
   else
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(instruction), "r"((uint32_t)add)
+        "{\n\t.reg .pred q, no, yes;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "setp.ne.b32 no, 0, 0;\n\tsetp.eq.b32 yes, 0, 0;\n\t"
+        "add.s64 a1, %1, 2;\n\tadd.s64 a2, %1, 4;\n\tadd.s64 a3, %1, 6;\n\t"
+        "add.s64 b1, %2, 2;\n\tadd.s64 b2, %2, 4;\n\tadd.s64 b3, %2, 6;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, no;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a1, b1, %3, yes;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a2, b2, %3, yes;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a3, b3, %3, yes;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(instruction), "r"(done), "r"(read)
         : "memory");
 }
 
-// The barrier is arrived on once the issuing thread's products so far are done.
-__device__ __forceinline__ void mma_commit(uint64_t *bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
-}
-
-// The same in both CTAs of a pair.
-__device__ __forceinline__ void mma_commit_pair(uint64_t *bar) {
+// One thread of a converged warp announces `bytes` on `bar` and loads a box of each
+// operand, both in the same columns.
+__device__ __forceinline__ void load_block(uint32_t dst, const CUtensorMap *r, int32_t r0, uint32_t c_dst, const CUtensorMap *c,
+                                           int32_t c0, int32_t x, uint32_t bar, uint32_t bytes) {
   asm volatile(
-      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)),
-      "h"((uint16_t)3)
+      "{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+      "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%7], %8;\n\t"
+      "@q cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%6, %2}], [%7];\n\t"
+      "@q cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%3], [%4, {%6, %5}], [%7];\n\t}" ::"r"(dst),
+      "l"(r), "r"(r0), "r"(c_dst), "l"(c), "r"(c0), "r"(x), "r"(bar), "r"(bytes)
       : "memory");
 }
+
+// The same for a pair of CTAs, whose first one's barrier `first_bar` counts both's
+// boxes; bytes: announced on this CTA's `bar`, 0 in the second.
+__device__ __forceinline__ void load_block_pair(uint32_t dst, const CUtensorMap *r, int32_t r0, uint32_t c_dst, const CUtensorMap *c,
+                                                int32_t c0, int32_t x, uint32_t first_bar, uint32_t bar, uint32_t bytes) {
+  asm volatile(
+      "{\n\t.reg .pred q, t;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.and.b32 t, %9, 0, q;\n\t"
+      "@t mbarrier.arrive.expect_tx.shared::cta.b64 _, [%8], %9;\n\t"
+      "@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%6, %2}], [%7];\n\t"
+      "@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%3], [%4, {%6, %5}], "
+      "[%7];\n\t}" ::"r"(dst),
+      "l"(r), "r"(r0), "r"(c_dst), "l"(c), "r"(c0), "r"(x), "r"(first_bar), "r"(bar), "r"(bytes)
+      : "memory");
+}
+
+// A place in a ring and the parity of its current use.  A consumer waits for
+// `phase`, a producer for the use before: phase ^ 1, which a new barrier passes.
+template <int N>
+struct Turn {
+  uint32_t at = 0, phase = 0;
+  __device__ __forceinline__ void next() {
+    if (++at == N) at = 0, phase ^= 1;
+  }
+  __device__ __forceinline__ void back() {
+    if (at-- == 0) at = N - 1, phase ^= 1;
+  }
+};
 
 // ---- a word from global to shared memory without a register, and the arrival of
 // the calling thread's words so far
