@@ -102,6 +102,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
   const uint32_t tiles = p.row_tiles * p.col_tiles;
   const uint32_t b0 = (uint32_t)((uint64_t)p.blocks * rank / split), b1 = (uint32_t)((uint64_t)p.blocks * (rank + 1) / split);
 
+  if (threadIdx.x == 32) prefetch_map(&map_r), prefetch_map(&map_c);
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kStages; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
     for (int i = 0; i < S::kAcc; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 4);
@@ -334,6 +335,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, rank = cluster_rank();
   const uint32_t first = blockIdx.x / 2, step = gridDim.x / 2, tiles = p.row_tiles * p.col_tiles;
 
+  if (threadIdx.x == 32) prefetch_map(&map_a), prefetch_map(&map_b);
   if (threadIdx.x == 0) {
     for (int i = 0; i < kBigStages; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
     for (int i = 0; i < 2; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 2 * kBigWarps);
@@ -451,17 +453,21 @@ __global__ void __launch_bounds__(kBigThreads, 1)
         if (!(ok = warp_wait(&acc_full[buf.at], buf.phase))) break;
         tc_fence_after();
         const uint32_t at = tmem + buf.at * 256 + part * kBigCols + (quad << 21);
+        // each load runs under the additions of the one before
+        uint32_t d[2][kBigLoad];
+        tmem_load(d[0], at);
 #pragma unroll
         for (int c = 0; c < kBigCols; c += kBigLoad) {
-          uint32_t d[kBigLoad];
-          tmem_load(d, at + c);
-          tmem_landed(d);
-          if (c + kBigLoad == kBigCols) {
+          const int i = c / kBigLoad % 2;
+          tmem_landed(d[i]);
+          if (c + kBigLoad < kBigCols) {
+            tmem_load(d[i ^ 1], at + c + kBigLoad);
+          } else {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive_remote_relaxed(empty_bars + buf.at * 8);
           }
-          add(d, c, sr, s);
+          add(d[i], c, sr, s);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&scale_empty[slot.at]);

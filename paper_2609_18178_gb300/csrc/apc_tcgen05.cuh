@@ -81,6 +81,10 @@ __device__ __forceinline__ bool wait_for_cluster(uint64_t *bar, uint32_t parity)
   return ok;
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
 // ---- tensor memory
 template <int PAIR>
 __device__ __forceinline__ void tmem_alloc(uint32_t *at, uint32_t columns) {  // a whole warp
