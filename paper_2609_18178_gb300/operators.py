@@ -39,33 +39,64 @@ class _Distill(ctypes.Structure):
                [(n, ctypes.c_double) for n in ("temperature", "kd_weight", "label_weight")]
 
 
-def _here(x, name: str, device: int) -> None:
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # the handle without a Stream object around it
+_lib = None
+
+# The checks below read each attribute of a tensor once (0.1 us apiece): a call of
+# small size is bound by them.
+
+
+def _library():
+    global _lib
+    if _lib is None:
+        from . import library
+        _lib = library()
+    return _lib
+
+
+def _stream(stream, device: int) -> int:
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device)
+    from . import _stream as handle
+    return handle(stream)
+
+
+def _elsewhere(x, name: str, device: int):
     if not x.is_cuda:
         raise ValueError("%s is not on a CUDA device" % name)
+    raise ValueError("%s is on cuda:%d but the current device is cuda:%d (use torch.cuda.device(...))"
+                     % (name, x.get_device(), device))
+
+
+def _matrix(x, name: str, kinds, device: int):
+    """Code of the type, rows, columns and pitch of a two-dimensional tensor on
+    the current device whose type is one of `kinds`."""
     if x.get_device() != device:
-        raise ValueError("%s is on cuda:%d but the current device is cuda:%d (use torch.cuda.device(...))"
-                         % (name, x.get_device(), device))
-
-
-def _matrix(x, name: str, kinds, device: int, shape=None) -> int:
-    """The pitch of a two-dimensional tensor on the current device, of one of
-    the types and of the shape given."""
-    _here(x, name, device)
-    if x.dtype not in kinds:
+        _elsewhere(x, name, device)
+    kind = kinds.get(x.dtype)
+    if kind is None:
         raise ValueError("%s has type %s" % (name, x.dtype))
     if x.dim() != 2:
         raise ValueError("%s has %d dimensions, expected 2" % (name, x.dim()))
     r, c = x.shape
-    if shape is not None and (r, c) != shape:
-        raise ValueError("%s is %d x %d, expected %d x %d" % (name, r, c, *shape))
     pitch, step = x.stride()
     if step != 1 and c > 1:
         raise ValueError("%s: neighbours in a row are %d elements apart, expected 1" % (name, step))
-    return pitch if r > 1 else c
+    return kind, r, c, pitch if r > 1 else c
+
+
+def _sized(x, name: str, kinds, device: int, rows: int, cols: int):
+    """Code of the type and pitch of a matrix of the given size."""
+    kind, r, c, pitch = _matrix(x, name, kinds, device)
+    if r != rows or c != cols:
+        raise ValueError("%s is %d x %d, expected %d x %d" % (name, r, c, rows, cols))
+    return kind, pitch
 
 
 def _vector(x, name: str, kinds, device: int, n: int) -> int:
-    _here(x, name, device)
+    if x.get_device() != device:
+        _elsewhere(x, name, device)
     if x.dtype not in kinds:
         raise ValueError("%s has type %s" % (name, x.dtype))
     if x.numel() != n or not x.is_contiguous():
@@ -80,18 +111,17 @@ def _blocks(n: int) -> int:
     return (n + BLOCK - 1) // BLOCK
 
 
-def _fp8(data, scale, name: str, device: int, block=None) -> _Fp8Matrix:
-    """The C structure of an 8-bit matrix; block: its rows per scale, found from
-    the scale's shape if not given."""
-    pitch = _matrix(data, name, _FORMAT, device)
-    r, c = data.shape
-    scale_pitch = _matrix(scale, name + "_scale", _F32, device)
+def _fp8(data, scale, name: str, device: int, block=None):
+    """The C structure of an 8-bit matrix, its rows and columns; block: its rows
+    per scale, found from the scale's shape if not given."""
+    kind, r, c, pitch = _matrix(data, name, _FORMAT, device)
+    _, lines, width, scale_pitch = _matrix(scale, name + "_scale", _F32, device)
     if block is None:
-        block = 1 if scale.shape[1] == r else BLOCK
-    if tuple(scale.shape) != (_blocks(c), -(-r // block)):
+        block = 1 if width == r else BLOCK
+    if lines != (c + BLOCK - 1) // BLOCK or width != (r if block == 1 else -(-r // block)):
         raise ValueError("%s_scale is %d x %d: expected %d x %d, or %d columns for square blocks"
-                         % (name, *scale.shape, _blocks(c), r, _blocks(r)))
-    return _Fp8Matrix(data.data_ptr(), scale.data_ptr(), pitch, scale_pitch, _FORMAT[data.dtype], block)
+                         % (name, lines, width, _blocks(c), r, _blocks(r)))
+    return _Fp8Matrix(data.data_ptr(), scale.data_ptr(), pitch, scale_pitch, kind, block), r, c
 
 
 def _fp8_empty(rows: int, cols: int, block: int, dtype, like):
@@ -99,21 +129,10 @@ def _fp8_empty(rows: int, cols: int, block: int, dtype, like):
             torch.empty(_blocks(cols), -(-rows // block), dtype=torch.float32, device=like.device))
 
 
-def _call(f, *args) -> None:
-    status = f(*args)
+def _check(status: int) -> None:
     if status:
-        from . import _check
-        _check(status)
-
-
-def _library():
-    from . import library
-    return library()
-
-
-def _stream(stream):
-    from . import _stream as handle
-    return handle(stream)
+        from . import _check as check
+        check(status)
 
 
 def quantize_fp8(x, block_rows: int = 1, dtype=torch.float8_e4m3fn, transposed: bool = False, out=None, stream=None):
@@ -125,27 +144,28 @@ def quantize_fp8(x, block_rows: int = 1, dtype=torch.float8_e4m3fn, transposed: 
     scale_t)`` with the transpose quantized from the same reading of ``x``,
     its blocks along its own rows.  ``out`` takes tensors of those shapes."""
     lib = _library()
-    device = torch.cuda.current_device()
-    pitch = _matrix(x, "x", _DTYPE, device)
+    device = _current_device()
+    kind, r, c, pitch = _matrix(x, "x", _DTYPE, device)
     if dtype not in _FORMAT:
         raise ValueError("dtype %s is not an 8-bit floating type" % dtype)
     if block_rows not in (1, BLOCK):
         raise ValueError("block_rows %r is neither 1 nor %d" % (block_rows, BLOCK))
-    r, c = x.shape
     if out is None:
         out = _fp8_empty(r, c, block_rows, dtype, x)
         if transposed:
             out += _fp8_empty(c, r, block_rows, dtype, x)
     elif len(out) != (4 if transposed else 2):
         raise ValueError("out has %d tensors, expected %d" % (len(out), 4 if transposed else 2))
-    for i, (shape, name) in enumerate((((r, c), "q"), ((c, r), "qt"))[:len(out) // 2]):
-        if tuple(out[2 * i].shape) != shape or out[2 * i].dtype != dtype:
-            raise ValueError("out: %s is %s of %s, expected %s of %s"
-                             % (name, tuple(out[2 * i].shape), out[2 * i].dtype, shape, dtype))
-    q = _fp8(out[0], out[1], "q", device, block_rows)
-    qt = _fp8(out[2], out[3], "qt", device, block_rows) if transposed else None
-    _call(lib.apc_quantize_fp8, x.data_ptr(), r, c, pitch, _DTYPE[x.dtype], ctypes.addressof(q),
-          ctypes.addressof(qt) if transposed else None, _stream(stream))
+    q, qr, qc = _fp8(out[0], out[1], "q", device, block_rows)
+    if qr != r or qc != c or q.format != _FORMAT[dtype]:
+        raise ValueError("out: q is %d x %d of %s, expected %d x %d of %s" % (qr, qc, out[0].dtype, r, c, dtype))
+    qt = None
+    if transposed:
+        qt, qr, qc = _fp8(out[2], out[3], "qt", device, block_rows)
+        if qr != c or qc != r or qt.format != _FORMAT[dtype]:
+            raise ValueError("out: qt is %d x %d of %s, expected %d x %d of %s" % (qr, qc, out[2].dtype, c, r, dtype))
+        qt = ctypes.byref(qt)
+    _check(lib.apc_quantize_fp8(x.data_ptr(), r, c, pitch, kind, ctypes.byref(q), qt, _stream(stream, device)))
     return tuple(out)
 
 
@@ -154,47 +174,43 @@ def matmul_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, strea
     k]``) with their scales.  Returns ``out`` (``[m, n]`` of ``out_dtype``:
     fp32, bf16 or fp16), or fills the one given, of any row pitch."""
     lib = _library()
-    device = torch.cuda.current_device()
-    p, q = _fp8(a, a_scale, "a", device), _fp8(b, b_scale, "b", device)
-    m, k = a.shape
-    n = b.shape[0]
-    if b.shape[1] != k:
-        raise ValueError("a has %d columns and b has %d" % (k, b.shape[1]))
+    device = _current_device()
+    p, m, k = _fp8(a, a_scale, "a", device)
+    q, n, kb = _fp8(b, b_scale, "b", device)
+    if kb != k:
+        raise ValueError("a has %d columns and b has %d" % (k, kb))
     if out is None:
         out = torch.empty(m, n, dtype=out_dtype, device=a.device)
-    pitch = _matrix(out, "out", _DTYPE, device, (m, n))
-    _call(lib.apc_matmul_fp8, ctypes.addressof(p), ctypes.addressof(q), m, n, k, out.data_ptr(), pitch,
-          _DTYPE[out.dtype], _stream(stream))
+    kind, pitch = _sized(out, "out", _DTYPE, device, m, n)
+    _check(lib.apc_matmul_fp8(ctypes.byref(p), ctypes.byref(q), m, n, k, out.data_ptr(), pitch, kind, _stream(stream, device)))
     return out
 
 
 def _distill(logits, ids, teacher, temperature, kd_weight, teacher_lse, labels, label_weight, device) -> _Distill:
-    pitch = _matrix(logits, "logits", _DTYPE, device)
-    rows, vocab = logits.shape
-    ids_pitch = _matrix(ids, "ids", _INDEX, device)
-    k = ids.shape[1]
-    teacher_pitch = _matrix(teacher, "teacher", _DTYPE, device, (rows, k))
-    if ids.shape[0] != rows:
-        raise ValueError("ids has %d rows and the logits %d" % (ids.shape[0], rows))
+    kind, rows, vocab, pitch = _matrix(logits, "logits", _DTYPE, device)
+    ids_kind, ids_rows, k, ids_pitch = _matrix(ids, "ids", _INDEX, device)
+    teacher_kind, teacher_pitch = _sized(teacher, "teacher", _DTYPE, device, rows, k)
+    if ids_rows != rows:
+        raise ValueError("ids has %d rows and the logits %d" % (ids_rows, rows))
     return _Distill(
         logits.data_ptr(), ids.data_ptr(), teacher.data_ptr(),
         None if teacher_lse is None else _vector(teacher_lse, "teacher_lse", _F32, device, rows),
         None if labels is None else _vector(labels, "labels", _INDEX, device, rows),
-        rows, vocab, k, pitch, ids_pitch, teacher_pitch, _DTYPE[logits.dtype], _INDEX[ids.dtype],
-        _DTYPE[teacher.dtype], 0 if labels is None else _INDEX[labels.dtype], temperature, kd_weight, label_weight)
+        rows, vocab, k, pitch, ids_pitch, teacher_pitch, kind, ids_kind, teacher_kind,
+        0 if labels is None else _INDEX[labels.dtype], temperature, kd_weight, label_weight)
 
 
-def _lse_room(lse, logits, labels, device):
+def _lse_room(lse, logits, labels, device, rows):
     n = 1 if labels is None else 2
     if lse is None:
-        lse = torch.empty(n, logits.shape[0], dtype=torch.float32, device=logits.device)
-    return lse, _vector(lse, "lse", _F32, device, n * logits.shape[0])
+        lse = torch.empty(n, rows, dtype=torch.float32, device=logits.device)
+    return lse, _vector(lse, "lse", _F32, device, n * rows)
 
 
-def _dlogits_room(out, logits, device):
+def _dlogits_room(out, logits, device, d):
     if out is None:
         out = torch.empty_like(logits, memory_format=torch.contiguous_format)
-    return out, _matrix(out, "out", {logits.dtype: 0}, device, tuple(logits.shape))
+    return out, _sized(out, "out", {logits.dtype: 0}, device, d.rows, d.vocab)[1]
 
 
 def distill_loss(logits, ids, teacher, *, temperature=1.0, kd_weight=1.0, teacher_lse=None, labels=None,
@@ -213,12 +229,12 @@ def distill_loss(logits, ids, teacher, *, temperature=1.0, kd_weight=1.0, teache
     Returns ``(loss, lse)``: fp32 ``[rows]``, and the statistics that
     :func:`distill_grad` takes, fp32 ``[1 or, with labels, 2, rows]``."""
     lib = _library()
-    device = torch.cuda.current_device()
+    device = _current_device()
     d = _distill(logits, ids, teacher, temperature, kd_weight, teacher_lse, labels, label_weight, device)
     if loss is None:
         loss = torch.empty(d.rows, dtype=torch.float32, device=logits.device)
-    lse, at = _lse_room(lse, logits, labels, device)
-    _call(lib.apc_distill_loss, ctypes.addressof(d), _vector(loss, "loss", _F32, device, d.rows), at, _stream(stream))
+    lse, at = _lse_room(lse, logits, labels, device, d.rows)
+    _check(lib.apc_distill_loss(ctypes.byref(d), _vector(loss, "loss", _F32, device, d.rows), at, _stream(stream, device)))
     return loss, lse
 
 
@@ -229,12 +245,12 @@ def distill_grad(logits, ids, teacher, lse, grad_loss, *, temperature=1.0, kd_we
     Rows with a ``grad_loss`` of 0 get zeros.  Returns it in the logits' type,
     or in ``out``, which may be ``logits`` itself."""
     lib = _library()
-    device = torch.cuda.current_device()
+    device = _current_device()
     d = _distill(logits, ids, teacher, temperature, kd_weight, teacher_lse, labels, label_weight, device)
-    out, pitch = _dlogits_room(out, logits, device)
-    lse, at = _lse_room(lse, logits, labels, device)
-    _call(lib.apc_distill_grad, ctypes.addressof(d), at, _vector(grad_loss, "grad_loss", _F32, device, d.rows),
-          out.data_ptr(), pitch, _stream(stream))
+    out, pitch = _dlogits_room(out, logits, device, d)
+    lse, at = _lse_room(lse, logits, labels, device, d.rows)
+    _check(lib.apc_distill_grad(ctypes.byref(d), at, _vector(grad_loss, "grad_loss", _F32, device, d.rows), out.data_ptr(),
+                                pitch, _stream(stream, device)))
     return out
 
 
@@ -244,12 +260,13 @@ def distill_loss_grad(logits, ids, teacher, grad_loss, *, temperature=1.0, kd_we
     the logits, for a ``grad_loss`` known before the loss (a mean's weights, a
     loss scale).  Returns ``(loss, lse, dlogits)``."""
     lib = _library()
-    device = torch.cuda.current_device()
+    device = _current_device()
     d = _distill(logits, ids, teacher, temperature, kd_weight, teacher_lse, labels, label_weight, device)
     if loss is None:
         loss = torch.empty(d.rows, dtype=torch.float32, device=logits.device)
-    lse, at = _lse_room(lse, logits, labels, device)
-    out, pitch = _dlogits_room(out, logits, device)
-    _call(lib.apc_distill_loss_grad, ctypes.addressof(d), _vector(grad_loss, "grad_loss", _F32, device, d.rows),
-          _vector(loss, "loss", _F32, device, d.rows), at, out.data_ptr(), pitch, _stream(stream))
+    lse, at = _lse_room(lse, logits, labels, device, d.rows)
+    out, pitch = _dlogits_room(out, logits, device, d)
+    _check(lib.apc_distill_loss_grad(ctypes.byref(d), _vector(grad_loss, "grad_loss", _F32, device, d.rows),
+                                     _vector(loss, "loss", _F32, device, d.rows), at, out.data_ptr(), pitch,
+                                     _stream(stream, device)))
     return loss, lse, out
