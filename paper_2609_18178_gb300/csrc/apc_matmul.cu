@@ -64,7 +64,7 @@ constexpr int kScaleSlots = 8;  // blocks whose scales are on their way or in us
 // A wait that gives up marks the CTA dead: it stops loading and issuing, waits for
 // what is in flight, and its sums go on without waiting, so that every barrier is
 // reached.
-constexpr int kMidThreads = 224;
+constexpr int kMidThreads = 384;  // copies, products, scales, products; 8 warps that add
 
 template <int BN, bool SPLIT>
 struct MidShape {
@@ -79,6 +79,10 @@ struct MidShape {
   // many times as long as either
   static constexpr int kAcc = 512 / BN < 8 ? 512 / BN : 8;
   static constexpr int kTmem = kAcc * BN;
+  // a warp adds half the columns, and few of them of several blocks at a time:
+  // their waits and loads overlap
+  static constexpr int kCols = BN / 2, kGroup = BN == 16 ? 4 : BN == 32 ? 2 : 1;
+  static constexpr int kLoad = kCols < 32 ? kCols : 32;
 };
 
 template <int BN, bool SPLIT, typename T>
@@ -105,10 +109,10 @@ __global__ void __launch_bounds__(kMidThreads, 1)
   if (threadIdx.x == 32) prefetch_map(&map_r), prefetch_map(&map_c);
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kStages; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
-    for (int i = 0; i < S::kAcc; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 4);
-    for (int i = 0; i < kScaleSlots; ++i) mbar_init(&scale_full[i], 32), mbar_init(&scale_empty[i], 4);
+    for (int i = 0; i < S::kAcc; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 8);
+    for (int i = 0; i < kScaleSlots; ++i) mbar_init(&scale_full[i], 32), mbar_init(&scale_empty[i], 8);
     mbar_init(&recv_full, 1);
-    mbar_init(&recv_free, 4 * split);
+    mbar_init(&recv_free, 8 * split);
     dead = 0;
     mbar_init_fence();
   }
@@ -143,7 +147,10 @@ __global__ void __launch_bounds__(kMidThreads, 1)
     }
     if (!ok)  // let the copies in flight land
       for (uint32_t i = min(issued, (uint32_t)S::kStages); i; --i) st.back(), wait_for(&full[st.at], st.phase);
-  } else if (warp == 1) {
+  } else if (warp == 1 || warp == 3) {
+    // two warps issue every other block's products: the waits and the issue of one
+    // take longer (450 cycles) than its bytes should
+    const uint32_t parity = warp == 3;
     Turn<S::kStages> st;
     Turn<S::kAcc> acc;
     uint32_t issued = 0;
@@ -151,6 +158,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
     const uint64_t r_desc = operand_desc(smem_addr(smem)), c_desc = operand_desc(smem_addr(smem) + S::kRowBytes);
     for (uint32_t t = first; t < tiles && ok; t += step)
       for (uint32_t b = b0; b < b1; ++b, st.next(), acc.next(), ++issued) {
+        if ((issued & 1) != parity) continue;
         if (!(ok = alive(&acc_empty[acc.at], acc.phase ^ 1) && alive(&full[st.at], st.phase))) break;
         tc_fence_after();
         const uint64_t off = st.at * (S::kStageBytes >> 4);
@@ -158,7 +166,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
       }
     if (!ok)  // let the products in flight end
       for (uint32_t i = min(issued, (uint32_t)S::kAcc); i; --i) acc.back(), wait_for(&acc_full[acc.at], acc.phase);
-  } else if (warp == 6) {
+  } else if (warp == 2) {
     Turn<kScaleSlots> slot;
     for (uint32_t t = first; t < tiles && !dead; t += step) {
       const uint32_t r0 = t % p.row_tiles * 128 + lane, c0 = t / p.row_tiles * BN + lane;
@@ -176,73 +184,95 @@ __global__ void __launch_bounds__(kMidThreads, 1)
     }
     words_landed();
   } else {
-    const uint32_t quad = warp & 3, row = quad * 32 + lane;
+    constexpr int kCols = S::kCols, kGroup = S::kGroup, kLoad = S::kLoad;
+    const uint32_t quad = warp & 3, row = quad * 32 + lane, half = (warp - 4) / 4;
     Turn<S::kAcc> buf;
     Turn<kScaleSlots> slot;
     uint32_t done = 0;
-    if (SPLIT && threadIdx.x == 64) mbar_arrive_expect_tx(&recv_full, S::kShareBytes);
+    if (SPLIT && threadIdx.x == 128) mbar_arrive_expect_tx(&recv_full, S::kShareBytes);
     for (uint32_t t = first; t < tiles; t += step, ++done) {
       const uint32_t r0 = t % p.row_tiles * 128, c0 = t / p.row_tiles * BN;
-      uint64_t acc[BN / 2];
+      uint64_t acc[kCols / 2];
 #pragma unroll
-      for (int i = 0; i < BN / 2; ++i) acc[i] = 0;
-      for (uint32_t b = b0; b < b1; ++b, buf.next(), slot.next()) {
-        const float *s = scales + slot.at * (128 + BN) + 128;
-        alive(&scale_full[slot.at], slot.phase);
-        const float one = s[(int)row - 128];
-        const uint64_t sr = pack2(one, one);
-        alive(&acc_full[buf.at], buf.phase);
+      for (int i = 0; i < kCols / 2; ++i) acc[i] = 0;
+      for (uint32_t b = b0; b < b1; b += kGroup) {
+        const uint32_t n = min((uint32_t)kGroup, b1 - b);
+        uint32_t at[kGroup], bar[kGroup];
+        uint64_t sr[kGroup];
+        const float *s[kGroup];
+#pragma unroll
+        for (int g = 0; g < kGroup; ++g) {
+          if (g >= n) break;
+          alive(&scale_full[slot.at], slot.phase);
+          const float *line = scales + slot.at * (128 + BN);
+          s[g] = line + 128 + half * kCols;
+          sr[g] = pack2(line[row], line[row]);
+          alive(&acc_full[buf.at], buf.phase);
+          at[g] = tmem + buf.at * BN + half * kCols + (quad << 21);  // lane 32 * quad in bits 16 up
+          bar[g] = buf.at | slot.at << 16;
+          buf.next(), slot.next();
+        }
         tc_fence_after();
-        const uint32_t at = tmem + buf.at * BN + (quad << 21);  // lane 32 * quad in bits 16 up
-        constexpr int kChunk = BN < 32 ? 16 : 32;
 #pragma unroll
-        for (int c = 0; c < BN; c += kChunk) {
-          uint32_t d[kChunk];
-          tmem_load(d, at + c);
-          tmem_landed(d);
-          if (c + kChunk == BN) {
+        for (int c = 0; c < kCols; c += kLoad) {
+          uint32_t d[kGroup][kLoad];
+#pragma unroll
+          for (int g = 0; g < kGroup; ++g)
+            if (g < n) tmem_load(d[g], at[g] + c);
+#pragma unroll
+          for (int g = 0; g < kGroup; ++g) tmem_landed(d[g]);
+          if (c + kLoad == kCols) {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&acc_empty[buf.at]);
+#pragma unroll
+            for (int g = 0; g < kGroup; ++g)
+              if (lane == 0 && g < n) mbar_arrive(&acc_empty[bar[g] & 0xffff]);
           }
 #pragma unroll
-          for (int i = 0; i < kChunk; i += 4) {
-            const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(s + c + i);
-            acc[(c + i) / 2] = fma2(pack2(d[i], d[i + 1]), mul2(sr, v.x), acc[(c + i) / 2]);
-            acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), mul2(sr, v.y), acc[(c + i) / 2 + 1]);
+          for (int g = 0; g < kGroup; ++g) {
+            if (g >= n) break;
+#pragma unroll
+            for (int i = 0; i < kLoad; i += 4) {
+              const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(s[g] + c + i);
+              acc[(c + i) / 2] = fma2(pack2(d[g][i], d[g][i + 1]), mul2(sr[g], v.x), acc[(c + i) / 2]);
+              acc[(c + i) / 2 + 1] = fma2(pack2(d[g][i + 2], d[g][i + 3]), mul2(sr[g], v.y), acc[(c + i) / 2 + 1]);
+            }
           }
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(&scale_empty[slot.at]);
+#pragma unroll
+        for (int g = 0; g < kGroup; ++g)
+          if (lane == 0 && g < n) mbar_arrive(&scale_empty[bar[g] >> 16]);
       }
       T *out = static_cast<T *>(p.out) + (int64_t)(r0 + row) * p.row_step;
       const bool in = r0 + row < p.rows;
       if (!SPLIT) {
+        const uint32_t c1 = c0 + half * kCols;
 #pragma unroll
-        for (int i = 0; i < BN; ++i) {
+        for (int i = 0; i < kCols; ++i) {
           const float2 v = unpack2(acc[i / 2]);
-          if (in && c0 + i < p.cols) out[(int64_t)(c0 + i) * p.col_step] = from_float<T>(i % 2 ? v.y : v.x);
+          if (in && c1 + i < p.cols) out[(int64_t)(c1 + i) * p.col_step] = from_float<T>(i % 2 ? v.y : v.x);
         }
         continue;
       }
       // a share to each CTA of the cluster, once all have read the tile before
       if (done) alive(&recv_free, (done + 1) & 1);
 #pragma unroll
-      for (int i = 0; i < BN; ++i) {
+      for (int i = 0; i < kCols; ++i) {
         const float2 v = unpack2(acc[i / 2]);
-        share[i * 128 + row] = i % 2 ? v.y : v.x;
+        share[(half * kCols + i) * 128 + row] = i % 2 ? v.y : v.x;
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      asm volatile("bar.sync 1, 128;" ::: "memory");
+      asm volatile("bar.sync 1, 256;" ::: "memory");
       const uint32_t per = 1u << (kLog2Bn - split_log2);  // columns that a CTA owns
-      if (threadIdx.x - 64 < split) {
-        const uint32_t owner = threadIdx.x - 64;
+      if (threadIdx.x - 128 < split) {
+        const uint32_t owner = threadIdx.x - 128;
         bulk_s2s(map_rank(smem_addr(recv + rank * per * 128), owner), smem_addr(share + owner * per * 128), per * 512,
                  map_rank(smem_addr(&recv_full), owner));
       }
       alive(&recv_full, done & 1);
-      if (threadIdx.x == 64) mbar_arrive_expect_tx(&recv_full, S::kShareBytes);
-      for (uint32_t c = 0; c < per; ++c) {
+      if (threadIdx.x == 128) mbar_arrive_expect_tx(&recv_full, S::kShareBytes);
+      for (uint32_t c = half * (per / 2); c < (half + 1) * (per / 2); ++c) {
         float sum = recv[c * 128 + row];
         for (uint32_t k = 1; k < split; ++k) sum += recv[(k * per + c) * 128 + row];
         const uint32_t col = c0 + rank * per + c;
