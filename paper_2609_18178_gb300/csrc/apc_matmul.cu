@@ -311,7 +311,8 @@ constexpr int kBigThreads = 128 + 32 * kBigWarps, kBigStages = APC_BIG_STAGES;
 constexpr int kBigCols = 1024 / kBigWarps;  // columns that a warp adds up
 constexpr int kBigHalf = 128 * kBlock, kBigStageBytes = 2 * kBigHalf;
 constexpr int kBigScaleBytes = kScaleSlots * (128 + 256) * 4;
-constexpr int kBigBytes = 1024 + kBigStages * kBigStageBytes + kBigScaleBytes;
+constexpr int kBigTurnBytes = 32 * 17 * 4;  // a warp's, for rows of out that are not aligned
+constexpr int kBigBytes = 1024 + kBigStages * kBigStageBytes + kBigScaleBytes + kBigWarps * kBigTurnBytes;
 constexpr uint32_t kBigGroup = 16;  // row tiles that are walked together
 
 // Tile t of the walk: groups of row tiles, in each the row tile first, so that
@@ -323,10 +324,19 @@ __device__ __forceinline__ void big_tile(const ProductPlan &p, uint32_t t, uint3
   *c = i / height;
 }
 
-template <typename T>
-__device__ __forceinline__ void store_row(T *out, const uint64_t (&acc)[kBigCols / 2], uint32_t count) {
+// A warp's 32 rows of kBigCols sums, a row a lane, to out (this lane's row), of which
+// `count` columns and, where `in`, the row exist.  Rows that start on 16-byte
+// boundaries are stored by their lanes; others go through shared memory, 16 columns
+// at a time, so that a store instruction writes two rows' neighbours and not 32
+// rows' single elements.
+constexpr int kTurnCols = 16, kTurnPitch = kTurnCols + 1;
+
+template <bool ALIGNED, typename T>
+__device__ __forceinline__ void store_rows(T *out, const uint64_t (&acc)[kBigCols / 2], uint32_t count, bool in, int64_t step,
+                                           float *turn, uint32_t lane) {
   constexpr int kPer = 16 / sizeof(T);
-  if (count == kBigCols && (uintptr_t)out % 16 == 0) {
+  if constexpr (ALIGNED) {
+    if (!in) return;
 #pragma unroll
     for (int i = 0; i < kBigCols; i += kPer) {
       union {
@@ -339,20 +349,38 @@ __device__ __forceinline__ void store_row(T *out, const uint64_t (&acc)[kBigCols
         u.v[j] = from_float<T>(v.x);
         u.v[j + 1] = from_float<T>(v.y);
       }
-      *reinterpret_cast<uint4 *>(out + i) = u.q;
-    }
-  } else {
+      if (i + kPer <= count) {
+        *reinterpret_cast<uint4 *>(out + i) = u.q;
+      } else {
 #pragma unroll
-    for (int i = 0; i < kBigCols / 2; ++i) {
-      const float2 v = unpack2(acc[i]);
-      if (2 * i < count) out[2 * i] = from_float<T>(v.x);
-      if (2 * i + 1 < count) out[2 * i + 1] = from_float<T>(v.y);
+        for (int j = 0; j < kPer; ++j)
+          if (i + j < count) out[i + j] = u.v[j];
+      }
     }
+    return;
+  }
+  const uint32_t rows = __ballot_sync(~0u, in);
+  T *first = out - (int64_t)lane * step;  // lane 0's row
+#pragma unroll
+  for (int c = 0; c < kBigCols; c += kTurnCols) {
+#pragma unroll
+    for (int i = 0; i < kTurnCols; i += 2) {
+      const float2 v = unpack2(acc[(c + i) / 2]);
+      turn[lane * kTurnPitch + i] = v.x;
+      turn[lane * kTurnPitch + i + 1] = v.y;
+    }
+    __syncwarp();
+    const uint32_t col = lane % kTurnCols;
+#pragma unroll 4
+    for (uint32_t r = lane / kTurnCols; r < 32; r += 32 / kTurnCols)
+      if ((rows >> r & 1) && c + col < count) first[(int64_t)r * step + c + col] = from_float<T>(turn[r * kTurnPitch + col]);
+    __syncwarp();
   }
 }
 
-// ROWS: the scales of b change from column to column.
-template <typename T, bool ROWS>
+// ROWS: the scales of b change from column to column.  ALIGNED: every row of out
+// starts on a 16-byte boundary.
+template <typename T, bool ROWS, bool ALIGNED>
 __global__ void __launch_bounds__(kBigThreads, 1)
     big_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ ProductPlan p) {
@@ -452,6 +480,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kBigWarps == 8 ? 224 : 112));
     const uint32_t quad = warp & 3, part = (warp - 4) / 4, row = quad * 32 + lane;
     const uint32_t empty_bars = map_rank(smem_addr(acc_empty), 0);
+    float *turn = scales + kBigScaleBytes / 4 + (warp - 4) * (kBigTurnBytes / 4);
     Turn<2> buf;
     Turn<kScaleSlots> slot;
     bool ok = true;
@@ -503,8 +532,9 @@ __global__ void __launch_bounds__(kBigThreads, 1)
         if (lane == 0) mbar_arrive(&scale_empty[slot.at]);
       }
       if (!ok) break;
-      if (r0 + row < p.rows && c0 < p.cols)
-        store_row(static_cast<T *>(p.out) + (int64_t)(r0 + row) * p.row_step + c0, acc, min((uint32_t)kBigCols, p.cols - c0));
+      if (c0 < p.cols)
+        store_rows<ALIGNED>(static_cast<T *>(p.out) + (int64_t)(r0 + row) * p.row_step + c0, acc, min((uint32_t)kBigCols, p.cols - c0),
+                   r0 + row < p.rows, p.row_step, turn, lane);
     }
     if (!ok) give_up(p.status);
   }
@@ -554,8 +584,36 @@ int launch_cluster(K kernel, unsigned grid, unsigned threads, unsigned smem, uns
 
 uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
+// Which kernel, and for few columns how many and how far k is split: the least of
+// the estimated times, in nanoseconds, of measured parts (one GB300, 152 SMs):
+//   a block of 128 k takes a CTA 270, 330, 385 and 535 ns with 16, 32, 64 and 128
+//   columns, a pair 435 ns with a tile of 256 x 256;
+//   a cluster's exchange 2.2, 3 and 6.5 us for 2, 4 and 8 CTAs; a call 4 us beside
+//   that, 8 with pairs.
+// For example 100 x 4096 x 4096: 64 columns in two halves 13.8 us, whole 16.7, tiles
+// of 128 22.0, of 256 x 256 19.6; 512 x 4096 x 4096: 30.7, 22.6 and 20.8 with tiles
+// of 64, 128 and 256.  By sizes and the GPU's SMs alone: the cap of a grid does not
+// change results.
+struct Choice {
+  uint32_t cols, split_log2;  // cols 256: the pairs' kernel
+};
+
+Choice choose(uint32_t m, uint32_t n, uint32_t blocks, uint32_t sms) {
+  static constexpr uint32_t kBlockNs[4] = {270, 330, 385, 535}, kExchangeNs[4] = {0, 2200, 3000, 6500};
+  const uint64_t pairs = sms / 2 ? sms / 2 : 1;
+  Choice best = {256, 0};
+  uint64_t least = 8000 + ceil_div((uint64_t)ceil_div(m, 256) * ceil_div(n, 256), pairs) * ((uint64_t)blocks * 435 + 1000);
+  for (uint32_t c = 0; c < 4; ++c)
+    for (uint32_t s = 0; s <= (c == 3 ? 0u : 3u) && (1u << s) <= blocks && (1u << s) <= sms; ++s) {
+      const uint64_t tiles = (uint64_t)ceil_div(n, 128) * ceil_div(m, 16u << c);
+      const uint64_t t = 4000 + ceil_div(tiles, sms >> s) * ((uint64_t)ceil_div(blocks, 1u << s) * kBlockNs[c] + kExchangeNs[s]);
+      if (t < least) least = t, best = {16u << c, s};
+    }
+  return best;
+}
+
 template <int BN, typename T>
-int launch_mid(const MatmulArgs &a, ProductPlan p, unsigned cap, unsigned sms, void *stream) {
+int launch_mid(const MatmulArgs &a, ProductPlan p, uint32_t best, unsigned cap, void *stream) {
   p.r_scale = a.b_scale, p.c_scale = a.a_scale;
   p.r_scale_pitch = a.b_scale_pitch, p.c_scale_pitch = a.a_scale_pitch;
   p.r_shift = a.b_shift, p.c_shift = a.a_shift;
@@ -568,14 +626,6 @@ int launch_mid(const MatmulArgs &a, ProductPlan p, unsigned cap, unsigned sms, v
   if (!e) e = encode(&c, a.a, a.m, a.k, a.a_pitch, BN);
   if (e) return e;
   const uint64_t tiles = (uint64_t)p.row_tiles * p.col_tiles;
-  // the split that leaves the least to the CTA with the most to do, a cluster's
-  // exchange counting as three blocks; it follows the sizes and the GPU, not the cap
-  uint32_t best = 0;
-  uint64_t best_cost = UINT64_MAX;
-  for (uint32_t s = 0; s <= (BN == 128 ? 0 : 3) && (1u << s) <= p.blocks; ++s) {
-    const uint64_t cost = (uint64_t)ceil_div(tiles, sms >> s) * (ceil_div(p.blocks, 1u << s) + (s ? 3 : 1));
-    if (cost < best_cost) best = s, best_cost = cost;
-  }
   const uint64_t clusters = tiles < (cap >> best) ? tiles : (cap >> best);
   const unsigned grid = (unsigned)(clusters ? clusters : 1) << best;
   if (BN < 128 && best)
@@ -592,14 +642,17 @@ int launch_big(const MatmulArgs &a, ProductPlan p, unsigned cap, void *stream) {
   p.row_tiles = ceil_div(a.m, 256), p.col_tiles = ceil_div(a.n, 256);
   p.instruction = 1u << 4 | a.a_e5m2 << 7 | a.b_e5m2 << 10 | (256u >> 3) << 17 | (256u >> 4) << 24;
   p.row_step = a.out_pitch, p.col_step = 1;
+  const uint64_t size = a.out_dtype == APC_F32 ? 4 : 2;
+  const bool aligned = (uintptr_t)a.out % 16 == 0 && (a.m <= 1 || (uint64_t)a.out_pitch * size % 16 == 0);
   CUtensorMap ma, mb;
   int e = encode(&ma, a.a, a.m, a.k, a.a_pitch, 128);
   if (!e) e = encode(&mb, a.b, a.n, a.k, a.b_pitch, 128);
   if (e) return e;
   const uint64_t tiles = (uint64_t)p.row_tiles * p.col_tiles, pairs = cap >= 2 ? cap / 2 : 1;
   const unsigned grid = (unsigned)(tiles < pairs ? tiles : pairs) * 2;
-  return a.b_shift ? launch_cluster(big_kernel<T, false>, grid, kBigThreads, kBigBytes, 2, stream, ma, mb, p)
-                   : launch_cluster(big_kernel<T, true>, grid, kBigThreads, kBigBytes, 2, stream, ma, mb, p);
+  auto go = [&](auto kernel) { return launch_cluster(kernel, grid, kBigThreads, kBigBytes, 2, stream, ma, mb, p); };
+  if (aligned) return a.b_shift ? go(big_kernel<T, false, true>) : go(big_kernel<T, true, true>);
+  return a.b_shift ? go(big_kernel<T, false, false>) : go(big_kernel<T, true, false>);
 }
 
 }  // namespace
@@ -614,14 +667,16 @@ int launch_matmul(const MatmulArgs &a, unsigned cap, unsigned sms, void *stream)
   p.out = a.out;
   int e = commit_status_word(&p.status);
   if (e) return e;
+  const Choice c = choose(a.m, a.n, p.blocks, sms);
   return with_dtype(a.out_dtype, [&](auto t) {
     using T = decltype(t);
-    if (a.m > 128 && (uint64_t)ceil_div(a.m, 256) * ceil_div(a.n, 256) >= sms / 4) return launch_big<T>(a, p, cap, stream);
-    if (a.m <= 16) return launch_mid<16, T>(a, p, cap, sms, stream);
-    if (a.m <= 32) return launch_mid<32, T>(a, p, cap, sms, stream);
-    // 64 columns a tile until tiles of 128 fill the GPU
-    if (a.m <= 64 || (uint64_t)ceil_div(a.n, 128) * ceil_div(a.m, 128) < sms) return launch_mid<64, T>(a, p, cap, sms, stream);
-    return launch_mid<128, T>(a, p, cap, sms, stream);
+    switch (c.cols) {
+      case 16: return launch_mid<16, T>(a, p, c.split_log2, cap, stream);
+      case 32: return launch_mid<32, T>(a, p, c.split_log2, cap, stream);
+      case 64: return launch_mid<64, T>(a, p, c.split_log2, cap, stream);
+      case 128: return launch_mid<128, T>(a, p, c.split_log2, cap, stream);
+    }
+    return launch_big<T>(a, p, cap, stream);
   });
 }
 
