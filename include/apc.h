@@ -260,7 +260,7 @@ typedef struct apc_fp8_matrix {
  *           division is exact, so q is the same on every machine
  * Non-finite values do not enter the scale: a NaN becomes a NaN, an infinity a
  * NaN in E4M3 (which has no infinities) and an infinity in E5M2.
- * q and qt take the same block_rows; their formats may differ.
+ * q and qt take the same block_rows and format.
  * Returns APC_EINVAL (null or overlapping buffers, unknown types, a pitch below
  * the width, memory of another device), APC_EALIGN (x not aligned to its
  * element; data or its pitch not to 16 bytes; scale not to 4), APC_ERANGE

@@ -25,9 +25,10 @@ __device__ __forceinline__ __half from_float<__half>(float x) { return __float2h
 
 // Two values to 8 bits each, nearest even, `lo` in the low byte.  The
 // instruction saturates: infinities are the caller's.
-__device__ __forceinline__ uint32_t to_fp8x2(float lo, float hi, bool e5m2) {
+template <bool E5M2>
+__device__ __forceinline__ uint32_t to_fp8x2(float lo, float hi) {
   uint16_t r;
-  if (e5m2) asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  if (E5M2) asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   else asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }

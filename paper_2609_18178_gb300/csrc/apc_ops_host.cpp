@@ -86,8 +86,9 @@ APC_EXPORT apc_status apc_quantize_fp8(const void *x, int64_t rows, int64_t cols
   if ((st = check_fp8("q", q, rows, cols, true, &rs)) != APC_OK) return st;
   if (qt) {
     if ((st = check_fp8("qt", qt, cols, rows, true, &rs)) != APC_OK) return st;
-    if (qt->block_rows != q->block_rows)
-      return op_fail(APC_EINVAL, "q and qt have block_rows of %u and %u", q->block_rows, qt->block_rows);
+    if (qt->block_rows != q->block_rows || qt->format != q->format)
+      return op_fail(APC_EINVAL, "q and qt differ in block_rows (%u, %u) or format (%u, %u)", q->block_rows, qt->block_rows,
+                     q->format, qt->format);
   }
   if (rows == 0 || cols == 0) return APC_OK;
   if ((st = apc::op_ranges(rs.r, rs.n)) != APC_OK) return st;

@@ -10,6 +10,7 @@
 #include <cuda_runtime.h>
 
 #include "apc_ops.cuh"
+#include "apc_tcgen05.cuh"
 
 namespace apc {
 
@@ -76,9 +77,10 @@ __device__ __forceinline__ uint32_t larger(uint32_t w) {
 // The exponent e of the scale, biased by 127: 2^e * largest >= amax > 2^(e-1) *
 // largest.  The largest value is 1.75 * 2^8 (E4M3) or 1.75 * 2^15 (E5M2), so only
 // fractions above 1.75 need the next power.
-__device__ __forceinline__ uint32_t scale_exponent(float amax, bool e5m2) {
+template <bool E5M2>
+__device__ __forceinline__ uint32_t scale_exponent(float amax) {
   const uint32_t b = __float_as_uint(amax) + 0x1fffffu;  // carries into the exponent above a fraction of 1.75
-  const int e = (int)(b >> 23) - (e5m2 ? 15 : 8);        // a subnormal amax is below 2^-126 * largest as it is
+  const int e = (int)(b >> 23) - (E5M2 ? 15 : 8);        // a subnormal amax is below 2^-126 * largest as it is
   return amax == 0.0f ? 127u : (uint32_t)max(e, 1);
 }
 
@@ -86,29 +88,23 @@ __device__ __forceinline__ float power(uint32_t biased) { return __uint_as_float
 // 2^-e: 2^127 (e = -127) does not occur, 2^-126 does.
 __device__ __forceinline__ float inverse_power(uint32_t biased) { return __uint_as_float((254u - biased) << 23); }
 
-// The 8-bit value of a non-finite x; sign kept.
-__device__ __forceinline__ uint32_t non_finite(float x, bool e5m2) {
-  const uint32_t b = __float_as_uint(x);
-  return (e5m2 && (b & 0x7fffffffu) == 0x7f800000u ? 0x7cu : 0x7fu) | (b >> 24 & 0x80u);
+// The 8-bit value of x times a power of two; non-finite values with their sign.
+template <bool E5M2>
+__device__ __forceinline__ uint8_t any_to_fp8(float x, float inv) {
+  const uint32_t b = __float_as_uint(x), m = b & 0x7fffffffu;
+  if (m >= 0x7f800000u) return (uint8_t)((E5M2 && m == 0x7f800000u ? 0x7cu : 0x7fu) | (b >> 24 & 0x80u));
+  return (uint8_t)to_fp8x2<E5M2>(x * inv, 0.0f);
 }
 
-// Two values to 8 bits, x0 in the low byte.  AWKWARD: they may be non-finite.
-template <bool AWKWARD>
-__device__ __forceinline__ uint32_t pair_to_fp8(float x0, float x1, float inv0, float inv1, bool e5m2) {
-  uint32_t r = to_fp8x2(x0 * inv0, x1 * inv1, e5m2);
-  if (AWKWARD) {
-    if (!(fabsf(x0) <= 3.402823466e38f)) r = (r & 0xff00u) | non_finite(x0, e5m2);
-    if (!(fabsf(x1) <= 3.402823466e38f)) r = (r & 0xffu) | non_finite(x1, e5m2) << 8;
-  }
-  return r;
-}
-
-// 8 values in a row, little-endian.
-template <typename T, bool AWKWARD>
-__device__ __forceinline__ uint2 row_to_fp8(const uint32_t *w, float inv, bool e5m2) {
+// Pairs (lo, hi) of finite values times inv, 8 in a row, little-endian.
+template <bool E5M2>
+__device__ __forceinline__ uint2 to_fp8x8(const uint64_t (&v)[4], uint64_t inv) {
   uint32_t h[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = pair_to_fp8<AWKWARD>(element<T>(w, 2 * i), element<T>(w, 2 * i + 1), inv, inv, e5m2);
+  for (int i = 0; i < 4; ++i) {
+    const float2 y = unpack2(mul2(v[i], inv));
+    h[i] = to_fp8x2<E5M2>(y.x, y.y);
+  }
   return {__byte_perm(h[0], h[1], 0x5410), __byte_perm(h[2], h[3], 0x5410)};
 }
 
@@ -148,9 +144,12 @@ __device__ __forceinline__ void store8(uint8_t *at, uint2 v, int n) {
 // ---------------------------------------------------------------------------
 // Rows alone.  The blocks of the whole matrix in row order; half a warp takes
 // one, 8 elements a lane, kRowUnroll of them in flight.
-constexpr int kRowThreads = 256, kRowUnroll = 4;
+#ifndef APC_ROW_UNROLL
+#define APC_ROW_UNROLL 2
+#endif
+constexpr int kRowThreads = 256, kRowUnroll = APC_ROW_UNROLL;
 
-template <typename T>
+template <typename T, bool E5M2>
 __global__ void __launch_bounds__(kRowThreads) rows_kernel(const T *x, int64_t pitch, uint32_t rows, uint32_t cols, QuantOut q,
                                                            bool wide) {
   constexpr int kWords = 8 / Word<T>::kPer;
@@ -160,14 +159,17 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(const T *x, int64_t p
   for (uint64_t b0 = ((uint64_t)blockIdx.x * (kRowThreads / 32) + threadIdx.x / 32) * (2 * kRowUnroll); b0 < blocks; b0 += step) {
     uint32_t w[kRowUnroll][kWords], row[kRowUnroll], bc[kRowUnroll];
     int n[kRowUnroll];
+    uint64_t left = blocks - b0;
+    uint32_t r = blocks >> 32 ? (uint32_t)((b0 + side) / across) : (uint32_t)(b0 + side) / across;
+    uint32_t b = (uint32_t)(b0 + side - (uint64_t)r * across);
 #pragma unroll
     for (int u = 0; u < kRowUnroll; ++u) {
-      const uint64_t b = b0 + 2 * u + side;
-      row[u] = blocks >> 32 ? (uint32_t)(b / across) : (uint32_t)b / across;
-      bc[u] = (uint32_t)b - row[u] * across;
-      const uint32_t c = bc[u] * kBlock + c8;
-      n[u] = b < blocks && c < cols ? (int)min(8u, cols - c) : 0;
-      load8<T>(w[u], x + (int64_t)row[u] * pitch + c, n[u], wide);
+      const uint32_t c = b * kBlock + c8;
+      row[u] = r, bc[u] = b;
+      n[u] = 2 * u + side < left && c < cols ? (int)min(8u, cols - c) : 0;
+      load8<T>(w[u], x + (int64_t)r * pitch + c, n[u], wide);
+      b += 2;
+      while (b >= across) b -= across, ++r;
     }
 #pragma unroll
     for (int u = 0; u < kRowUnroll; ++u) {
@@ -178,170 +180,208 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(const T *x, int64_t p
 #pragma unroll
       for (int o = 8; o; o >>= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
       const bool awkward = __any_sync(~0u, top >= inf_bits<T>());
-      if (awkward) {
+      if (awkward) {  // something is not finite
         m = 0;
         for (int i = 0; i < kWords; ++i) m = Word<T>::max(m, finite_abs<T>(w[u][i]));
         top = larger<T>(m);
         for (int o = 8; o; o >>= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
       }
-      const uint32_t e = scale_exponent(bits_to_float<T>(top), q.e5m2);
+      const uint32_t e = scale_exponent<E5M2>(bits_to_float<T>(top));
       const float inv = inverse_power(e);
-      if (c8 == 0 && n[u]) q.scale[(int64_t)bc[u] * q.scale_pitch + row[u]] = power(e);
-      if (n[u])
-        store8(q.data + (int64_t)row[u] * q.pitch + bc[u] * kBlock + c8,
-               awkward ? row_to_fp8<T, true>(w[u], inv, q.e5m2) : row_to_fp8<T, false>(w[u], inv, q.e5m2), n[u]);
+      if (!n[u]) continue;
+      if (c8 == 0) q.scale[(int64_t)bc[u] * q.scale_pitch + row[u]] = power(e);
+      uint8_t *at = q.data + (int64_t)row[u] * q.pitch + bc[u] * kBlock + c8;
+      if (!awkward) {
+        uint64_t v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = pack2(element<T>(w[u], 2 * i), element<T>(w[u], 2 * i + 1));
+        store8(at, to_fp8x8<E5M2>(v, pack2(inv, inv)), n[u]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < n[u]) at[i] = any_to_fp8<E5M2>(element<T>(w[u], i), inv);
+      }
     }
   }
 }
 
 // ---------------------------------------------------------------------------
 // Tiles of 128 x 128.  Thread (tx, ty) holds rows 8 ty + 0..7 of columns 8 tx +
-// 0..7 in registers from one load to both stores.  Row maxima are reduced over the
-// 16 lanes of a row, column maxima through shared memory; the transpose goes
-// through shared memory in 8-byte pieces, swizzled so that neither side meets a
-// bank twice.
+// 0..7 in registers from one load to both stores.  Its maxima of rows and columns go
+// to shared memory, where each row and each column is then one thread's: that
+// thread stores the scale and leaves its inverse.  The transpose goes through
+// shared memory in 8-byte pieces, swizzled so that neither side meets a bank twice.
+#ifndef APC_TILE_CTAS
+#define APC_TILE_CTAS 3
+#endif
 constexpr int kTileThreads = 256;
 
-template <typename T, bool AWKWARD>
-__device__ __forceinline__ void store_tile(const uint32_t (&w)[8][8 / Word<T>::kPer], const uint32_t (&re)[8], const uint32_t (&ce)[8],
-                                           const QuantArgs &a, uint32_t r0, uint32_t c0, uint32_t tx, uint32_t ty, uint2 *turn) {
-  const uint32_t r = r0 + 8 * ty, c = c0 + 8 * tx;
-  const int nc = c < a.cols ? (int)min(8u, a.cols - c) : 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (r + i < a.rows && nc)
-      store8(a.q.data + (int64_t)(r + i) * a.q.pitch + c, row_to_fp8<T, AWKWARD>(w[i], inverse_power(re[i]), a.q.e5m2), nc);
-  if (!a.qt.data) return;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    uint32_t h[4];
-    const float inv = inverse_power(ce[j]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = pair_to_fp8<AWKWARD>(element<T>(w[2 * i], j), element<T>(w[2 * i + 1], j), inv, inv, a.qt.e5m2);
-    turn[(8 * tx + j) * 16 + (ty ^ tx)] = {__byte_perm(h[0], h[1], 0x5410), __byte_perm(h[2], h[3], 0x5410)};
+struct TileShared {
+  uint2 turn[128 * 16];
+  uint32_t col[8][128];  // by warp: column maxima
+  uint32_t row[128];
+  float inv[2][128];     // rows', columns'
+  uint32_t all[8];
+};
+
+// A tile that holds something not finite, element by element: seldom.
+template <typename T, bool SQUARE, bool E5M2>
+__device__ __noinline__ void awkward_tile(const QuantArgs &a, uint32_t tr, uint32_t tc, TileShared &sh) {
+  const uint32_t r0 = tr * kBlock, c0 = tc * kBlock, t = threadIdx.x % 128, side = threadIdx.x / 128;
+  const T *x = static_cast<const T *>(a.x) + (int64_t)r0 * a.pitch + c0;
+  const uint32_t nr = min((uint32_t)kBlock, a.rows - r0), nc = min((uint32_t)kBlock, a.cols - c0);
+  __syncthreads();
+  float top = 0.0f;
+  if (t < (side ? nc : nr))
+    for (uint32_t i = 0; i < (side ? nr : nc); ++i) {
+      const float v = fabsf(to_float(side ? x[(int64_t)i * a.pitch + t] : x[(int64_t)t * a.pitch + i]));
+      if (v <= 3.402823466e38f) top = fmaxf(top, v);
+    }
+  sh.inv[side][t] = top;
+  __syncthreads();
+  if (SQUARE) {
+    for (int i = 0; i < 128; ++i) top = fmaxf(top, sh.inv[0][i]);
+    __syncthreads();
+  }
+  const uint32_t e = scale_exponent<E5M2>(top);
+  sh.inv[side][t] = inverse_power(e);
+  if (SQUARE ? t == 0 : t < (side ? nc : nr)) {
+    if (side == 0) a.q.scale[(int64_t)tc * a.q.scale_pitch + (SQUARE ? tr : r0 + t)] = power(e);
+    else if (a.qt.data) a.qt.scale[(int64_t)tr * a.qt.scale_pitch + (SQUARE ? tc : c0 + t)] = power(e);
   }
   __syncthreads();
-  const uint32_t rr = r0 + 8 * tx;  // now tx counts pieces down a column
-  const int nr = rr < a.rows ? (int)min(8u, a.rows - rr) : 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t col = 16 * i + ty;
-    if (c0 + col < a.cols && nr)
-      store8(a.qt.data + (int64_t)(c0 + col) * a.qt.pitch + rr, turn[col * 16 + (tx ^ col / 8)], nr);
+  for (uint32_t i = threadIdx.x; i < kBlock * kBlock; i += kTileThreads) {
+    const uint32_t r = i / kBlock, c = i % kBlock;
+    if (r >= nr || c >= nc) continue;
+    const float v = to_float(x[(int64_t)r * a.pitch + c]);
+    a.q.data[(int64_t)(r0 + r) * a.q.pitch + c0 + c] = any_to_fp8<E5M2>(v, sh.inv[0][r]);
+    if (a.qt.data) a.qt.data[(int64_t)(c0 + c) * a.qt.pitch + r0 + r] = any_to_fp8<E5M2>(v, sh.inv[1][c]);
   }
 }
 
-template <typename T, bool SQUARE>
-__global__ void __launch_bounds__(kTileThreads, sizeof(T) == 4 ? 2 : 3) tile_kernel(const __grid_constant__ QuantArgs a, bool wide) {
+template <typename T, bool SQUARE, bool E5M2>
+__global__ void __launch_bounds__(kTileThreads, sizeof(T) == 4 ? 2 : APC_TILE_CTAS) tile_kernel(const __grid_constant__ QuantArgs a, bool wide) {
   constexpr int kWords = 8 / Word<T>::kPer;  // words of 8 elements
-  __shared__ uint2 turn[128 * 16];
-  __shared__ __align__(16) uint32_t s_col[8][16 * kWords];
+  __shared__ __align__(16) TileShared sh;
   const uint32_t tx = threadIdx.x % 16, ty = threadIdx.x / 16, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t across = (a.cols + kBlock - 1) / kBlock, down = (a.rows + kBlock - 1) / kBlock;
   for (uint64_t t = blockIdx.x; t < (uint64_t)across * down; t += gridDim.x) {
     const uint32_t tr = (uint32_t)(t / across), tc = (uint32_t)(t % across), r0 = tr * kBlock, c0 = tc * kBlock;
+    const uint32_t r = r0 + 8 * ty, c = c0 + 8 * tx;
+    const int nc = c < a.cols ? (int)min(8u, a.cols - c) : 0;
     uint32_t w[8][kWords];
     {
-      const uint32_t r = r0 + 8 * ty, c = c0 + 8 * tx;
-      const int nc = c < a.cols ? (int)min(8u, a.cols - c) : 0;
       const T *x = static_cast<const T *>(a.x) + (int64_t)r * a.pitch + c;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) load8<T>(w[i], x + (int64_t)i * a.pitch, r + i < a.rows ? nc : 0, wide);
+      for (int i = 0; i < 8; ++i, x += a.pitch) load8<T>(w[i], x, r + i < a.rows ? nc : 0, wide);
     }
-    uint32_t re[8], ce[8];  // exponents of the scales
-    // The maxima of the tile's rows and columns; whether something in it is not finite.
-    auto reduce = [&](auto magnitude) {
-      uint32_t col[kWords], row[8];
+    uint32_t col[kWords], row[8], any = 0;
 #pragma unroll
-      for (int k = 0; k < kWords; ++k) col[k] = 0;
+    for (int k = 0; k < kWords; ++k) col[k] = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        uint32_t m = 0;
+    for (int i = 0; i < 8; ++i) {
+      uint32_t m = 0;
 #pragma unroll
-        for (int k = 0; k < kWords; ++k) {
-          const uint32_t v = magnitude(w[i][k]);
-          col[k] = Word<T>::max(col[k], v);
-          m = Word<T>::max(m, v);
-        }
-        row[i] = larger<T>(m);
+      for (int k = 0; k < kWords; ++k) {
+        const uint32_t v = w[i][k] & Word<T>::kAbs;
+        col[k] = Word<T>::max(col[k], v);
+        m = Word<T>::max(m, v);
       }
-      if (SQUARE) {
-        uint32_t m = row[0];
+      row[i] = larger<T>(m);
+      any = max(any, row[i]);
+    }
+    if (SQUARE) {
+      any = __reduce_max_sync(~0u, any);
+      if (lane == 0) sh.all[warp] = any;
+    } else {
+      // rows: each step halves the rows that a lane still holds and the lanes that hold them
 #pragma unroll
-        for (int i = 1; i < 8; ++i) m = max(m, row[i]);
-        m = __reduce_max_sync(~0u, m);
-        if (lane == 0) s_col[0][warp] = m;
-        __syncthreads();
-        m = s_col[0][lane % 8];
-        m = __reduce_max_sync(~0u, m);
-        const uint32_t eq = scale_exponent(bits_to_float<T>(m), a.q.e5m2), et = scale_exponent(bits_to_float<T>(m), a.qt.e5m2);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) re[i] = eq, ce[i] = et;
-        return m >= inf_bits<T>();
-      }
-      // rows: 16-bit maxima travel in pairs
-      uint32_t top = 0;
-      if (sizeof(T) == 2) {
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-          uint32_t p = row[i] | row[i + 1] << 16;
-#pragma unroll
-          for (int o = 8; o; o >>= 1) p = __vmaxu2(p, __shfl_xor_sync(~0u, p, o));
-          row[i] = p & 0xffffu, row[i + 1] = p >> 16;
-          top = max(top, max(row[i], row[i + 1]));
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-#pragma unroll
-          for (int o = 8; o; o >>= 1) row[i] = max(row[i], __shfl_xor_sync(~0u, row[i], o));
-          top = max(top, row[i]);
-        }
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t keep = lane & 8 ? row[i + 4] : row[i], give = lane & 8 ? row[i] : row[i + 4];
+        row[i] = max(keep, __shfl_xor_sync(~0u, give, 8));
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) re[i] = scale_exponent(bits_to_float<T>(row[i]), a.q.e5m2);
-      // columns
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t keep = lane & 4 ? row[i + 2] : row[i], give = lane & 4 ? row[i] : row[i + 2];
+        row[i] = max(keep, __shfl_xor_sync(~0u, give, 4));
+      }
+      const uint32_t keep = lane & 2 ? row[1] : row[0], give = lane & 2 ? row[0] : row[1];
+      row[0] = max(keep, __shfl_xor_sync(~0u, give, 2));
+      row[0] = max(row[0], __shfl_xor_sync(~0u, row[0], 1));
+      if (!(lane & 1)) sh.row[8 * ty + (lane & 8 ? 4 : 0) + (lane & 4 ? 2 : 0) + (lane & 2 ? 1 : 0)] = row[0];
+      // columns: two rows of threads a warp
 #pragma unroll
       for (int k = 0; k < kWords; ++k) col[k] = Word<T>::max(col[k], __shfl_xor_sync(~0u, col[k], 16));
       if (lane < 16) {
 #pragma unroll
         for (int k = 0; k < kWords; k += 4)
-          *reinterpret_cast<uint4 *>(&s_col[warp][tx * kWords + k]) = make_uint4(col[k], col[k + 1], col[k + 2], col[k + 3]);
+          *reinterpret_cast<uint4 *>(&sh.col[warp][tx * kWords + k]) = make_uint4(col[k], col[k + 1], col[k + 2], col[k + 3]);
       }
-      const bool awkward = __syncthreads_or(top >= inf_bits<T>());
-#pragma unroll
-      for (int v = 0; v < 8; ++v) {
-#pragma unroll
-        for (int k = 0; k < kWords; k += 4) {
-          const uint4 o = *reinterpret_cast<const uint4 *>(&s_col[v][tx * kWords + k]);
-          col[k] = Word<T>::max(col[k], o.x), col[k + 1] = Word<T>::max(col[k + 1], o.y);
-          col[k + 2] = Word<T>::max(col[k + 2], o.z), col[k + 3] = Word<T>::max(col[k + 3], o.w);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) ce[j] = scale_exponent(bits_to_float<T>(element_bits<T>(col, j)), a.qt.e5m2);
-      return awkward;
-    };
-    const bool awkward = reduce([](uint32_t v) { return v & Word<T>::kAbs; });
-    if (awkward) {
-      __syncthreads();
-      reduce([](uint32_t v) { return finite_abs<T>(v); });
     }
+    if (__syncthreads_or(any >= inf_bits<T>())) {
+      awkward_tile<T, SQUARE, E5M2>(a, tr, tc, sh);
+      __syncthreads();
+      continue;
+    }
+    float inv = 0.0f;  // of a square block
     if (SQUARE) {
+      uint32_t m = sh.all[0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) m = max(m, sh.all[i]);
+      const uint32_t e = scale_exponent<E5M2>(bits_to_float<T>(m));
       if (threadIdx.x == 0) {
-        a.q.scale[(int64_t)tc * a.q.scale_pitch + tr] = power(re[0]);
-        if (a.qt.data) a.qt.scale[(int64_t)tr * a.qt.scale_pitch + tc] = power(ce[0]);
+        a.q.scale[(int64_t)tc * a.q.scale_pitch + tr] = power(e);
+        if (a.qt.data) a.qt.scale[(int64_t)tr * a.qt.scale_pitch + tc] = power(e);
       }
+      inv = inverse_power(e);
     } else {
+      const uint32_t k = threadIdx.x % 128, side = threadIdx.x / 128;
+      uint32_t m = 0;
+      if (side) {
+#pragma unroll
+        for (int v = 0; v < 8; ++v) m = Word<T>::max(m, sh.col[v][k / Word<T>::kPer]);
+        if (sizeof(T) == 2) m = k % 2 ? m >> 16 : m & 0xffffu;
+      } else {
+        m = sh.row[k];
+      }
+      const uint32_t e = scale_exponent<E5M2>(bits_to_float<T>(m));
+      sh.inv[side][k] = inverse_power(e);
+      if (side) {
+        if (c0 + k < a.cols) a.qt.scale[(int64_t)tr * a.qt.scale_pitch + c0 + k] = power(e);
+      } else {
+        if (r0 + k < a.rows) a.q.scale[(int64_t)tc * a.q.scale_pitch + r0 + k] = power(e);
+      }
+      __syncthreads();
+    }
+    uint8_t *to = a.q.data + (int64_t)r * a.q.pitch + c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i, to += a.q.pitch) {
+      uint64_t v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = pack2(element<T>(w[i], 2 * j), element<T>(w[i], 2 * j + 1));
+      const float scale = SQUARE ? inv : sh.inv[0][8 * ty + i];
+      const uint2 y = to_fp8x8<E5M2>(v, pack2(scale, scale));
+      if (r + i < a.rows && nc) store8(to, y, nc);
+    }
+    if (a.qt.data) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const uint32_t r = r0 + 8 * ty + j, c = c0 + 8 * tx + j;
-        if (tx == j && r < a.rows) a.q.scale[(int64_t)tc * a.q.scale_pitch + r] = power(re[j]);
-        if (ty == j && c < a.cols) a.qt.scale[(int64_t)tr * a.qt.scale_pitch + c] = power(ce[j]);
+        uint64_t v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = pack2(element<T>(w[2 * i], j), element<T>(w[2 * i + 1], j));
+        const float scale = SQUARE ? inv : sh.inv[1][8 * tx + j];
+        sh.turn[(8 * tx + j) * 16 + (ty ^ tx)] = to_fp8x8<E5M2>(v, pack2(scale, scale));
+      }
+      __syncthreads();
+      const uint32_t rr = r0 + 8 * tx;  // now tx counts pieces down a column
+      const int nr = rr < a.rows ? (int)min(8u, a.rows - rr) : 0;
+      to = a.qt.data + (int64_t)(c0 + ty) * a.qt.pitch + rr;
+#pragma unroll
+      for (int i = 0; i < 8; ++i, to += 16 * a.qt.pitch) {
+        const uint32_t k = 16 * i + ty;
+        if (c0 + k < a.cols && nr) store8(to, sh.turn[k * 16 + (tx ^ k / 8)], nr);
       }
     }
-    if (awkward) store_tile<T, true>(w, re, ce, a, r0, c0, tx, ty, turn);
-    else store_tile<T, false>(w, re, ce, a, r0, c0, tx, ty, turn);
     __syncthreads();
   }
 }
@@ -351,7 +391,7 @@ bool rows_alone(const QuantArgs &a) { return !a.square && !a.qt.data; }
 
 }  // namespace
 
-int quantize_per_sm(const QuantArgs &a) { return rows_alone(a) ? 8 : a.dtype == APC_F32 ? 2 : 3; }
+int quantize_per_sm(const QuantArgs &a) { return rows_alone(a) ? 8 : a.dtype == APC_F32 ? 2 : APC_TILE_CTAS; }
 
 int launch_quantize(const QuantArgs &a, unsigned cap, void *stream) {
   return with_dtype(a.dtype, [&](auto t) {
@@ -359,15 +399,15 @@ int launch_quantize(const QuantArgs &a, unsigned cap, void *stream) {
     const bool wide = (uintptr_t)a.x % 16 == 0 && a.pitch * sizeof(T) % 16 == 0;
     const uint32_t across = (a.cols + kBlock - 1) / kBlock, down = (a.rows + kBlock - 1) / kBlock;
     cudaStream_t s = (cudaStream_t)stream;
+    const auto rows = a.q.e5m2 ? rows_kernel<T, true> : rows_kernel<T, false>;
+    const auto tiles = a.square ? a.q.e5m2 ? tile_kernel<T, true, true> : tile_kernel<T, true, false>
+                                : a.q.e5m2 ? tile_kernel<T, false, true> : tile_kernel<T, false, false>;
     if (rows_alone(a)) {
       const uint64_t each = kRowThreads / 32 * 2 * kRowUnroll, want = ((uint64_t)across * a.rows + each - 1) / each;
-      rows_kernel<T><<<(unsigned)(want < cap ? want : cap), kRowThreads, 0, s>>>(static_cast<const T *>(a.x), a.pitch, a.rows, a.cols,
-                                                                                 a.q, wide);
+      rows<<<(unsigned)(want < cap ? want : cap), kRowThreads, 0, s>>>(static_cast<const T *>(a.x), a.pitch, a.rows, a.cols, a.q, wide);
     } else {
       const uint64_t want = (uint64_t)across * down;
-      const unsigned grid = (unsigned)(want < cap ? want : cap);
-      if (a.square) tile_kernel<T, true><<<grid, kTileThreads, 0, s>>>(a, wide);
-      else tile_kernel<T, false><<<grid, kTileThreads, 0, s>>>(a, wide);
+      tiles<<<(unsigned)(want < cap ? want : cap), kTileThreads, 0, s>>>(a, wide);
     }
     return (int)cudaGetLastError();
   });

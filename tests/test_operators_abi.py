@@ -60,6 +60,7 @@ def distill(what="loss_grad", loss=AT + (5 << 32), lse=AT + (6 << 32), g=AT + (7
     (EINVAL, dict(q=fp8(fmt=2))),
     (EINVAL, dict(q=fp8(block=64))),
     (EINVAL, dict(q=fp8(), qt=fp8(AT + (1 << 33), AT + (1 << 34), block=128))),
+    (EINVAL, dict(q=fp8(), qt=fp8(AT + (1 << 33), AT + (1 << 34), fmt=1))),
     (EINVAL, dict(q=fp8(), qt=fp8(AT + 4096, AT + (1 << 34)))),       # the two outputs overlap
     (EINVAL, dict(x=AT)),                                               # an output over the input
 ])
