@@ -28,24 +28,15 @@ namespace apc {
 
 namespace {
 
-#ifndef APC_DISTILL_WARPS
-#define APC_DISTILL_WARPS 8
-#endif
-#ifndef APC_DISTILL_CTAS
-#define APC_DISTILL_CTAS 2
-#endif
-#ifndef APC_DISTILL_TEACHERS
-#define APC_DISTILL_TEACHERS 4
-#endif
-#ifndef APC_DISTILL_VECTORS
-#define APC_DISTILL_VECTORS 8
-#endif
 // Warps on the logits and on the teacher's entries, vectors of 16 bytes that each
-// of the former's threads takes of a chunk, CTAs on an SM.
-constexpr int kWarps = APC_DISTILL_WARPS, kWorkers = 32 * kWarps, kTeachers = APC_DISTILL_TEACHERS;
+// of the former's threads takes of a chunk, CTAs on an SM.  Measured on loss and
+// gradient of 8192 x 32768 with labels: 254 us; 1 CTA of 16 warps 310, 12 warps
+// 275, 4 warps 282 and, with 3 CTAs, 313; 2 vectors 325, 4 vectors 262; 2 teachers
+// 266.
+constexpr int kWarps = 8, kWorkers = 32 * kWarps, kTeachers = 4;
 constexpr int kThreads = kWorkers + 32 * kTeachers + 32;
-constexpr int kVectors = APC_DISTILL_VECTORS, kChunk = kWorkers * kVectors, kMaxChunks = 16;
-constexpr int kCtas = APC_DISTILL_CTAS;
+constexpr int kVectors = 8, kChunk = kWorkers * kVectors, kMaxChunks = 16;
+constexpr int kCtas = 2;
 constexpr int kMaxSplit = 8;
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;

@@ -64,7 +64,7 @@ constexpr int kScaleSlots = 8;  // blocks whose scales are on their way or in us
 // A wait that gives up marks the CTA dead: it stops loading and issuing, waits for
 // what is in flight, and its sums go on without waiting, so that every barrier is
 // reached.
-constexpr int kMidThreads = 384;  // copies, products, scales, products; 8 warps that add
+constexpr int kMidThreads = 384;  // warps: copies, products, scales, none; 8 that add
 
 template <int BN, bool SPLIT>
 struct MidShape {
@@ -147,10 +147,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
     }
     if (!ok)  // let the copies in flight land
       for (uint32_t i = min(issued, (uint32_t)S::kStages); i; --i) st.back(), wait_for(&full[st.at], st.phase);
-  } else if (warp == 1 || warp == 3) {
-    // two warps issue every other block's products: the waits and the issue of one
-    // take longer (450 cycles) than its bytes should
-    const uint32_t parity = warp == 3;
+  } else if (warp == 1) {
     Turn<S::kStages> st;
     Turn<S::kAcc> acc;
     uint32_t issued = 0;
@@ -158,7 +155,6 @@ __global__ void __launch_bounds__(kMidThreads, 1)
     const uint64_t r_desc = operand_desc(smem_addr(smem)), c_desc = operand_desc(smem_addr(smem) + S::kRowBytes);
     for (uint32_t t = first; t < tiles && ok; t += step)
       for (uint32_t b = b0; b < b1; ++b, st.next(), acc.next(), ++issued) {
-        if ((issued & 1) != parity) continue;
         if (!(ok = alive(&acc_empty[acc.at], acc.phase ^ 1) && alive(&full[st.at], st.phase))) break;
         tc_fence_after();
         const uint64_t off = st.at * (S::kStageBytes >> 4);
@@ -183,7 +179,7 @@ __global__ void __launch_bounds__(kMidThreads, 1)
       }
     }
     words_landed();
-  } else {
+  } else if (warp >= 4) {
     constexpr int kCols = S::kCols, kGroup = S::kGroup, kLoad = S::kLoad;
     const uint32_t quad = warp & 3, row = quad * 32 + lane, half = (warp - 4) / 4;
     Turn<S::kAcc> buf;
@@ -297,18 +293,11 @@ __global__ void __launch_bounds__(kMidThreads, 1)
 // it holds half in shared memory (tcgen05.mma.cta_group::2 reads both halves).
 // The first CTA's thread issues for both.  Persistent: the pair's next tile is
 // loaded and multiplied while the epilogue stores.
-#ifndef APC_BIG_WARPS
-#define APC_BIG_WARPS 8
-#endif
-#ifndef APC_BIG_LOAD
-#define APC_BIG_LOAD 16
-#endif
-#ifndef APC_BIG_STAGES
-#define APC_BIG_STAGES 6
-#endif
-constexpr int kBigWarps = APC_BIG_WARPS, kBigLoad = APC_BIG_LOAD;
-constexpr int kBigThreads = 128 + 32 * kBigWarps, kBigStages = APC_BIG_STAGES;
-constexpr int kBigCols = 1024 / kBigWarps;  // columns that a warp adds up
+// Warps 0 to 3 load and issue with 56 registers a thread, 4 to 11 add with 224 (of
+// the launch's 168 each: 128 x 56 + 256 x 224 = 384 x 168).
+constexpr int kBigWarps = 8, kBigThreads = 128 + 32 * kBigWarps, kBigStages = 6;
+constexpr int kBigCols = 1024 / kBigWarps;  // columns that a warp adds
+constexpr int kBigLoad = 16;                // in loads of so many
 constexpr int kBigHalf = 128 * kBlock, kBigStageBytes = 2 * kBigHalf;
 constexpr int kBigScaleBytes = kScaleSlots * (128 + 256) * 4;
 constexpr int kBigTurnBytes = 32 * 17 * 4;  // a warp's, for rows of out that are not aligned
@@ -408,7 +397,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   const uint32_t tmem = tmem_at;
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBigWarps == 8 ? 56 : 32));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 0) {
       Turn<kBigStages> st;
       uint32_t issued = 0;
@@ -477,7 +466,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kBigWarps == 8 ? 224 : 112));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     const uint32_t quad = warp & 3, part = (warp - 4) / 4, row = quad * 32 + lane;
     const uint32_t empty_bars = map_rank(smem_addr(acc_empty), 0);
     float *turn = scales + kBigScaleBytes / 4 + (warp - 4) * (kBigTurnBytes / 4);

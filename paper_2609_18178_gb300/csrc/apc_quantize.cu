@@ -144,10 +144,7 @@ __device__ __forceinline__ void store8(uint8_t *at, uint2 v, int n) {
 // ---------------------------------------------------------------------------
 // Rows alone.  The blocks of the whole matrix in row order; half a warp takes
 // one, 8 elements a lane, kRowUnroll of them in flight.
-#ifndef APC_ROW_UNROLL
-#define APC_ROW_UNROLL 2
-#endif
-constexpr int kRowThreads = 256, kRowUnroll = APC_ROW_UNROLL;
+constexpr int kRowThreads = 256, kRowUnroll = 2;
 
 template <typename T, bool E5M2>
 __global__ void __launch_bounds__(kRowThreads) rows_kernel(const T *x, int64_t pitch, uint32_t rows, uint32_t cols, QuantOut q,
@@ -211,9 +208,6 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(const T *x, int64_t p
 // to shared memory, where each row and each column is then one thread's: that
 // thread stores the scale and leaves its inverse.  The transpose goes through
 // shared memory in 8-byte pieces, swizzled so that neither side meets a bank twice.
-#ifndef APC_TILE_CTAS
-#define APC_TILE_CTAS 3
-#endif
 constexpr int kTileThreads = 256;
 
 struct TileShared {
@@ -260,7 +254,7 @@ __device__ __noinline__ void awkward_tile(const QuantArgs &a, uint32_t tr, uint3
 }
 
 template <typename T, bool SQUARE, bool E5M2>
-__global__ void __launch_bounds__(kTileThreads, sizeof(T) == 4 ? 2 : APC_TILE_CTAS) tile_kernel(const __grid_constant__ QuantArgs a, bool wide) {
+__global__ void __launch_bounds__(kTileThreads, sizeof(T) == 4 ? 2 : 3) tile_kernel(const __grid_constant__ QuantArgs a, bool wide) {
   constexpr int kWords = 8 / Word<T>::kPer;  // words of 8 elements
   __shared__ __align__(16) TileShared sh;
   const uint32_t tx = threadIdx.x % 16, ty = threadIdx.x / 16, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -391,7 +385,7 @@ bool rows_alone(const QuantArgs &a) { return !a.square && !a.qt.data; }
 
 }  // namespace
 
-int quantize_per_sm(const QuantArgs &a) { return rows_alone(a) ? 8 : a.dtype == APC_F32 ? 2 : APC_TILE_CTAS; }
+int quantize_per_sm(const QuantArgs &a) { return rows_alone(a) ? 8 : a.dtype == APC_F32 ? 2 : 3; }
 
 int launch_quantize(const QuantArgs &a, unsigned cap, void *stream) {
   return with_dtype(a.dtype, [&](auto t) {

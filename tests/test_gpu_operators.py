@@ -580,3 +580,42 @@ def test_distill_refusals():
     with pytest.raises(apc.ApcError) as e:
         apc.distill_loss_grad(z, ids, u, g, loss=g)  # the loss over its own weights
     assert e.value.status == 1
+
+
+def test_example_learns_and_its_replicas_agree():
+    """The operators as they are used together: a distilled head's steps."""
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "distill_head.py")
+    spec = importlib.util.spec_from_file_location("distill_head", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    losses = example.main(["--tokens", "300", "--vocab", "2003", "--hidden", "520", "--k", "20", "--steps", "6"])
+    assert all(b < a for a, b in zip(losses, losses[1:]))
+
+
+def test_head_gradients_against_64_bits():
+    """The chain's gradients, from the quantized operands that it used, as the
+    formula gives them in 64 bits."""
+    tokens, vocab, hidden, k = 200, 1003, 272, 12
+    x = torch.randn(tokens, hidden, generator=gen(1), device="cuda").bfloat16()
+    w = torch.randn(vocab, hidden, generator=gen(2), device="cuda").mul_(0.1).bfloat16()
+    x8, xs, x8t, xst = apc.quantize_fp8(x, transposed=True)
+    w8, ws, w8t, wst = apc.quantize_fp8(w, block_rows=128, transposed=True)
+    logits = apc.matmul_fp8(x8, xs, w8, ws, out_dtype=torch.float32)
+    ids, u = teacher_of(tokens, vocab, k, 3)
+    g = torch.full((tokens,), 1.0 / tokens, device="cuda")
+    _, _, d = apc.distill_loss_grad(logits, ids, u, g, temperature=2.0)
+    _, _, want, size, _ = ref_distill(logits, ids, u, g, 2.0, 1.0, 0.0)
+    close(d, want, size * (UNIT[torch.float32] + 2 * relative(logits, u, 2.0)) + TINY[torch.float32])
+    d8, ds, d8t, dst = apc.quantize_fp8(d, transposed=True)
+    for a, sa, ba, b, sb, bb in ((d8, ds, 1, w8t, wst, 128), (d8t, dst, 1, x8t, xst, 1)):
+        ref, size = ref_matmul(a, sa, ba, b, sb, bb)
+        check_matmul(apc.matmul_fp8(a, sa, b, sb, out_dtype=torch.float32), ref, size, a.shape[1])
+    # and the gradient of the head within what 8 bits keep: half an ulp of E4M3, 2^-4, of each factor
+    dw = apc.matmul_fp8(d8t, dst, x8t, xst, out_dtype=torch.float32).double()
+    full = d.double().t() @ x.double()
+    size = d.double().abs().t() @ x.double().abs()
+    floor = (d8t.shape[1] * 2.0 ** -10) * dst.max().double() * x.double().abs().max()  # values below the least normal one
+    assert ((dw - full).abs() <= size * (2 * 2.0 ** -4 + 2.0 ** -8) + floor * 2).all()
