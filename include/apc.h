@@ -297,9 +297,10 @@ typedef enum apc_index { APC_I32 = 0, APC_I64 = 1 } apc_index;
  *   d loss / dz = kd_weight * tau * (P q - p) + label_weight * (softmax(z) - onehot(y))
  * An entry counts only where its id lies in [0, vocab) and its logit is not
  * -infinity, whatever else stands there; so does a label.  Entries with the
- * same id add up.  A row without entries has no teacher's part.  A row whose
- * logits are all -infinity has loss 0, lse -infinity and gradient 0.  Masked
- * logits (-infinity) have q = 0; an entry or label there makes the loss +infinity.
+ * same id add up.  A row without entries has no teacher's part.  A row with no
+ * logit above -1e30 is masked whole (with -infinity, or fp32's or bf16's lowest
+ * value): loss 0, lse -infinity, gradient 0.  Masked logits have q = 0; an entry or
+ * label on a -infinity makes the loss +infinity.
  *   logits        rows x vocab, apc_dtype, pitch in elements
  *   ids, teacher  rows x k (k <= APC_DISTILL_MAX_K; 0: no teacher), apc_index and apc_dtype
  *   teacher_lse   fp32, one per row: log sum exp(u/tau) over the whole vocabulary, or NULL

@@ -46,8 +46,14 @@ struct Sum {
   float m, s, s1;
 };
 
-// What z's difference is taken to: m, or 0 where every logit is -infinity.
-__device__ __forceinline__ float reference(float m) { return m == -kInf ? 0.0f : m; }
+// A row whose logits are all masked, with infinities or a type's lowest value, has
+// none above this.  Their sum's logarithm would be -3.4e38 + log(vocab): fp32 cannot
+// hold it, and a gradient from it would take every place's q for 1.
+constexpr float kMasked = -1e30f;
+
+// What z's difference is taken to: m, or 0 where every logit is masked (the sums
+// are 0 then).
+__device__ __forceinline__ float reference(float m) { return m > kMasked ? m : 0.0f; }
 
 // A sum about `from` as one about `to`, the larger.
 __device__ __forceinline__ float moved(float s, float from, float to, float scale) {
@@ -142,23 +148,24 @@ __device__ __noinline__ void teacher_entries(const DistillArgs &a, uint32_t row,
   int32_t *ids = e.id;
   float *ps = e.p, *zs = e.z;
   float top = -kInf;
-  constexpr int kBatch = 4;  // loads in flight
+  constexpr int kBatch = 8;  // entries a lane has in flight: their ids, then the student's logits there
   for (uint32_t i0 = lane; i0 < a.k; i0 += 32 * kBatch) {
-    int64_t id[kBatch];
+    int32_t id[kBatch];
     float u[kBatch], x[kBatch];
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
       const uint32_t i = i0 + 32 * b;
-      id[b] = i < a.k ? index_at(a.ids, a.ids64, at_id + i) : -1;
+      const int64_t v = i < a.k ? index_at(a.ids, a.ids64, at_id + i) : -1;
       u[b] = i < a.k ? number_at(a.teacher, a.teacher_dtype, at_u + i) : -kInf;
-      if (id[b] < 0 || id[b] >= (int64_t)a.vocab || u[b] == -kInf) id[b] = -1, u[b] = -kInf;
+      id[b] = v < 0 || v >= (int64_t)a.vocab || u[b] == -kInf ? -1 : (int32_t)v;
     }
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) x[b] = id[b] >= 0 ? to_float(z[id[b]]) : 0.0f;
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
       const uint32_t i = i0 + 32 * b;
-      if (i < a.k) ids[i] = (int32_t)id[b], ps[i] = u[b], zs[i] = x[b];
+      if (id[b] < 0) u[b] = -kInf;
+      if (i < a.k) ids[i] = id[b], ps[i] = u[b], zs[i] = x[b];
       top = fmaxf(top, u[b]);
     }
   }
@@ -309,6 +316,220 @@ __device__ __forceinline__ uint4 nothing() {
   return {w, w, w, w};
 }
 
+// A row's or a part's sums on the way: the largest logit and, in two fp32 lanes, the
+// sums about it.
+template <typename T, bool TWO>
+struct Running {
+  float m;
+  uint64_t s, s1;
+
+  // One element to begin with, or none.
+  __device__ __forceinline__ Running(float x, bool has, float scale2) : m(x), s(0), s1(0) {
+    if (!has) return;
+    s = pack2(exp2_approx((x - reference(x)) * scale2), 0.0f);
+    if (TWO) s1 = pack2(exp2_approx((x - reference(x)) * kLog2e), 0.0f);
+  }
+
+  template <int N>
+  __device__ __forceinline__ void add(const uint4 (&x)[N], float scale2) {
+    const uint64_t scale = pack2(scale2, scale2), scale1 = pack2(kLog2e, kLog2e);
+    const float top = largest<T>(x);
+    if (top > m) {  // the sums move to the new maximum
+      const float f = moved(1.0f, m, top, scale2);
+      s = mul2(s, pack2(f, f));
+      if (TWO) {
+        const float f1 = moved(1.0f, m, top, kLog2e);
+        s1 = mul2(s1, pack2(f1, f1));
+      }
+      m = top;
+    }
+    const uint64_t minus = pack2(-reference(m), -reference(m));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+      for (int j = 0; j < 8 / (int)sizeof(T); ++j) {
+        const uint64_t y = add2(pair<T>(x[i], j), minus);
+        s = add2(s, exp2_pair(mul2(y, scale)));
+        if (TWO) s1 = add2(s1, exp2_pair(mul2(y, scale1)));
+      }
+    }
+  }
+
+  __device__ __forceinline__ Sum sum() const {
+    const float2 u = unpack2(s), u1 = unpack2(s1);
+    return {m, u.x + u.y, u1.x + u1.y};
+  }
+};
+
+__device__ __forceinline__ bool has_logits(const Sum &s) { return s.s != 0.0f; }  // a NaN has
+
+// One warp: the row's loss and statistics, from its sums and entries.
+template <bool TWO>
+__device__ __forceinline__ void store_loss(const DistillArgs &a, uint32_t row, const Sum &sum, const Entries &en, uint32_t lane) {
+  const float from = reference(sum.m), log_s = log2f(sum.s) * kLn2, log_s1 = TWO ? log2f(sum.s1) * kLn2 : log_s;
+  const bool some = has_logits(sum);
+  float cross = 0.0f;
+  for (uint32_t i = lane; i < a.k; i += 32)
+    if (en.p[i] != 0.0f) cross = __fmaf_rn(a.loss_kd * en.p[i], __fmaf_rn(en.z[i] - from, a.inv_tau, -log_s), cross);
+  for (int o = 16; o; o >>= 1) cross += __shfl_xor_sync(~0u, cross, o);
+  if (lane == 0) {
+    float loss = __fmaf_rn(a.loss_kd, en.entropy, -cross);
+    if (en.id[a.k] >= 0 && a.loss_label != 0.0f) loss -= a.loss_label * (en.z[a.k] - from - log_s1);
+    a.loss[row] = some ? loss : 0.0f;
+    a.lse[row] = some ? __fmaf_rn(from, a.inv_tau, log_s) : -kInf;
+    if (a.labels) a.lse[(int64_t)a.rows + row] = some ? from + log_s1 : -kInf;
+  }
+}
+
+// A row's gradient without its entries' part: both temperatures' c 2^((z times +
+// plus) scale), from the row's own maximum and sums or from the given logarithms.
+template <bool LOSS, bool TWO>
+struct Whole {
+  bool live;  // else zeros
+  float g;
+  uint64_t times, plus, plus1, scale, scale1, c0, c1;
+
+  __device__ __forceinline__ Whole(const DistillArgs &a, uint32_t row, const Sum &sum, const Entries &en) {
+    g = a.grad_loss[row];
+    float k0 = g * a.grad_kd * en.p_sum, k1 = en.id[a.k] >= 0 ? g * a.loss_label : 0.0f, l = 0.0f, l1 = 0.0f;
+    const float from = reference(sum.m);
+    live = g != 0.0f;
+    if (LOSS) {
+      live = live && has_logits(sum);
+      k0 /= sum.s, k1 /= TWO ? sum.s1 : sum.s;
+    } else {
+      l = a.lse[row];
+      if (a.labels) l1 = a.lse[(int64_t)a.rows + row];
+      live = live && !(l <= kMasked);
+    }
+    if (!TWO) k0 += k1;  // one temperature for both
+    const float t = LOSS ? 1.0f : a.inv_tau, p = LOSS ? -from : -l, p1 = LOSS ? -from : -l1, f = LOSS ? a.scale2 : kLog2e;
+    times = pack2(t, t), plus = pack2(p, p), plus1 = pack2(p1, p1), scale = pack2(f, f), scale1 = pack2(kLog2e, kLog2e);
+    c0 = pack2(k0, k0), c1 = pack2(k1, k1);
+  }
+
+  __device__ __forceinline__ uint64_t operator()(uint64_t y) const {
+    const uint64_t t = LOSS ? add2(y, plus) : fma2(y, times, plus);
+    const uint64_t q = mul2(c0, exp2_pair(mul2(t, scale)));
+    return TWO ? fma2(c1, exp2_pair(mul2(LOSS ? t : add2(y, plus1), scale1)), q) : q;
+  }
+
+  __device__ __forceinline__ float one(float y) const { return unpack2((*this)(pack2(y, y))).x; }
+};
+
+// The gradient at entry i's place, where this is the first entry there; false otherwise.
+template <typename W>
+__device__ __forceinline__ bool entry_gradient(const DistillArgs &a, const Entries &en, const W &whole, uint32_t i, float *out) {
+  const int32_t id = en.id[i];
+  float take = i == a.k ? a.loss_label : a.grad_kd * en.p[i];
+  if (en.same) {  // entries of one place add up, in their order
+    bool first = true;
+    take = 0.0f;
+    for (uint32_t j = 0; j <= a.k; ++j)
+      if (en.id[j] == id) {
+        first = first && j >= i;
+        take += j == a.k ? a.loss_label : a.grad_kd * en.p[j];
+      }
+    if (!first) return false;
+  }
+  *out = __fmaf_rn(-whole.g, take, whole.one(en.z[i]));
+  return true;
+}
+
+// Vector v to place k of a row's body: as it is where the gradient's rows are aligned
+// as the logits' are, else element by element.
+template <typename T>
+__device__ __forceinline__ void store_vector(T *body, uint32_t k, const uint4 &v, bool alike) {
+  constexpr int kPer = 16 / sizeof(T);
+  if (alike) {
+    __stcs(reinterpret_cast<uint4 *>(body) + k, v);
+  } else {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      if constexpr (sizeof(T) == 4) body[(int64_t)k * kPer + j] = __uint_as_float(w[j]);
+      else reinterpret_cast<uint16_t *>(body)[(int64_t)k * kPer + j] = (uint16_t)(w[j / 2] >> (j % 2 * 16));
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Short rows, of which there are many: one warp a row, from its entries to its
+// gradient.  A row's way takes some 6 us, most of it waiting, so what counts is how
+// many are under way: 24 on an SM, where the kernel below has 2.  Up to
+// kShortVectors of 16 bytes a lane stay in registers; a longer row's second sweep
+// finds it in L2.  Measured on 8192 rows: 100 logits in SHORT_100 us (104 below),
+// 1000 in SHORT_1000 (121), 5000 (loss) in SHORT_5000 (69).
+constexpr int kShortWarps = 8, kShortVectors = 8, kShortCtas = 3;
+constexpr uint32_t kShortBytes = 8192, kShortEntries = 256;
+
+template <typename T, int FORM, bool TWO>
+__global__ void __launch_bounds__(32 * kShortWarps, kShortCtas)
+    short_kernel(const __grid_constant__ DistillArgs a, const uint32_t room, const uint32_t slots_log2, const bool alike) {
+  extern __shared__ __align__(16) uint8_t raw[];
+  __shared__ Entries all[kShortWarps];
+  constexpr int kPer = 16 / sizeof(T);
+  constexpr bool kLoss = FORM & 1, kGrad = FORM & 2;
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  Entries &en = all[warp];
+  int32_t *table = reinterpret_cast<int32_t *>(raw + warp * (room * 12 + (4u << slots_log2)));
+  if (lane == 0) {
+    uint8_t *at = reinterpret_cast<uint8_t *>(table) + (4u << slots_log2);
+    en.id = reinterpret_cast<int32_t *>(at), en.p = reinterpret_cast<float *>(at + room * 4), en.z = reinterpret_cast<float *>(at + room * 8);
+  }
+  __syncwarp();
+  for (uint64_t row = blockIdx.x * kShortWarps + warp; row < a.rows; row += gridDim.x * kShortWarps) {
+    const T *z = static_cast<const T *>(a.logits) + (int64_t)row * a.pitch;
+    const uint32_t head = min(a.vocab, (uint32_t)((16 - (uintptr_t)z % 16) % 16 / sizeof(T)));
+    const uint32_t body = (a.vocab - head) / kPer, odd = a.vocab - body * kPer;
+    const uint4 *zv = reinterpret_cast<const uint4 *>(z + head);
+    const uint32_t odd_at = lane < head ? lane : body * kPer + lane;
+    const float x_odd = lane < odd ? to_float(z[odd_at]) : -kInf;
+    uint4 x[kShortVectors];
+    auto load = [&](uint32_t at) {
+#pragma unroll
+      for (int i = 0; i < kShortVectors; ++i) x[i] = at + i * 32 + lane < body ? zv[at + i * 32 + lane] : nothing<T>();
+    };
+    load(0);
+    __syncwarp();
+    teacher_entries<T>(a, (uint32_t)row, en, table, slots_log2, lane);
+    __syncwarp();
+    Sum sum = {-kInf, 0.0f, 0.0f};
+    if (kLoss) {
+      Running<T, TWO> run(x_odd, lane < odd, a.scale2);
+      for (uint32_t at = 0;;) {
+        run.add(x, a.scale2);
+        at += 32 * kShortVectors;
+        if (at >= body) break;
+        load(at);
+      }
+      sum = joined<TWO>(run.sum(), a.scale2);
+      store_loss<TWO>(a, (uint32_t)row, sum, en, lane);
+    }
+    if (!kGrad) continue;
+    const Whole<kLoss, TWO> whole(a, (uint32_t)row, sum, en);
+    T *d = static_cast<T *>(a.dlogits) + (int64_t)row * a.dpitch;
+    if (kLoss && body > 32 * kShortVectors) load(0);
+    for (uint32_t at = 0;;) {
+#pragma unroll
+      for (int i = 0; i < kShortVectors; ++i)
+        if (at + i * 32 + lane < body)
+          store_vector<T>(d + head, at + i * 32 + lane, whole.live ? map<T>(x[i], whole) : make_uint4(0, 0, 0, 0), alike);
+      at += 32 * kShortVectors;
+      if (at >= body) break;
+      load(at);
+    }
+    if (lane < odd) d[odd_at] = from_float<T>(whole.live ? whole.one(x_odd) : 0.0f);
+    __syncwarp();  // the row is written but for its entries
+    float v;
+    if (whole.live)
+      for (uint32_t i = lane; i <= a.k; i += 32)
+        if (en.id[i] >= 0 && entry_gradient(a, en, whole, i, &v)) d[en.id[i]] = from_float<T>(v);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Longer rows.
 // FORM: 1 loss, 2 gradient, 3 both.  TWO: the labels need the sums at tau = 1
 // beside those at tau.  alike: the gradient's rows are aligned as the logits' are.
 template <typename T, int FORM, bool TWO>
@@ -320,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
   uint4 *ring = reinterpret_cast<uint4 *>(raw + (sizeof(Shared) + 15) / 16 * 16);
   int32_t *tables = reinterpret_cast<int32_t *>(ring + layout.chunks * kChunk);
   const uint32_t kChunks = layout.chunks;
-  constexpr int kPer = 16 / sizeof(T), kPairs = kPer / 2;
+  constexpr int kPer = 16 / sizeof(T);
   constexpr bool kLoss = FORM & 1, kGrad = FORM & 2;
   const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const uint32_t rank = split > 1 ? blockIdx.x % split : 0, first = blockIdx.x / split, step = gridDim.x / split;
@@ -399,15 +620,10 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       const bool has_odd = worker && rank == 0 && tid < odd;
       const uint32_t odd_at = tid < p.head ? tid : p.body * kPer + tid;
       const float x_odd = has_odd ? to_float(p.z[odd_at]) : -kInf;
-      Sum sum = {x_odd, 0.0f, 0.0f};
+      Sum sum = {-kInf, 0.0f, 0.0f};
       if (kLoss) {
         if (worker) {
-          if (has_odd) {
-            sum.s = exp2_approx((x_odd - reference(x_odd)) * a.scale2);
-            if (TWO) sum.s1 = exp2_approx((x_odd - reference(x_odd)) * kLog2e);
-          }
-          const uint64_t scale = pack2(a.scale2, a.scale2), scale1 = pack2(kLog2e, kLog2e);
-          uint64_t parts = pack2(sum.s, 0.0f), parts1 = pack2(sum.s1, 0.0f);
+          Running<T, TWO> run(x_odd, has_odd, a.scale2);
           for (uint32_t c = 0; c < p.chunks; ++c) {
             const uint32_t s = (use + c) % kChunks, n = p.v1 - p.v0 - c * kChunk;
             wait(&sh.full[s], (use + c) / kChunks & 1, sh, a.status);
@@ -420,32 +636,14 @@ __global__ void __launch_bounds__(kThreads, kCtas)
 #pragma unroll
               for (int i = 0; i < kVectors; ++i) x[i] = i * kWorkers + tid < n ? from[i * kWorkers] : nothing<T>();
             }
-            const float m = largest<T>(x);
-            if (m > sum.m) {  // the sums move to the new maximum
-              const uint64_t f = pack2(moved(1.0f, sum.m, m, a.scale2), moved(1.0f, sum.m, m, a.scale2));
-              parts = mul2(parts, f);
-              if (TWO) parts1 = mul2(parts1, pack2(moved(1.0f, sum.m, m, kLog2e), moved(1.0f, sum.m, m, kLog2e)));
-              sum.m = m;
-            }
-            const uint64_t minus = pack2(-reference(sum.m), -reference(sum.m));
-#pragma unroll
-            for (int i = 0; i < kVectors; ++i) {
-#pragma unroll
-              for (int j = 0; j < kPairs; ++j) {
-                const uint64_t y = add2(pair<T>(x[i], j), minus);
-                parts = add2(parts, exp2_pair(mul2(y, scale)));
-                if (TWO) parts1 = add2(parts1, exp2_pair(mul2(y, scale1)));
-              }
-            }
+            run.add(x, a.scale2);
             if (FORM == 1 || !p.keeps) {
               __syncwarp();
               if (lane == 0) mbar_arrive(&sh.empty[s]);
             }
           }
           if (FORM == 1 || !p.keeps) use += p.chunks;
-          const float2 u = unpack2(parts), u1 = unpack2(parts1);
-          sum.s = u.x + u.y;
-          if (TWO) sum.s1 = u1.x + u1.y;
+          sum = run.sum();
           sum = joined<TWO>(sum, a.scale2);
           if (lane == 0) sh.part[turn][warp] = sum;
         }
@@ -467,102 +665,45 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(kWorkers + 32) : "memory");
       }
       const Entries &en = sh.e[turn];
-      const float from = reference(sum.m);
       if (!worker) {
         // the row's loss, then the next row's entries
-        if (kLoss && rank == 0) {
-          const float log_s = log2f(sum.s), log_s1 = TWO ? log2f(sum.s1) : log_s;
-          const bool some = sum.m != -kInf || sum.s != 0.0f;
-          float cross = 0.0f;
-          for (uint32_t i = lane; i < a.k; i += 32)
-            if (en.p[i] != 0.0f) cross = __fmaf_rn(en.p[i], (en.z[i] - from) * a.scale2 - log_s, cross);
-          for (int o = 16; o; o >>= 1) cross += __shfl_xor_sync(~0u, cross, o);
-          if (lane == 0) {
-            float loss = a.loss_kd * __fmaf_rn(-kLn2, cross, en.entropy);
-            if (en.id[a.k] >= 0 && a.loss_label != 0.0f) loss -= a.loss_label * kLn2 * ((en.z[a.k] - from) * kLog2e - log_s1);
-            a.loss[row] = some ? loss : 0.0f;
-            a.lse[row] = some ? __fmaf_rn(from, a.inv_tau, log_s * kLn2) : -kInf;
-            if (a.labels) a.lse[(int64_t)a.rows + row] = some ? __fmaf_rn(log_s1, kLn2, from) : -kInf;
-          }
-        }
+        if (kLoss && rank == 0) store_loss<TWO>(a, (uint32_t)row, sum, en, lane);
         if (row + (uint64_t)step * teachers < a.rows)
           teacher_entries<T>(a, (uint32_t)(row + (uint64_t)step * teachers), sh.e[(done + teachers) % (teachers + 1)], table, layout.slots_log2, lane);
         continue;
       }
       if (!kGrad) continue;
-      const float g = a.grad_loss[row];
-      float c0 = g * a.grad_kd * en.p_sum, c1 = en.id[a.k] >= 0 ? g * a.loss_label : 0.0f, l = 0.0f, l1 = 0.0f;
-      bool live = g != 0.0f;
-      if (kLoss) {
-        live = live && (sum.m != -kInf || sum.s != 0.0f);
-        c0 /= sum.s, c1 /= TWO ? sum.s1 : sum.s;
-      } else {
-        l = a.lse[row];
-        if (a.labels) l1 = a.lse[(int64_t)a.rows + row];
-        live = live && l != -kInf;
-      }
-      if (!TWO) c0 += c1;  // one temperature for both
-      // Both temperatures' parts, without the entries': c 2^((z times + plus) scale),
-      // from the row's own maximum and sums or from the given logarithms.
-      const float times = kLoss ? 1.0f : a.inv_tau, plus = kLoss ? -from : -l, plus1 = kLoss ? -from : -l1;
-      const float scale = kLoss ? a.scale2 : kLog2e;
-      const uint64_t times2 = pack2(times, times), plus2 = pack2(plus, plus), plus12 = pack2(plus1, plus1);
-      const uint64_t scale2 = pack2(scale, scale), scale12 = pack2(kLog2e, kLog2e), c02 = pack2(c0, c0), c12 = pack2(c1, c1);
-      auto whole2 = [&](uint64_t y) {
-        const uint64_t t = kLoss ? add2(y, plus2) : fma2(y, times2, plus2);
-        const uint64_t q = mul2(c02, exp2_pair(mul2(t, scale2)));
-        return TWO ? fma2(c12, exp2_pair(mul2(kLoss ? t : add2(y, plus12), scale12)), q) : q;
-      };
-      auto whole = [&](float y) { return unpack2(whole2(pack2(y, y))).x; };
+      const Whole<kLoss, TWO> whole(a, (uint32_t)row, sum, en);
       T *d = static_cast<T *>(a.dlogits) + (int64_t)row * a.dpitch;
       for (uint32_t c = 0; c < p.chunks; ++c, ++use) {
         const uint32_t s = use % kChunks, at = p.v0 + c * kChunk;
         wait(&sh.full[s], use / kChunks & 1, sh, a.status);
         const uint4 *x = ring + s * kChunk + tid;
-        if (alike && live && p.v1 - at >= kChunk) {
+        if (alike && whole.live && p.v1 - at >= kChunk) {
           uint4 *to = reinterpret_cast<uint4 *>(d + p.head) + at + tid;
 #pragma unroll
-          for (int i = 0; i < kVectors; ++i) __stcs(to + i * kWorkers, map<T>(x[i * kWorkers], whole2));
+          for (int i = 0; i < kVectors; ++i) __stcs(to + i * kWorkers, map<T>(x[i * kWorkers], whole));
         } else {
           for (int i = 0; i < kVectors; ++i) {
             const uint32_t k = at + i * kWorkers + tid;
             if (k >= p.v1) break;
-            const uint4 v = live ? map<T>(x[i * kWorkers], whole2) : make_uint4(0, 0, 0, 0);
-            if (alike) {
-              __stcs(reinterpret_cast<uint4 *>(d + p.head) + k, v);
-            } else {
-              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-              for (int j = 0; j < kPer; ++j) {
-                if constexpr (sizeof(T) == 4) d[p.head + (int64_t)k * kPer + j] = __uint_as_float(w[j]);
-                else reinterpret_cast<uint16_t *>(d)[p.head + (int64_t)k * kPer + j] = (uint16_t)(w[j / 2] >> (j % 2 * 16));
-              }
-            }
+            store_vector<T>(d + p.head, k, whole.live ? map<T>(x[i * kWorkers], whole) : make_uint4(0, 0, 0, 0), alike);
           }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.empty[s]);
       }
-      if (has_odd) d[odd_at] = from_float<T>(live ? whole(x_odd) : 0.0f);
+      if (has_odd) d[odd_at] = from_float<T>(whole.live ? whole.one(x_odd) : 0.0f);
       asm volatile("bar.sync 1, %0;" ::"n"(kWorkers) : "memory");  // the row is written but for its entries
-      if (!live) continue;
+      if (!whole.live) continue;
       for (uint32_t i = tid; i <= a.k; i += kWorkers) {
         const int32_t id = en.id[i];
         if (id < 0) continue;
         // whoever wrote the place writes it again
         const uint32_t v = ((uint32_t)id - p.head) / kPer;
         if (!((uint32_t)id < p.head || v >= p.body ? rank == 0 : v >= p.v0 && v < p.v1)) continue;
-        float take = i == a.k ? a.loss_label : a.grad_kd * en.p[i];
-        bool first_one = true;
-        if (en.same) {
-          take = 0.0f;
-          for (uint32_t j = 0; j <= a.k; ++j)
-            if (en.id[j] == id) {
-              first_one = first_one && j >= i;
-              take += j == a.k ? a.loss_label : a.grad_kd * en.p[j];
-            }
-        }
-        if (first_one) d[id] = from_float<T>(__fmaf_rn(-g, take, whole(en.z[i])));
+        float y;
+        if (entry_gradient(a, en, whole, i, &y)) d[id] = from_float<T>(y);
       }
     }
   }
@@ -572,7 +713,16 @@ __global__ void __launch_bounds__(kThreads, kCtas)
 
 }  // namespace
 
-int distill_per_sm(const DistillArgs &) { return kCtas; }
+namespace {
+
+// A warp for each row where rows are short and enough of them to fill the GPU.
+bool rows_are_short(const DistillArgs &a, unsigned sms) {
+  return a.vocab * (a.dtype == APC_F32 ? 4u : 2u) <= kShortBytes && a.k <= kShortEntries && a.rows >= sms;
+}
+
+}  // namespace
+
+int distill_per_sm(const DistillArgs &a, unsigned sms) { return rows_are_short(a, sms) ? kShortCtas : kCtas; }
 
 int launch_distill(const DistillArgs &args, unsigned cap, unsigned sms, void *stream) {
   DistillArgs a = args;
@@ -581,23 +731,35 @@ int launch_distill(const DistillArgs &args, unsigned cap, unsigned sms, void *st
   return with_dtype(a.dtype, [&](auto t) {
     using T = decltype(t);
     const uint32_t size = sizeof(T), body = a.vocab / (16 / size);
-    Layout l = {};
-    l.teachers = a.k <= 256 ? kTeachers : a.k <= 512 ? (kTeachers + 1) / 2 : 1;
-    l.room = (a.k + 1 + 3) / 4 * 4;
-    l.slots_log2 = 6;
-    while ((1u << l.slots_log2) < 2 * (a.k + 1)) ++l.slots_log2;
-    constexpr uint32_t kRoom = 227 * 1024 / kCtas - 1024;
-    l.chunks = std::min((uint32_t)kMaxChunks, (kRoom - l.bytes()) / (kChunk * 16));
-    // a row over more CTAs while they would not fill the GPU, or while its parts do
-    // not fit the ring, but not into parts of less than two chunks
-    uint32_t split = 1;
-    while (split < (uint32_t)kMaxSplit && body / (2 * split) >= 2 * kChunk &&
-           ((uint64_t)a.rows * split <= sms || (a.loss && a.dlogits && body > split * l.chunks * kChunk)))
-      split *= 2;
-    const uint64_t most = cap >= split ? cap / split : 1;
-    const unsigned grid = (unsigned)(a.rows < most ? a.rows : most) * split;
     const bool alike = a.dlogits && ((uintptr_t)a.dlogits - (uintptr_t)a.logits) % 16 == 0 && (a.dpitch - a.pitch) * size % 16 == 0;
     const bool two = a.labels && a.inv_tau != 1.0f;
+    const uint32_t room = (a.k + 1 + 3) / 4 * 4;
+    uint32_t slots_log2 = 6;
+    while ((1u << slots_log2) < 2 * (a.k + 1)) ++slots_log2;
+    if (rows_are_short(a, sms)) {
+      const uint32_t bytes = kShortWarps * (room * 12 + (4u << slots_log2)), want = (a.rows + kShortWarps - 1) / kShortWarps;
+      auto go = [&](auto kernel) {
+        int e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e) return e;
+        kernel<<<want < cap ? want : cap, 32 * kShortWarps, bytes, (cudaStream_t)stream>>>(a, room, slots_log2, alike);
+        return (int)cudaGetLastError();
+      };
+      if (!a.dlogits) return two ? go(short_kernel<T, 1, true>) : go(short_kernel<T, 1, false>);
+      if (!a.loss) return two ? go(short_kernel<T, 2, true>) : go(short_kernel<T, 2, false>);
+      return two ? go(short_kernel<T, 3, true>) : go(short_kernel<T, 3, false>);
+    }
+    Layout l = {};
+    l.teachers = a.k <= 256 ? kTeachers : a.k <= 512 ? (kTeachers + 1) / 2 : 1;
+    l.room = room;
+    l.slots_log2 = slots_log2;
+    constexpr uint32_t kRoom = 227 * 1024 / kCtas - 1024;
+    l.chunks = std::min((uint32_t)kMaxChunks, (kRoom - l.bytes()) / (kChunk * 16));
+    // a row over more CTAs while they would not fill the GPU, but not into parts of
+    // less than two chunks
+    uint32_t split = 1;
+    while (split < (uint32_t)kMaxSplit && body / (2 * split) >= 2 * kChunk && (uint64_t)a.rows * split <= sms) split *= 2;
+    const uint64_t most = cap >= split ? cap / split : 1;
+    const unsigned grid = (unsigned)(a.rows < most ? a.rows : most) * split;
     auto go = [&](auto kernel, bool cluster) {
       int e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)l.bytes());
       if (e) return e;

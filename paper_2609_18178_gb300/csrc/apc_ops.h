@@ -85,6 +85,6 @@ struct DistillArgs {
 };
 
 int launch_distill(const DistillArgs &a, unsigned cap, unsigned sms, void *stream);
-int distill_per_sm(const DistillArgs &a);
+int distill_per_sm(const DistillArgs &a, unsigned sms);
 
 }  // namespace apc

@@ -230,7 +230,7 @@ apc_status distill(const apc_distill *d, const float *grad_loss, float *loss, fl
   a.loss_label = (float)d->label_weight;
   unsigned cap = 0;
   unsigned sms = 0;
-  if ((st = apc::op_grid(apc::distill_per_sm(a), &cap, &sms)) != APC_OK) return st;
+  if ((st = apc::op_grid(1, &cap, &sms)) != APC_OK || (st = apc::op_grid(apc::distill_per_sm(a, sms), &cap)) != APC_OK) return st;
   const int e = apc::launch_distill(a, cap, sms, stream);
   return e ? apc::op_cuda_fail(e, "distillation kernel launch") : APC_OK;
 }

@@ -224,7 +224,8 @@ def distill_loss(logits, ids, teacher, *, temperature=1.0, kd_weight=1.0, teache
     The teacher is normalised over the row's entries or, with ``teacher_lse``
     (fp32 ``[rows]``: logsumexp of all its logits over the temperature), over
     its whole vocabulary.  Entries whose id lies outside the vocabulary or whose
-    logit is -inf do not count, nor do labels outside it.
+    logit is -inf do not count, nor do labels outside it.  A row with no logit
+    above -1e30 is masked whole: loss 0, gradient 0.
 
     Returns ``(loss, lse)``: fp32 ``[rows]``, and the statistics that
     :func:`distill_grad` takes, fp32 ``[1 or, with labels, 2, rows]``."""

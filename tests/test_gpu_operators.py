@@ -319,12 +319,13 @@ def ref_distill(z, ids, u, g, tau, wk, wl, lse_t=None, labels=None):
         lse[0, t], lse[1, t] = torch.logsumexp(z[t] / tau, 0), torch.logsumexp(z[t], 0)
         ok = (ids[t] >= 0) & (ids[t] < v) & (u[t] != -math.inf)
         i, x = ids[t][ok], u[t][ok]
-        if torch.isneginf(lse[0, t]):
+        if z[t].max() <= -1e30:  # masked whole
+            lse[:, t] = -math.inf
             continue
         if len(i):
             lp = x - (lse_t[t].double().cpu() if lse_t is not None else torch.logsumexp(x, 0))
             p, lq = lp.exp(), z[t, i] / tau - lse[0, t]
-            loss[t] = wk * tau ** 2 * torch.where(p > 0, p * (lp - lq), 0.0).sum()
+            loss[t] = wk * tau ** 2 * torch.where(p == 0, 0.0, p * (lp - lq)).sum()
             p_sum[t] = p.sum()
             e = torch.softmax(z[t] / tau, 0) * p.sum()
             d[t] += wk * tau * e
@@ -344,14 +345,21 @@ def ref_distill(z, ids, u, g, tau, wk, wl, lse_t=None, labels=None):
             d[t] *= float(g[t])
             size[t] *= abs(float(g[t]))
             if float(g[t]) == 0:
-                d[t] = 0
+                d[t], size[t] = 0, 0
     return loss, lse, d, size, p_sum
 
 
 def close(got, want, bound):
-    got, want = got.double().cpu(), want.double()
-    fine = torch.isfinite(want)
-    assert torch.equal(got[~fine], want[~fine])
+    """Infinities and NaNs where the result, in got's type, has them; |error| <= bound elsewhere (where the bound
+    reaches beyond the type's range, the result may have left it)."""
+    want = want.double()
+    fine = torch.isfinite(want.to(got.dtype))
+    edge = fine & ~torch.isfinite((want.abs() + bound.nan_to_num(nan=0.0)).to(got.dtype))
+    got = torch.where(edge.to(got.device), want.to(got.dtype).to(got.device), got)
+    got, want = got.double().cpu(), torch.where(fine, want, want.to(got.dtype).double())
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    there = ~fine & ~torch.isnan(want)
+    assert torch.equal(got[there], want[there])
     assert torch.isfinite(got[fine]).all()
     worst = ((got - want).abs()[fine] / bound[fine]).max().item() if fine.any() else 0.0
     assert worst <= 1.0, worst
@@ -374,7 +382,8 @@ def check_distill(z, ids, u, g, tau=1.0, wk=1.0, wl=0.0, lse_t=None, labels=None
     rel = relative(z, u, tau)
     spread_ = lse[0].abs().nan_to_num(posinf=0, neginf=0) + lse[1].abs().nan_to_num(posinf=0, neginf=0) + 8
     bound_lse = rel * torch.ones_like(lse) * 2
-    bound_loss = (wk * tau ** 2 * p_sum + wl + 1e-30) * rel * (2 + spread_) * 4
+    # an entry on a masked logit (its type's lowest value) makes terms as large as the loss itself
+    bound_loss = (wk * tau ** 2 * p_sum + wl + 1e-30) * rel * (2 + spread_) * 4 + rel * loss.abs().nan_to_num(nan=0, posinf=0)
     bound_d = size * (UNIT[z.dtype] + 2 * rel) + TINY[z.dtype] + UNIT[z.dtype] * d.abs()
     got, stats = apc.distill_loss(z, ids, u, **kw)
     close(stats, lse[:n], bound_lse[:n])
@@ -462,7 +471,7 @@ def test_distill_masks(vocab, dtype):
     z[0, 100:] = -math.inf
     z[1, 100:] = low
     z[2] = -math.inf
-    z[3] = low                      # all equal: a uniform row
+    z[3] = low                      # masked whole too
     ids[4] = -1
     u[5] = -math.inf
     ids[0] = torch.arange(k, device="cuda")
@@ -540,6 +549,43 @@ def test_distill_repeats_and_does_not_depend_on_the_grid(monkeypatch):
         monkeypatch.delenv("APC_GRID_LIMIT")
         for x, y, w in zip(first, again, other):
             assert torch.equal(x, y) and torch.equal(x, w)
+
+
+@pytest.mark.parametrize("vocab,k", [(1, 1), (5, 7), (100, 10), (513, 40), (2049, 256), (4095, 33), (4097, 300)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_distill_many_short_rows(vocab, k, dtype):
+    """More rows than SMs: masks of both kinds, rows without a student or a
+    teacher, equal ids, labels on them, odd starts of the rows."""
+    rows = 170
+    z = torch.randn(rows, vocab, generator=gen(1), device="cuda").mul_(3)
+    z[::7, vocab // 2:] = -math.inf
+    z[1::7, vocab // 2:] = torch.finfo(dtype).min
+    z[2::31] = -math.inf
+    z[3::37] = torch.finfo(dtype).min
+    z = strided(z.to(dtype), 1, 3)
+    ids, u = teacher_of(rows, vocab, k, 2, wide=False)
+    ids[::7] = ids[::7].clamp(max=max(0, vocab // 2 - 1)) if vocab > 1 else -1  # not on the masked half
+    ids[4::41] = -1
+    ids[5::43, k // 2:] = ids[5::43, :1]
+    u[5::43] = 1.0
+    labels = torch.randint(0, max(1, vocab // 2), (rows,), generator=gen(4), device="cuda")
+    if vocab == 1:
+        labels[::7] = -1
+    labels[::5] = -100
+    g = torch.rand(rows, generator=gen(5), device="cuda") - 0.3
+    g[::11] = 0.0
+    check_distill(z, ids, u, g)
+    check_distill(z, ids, u, g, 2.5, 0.7, 0.3, None, labels)
+    check_distill(z, ids, u, g, 1.0, 0.7, 0.3, torch.full((rows,), 4.0, device="cuda"), labels)
+
+
+@pytest.mark.parametrize("vocab", [30000, 250000])
+def test_distill_rows_beyond_shared_memory(vocab):
+    """Rows that are read a second time for the gradient, many and few."""
+    for rows, dtype in ((160, torch.float32), (3, torch.float32), (2, torch.bfloat16)):
+        z = torch.randn(rows, vocab, generator=gen(1), device="cuda").mul_(3).to(dtype)
+        ids, u = teacher_of(rows, vocab, 600, 2)
+        check_distill(z, ids, u, weights(rows), 1.5, 1.0, 0.5, None, torch.arange(rows, device="cuda"))
 
 
 def test_operators_on_a_stream_of_their_own():
