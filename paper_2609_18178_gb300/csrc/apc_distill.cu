@@ -148,7 +148,9 @@ __device__ __noinline__ void teacher_entries(const DistillArgs &a, uint32_t row,
   int32_t *ids = e.id;
   float *ps = e.p, *zs = e.z;
   float top = -kInf;
-  constexpr int kBatch = 8;  // entries a lane has in flight: their ids, then the student's logits there
+  // entries a lane has in flight: their ids, then the student's logits there (8
+  // cost the rows' own arithmetic more than they saved: 268 us for 8192 x 32768, 246)
+  constexpr int kBatch = 2;
   for (uint32_t i0 = lane; i0 < a.k; i0 += 32 * kBatch) {
     int32_t id[kBatch];
     float u[kBatch], x[kBatch];
@@ -458,10 +460,11 @@ __device__ __forceinline__ void store_vector(T *body, uint32_t k, const uint4 &v
 // gradient.  A row's way takes some 6 us, most of it waiting, so what counts is how
 // many are under way: 24 on an SM, where the kernel below has 2.  Up to
 // kShortVectors of 16 bytes a lane stay in registers; a longer row's second sweep
-// finds it in L2.  Measured on 8192 rows: 100 logits in SHORT_100 us (104 below),
-// 1000 in SHORT_1000 (121), 5000 (loss) in SHORT_5000 (69).
+// finds it in L2.  Loss and gradient of 8192 rows of bf16: 100 logits 21 us (104
+// below), 1000 with labels 29 (121), 5000 48 (118); 300 rows of 4000 12 (9.4), 4096
+// rows of 32768 (loss) 69 (53): hence the limits on both sides.
 constexpr int kShortWarps = 8, kShortVectors = 8, kShortCtas = 3;
-constexpr uint32_t kShortBytes = 8192, kShortEntries = 256;
+constexpr uint32_t kShortBytes = 24576, kShortEntries = 256;
 
 template <typename T, int FORM, bool TWO>
 __global__ void __launch_bounds__(32 * kShortWarps, kShortCtas)
@@ -717,7 +720,7 @@ namespace {
 
 // A warp for each row where rows are short and enough of them to fill the GPU.
 bool rows_are_short(const DistillArgs &a, unsigned sms) {
-  return a.vocab * (a.dtype == APC_F32 ? 4u : 2u) <= kShortBytes && a.k <= kShortEntries && a.rows >= sms;
+  return a.vocab * (a.dtype == APC_F32 ? 4u : 2u) <= kShortBytes && a.k <= kShortEntries && a.rows >= 4 * sms;
 }
 
 }  // namespace
