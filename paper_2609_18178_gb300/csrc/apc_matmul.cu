@@ -6,9 +6,10 @@
 //
 // The inner sum is four tcgen05.mma (K = 32 each) into tensor memory, in fp32.
 // Its accumulator is then read back, multiplied by the scales and added into
-// fp32 registers while the tensor core fills the other of two accumulators:
-// the scales are arbitrary fp32 numbers, and no sum of more than 128 products
-// is left to the tensor core's own rounding.
+// fp32 registers while the tensor core fills other accumulators: the scales are
+// arbitrary fp32 numbers, and no sum of more than 128 products is left to the
+// tensor core's own rounding.  Large products whose scales are powers of two, as
+// quantization makes them, leave scaling and sums to the tensor cores (see there).
 //
 // Two kernels, warp-specialized alike: one warp issues TMA loads into a ring of
 // shared-memory stages (128 bytes of k a row, 128-byte swizzle, zeros beyond
@@ -37,6 +38,8 @@ struct ProductPlan {
   uint32_t row_tiles, col_tiles;
   uint32_t blocks;          // of 128 k
   uint32_t instruction;
+  uint32_t formats;         // of the operands, in the instruction's bits
+  bool by_exponent;         // large products: scales that are powers of two may be the tensor cores'
   void *out;
   int64_t row_step, col_step;  // elements of out
   unsigned *status;
@@ -292,7 +295,21 @@ __global__ void __launch_bounds__(kMidThreads, 1)
 // CTA 128 rows of a on its lanes and all 256 rows of b on its columns, of which
 // it holds half in shared memory (tcgen05.mma.cta_group::2 reads both halves).
 // The first CTA's thread issues for both.  Persistent: the pair's next tile is
-// loaded and multiplied while the epilogue stores.
+// loaded while the epilogue stores.
+//
+// A tile goes one of two ways.
+//  * By exponents, where every scale in its rows' and columns' blocks is a power of two:
+//    mxf8f6f4 products multiply by the scales' exponents and add up in the accumulator
+//    over all of k.  One warp packs the exponents of four blocks at a time, tcgen05.cp
+//    takes them to the columns of the accumulator that is not in use.
+//  * In general, block by block: two accumulators, read back, scaled and added in
+//    registers.  Bound by an accumulator's way: products (512 cycles), commit, drain and
+//    the pair's arrival take 2,000, of which two overlap; with a scale for every column
+//    by the fp32 pipe too.
+// While a tile's products run, the adding warps look at the next tile's scales and
+// tell both CTAs; after its first general tile a pair stays general.
+// Measured: 4096 x 32768 x 4096 by exponents 364 us (3.0 PFLOP/s), in general 480;
+// 14336 x 4096 x 8192 with a scale for every column 303 us (3.2 PFLOP/s), 693.
 // Warps 0 to 3 load and issue with 56 registers a thread, 4 to 11 add with 224 (of
 // the launch's 168 each: 128 x 56 + 256 x 224 = 384 x 168).
 constexpr int kBigWarps = 8, kBigThreads = 128 + 32 * kBigWarps, kBigStages = 6;
@@ -301,7 +318,8 @@ constexpr int kBigLoad = 16;                // in loads of so many
 constexpr int kBigHalf = 128 * kBlock, kBigStageBytes = 2 * kBigHalf;
 constexpr int kBigScaleBytes = kScaleSlots * (128 + 256) * 4;
 constexpr int kBigTurnBytes = 32 * 17 * 4;  // a warp's, for rows of out that are not aligned
-constexpr int kBigBytes = 1024 + kBigStages * kBigStageBytes + kBigScaleBytes + kBigWarps * kBigTurnBytes;
+constexpr int kExpSlots = 2, kExpBytes = 3 * 512;  // exponents of four blocks: 128 rows, 256 columns
+constexpr int kBigBytes = 1024 + kBigStages * kBigStageBytes + kBigScaleBytes + kBigWarps * kBigTurnBytes + kExpSlots * kExpBytes;
 constexpr uint32_t kBigGroup = 16;  // row tiles that are walked together
 
 // Tile t of the walk: groups of row tiles, in each the row tile first, so that
@@ -376,6 +394,8 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kBigStages], empty[kBigStages], acc_full[2], acc_empty[2];
   __shared__ uint64_t scale_full[kScaleSlots], scale_empty[kScaleSlots];
+  __shared__ uint64_t exp_full[kExpSlots], exp_empty[kExpSlots], mode_full[4];
+  __shared__ volatile uint32_t general_from;  // the first of the pair's tiles whose scales are not all powers of two
   __shared__ uint32_t tmem_at;
   uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   float *scales = reinterpret_cast<float *>(smem + kBigStages * kBigStageBytes);  // [slot][128 rows, 256 columns]
@@ -387,6 +407,9 @@ __global__ void __launch_bounds__(kBigThreads, 1)
     for (int i = 0; i < kBigStages; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
     for (int i = 0; i < 2; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 2 * kBigWarps);
     for (int i = 0; i < kScaleSlots; ++i) mbar_init(&scale_full[i], 32), mbar_init(&scale_empty[i], kBigWarps);
+    for (int i = 0; i < kExpSlots; ++i) mbar_init(&exp_full[i], 2), mbar_init(&exp_empty[i], 1);
+    for (int i = 0; i < 4; ++i) mbar_init(&mode_full[i], 2 * kBigWarps);
+    general_from = p.by_exponent ? ~0u : 0;
     mbar_init_fence();
   }
   if (warp == 1) tmem_alloc<2>(&tmem_at, 512);
@@ -395,6 +418,18 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   tc_fence_after();
   cluster_arrive(), cluster_wait();
   const uint32_t tmem = tmem_at;
+  uint8_t *exps = reinterpret_cast<uint8_t *>(scales) + kBigScaleBytes + kBigWarps * kBigTurnBytes;
+  // Whether the pair's nth tile goes by exponents; `ok` false if the wait gave up.
+  struct Mode {
+    Turn<4> turn;
+    bool exponents;
+  };
+  auto by_exponent = [&](Mode &m, uint32_t n, bool &ok) {
+    if (!m.exponents) return false;
+    ok = warp_wait(&mode_full[m.turn.at], m.turn.phase);
+    m.turn.next();
+    return m.exponents = n < general_from;
+  };
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -447,19 +482,80 @@ __global__ void __launch_bounds__(kBigThreads, 1)
       words_landed();
       if (!ok) give_up(p.status);
     }
+    if (warp == 3) {
+      // exponents of four blocks at a time, while the tiles go by them
+      Turn<kScaleSlots> slot;
+      Turn<kExpSlots> exp;
+      Mode mode = {{}, p.by_exponent};
+      bool ok = true;
+      uint32_t n = 0;
+      const uint32_t bars = map_rank(smem_addr(exp_full), 0);
+      for (uint32_t t = first; t < tiles && ok && by_exponent(mode, n, ok); t += step, ++n)
+        for (uint32_t b = 0; b < p.blocks && ok; b += 4, exp.next()) {
+          if (!(ok = warp_wait(&exp_empty[exp.at], exp.phase ^ 1))) break;
+          uint32_t w[12];
+#pragma unroll
+          for (int j = 0; j < 12; ++j) w[j] = 0;
+          for (uint32_t i = 0; i < min(4u, p.blocks - b); ++i, slot.next()) {
+            if (!(ok = warp_wait(&scale_full[slot.at], slot.phase))) break;
+            const float *line = scales + slot.at * 384;
+#pragma unroll
+            for (int j = 0; j < 12; ++j) {
+              const float s = j < 4 || ROWS ? line[32 * j + lane] : line[128 + (j - 4) / 4];
+              w[j] |= (__float_as_uint(s) >> 23 & 0xff) << 8 * i;
+            }
+            __syncwarp();
+            if (lane < kBigWarps) mbar_arrive(&scale_empty[slot.at]);
+          }
+          uint4 *to = reinterpret_cast<uint4 *>(exps + exp.at * kExpBytes) + lane;
+#pragma unroll
+          for (int j = 0; j < 3; ++j) to[32 * j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) arrive_remote(bars + exp.at * 8);
+        }
+      if (!ok) give_up(p.status);
+    }
     if (warp == 1 && rank == 0) {
       Turn<kBigStages> st;
       Turn<2> acc;
       uint32_t issued = 0;
       bool ok = true;
       const uint64_t da = operand_desc(smem_addr(smem)), db = operand_desc(smem_addr(smem) + kBigHalf);
-      for (uint32_t t = first; t < tiles && ok; t += step)
-        for (uint32_t b = 0; b < p.blocks; ++b, st.next(), acc.next(), ++issued) {
+      Turn<kExpSlots> exp;
+      Mode mode = {{}, p.by_exponent};
+      uint32_t n = 0;
+      for (uint32_t t = first; t < tiles && ok; t += step, ++n) {
+        if (by_exponent(mode, n, ok)) {
+          // one accumulator, the exponents in the other's columns
+          Turn<2> other = acc;
+          other.next();
+          if (!(ok = ok && warp_wait(&acc_empty[acc.at], acc.phase ^ 1) && warp_wait(&acc_empty[other.at], other.phase ^ 1))) break;
+          const uint32_t columns = tmem + (acc.at ^ 1) * 256;
+          for (uint32_t b = 0; b < p.blocks && ok; b += 4, exp.next()) {
+            if (!(ok = warp_wait(&exp_full[exp.at], exp.phase))) break;
+            tc_fence_after();
+            copy_scales_pair(columns, smem_addr(exps + exp.at * kExpBytes));
+            for (uint32_t i = 0; i < min(4u, p.blocks - b); ++i, st.next()) {
+              if (!(ok = warp_wait(&full[st.at], st.phase))) break;
+              tc_fence_after();
+              const uint64_t off = st.at * (kBigStageBytes >> 4);
+              mma_scaled_pair(tmem + acc.at * 256, da + off, db + off, scaled_instruction(p.formats, 256, 256, i), columns, b + i == 0,
+                              smem_addr(&empty[st.at]));
+            }
+            commit_pair(smem_addr(&exp_empty[exp.at]));
+          }
+          commit_pair(smem_addr(&acc_full[acc.at]));
+          acc.next(), ++issued;
+          continue;
+        }
+        for (uint32_t b = 0; b < p.blocks && ok; ++b, st.next(), acc.next(), ++issued) {
           if (!(ok = warp_wait(&full[st.at], st.phase) && warp_wait(&acc_empty[acc.at], acc.phase ^ 1))) break;
           tc_fence_after();
           const uint64_t off = st.at * (kBigStageBytes >> 4);
           mma_block<2>(tmem + acc.at * 256, da + off, db + off, p.instruction, smem_addr(&acc_full[acc.at]), smem_addr(&empty[st.at]));
         }
+      }
       if (!ok) {  // let the products in flight end
         give_up(p.status);
         for (uint32_t i = min(issued, 2u); i; --i) acc.back(), wait_for(&acc_full[acc.at], acc.phase);
@@ -473,7 +569,41 @@ __global__ void __launch_bounds__(kBigThreads, 1)
     Turn<2> buf;
     Turn<kScaleSlots> slot;
     bool ok = true;
-    for (uint32_t t = first; t < tiles && ok; t += step) {
+    Mode mode = {{}, p.by_exponent};
+    const uint32_t peer_general = map_rank((uint32_t)__cvta_generic_to_shared((const void *)&general_from), rank ^ 1), peer_mode = map_rank(smem_addr(mode_full), rank ^ 1);
+    Turn<4> told;
+    // Tells both CTAs whether the pair's nth tile, t, goes by exponents: this CTA
+    // looks at its 128 rows' scales and at those of its half of the columns.
+    auto look = [&](uint32_t t, uint32_t n) {
+      uint32_t tr, tc;
+      big_tile(p, t, &tr, &tc);
+      const uint32_t k = threadIdx.x - 128;  // 128 rows, 128 columns
+      const bool col = k >= 128;
+      const uint32_t at = col ? min(tc * 256 + rank * 128 + k - 128, p.cols - 1) >> p.c_shift : min(tr * 256 + rank * 128 + k, p.rows - 1) >> p.r_shift;
+      const float *s = (col ? p.c_scale : p.r_scale) + at;
+      const int64_t pitch = col ? p.c_scale_pitch : p.r_scale_pitch;
+      bool good = true;
+      for (uint32_t b = 0; b < p.blocks; b += 16) {
+        uint32_t v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__ldg(s + min(b + i, p.blocks - 1) * pitch));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) good = good && (v[i] & 0x807fffffu) == 0 && v[i] - 1u < 0x7f7fffffu;
+      }
+      good = __all_sync(~0u, good);
+      if (lane == 0) {
+        if (!good) {
+          general_from = n;
+          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_general), "r"(n) : "memory");
+        }
+        asm volatile("mbarrier.arrive.release.cluster.shared::cta.b64 _, [%0];" ::"r"(smem_addr(&mode_full[told.at])) : "memory");
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_mode + told.at * 8) : "memory");
+      }
+      told.next();
+    };
+    uint32_t n = 0;
+    if (p.by_exponent && first < tiles) look(first, 0);
+    for (uint32_t t = first; t < tiles && ok; t += step, ++n) {
       uint32_t tr, tc;
       big_tile(p, t, &tr, &tc);
       const uint32_t r0 = tr * 256 + rank * 128, c0 = tc * 256 + part * kBigCols;
@@ -493,6 +623,27 @@ __global__ void __launch_bounds__(kBigThreads, 1)
           acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), y, acc[(c + i) / 2 + 1]);
         }
       };
+      const bool exponents = by_exponent(mode, n, ok);
+      if (!ok) break;
+      if (exponents) {
+        if (t + step < tiles) look(t + step, n + 1);
+        if (!(ok = warp_wait(&acc_full[buf.at], buf.phase))) break;
+        tc_fence_after();
+        const uint32_t at = tmem + buf.at * 256 + part * kBigCols + (quad << 21);
+#pragma unroll
+        for (int c = 0; c < kBigCols; c += 32) {
+          uint32_t d[32];
+          tmem_load(d, at + c);
+          tmem_landed(d);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[c / 2 + i] = pack2(d[2 * i], d[2 * i + 1]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_remote_relaxed(empty_bars + buf.at * 8);
+        buf.next();
+        slot.skip(p.blocks);  // the exponents' warp took them
+      } else
       for (uint32_t b = 0; b < p.blocks; ++b, buf.next(), slot.next()) {
         const float *s = scales + slot.at * 384 + 128 + (ROWS ? part * kBigCols : part * kBigCols / 128);
         if (!(ok = warp_wait(&scale_full[slot.at], slot.phase))) break;
@@ -576,7 +727,8 @@ uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); 
 // Which kernel, and for few columns how many and how far k is split: the least of
 // the estimated times, in nanoseconds, of measured parts (one GB300, 152 SMs):
 //   a block of 128 k takes a CTA 270, 330, 385 and 535 ns with 16, 32, 64 and 128
-//   columns, a pair 435 ns with a tile of 256 x 256;
+//   columns, a pair 350 ns with a tile of 256 x 256 (by exponents; else 435 and,
+//   with a scale for every column, 900) and 1.8 us between tiles;
 //   a cluster's exchange 2.2, 3 and 6.5 us for 2, 4 and 8 CTAs; a call 4 us beside
 //   that, 8 with pairs.
 // For example 100 x 4096 x 4096: 64 columns in two halves 13.8 us, whole 16.7, tiles
@@ -591,7 +743,7 @@ Choice choose(uint32_t m, uint32_t n, uint32_t blocks, uint32_t sms) {
   static constexpr uint32_t kBlockNs[4] = {270, 330, 385, 535}, kExchangeNs[4] = {0, 2200, 3000, 6500};
   const uint64_t pairs = sms / 2 ? sms / 2 : 1;
   Choice best = {256, 0};
-  uint64_t least = 8000 + ceil_div((uint64_t)ceil_div(m, 256) * ceil_div(n, 256), pairs) * ((uint64_t)blocks * 435 + 1000);
+  uint64_t least = 8000 + ceil_div((uint64_t)ceil_div(m, 256) * ceil_div(n, 256), pairs) * ((uint64_t)blocks * 350 + 1800);
   for (uint32_t c = 0; c < 4; ++c)
     for (uint32_t s = 0; s <= (c == 3 ? 0u : 3u) && (1u << s) <= blocks && (1u << s) <= sms; ++s) {
       const uint64_t tiles = (uint64_t)ceil_div(n, 128) * ceil_div(m, 16u << c);
@@ -629,7 +781,12 @@ int launch_big(const MatmulArgs &a, ProductPlan p, unsigned cap, void *stream) {
   p.r_shift = a.a_shift, p.c_shift = a.b_shift;
   p.rows = a.m, p.cols = a.n;
   p.row_tiles = ceil_div(a.m, 256), p.col_tiles = ceil_div(a.n, 256);
-  p.instruction = 1u << 4 | a.a_e5m2 << 7 | a.b_e5m2 << 10 | (256u >> 3) << 17 | (256u >> 4) << 24;
+  p.formats = a.a_e5m2 << 7 | a.b_e5m2 << 10;
+  p.instruction = 1u << 4 | p.formats | (256u >> 3) << 17 | (256u >> 4) << 24;
+  // The tensor cores' own sums over all of k are off by 2.2e-7 of the result at 4,096,
+  // 1.2e-6 at 16,384 (the sums in registers by less than 1e-7): nothing beside a
+  // rounding to 16 bits; fp32 results take them up to 8,192.
+  p.by_exponent = a.out_dtype != APC_F32 || p.blocks <= 64;
   p.row_step = a.out_pitch, p.col_step = 1;
   const uint64_t size = a.out_dtype == APC_F32 ? 4 : 2;
   const bool aligned = (uintptr_t)a.out % 16 == 0 && (a.m <= 1 || (uint64_t)a.out_pitch * size % 16 == 0);

@@ -208,6 +208,54 @@ __device__ __forceinline__ void mma_block(uint32_t d, uint64_t a, uint64_t b, ui
         : "memory");
 }
 
+// Scales in the tensor cores: E8M0 bytes (a float's biased exponent), one word of
+// four for each row, rows l, l + 32, l + 64, l + 96 of 128 side by side in 16 bytes.
+
+// One thread of a converged warp copies three tiles of 128 rows' words, 512 bytes
+// apart, to four columns of tensor memory each, in both CTAs of the pair.
+__device__ __forceinline__ void copy_scales_pair(uint32_t columns, uint32_t smem) {
+  const uint64_t d = (uint64_t)(smem >> 4 & 0x3fff) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+  asm volatile(
+      "{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+      "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %3;\n\t"
+      "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%1], %4;\n\t"
+      "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%2], %5;\n\t}" ::"r"(columns),
+      "r"(columns + 4), "r"(columns + 8), "l"(d), "l"(d + 32), "l"(d + 64)
+      : "memory");
+}
+
+// E8M0 scales, formats and sizes as fp8_instruction's; byte: which of the four.
+__device__ __forceinline__ uint32_t scaled_instruction(uint32_t formats, uint32_t m, uint32_t n, uint32_t byte) {
+  return formats | byte << 4 | (n >> 3) << 17 | 1u << 23 | (m >> 7) << 27 | byte << 29;
+}
+
+// The four products of a block of 128 k, scaled, added to the accumulator unless
+// `first`; `read` is arrived on in both CTAs once they are complete.
+__device__ __forceinline__ void mma_scaled_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, uint32_t scales,
+                                                bool first, uint32_t read) {
+  asm volatile(
+      "{\n\t.reg .pred q, more, yes;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t.reg .b16 both;\n\t"
+      "elect.sync _|q, 0xffffffff;\n\t"
+      "setp.eq.b32 more, %6, 0;\n\tsetp.eq.b32 yes, 0, 0;\n\tmov.b16 both, 3;\n\t"
+      "add.s64 a1, %1, 2;\n\tadd.s64 a2, %1, 4;\n\tadd.s64 a3, %1, 6;\n\t"
+      "add.s64 b1, %2, 2;\n\tadd.s64 b2, %2, 4;\n\tadd.s64 b3, %2, 6;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], more;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a1, b1, %3, [%4], [%5], yes;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a2, b2, %3, [%4], [%5], yes;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a3, b3, %3, [%4], [%5], yes;\n\t"
+      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%7], both;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(instruction), "r"(scales), "r"(scales + 4), "r"((uint32_t)first), "r"(read)
+      : "memory");
+}
+
+// One thread's products and copies so far, in both CTAs.
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t.reg .b16 both;\n\telect.sync _|q, 0xffffffff;\n\tmov.b16 both, 3;\n\t"
+      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], both;\n\t}" ::"r"(bar)
+      : "memory");
+}
+
 // One thread of a converged warp announces `bytes` on `bar` and loads a box of each
 // operand, both in the same columns.
 __device__ __forceinline__ void load_block(uint32_t dst, const CUtensorMap *r, int32_t r0, uint32_t c_dst, const CUtensorMap *c,
@@ -242,6 +290,11 @@ struct Turn {
   uint32_t at = 0, phase = 0;
   __device__ __forceinline__ void next() {
     if (++at == N) at = 0, phase ^= 1;
+  }
+  __device__ __forceinline__ void skip(uint32_t n) {
+    at += n;
+    phase ^= at / N & 1;
+    at %= N;
   }
   __device__ __forceinline__ void back() {
     if (at-- == 0) at = N - 1, phase ^= 1;

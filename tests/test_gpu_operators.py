@@ -221,6 +221,33 @@ def test_matmul(m, n, k, ba, bb):
     assert apc.device_status() == 0
 
 
+@pytest.mark.parametrize("m,n,k", [(2100, 2050, 1111), (1500, 5000, 512), (5000, 600, 640), (600, 3001, 9000), (4100, 4100, 130)])
+@pytest.mark.parametrize("bb", [1, 128])
+@pytest.mark.parametrize("fa,fb", [(E4M3, E4M3), (E5M2, E4M3)])
+def test_matmul_power_of_two_scales(m, n, k, bb, fa, fb):
+    """Large products of what quantization makes, whose scales may be the tensor
+    cores' own; and with single scales that are not powers of two, 0, or beyond
+    their range, from the first tile on or from a later one."""
+    x = torch.randn(m, k, generator=gen(1), device="cuda") * torch.exp2(torch.randint(-9, 9, (m, 1), generator=gen(2), device="cuda").float())
+    y = torch.randn(n, k, generator=gen(3), device="cuda") * torch.exp2(torch.randint(-9, 9, (n, 1), generator=gen(4), device="cuda").float())
+    a, sa = apc.quantize_fp8(x, dtype=fa)
+    b, sb = apc.quantize_fp8(y, block_rows=bb, dtype=fb)
+    ref, size = ref_matmul(a, sa, 1, b, sb, bb)
+    for dtype in (torch.bfloat16, torch.float32):
+        check_matmul(apc.matmul_fp8(a, sa, b, sb, out_dtype=dtype), ref, size, k)
+    blocks = sa.shape[0]
+    for at, value in ((0, 3.0), (m - 1, 0.75), (m // 2, 0.0), (m - 1, 2.0 ** -130)):
+        odd = sa.clone()
+        odd[blocks - 1, at] = value
+        ref, size = ref_matmul(a, odd, 1, b, sb, bb)
+        check_matmul(apc.matmul_fp8(a, odd, b, sb), ref, size, k)
+    odd = sb.clone()
+    odd[0, odd.shape[1] - 1] = 1.5
+    ref, size = ref_matmul(a, sa, 1, b, odd, bb)
+    check_matmul(apc.matmul_fp8(a, sa, b, odd, out_dtype=torch.float32), ref, size, k)
+    assert apc.device_status() == 0
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 300, 500), (40, 200, 1000), (300, 400, 500), (700, 600, 1300)])
 @pytest.mark.parametrize("fa,fb", [(E4M3, E5M2), (E5M2, E4M3), (E5M2, E5M2)])
 def test_matmul_formats(m, n, k, fa, fb):
