@@ -317,7 +317,7 @@ constexpr int kBigCols = 1024 / kBigWarps;  // columns that a warp adds
 constexpr int kBigLoad = 16;                // in loads of so many
 constexpr int kBigHalf = 128 * kBlock, kBigStageBytes = 2 * kBigHalf;
 constexpr int kBigScaleBytes = kScaleSlots * (128 + 256) * 4;
-constexpr int kBigTurnBytes = 32 * 17 * 4;  // a warp's, for rows of out that are not aligned
+constexpr int kBigTurnBytes = 32 * 68;  // a warp's, for its way to out
 constexpr int kExpSlots = 2, kExpBytes = 3 * 512;  // exponents of four blocks: 128 rows, 256 columns
 constexpr int kBigBytes = 1024 + kBigStages * kBigStageBytes + kBigScaleBytes + kBigWarps * kBigTurnBytes + kExpSlots * kExpBytes;
 constexpr uint32_t kBigGroup = 16;  // row tiles that are walked together
@@ -331,56 +331,62 @@ __device__ __forceinline__ void big_tile(const ProductPlan &p, uint32_t t, uint3
   *c = i / height;
 }
 
-// A warp's 32 rows of kBigCols sums, a row a lane, to out (this lane's row), of which
-// `count` columns and, where `in`, the row exist.  Rows that start on 16-byte
-// boundaries are stored by their lanes; others go through shared memory, 16 columns
-// at a time, so that a store instruction writes two rows' neighbours and not 32
-// rows' single elements.
-constexpr int kTurnCols = 16, kTurnPitch = kTurnCols + 1;
-
+// A warp's 32 rows of kBigCols sums, a row a lane, to out (lane 0's row), of which
+// `count` columns and the rows of `rows` exist.  They go through shared memory, 64
+// bytes of each row at a time, so that a store instruction writes neighbours in a
+// row: 8 rows' 64 bytes where rows start on 16-byte boundaries, one row's otherwise.
+// (Stored by their own lanes, 16 bytes in each of 32 rows, a tile took 9 us.)
 template <bool ALIGNED, typename T>
-__device__ __forceinline__ void store_rows(T *out, const uint64_t (&acc)[kBigCols / 2], uint32_t count, bool in, int64_t step,
+__device__ __forceinline__ void store_rows(T *out, const uint64_t (&acc)[kBigCols / 2], uint32_t count, uint32_t rows, int64_t step,
                                            float *turn, uint32_t lane) {
-  constexpr int kPer = 16 / sizeof(T);
-  if constexpr (ALIGNED) {
-    if (!in) return;
-#pragma unroll
-    for (int i = 0; i < kBigCols; i += kPer) {
-      union {
-        T v[kPer];
-        uint4 q;
-      } u;
-#pragma unroll
-      for (int j = 0; j < kPer; j += 2) {
-        const float2 v = unpack2(acc[(i + j) / 2]);
-        u.v[j] = from_float<T>(v.x);
-        u.v[j + 1] = from_float<T>(v.y);
-      }
-      if (i + kPer <= count) {
-        *reinterpret_cast<uint4 *>(out + i) = u.q;
-      } else {
-#pragma unroll
-        for (int j = 0; j < kPer; ++j)
-          if (i + j < count) out[i + j] = u.v[j];
-      }
-    }
-    return;
-  }
-  const uint32_t rows = __ballot_sync(~0u, in);
-  T *first = out - (int64_t)lane * step;  // lane 0's row
+  constexpr int kPer = 16 / sizeof(T), kTurnCols = 64 / sizeof(T);
+  constexpr int kTurnPitch = (ALIGNED ? 64 : 68) / sizeof(T);  // aligned: 16-byte pieces, swizzled over the banks
+  T *mine = reinterpret_cast<T *>(turn);
 #pragma unroll
   for (int c = 0; c < kBigCols; c += kTurnCols) {
+    if constexpr (ALIGNED) {
 #pragma unroll
-    for (int i = 0; i < kTurnCols; i += 2) {
-      const float2 v = unpack2(acc[(c + i) / 2]);
-      turn[lane * kTurnPitch + i] = v.x;
-      turn[lane * kTurnPitch + i + 1] = v.y;
+      for (int i = 0; i < kTurnCols; i += kPer) {
+        union {
+          T v[kPer];
+          uint4 q;
+        } u;
+#pragma unroll
+        for (int j = 0; j < kPer; j += 2) {
+          const float2 v = unpack2(acc[(c + i + j) / 2]);
+          u.v[j] = from_float<T>(v.x);
+          u.v[j + 1] = from_float<T>(v.y);
+        }
+        *reinterpret_cast<uint4 *>(mine + lane * kTurnPitch + (i / kPer ^ (lane >> 1 & 3)) * kPer) = u.q;
+      }
+      __syncwarp();
+      const uint32_t col = lane % 4 * kPer;
+#pragma unroll
+      for (uint32_t r = lane / 4; r < 32; r += 8) {
+        const T *from = mine + r * kTurnPitch + (lane % 4 ^ (r >> 1 & 3)) * kPer;
+        T *to = out + (int64_t)r * step + c + col;
+        if (!(rows >> r & 1)) continue;
+        if (c + col + kPer <= count) {
+          *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from);
+        } else {
+          for (int j = 0; j < kPer; ++j)
+            if (c + col + j < count) to[j] = from[j];
+        }
+      }
+    } else {
+      constexpr int kRows = 32 / kTurnCols;  // rows a store writes
+#pragma unroll
+      for (int i = 0; i < kTurnCols; i += 2) {
+        const float2 v = unpack2(acc[(c + i) / 2]);
+        mine[lane * kTurnPitch + i] = from_float<T>(v.x);
+        mine[lane * kTurnPitch + i + 1] = from_float<T>(v.y);
+      }
+      __syncwarp();
+      const uint32_t col = lane % kTurnCols;
+#pragma unroll 8
+      for (uint32_t r = lane / kTurnCols; r < 32; r += kRows)
+        if ((rows >> r & 1) && c + col < count) out[(int64_t)r * step + c + col] = mine[r * kTurnPitch + col];
     }
-    __syncwarp();
-    const uint32_t col = lane % kTurnCols;
-#pragma unroll 4
-    for (uint32_t r = lane / kTurnCols; r < 32; r += 32 / kTurnCols)
-      if ((rows >> r & 1) && c + col < count) first[(int64_t)r * step + c + col] = from_float<T>(turn[r * kTurnPitch + col]);
     __syncwarp();
   }
 }
@@ -570,7 +576,8 @@ __global__ void __launch_bounds__(kBigThreads, 1)
     Turn<kScaleSlots> slot;
     bool ok = true;
     Mode mode = {{}, p.by_exponent};
-    const uint32_t peer_general = map_rank((uint32_t)__cvta_generic_to_shared((const void *)&general_from), rank ^ 1), peer_mode = map_rank(smem_addr(mode_full), rank ^ 1);
+    const uint32_t peer_general = map_rank((uint32_t)__cvta_generic_to_shared((const void *)&general_from), rank ^ 1);
+    const uint32_t peer_mode = map_rank(smem_addr(mode_full), rank ^ 1), own_mode = map_rank(smem_addr(mode_full), rank);
     Turn<4> told;
     // Tells both CTAs whether the pair's nth tile, t, goes by exponents: this CTA
     // looks at its 128 rows' scales and at those of its half of the columns.
@@ -595,9 +602,11 @@ __global__ void __launch_bounds__(kBigThreads, 1)
         if (!good) {
           general_from = n;
           asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_general), "r"(n) : "memory");
+          asm volatile("fence.acq_rel.cluster;" ::: "memory");
         }
-        asm volatile("mbarrier.arrive.release.cluster.shared::cta.b64 _, [%0];" ::"r"(smem_addr(&mode_full[told.at])) : "memory");
-        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_mode + told.at * 8) : "memory");
+        // no release where there is nothing to see: it would wait for the last tile's stores
+        arrive_remote_relaxed(own_mode + told.at * 8);
+        arrive_remote_relaxed(peer_mode + told.at * 8);
       }
       told.next();
     };
@@ -673,8 +682,8 @@ __global__ void __launch_bounds__(kBigThreads, 1)
       }
       if (!ok) break;
       if (c0 < p.cols)
-        store_rows<ALIGNED>(static_cast<T *>(p.out) + (int64_t)(r0 + row) * p.row_step + c0, acc, min((uint32_t)kBigCols, p.cols - c0),
-                   r0 + row < p.rows, p.row_step, turn, lane);
+        store_rows<ALIGNED>(static_cast<T *>(p.out) + (int64_t)(r0 + quad * 32) * p.row_step + c0, acc,
+                            min((uint32_t)kBigCols, p.cols - c0), __ballot_sync(~0u, r0 + row < p.rows), p.row_step, turn, lane);
     }
     if (!ok) give_up(p.status);
   }
