@@ -67,7 +67,7 @@ constexpr int kScaleSlots = 8;  // blocks whose scales are on their way or in us
 // A wait that gives up marks the CTA dead: it stops loading and issuing, waits for
 // what is in flight, and its sums go on without waiting, so that every barrier is
 // reached.
-constexpr int kMidThreads = 384;  // warps: copies, products, scales, none; 8 that add
+constexpr int kMidThreads = 352;  // warps: copies, products, scales; 8 that add
 
 template <int BN, bool SPLIT>
 struct MidShape {
@@ -82,10 +82,7 @@ struct MidShape {
   // many times as long as either
   static constexpr int kAcc = 512 / BN < 8 ? 512 / BN : 8;
   static constexpr int kTmem = kAcc * BN;
-  // a warp adds half the columns, and few of them of several blocks at a time:
-  // their waits and loads overlap
-  static constexpr int kCols = BN / 2, kGroup = BN == 16 ? 4 : BN == 32 ? 2 : 1;
-  static constexpr int kLoad = kCols < 32 ? kCols : 32;
+  static constexpr int kCols = BN / 2, kLoad = kCols < 32 ? kCols : 32;  // a warp adds half the columns
 };
 
 template <int BN, bool SPLIT, typename T>
@@ -182,66 +179,44 @@ __global__ void __launch_bounds__(kMidThreads, 1)
       }
     }
     words_landed();
-  } else if (warp >= 4) {
-    constexpr int kCols = S::kCols, kGroup = S::kGroup, kLoad = S::kLoad;
-    const uint32_t quad = warp & 3, row = quad * 32 + lane, half = (warp - 4) / 4;
+  } else {
+    constexpr int kCols = S::kCols, kLoad = S::kLoad;
+    const uint32_t quad = warp & 3, row = quad * 32 + lane, half = (warp - 3) / 4;
     Turn<S::kAcc> buf;
     Turn<kScaleSlots> slot;
     uint32_t done = 0;
-    if (SPLIT && threadIdx.x == 128) mbar_arrive_expect_tx(&recv_full, S::kShareBytes);
+    if (SPLIT && threadIdx.x == 96) mbar_arrive_expect_tx(&recv_full, S::kShareBytes);
     for (uint32_t t = first; t < tiles; t += step, ++done) {
       const uint32_t r0 = t % p.row_tiles * 128, c0 = t / p.row_tiles * BN;
       uint64_t acc[kCols / 2];
 #pragma unroll
       for (int i = 0; i < kCols / 2; ++i) acc[i] = 0;
-      for (uint32_t b = b0; b < b1; b += kGroup) {
-        const uint32_t n = min((uint32_t)kGroup, b1 - b);
-        uint32_t at[kGroup], bar[kGroup];
-        uint64_t sr[kGroup];
-        const float *s[kGroup];
-#pragma unroll
-        for (int g = 0; g < kGroup; ++g) {
-          if (g >= n) break;
-          alive(&scale_full[slot.at], slot.phase);
-          const float *line = scales + slot.at * (128 + BN);
-          s[g] = line + 128 + half * kCols;
-          sr[g] = pack2(line[row], line[row]);
-          alive(&acc_full[buf.at], buf.phase);
-          at[g] = tmem + buf.at * BN + half * kCols + (quad << 21);  // lane 32 * quad in bits 16 up
-          bar[g] = buf.at | slot.at << 16;
-          buf.next(), slot.next();
-        }
+      for (uint32_t b = b0; b < b1; ++b, buf.next(), slot.next()) {
+        alive(&scale_full[slot.at], slot.phase);
+        const float *line = scales + slot.at * (128 + BN), *s = line + 128 + half * kCols;
+        const uint64_t sr = pack2(line[row], line[row]);
+        alive(&acc_full[buf.at], buf.phase);
         tc_fence_after();
+        const uint32_t at = tmem + buf.at * BN + half * kCols + (quad << 21);  // lane 32 * quad in bits 16 up
 #pragma unroll
         for (int c = 0; c < kCols; c += kLoad) {
-          uint32_t d[kGroup][kLoad];
-#pragma unroll
-          for (int g = 0; g < kGroup; ++g)
-            if (g < n) tmem_load(d[g], at[g] + c);
-#pragma unroll
-          for (int g = 0; g < kGroup; ++g) tmem_landed(d[g]);
+          uint32_t d[kLoad];
+          tmem_load(d, at + c);
+          tmem_landed(d);
           if (c + kLoad == kCols) {
             tc_fence_before();
             __syncwarp();
-#pragma unroll
-            for (int g = 0; g < kGroup; ++g)
-              if (lane == 0 && g < n) mbar_arrive(&acc_empty[bar[g] & 0xffff]);
+            if (lane == 0) mbar_arrive(&acc_empty[buf.at]);
           }
 #pragma unroll
-          for (int g = 0; g < kGroup; ++g) {
-            if (g >= n) break;
-#pragma unroll
-            for (int i = 0; i < kLoad; i += 4) {
-              const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(s[g] + c + i);
-              acc[(c + i) / 2] = fma2(pack2(d[g][i], d[g][i + 1]), mul2(sr[g], v.x), acc[(c + i) / 2]);
-              acc[(c + i) / 2 + 1] = fma2(pack2(d[g][i + 2], d[g][i + 3]), mul2(sr[g], v.y), acc[(c + i) / 2 + 1]);
-            }
+          for (int i = 0; i < kLoad; i += 4) {
+            const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(s + c + i);
+            acc[(c + i) / 2] = fma2(pack2(d[i], d[i + 1]), mul2(sr, v.x), acc[(c + i) / 2]);
+            acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), mul2(sr, v.y), acc[(c + i) / 2 + 1]);
           }
         }
         __syncwarp();
-#pragma unroll
-        for (int g = 0; g < kGroup; ++g)
-          if (lane == 0 && g < n) mbar_arrive(&scale_empty[bar[g] >> 16]);
+        if (lane == 0) mbar_arrive(&scale_empty[slot.at]);
       }
       T *out = static_cast<T *>(p.out) + (int64_t)(r0 + row) * p.row_step;
       const bool in = r0 + row < p.rows;
@@ -264,13 +239,13 @@ __global__ void __launch_bounds__(kMidThreads, 1)
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       asm volatile("bar.sync 1, 256;" ::: "memory");
       const uint32_t per = 1u << (kLog2Bn - split_log2);  // columns that a CTA owns
-      if (threadIdx.x - 128 < split) {
-        const uint32_t owner = threadIdx.x - 128;
+      if (threadIdx.x - 96 < split) {
+        const uint32_t owner = threadIdx.x - 96;
         bulk_s2s(map_rank(smem_addr(recv + rank * per * 128), owner), smem_addr(share + owner * per * 128), per * 512,
                  map_rank(smem_addr(&recv_full), owner));
       }
       alive(&recv_full, done & 1);
-      if (threadIdx.x == 128) mbar_arrive_expect_tx(&recv_full, S::kShareBytes);
+      if (threadIdx.x == 96) mbar_arrive_expect_tx(&recv_full, S::kShareBytes);
       for (uint32_t c = half * (per / 2); c < (half + 1) * (per / 2); ++c) {
         float sum = recv[c * 128 + row];
         for (uint32_t k = 1; k < split; ++k) sum += recv[(k * per + c) * 128 + row];
