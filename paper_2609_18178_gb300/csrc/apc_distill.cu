@@ -20,6 +20,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "apc_ops.cuh"
 #include "apc_tcgen05.cuh"
@@ -60,24 +61,24 @@ __device__ __forceinline__ float moved(float s, float from, float to, float scal
   return s * exp2_approx((from - reference(to)) * scale);
 }
 
-template <bool TWO>
+template <int K>
 __device__ __forceinline__ void join(Sum &a, const Sum &b, float scale) {
   const float t = fmaxf(a.m, b.m);
   a.s = moved(a.s, a.m, t, scale) + moved(b.s, b.m, t, scale);
-  if (TWO) a.s1 = moved(a.s1, a.m, t, kLog2e) + moved(b.s1, b.m, t, kLog2e);
+  if (K) a.s1 = moved(a.s1, a.m, t, kLog2e) + moved(b.s1, b.m, t, kLog2e);
   a.m = t;
 }
 
 // Over the lanes of a warp (or the first `lanes` of them), the same in each.
-template <bool TWO>
+template <int K>
 __device__ __forceinline__ Sum joined(Sum a, float scale, int lanes = 32) {
   float t = a.m;
   for (int o = lanes / 2; o; o >>= 1) t = fmaxf(t, __shfl_xor_sync(~0u, t, o));
   a.s = moved(a.s, a.m, t, scale);
-  if (TWO) a.s1 = moved(a.s1, a.m, t, kLog2e);
+  if (K) a.s1 = moved(a.s1, a.m, t, kLog2e);
   for (int o = lanes / 2; o; o >>= 1) {
     a.s += __shfl_xor_sync(~0u, a.s, o);
-    if (TWO) a.s1 += __shfl_xor_sync(~0u, a.s1, o);
+    if (K) a.s1 += __shfl_xor_sync(~0u, a.s1, o);
   }
   a.m = t;
   return a;
@@ -190,7 +191,7 @@ __device__ __noinline__ void teacher_entries(const DistillArgs &a, uint32_t row,
   } else {
     if (top == -kInf) top = 0.0f;
     float s = 0.0f;
-    for (uint32_t i = lane; i < a.k; i += 32) s += exp2f((ps[i] - top) * a.scale2);
+    for (uint32_t i = lane; i < a.k; i += 32) s += exp2_approx((ps[i] - top) * a.scale2);
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
     norm = logf(s);
   }
@@ -200,7 +201,7 @@ __device__ __noinline__ void teacher_entries(const DistillArgs &a, uint32_t row,
   for (uint32_t i = lane; i <= a.k; i += 32) {
     const int32_t id = ids[i];
     if (i < a.k) {
-      const float lp = id >= 0 ? __fmaf_rn(ps[i] - top, a.inv_tau, -norm) : -kInf, p = expf(lp);
+      const float lp = id >= 0 ? __fmaf_rn(ps[i] - top, a.inv_tau, -norm) : -kInf, p = exp2_approx(lp * kLog2e);
       ps[i] = p;
       p_sum += p;
       if (p != 0.0f) entropy = __fmaf_rn(p, lp, entropy);
@@ -318,9 +319,13 @@ __device__ __forceinline__ uint4 nothing() {
   return {w, w, w, w};
 }
 
+// K: what the labels need beside the sums at tau.  0: nothing (no labels, or tau =
+// 1); 1: exponentials of their own; 2, 4: tau is that number, and the exponential at
+// 1 the power of the one at tau (17 instructions a pair of elements and both passes, for 23).
+
 // A row's or a part's sums on the way: the largest logit and, in two fp32 lanes, the
 // sums about it.
-template <typename T, bool TWO>
+template <typename T, int K>
 struct Running {
   float m;
   uint64_t s, s1;
@@ -329,7 +334,7 @@ struct Running {
   __device__ __forceinline__ Running(float x, bool has, float scale2) : m(x), s(0), s1(0) {
     if (!has) return;
     s = pack2(exp2_approx((x - reference(x)) * scale2), 0.0f);
-    if (TWO) s1 = pack2(exp2_approx((x - reference(x)) * kLog2e), 0.0f);
+    if (K) s1 = pack2(exp2_approx((x - reference(x)) * kLog2e), 0.0f);
   }
 
   template <int N>
@@ -339,7 +344,7 @@ struct Running {
     if (top > m) {  // the sums move to the new maximum
       const float f = moved(1.0f, m, top, scale2);
       s = mul2(s, pack2(f, f));
-      if (TWO) {
+      if (K) {
         const float f1 = moved(1.0f, m, top, kLog2e);
         s1 = mul2(s1, pack2(f1, f1));
       }
@@ -350,9 +355,11 @@ struct Running {
     for (int i = 0; i < N; ++i) {
 #pragma unroll
       for (int j = 0; j < 8 / (int)sizeof(T); ++j) {
-        const uint64_t y = add2(pair<T>(x[i], j), minus);
-        s = add2(s, exp2_pair(mul2(y, scale)));
-        if (TWO) s1 = add2(s1, exp2_pair(mul2(y, scale1)));
+        const uint64_t y = add2(pair<T>(x[i], j), minus), e = exp2_pair(mul2(y, scale));
+        s = add2(s, e);
+        if (K == 1) s1 = add2(s1, exp2_pair(mul2(y, scale1)));
+        if (K == 2) s1 = fma2(e, e, s1);
+        if (K == 4) s1 = fma2(mul2(e, e), mul2(e, e), s1);
       }
     }
   }
@@ -366,9 +373,9 @@ struct Running {
 __device__ __forceinline__ bool has_logits(const Sum &s) { return s.s != 0.0f; }  // a NaN has
 
 // One warp: the row's loss and statistics, from its sums and entries.
-template <bool TWO>
+template <int K>
 __device__ __forceinline__ void store_loss(const DistillArgs &a, uint32_t row, const Sum &sum, const Entries &en, uint32_t lane) {
-  const float from = reference(sum.m), log_s = log2f(sum.s) * kLn2, log_s1 = TWO ? log2f(sum.s1) * kLn2 : log_s;
+  const float from = reference(sum.m), log_s = log2f(sum.s) * kLn2, log_s1 = K ? log2f(sum.s1) * kLn2 : log_s;
   const bool some = has_logits(sum);
   float cross = 0.0f;
   for (uint32_t i = lane; i < a.k; i += 32)
@@ -385,7 +392,7 @@ __device__ __forceinline__ void store_loss(const DistillArgs &a, uint32_t row, c
 
 // A row's gradient without its entries' part: both temperatures' c 2^((z times +
 // plus) scale), from the row's own maximum and sums or from the given logarithms.
-template <bool LOSS, bool TWO>
+template <bool LOSS, int K>
 struct Whole {
   bool live;  // else zeros
   float g;
@@ -398,22 +405,25 @@ struct Whole {
     live = g != 0.0f;
     if (LOSS) {
       live = live && has_logits(sum);
-      k0 /= sum.s, k1 /= TWO ? sum.s1 : sum.s;
+      k0 /= sum.s, k1 /= K ? sum.s1 : sum.s;
     } else {
       l = a.lse[row];
       if (a.labels) l1 = a.lse[(int64_t)a.rows + row];
       live = live && !(l <= kMasked);
+      if (K > 1 && k1 != 0.0f) k1 *= expf(__fmaf_rn((float)K, l, -l1));  // exp(z - l1) = exp(z/tau - l)^tau exp(tau l - l1)
     }
-    if (!TWO) k0 += k1;  // one temperature for both
+    if (K == 0) k0 += k1;  // one temperature for both
     const float t = LOSS ? 1.0f : a.inv_tau, p = LOSS ? -from : -l, p1 = LOSS ? -from : -l1, f = LOSS ? a.scale2 : kLog2e;
     times = pack2(t, t), plus = pack2(p, p), plus1 = pack2(p1, p1), scale = pack2(f, f), scale1 = pack2(kLog2e, kLog2e);
     c0 = pack2(k0, k0), c1 = pack2(k1, k1);
   }
 
   __device__ __forceinline__ uint64_t operator()(uint64_t y) const {
-    const uint64_t t = LOSS ? add2(y, plus) : fma2(y, times, plus);
-    const uint64_t q = mul2(c0, exp2_pair(mul2(t, scale)));
-    return TWO ? fma2(c1, exp2_pair(mul2(LOSS ? t : add2(y, plus1), scale1)), q) : q;
+    const uint64_t t = LOSS ? add2(y, plus) : fma2(y, times, plus), e = exp2_pair(mul2(t, scale));
+    if (K == 0) return mul2(c0, e);
+    if (K == 1) return fma2(c1, exp2_pair(mul2(LOSS ? t : add2(y, plus1), scale1)), mul2(c0, e));
+    if (K == 2) return mul2(e, fma2(c1, e, c0));
+    return mul2(e, fma2(c1, mul2(e, mul2(e, e)), c0));
   }
 
   __device__ __forceinline__ float one(float y) const { return unpack2((*this)(pack2(y, y))).x; }
@@ -466,7 +476,7 @@ __device__ __forceinline__ void store_vector(T *body, uint32_t k, const uint4 &v
 constexpr int kShortWarps = 8, kShortVectors = 8, kShortCtas = 3;
 constexpr uint32_t kShortBytes = 24576, kShortEntries = 256;
 
-template <typename T, int FORM, bool TWO>
+template <typename T, int FORM, int K>
 __global__ void __launch_bounds__(32 * kShortWarps, kShortCtas)
     short_kernel(const __grid_constant__ DistillArgs a, const uint32_t room, const uint32_t slots_log2, const bool alike) {
   extern __shared__ __align__(16) uint8_t raw[];
@@ -499,18 +509,18 @@ __global__ void __launch_bounds__(32 * kShortWarps, kShortCtas)
     __syncwarp();
     Sum sum = {-kInf, 0.0f, 0.0f};
     if (kLoss) {
-      Running<T, TWO> run(x_odd, lane < odd, a.scale2);
+      Running<T, K> run(x_odd, lane < odd, a.scale2);
       for (uint32_t at = 0;;) {
         run.add(x, a.scale2);
         at += 32 * kShortVectors;
         if (at >= body) break;
         load(at);
       }
-      sum = joined<TWO>(run.sum(), a.scale2);
-      store_loss<TWO>(a, (uint32_t)row, sum, en, lane);
+      sum = joined<K>(run.sum(), a.scale2);
+      store_loss<K>(a, (uint32_t)row, sum, en, lane);
     }
     if (!kGrad) continue;
-    const Whole<kLoss, TWO> whole(a, (uint32_t)row, sum, en);
+    const Whole<kLoss, K> whole(a, (uint32_t)row, sum, en);
     T *d = static_cast<T *>(a.dlogits) + (int64_t)row * a.dpitch;
     if (kLoss && body > 32 * kShortVectors) load(0);
     for (uint32_t at = 0;;) {
@@ -533,9 +543,8 @@ __global__ void __launch_bounds__(32 * kShortWarps, kShortCtas)
 
 // ---------------------------------------------------------------------------
 // Longer rows.
-// FORM: 1 loss, 2 gradient, 3 both.  TWO: the labels need the sums at tau = 1
-// beside those at tau.  alike: the gradient's rows are aligned as the logits' are.
-template <typename T, int FORM, bool TWO>
+// FORM: 1 loss, 2 gradient, 3 both.  alike: the gradient's rows are aligned as the logits' are.
+template <typename T, int FORM, int K>
 __global__ void __launch_bounds__(kThreads, kCtas)
     distill_kernel(const __grid_constant__ DistillArgs a, const __grid_constant__ Layout layout, const uint32_t split,
                    const bool alike) {
@@ -626,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       Sum sum = {-kInf, 0.0f, 0.0f};
       if (kLoss) {
         if (worker) {
-          Running<T, TWO> run(x_odd, has_odd, a.scale2);
+          Running<T, K> run(x_odd, has_odd, a.scale2);
           for (uint32_t c = 0; c < p.chunks; ++c) {
             const uint32_t s = (use + c) % kChunks, n = p.v1 - p.v0 - c * kChunk;
             wait(&sh.full[s], (use + c) / kChunks & 1, sh, a.status);
@@ -647,12 +656,13 @@ __global__ void __launch_bounds__(kThreads, kCtas)
           }
           if (FORM == 1 || !p.keeps) use += p.chunks;
           sum = run.sum();
-          sum = joined<TWO>(sum, a.scale2);
+          sum = joined<K>(sum, a.scale2);
           if (lane == 0) sh.part[turn][warp] = sum;
         }
         asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(kWorkers + 32) : "memory");
+        if (FORM == 1 && worker && !together) continue;  // the rest is the teacher's
         sum = lane < kWarps ? sh.part[turn][lane] : Sum{-kInf, 0.0f, 0.0f};
-        sum = joined<TWO>(sum, a.scale2);
+        sum = joined<K>(sum, a.scale2);
         if (together) {
           if (tid < split) {
             const uint32_t at = map_rank(smem_addr(&sh.peer[turn][rank]), tid), bar = map_rank(smem_addr(&sh.peer_full[turn]), tid);
@@ -662,7 +672,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
           asm volatile("fence.acq_rel.cluster;" ::: "memory");
           if (tid == 0) mbar_arrive_expect_tx(&sh.peer_full[turn], split * 12);  // for the next round
           sum = sh.peer[turn][0];
-          for (uint32_t k = 1; k < split; ++k) join<TWO>(sum, sh.peer[turn][k], a.scale2);
+          for (uint32_t k = 1; k < split; ++k) join<K>(sum, sh.peer[turn][k], a.scale2);
         }
       } else {
         asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(kWorkers + 32) : "memory");
@@ -670,13 +680,13 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       const Entries &en = sh.e[turn];
       if (!worker) {
         // the row's loss, then the next row's entries
-        if (kLoss && rank == 0) store_loss<TWO>(a, (uint32_t)row, sum, en, lane);
+        if (kLoss && rank == 0) store_loss<K>(a, (uint32_t)row, sum, en, lane);
         if (row + (uint64_t)step * teachers < a.rows)
           teacher_entries<T>(a, (uint32_t)(row + (uint64_t)step * teachers), sh.e[(done + teachers) % (teachers + 1)], table, layout.slots_log2, lane);
         continue;
       }
       if (!kGrad) continue;
-      const Whole<kLoss, TWO> whole(a, (uint32_t)row, sum, en);
+      const Whole<kLoss, K> whole(a, (uint32_t)row, sum, en);
       T *d = static_cast<T *>(a.dlogits) + (int64_t)row * a.dpitch;
       for (uint32_t c = 0; c < p.chunks; ++c, ++use) {
         const uint32_t s = use % kChunks, at = p.v0 + c * kChunk;
@@ -723,6 +733,23 @@ bool rows_are_short(const DistillArgs &a, unsigned sms) {
   return a.vocab * (a.dtype == APC_F32 ? 4u : 2u) <= kShortBytes && a.k <= kShortEntries && a.rows >= 4 * sms;
 }
 
+template <int V>
+using Int = std::integral_constant<int, V>;
+
+// f(FORM, K) of a call.
+template <typename F>
+int with_form(const DistillArgs &a, int k, F f) {
+  auto with_power = [&](auto form) {
+    switch (k) {
+      case 0: return f(form, Int<0>{});
+      case 2: return f(form, Int<2>{});
+      case 4: return f(form, Int<4>{});
+    }
+    return f(form, Int<1>{});
+  };
+  return !a.dlogits ? with_power(Int<1>{}) : !a.loss ? with_power(Int<2>{}) : with_power(Int<3>{});
+}
+
 }  // namespace
 
 int distill_per_sm(const DistillArgs &a, unsigned sms) { return rows_are_short(a, sms) ? kShortCtas : kCtas; }
@@ -735,7 +762,7 @@ int launch_distill(const DistillArgs &args, unsigned cap, unsigned sms, void *st
     using T = decltype(t);
     const uint32_t size = sizeof(T), body = a.vocab / (16 / size);
     const bool alike = a.dlogits && ((uintptr_t)a.dlogits - (uintptr_t)a.logits) % 16 == 0 && (a.dpitch - a.pitch) * size % 16 == 0;
-    const bool two = a.labels && a.inv_tau != 1.0f;
+    const int k = !a.labels || a.inv_tau == 1.0f ? 0 : a.inv_tau == 0.5f ? 2 : a.inv_tau == 0.25f ? 4 : 1;
     const uint32_t room = (a.k + 1 + 3) / 4 * 4;
     uint32_t slots_log2 = 6;
     while ((1u << slots_log2) < 2 * (a.k + 1)) ++slots_log2;
@@ -747,12 +774,10 @@ int launch_distill(const DistillArgs &args, unsigned cap, unsigned sms, void *st
         kernel<<<want < cap ? want : cap, 32 * kShortWarps, bytes, (cudaStream_t)stream>>>(a, room, slots_log2, alike);
         return (int)cudaGetLastError();
       };
-      if (!a.dlogits) return two ? go(short_kernel<T, 1, true>) : go(short_kernel<T, 1, false>);
-      if (!a.loss) return two ? go(short_kernel<T, 2, true>) : go(short_kernel<T, 2, false>);
-      return two ? go(short_kernel<T, 3, true>) : go(short_kernel<T, 3, false>);
+      return with_form(a, k, [&](auto form, auto power) { return go(short_kernel<T, form.value, power.value>); });
     }
     Layout l = {};
-    l.teachers = a.k <= 256 ? kTeachers : a.k <= 512 ? (kTeachers + 1) / 2 : 1;
+    l.teachers = a.k <= 512 ? kTeachers : 1;  // as many as leave the ring two chunks
     l.room = room;
     l.slots_log2 = slots_log2;
     constexpr uint32_t kRoom = 227 * 1024 / kCtas - 1024;
@@ -778,9 +803,7 @@ int launch_distill(const DistillArgs &args, unsigned cap, unsigned sms, void *st
       cfg.numAttrs = cluster && split > 1 ? 1 : 0;
       return (int)cudaLaunchKernelEx(&cfg, kernel, a, l, split, alike);
     };
-    if (!a.dlogits) return two ? go(distill_kernel<T, 1, true>, true) : go(distill_kernel<T, 1, false>, true);
-    if (!a.loss) return two ? go(distill_kernel<T, 2, true>, false) : go(distill_kernel<T, 2, false>, false);
-    return two ? go(distill_kernel<T, 3, true>, true) : go(distill_kernel<T, 3, false>, true);
+    return with_form(a, k, [&](auto form, auto power) { return go(distill_kernel<T, form.value, power.value>, form.value != 2); });
   });
 }
 
