@@ -102,12 +102,22 @@ struct Shared {
   int32_t pad_;
 };
 
-// How the rest of shared memory is shared out: the ring, the entries of one row
-// more than there are teachers, each teacher's table of ids.
+// A place in a ring of n and the parity of its use; no divisions: they and the other
+// index arithmetic between two rows took a quarter of a row's time.
+struct RingTurn {
+  uint32_t at = 0, phase = 0;
+  __device__ __forceinline__ void next(uint32_t n) {
+    if (++at == n) at = 0, phase ^= 1;
+  }
+};
+
+// How the rest of shared memory is shared out: the ring, each teacher's table of
+// ids, the entries of one row more than there are teachers and, for the loss alone,
+// as many rows' sums of every worker.
 struct Layout {
-  uint32_t chunks, teachers, room, slots_log2;  // room: entries of a row, the label's among them
+  uint32_t chunks, teachers, room, slots_log2, sums;  // room: entries of a row, the label's among them; sums: words of them
   __host__ __device__ uint32_t bytes() const {
-    return (uint32_t)sizeof(Shared) + 16 + chunks * kChunk * 16 + (teachers + 1) * room * 12 + (teachers * 4 << slots_log2);
+    return (uint32_t)sizeof(Shared) + 16 + chunks * kChunk * 16 + (teachers + 1) * (room * 12 + sums * 4) + (teachers * 4 << slots_log2);
   }
 };
 
@@ -546,17 +556,18 @@ __global__ void __launch_bounds__(32 * kShortWarps, kShortCtas)
 // FORM: 1 loss, 2 gradient, 3 both.  alike: the gradient's rows are aligned as the logits' are.
 template <typename T, int FORM, int K>
 __global__ void __launch_bounds__(kThreads, kCtas)
-    distill_kernel(const __grid_constant__ DistillArgs a, const __grid_constant__ Layout layout, const uint32_t split,
+    distill_kernel(const __grid_constant__ DistillArgs a, const __grid_constant__ Layout layout, const uint32_t split_log2,
                    const bool alike) {
   extern __shared__ __align__(16) uint8_t raw[];
   Shared &sh = *reinterpret_cast<Shared *>(raw);
   uint4 *ring = reinterpret_cast<uint4 *>(raw + (sizeof(Shared) + 15) / 16 * 16);
   int32_t *tables = reinterpret_cast<int32_t *>(ring + layout.chunks * kChunk);
+  float *sums = reinterpret_cast<float *>(tables + (layout.teachers << layout.slots_log2)) + (layout.teachers + 1) * layout.room * 3;
   const uint32_t kChunks = layout.chunks;
   constexpr int kPer = 16 / sizeof(T);
   constexpr bool kLoss = FORM & 1, kGrad = FORM & 2;
-  const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  const uint32_t rank = split > 1 ? blockIdx.x % split : 0, first = blockIdx.x / split, step = gridDim.x / split;
+  const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32, split = 1u << split_log2;
+  const uint32_t rank = blockIdx.x & (split - 1), first = blockIdx.x >> split_log2, step = gridDim.x >> split_log2;
   const bool together = kLoss && split > 1;  // the CTAs of a row are a cluster
   if (tid == 0) {
     for (uint32_t i = 0; i < kChunks; ++i) mbar_init(&sh.full[i], 1), mbar_init(&sh.empty[i], kWarps);
@@ -587,7 +598,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     p.z = static_cast<const T *>(a.logits) + (int64_t)row * a.pitch;
     p.head = min(a.vocab, (uint32_t)((16 - (uintptr_t)p.z % 16) % 16 / sizeof(T)));
     p.body = (a.vocab - p.head) / kPer;
-    p.v0 = (uint32_t)((uint64_t)p.body * rank / split), p.v1 = (uint32_t)((uint64_t)p.body * (rank + 1) / split);
+    p.v0 = (uint32_t)((uint64_t)p.body * rank >> split_log2), p.v1 = (uint32_t)((uint64_t)p.body * (rank + 1) >> split_log2);
     p.chunks = (p.v1 - p.v0 + kChunk - 1) / kChunk;
     p.keeps = p.chunks <= kChunks;
     return p;
@@ -597,21 +608,22 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     // copies
     if (lane == 0) {
       const uint64_t policy = l2_evict_first();
-      uint32_t use = 0;
+      RingTurn to;
+      uint32_t issued = 0;
       for (uint32_t row = first; row < a.rows; row += step) {
         const Part p = part_of(row);
         for (int sweep = 0; sweep < (FORM == 3 && !p.keeps ? 2 : 1); ++sweep)
-          for (uint32_t c = 0; c < p.chunks; ++c, ++use) {
-            const uint32_t s = use % kChunks, from = p.v0 + c * kChunk, bytes = min((uint32_t)kChunk, p.v1 - from) * 16;
-            if (use >= kChunks) wait(&sh.empty[s], (use / kChunks + 1) & 1, sh, a.status);
+          for (uint32_t c = 0; c < p.chunks; ++c, ++issued, to.next(kChunks)) {
+            const uint32_t from = p.v0 + c * kChunk, bytes = min((uint32_t)kChunk, p.v1 - from) * 16;
+            wait(&sh.empty[to.at], to.phase ^ 1, sh, a.status);
             if (*(volatile int32_t *)&sh.dead) goto drain;
-            mbar_arrive_expect_tx(&sh.full[s], bytes);
-            bulk_g2s(ring + s * kChunk, reinterpret_cast<const uint4 *>(p.z + p.head) + from, bytes, &sh.full[s], policy);
+            mbar_arrive_expect_tx(&sh.full[to.at], bytes);
+            bulk_g2s(ring + to.at * kChunk, reinterpret_cast<const uint4 *>(p.z + p.head) + from, bytes, &sh.full[to.at], policy);
           }
       }
     drain:
       if (*(volatile int32_t *)&sh.dead)
-        for (uint32_t u = use > kChunks ? use - kChunks : 0; u < use; ++u) wait_for(&sh.full[u % kChunks], u / kChunks & 1);
+        for (uint32_t u = issued > kChunks ? issued - kChunks : 0; u < issued; ++u) wait_for(&sh.full[u % kChunks], u / kChunks & 1);
     }
   } else if (warp < kWarps + layout.teachers) {
     // Row i is teacher i's (modulo their number).  It meets the workers at a barrier
@@ -622,11 +634,18 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     const bool worker = warp < kWarps;
     const uint32_t teachers = layout.teachers, own = worker ? 0 : warp - kWarps;
     int32_t *table = tables + (own << layout.slots_log2);
-    uint32_t use = 0, done = own;
+    RingTurn ring_at;
+    uint32_t done = own, turn = 0, round = 0, barrier = 2;
     if (!worker && first + (uint64_t)own * step < a.rows)
       teacher_entries<T>(a, first + own * step, sh.e[own], table, layout.slots_log2, lane);
     for (uint64_t row = first + (uint64_t)own * step; row < a.rows; row += worker ? step : (uint64_t)step * teachers, done += worker ? 1 : teachers) {
-      const uint32_t turn = done % (teachers + 1), round = done / (teachers + 1), barrier = 2 + done % teachers;
+      if (!worker) {
+        turn = done % (teachers + 1), round = done / (teachers + 1), barrier = 2 + own;
+      } else if (done) {
+        if (turn++ == teachers) turn = 0, ++round;
+        if (++barrier == 2 + teachers) barrier = 2;
+      }
+      float *own_sums = sums + turn * (3 * kWorkers);  // the loss alone: every worker's
       const Part p = part_of(row);
       const uint32_t odd = a.vocab - p.body * kPer;
       const bool has_odd = worker && rank == 0 && tid < odd;
@@ -636,9 +655,11 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       if (kLoss) {
         if (worker) {
           Running<T, K> run(x_odd, has_odd, a.scale2);
+          RingTurn at = ring_at;
           for (uint32_t c = 0; c < p.chunks; ++c) {
-            const uint32_t s = (use + c) % kChunks, n = p.v1 - p.v0 - c * kChunk;
-            wait(&sh.full[s], (use + c) / kChunks & 1, sh, a.status);
+            const uint32_t s = at.at, n = p.v1 - p.v0 - c * kChunk;
+            wait(&sh.full[s], at.phase, sh, a.status);
+            at.next(kChunks);
             uint4 x[kVectors];
             const uint4 *from = ring + s * kChunk + tid;
             if (n >= kChunk) {
@@ -654,14 +675,31 @@ __global__ void __launch_bounds__(kThreads, kCtas)
               if (lane == 0) mbar_arrive(&sh.empty[s]);
             }
           }
-          if (FORM == 1 || !p.keeps) use += p.chunks;
+          if (FORM == 1 || !p.keeps) ring_at = at;
           sum = run.sum();
-          sum = joined<K>(sum, a.scale2);
-          if (lane == 0) sh.part[turn][warp] = sum;
+          if (FORM == 1 && !together) {  // the teacher joins them
+            own_sums[tid] = sum.m, own_sums[kWorkers + tid] = sum.s;
+            if (K) own_sums[2 * kWorkers + tid] = sum.s1;
+          } else {
+            sum = joined<K>(sum, a.scale2);
+            if (lane == 0) sh.part[turn][warp] = sum;
+          }
         }
         asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(kWorkers + 32) : "memory");
         if (FORM == 1 && worker && !together) continue;  // the rest is the teacher's
-        sum = lane < kWarps ? sh.part[turn][lane] : Sum{-kInf, 0.0f, 0.0f};
+        if (FORM == 1 && !together) {
+          sum = {-kInf, 0.0f, 0.0f};
+#pragma unroll
+          for (int w = 0; w < kWarps; ++w) sum.m = fmaxf(sum.m, own_sums[32 * w + lane]);
+#pragma unroll
+          for (int w = 0; w < kWarps; ++w) {
+            const float m = own_sums[32 * w + lane];
+            sum.s += moved(own_sums[kWorkers + 32 * w + lane], m, sum.m, a.scale2);
+            if (K) sum.s1 += moved(own_sums[2 * kWorkers + 32 * w + lane], m, sum.m, kLog2e);
+          }
+        } else {
+          sum = lane < kWarps ? sh.part[turn][lane] : Sum{-kInf, 0.0f, 0.0f};
+        }
         sum = joined<K>(sum, a.scale2);
         if (together) {
           if (tid < split) {
@@ -688,9 +726,9 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       if (!kGrad) continue;
       const Whole<kLoss, K> whole(a, (uint32_t)row, sum, en);
       T *d = static_cast<T *>(a.dlogits) + (int64_t)row * a.dpitch;
-      for (uint32_t c = 0; c < p.chunks; ++c, ++use) {
-        const uint32_t s = use % kChunks, at = p.v0 + c * kChunk;
-        wait(&sh.full[s], use / kChunks & 1, sh, a.status);
+      for (uint32_t c = 0; c < p.chunks; ++c, ring_at.next(kChunks)) {
+        const uint32_t s = ring_at.at, at = p.v0 + c * kChunk;
+        wait(&sh.full[s], ring_at.phase, sh, a.status);
         const uint4 *x = ring + s * kChunk + tid;
         if (alike && whole.live && p.v1 - at >= kChunk) {
           uint4 *to = reinterpret_cast<uint4 *>(d + p.head) + at + tid;
@@ -780,12 +818,15 @@ int launch_distill(const DistillArgs &args, unsigned cap, unsigned sms, void *st
     l.teachers = a.k <= 512 ? kTeachers : 1;  // as many as leave the ring two chunks
     l.room = room;
     l.slots_log2 = slots_log2;
-    constexpr uint32_t kRoom = 227 * 1024 / kCtas - 1024;
+    l.sums = a.dlogits ? 0 : 3 * kWorkers;
+    constexpr uint32_t kRoom = 228 * 1024 / kCtas - 1024;  // an SM's shared memory; 1 KB of each CTA's is the system's
     l.chunks = std::min((uint32_t)kMaxChunks, (kRoom - l.bytes()) / (kChunk * 16));
     // a row over more CTAs while they would not fill the GPU, but not into parts of
     // less than two chunks
-    uint32_t split = 1;
-    while (split < (uint32_t)kMaxSplit && body / (2 * split) >= 2 * kChunk && (uint64_t)a.rows * split <= sms) split *= 2;
+    uint32_t split_log2 = 0;
+    while ((1u << split_log2) < (uint32_t)kMaxSplit && body >> (split_log2 + 1) >= 2 * kChunk && (uint64_t)a.rows << split_log2 <= sms)
+      ++split_log2;
+    const uint32_t split = 1u << split_log2;
     const uint64_t most = cap >= split ? cap / split : 1;
     const unsigned grid = (unsigned)(a.rows < most ? a.rows : most) * split;
     auto go = [&](auto kernel, bool cluster) {
@@ -801,7 +842,7 @@ int launch_distill(const DistillArgs &args, unsigned cap, unsigned sms, void *st
       cfg.stream = (cudaStream_t)stream;
       cfg.attrs = &attr;
       cfg.numAttrs = cluster && split > 1 ? 1 : 0;
-      return (int)cudaLaunchKernelEx(&cfg, kernel, a, l, split, alike);
+      return (int)cudaLaunchKernelEx(&cfg, kernel, a, l, split_log2, alike);
     };
     return with_form(a, k, [&](auto form, auto power) { return go(distill_kernel<T, form.value, power.value>, form.value != 2); });
   });
