@@ -29,14 +29,22 @@ namespace apc {
 
 namespace {
 
-// Warps on the logits and on the teacher's entries, vectors of 16 bytes that each
-// of the former's threads takes of a chunk, CTAs on an SM.  Measured on loss and
-// gradient of 8192 x 32768 with labels: 254 us; 1 CTA of 16 warps 310, 12 warps
-// 275, 4 warps 282 and, with 3 CTAs, 313; 2 vectors 325, 4 vectors 262; 2 teachers
-// 266.
+// Warps on the logits and on the teacher's entries, CTAs on an SM.  Measured on loss
+// and gradient of 8192 x 32768 with labels, when this shape took 254 us: 1 CTA of 16
+// warps 310, 12 warps 275, 4 warps 282 and, with 3 CTAs, 313.  Since then (199 us): 3
+// teachers 215, 2 252.
 constexpr int kWarps = 8, kWorkers = 32 * kWarps, kTeachers = 4;
 constexpr int kThreads = kWorkers + 32 * kTeachers + 32;
-constexpr int kVectors = 8, kChunk = kWorkers * kVectors, kMaxChunks = 16;
+constexpr int kMaxChunks = 16;
+constexpr int kMinPart = 16 * kWorkers;  // vectors of a row's part: 64 KB
+// Vectors of 16 bytes that each thread on the logits takes of a chunk.  Loss and
+// gradient hold a row between their passes, and smaller chunks let more of the next
+// row in meanwhile: 199 us on the same case (8 vectors 208, 5 219, 2 230).  The others let
+// chunks go at once and want fewer turns: loss of 4096 x 32768 41.9 us (4 vectors
+// 43.9), gradient of 1021 x 100003 83.7 (85.1).
+template <int FORM>
+constexpr int kVectorsOf = FORM == 3 ? 4 : 8;
+
 constexpr int kCtas = 2;
 constexpr int kMaxSplit = 8;
 constexpr float kInf = __builtin_huge_valf();
@@ -115,9 +123,9 @@ struct RingTurn {
 // ids, the entries of one row more than there are teachers and, for the loss alone,
 // as many rows' sums of every worker.
 struct Layout {
-  uint32_t chunks, teachers, room, slots_log2, sums;  // room: entries of a row, the label's among them; sums: words of them
+  uint32_t chunk, chunks, teachers, room, slots_log2, sums;  // room: entries of a row, the label's among them; sums: words of them
   __host__ __device__ uint32_t bytes() const {
-    return (uint32_t)sizeof(Shared) + 16 + chunks * kChunk * 16 + (teachers + 1) * (room * 12 + sums * 4) + (teachers * 4 << slots_log2);
+    return (uint32_t)sizeof(Shared) + 16 + chunks * chunk * 16 + (teachers + 1) * (room * 12 + sums * 4) + (teachers * 4 << slots_log2);
   }
 };
 
@@ -561,10 +569,10 @@ __global__ void __launch_bounds__(kThreads, kCtas)
   extern __shared__ __align__(16) uint8_t raw[];
   Shared &sh = *reinterpret_cast<Shared *>(raw);
   uint4 *ring = reinterpret_cast<uint4 *>(raw + (sizeof(Shared) + 15) / 16 * 16);
-  int32_t *tables = reinterpret_cast<int32_t *>(ring + layout.chunks * kChunk);
+  int32_t *tables = reinterpret_cast<int32_t *>(ring + layout.chunks * layout.chunk);
   float *sums = reinterpret_cast<float *>(tables + (layout.teachers << layout.slots_log2)) + (layout.teachers + 1) * layout.room * 3;
   const uint32_t kChunks = layout.chunks;
-  constexpr int kPer = 16 / sizeof(T);
+  constexpr int kPer = 16 / sizeof(T), kVectors = kVectorsOf<FORM>, kChunk = kWorkers * kVectors;
   constexpr bool kLoss = FORM & 1, kGrad = FORM & 2;
   const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32, split = 1u << split_log2;
   const uint32_t rank = blockIdx.x & (split - 1), first = blockIdx.x >> split_log2, step = gridDim.x >> split_log2;
@@ -818,13 +826,14 @@ int launch_distill(const DistillArgs &args, unsigned cap, unsigned sms, void *st
     l.teachers = a.k <= 512 ? kTeachers : 1;  // as many as leave the ring two chunks
     l.room = room;
     l.slots_log2 = slots_log2;
+    l.chunk = (a.loss && a.dlogits ? kVectorsOf<3> : kVectorsOf<1>) * kWorkers;
     l.sums = a.dlogits ? 0 : 3 * kWorkers;
     constexpr uint32_t kRoom = 228 * 1024 / kCtas - 1024;  // an SM's shared memory; 1 KB of each CTA's is the system's
-    l.chunks = std::min((uint32_t)kMaxChunks, (kRoom - l.bytes()) / (kChunk * 16));
+    l.chunks = std::min((uint32_t)kMaxChunks, (kRoom - l.bytes()) / (l.chunk * 16));
     // a row over more CTAs while they would not fill the GPU, but not into parts of
-    // less than two chunks
+    // less than 64 KB
     uint32_t split_log2 = 0;
-    while ((1u << split_log2) < (uint32_t)kMaxSplit && body >> (split_log2 + 1) >= 2 * kChunk && (uint64_t)a.rows << split_log2 <= sms)
+    while ((1u << split_log2) < (uint32_t)kMaxSplit && body >> (split_log2 + 1) >= kMinPart && (uint64_t)a.rows << split_log2 <= sms)
       ++split_log2;
     const uint32_t split = 1u << split_log2;
     const uint64_t most = cap >= split ? cap / split : 1;
