@@ -168,7 +168,7 @@ __device__ __noinline__ void teacher_entries(const DistillArgs &a, uint32_t row,
   float *ps = e.p, *zs = e.z;
   float top = -kInf;
   // entries a lane has in flight: their ids, then the student's logits there (8
-  // cost the rows' own arithmetic more than they saved: 268 us for 8192 x 32768, 246)
+  // cost the rows' own arithmetic more than they saved: 268 us for 8192 x 32768 when 2 took 246)
   constexpr int kBatch = 2;
   for (uint32_t i0 = lane; i0 < a.k; i0 += 32 * kBatch) {
     int32_t id[kBatch];
@@ -488,9 +488,9 @@ __device__ __forceinline__ void store_vector(T *body, uint32_t k, const uint4 &v
 // gradient.  A row's way takes some 6 us, most of it waiting, so what counts is how
 // many are under way: 24 on an SM, where the kernel below has 2.  Up to
 // kShortVectors of 16 bytes a lane stay in registers; a longer row's second sweep
-// finds it in L2.  Loss and gradient of 8192 rows of bf16: 100 logits 21 us (104
-// below), 1000 with labels 29 (121), 5000 48 (118); 300 rows of 4000 12 (9.4), 4096
-// rows of 32768 (loss) 69 (53): hence the limits on both sides.
+// finds it in L2.  Loss and gradient of 8192 rows of bf16: 100 logits 19 us (79 by the
+// kernel below), 5000 47 (85); 300 rows of 4000 10.5 (8.7), 4096 rows of 32768
+// (loss) 58 (42): hence the limits on both sides.
 constexpr int kShortWarps = 8, kShortVectors = 8, kShortCtas = 3;
 constexpr uint32_t kShortBytes = 24576, kShortEntries = 256;
 
@@ -560,7 +560,11 @@ __global__ void __launch_bounds__(32 * kShortWarps, kShortCtas)
 }
 
 // ---------------------------------------------------------------------------
-// Longer rows.
+// Longer rows.  Bound by issue: 60% of the issue slots with labels (17 instructions
+// a pair of elements); the rest goes at the rows' turns.  Measured: loss
+// and gradient of 8192 x 32768 with labels 199 us (5.4 TB/s), loss of 4096 x 32768 42 us
+// (6.4 TB/s), gradient of 1021 x 100003 84 us (4.9 TB/s), loss and gradient of 1600 x
+// 150000 226 us.
 // FORM: 1 loss, 2 gradient, 3 both.  alike: the gradient's rows are aligned as the logits' are.
 template <typename T, int FORM, int K>
 __global__ void __launch_bounds__(kThreads, kCtas)

