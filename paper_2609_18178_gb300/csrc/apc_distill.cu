@@ -106,6 +106,7 @@ struct Shared {
   Sum part[kTeachers + 1][kWarps];
   Sum peer[kTeachers + 1][kMaxSplit];
   uint64_t full[kMaxChunks], empty[kMaxChunks], peer_full[kTeachers + 1];
+  uint64_t read[kTeachers + 1];  // a row's loss no longer needs its entries
   int32_t dead;
   int32_t pad_;
 };
@@ -583,7 +584,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
   const bool together = kLoss && split > 1;  // the CTAs of a row are a cluster
   if (tid == 0) {
     for (uint32_t i = 0; i < kChunks; ++i) mbar_init(&sh.full[i], 1), mbar_init(&sh.empty[i], kWarps);
-    for (int i = 0; i <= kTeachers; ++i) mbar_init(&sh.peer_full[i], 1);
+    for (int i = 0; i <= kTeachers; ++i) mbar_init(&sh.peer_full[i], 1), mbar_init(&sh.read[i], 1);
     sh.dead = 0;
     uint8_t *entries = reinterpret_cast<uint8_t *>(tables + (layout.teachers << layout.slots_log2));
     for (uint32_t i = 0; i <= layout.teachers; ++i, entries += layout.room * 12) {
@@ -641,8 +642,10 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     // Row i is teacher i's (modulo their number).  It meets the workers at a barrier
     // of its own when its entries are there and their sums are, and then goes on to
     // the entries of row i + teachers.  Entries, sums and the cluster's sums have one
-    // place more than there are teachers: at row i's barrier everyone is through
-    // with row i - 1 but its own teacher, who is with row i - 1 + teachers.
+    // place more than there are teachers: the entries of row i + teachers take row
+    // i - 1's.  At row i's barrier the workers are through with row i - 1, but its own
+    // teacher, who does not come to that barrier, may still be at its loss: `read` says when
+    // it is done.  Sums are written again a row later, behind a barrier of that teacher's.
     const bool worker = warp < kWarps;
     const uint32_t teachers = layout.teachers, own = worker ? 0 : warp - kWarps;
     int32_t *table = tables + (own << layout.slots_log2);
@@ -730,9 +733,16 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       const Entries &en = sh.e[turn];
       if (!worker) {
         // the row's loss, then the next row's entries
-        if (kLoss && rank == 0) store_loss<K>(a, (uint32_t)row, sum, en, lane);
-        if (row + (uint64_t)step * teachers < a.rows)
-          teacher_entries<T>(a, (uint32_t)(row + (uint64_t)step * teachers), sh.e[(done + teachers) % (teachers + 1)], table, layout.slots_log2, lane);
+        if (kLoss) {
+          if (rank == 0) store_loss<K>(a, (uint32_t)row, sum, en, lane);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.read[turn]);
+        }
+        if (row + (uint64_t)step * teachers < a.rows) {
+          const uint32_t next = (done + teachers) % (teachers + 1), use = (done + teachers) / (teachers + 1);
+          if (kLoss) wait(&sh.read[next], use & 1 ^ 1, sh, a.status);  // the first use passes
+          teacher_entries<T>(a, (uint32_t)(row + (uint64_t)step * teachers), sh.e[next], table, layout.slots_log2, lane);
+        }
         continue;
       }
       if (!kGrad) continue;

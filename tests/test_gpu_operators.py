@@ -692,3 +692,18 @@ def test_head_gradients_against_64_bits():
     size = d.double().abs().t() @ x.double().abs()
     floor = (d8t.shape[1] * 2.0 ** -10) * dst.max().double() * x.double().abs().max()  # values below the least normal one
     assert ((dw - full).abs() <= size * (2 * 2.0 ** -4 + 2.0 ** -8) + floor * 2).all()
+
+
+@pytest.mark.parametrize("vocab,k", [(900, 300), (2500, 512), (5000, 40), (5000, 1000), (70001, 33)])
+@pytest.mark.parametrize("limit", ["1", "3"])
+def test_distill_many_rows_a_block(vocab, k, limit, monkeypatch):
+    """Rows one after the other in few blocks, in every form: what a row leaves in
+    shared memory is taken again only when its loss and gradient are through."""
+    rows = 61
+    z = torch.randn(rows, vocab, generator=gen(1), device="cuda").mul_(3).bfloat16()
+    ids, u = teacher_of(rows, vocab, k, 2)
+    labels = torch.randint(0, vocab, (rows,), generator=gen(4), device="cuda")
+    monkeypatch.setenv("APC_GRID_LIMIT", limit)
+    check_distill(z, ids, u, weights(rows))
+    check_distill(z, ids, u, weights(rows), 2.0, 0.7, 0.3, None, labels)
+    assert apc.device_status() == 0
