@@ -300,7 +300,8 @@ typedef enum apc_index { APC_I32 = 0, APC_I64 = 1 } apc_index;
  * same id add up.  A row without entries has no teacher's part.  A row with no
  * logit above -1e30 is masked whole (with -infinity, or fp32's or bf16's lowest
  * value): loss 0, lse -infinity, gradient 0.  Masked logits have q = 0; an entry or
- * label on a -infinity makes the loss +infinity.
+ * label on a -infinity makes the loss +infinity.  A part whose weight is 0 is left
+ * out of loss and gradient, whatever its inputs hold.
  *   logits        rows x vocab, apc_dtype, pitch in elements
  *   ids, teacher  rows x k (k <= APC_DISTILL_MAX_K; 0: no teacher), apc_index and apc_dtype
  *   teacher_lse   fp32, one per row: log sum exp(u/tau) over the whole vocabulary, or NULL

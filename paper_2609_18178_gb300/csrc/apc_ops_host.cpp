@@ -203,22 +203,25 @@ apc_status distill(const apc_distill *d, const float *grad_loss, float *loss, fl
   if (rows == 0) return APC_OK;
   if ((st = apc::op_ranges(rs.r, rs.n)) != APC_OK) return st;
   apc::DistillArgs a = {};
+  // without a weight there is no teacher's part: its probabilities times 0 would be NaN where
+  // a logarithm is infinite
+  const int64_t k = (float)d->kd_weight != 0.0f ? d->k : 0;
   a.logits = d->logits;
   a.ids = d->ids;
   a.teacher = d->teacher;
   a.labels = d->labels;
-  a.teacher_lse = d->k ? d->teacher_lse : nullptr;
+  a.teacher_lse = k ? d->teacher_lse : nullptr;
   a.grad_loss = grad_loss;
   a.loss = loss;
   a.lse = lse;
   a.dlogits = dlogits;
   a.pitch = pitch_of(rows, v, d->pitch);
-  a.ids_pitch = pitch_of(rows, d->k, d->ids_pitch);
-  a.teacher_pitch = pitch_of(rows, d->k, d->teacher_pitch);
+  a.ids_pitch = pitch_of(rows, k, d->ids_pitch);
+  a.teacher_pitch = pitch_of(rows, k, d->teacher_pitch);
   a.dpitch = pitch_of(rows, v, dpitch);
   a.rows = (uint32_t)rows;
   a.vocab = (uint32_t)v;
-  a.k = (uint32_t)d->k;
+  a.k = (uint32_t)k;
   a.dtype = d->dtype;
   a.teacher_dtype = d->teacher_dtype;
   a.ids64 = d->ids_dtype == APC_I64;

@@ -707,3 +707,26 @@ def test_distill_many_rows_a_block(vocab, k, limit, monkeypatch):
     check_distill(z, ids, u, weights(rows))
     check_distill(z, ids, u, weights(rows), 2.0, 0.7, 0.3, None, labels)
     assert apc.device_status() == 0
+
+
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("tau,wl", [(1.0, 0.5), (2.0, 0.5), (1.5, 0.0)])
+def test_distill_without_the_teachers_weight(many, tau, wl):
+    """A weight of 0 leaves the teacher out: entries on masked logits and a teacher
+    that is not finite change nothing.  Few rows and as many as one warp each takes."""
+    rows = 4 * torch.cuda.get_device_properties(0).multi_processor_count + 3 if many else 7
+    vocab, k = 600, 20
+    z = torch.randn(rows, vocab, generator=gen(1), device="cuda").mul_(3)
+    z[:, 300:] = -math.inf
+    ids, u = teacher_of(rows, vocab, k, 2, ragged=False)
+    assert (ids >= 300).any(1).float().mean() > 0.9
+    u[1, 2], u[2, 3] = math.nan, math.inf
+    labels = torch.randint(0, 300, (rows,), generator=gen(4), device="cuda")
+    kw = dict(temperature=tau, kd_weight=0.0, labels=labels, label_weight=wl)
+    none = check_distill(z, ids[:, :0], u[:, :0], weights(rows), tau, 0.0, wl, None, labels)
+    loss, stats = apc.distill_loss(z, ids, u, **kw)
+    both = apc.distill_loss_grad(z, ids, u, weights(rows), **kw)
+    assert torch.isfinite(loss).all()
+    assert torch.equal(loss, none[0]) and torch.equal(stats, none[1])
+    assert torch.equal(both[0], loss) and torch.equal(both[1], stats)
+    assert torch.equal(apc.distill_grad(z, ids, u, stats, weights(rows), **kw), none[2])
