@@ -95,6 +95,8 @@ def _sized(x, name: str, kinds, device: int, rows: int, cols: int):
 
 
 def _vector(x, name: str, kinds, device: int, n: int) -> int:
+    if x is None:
+        raise ValueError("%s is None" % name)
     if x.get_device() != device:
         _elsewhere(x, name, device)
     if x.dtype not in kinds:
@@ -248,8 +250,8 @@ def distill_grad(logits, ids, teacher, lse, grad_loss, *, temperature=1.0, kd_we
     lib = _library()
     device = _current_device()
     d = _distill(logits, ids, teacher, temperature, kd_weight, teacher_lse, labels, label_weight, device)
+    at = _vector(lse, "lse", _F32, device, (1 if labels is None else 2) * d.rows)
     out, pitch = _dlogits_room(out, logits, device, d)
-    lse, at = _lse_room(lse, logits, labels, device, d.rows)
     _check(lib.apc_distill_grad(ctypes.byref(d), at, _vector(grad_loss, "grad_loss", _F32, device, d.rows), out.data_ptr(),
                                 pitch, _stream(stream, device)))
     return out

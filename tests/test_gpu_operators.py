@@ -730,3 +730,16 @@ def test_distill_without_the_teachers_weight(many, tau, wl):
     assert torch.equal(loss, none[0]) and torch.equal(stats, none[1])
     assert torch.equal(both[0], loss) and torch.equal(both[1], stats)
     assert torch.equal(apc.distill_grad(z, ids, u, stats, weights(rows), **kw), none[2])
+
+
+def test_distill_grad_needs_statistics_and_weights():
+    """What a call reads has to be given: it is not allocated in the caller's place."""
+    z = torch.randn(4, 50, device="cuda")
+    ids, u = teacher_of(4, 50, 5, 2)
+    g = torch.ones(4, device="cuda")
+    _, lse = apc.distill_loss(z, ids, u)
+    for bad in (lambda: apc.distill_grad(z, ids, u, None, g), lambda: apc.distill_grad(z, ids, u, lse, None),
+                lambda: apc.distill_loss_grad(z, ids, u, None),
+                lambda: apc.distill_grad(z, ids, u, lse, g, labels=torch.zeros(4, dtype=torch.int64, device="cuda"))):
+        with pytest.raises(ValueError):
+            bad()
