@@ -23,6 +23,11 @@ Entry points mirror the C names:
   (``quantize_fp8``, ``matmul_fp8``, ``distill_loss``, ``distill_grad``,
   ``distill_loss_grad``, here too).
 
+``stream`` is a ``torch.cuda.Stream`` or a handle, the current stream if not
+given.  Outputs that a call allocates are memory of that stream: code on another
+one waits for it first and, as with any tensor, tells the allocator
+(``Tensor.record_stream``).
+
 A table or buffer list that is used every step can be marshalled once with
 :func:`prepare_table` / :func:`prepare_buffers` and passed in its place.
 """
@@ -177,6 +182,20 @@ def _stream(stream) -> int:
     return stream.cuda_stream
 
 
+def _empty(shape, dtype, device, stream):
+    """An output that a call allocates for itself is memory of the stream that
+    writes it: in memory of another stream, work that this one still holds on
+    a block just freed would run beside the call's."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream(stream)
+        stream = torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 @dataclass
 class TensorEntry:
     """One chunk-table entry: fp32 p, m, v (updated in place), bf16 g (read),
@@ -224,12 +243,12 @@ class BufferEntry:
     n: int | None = None
 
 
-def _out(out, nslots: int, like):
+def _out(out, nslots: int, like, stream):
     if out is not None:
         return out
     import torch
     dev = like.device if hasattr(like, "device") else torch.device("cuda", torch.cuda.current_device())
-    return torch.empty(nslots, dtype=torch.int64, device=dev)
+    return _empty(nslots, torch.int64, dev, stream)
 
 
 COMMIT_ZERO_GRAD = 1
@@ -294,7 +313,7 @@ def commit_step(table: Sequence[TensorEntry] | PreparedTable, step: int, hparams
     Returns the device int64[4] tensor that receives {D_p', D_m', D_v', D_w}
     (bit patterns of the unsigned digests; see :func:`digests_to_host`)."""
     arr, n, first = _commit_array(table, "f32")
-    out = _out(out, 4, first)
+    out = _out(out, 4, first, stream)
     hp = _hp(hparams)
     if zero_grad:
         _check(library().apc_commit_step_ex(ctypes.addressof(arr), n, ctypes.addressof(hp), int(step),
@@ -311,7 +330,7 @@ def commit_step_bf16(table: Sequence[TensorEntryBF16] | PreparedTable, step: int
     """Enqueue the bf16-state committed step (``apc_commit_step_bf16``).
     Returns the device int64[3] tensor of {D_p', D_m', D_v'}."""
     arr, n, first = _commit_array(table, "bf16")
-    out = _out(out, 3, first)
+    out = _out(out, 3, first, stream)
     hp = _hp(hparams)
     _check(library().apc_commit_step_bf16(ctypes.addressof(arr), n, ctypes.addressof(hp), int(step),
                                           COMMIT_ZERO_GRAD if zero_grad else 0, _stream(stream),
@@ -354,7 +373,7 @@ def digest(buffers: Iterable[BufferEntry] | PreparedTable, num_slots: int = 4, s
     slots (``apc_digest``).  Returns the device int64[num_slots] output
     tensor."""
     arr, n, first = _buffers(buffers)
-    out = _out(out, num_slots, first)
+    out = _out(out, num_slots, first, stream)
     _check(library().apc_digest(ctypes.addressof(arr), n, int(num_slots), _stream(stream),
                                 _ptr(out, 8)))
     return out
@@ -364,7 +383,7 @@ def count_nonzero(buffers: Iterable[BufferEntry] | PreparedTable, num_slots: int
     """Enqueue the quiescence guard (``apc_count_nonzero``): per-slot counts
     of nonzero words.  Returns the device int64[num_slots] output tensor."""
     arr, n, first = _buffers(buffers)
-    out = _out(out, num_slots, first)
+    out = _out(out, num_slots, first, stream)
     _check(library().apc_count_nonzero(ctypes.addressof(arr), n, int(num_slots), _stream(stream),
                                        _ptr(out, 8)))
     return out

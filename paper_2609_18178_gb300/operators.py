@@ -12,6 +12,9 @@ An 8-bit matrix is a pair of tensors: the data, ``[rows, cols]`` of
 ``torch.float8_e4m3fn`` or ``torch.float8_e5m2`` whose rows start at multiples
 of 16 bytes, and the scales, fp32 ``[ceil(cols/128), rows]`` (one for every 128
 values of a row) or ``[ceil(cols/128), ceil(rows/128)]`` (square blocks).
+
+``stream`` is a ``torch.cuda.Stream`` or a handle, the current stream if not
+given; outputs that a call allocates are memory of that stream.
 """
 from __future__ import annotations
 
@@ -126,9 +129,16 @@ def _fp8(data, scale, name: str, device: int, block=None):
     return _Fp8Matrix(data.data_ptr(), scale.data_ptr(), pitch, scale_pitch, kind, block), r, c
 
 
-def _fp8_empty(rows: int, cols: int, block: int, dtype, like):
-    return (torch.empty(rows, (cols + 15) // 16 * 16, dtype=dtype, device=like.device)[:, :cols],
-            torch.empty(_blocks(cols), -(-rows // block), dtype=torch.float32, device=like.device))
+def _empty(shape, dtype, like, stream):
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    from . import _empty as empty
+    return empty(shape, dtype, like.device, stream)
+
+
+def _fp8_empty(rows: int, cols: int, block: int, dtype, like, stream):
+    return (_empty((rows, (cols + 15) // 16 * 16), dtype, like, stream)[:, :cols],
+            _empty((_blocks(cols), -(-rows // block)), torch.float32, like, stream))
 
 
 def _check(status: int) -> None:
@@ -153,9 +163,9 @@ def quantize_fp8(x, block_rows: int = 1, dtype=torch.float8_e4m3fn, transposed: 
     if block_rows not in (1, BLOCK):
         raise ValueError("block_rows %r is neither 1 nor %d" % (block_rows, BLOCK))
     if out is None:
-        out = _fp8_empty(r, c, block_rows, dtype, x)
+        out = _fp8_empty(r, c, block_rows, dtype, x, stream)
         if transposed:
-            out += _fp8_empty(c, r, block_rows, dtype, x)
+            out += _fp8_empty(c, r, block_rows, dtype, x, stream)
     elif len(out) != (4 if transposed else 2):
         raise ValueError("out has %d tensors, expected %d" % (len(out), 4 if transposed else 2))
     q, qr, qc = _fp8(out[0], out[1], "q", device, block_rows)
@@ -182,7 +192,7 @@ def matmul_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, strea
     if kb != k:
         raise ValueError("a has %d columns and b has %d" % (k, kb))
     if out is None:
-        out = torch.empty(m, n, dtype=out_dtype, device=a.device)
+        out = _empty((m, n), out_dtype, a, stream)
     kind, pitch = _sized(out, "out", _DTYPE, device, m, n)
     _check(lib.apc_matmul_fp8(ctypes.byref(p), ctypes.byref(q), m, n, k, out.data_ptr(), pitch, kind, _stream(stream, device)))
     return out
@@ -202,16 +212,16 @@ def _distill(logits, ids, teacher, temperature, kd_weight, teacher_lse, labels, 
         0 if labels is None else _INDEX[labels.dtype], temperature, kd_weight, label_weight)
 
 
-def _lse_room(lse, logits, labels, device, rows):
+def _lse_room(lse, logits, labels, device, rows, stream):
     n = 1 if labels is None else 2
     if lse is None:
-        lse = torch.empty(n, rows, dtype=torch.float32, device=logits.device)
+        lse = _empty((n, rows), torch.float32, logits, stream)
     return lse, _vector(lse, "lse", _F32, device, n * rows)
 
 
-def _dlogits_room(out, logits, device, d):
+def _dlogits_room(out, logits, device, d, stream):
     if out is None:
-        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+        out = _empty((d.rows, d.vocab), logits.dtype, logits, stream)
     return out, _sized(out, "out", {logits.dtype: 0}, device, d.rows, d.vocab)[1]
 
 
@@ -235,8 +245,8 @@ def distill_loss(logits, ids, teacher, *, temperature=1.0, kd_weight=1.0, teache
     device = _current_device()
     d = _distill(logits, ids, teacher, temperature, kd_weight, teacher_lse, labels, label_weight, device)
     if loss is None:
-        loss = torch.empty(d.rows, dtype=torch.float32, device=logits.device)
-    lse, at = _lse_room(lse, logits, labels, device, d.rows)
+        loss = _empty((d.rows,), torch.float32, logits, stream)
+    lse, at = _lse_room(lse, logits, labels, device, d.rows, stream)
     _check(lib.apc_distill_loss(ctypes.byref(d), _vector(loss, "loss", _F32, device, d.rows), at, _stream(stream, device)))
     return loss, lse
 
@@ -251,7 +261,7 @@ def distill_grad(logits, ids, teacher, lse, grad_loss, *, temperature=1.0, kd_we
     device = _current_device()
     d = _distill(logits, ids, teacher, temperature, kd_weight, teacher_lse, labels, label_weight, device)
     at = _vector(lse, "lse", _F32, device, (1 if labels is None else 2) * d.rows)
-    out, pitch = _dlogits_room(out, logits, device, d)
+    out, pitch = _dlogits_room(out, logits, device, d, stream)
     _check(lib.apc_distill_grad(ctypes.byref(d), at, _vector(grad_loss, "grad_loss", _F32, device, d.rows), out.data_ptr(),
                                 pitch, _stream(stream, device)))
     return out
@@ -266,9 +276,9 @@ def distill_loss_grad(logits, ids, teacher, grad_loss, *, temperature=1.0, kd_we
     device = _current_device()
     d = _distill(logits, ids, teacher, temperature, kd_weight, teacher_lse, labels, label_weight, device)
     if loss is None:
-        loss = torch.empty(d.rows, dtype=torch.float32, device=logits.device)
-    lse, at = _lse_room(lse, logits, labels, device, d.rows)
-    out, pitch = _dlogits_room(out, logits, device, d)
+        loss = _empty((d.rows,), torch.float32, logits, stream)
+    lse, at = _lse_room(lse, logits, labels, device, d.rows, stream)
+    out, pitch = _dlogits_room(out, logits, device, d, stream)
     _check(lib.apc_distill_loss_grad(ctypes.byref(d), _vector(grad_loss, "grad_loss", _F32, device, d.rows),
                                      _vector(loss, "loss", _F32, device, d.rows), at, out.data_ptr(), pitch,
                                      _stream(stream, device)))

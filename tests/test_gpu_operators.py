@@ -743,3 +743,23 @@ def test_distill_grad_needs_statistics_and_weights():
                 lambda: apc.distill_grad(z, ids, u, lse, g, labels=torch.zeros(4, dtype=torch.int64, device="cuda"))):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_outputs_of_a_given_stream_while_the_current_one_is_busy():
+    """Memory that the current stream has just freed, with work on it still to
+    run, is not where a call on another stream writes."""
+    x = torch.randn(1024, 1024, generator=gen(1), device="cuda")
+    want = apc.quantize_fp8(x)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (s, s.cuda_stream):
+        torch.cuda._sleep(20_000_000)
+        for _ in range(8):
+            old = [torch.empty_like(want[0]), torch.empty_like(want[1])]
+            for t in old:
+                t.view(torch.uint8).fill_(0x11)
+            del old, t
+        got = apc.quantize_fp8(x, stream=stream)
+        s.synchronize()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0].view(torch.uint8), want[0].view(torch.uint8)) and torch.equal(got[1], want[1])

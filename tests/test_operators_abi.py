@@ -133,3 +133,55 @@ def test_empty_calls_need_no_device():
 def test_struct_layout():
     assert ctypes.sizeof(_Fp8Matrix) == 40
     assert ctypes.sizeof(_Distill) == 5 * 8 + 6 * 8 + 4 * 4 + 3 * 8
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_allocated_outputs_are_memory_of_the_stream_given(handle, monkeypatch):
+    """Every output that a call allocates, on the CPU: the allocator is asked
+    while the stream given is the current one."""
+    import contextlib
+
+    import torch
+
+    from paper_2609_18178_gb300 import operators
+
+    class Stream:
+        cuda_stream = 0x1230
+
+        def __init__(self, handle=0x1230, device=None):
+            assert handle == 0x1230
+
+    current, asked = [], []
+
+    @contextlib.contextmanager
+    def use(stream):
+        current.append(stream.cuda_stream)
+        yield
+        current.pop()
+
+    empty, lib = torch.empty, type("Library", (), {"__getattr__": lambda self, name: lambda *a: 0})()
+
+    def recorded(*a, **kw):
+        asked.append(list(current))
+        return empty(*a, **kw)
+
+    # what the checks take for the current device is the CPU's
+    monkeypatch.setattr(operators, "_current_device", lambda: -1)
+    monkeypatch.setattr(operators, "_lib", lib)
+    monkeypatch.setattr(apc, "_lib", lib)
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
+    monkeypatch.setattr(torch.cuda, "stream", use)
+    x, f8 = torch.zeros(4, 32), torch.zeros(4, 32).to(torch.float8_e4m3fn)
+    scale, ids, g = torch.ones(1, 4), torch.zeros(4, 2, dtype=torch.int64), torch.ones(4)
+    monkeypatch.setattr(torch, "empty", recorded)
+    s = 0x1230 if handle else Stream()
+    for call, outputs in ((lambda: apc.quantize_fp8(x, transposed=True, stream=s), 4),
+                          (lambda: apc.matmul_fp8(f8, scale, f8, scale, stream=s), 1),
+                          (lambda: apc.distill_loss(x, ids, x[:, :2], stream=s), 2),
+                          (lambda: apc.distill_grad(x, ids, x[:, :2], g[None], g, stream=s), 1),
+                          (lambda: apc.distill_loss_grad(x, ids, x[:, :2], g, stream=s), 3),
+                          (lambda: apc._out(None, 4, x, s), 1)):  # digests and counts
+        del asked[:]
+        call()
+        assert asked == [[0x1230]] * outputs
