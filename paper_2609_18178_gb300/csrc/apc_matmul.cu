@@ -285,8 +285,11 @@ __global__ void __launch_bounds__(kMidThreads, 1)
 //    registers.  Bound by an accumulator's way: products (512 cycles), commit, drain and
 //    the pair's arrival take 2,000, of which two overlap; with a scale for every column
 //    by the fp32 pipe too.
-// While a tile's products run, the adding warps look at the next tile's scales and
-// tell both CTAs; after its first general tile a pair stays general.
+// While a tile's products run, its next one's scales are looked at and both CTAs told:
+// in a tile by exponents by the adding warps, which wait then, in a general one by the
+// exponents' warp, which has nothing else to do there.
+// A tile's way is its own scales' alone, whatever its pair did before, so results do
+// not depend on which tiles a pair gets.
 // Measured: 4096 x 32768 x 4096 by exponents 331 us (3.3 PFLOP/s; the tensor cores busy for
 // 75% of the cycles, at 8192 columns), in general 480; 14336 x 4096 x 8192 with a
 // scale for every column 302 us (3.2 PFLOP/s), 693.  Back to back for seconds the
@@ -302,6 +305,9 @@ constexpr int kBigTurnBytes = 32 * 68;  // a warp's, for its way to out
 constexpr int kExpSlots = 2, kExpBytes = 3 * 512;  // exponents of four blocks: 128 rows, 256 columns
 constexpr int kBigBytes = 1024 + kBigStages * kBigStageBytes + kBigScaleBytes + kBigWarps * kBigTurnBytes + kExpSlots * kExpBytes;
 constexpr uint32_t kBigGroup = 16;  // row tiles that are walked together
+// Tiles whose way is told and not yet read by all: of one block each, the exponents' warp can
+// be as many ahead as there are slots of scales, and the pair's other one a tile beside that.
+constexpr uint32_t kModes = 16;
 
 // Tile t of the walk: groups of row tiles, in each the row tile first, so that
 // the tiles in flight share few rows of both operands in L2.
@@ -381,8 +387,8 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kBigStages], empty[kBigStages], acc_full[2], acc_empty[2];
   __shared__ uint64_t scale_full[kScaleSlots], scale_empty[kScaleSlots];
-  __shared__ uint64_t exp_full[kExpSlots], exp_empty[kExpSlots], mode_full[4];
-  __shared__ volatile uint32_t general_from;  // the first of the pair's tiles whose scales are not all powers of two
+  __shared__ uint64_t exp_full[kExpSlots], exp_empty[kExpSlots], mode_full[kModes];
+  __shared__ volatile uint32_t general[kModes];  // n where the pair's nth tile's scales are not all powers of two, at n mod kModes
   __shared__ uint32_t tmem_at;
   uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   float *scales = reinterpret_cast<float *>(smem + kBigStages * kBigStageBytes);  // [slot][128 rows, 256 columns]
@@ -393,10 +399,10 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < kBigStages; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
     for (int i = 0; i < 2; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 2 * kBigWarps);
-    for (int i = 0; i < kScaleSlots; ++i) mbar_init(&scale_full[i], 32), mbar_init(&scale_empty[i], kBigWarps);
+    for (int i = 0; i < kScaleSlots; ++i) mbar_init(&scale_full[i], 32), mbar_init(&scale_empty[i], kBigWarps + p.by_exponent);
     for (int i = 0; i < kExpSlots; ++i) mbar_init(&exp_full[i], 2), mbar_init(&exp_empty[i], 1);
-    for (int i = 0; i < 4; ++i) mbar_init(&mode_full[i], 2 * kBigWarps);
-    general_from = p.by_exponent ? ~0u : 0;
+    for (uint32_t i = 0; i < kModes; ++i) mbar_init(&mode_full[i], 2 * kBigWarps);
+    for (uint32_t i = 0; i < kModes; ++i) general[i] = ~0u;
     mbar_init_fence();
   }
   if (warp == 1) tmem_alloc<2>(&tmem_at, 512);
@@ -407,16 +413,26 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   const uint32_t tmem = tmem_at;
   uint8_t *exps = reinterpret_cast<uint8_t *>(scales) + kBigScaleBytes + kBigWarps * kBigTurnBytes;
   // Whether the pair's nth tile goes by exponents; `ok` false if the wait gave up.
-  struct Mode {
-    Turn<4> turn;
-    bool exponents;
+  auto by_exponent = [&](uint32_t n, bool &ok) {
+    if (!p.by_exponent) return false;
+    ok = warp_wait(&mode_full[n % kModes], n / kModes & 1);
+    return general[n % kModes] != n;
   };
-  auto by_exponent = [&](Mode &m, uint32_t n, bool &ok) {
-    if (!m.exponents) return false;
-    ok = warp_wait(&mode_full[m.turn.at], m.turn.phase);
-    m.turn.next();
-    return m.exponents = n < general_from;
+  // kBigWarps threads of each CTA tell both CTAs whether the pair's nth tile goes by
+  // exponents.  No release where there is nothing to see: it would wait for the last tile's
+  // stores.
+  auto tell = [&](uint32_t n, bool good) {
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared((const void *)general) + n % kModes * 4, bar = smem_addr(mode_full) + n % kModes * 8;
+    if (!good) {
+      general[n % kModes] = n;
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_rank(at, rank ^ 1)), "r"(n) : "memory");
+      asm volatile("fence.acq_rel.cluster;" ::: "memory");
+    }
+    arrive_remote_relaxed(map_rank(bar, 0));
+    arrive_remote_relaxed(map_rank(bar, 1));
   };
+  // 0 for a float 2^-126 to 2^127.  Without a branch: the loads before stay together.
+  auto no_power_of_two = [](uint32_t bits) { return bits & 0x807fffffu | (uint32_t)(bits - 1u >= 0x7f7fffffu); };
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -470,14 +486,40 @@ __global__ void __launch_bounds__(kBigThreads, 1)
       if (!ok) give_up(p.status);
     }
     if (warp == 3) {
-      // exponents of four blocks at a time, while the tiles go by them
+      // exponents of four blocks at a time, in tiles that go by them; in the others every
+      // block's slot is passed on, and a block of the next tile's scales is looked at
       Turn<kScaleSlots> slot;
       Turn<kExpSlots> exp;
-      Mode mode = {{}, p.by_exponent};
       bool ok = true;
       uint32_t n = 0;
       const uint32_t bars = map_rank(smem_addr(exp_full), 0);
-      for (uint32_t t = first; t < tiles && ok && by_exponent(mode, n, ok); t += step, ++n)
+      for (uint32_t t = first; t < tiles && ok && p.by_exponent; t += step, ++n) {
+        if (!by_exponent(n, ok)) {
+          const bool more = t + step < tiles;
+          uint32_t tr, tc, seen = more ? 0 : p.blocks;  // blocks of the next tile
+          if (more) big_tile(p, t + step, &tr, &tc);
+          const uint32_t r0 = tr * 256 + rank * 128 + lane, c0 = tc * 256 + rank * 128 + lane;
+          for (uint32_t b = 0; b < p.blocks && ok; ++b, slot.next()) {
+            if (seen < p.blocks) {
+              const float *rs = p.r_scale + seen * p.r_scale_pitch, *cs = p.c_scale + seen * p.c_scale_pitch;
+              uint32_t v[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const uint32_t o = i % 4 * 32;
+                v[i] = __float_as_uint(__ldg(i < 4 ? rs + (min(r0 + o, p.rows - 1) >> p.r_shift) : cs + (min(c0 + o, p.cols - 1) >> p.c_shift)));
+              }
+              uint32_t bad = 0;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) bad |= no_power_of_two(v[i]);
+              const bool good = __all_sync(~0u, bad == 0);
+              seen = good ? seen + 1 : ~0u;
+              if (seen >= p.blocks && lane < kBigWarps) tell(n + 1, good);
+            }
+            if (!(ok = warp_wait(&scale_full[slot.at], slot.phase))) break;
+            if (lane == 0) mbar_arrive(&scale_empty[slot.at]);
+          }
+          continue;
+        }
         for (uint32_t b = 0; b < p.blocks && ok; b += 4, exp.next()) {
           if (!(ok = warp_wait(&exp_empty[exp.at], exp.phase ^ 1))) break;
           uint32_t w[12];
@@ -492,7 +534,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
               w[j] |= (__float_as_uint(s) >> 23 & 0xff) << 8 * i;
             }
             __syncwarp();
-            if (lane < kBigWarps) mbar_arrive(&scale_empty[slot.at]);
+            if (lane < kBigWarps + 1) mbar_arrive(&scale_empty[slot.at]);  // for the adding warps too
           }
           uint4 *to = reinterpret_cast<uint4 *>(exps + exp.at * kExpBytes) + lane;
 #pragma unroll
@@ -501,6 +543,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
           __syncwarp();
           if (lane == 0) arrive_remote(bars + exp.at * 8);
         }
+      }
       if (!ok) give_up(p.status);
     }
     if (warp == 1 && rank == 0) {
@@ -510,14 +553,15 @@ __global__ void __launch_bounds__(kBigThreads, 1)
       bool ok = true;
       const uint64_t da = operand_desc(smem_addr(smem)), db = operand_desc(smem_addr(smem) + kBigHalf);
       Turn<kExpSlots> exp;
-      Mode mode = {{}, p.by_exponent};
       uint32_t n = 0;
       for (uint32_t t = first; t < tiles && ok; t += step, ++n) {
-        if (by_exponent(mode, n, ok)) {
+        const bool exponents = by_exponent(n, ok);
+        if (!ok) break;
+        if (exponents) {
           // one accumulator, the exponents in the other's columns
           Turn<2> other = acc;
           other.next();
-          if (!(ok = ok && warp_wait(&acc_empty[acc.at], acc.phase ^ 1) && warp_wait(&acc_empty[other.at], other.phase ^ 1))) break;
+          if (!(ok = warp_wait(&acc_empty[acc.at], acc.phase ^ 1) && warp_wait(&acc_empty[other.at], other.phase ^ 1))) break;
           const uint32_t columns = tmem + (acc.at ^ 1) * 256;
           for (uint32_t b = 0; b < p.blocks && ok; b += 4, exp.next()) {
             if (!(ok = warp_wait(&exp_full[exp.at], exp.phase))) break;
@@ -556,12 +600,8 @@ __global__ void __launch_bounds__(kBigThreads, 1)
     Turn<2> buf;
     Turn<kScaleSlots> slot;
     bool ok = true;
-    Mode mode = {{}, p.by_exponent};
-    const uint32_t peer_general = map_rank((uint32_t)__cvta_generic_to_shared((const void *)&general_from), rank ^ 1);
-    const uint32_t peer_mode = map_rank(smem_addr(mode_full), rank ^ 1), own_mode = map_rank(smem_addr(mode_full), rank);
-    Turn<4> told;
-    // Tells both CTAs whether the pair's nth tile, t, goes by exponents: this CTA
-    // looks at its 128 rows' scales and at those of its half of the columns.
+    // Looks at the scales of the pair's nth tile, t, and tells: this CTA at its 128 rows' and
+    // at those of its half of the columns, a thread at one.
     auto look = [&](uint32_t t, uint32_t n) {
       uint32_t tr, tc;
       big_tile(p, t, &tr, &tc);
@@ -570,26 +610,16 @@ __global__ void __launch_bounds__(kBigThreads, 1)
       const uint32_t at = col ? min(tc * 256 + rank * 128 + k - 128, p.cols - 1) >> p.c_shift : min(tr * 256 + rank * 128 + k, p.rows - 1) >> p.r_shift;
       const float *s = (col ? p.c_scale : p.r_scale) + at;
       const int64_t pitch = col ? p.c_scale_pitch : p.r_scale_pitch;
-      bool good = true;
+      uint32_t bad = 0;
       for (uint32_t b = 0; b < p.blocks; b += 16) {
         uint32_t v[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__ldg(s + min(b + i, p.blocks - 1) * pitch));
 #pragma unroll
-        for (int i = 0; i < 16; ++i) good = good && (v[i] & 0x807fffffu) == 0 && v[i] - 1u < 0x7f7fffffu;
+        for (int i = 0; i < 16; ++i) bad |= no_power_of_two(v[i]);
       }
-      good = __all_sync(~0u, good);
-      if (lane == 0) {
-        if (!good) {
-          general_from = n;
-          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_general), "r"(n) : "memory");
-          asm volatile("fence.acq_rel.cluster;" ::: "memory");
-        }
-        // no release where there is nothing to see: it would wait for the last tile's stores
-        arrive_remote_relaxed(own_mode + told.at * 8);
-        arrive_remote_relaxed(peer_mode + told.at * 8);
-      }
-      told.next();
+      const bool good = __all_sync(~0u, bad == 0);
+      if (lane == 0) tell(n, good);
     };
     uint32_t n = 0;
     if (p.by_exponent && first < tiles) look(first, 0);
@@ -613,7 +643,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
           acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), y, acc[(c + i) / 2 + 1]);
         }
       };
-      const bool exponents = by_exponent(mode, n, ok);
+      const bool exponents = by_exponent(n, ok);
       if (!ok) break;
       if (exponents) {
         if (t + step < tiles) look(t + step, n + 1);
@@ -633,33 +663,34 @@ __global__ void __launch_bounds__(kBigThreads, 1)
         if (lane == 0) arrive_remote_relaxed(empty_bars + buf.at * 8);
         buf.next();
         slot.skip(p.blocks);  // the exponents' warp took them
-      } else
-      for (uint32_t b = 0; b < p.blocks; ++b, buf.next(), slot.next()) {
-        const float *s = scales + slot.at * 384 + 128 + (ROWS ? part * kBigCols : part * kBigCols / 128);
-        if (!(ok = warp_wait(&scale_full[slot.at], slot.phase))) break;
-        const float mine = scales[slot.at * 384 + row], one = ROWS ? mine : mine * s[0];
-        const uint64_t sr = pack2(one, one);
-        if (!(ok = warp_wait(&acc_full[buf.at], buf.phase))) break;
-        tc_fence_after();
-        const uint32_t at = tmem + buf.at * 256 + part * kBigCols + (quad << 21);
-        // each load runs under the additions of the one before
-        uint32_t d[2][kBigLoad];
-        tmem_load(d[0], at);
+      } else {
+        for (uint32_t b = 0; b < p.blocks; ++b, buf.next(), slot.next()) {
+          const float *s = scales + slot.at * 384 + 128 + (ROWS ? part * kBigCols : part * kBigCols / 128);
+          if (!(ok = warp_wait(&scale_full[slot.at], slot.phase))) break;
+          const float mine = scales[slot.at * 384 + row], one = ROWS ? mine : mine * s[0];
+          const uint64_t sr = pack2(one, one);
+          if (!(ok = warp_wait(&acc_full[buf.at], buf.phase))) break;
+          tc_fence_after();
+          const uint32_t at = tmem + buf.at * 256 + part * kBigCols + (quad << 21);
+          // each load runs under the additions of the one before
+          uint32_t d[2][kBigLoad];
+          tmem_load(d[0], at);
 #pragma unroll
-        for (int c = 0; c < kBigCols; c += kBigLoad) {
-          const int i = c / kBigLoad % 2;
-          tmem_landed(d[i]);
-          if (c + kBigLoad < kBigCols) {
-            tmem_load(d[i ^ 1], at + c + kBigLoad);
-          } else {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_remote_relaxed(empty_bars + buf.at * 8);
+          for (int c = 0; c < kBigCols; c += kBigLoad) {
+            const int i = c / kBigLoad % 2;
+            tmem_landed(d[i]);
+            if (c + kBigLoad < kBigCols) {
+              tmem_load(d[i ^ 1], at + c + kBigLoad);
+            } else {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) arrive_remote_relaxed(empty_bars + buf.at * 8);
+            }
+            add(d[i], c, sr, s);
           }
-          add(d[i], c, sr, s);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&scale_empty[slot.at]);
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&scale_empty[slot.at]);
       }
       if (!ok) break;
       if (c0 < p.cols)

@@ -763,3 +763,33 @@ def test_outputs_of_a_given_stream_while_the_current_one_is_busy():
         s.synchronize()
         torch.cuda.synchronize()
         assert torch.equal(got[0].view(torch.uint8), want[0].view(torch.uint8)) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("m,n,k", [(4100, 4357, 2000), (8200, 8300, 500)])
+@pytest.mark.parametrize("bb", [1, 128])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_matmul_grid_with_scales_of_both_kinds(m, n, k, bb, dtype, monkeypatch):
+    """Scales that are powers of two, and others in some rows and columns: a tile's
+    bits follow from its own scales, not from the tiles that its blocks had before."""
+    x = torch.randn(m, k, generator=gen(1), device="cuda")
+    y = torch.randn(n, k, generator=gen(2), device="cuda")
+    a, sa = apc.quantize_fp8(x)
+    b, sb = apc.quantize_fp8(y, block_rows=bb)
+    for at in ((), (0, 1500, 1501, 3900), (m - 1,)):
+        odd, odd_b = sa.clone(), sb.clone()
+        odd[3, list(at)] *= 1.5
+        odd_b[-1, sb.shape[1] // 2] *= 1.25 if len(at) == 4 else 1.0
+        ref, size = ref_matmul(a, odd, 1, b, odd_b, bb)
+        first = apc.matmul_fp8(a, odd, b, odd_b, out_dtype=dtype)
+        check_matmul(first, ref, size, k)
+        for limit in ("7", "40", "3"):
+            monkeypatch.setenv("APC_GRID_LIMIT", limit)
+            assert torch.equal(first, apc.matmul_fp8(a, odd, b, odd_b, out_dtype=dtype))
+        monkeypatch.delenv("APC_GRID_LIMIT")
+        # nor from other rows' scales, a tile's height away
+        if at:
+            apart = torch.ones(m, dtype=torch.bool, device="cuda")
+            for i in at:
+                apart[i // 256 * 256:i // 256 * 256 + 256] = False
+            assert torch.equal(first[apart], apc.matmul_fp8(a, sa, b, odd_b, out_dtype=dtype)[apart])
+    assert apc.device_status() == 0
