@@ -8,8 +8,8 @@
 // Its accumulator is then read back, multiplied by the scales and added into
 // fp32 registers while the tensor core fills other accumulators: the scales are
 // arbitrary fp32 numbers, and no sum of more than 128 products is left to the
-// tensor core's own rounding.  Large products whose scales are powers of two, as
-// quantization makes them, leave scaling and sums to the tensor cores (see there).
+// tensor core's own rounding.  Large products to 16 bits whose scales are powers of two,
+// as quantization makes them, leave scaling and sums to the tensor cores (may_go_by_exponents).
 //
 // Two kernels, warp-specialized alike: one warp issues TMA loads into a ring of
 // shared-memory stages (128 bytes of k a row, 128-byte swizzle, zeros beyond
@@ -745,11 +745,22 @@ int launch_cluster(K kernel, unsigned grid, unsigned threads, unsigned smem, uns
 
 uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
+// Whether a large product's sums over all of k may be the tensor cores' own.  These cut off
+// each of the k/32 additions at up to 2^-23 of the sum so far, which over terms of one
+// sign makes k 2^-29 of the result at most (measured with positive values: 1.5e-6 at 4,096, 3.9e-6
+// at 8,192; with both signs 2.2e-7 and 4.9e-7; sums in registers 1e-7 and less, with no bias).
+// That is to stay below a sixteenth of the rounding to out's type, 2^-8 or 2^-11: up to
+// 131,072 in bf16 and 16,384 in fp16.  fp32 results are not rounded and never take them.
+bool may_go_by_exponents(uint32_t out_dtype, uint32_t blocks) {
+  return out_dtype == APC_BF16 ? blocks <= 1024 : out_dtype == APC_F16 ? blocks <= 128 : false;
+}
+
 // Which kernel, and for few columns how many and how far k is split: the least of
 // the estimated times, in nanoseconds, of measured parts (one GB300, 152 SMs):
 //   a block of 128 k takes a CTA 270, 330, 385 and 535 ns with 16, 32, 64 and 128
-//   columns, a pair 350 ns with a tile of 256 x 256 (by exponents; else 435 and,
-//   with a scale for every column, 900) and 1.8 us between tiles;
+//   columns, a pair with a tile of 256 x 256 350 ns where it may go by exponents (the
+//   scales are not known here), else 540 and, with a scale for every column, 930, and
+//   1.8 us between tiles;
 //   a cluster's exchange 2.2, 3 and 6.5 us for 2, 4 and 8 CTAs; a call 4 us beside
 //   that, 8 with pairs.
 // For example 100 x 4096 x 4096: 64 columns in two halves 13.8 us, whole 16.7, tiles
@@ -760,11 +771,11 @@ struct Choice {
   uint32_t cols, split_log2;  // cols 256: the pairs' kernel
 };
 
-Choice choose(uint32_t m, uint32_t n, uint32_t blocks, uint32_t sms) {
+Choice choose(uint32_t m, uint32_t n, uint32_t blocks, uint32_t pair_ns, uint32_t sms) {
   static constexpr uint32_t kBlockNs[4] = {270, 330, 385, 535}, kExchangeNs[4] = {0, 2200, 3000, 6500};
   const uint64_t pairs = sms / 2 ? sms / 2 : 1;
   Choice best = {256, 0};
-  uint64_t least = 8000 + ceil_div((uint64_t)ceil_div(m, 256) * ceil_div(n, 256), pairs) * ((uint64_t)blocks * 350 + 1800);
+  uint64_t least = 8000 + ceil_div((uint64_t)ceil_div(m, 256) * ceil_div(n, 256), pairs) * ((uint64_t)blocks * pair_ns + 1800);
   for (uint32_t c = 0; c < 4; ++c)
     for (uint32_t s = 0; s <= (c == 3 ? 0u : 3u) && (1u << s) <= blocks && (1u << s) <= sms; ++s) {
       const uint64_t tiles = (uint64_t)ceil_div(n, 128) * ceil_div(m, 16u << c);
@@ -804,10 +815,7 @@ int launch_big(const MatmulArgs &a, ProductPlan p, unsigned cap, void *stream) {
   p.row_tiles = ceil_div(a.m, 256), p.col_tiles = ceil_div(a.n, 256);
   p.formats = a.a_e5m2 << 7 | a.b_e5m2 << 10;
   p.instruction = 1u << 4 | p.formats | (256u >> 3) << 17 | (256u >> 4) << 24;
-  // The tensor cores' own sums over all of k are off by 2.2e-7 of the result at 4,096,
-  // 1.2e-6 at 16,384 (the sums in registers by less than 1e-7): nothing beside a
-  // rounding to 16 bits; fp32 results take them up to 8,192.
-  p.by_exponent = a.out_dtype != APC_F32 || p.blocks <= 64;
+  p.by_exponent = may_go_by_exponents(a.out_dtype, p.blocks);
   p.row_step = a.out_pitch, p.col_step = 1;
   const uint64_t size = a.out_dtype == APC_F32 ? 4 : 2;
   const bool aligned = (uintptr_t)a.out % 16 == 0 && (a.m <= 1 || (uint64_t)a.out_pitch * size % 16 == 0);
@@ -834,7 +842,8 @@ int launch_matmul(const MatmulArgs &a, unsigned cap, unsigned sms, void *stream)
   p.out = a.out;
   int e = commit_status_word(&p.status);
   if (e) return e;
-  const Choice c = choose(a.m, a.n, p.blocks, sms);
+  const uint32_t pair_ns = may_go_by_exponents(a.out_dtype, p.blocks) ? 350 : a.b_shift ? 540 : 930;
+  const Choice c = choose(a.m, a.n, p.blocks, pair_ns, sms);
   return with_dtype(a.out_dtype, [&](auto t) {
     using T = decltype(t);
     switch (c.cols) {

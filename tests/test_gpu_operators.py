@@ -793,3 +793,32 @@ def test_matmul_grid_with_scales_of_both_kinds(m, n, k, bb, dtype, monkeypatch):
                 apart[i // 256 * 256:i // 256 * 256 + 256] = False
             assert torch.equal(first[apart], apc.matmul_fp8(a, sa, b, odd_b, out_dtype=dtype)[apart])
     assert apc.device_status() == 0
+
+
+def one_sign(m, n, k, seed=1):
+    """Quantized operands of positive values, whose sums' roundings do not cancel, and their product."""
+    x = torch.randn(m, k, generator=gen(seed), device="cuda").abs()
+    y = torch.randn(n, k, generator=gen(seed + 1), device="cuda").abs()
+    a, sa = apc.quantize_fp8(x)
+    b, sb = apc.quantize_fp8(y, block_rows=128)
+    return a, sa, b, sb, ref_matmul(a, sa, 1, b, sb, 128)[0]
+
+
+@pytest.mark.parametrize("m,n,k", [(4096, 4096, 2048), (4096, 4096, 8192), (1500, 5000, 7777), (64, 4096, 8192)])
+def test_matmul_to_32_bits_has_no_bias(m, n, k):
+    """The tensor cores sum 128 products in four steps, each off by at most 2^-23 and on
+    average half that: 2^-22 of the mean.  Sums over k are rounded to nearest."""
+    a, sa, b, sb, ref = one_sign(m, n, k)
+    off = apc.matmul_fp8(a, sa, b, sb, out_dtype=torch.float32).double() / ref - 1
+    assert off.mean().abs().item() <= 2.0 ** -22
+    assert off.abs().max().item() <= 2.0 ** -22 * 2 + (k / 128) ** 0.5 * 6 * 2.0 ** -24  # six deviations of the sums' own
+    assert apc.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype,k", [(torch.float16, 16384), (torch.float16, 16500), (torch.bfloat16, 131072), (torch.bfloat16, 131200)])
+def test_matmul_to_16_bits_over_long_sums(dtype, k):
+    """The rounding to 16 bits, and a sixteenth of it for the sum."""
+    a, sa, b, sb, ref = one_sign(2048, 2304, k)
+    out = apc.matmul_fp8(a, sa, b, sb, out_dtype=dtype)
+    assert ((out.double() / ref - 1).abs().max() <= UNIT[dtype] * (1 + 1 / 16)).item()
+    assert apc.device_status() == 0
