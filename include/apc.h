@@ -271,12 +271,12 @@ apc_status apc_quantize_fp8(const void *x, int64_t rows, int64_t cols, int64_t p
 /* out = a b^T: out[i, j] = sum over k of a[i, k] b[j, k], for a (m x k) and b
  * (n x k) in 8 bits and out (m x n, apc_dtype, out_pitch in elements).
  * The products of each 128 values of k are summed by the tensor cores in fp32,
- * the sums are multiplied by both blocks' scales and added in fp32 in a fixed
- * order, and the total is rounded once to out's type.  In large products to 16 bits
- * (k at most 131,072 for bf16, 16,384 for fp16), tiles of 256 x 256 all of whose scales
- * are powers of two are scaled and summed over k by the tensor cores: their fp32 sums
- * cut off rather than round, by k 2^-29 of the sum of magnitudes at most, a
- * sixteenth of the final rounding.  k = 0 writes zeros.
+ * the sums are multiplied by the scale of b's block, then by that of a's, and added
+ * in a fixed order, all in fp32, and the total is rounded once to out's type.  In large
+ * products to 16 bits (k at most 131,072 for bf16, 16,384 for fp16), tiles of 256 x 256 all
+ * of whose scales are powers of two up to 2^63 are scaled and summed over k by the tensor
+ * cores: their fp32 sums cut off rather than round, by k 2^-29 of the sum of magnitudes
+ * at most, a sixteenth of the final rounding.  k = 0 writes zeros.
  * The two formats and the two block sizes may differ.
  * Errors as apc_quantize_fp8; APC_ETIMEOUT is reported by apc_device_status
  * if a bounded wait of the kernel gave up (out is then incomplete and the call

@@ -2,7 +2,7 @@
 // 5th-generation tensor cores.
 //
 //   out[i, j] = sum over blocks c of 128 k:
-//                 sa[c, i] sb[c, j] * (sum over k in c of a[i, k] b[j, k])
+//                 (sum over k in c of a[i, k] b[j, k]) sb[c, j] sa[c, i]
 //
 // The inner sum is four tcgen05.mma (K = 32 each) into tensor memory, in fp32.
 // Its accumulator is then read back, multiplied by the scales and added into
@@ -215,8 +215,8 @@ __global__ void __launch_bounds__(kMidThreads, 1)
 #pragma unroll
           for (int i = 0; i < kLoad; i += 4) {
             const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(s + c + i);
-            acc[(c + i) / 2] = fma2(pack2(d[i], d[i + 1]), mul2(sr, v.x), acc[(c + i) / 2]);
-            acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), mul2(sr, v.y), acc[(c + i) / 2 + 1]);
+            acc[(c + i) / 2] = fma2(mul2(pack2(d[i], d[i + 1]), sr), v.x, acc[(c + i) / 2]);
+            acc[(c + i) / 2 + 1] = fma2(mul2(pack2(d[i + 2], d[i + 3]), sr), v.y, acc[(c + i) / 2 + 1]);
           }
         }
         __syncwarp();
@@ -298,7 +298,6 @@ __global__ void __launch_bounds__(kMidThreads, 1)
 // the launch's 168 each: 128 x 56 + 256 x 224 = 384 x 168).
 constexpr int kBigWarps = 8, kBigThreads = 128 + 32 * kBigWarps, kBigStages = 6;
 constexpr int kBigCols = 1024 / kBigWarps;  // columns that a warp adds
-constexpr int kBigLoad = 16;                // in loads of so many
 constexpr int kBigHalf = 128 * kBlock, kBigStageBytes = 2 * kBigHalf;
 constexpr int kBigScaleBytes = kScaleSlots * (128 + 256) * 4;
 constexpr int kBigTurnBytes = 32 * 68;  // a warp's, for its way to out
@@ -384,6 +383,7 @@ template <typename T, bool ROWS, bool ALIGNED>
 __global__ void __launch_bounds__(kBigThreads, 1)
     big_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ ProductPlan p) {
+  constexpr int kLoad = ROWS ? 32 : 16;  // columns in a load from the accumulator
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kBigStages], empty[kBigStages], acc_full[2], acc_empty[2];
   __shared__ uint64_t scale_full[kScaleSlots], scale_empty[kScaleSlots];
@@ -431,8 +431,10 @@ __global__ void __launch_bounds__(kBigThreads, 1)
     arrive_remote_relaxed(map_rank(bar, 0));
     arrive_remote_relaxed(map_rank(bar, 1));
   };
-  // 0 for a float 2^-126 to 2^127.  Without a branch: the loads before stay together.
-  auto no_power_of_two = [](uint32_t bits) { return bits & 0x807fffffu | (uint32_t)(bits - 1u >= 0x7f7fffffu); };
+  // 0 for a float 2^-126 to 2^63: the tensor cores' product of two larger ones may be an
+  // infinity, and an infinity times 0 is no 0.  (Small ones they multiply exactly, below
+  // 2^-126 too.)  Without a branch: the loads before stay together.
+  auto no_exponent = [](uint32_t bits) { return bits & 0x807fffffu | (uint32_t)(bits - 1u >= (63 + 127 << 23)); };
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -510,7 +512,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
               }
               uint32_t bad = 0;
 #pragma unroll
-              for (int i = 0; i < 8; ++i) bad |= no_power_of_two(v[i]);
+              for (int i = 0; i < 8; ++i) bad |= no_exponent(v[i]);
               const bool good = __all_sync(~0u, bad == 0);
               seen = good ? seen + 1 : ~0u;
               if (seen >= p.blocks && lane < kBigWarps) tell(n + 1, good);
@@ -616,7 +618,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__ldg(s + min(b + i, p.blocks - 1) * pitch));
 #pragma unroll
-        for (int i = 0; i < 16; ++i) bad |= no_power_of_two(v[i]);
+        for (int i = 0; i < 16; ++i) bad |= no_exponent(v[i]);
       }
       const bool good = __all_sync(~0u, bad == 0);
       if (lane == 0) tell(n, good);
@@ -630,17 +632,20 @@ __global__ void __launch_bounds__(kBigThreads, 1)
       uint64_t acc[kBigCols / 2];
 #pragma unroll
       for (int i = 0; i < kBigCols / 2; ++i) acc[i] = 0;
-      // adds some columns of a sum of 128 products, scaled; c: the first, within the warp's
-      auto add = [&](const uint32_t (&d)[kBigLoad], int c, uint64_t sr, const float *s) {
+      // adds some columns of a sum of 128 products, scaled; c: the first, within the warp's.  The
+      // sums are multiplied by b's scale and then by a's: their product may leave fp32's range
+      // where a sum is 0 or the result small.  (With the product first, which without scales of the
+      // columns is one for all of them: 523 us for 4096 x 32768 x 4096 in place of 568.)
+      auto add = [&](const uint32_t (&d)[kLoad], int c, uint64_t sr, uint64_t sc, const float *s) {
 #pragma unroll
-        for (int i = 0; i < kBigLoad; i += 4) {
-          uint64_t x = sr, y = sr;
+        for (int i = 0; i < kLoad; i += 4) {
+          uint64_t x = sc, y = sc;
           if (ROWS) {
             const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(s + c + i);
-            x = mul2(sr, v.x), y = mul2(sr, v.y);
+            x = v.x, y = v.y;
           }
-          acc[(c + i) / 2] = fma2(pack2(d[i], d[i + 1]), x, acc[(c + i) / 2]);
-          acc[(c + i) / 2 + 1] = fma2(pack2(d[i + 2], d[i + 3]), y, acc[(c + i) / 2 + 1]);
+          acc[(c + i) / 2] = fma2(mul2(pack2(d[i], d[i + 1]), x), sr, acc[(c + i) / 2]);
+          acc[(c + i) / 2 + 1] = fma2(mul2(pack2(d[i + 2], d[i + 3]), y), sr, acc[(c + i) / 2 + 1]);
         }
       };
       const bool exponents = by_exponent(n, ok);
@@ -667,26 +672,26 @@ __global__ void __launch_bounds__(kBigThreads, 1)
         for (uint32_t b = 0; b < p.blocks; ++b, buf.next(), slot.next()) {
           const float *s = scales + slot.at * 384 + 128 + (ROWS ? part * kBigCols : part * kBigCols / 128);
           if (!(ok = warp_wait(&scale_full[slot.at], slot.phase))) break;
-          const float mine = scales[slot.at * 384 + row], one = ROWS ? mine : mine * s[0];
-          const uint64_t sr = pack2(one, one);
+          const float mine = scales[slot.at * 384 + row];
+          const uint64_t sr = pack2(mine, mine), sc = ROWS ? 0 : pack2(s[0], s[0]);
           if (!(ok = warp_wait(&acc_full[buf.at], buf.phase))) break;
           tc_fence_after();
           const uint32_t at = tmem + buf.at * 256 + part * kBigCols + (quad << 21);
           // each load runs under the additions of the one before
-          uint32_t d[2][kBigLoad];
+          uint32_t d[2][kLoad];
           tmem_load(d[0], at);
 #pragma unroll
-          for (int c = 0; c < kBigCols; c += kBigLoad) {
-            const int i = c / kBigLoad % 2;
+          for (int c = 0; c < kBigCols; c += kLoad) {
+            const int i = c / kLoad % 2;
             tmem_landed(d[i]);
-            if (c + kBigLoad < kBigCols) {
-              tmem_load(d[i ^ 1], at + c + kBigLoad);
+            if (c + kLoad < kBigCols) {
+              tmem_load(d[i ^ 1], at + c + kLoad);
             } else {
               tc_fence_before();
               __syncwarp();
               if (lane == 0) arrive_remote_relaxed(empty_bars + buf.at * 8);
             }
-            add(d[i], c, sr, s);
+            add(d[i], c, sr, sc, s);
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(&scale_empty[slot.at]);
@@ -759,7 +764,7 @@ bool may_go_by_exponents(uint32_t out_dtype, uint32_t blocks) {
 // the estimated times, in nanoseconds, of measured parts (one GB300, 152 SMs):
 //   a block of 128 k takes a CTA 270, 330, 385 and 535 ns with 16, 32, 64 and 128
 //   columns, a pair with a tile of 256 x 256 350 ns where it may go by exponents (the
-//   scales are not known here), else 540 and, with a scale for every column, 930, and
+//   scales are not known here), else 600 and, with a scale for every column, 900, and
 //   1.8 us between tiles;
 //   a cluster's exchange 2.2, 3 and 6.5 us for 2, 4 and 8 CTAs; a call 4 us beside
 //   that, 8 with pairs.
@@ -842,7 +847,7 @@ int launch_matmul(const MatmulArgs &a, unsigned cap, unsigned sms, void *stream)
   p.out = a.out;
   int e = commit_status_word(&p.status);
   if (e) return e;
-  const uint32_t pair_ns = may_go_by_exponents(a.out_dtype, p.blocks) ? 350 : a.b_shift ? 540 : 930;
+  const uint32_t pair_ns = may_go_by_exponents(a.out_dtype, p.blocks) ? 350 : a.b_shift ? 600 : 900;
   const Choice c = choose(a.m, a.n, p.blocks, pair_ns, sms);
   return with_dtype(a.out_dtype, [&](auto t) {
     using T = decltype(t);

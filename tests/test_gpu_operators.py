@@ -822,3 +822,45 @@ def test_matmul_to_16_bits_over_long_sums(dtype, k):
     out = apc.matmul_fp8(a, sa, b, sb, out_dtype=dtype)
     assert ((out.double() / ref - 1).abs().max() <= UNIT[dtype] * (1 + 1 / 16)).item()
     assert apc.device_status() == 0
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 300, 700), (40, 333, 2000), (130, 257, 300), (777, 1001, 640), (2100, 2050, 1111),
+                                   (4100, 4357, 600)])
+@pytest.mark.parametrize("bb", [1, 128])
+@pytest.mark.parametrize("powers", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_matmul_scales_far_apart(m, n, k, bb, powers, dtype):
+    """Scales whose product leaves fp32's range, or its normal numbers, though the
+    result need not: zeros stay zeros, small sums times large scales are finite, and large
+    sums times small scales keep their digits.  A block's sum is rounded to fp32 times b's
+    scale, at 2^-150 where that is not normal, and then times a's."""
+    a, sa = operand(m, k, 1, E4M3, 1)
+    b, sb = operand(n, k, bb, E4M3, 2)
+    a.view(torch.uint8)[::5] = 0
+    e = torch.randint(-125, 126, (m,), generator=gen(3), device="cuda")
+    f = torch.randint(-125, 126, (sb.shape[1],), generator=gen(4), device="cuda")
+    e[::7] = 120
+    f[::3] = 100                       # with the rows above: zeros, or an overflow
+    e[1::7], f[1::3] = -70, -65        # a product of scales that is not normal
+    near = torch.arange(m, device="cuda") % 7 == 2
+    e[near], f[2::3] = 70, 60          # beyond the range but for small sums
+    small = a[near].float() * 2.0 ** -6
+    a[near] = small.to(E4M3)
+    room = b.float()
+    room[2 * bb:3 * bb] *= 2.0 ** -8
+    b.copy_(room.to(E4M3))
+    sa = torch.exp2(e.double()).float() * (1.0 if powers else sa * 100)
+    sb = torch.exp2(f.double()).float() * (1.0 if powers else sb * 100)
+    sa, sb = sa.expand(-(-k // 128), m).contiguous(), sb.expand(-(-k // 128), f.numel()).contiguous()
+    ref, size = ref_matmul(a, sa, 1, b, sb, bb)
+    out = apc.matmul_fp8(a, sa, b, sb, out_dtype=dtype)
+    bound = UNIT[dtype] * ref.abs() + size * (2.0 ** -23 * (128 + k / 128 + 5)) * (1 + UNIT[dtype]) + TINY[dtype] + \
+        -(-k // 128) * 2.0 ** -150 * (1 + sa[0].double()[:, None])
+    top = torch.finfo(dtype).max
+    inside = size * torch.clamp(1 / sa[0].double()[:, None], min=1) + bound < top
+    beyond = ref.abs() - bound > top * (1 + UNIT[dtype])  # between: sums that leave the range on the way
+    assert not out[::5].any()
+    worst = ((out.double() - ref).abs() / bound)[inside].max().item()
+    assert worst <= 1.0, worst
+    assert not torch.isfinite(out[beyond]).any()  # blocks' sums beyond the range, of both signs where they are a NaN
+    assert apc.device_status() == 0
