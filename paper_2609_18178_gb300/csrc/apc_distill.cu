@@ -19,9 +19,9 @@
 // word, and the CTA goes through its rows without waiting or copying further.
 #include <cuda_runtime.h>
 
-#include <algorithm>
 #include <type_traits>
 
+#include "apc_distill_plan.h"
 #include "apc_ops.cuh"
 #include "apc_tcgen05.cuh"
 
@@ -29,23 +29,8 @@ namespace apc {
 
 namespace {
 
-// Warps on the logits and on the teacher's entries, CTAs on an SM.  Measured on loss
-// and gradient of 8192 x 32768 with labels, when this shape took 254 us: 1 CTA of 16
-// warps 310, 12 warps 275, 4 warps 282 and, with 3 CTAs, 313.  Since then (199 us): 3
-// teachers 215, 2 252.
-constexpr int kWarps = 8, kWorkers = 32 * kWarps, kTeachers = 4;
 constexpr int kThreads = kWorkers + 32 * kTeachers + 32;
-constexpr int kMaxChunks = 16;
 constexpr int kMinPart = 16 * kWorkers;  // vectors of a row's part: 64 KB
-// Vectors of 16 bytes that each thread on the logits takes of a chunk.  Loss and
-// gradient hold a row between their passes, and smaller chunks let more of the next
-// row in meanwhile: 199 us on the same case (8 vectors 208, 5 219, 2 230).  The others let
-// chunks go at once and want fewer turns: loss of 4096 x 32768 41.9 us (4 vectors
-// 43.9), gradient of 1021 x 100003 83.7 (85.1).
-template <int FORM>
-constexpr int kVectorsOf = FORM == 3 ? 4 : 8;
-
-constexpr int kCtas = 2;
 constexpr int kMaxSplit = 8;
 constexpr float kInf = __builtin_huge_valf();
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -110,6 +95,7 @@ struct Shared {
   int32_t dead;
   int32_t pad_;
 };
+static_assert(sizeof(Shared) <= kSharedBytes, "more than the layout keeps for it");
 
 // A place in a ring of n and the parity of its use; no divisions: they and the other
 // index arithmetic between two rows took a quarter of a row's time.
@@ -117,16 +103,6 @@ struct RingTurn {
   uint32_t at = 0, phase = 0;
   __device__ __forceinline__ void next(uint32_t n) {
     if (++at == n) at = 0, phase ^= 1;
-  }
-};
-
-// How the rest of shared memory is shared out: the ring, each teacher's table of
-// ids, the entries of one row more than there are teachers and, for the loss alone,
-// as many rows' sums of every worker.
-struct Layout {
-  uint32_t chunk, chunks, teachers, room, slots_log2, sums;  // room: entries of a row, the label's among them; sums: words of them
-  __host__ __device__ uint32_t bytes() const {
-    return (uint32_t)sizeof(Shared) + 16 + chunks * chunk * 16 + (teachers + 1) * (room * 12 + sums * 4) + (teachers * 4 << slots_log2);
   }
 };
 
@@ -573,9 +549,9 @@ __global__ void __launch_bounds__(kThreads, kCtas)
                    const bool alike) {
   extern __shared__ __align__(16) uint8_t raw[];
   Shared &sh = *reinterpret_cast<Shared *>(raw);
-  uint4 *ring = reinterpret_cast<uint4 *>(raw + (sizeof(Shared) + 15) / 16 * 16);
+  uint4 *ring = reinterpret_cast<uint4 *>(raw + kSharedBytes);
   int32_t *tables = reinterpret_cast<int32_t *>(ring + layout.chunks * layout.chunk);
-  float *sums = reinterpret_cast<float *>(tables + (layout.teachers << layout.slots_log2)) + (layout.teachers + 1) * layout.room * 3;
+  float *sums = reinterpret_cast<float *>(tables + layout.tables) + (layout.teachers + 1) * layout.room * 3;
   const uint32_t kChunks = layout.chunks;
   constexpr int kPer = 16 / sizeof(T), kVectors = kVectorsOf<FORM>, kChunk = kWorkers * kVectors;
   constexpr bool kLoss = FORM & 1, kGrad = FORM & 2;
@@ -586,7 +562,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     for (uint32_t i = 0; i < kChunks; ++i) mbar_init(&sh.full[i], 1), mbar_init(&sh.empty[i], kWarps);
     for (int i = 0; i <= kTeachers; ++i) mbar_init(&sh.peer_full[i], 1), mbar_init(&sh.read[i], 1);
     sh.dead = 0;
-    uint8_t *entries = reinterpret_cast<uint8_t *>(tables + (layout.teachers << layout.slots_log2));
+    uint8_t *entries = reinterpret_cast<uint8_t *>(tables + layout.tables);
     for (uint32_t i = 0; i <= layout.teachers; ++i, entries += layout.room * 12) {
       sh.e[i].id = reinterpret_cast<int32_t *>(entries);
       sh.e[i].p = reinterpret_cast<float *>(entries + layout.room * 4);
@@ -823,10 +799,8 @@ int launch_distill(const DistillArgs &args, unsigned cap, unsigned sms, void *st
     const uint32_t size = sizeof(T), body = a.vocab / (16 / size);
     const bool alike = a.dlogits && ((uintptr_t)a.dlogits - (uintptr_t)a.logits) % 16 == 0 && (a.dpitch - a.pitch) * size % 16 == 0;
     const int k = !a.labels || a.inv_tau == 1.0f ? 0 : a.inv_tau == 0.5f ? 2 : a.inv_tau == 0.25f ? 4 : 1;
-    const uint32_t room = (a.k + 1 + 3) / 4 * 4;
-    uint32_t slots_log2 = 6;
-    while ((1u << slots_log2) < 2 * (a.k + 1)) ++slots_log2;
     if (rows_are_short(a, sms)) {
+      const uint32_t room = room_of(a.k), slots_log2 = slots_log2_of(a.k);
       const uint32_t bytes = kShortWarps * (room * 12 + (4u << slots_log2)), want = (a.rows + kShortWarps - 1) / kShortWarps;
       auto go = [&](auto kernel) {
         int e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
@@ -836,14 +810,7 @@ int launch_distill(const DistillArgs &args, unsigned cap, unsigned sms, void *st
       };
       return with_form(a, k, [&](auto form, auto power) { return go(short_kernel<T, form.value, power.value>); });
     }
-    Layout l = {};
-    l.teachers = a.k <= 512 ? kTeachers : 1;  // as many as leave the ring two chunks
-    l.room = room;
-    l.slots_log2 = slots_log2;
-    l.chunk = (a.loss && a.dlogits ? kVectorsOf<3> : kVectorsOf<1>) * kWorkers;
-    l.sums = a.dlogits ? 0 : 3 * kWorkers;
-    constexpr uint32_t kRoom = 228 * 1024 / kCtas - 1024;  // an SM's shared memory; 1 KB of each CTA's is the system's
-    l.chunks = std::min((uint32_t)kMaxChunks, (kRoom - l.bytes()) / (l.chunk * 16));
+    const Layout l = distill_layout(a.k, a.loss, a.dlogits);
     // a row over more CTAs while they would not fill the GPU, but not into parts of
     // less than 64 KB
     uint32_t split_log2 = 0;

@@ -864,3 +864,18 @@ def test_matmul_scales_far_apart(m, n, k, bb, powers, dtype):
     assert worst <= 1.0, worst
     assert not torch.isfinite(out[beyond]).any()  # blocks' sums beyond the range, of both signs where they are a NaN
     assert apc.device_status() == 0
+
+
+@pytest.mark.parametrize("k", [255, 256, 279, 280, 511, 512, 513, 700, 1024])
+def test_distill_over_the_kernel_s_shapes(k, monkeypatch):
+    """Every number of teachers' warps and ring of the kernel for longer rows, with
+    several rows a block."""
+    rows, vocab = 13, 33001
+    z = torch.randn(rows, vocab, generator=gen(1), device="cuda").mul_(3).bfloat16()
+    ids, u = teacher_of(rows, vocab, k, 2, wide=False)
+    labels = torch.randint(0, vocab, (rows,), generator=gen(4), device="cuda")
+    labels[:4] = ids[:4, 0].clamp(0, vocab - 1)
+    monkeypatch.setenv("APC_GRID_LIMIT", "2")
+    check_distill(z, ids, u, weights(rows))
+    check_distill(z, ids, u, weights(rows), 4.0, 0.7, 0.3, None, labels)
+    assert apc.device_status() == 0
