@@ -879,3 +879,48 @@ def test_distill_over_the_kernel_s_shapes(k, monkeypatch):
     check_distill(z, ids, u, weights(rows))
     check_distill(z, ids, u, weights(rows), 4.0, 0.7, 0.3, None, labels)
     assert apc.device_status() == 0
+
+
+@pytest.mark.parametrize("vocab,k,tau", [(1, 1, 2.0), (5, 7, 4.0), (100, 10, 2.5), (513, 40, 1.0), (2049, 256, 4.0), (4095, 33, 2.0)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_distill_one_warp_a_row(vocab, k, tau, dtype):
+    """As many rows as take a warp each (four for each SM), a few blocks going through
+    several: masks of both kinds, rows without a student or a teacher, equal ids, labels
+    on them and beyond the vocabulary, odd starts of the rows, every power of the temperature."""
+    rows = 4 * torch.cuda.get_device_properties(0).multi_processor_count + 3
+    z = torch.randn(rows, vocab, generator=gen(1), device="cuda").mul_(3)
+    z[::7, vocab // 2:] = -math.inf
+    z[1::7, vocab // 2:] = torch.finfo(dtype).min
+    z[2::31] = -math.inf
+    z[3::37] = torch.finfo(dtype).min
+    z = strided(z.to(dtype), 1, 3)
+    ids, u = teacher_of(rows, vocab, k, 2, wide=vocab % 2 == 0)
+    ids[::7] = ids[::7].clamp(max=max(0, vocab // 2 - 1)) if vocab > 1 else -1  # not on the masked half
+    ids[4::41] = -1
+    ids[5::43, k // 2:] = ids[5::43, :1]
+    u[5::43] = 1.0
+    labels = torch.randint(0, max(1, vocab // 2), (rows,), generator=gen(4), device="cuda")
+    on = (ids[:, 0] >= 0) & (ids[:, 0] < max(1, vocab // 2))
+    labels = torch.where(on & (torch.arange(rows, device="cuda") % 2 == 0), ids[:, 0].to(labels.dtype), labels)
+    if vocab == 1:
+        labels[::7] = -1
+    labels[::5] = -100
+    g = torch.rand(rows, generator=gen(5), device="cuda") - 0.3
+    g[::11] = 0.0
+    check_distill(z, ids, u, g)
+    check_distill(z, ids, u, g, tau, 0.7, 0.3, torch.full((rows,), 4.0, device="cuda") if k == 40 else None, labels)
+
+
+@pytest.mark.parametrize("vocab", [100, 4095])
+def test_distill_one_warp_a_row_does_not_depend_on_the_grid(vocab, monkeypatch):
+    rows = 5 * torch.cuda.get_device_properties(0).multi_processor_count
+    z = torch.randn(rows, vocab, generator=gen(1), device="cuda").bfloat16()
+    ids, u = teacher_of(rows, vocab, 30, 2)
+    g = weights(rows)
+    first = apc.distill_loss_grad(z, ids, u, g, temperature=2.0)
+    grad = apc.distill_grad(z, ids, u, first[1], g, temperature=2.0)
+    monkeypatch.setenv("APC_GRID_LIMIT", "2")
+    for x, y in zip(first, apc.distill_loss_grad(z, ids, u, g, temperature=2.0)):
+        assert torch.equal(x, y)
+    assert torch.equal(apc.distill_loss(z, ids, u, temperature=2.0)[0], first[0])
+    assert torch.equal(apc.distill_grad(z, ids, u, first[1], g, temperature=2.0), grad)
