@@ -489,12 +489,12 @@ __all__ += ["digests_to_host", "state_buffers", "device_status", "selftest_wait_
             "COMMIT_ZERO_GRAD", "TensorEntryBF16", "commit_step_bf16", "state_buffers_bf16"]
 
 _OPERATORS = ("quantize_fp8", "matmul_fp8", "distill_loss", "distill_grad", "distill_loss_grad")
-__all__ += list(_OPERATORS)
 
 
 def __getattr__(name: str):
     """The operators need torch, which the rest of this module imports only
-    where it is used: they are loaded when they are first asked for."""
+    where it is used: they are loaded when they are first asked for, by their
+    names alone (``import *`` loads no torch)."""
     if name in _OPERATORS:
         from . import operators
         globals().update((n, getattr(operators, n)) for n in _OPERATORS)

@@ -185,3 +185,17 @@ def test_allocated_outputs_are_memory_of_the_stream_given(handle, monkeypatch):
         del asked[:]
         call()
         assert asked == [[0x1230]] * outputs
+
+
+def test_star_import_needs_no_torch():
+    """The package without the operators works where torch cannot be imported."""
+    import os
+    import subprocess
+    import sys
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(apc.__file__)))
+    code = "import sys; sys.modules['torch'] = None\nfrom paper_2609_18178_gb300 import *\nprint(DEFAULT_HPARAMS['lr'], commit_step)"
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    assert "3e-04" in r.stdout or "0.0003" in r.stdout
+    assert apc.quantize_fp8.__module__.endswith("operators")
