@@ -164,9 +164,9 @@ apc_status distill(const apc_distill *d, const float *grad_loss, float *loss, fl
   const double tau = d->temperature;
   if (!std::isfinite(tau) || !((float)tau > 0.0f) || !std::isfinite((float)(1.0 / tau) * 1.4426950408889634f))
     return op_fail(APC_EINVAL, "temperature %g is not a positive binary32 number with a finite reciprocal", tau);
-  for (const double w : {d->kd_weight, d->label_weight})
-    if (!std::isfinite(w) || w < 0 || !std::isfinite((float)(w * tau * tau)) || !std::isfinite((float)w))
-      return op_fail(APC_EINVAL, "weight %g is negative or too large", w);
+  for (const double w : {d->kd_weight, d->kd_weight * tau, d->kd_weight * tau * tau, d->label_weight})
+    if (!std::isfinite(w) || w < 0 || !std::isfinite((float)w))
+      return op_fail(APC_EINVAL, "weight %g is negative or too large (the teacher's is taken times the temperature's square)", w);
   const int64_t es = size_of(d->dtype), ts = size_of(d->teacher_dtype), is = d->ids_dtype == APC_I64 ? 8 : 4;
   const int64_t ls = d->labels_dtype == APC_I64 ? 8 : 4, rows = d->rows, v = d->vocab;
   if (rows > 0 && v == 0) return op_fail(APC_EINVAL, "vocab is 0");

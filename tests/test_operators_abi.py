@@ -199,3 +199,17 @@ def test_star_import_needs_no_torch():
     assert r.returncode == 0, r.stderr
     assert "3e-04" in r.stdout or "0.0003" in r.stdout
     assert apc.quantize_fp8.__module__.endswith("operators")
+
+
+@pytest.mark.parametrize("kw,fine", [
+    (dict(kd_weight=0.0, label_weight=1.0, temperature=1e20), True),    # the square scales the teacher's part alone
+    (dict(kd_weight=0.0, label_weight=3e38, temperature=2.0), True),
+    (dict(kd_weight=1.0, label_weight=0.0, temperature=1e20), False),
+    (dict(kd_weight=3e38, label_weight=0.0, temperature=2.0), False),
+    (dict(kd_weight=float("nan"), label_weight=0.0), False),
+    (dict(kd_weight=0.0, label_weight=-1.0), False),
+])
+def test_distill_weights(kw, fine):
+    """Refused for a weight or not: without a device a call ends later all the same."""
+    distill(labels=AT + (9 << 32), **kw)
+    assert (b"weight" in apc.library().apc_last_error()) == (not fine)
