@@ -833,7 +833,7 @@ apc_status op_cuda_fail(int err, const char *what) { return cuda_fail(err, what)
 apc_status op_ranges(const OpRange *r, int n) {
   for (int i = 0; i < n; ++i)
     for (int j = 0; j < i; ++j)
-      if ((r[i].written || r[j].written) && r[i].lo < r[j].hi && r[j].lo < r[i].hi)
+      if ((r[i].written || r[j].written) && r[i].overlaps(r[j]))
         return fail(APC_EINVAL, "%s overlaps %s", r[i].name, r[j].name);
   int dev = 0;
   int e = (int)cudaGetDevice(&dev);

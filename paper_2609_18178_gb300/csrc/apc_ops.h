@@ -12,8 +12,17 @@ namespace apc {
 // ---- of apc_host.cpp: the error text, the pointer checks, the persistent grid
 struct OpRange {
   uintptr_t lo, hi;  // [lo, hi), not empty
+  uintptr_t width, pitch;  // rows of so many bytes, so far apart; a single one: pitch 0
   const char *name;
   bool written;
+
+  // Column ranges of one buffer lie between each other's rows.
+  bool overlaps(const OpRange &o) const {
+    if (lo >= o.hi || o.lo >= hi) return false;
+    if (!pitch || pitch != o.pitch) return true;
+    const uintptr_t at = (lo > o.lo ? lo - o.lo : pitch - (o.lo - lo) % pitch) % pitch;  // this one's columns behind the other's
+    return at < o.width || at + width > pitch;
+  }
 };
 
 void op_begin();

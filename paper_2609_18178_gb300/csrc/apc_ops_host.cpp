@@ -24,7 +24,8 @@ struct Ranges {
 
   // A matrix of so many rows, `width` bytes each, `pitch` bytes apart.
   void add(const char *name, const void *p, int64_t rows, int64_t width, int64_t pitch, bool written) {
-    if (rows > 0 && width > 0) r[n++] = {(uintptr_t)p, (uintptr_t)p + (uintptr_t)((rows - 1) * pitch + width), name, written};
+    if (rows > 0 && width > 0)
+      r[n++] = {(uintptr_t)p, (uintptr_t)p + (uintptr_t)((rows - 1) * pitch + width), (uintptr_t)width, rows > 1 ? (uintptr_t)pitch : 0, name, written};
   }
 };
 

@@ -924,3 +924,15 @@ def test_distill_one_warp_a_row_does_not_depend_on_the_grid(vocab, monkeypatch):
         assert torch.equal(x, y)
     assert torch.equal(apc.distill_loss(z, ids, u, temperature=2.0)[0], first[0])
     assert torch.equal(apc.distill_grad(z, ids, u, first[1], g, temperature=2.0), grad)
+
+
+def test_columns_of_one_buffer():
+    """Logits and their gradient as two halves of a buffer."""
+    rows, vocab, k = 9, 5000, 12
+    z = torch.randn(rows, vocab, generator=gen(1), device="cuda").bfloat16()
+    ids, u = teacher_of(rows, vocab, k, 2)
+    want = apc.distill_loss_grad(z, ids, u, weights(rows))
+    room = torch.zeros(rows, 2 * vocab, dtype=torch.bfloat16, device="cuda")
+    room[:, :vocab] = z
+    got = apc.distill_loss_grad(room[:, :vocab], ids, u, weights(rows), out=room[:, vocab:])
+    assert torch.equal(got[0], want[0]) and torch.equal(room[:, vocab:], want[2]) and torch.equal(room[:, :vocab], z)

@@ -213,3 +213,18 @@ def test_distill_weights(kw, fine):
     """Refused for a weight or not: without a device a call ends later all the same."""
     distill(labels=AT + (9 << 32), **kw)
     assert (b"weight" in apc.library().apc_last_error()) == (not fine)
+
+
+@pytest.mark.parametrize("d,dpitch,pitch,apart", [
+    (AT + 2000, 2000, 2000, True),          # two halves of one buffer
+    (AT + 2000 + 4000 * 3, 2000, 2000, True),   # the second half, some rows further on
+    (AT - 4000 * 2 + 2000, 2000, 2000, True),   # and some rows before
+    (AT + 1998, 2000, 2000, False),         # one element into the logits
+    (AT + 2002, 2000, 2000, False),         # and into their next row
+    (AT + 2000, 2008, 2000, False),         # rows that do not keep step
+    (AT - 4000 * 2 + 2002, 2000, 2000, False),
+])
+def test_columns_of_one_buffer_do_not_overlap(d, dpitch, pitch, apart):
+    """Logits and gradient side by side in a buffer: 16 rows of 1000 16-bit elements."""
+    distill(d=d, dpitch=dpitch, pitch=pitch)
+    assert (b"overlaps" in apc.library().apc_last_error()) == (not apart)
