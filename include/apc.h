@@ -222,9 +222,11 @@ apc_status apc_count_nonzero(const apc_buffer *bufs, int32_t num_bufs, int32_t n
  * What makes the gradient that apc_commit_step consumes, for a model whose
  * head is distilled in 8 bits: quantization with a scale per block of 128, the
  * matrix product of such operands, and the distillation loss with its
- * gradient.  Every sum has a fixed order and no result depends on the order of
- * atomics, so replicas that run the same step commit identical bits and their
- * digests agree.
+ * gradient.  Every sum has a fixed order that follows the call's arguments and the
+ * number of the GPU's SMs, not the grid or the order of atomics, so replicas that run
+ * the same step on the same kind of GPU commit identical bits and their digests agree.
+ * One argument's address counts: sums over a row of logits follow the row's place
+ * within 16 bytes, so equal bits need rows that are aligned alike.
  *
  * Matrices are row-major: element (i, j) of a matrix with pitch P sits at
  * i*P + j, and columns behind the last are neither read nor written.  A matrix

@@ -65,8 +65,8 @@ constexpr int kScaleSlots = 8;  // blocks whose scales are on their way or in us
 // ranks and stores.  The loads of the next tile run meanwhile.
 //
 // Bound by memory while it streams, and by launch, first loads and exchange, some 7 us.
-// Measured: 1 x 14336 x 4096 13.8 us (4.3 TB/s), 37 x 4096 x 14336 17.1 us (3.5 TB/s),
-// 777 x 1001 x 2500 to fp32 10.4 us.
+// Measured: 1 x 14336 x 4096 14.0 us (4.2 TB/s), 37 x 4096 x 14336 17.2 us (3.5 TB/s),
+// 777 x 1001 x 2500 to fp32 10.6 us.
 //
 // A wait that gives up marks the CTA dead: it stops loading and issuing, waits for
 // what is in flight, and its sums go on without waiting, so that every barrier is
@@ -290,10 +290,10 @@ __global__ void __launch_bounds__(kMidThreads, 1)
 // exponents' warp, which has nothing else to do there.
 // A tile's way is its own scales' alone, whatever its pair did before, so results do
 // not depend on which tiles a pair gets.
-// Measured: 4096 x 32768 x 4096 by exponents 331 us (3.3 PFLOP/s; the tensor cores busy for
-// 75% of the cycles, at 8192 columns), in general 480; 14336 x 4096 x 8192 with a
-// scale for every column 302 us (3.2 PFLOP/s), 693.  Back to back for seconds the
-// GPU's power limit takes the clock to 1.5 GHz: 384 and 342 us.
+// Measured: 4096 x 32768 x 4096 by exponents 322 us (3.4 PFLOP/s; the tensor cores busy for
+// 75% of the cycles, at 8192 columns), in general 567; 14336 x 4096 x 8192 with a
+// scale for every column 290 us (3.3 PFLOP/s), 724; 4096 x 8192 x 4096 to fp32 167.  Back to
+// back for seconds the GPU's power limit takes the clock to 1.5 GHz: 380 and 339 us.
 // Warps 0 to 3 load and issue with 56 registers a thread, 4 to 11 add with 224 (of
 // the launch's 168 each: 128 x 56 + 256 x 224 = 384 x 168).
 constexpr int kBigWarps = 8, kBigThreads = 128 + 32 * kBigWarps, kBigStages = 6;
@@ -770,8 +770,8 @@ bool may_go_by_exponents(uint32_t out_dtype, uint32_t blocks) {
 //   that, 8 with pairs.
 // For example 100 x 4096 x 4096: 64 columns in two halves 13.8 us, whole 16.7, tiles
 // of 128 22.0, of 256 x 256 19.6; 512 x 4096 x 4096: 30.7, 22.6 and 20.8 with tiles
-// of 64, 128 and 256.  By sizes and the GPU's SMs alone: the cap of a grid does not
-// change results.
+// of 64, 128 and 256 (12.8 and 17.0 since for the two that are taken).  By sizes, out's type
+// and the GPU's SMs alone: the cap of a grid does not change results.
 struct Choice {
   uint32_t cols, split_log2;  // cols 256: the pairs' kernel
 };
