@@ -117,7 +117,7 @@ typedef struct apc_tensor {
   uint64_t global_offset;
 } apc_tensor;
 
-typedef enum apc_dtype { APC_F32 = 0, APC_BF16 = 1, APC_F16 = 2 } apc_dtype;  /* APC_F16: the operators below only */
+typedef enum apc_dtype { APC_F32 = 0, APC_BF16 = 1, APC_F16 = 2 } apc_dtype;  /* APC_F16: the operators and apc_grad_norm only */
 
 /* One buffer for apc_digest: n elements of `dtype` at `data` (device), whose
  * element 0 has index global_offset in the flat model, summed into digest
@@ -217,6 +217,41 @@ apc_status apc_digest(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slot
 apc_status apc_count_nonzero(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots, apc_stream_t stream,
                              uint64_t *out_counts);
 
+#define APC_GRAD_NORM_WORKSPACE 2056 /* bytes */
+
+/* The 2-norm of the elements of a list of buffers, read only: the norm of a
+ * step's gradients, by which apc_commit_step_clipped clips them.
+ *   out_norms[slot] = sqrt(sum of x^2 over the slot's buffers), rounded to fp32
+ * Squares are summed in fp32 over tiles of a buffer that are counted from its
+ * first element, and the tiles' sums exactly: the result depends on the buffers'
+ * contents and lengths alone, not on their addresses, their order, the grid or the
+ * GPU, and is within 2^-19 of itself for any values.  Neither large nor tiny values
+ * overflow or vanish.  A slot with a NaN gives NaN, one with an infinity infinity; one
+ * without elements 0.
+ *   bufs       as for apc_digest, of any apc_dtype, any alignment to their elements
+ *              (global_offset is ignored)
+ *   workspace  device, 8-byte aligned, APC_GRAD_NORM_WORKSPACE bytes that no other
+ *              call uses before this one has completed; need not be initialised
+ *   out_norms  device, fp32, num_slots of them
+ * Errors as apc_digest. */
+apc_status apc_grad_norm(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots, void *workspace, apc_stream_t stream,
+                         float *out_norms);
+
+/* apc_commit_step_ex and apc_commit_step_bf16 with the gradients clipped in the same pass:
+ *   c  = 1 if *grad_norm <= max_norm, else max_norm / *grad_norm (IEEE divide)
+ *   g' = c * g in binary32, one rounding, takes g's place in the update; the gradient
+ *        buffers are left as they are (or zeroed, by flags)
+ * grad_norm (device, fp32, one value) is read when the kernel runs: apc_grad_norm's output
+ * on the same stream, or that of all ranks together.  An infinite norm gives c = 0, a NaN
+ * c = NaN.  max_norm: > 0 and finite, as binary32 too.
+ * Errors as apc_commit_step_ex; grad_norm must not overlap anything that is written. */
+apc_status apc_commit_step_clipped(const apc_tensor *table, int32_t num_tensors, const apc_adamw_hparams *hp, int64_t step,
+                                   uint32_t flags, const float *grad_norm, double max_norm, apc_stream_t stream,
+                                   uint64_t *out_digests);
+apc_status apc_commit_step_bf16_clipped(const apc_tensor_bf16 *table, int32_t num_tensors, const apc_adamw_hparams *hp,
+                                        int64_t step, uint32_t flags, const float *grad_norm, double max_norm,
+                                        apc_stream_t stream, uint64_t *out_digests);
+
 /* ---- The operators around a training step's output head -----------------
  *
  * What makes the gradient that apc_commit_step consumes, for a model whose
@@ -285,6 +320,64 @@ apc_status apc_quantize_fp8(const void *x, int64_t rows, int64_t cols, int64_t p
  * can be repeated). */
 apc_status apc_matmul_fp8(const apc_fp8_matrix *a, const apc_fp8_matrix *b, int64_t m, int64_t n, int64_t k, void *out,
                           int64_t out_pitch, uint32_t out_dtype, apc_stream_t stream);
+
+/* The root-mean-square norm of each row, after the residual's addition: what
+ * stands in front of the head, whose operand it can write.
+ *   h    = x + residual, rounded to x's type and kept in sum; x without a residual
+ *   rstd = 1 / sqrt(mean of h^2 + eps), fp32: the mean of the stored h, rounded once
+ *          from a sum that no thread layout changes beyond 2^-26 of itself
+ *   y    = (h * rstd) * weight in fp32
+ * Squares that overflow binary32 are taken scaled.  A row with a NaN has rstd NaN, one
+ * with an infinity 0 (and NaNs where the infinities are).
+ *   x, residual, sum  rows x cols, apc_dtype, pitches in elements; residual NULL: none,
+ *                     and sum NULL too.  sum may be x's or residual's own memory
+ *                     with the same pitch
+ *   weight            cols values of weight_dtype
+ *   eps               1e-20 or more as binary32, finite */
+typedef struct apc_norm {
+  const void *x, *residual, *weight;
+  void *sum;
+  int64_t rows, cols;
+  int64_t pitch, residual_pitch, sum_pitch;
+  uint32_t dtype, weight_dtype;
+  double eps;
+} apc_norm;
+
+/* out (rows x cols, x's type): y rounded once.  rstd: fp32, one per row, for the
+ * gradient.  Errors as apc_quantize_fp8. */
+apc_status apc_rms_norm(const apc_norm *d, void *out, int64_t out_pitch, float *rstd, apc_stream_t stream);
+
+/* The same with y in 8 bits, as apc_quantize_fp8 would write it from fp32 (block_rows 1):
+ * rows in q and, unless qt is NULL, the transpose in qt, its blocks along its own rows. */
+apc_status apc_rms_norm_fp8(const apc_norm *d, const apc_fp8_matrix *q, const apc_fp8_matrix *qt, float *rstd,
+                            apc_stream_t stream);
+
+/* The gradient of the norm: with z = h * rstd and g = dout * weight,
+ *   dx      = (g - z * mean of g z) * rstd + dresidual   (x's gradient and residual's)
+ *   dweight = sum over rows of dout * z
+ * in fp32, each rounded once.  The rows are summed in runs whose number follows rows and
+ * cols alone, and the runs in order.
+ *   x          h: the norm's sum, or its x where there was no residual
+ *   dresidual  the gradient that reaches sum otherwise, or NULL
+ *   rstd       as the norm left it */
+typedef struct apc_norm_grad {
+  const void *dout, *x, *weight, *dresidual;
+  const float *rstd;
+  int64_t rows, cols;
+  int64_t dout_pitch, pitch, dresidual_pitch;
+  uint32_t dtype, weight_dtype;
+} apc_norm_grad;
+
+/* Bytes of the workspace: host only, no CUDA call; 0 for sizes out of range. */
+int64_t apc_rms_norm_grad_workspace(int64_t rows, int64_t cols);
+
+/* dx (rows x cols, x's type) may be dout's or dresidual's own memory with the same pitch.
+ * dweight: cols values of dweight_dtype, or NULL with workspace NULL: not wanted; without
+ * rows it is zeros.  workspace: device, 4-byte aligned, apc_rms_norm_grad_workspace bytes
+ * that no other call uses before this one has completed; need not be initialised.
+ * Errors as apc_quantize_fp8. */
+apc_status apc_rms_norm_grad(const apc_norm_grad *d, void *dx, int64_t dx_pitch, void *dweight, uint32_t dweight_dtype,
+                             float *workspace, apc_stream_t stream);
 
 typedef enum apc_index { APC_I32 = 0, APC_I64 = 1 } apc_index;
 

@@ -13,15 +13,19 @@ Entry points mirror the C names:
   and the four state digests (p', m', v', w).
 * :func:`digest` -> ``apc_digest``: the same digests of arbitrary buffers,
   read only (post-recovery verification).
+* :func:`grad_norm` -> ``apc_grad_norm``: the norm of a table's gradients, by
+  which :func:`commit_step` and :func:`commit_step_bf16` clip them
+  (``apc_commit_step_clipped``, ``apc_commit_step_bf16_clipped``).
 * :func:`resolve_hparams` -> ``apc_resolve_hparams``: the step's binary32
   scalars (host only).
 * :func:`upload` -> ``apc_upload``: host-to-device upload executed by a
   bounded number of CTAs, and :func:`set_reserved_sms` ->
   ``apc_set_reserved_sms``: SMs the persistent kernels leave free for it.
-* :mod:`.operators`: 8-bit quantization, the block-scaled 8-bit product and
-  distillation, around the output head of the step that makes the gradient
-  (``quantize_fp8``, ``matmul_fp8``, ``distill_loss``, ``distill_grad``,
-  ``distill_loss_grad``, here too).
+* :mod:`.operators`: the norm in front of the output head and its gradient,
+  8-bit quantization, the block-scaled 8-bit product and distillation, around
+  the head of the step that makes the gradient (``rms_norm``, ``rms_norm_fp8``,
+  ``rms_norm_grad``, ``quantize_fp8``, ``matmul_fp8``, ``distill_loss``,
+  ``distill_grad``, ``distill_loss_grad``, here too).
 
 ``stream`` is a ``torch.cuda.Stream`` or a handle, the current stream if not
 given.  Outputs that a call allocates are memory of that stream: code on another
@@ -45,7 +49,7 @@ __all__ = ["TensorEntry", "TensorEntryBF16", "BufferEntry", "PreparedTable", "Ap
            "Segment", "upload", "prepare_segments", "set_reserved_sms", "library", "lib_path", "F32", "BF16",
            "DEFAULT_HPARAMS"]
 
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 MASK64 = (1 << 64) - 1
 DEFAULT_HPARAMS = dict(lr=3e-4, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1)
 
@@ -121,8 +125,22 @@ def library():
         lib.apc_set_reserved_sms.argtypes = [i32]
         lib.apc_set_reserved_sms.restype = ctypes.c_int
         u32 = ctypes.c_uint32
+        lib.apc_commit_step_clipped.argtypes = [vp, i32, vp, i64, u32, vp, ctypes.c_double, vp, vp]
+        lib.apc_commit_step_clipped.restype = ctypes.c_int
+        lib.apc_commit_step_bf16_clipped.argtypes = [vp, i32, vp, i64, u32, vp, ctypes.c_double, vp, vp]
+        lib.apc_commit_step_bf16_clipped.restype = ctypes.c_int
+        lib.apc_grad_norm.argtypes = [vp, i32, i32, vp, vp, vp]
+        lib.apc_grad_norm.restype = ctypes.c_int
         lib.apc_quantize_fp8.argtypes = [vp, i64, i64, i64, u32, vp, vp, vp]
         lib.apc_quantize_fp8.restype = ctypes.c_int
+        lib.apc_rms_norm.argtypes = [vp, vp, i64, vp, vp]
+        lib.apc_rms_norm.restype = ctypes.c_int
+        lib.apc_rms_norm_fp8.argtypes = [vp, vp, vp, vp, vp]
+        lib.apc_rms_norm_fp8.restype = ctypes.c_int
+        lib.apc_rms_norm_grad_workspace.argtypes = [i64, i64]
+        lib.apc_rms_norm_grad_workspace.restype = i64
+        lib.apc_rms_norm_grad.argtypes = [vp, vp, i64, vp, u32, vp, vp]
+        lib.apc_rms_norm_grad.restype = ctypes.c_int
         lib.apc_matmul_fp8.argtypes = [vp, vp, i64, i64, i64, vp, i64, u32, vp]
         lib.apc_matmul_fp8.restype = ctypes.c_int
         lib.apc_distill_loss.argtypes = [vp, vp, vp, vp]
@@ -262,6 +280,7 @@ class PreparedTable:
 
     def __init__(self, kind: str, arr, count: int, first, keep: list):
         self.kind, self.arr, self.count, self.first, self._keep = kind, arr, count, first, keep
+        self.grads = None  # a commit table's gradients as a buffer list, once grad_norm has asked for it
 
     def __len__(self) -> int:
         return self.count
@@ -303,19 +322,41 @@ def prepare_table(table: Sequence[TensorEntry] | Sequence[TensorEntryBF16]) -> P
     return PreparedTable(kind, arr, n, first, table)
 
 
+def _clip(grad_norm, max_norm):
+    """The address of the norm and the largest one allowed, or None without clipping."""
+    if grad_norm is None and max_norm is None:
+        return None
+    if grad_norm is None or max_norm is None:
+        raise ValueError("clipping takes both grad_norm and max_norm")
+    if not isinstance(grad_norm, int):
+        import torch
+        if grad_norm.dtype != torch.float32 or grad_norm.numel() != 1:
+            raise ValueError("grad_norm: expected one float32 value, got %s of %s" % (tuple(grad_norm.shape), grad_norm.dtype))
+    return _ptr(grad_norm), float(max_norm)
+
+
 def commit_step(table: Sequence[TensorEntry] | PreparedTable, step: int, hparams: dict | None = None, stream=None,
-                out=None, zero_grad: bool = False):
+                out=None, zero_grad: bool = False, grad_norm=None, max_norm: float | None = None):
     """Enqueue the committed AdamW step + digest over ``table`` on ``stream``
     (``apc_commit_step``, or ``apc_commit_step_ex`` with
     APC_COMMIT_ZERO_GRAD when ``zero_grad``: the gradients are also zeroed).
     ``table`` is a list of :class:`TensorEntry` or a :class:`PreparedTable`.
 
+    With ``grad_norm`` (a device float32 value, see :func:`grad_norm`) and
+    ``max_norm`` the update takes the gradients times ``max_norm / grad_norm``
+    where the norm exceeds ``max_norm`` (``apc_commit_step_clipped``).
+
     Returns the device int64[4] tensor that receives {D_p', D_m', D_v', D_w}
     (bit patterns of the unsigned digests; see :func:`digests_to_host`)."""
     arr, n, first = _commit_array(table, "f32")
+    clip = _clip(grad_norm, max_norm)
     out = _out(out, 4, first, stream)
     hp = _hp(hparams)
-    if zero_grad:
+    if clip:
+        _check(library().apc_commit_step_clipped(ctypes.addressof(arr), n, ctypes.addressof(hp), int(step),
+                                                 COMMIT_ZERO_GRAD if zero_grad else 0, *clip, _stream(stream),
+                                                 _ptr(out, 8)))
+    elif zero_grad:
         _check(library().apc_commit_step_ex(ctypes.addressof(arr), n, ctypes.addressof(hp), int(step),
                                             COMMIT_ZERO_GRAD, _stream(stream),
                                             _ptr(out, 8)))
@@ -326,15 +367,99 @@ def commit_step(table: Sequence[TensorEntry] | PreparedTable, step: int, hparams
 
 
 def commit_step_bf16(table: Sequence[TensorEntryBF16] | PreparedTable, step: int, hparams: dict | None = None,
-                     stream=None, out=None, zero_grad: bool = False):
-    """Enqueue the bf16-state committed step (``apc_commit_step_bf16``).
+                     stream=None, out=None, zero_grad: bool = False, grad_norm=None, max_norm: float | None = None):
+    """Enqueue the bf16-state committed step (``apc_commit_step_bf16``), with
+    the gradients clipped as in :func:`commit_step` if ``grad_norm`` and
+    ``max_norm`` are given (``apc_commit_step_bf16_clipped``).
     Returns the device int64[3] tensor of {D_p', D_m', D_v'}."""
     arr, n, first = _commit_array(table, "bf16")
+    clip = _clip(grad_norm, max_norm)
     out = _out(out, 3, first, stream)
     hp = _hp(hparams)
-    _check(library().apc_commit_step_bf16(ctypes.addressof(arr), n, ctypes.addressof(hp), int(step),
-                                          COMMIT_ZERO_GRAD if zero_grad else 0, _stream(stream),
-                                          _ptr(out, 8)))
+    flags = COMMIT_ZERO_GRAD if zero_grad else 0
+    if clip:
+        _check(library().apc_commit_step_bf16_clipped(ctypes.addressof(arr), n, ctypes.addressof(hp), int(step), flags,
+                                                      *clip, _stream(stream), _ptr(out, 8)))
+    else:
+        _check(library().apc_commit_step_bf16(ctypes.addressof(arr), n, ctypes.addressof(hp), int(step), flags,
+                                              _stream(stream), _ptr(out, 8)))
+    return out
+
+
+GRAD_NORM_WORKSPACE = 2056
+
+
+def _grads(grads):
+    """The C array of a gradient list, its length and a tensor of it."""
+    if isinstance(grads, PreparedTable):
+        if grads.kind == "grads":
+            return grads.arr, grads.count, grads.first
+        if grads.kind not in ("f32", "bf16"):
+            raise ValueError("prepared table is a %s table, expected gradients or a commit table" % grads.kind)
+        if grads.grads is None:  # the table's own gradients, once
+            arr = (_Buffer * max(1, grads.count))()
+            for i in range(grads.count):
+                arr[i] = _Buffer(grads.arr[i].g, grads.arr[i].n, 0, BF16, 0)
+            grads.grads = arr
+        return grads.grads, grads.count, grads.first
+    grads = list(grads)
+    arr = (_Buffer * max(1, len(grads)))()
+    first = kinds = None
+    for i, g in enumerate(grads):
+        slot, dt, n = 0, None, None
+        if isinstance(g, (TensorEntry, TensorEntryBF16)):
+            g, dt, n = g.g, BF16, g.count()
+        elif isinstance(g, BufferEntry):
+            g, slot, dt, n = g.data, g.slot, g.dtype, g.n
+        if isinstance(g, int) or g is None:
+            if dt is None or n is None:
+                raise ValueError("grads[%d]: a raw pointer takes a BufferEntry with dtype and n" % i)
+        else:
+            if kinds is None:
+                import torch
+                # 16-bit integers are bf16 bit patterns, as in the tables
+                kinds = {torch.float32: F32, torch.bfloat16: BF16, torch.int16: BF16, torch.float16: F16}
+            kind = kinds.get(g.dtype)
+            if kind is None or (dt is not None and dt != kind and g.dtype != torch.int16):
+                raise ValueError("grads[%d] has type %s" % (i, g.dtype))
+            dt = kind if dt is None else dt
+            n = g.numel() if n is None else n
+            if g.numel() < n:
+                raise ValueError("grads[%d] has %d < %d elements" % (i, g.numel(), n))
+            first = g if first is None else first
+        arr[i] = _Buffer(_ptr(g, 4 if dt == F32 else 2), int(n), 0, dt, int(slot))
+    return arr, len(grads), first
+
+
+def prepare_grads(grads) -> PreparedTable:
+    """Marshal a gradient list once for :func:`grad_norm`."""
+    grads = list(grads)
+    arr, n, first = _grads(grads)
+    return PreparedTable("grads", arr, n, first, grads)
+
+
+def grad_norm(grads, num_slots: int = 1, stream=None, out=None, workspace=None):
+    """Enqueue the 2-norm of all elements of ``grads`` (``apc_grad_norm``): a
+    list of tensors (fp32, bf16 or fp16; int16 holds bf16 bits),
+    :class:`BufferEntry` (whose slot's norm they enter) or commit-table entries
+    (their gradients), a commit table prepared by :func:`prepare_table`, or a
+    list prepared by :func:`prepare_grads`.
+
+    Returns the device float32[num_slots] tensor of norms.  ``workspace``:
+    ``GRAD_NORM_WORKSPACE`` bytes for a caller that keeps its own, which no
+    other call may use at the same time."""
+    arr, n, first = _grads(grads)
+    import torch
+    dev = first.device if hasattr(first, "device") else torch.device("cuda", torch.cuda.current_device())
+    if out is None:
+        out = _empty(num_slots, torch.float32, dev, stream)
+    elif not isinstance(out, int) and (out.dtype != torch.float32 or out.numel() < num_slots):
+        raise ValueError("out: expected %d float32 values, got %s of %s" % (num_slots, tuple(out.shape), out.dtype))
+    if workspace is None:
+        workspace = _empty(GRAD_NORM_WORKSPACE // 8, torch.int64, dev, stream)
+    elif not isinstance(workspace, int) and workspace.numel() * workspace.element_size() < GRAD_NORM_WORKSPACE:
+        raise ValueError("workspace holds fewer than %d bytes" % GRAD_NORM_WORKSPACE)
+    _check(library().apc_grad_norm(ctypes.addressof(arr), n, int(num_slots), _ptr(workspace), _stream(stream), _ptr(out)))
     return out
 
 
@@ -486,9 +611,10 @@ def state_buffers_bf16(p, m, v, global_offset: int = 0) -> list[BufferEntry]:
 
 
 __all__ += ["digests_to_host", "state_buffers", "device_status", "selftest_wait_timeout", "count_nonzero",
-            "COMMIT_ZERO_GRAD", "TensorEntryBF16", "commit_step_bf16", "state_buffers_bf16"]
+            "COMMIT_ZERO_GRAD", "GRAD_NORM_WORKSPACE", "F16", "grad_norm", "prepare_grads", "TensorEntryBF16", "commit_step_bf16", "state_buffers_bf16"]
 
-_OPERATORS = ("quantize_fp8", "matmul_fp8", "distill_loss", "distill_grad", "distill_loss_grad")
+_OPERATORS = ("quantize_fp8", "matmul_fp8", "rms_norm", "rms_norm_fp8", "rms_norm_grad", "distill_loss", "distill_grad",
+              "distill_loss_grad")
 
 
 def __getattr__(name: str):

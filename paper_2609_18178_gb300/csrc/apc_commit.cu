@@ -191,12 +191,12 @@ struct F32State {
   };
 
   // Elements e and e + kConsumers of a misaligned tile.
-  template <bool ZERO>
+  template <bool ZERO, bool CLIP>
   __device__ static void mis_pair(const StageDesc &sd, const Mis &x, uint32_t e, const Scalars &s, Acc &a) {
     const uint32_t f = e + kConsumers;
     float p[2] = {x.p[e], x.p[f]}, m[2] = {x.m[e], x.m[f]}, v[2] = {x.v[e], x.v[f]};
     const uint32_t gw[2] = {x.g[e], x.g[f]};
-    adamw_group<2>(p, m, v, gw, s);
+    adamw_group<2, CLIP>(p, m, v, gw, s);
     const uint32_t w = pack_bf16x2(p[0], p[1]);
     mis_store<ZERO>(sd, e, p[0], m[0], v[0], w & 0xFFFFu);
     mis_store<ZERO>(sd, f, p[1], m[1], v[1], w >> 16);
@@ -208,10 +208,10 @@ struct F32State {
   }
 
   // Element e of a misaligned tile.
-  template <bool ZERO>
+  template <bool ZERO, bool CLIP>
   __device__ static void mis_one(const StageDesc &sd, const Mis &x, uint32_t e, const Scalars &s, Acc &a) {
     float p = x.p[e], m = x.m[e], v = x.v[e];
-    const uint32_t w = adamw_element(p, m, v, x.g[e], s), G = sd.G + e;
+    const uint32_t w = adamw_element<CLIP>(p, m, v, x.g[e], s), G = sd.G + e;
     mis_store<ZERO>(sd, e, p, m, v, w);
     acc_add(a.p, digest_term(G, __float_as_uint(p), s.one), s.one);
     acc_add(a.m, digest_term(G, __float_as_uint(m), s.one), s.one);
@@ -230,7 +230,7 @@ struct F32State {
 
   // Four consecutive elements at the compile-time element offset OFF from
   // the thread's output addresses, whose first element has digest index G.
-  template <uint32_t OFF, bool ZERO, bool MIS>
+  template <uint32_t OFF, bool ZERO, bool MIS, bool CLIP>
   __device__ static void compute_store(const Dst &d, uint32_t G, const Regs &r, bool half, const Scalars &s, Acc &a) {
     constexpr uint32_t off = OFF;
     float p[4] = {r.p.x, r.p.y, r.p.z, r.p.w};
@@ -242,9 +242,9 @@ struct F32State {
       // instructions, measured slower here (453 M elements in 2,150 us
       // against 2,043)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) (void)adamw_element(p[j], m[j], v[j], gw[j], s);
+      for (int j = 0; j < 4; ++j) (void)adamw_element<CLIP>(p[j], m[j], v[j], gw[j], s);
     } else {
-      adamw_group<4>(p, m, v, gw, s);
+      adamw_group<4, CLIP>(p, m, v, gw, s);
     }
     __stcs(reinterpret_cast<float4 *>(static_cast<float *>(d.p) + off), make_float4(p[0], p[1], p[2], p[3]));
     __stcs(reinterpret_cast<float4 *>(static_cast<float *>(d.m) + off), make_float4(m[0], m[1], m[2], m[3]));
@@ -277,10 +277,11 @@ struct F32State {
     a.w += hterm<OFF + 2, 0, SHARED>(G, w23, one, top) + hterm<OFF + 3, 1, SHARED>(G, w23, one, top);
   }
 
+  template <bool CLIP>
   __device__ static void one(const CommitEntry &E, uint64_t i, const Scalars &s, Acc &a) {
     float *P = static_cast<float *>(E.p), *M = static_cast<float *>(E.m), *V = static_cast<float *>(E.v);
     float p = P[i], m = M[i], v = V[i];
-    const uint32_t w = adamw_element(p, m, v, (uint32_t)E.g[i], s);
+    const uint32_t w = adamw_element<CLIP>(p, m, v, (uint32_t)E.g[i], s);
     P[i] = p;
     M[i] = m;
     V[i] = v;
@@ -329,13 +330,13 @@ struct BF16State {
     }
   };
 
-  template <bool ZERO>
+  template <bool ZERO, bool CLIP>
   __device__ static void mis_pair(const StageDesc &sd, const Mis &x, uint32_t e, const Scalars &s, Acc &a) {
     const uint32_t f = e + kConsumers;
     float pf[2] = {bf16_value(x.p[e]), bf16_value(x.p[f])}, mf[2] = {bf16_value(x.m[e]), bf16_value(x.m[f])};
     float vf[2] = {bf16_value(x.v[e]), bf16_value(x.v[f])};
     const uint32_t gw[2] = {x.g[e], x.g[f]};
-    adamw_group<2>(pf, mf, vf, gw, s);
+    adamw_group<2, CLIP>(pf, mf, vf, gw, s);
     const uint32_t p = pack_bf16x2(pf[0], pf[1]), m = pack_bf16x2(mf[0], mf[1]), v = pack_bf16x2(vf[0], vf[1]);
     mis_store<ZERO>(sd, e, p & 0xFFFFu, m & 0xFFFFu, v & 0xFFFFu);
     mis_store<ZERO>(sd, f, p >> 16, m >> 16, v >> 16);
@@ -345,10 +346,10 @@ struct BF16State {
     a.v += digest_term<0>(G, v & 0xFFFFu, s.one) + digest_term<kConsumers>(G, v >> 16, s.one);
   }
 
-  template <bool ZERO>
+  template <bool ZERO, bool CLIP>
   __device__ static void mis_one(const StageDesc &sd, const Mis &x, uint32_t e, const Scalars &s, Acc &a) {
     float p = bf16_value(x.p[e]), m = bf16_value(x.m[e]), v = bf16_value(x.v[e]);
-    const uint32_t po = adamw_element(p, m, v, x.g[e], s), mo = bf16_rne_bits(m), vo = bf16_rne_bits(v);
+    const uint32_t po = adamw_element<CLIP>(p, m, v, x.g[e], s), mo = bf16_rne_bits(m), vo = bf16_rne_bits(v);
     mis_store<ZERO>(sd, e, po, mo, vo);
     const uint32_t G = sd.G + e;
     acc_add(a.p, digest_term(G, po, s.one), s.one);
@@ -364,7 +365,7 @@ struct BF16State {
     if (ZERO) __stcs(sd.g + e, (uint16_t)0);
   }
 
-  template <uint32_t OFF, bool ZERO, bool MIS>
+  template <uint32_t OFF, bool ZERO, bool MIS, bool CLIP>
   __device__ static void compute_store(const Dst &d, uint32_t G, const Regs &r, bool half, const Scalars &s, Acc &a) {
     constexpr uint32_t off = OFF;
     const uint32_t pw[4] = {r.p.x & 0xFFFFu, r.p.x >> 16, r.p.y & 0xFFFFu, r.p.y >> 16};
@@ -378,7 +379,7 @@ struct BF16State {
       mf[j] = bf16_value(mw[j]);
       vf[j] = bf16_value(vw[j]);
     }
-    adamw_group<4>(pf, mf, vf, gw, s);
+    adamw_group<4, CLIP>(pf, mf, vf, gw, s);
     const uint32_t p01 = pack_bf16x2(pf[0], pf[1]), p23 = pack_bf16x2(pf[2], pf[3]);
     const uint32_t m01 = pack_bf16x2(mf[0], mf[1]), m23 = pack_bf16x2(mf[2], mf[3]);
     const uint32_t v01 = pack_bf16x2(vf[0], vf[1]), v23 = pack_bf16x2(vf[2], vf[3]);
@@ -402,10 +403,11 @@ struct BF16State {
     a.v += hterm<K, 0, SHARED>(G, v, one, top) + hterm<K + 1, 1, SHARED>(G, v, one, top);
   }
 
+  template <bool CLIP>
   __device__ static void one(const CommitEntry &E, uint64_t i, const Scalars &s, Acc &a) {
     uint16_t *P = static_cast<uint16_t *>(E.p), *M = static_cast<uint16_t *>(E.m), *V = static_cast<uint16_t *>(E.v);
     float p = bf16_value(P[i]), m = bf16_value(M[i]), v = bf16_value(V[i]);
-    const uint32_t po = adamw_element(p, m, v, (uint32_t)E.g[i], s);
+    const uint32_t po = adamw_element<CLIP>(p, m, v, (uint32_t)E.g[i], s);
     const uint32_t mo = bf16_rne_bits(m), vo = bf16_rne_bits(v);
     P[i] = (uint16_t)po;
     M[i] = (uint16_t)mo;
@@ -421,7 +423,7 @@ struct BF16State {
 // offset K * 4 * L::kConsumers from the thread's output addresses, which
 // the stores carry as immediates and the digest terms fold into their
 // increment.
-template <class L, bool ZERO, bool MIS, int K>
+template <class L, bool ZERO, bool MIS, bool CLIP, int K>
 __device__ __forceinline__ void store_groups(const Dst &d, uint32_t G1, const typename L::Regs *r, const bool *ok, bool half,
                                              const Scalars &s, Acc &a) {
   constexpr uint32_t off = (uint32_t)(K * L::kConsumers) * 4;
@@ -430,9 +432,9 @@ __device__ __forceinline__ void store_groups(const Dst &d, uint32_t G1, const ty
       if (MIS && half) store_words4(d.g + off, make_uint2(0u, 0u));
       else __stcs(reinterpret_cast<uint2 *>(d.g + off), make_uint2(0u, 0u));
     }
-    L::template compute_store<off, ZERO, MIS>(d, G1, r[K], half, s, a);
+    L::template compute_store<off, ZERO, MIS, CLIP>(d, G1, r[K], half, s, a);
   }
-  if constexpr (K + 1 < L::kGroups) store_groups<L, ZERO, MIS, K + 1>(d, G1, r, ok, half, s, a);
+  if constexpr (K + 1 < L::kGroups) store_groups<L, ZERO, MIS, CLIP, K + 1>(d, G1, r, ok, half, s, a);
 }
 
 // The stage's four regions; with MIS each has 16 bytes more, for the blocks
@@ -485,7 +487,7 @@ __device__ __forceinline__ TileWalk tile_walk(uint64_t total) {
   return {t0, t0 + per + (b < rem ? 1 : 0), 1};
 }
 
-template <class L, int MAXE, bool ZERO, bool MIS>
+template <class L, int MAXE, bool ZERO, bool MIS, bool CLIP>
 __global__ void __launch_bounds__(L::kBoundThreads, kCommitBlocksPerSm)
     commit_kernel(const __grid_constant__ CommitPlan<MAXE> plan, unsigned long long *out) {
   constexpr bool kSweep = L::kDigests == 4 || ZERO;  // all but bf16 state without zeroing
@@ -510,9 +512,10 @@ __global__ void __launch_bounds__(L::kBoundThreads, kCommitBlocksPerSm)
   __syncthreads();
 
   Acc a{0, 0, 0, 0};
+  const float clip = CLIP ? clip_factor(__ldg(plan.clip_norm), plan.clip_max) : 1.0f;
   if (warp == L::kConsumerWarps) {
     // ------------------------------------------------------------ producer
-    const Scalars s{plan.h, plan.pair, plan.limit, plan.one};
+    const Scalars s{plan.h, plan.pair, plan.limit, plan.one, clip};
     uint32_t phase = 0;
     int stage = 0;
     uint64_t issued = 0;
@@ -572,7 +575,7 @@ __global__ void __launch_bounds__(L::kBoundThreads, kCommitBlocksPerSm)
       const CommitEntry &E = plan.e[e];
       if (lane < (uint32_t)(E.n - E.body)) {
         const uint64_t i = lane < E.head ? lane : lane + E.body;
-        L::one(E, i, s, a);
+        L::template one<CLIP>(E, i, s, a);
         if (ZERO) const_cast<uint16_t *>(E.g)[i] = 0;
       }
     }
@@ -591,7 +594,7 @@ __global__ void __launch_bounds__(L::kBoundThreads, kCommitBlocksPerSm)
     __syncwarp();
   } else {
     // ----------------------------------------------------------- consumers
-    const Scalars s{plan.h, plan.pair, plan.limit, plan.one};
+    const Scalars s{plan.h, plan.pair, plan.limit, plan.one, clip};
     const int ct = threadIdx.x;  // 0 .. L::kConsumers-1
     uint32_t phase = 0;
     int stage = 0;
@@ -609,8 +612,8 @@ __global__ void __launch_bounds__(L::kBoundThreads, kCommitBlocksPerSm)
         const typename L::Mis x(st, sd.cnt);
         uint32_t e = ct;
 #pragma unroll L::kMisUnroll
-        for (; e + L::kConsumers < cnt; e += 2 * L::kConsumers) L::template mis_pair<ZERO>(sd, x, e, s, a);
-        if (e < cnt) L::template mis_one<ZERO>(sd, x, e, s, a);
+        for (; e + L::kConsumers < cnt; e += 2 * L::kConsumers) L::template mis_pair<ZERO, CLIP>(sd, x, e, s, a);
+        if (e < cnt) L::template mis_one<ZERO, CLIP>(sd, x, e, s, a);
         __syncwarp();
         if (lane == 0) mbar_arrive(&empty[stage]);
       } else {
@@ -630,7 +633,7 @@ __global__ void __launch_bounds__(L::kBoundThreads, kCommitBlocksPerSm)
         const uint32_t ob = 4u * (uint32_t)ct;
         const Dst d{sd.p + ob * L::kES, sd.m + ob * L::kES, sd.v + ob * L::kES,
                     L::kDigests == 4 ? sd.w + ob : nullptr, sd.g + ob};
-        store_groups<L, ZERO, MIS, 0>(d, sd.G + ob, r, ok, half, s, a);
+        store_groups<L, ZERO, MIS, CLIP, 0>(d, sd.G + ob, r, ok, half, s, a);
       }
       if (++stage == L::kStages) {
         stage = 0;
@@ -666,7 +669,7 @@ __global__ void wait_timeout_kernel(uint64_t limit_ns) {
 // The dynamic shared-memory limit of one kernel instantiation, raised once
 // per device (the first launch on a device sets it; later launches, for
 // example inside a stream capture, only enqueue).
-template <class L, int MAXE, bool ZERO, bool MIS>
+template <class L, int MAXE, bool ZERO, bool MIS, bool CLIP>
 int ensure_smem_attribute() {
   static std::atomic<uint64_t> done_mask{0};
   int dev = 0;
@@ -674,11 +677,11 @@ int ensure_smem_attribute() {
   if (e != cudaSuccess) return (int)e;
   const uint64_t bit = dev < 64 ? (1ull << dev) : 0;
   if (bit && (done_mask.load(std::memory_order_acquire) & bit)) return 0;
-  e = cudaFuncSetAttribute(commit_kernel<L, MAXE, ZERO, MIS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  e = cudaFuncSetAttribute(commit_kernel<L, MAXE, ZERO, MIS, CLIP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            (int)smem_bytes<L, MIS>());
   if (e != cudaSuccess) return (int)e;
   if (APC_SMEM_CARVEOUT >= 0) {
-    e = cudaFuncSetAttribute(commit_kernel<L, MAXE, ZERO, MIS>, cudaFuncAttributePreferredSharedMemoryCarveout,
+    e = cudaFuncSetAttribute(commit_kernel<L, MAXE, ZERO, MIS, CLIP>, cudaFuncAttributePreferredSharedMemoryCarveout,
                              APC_SMEM_CARVEOUT);
     if (e != cudaSuccess) return (int)e;
   }
@@ -686,31 +689,37 @@ int ensure_smem_attribute() {
   return 0;
 }
 
-template <class L, int MAXE, bool ZERO, bool MIS>
+template <class L, int MAXE, bool ZERO, bool MIS, bool CLIP>
 int launch_t(const CommitPlan<MAXE> &plan, unsigned grid, void *stream, unsigned long long *out) {
-  int e = ensure_smem_attribute<L, MAXE, ZERO, MIS>();
+  int e = ensure_smem_attribute<L, MAXE, ZERO, MIS, CLIP>();
   if (e) return e;
-  return launch_plan(commit_kernel<L, MAXE, ZERO, MIS>, plan, plan.chained, grid, L::kThreads, smem_bytes<L, MIS>(),
+  return launch_plan(commit_kernel<L, MAXE, ZERO, MIS, CLIP>, plan, plan.chained, grid, L::kThreads, smem_bytes<L, MIS>(),
                      stream, out);
+}
+
+template <class L, int MAXE, bool CLIP>
+int launch_c(const CommitPlan<MAXE> &plan, bool zero_grad, unsigned grid, void *stream, unsigned long long *out) {
+  bool mis = false;
+  for (uint32_t k = 0; k < plan.count; ++k) mis |= plan.e[k].mis != 0;
+  if (mis)
+    return zero_grad ? launch_t<L, MAXE, true, true, CLIP>(plan, grid, stream, out)
+                     : launch_t<L, MAXE, false, true, CLIP>(plan, grid, stream, out);
+  return zero_grad ? launch_t<L, MAXE, true, false, CLIP>(plan, grid, stream, out)
+                   : launch_t<L, MAXE, false, false, CLIP>(plan, grid, stream, out);
 }
 
 template <class L, int MAXE>
 int launch_l(const CommitPlan<MAXE> &plan, bool zero_grad, unsigned grid, void *stream, unsigned long long *out) {
-  bool mis = false;
-  for (uint32_t k = 0; k < plan.count; ++k) mis |= plan.e[k].mis != 0;
-  if (mis)
-    return zero_grad ? launch_t<L, MAXE, true, true>(plan, grid, stream, out)
-                     : launch_t<L, MAXE, false, true>(plan, grid, stream, out);
-  return zero_grad ? launch_t<L, MAXE, true, false>(plan, grid, stream, out)
-                   : launch_t<L, MAXE, false, false>(plan, grid, stream, out);
+  return plan.clip_norm ? launch_c<L, MAXE, true>(plan, zero_grad, grid, stream, out)
+                        : launch_c<L, MAXE, false>(plan, zero_grad, grid, stream, out);
 }
 
 template <class L, int MAXE, bool MIS>
 int blocks_m(int *fewest) {
   int n = 0;
-  int e = ensure_smem_attribute<L, MAXE, false, MIS>();
+  int e = ensure_smem_attribute<L, MAXE, false, MIS, false>();
   if (e) return e;
-  e = (int)cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, commit_kernel<L, MAXE, false, MIS>, L::kThreads,
+  e = (int)cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, commit_kernel<L, MAXE, false, MIS, false>, L::kThreads,
                                                          smem_bytes<L, MIS>());
   if (n < *fewest) *fewest = n;
   return e;

@@ -28,11 +28,18 @@ struct Scalars {
   const uint64_t *pair;  // both lanes of the packed operations' constants (kPair*)
   float limit;           // adamw_group's bound on |m'| + den, negative if its form does not apply
   uint32_t one;          // 1, from the launch parameters (see digest_term)
+  float clip;            // the gradients' factor (CLIP)
 };
 
-// One element: p, m, v updated in place, returns the bf16 bits of p'.
+// The factor of gradients whose norm is not to exceed `max`: 0 for an infinite
+// norm, NaN for a NaN.
+__device__ __forceinline__ float clip_factor(float norm, float max) { return norm <= max ? 1.0f : __fdiv_rn(max, norm); }
+
+// One element: p, m, v updated in place, returns the bf16 bits of p'.  With CLIP
+// the gradient is multiplied by the factor first, one rounding more.
+template <bool CLIP = false>
 __device__ __forceinline__ uint32_t adamw_element(float &p, float &m, float &v, uint32_t g16, const Scalars &s) {
-  const float g = __uint_as_float(g16 << 16);
+  const float g0 = __uint_as_float(g16 << 16), g = CLIP ? __fmul_rn(g0, s.clip) : g0;
   const float t1 = __fmul_rn(s.h[0], m);
   const float t2 = __fmul_rn(s.h[1], g);
   const float mn = __fadd_rn(t1, t2);
@@ -130,13 +137,14 @@ __device__ __forceinline__ float rcp_approx(float x) {
 // 648; of bf16 state 510 (704, 638), 510 (808, 741) and 493.  In a group that is
 // left (infinities, NaNs, negative or huge moments, p and a nonzero m' both
 // tiny) all elements take the general operations.
-template <int N>
+template <int N, bool CLIP = false>
 __device__ __forceinline__ void adamw_group(float (&p)[N], float (&m)[N], float (&v)[N], const uint32_t (&g16)[N],
                                             const Scalars &s) {
   float t6[N], t7[N], high = 0.0f, low = 0.0f;
 #pragma unroll
   for (int j = 0; j < N; j += 2) {
-    const uint64_t g = pack2(__uint_as_float(g16[j] << 16), __uint_as_float(g16[j + 1] << 16));
+    const uint64_t g0 = pack2(__uint_as_float(g16[j] << 16), __uint_as_float(g16[j + 1] << 16));
+    const uint64_t g = CLIP ? mul2(g0, pack2(s.clip, s.clip)) : g0;
     const uint64_t t1 = mul2(s.pair[kPairB1], pack2(m[j], m[j + 1]));
     const uint64_t t2 = mul2(s.pair[kPair1B1], g);
     const uint64_t t3 = mul2(s.pair[kPairB2], pack2(v[j], v[j + 1]));

@@ -75,8 +75,9 @@ apc_status resolve(const apc_adamw_hparams *hp, int64_t step, float out[8]) {
 uint64_t ceil_div(uint64_t a, uint64_t b) { return a / b + (a % b != 0); }
 
 // What a range of a call is: one of a table's five buffers, a buffer of a list
-// (kBuffer + its type and slot), an output, or an upload's source or destination.
-enum Kind : uint8_t { kP, kM, kV, kG, kW, kSource, kDest, kOut, kBuffer };
+// (kBuffer + its type and slot), an output, the gradients' norm, a workspace, or an
+// upload's source or destination.
+enum Kind : uint8_t { kP, kM, kV, kG, kW, kSource, kDest, kOut, kNorm, kWork, kBuffer };
 
 // One memory range of a call, [lo, hi), and whether kernels write it; index:
 // its entry in the caller's list.
@@ -283,6 +284,8 @@ apc_status check_device_pointers(const Ordered &ranges, size_t count, const char
       char what[64];
       if (o.kind <= kW) snprintf(what, sizeof what, "table[%d].%s", (int)o.index, names[o.kind]);
       else if (o.kind >= kBuffer) snprintf(what, sizeof what, "bufs[%d].data", (int)o.index);
+      else if (o.kind == kNorm) snprintf(what, sizeof what, "grad_norm");
+      else if (o.kind == kWork) snprintf(what, sizeof what, "workspace");
       else snprintf(what, sizeof what, "%s", out_name);
       st = fail(APC_EINVAL, "%s is not memory of the current device %d (memory type %d, device %d)", what, dev,
                 (int)a.type, a.device);
@@ -365,13 +368,21 @@ void commit_scalars(const float h[8], apc::CommitPlan<MAXE> *plan) {
   plan->limit = fits ? std::min(0x1p30f, h[4] * 0x1p62f) : -1.0f;
 }
 
+// Gradients are scaled by max / *norm where *norm (on the device) exceeds max; norm null: not.
+struct Clip {
+  const float *norm = nullptr;
+  float max = 0.0f;
+};
+
 // Entries arrive without tile_begin; each batch places their tiles.
 template <int MAXE, typename Launch>
-apc_status run_commit_batches(const std::vector<apc::CommitEntry> &entries, const float h[8], int layout,
+apc_status run_commit_batches(const std::vector<apc::CommitEntry> &entries, const float h[8], Clip clip, int layout,
                               bool zero_grad, Grid grid_max, void *stream, unsigned long long *out,
                               Launch launch) {
   std::unique_ptr<apc::CommitPlan<MAXE>> plan(new apc::CommitPlan<MAXE>);  // not cleared: the kernel reads what is filled
   commit_scalars(h, plan.get());
+  plan->clip_norm = clip.norm;
+  plan->clip_max = clip.max;
   plan->one = 1;
   const bool chain = grid_max.whole && entries.size() > (size_t)MAXE;
   std::unique_lock<std::mutex> lock;
@@ -428,6 +439,7 @@ apc_status run_digest_batches(const std::vector<apc::DigestEntry> &entries, Grid
     plan->tiles32 = tiles32;
     plan->more = chain && i + k < entries.size();
     plan->chained = chain && i > 0;
+    plan->last = i + k == entries.size();
     const unsigned grid = (unsigned)std::max<uint64_t>(1, std::min<uint64_t>(std::max<uint64_t>(tiles, k), grid_max.cap));
     int e = launch(*plan, grid);
     if (e) return cuda_fail(e, what);
@@ -457,7 +469,7 @@ struct TableRow {
 // Shared by both layouts: validation, scalar resolution, overlap check,
 // planning and launches.  nslots digests are zeroed and accumulated.
 apc_status commit_common(int layout, const std::vector<TableRow> &rows, const apc_adamw_hparams *hp, int64_t step,
-                         uint32_t flags, apc_stream_t stream, uint64_t *out_digests, int nslots) {
+                         uint32_t flags, Clip clip, apc_stream_t stream, uint64_t *out_digests, int nslots) {
   if (flags & ~(uint32_t)APC_COMMIT_ZERO_GRAD) return fail(APC_EINVAL, "unknown flag bits 0x%x", flags);
   const bool zero_grad = (flags & APC_COMMIT_ZERO_GRAD) != 0;
   if (!out_digests) return fail(APC_EINVAL, "out_digests pointer is null");
@@ -506,7 +518,7 @@ apc_status commit_common(int layout, const std::vector<TableRow> &rows, const ap
     entries.push_back(e);
   }
   std::vector<Range> ranges;
-  ranges.reserve(entries.size() * 5 + 1);
+  ranges.reserve(entries.size() * 5 + 2);
   const auto add = [&](Kind kind, uint64_t size, bool written, const auto &at) {
     for (size_t k = 0; k < rows.size(); ++k) {
       const uintptr_t lo = (uintptr_t)at(rows[k]);
@@ -518,11 +530,12 @@ apc_status commit_common(int layout, const std::vector<TableRow> &rows, const ap
   add(kV, es, true, [](const TableRow &t) { return t.v; });
   add(kG, 2, zero_grad, [](const TableRow &t) { return t.g; });
   add(kW, 2, true, [](const TableRow &t) { return t.w; });  // null in the bf16 layout
-  const uintptr_t o = (uintptr_t)out_digests;
+  const uintptr_t o = (uintptr_t)out_digests, cn = (uintptr_t)clip.norm;
   ranges.push_back({o, o + (uintptr_t)nslots * sizeof(uint64_t), -1, kOut, true});
+  if (cn) ranges.push_back({cn, cn + sizeof(float), -1, kNorm, false});
   const Ordered ordered(ranges);
   if (overlaps(ordered))
-    return fail(APC_EINVAL, "table buffers or out_digests overlap (a written range meets another range)");
+    return fail(APC_EINVAL, "table buffers, out_digests or the norm overlap (a written range meets another range)");
   if ((st = check_device_pointers(ordered, ranges.size(), "out_digests")) != APC_OK) return st;
 
   unsigned long long *out = reinterpret_cast<unsigned long long *>(out_digests);
@@ -533,9 +546,45 @@ apc_status commit_common(int layout, const std::vector<TableRow> &rows, const ap
   if (entries.empty()) return APC_OK;
   const Grid grid_max = grid_for(d.sms, d.commit);
   return with_plan<apc::kCommitSmall, apc::kCommitMid, apc::kCommitLarge>(entries.size(), [&](auto size) {
-    return run_commit_batches<size.value>(entries, h, layout, zero_grad, grid_max, stream, out,
+    return run_commit_batches<size.value>(entries, h, clip, layout, zero_grad, grid_max, stream, out,
                                           apc::launch_commit<size.value>);
   });
+}
+
+}  // namespace
+
+namespace {
+
+apc_status commit_f32(const apc_tensor *table, int32_t num_tensors, const apc_adamw_hparams *hp, int64_t step, uint32_t flags,
+                      Clip clip, apc_stream_t stream, uint64_t *out_digests) {
+  if (num_tensors < 0) return fail(APC_EINVAL, "num_tensors %d < 0", num_tensors);
+  if (num_tensors > 0 && !table) return fail(APC_EINVAL, "table pointer is null");
+  std::vector<TableRow> rows((size_t)num_tensors);
+  for (int32_t k = 0; k < num_tensors; ++k)
+    rows[k] = TableRow{table[k].p, table[k].m, table[k].v, table[k].g, table[k].w, table[k].n,
+                       table[k].global_offset};
+  return commit_common(apc::kLayoutF32, rows, hp, step, flags, clip, stream, out_digests, 4);
+}
+
+apc_status commit_bf16(const apc_tensor_bf16 *table, int32_t num_tensors, const apc_adamw_hparams *hp, int64_t step,
+                       uint32_t flags, Clip clip, apc_stream_t stream, uint64_t *out_digests) {
+  if (num_tensors < 0) return fail(APC_EINVAL, "num_tensors %d < 0", num_tensors);
+  if (num_tensors > 0 && !table) return fail(APC_EINVAL, "table pointer is null");
+  std::vector<TableRow> rows((size_t)num_tensors);
+  for (int32_t k = 0; k < num_tensors; ++k)
+    rows[k] = TableRow{table[k].p, table[k].m, table[k].v, table[k].g, nullptr, table[k].n,
+                       table[k].global_offset};
+  return commit_common(apc::kLayoutBF16, rows, hp, step, flags, clip, stream, out_digests, 3);
+}
+
+apc_status clip_of(const float *grad_norm, double max_norm, Clip *clip) {
+  if (!grad_norm) return fail(APC_EINVAL, "grad_norm pointer is null");
+  if ((uintptr_t)grad_norm % 4) return fail(APC_EALIGN, "grad_norm not 4-byte aligned");
+  if (!((float)max_norm > 0.0f) || !std::isfinite((float)max_norm))
+    return fail(APC_EINVAL, "max_norm %g is not a positive finite binary32 number", max_norm);
+  clip->norm = grad_norm;
+  clip->max = (float)max_norm;
+  return APC_OK;
 }
 
 }  // namespace
@@ -544,13 +593,7 @@ APC_EXPORT apc_status apc_commit_step_ex(const apc_tensor *table, int32_t num_te
                                          const apc_adamw_hparams *hp, int64_t step, uint32_t flags,
                                          apc_stream_t stream, uint64_t *out_digests) {
   g_last_error[0] = 0;
-  if (num_tensors < 0) return fail(APC_EINVAL, "num_tensors %d < 0", num_tensors);
-  if (num_tensors > 0 && !table) return fail(APC_EINVAL, "table pointer is null");
-  std::vector<TableRow> rows((size_t)num_tensors);
-  for (int32_t k = 0; k < num_tensors; ++k)
-    rows[k] = TableRow{table[k].p, table[k].m, table[k].v, table[k].g, table[k].w, table[k].n,
-                       table[k].global_offset};
-  return commit_common(apc::kLayoutF32, rows, hp, step, flags, stream, out_digests, 4);
+  return commit_f32(table, num_tensors, hp, step, flags, Clip(), stream, out_digests);
 }
 
 APC_EXPORT apc_status apc_commit_step(const apc_tensor *table, int32_t num_tensors, const apc_adamw_hparams *hp,
@@ -558,17 +601,30 @@ APC_EXPORT apc_status apc_commit_step(const apc_tensor *table, int32_t num_tenso
   return apc_commit_step_ex(table, num_tensors, hp, step, 0u, stream, out_digests);
 }
 
+APC_EXPORT apc_status apc_commit_step_clipped(const apc_tensor *table, int32_t num_tensors, const apc_adamw_hparams *hp,
+                                              int64_t step, uint32_t flags, const float *grad_norm, double max_norm,
+                                              apc_stream_t stream, uint64_t *out_digests) {
+  g_last_error[0] = 0;
+  Clip clip;
+  const apc_status st = clip_of(grad_norm, max_norm, &clip);
+  return st != APC_OK ? st : commit_f32(table, num_tensors, hp, step, flags, clip, stream, out_digests);
+}
+
 APC_EXPORT apc_status apc_commit_step_bf16(const apc_tensor_bf16 *table, int32_t num_tensors,
                                            const apc_adamw_hparams *hp, int64_t step, uint32_t flags,
                                            apc_stream_t stream, uint64_t *out_digests) {
   g_last_error[0] = 0;
-  if (num_tensors < 0) return fail(APC_EINVAL, "num_tensors %d < 0", num_tensors);
-  if (num_tensors > 0 && !table) return fail(APC_EINVAL, "table pointer is null");
-  std::vector<TableRow> rows((size_t)num_tensors);
-  for (int32_t k = 0; k < num_tensors; ++k)
-    rows[k] = TableRow{table[k].p, table[k].m, table[k].v, table[k].g, nullptr, table[k].n,
-                       table[k].global_offset};
-  return commit_common(apc::kLayoutBF16, rows, hp, step, flags, stream, out_digests, 3);
+  return commit_bf16(table, num_tensors, hp, step, flags, Clip(), stream, out_digests);
+}
+
+APC_EXPORT apc_status apc_commit_step_bf16_clipped(const apc_tensor_bf16 *table, int32_t num_tensors,
+                                                   const apc_adamw_hparams *hp, int64_t step, uint32_t flags,
+                                                   const float *grad_norm, double max_norm, apc_stream_t stream,
+                                                   uint64_t *out_digests) {
+  g_last_error[0] = 0;
+  Clip clip;
+  const apc_status st = clip_of(grad_norm, max_norm, &clip);
+  return st != APC_OK ? st : commit_bf16(table, num_tensors, hp, step, flags, clip, stream, out_digests);
 }
 
 namespace {
@@ -578,26 +634,28 @@ namespace {
 // depend on the order): the digest kernel shares out each type's tiles on
 // their own, and a warp's walk over the plan seldom meets another slot and
 // flushes its running sum.
-apc_status buffer_entries(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots, uint64_t *out,
-                          std::vector<apc::DigestEntry> *entries) {
+// out: num_slots elements of out_size bytes; work: null, or a workspace.
+apc_status buffer_entries(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots, void *out, uint32_t out_size,
+                          uint32_t types, const void *work, uint64_t work_bytes, std::vector<apc::DigestEntry> *entries) {
   if (num_bufs < 0) return fail(APC_EINVAL, "num_bufs %d < 0", num_bufs);
   if (num_bufs > 0 && !bufs) return fail(APC_EINVAL, "bufs pointer is null");
   if (num_slots < 1 || num_slots > APC_MAX_SLOTS)
     return fail(APC_EINVAL, "num_slots %d outside 1..%d", num_slots, APC_MAX_SLOTS);
   if (!out) return fail(APC_EINVAL, "output pointer is null");
-  if ((uintptr_t)out % 8) return fail(APC_EALIGN, "output not 8-byte aligned");
+  if ((uintptr_t)out % out_size) return fail(APC_EALIGN, "output not %u-byte aligned", out_size);
   std::vector<Range> ranges;
-  size_t at[2 * APC_MAX_SLOTS + 1] = {0};  // first entry of each (type, slot), then the next one to place
+  constexpr int kGroups = 3 * APC_MAX_SLOTS;
+  size_t at[kGroups + 1] = {0};  // first entry of each (type, slot), then the next one to place
   for (int32_t k = 0; k < num_bufs; ++k) {
     const apc_buffer &b = bufs[k];
-    if (b.n && b.dtype <= APC_BF16 && b.slot < APC_MAX_SLOTS) ++at[b.dtype * APC_MAX_SLOTS + b.slot + 1];
+    if (b.n && b.dtype < types && b.slot < APC_MAX_SLOTS) ++at[b.dtype * APC_MAX_SLOTS + b.slot + 1];
   }
-  for (int g = 0; g < 2 * APC_MAX_SLOTS; ++g) at[g + 1] += at[g];
-  entries->resize(at[2 * APC_MAX_SLOTS]);
-  ranges.resize(at[2 * APC_MAX_SLOTS] + 1);  // by type and slot like the entries
+  for (int g = 0; g < kGroups; ++g) at[g + 1] += at[g];
+  entries->resize(at[kGroups]);
+  ranges.resize(at[kGroups] + (work ? 2 : 1));  // by type and slot like the entries
   for (int32_t k = 0; k < num_bufs; ++k) {
     const apc_buffer &b = bufs[k];
-    if (b.dtype != APC_F32 && b.dtype != APC_BF16) return fail(APC_EINVAL, "bufs[%d]: unknown dtype %u", k, b.dtype);
+    if (b.dtype >= types) return fail(APC_EINVAL, "bufs[%d]: unknown dtype %u", k, b.dtype);
     if (b.slot >= (uint32_t)num_slots) return fail(APC_EINVAL, "bufs[%d]: slot %u >= num_slots", k, b.slot);
     if (b.n == 0) continue;
     if (!b.data) return fail(APC_EINVAL, "bufs[%d]: null data pointer", k);
@@ -620,9 +678,10 @@ apc_status buffer_entries(const apc_buffer *bufs, int32_t num_bufs, int32_t num_
     ranges[place] = {a, a + es * b.n, k, (uint8_t)(kBuffer + b.dtype * APC_MAX_SLOTS + b.slot), false};
   }
   const uintptr_t o = (uintptr_t)out;
-  ranges.back() = {o, o + (uintptr_t)num_slots * sizeof(uint64_t), -1, kOut, true};
+  ranges.back() = {o, o + (uintptr_t)num_slots * out_size, -1, kOut, true};
+  if (work) ranges[ranges.size() - 2] = {(uintptr_t)work, (uintptr_t)work + work_bytes, -1, kWork, true};
   const Ordered ordered(ranges);
-  if (overlaps(ordered)) return fail(APC_EINVAL, "the output overlaps a buffer of the list");
+  if (overlaps(ordered)) return fail(APC_EINVAL, "the output%s overlaps a buffer of the list", work ? " or the workspace" : "");
   return check_device_pointers(ordered, ranges.size(), "output");
 }
 
@@ -632,7 +691,7 @@ APC_EXPORT apc_status apc_digest(const apc_buffer *bufs, int32_t num_bufs, int32
                                  uint64_t *out_digests) {
   g_last_error[0] = 0;
   std::vector<apc::DigestEntry> entries;
-  apc_status st = buffer_entries(bufs, num_bufs, num_slots, out_digests, &entries);
+  apc_status st = buffer_entries(bufs, num_bufs, num_slots, out_digests, 8, 2, nullptr, 0, &entries);
   if (st != APC_OK) return st;
   unsigned long long *out = reinterpret_cast<unsigned long long *>(out_digests);
   Device d;
@@ -660,7 +719,7 @@ APC_EXPORT apc_status apc_count_nonzero(const apc_buffer *bufs, int32_t num_bufs
                                         apc_stream_t stream, uint64_t *out_counts) {
   g_last_error[0] = 0;
   std::vector<apc::DigestEntry> entries;
-  apc_status st = buffer_entries(bufs, num_bufs, num_slots, out_counts, &entries);
+  apc_status st = buffer_entries(bufs, num_bufs, num_slots, out_counts, 8, 2, nullptr, 0, &entries);
   if (st != APC_OK) return st;
   Device d;
   if (!entries.empty() && (st = device_info(&d)) != APC_OK) return st;
@@ -855,6 +914,36 @@ apc_status op_grid(int per_sm, unsigned *cap, unsigned *sms) {
   *cap = grid_for(d.sms, per_sm).cap;
   if (sms) *sms = (unsigned)d.sms;
   return st;
+}
+
+// The norm kernel's tiles begin at a buffer's first element; the last one may be short.
+apc_status grad_norm(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots, void *work, apc_stream_t stream, float *out,
+                     NormLaunch launch) {
+  if (!work) return fail(APC_EINVAL, "workspace pointer is null");
+  if ((uintptr_t)work % 8) return fail(APC_EALIGN, "workspace not 8-byte aligned");
+  std::vector<DigestEntry> entries;
+  apc_status st = buffer_entries(bufs, num_bufs, num_slots, out, 4, 3, work, APC_GRAD_NORM_WORKSPACE, &entries);
+  if (st != APC_OK) return st;
+  Device d;
+  if (!entries.empty() && (st = device_info(&d)) != APC_OK) return st;
+  if (entries.empty()) {
+    const int e = (int)cudaMemsetAsync(out, 0, (size_t)num_slots * sizeof(float), (cudaStream_t)stream);
+    return e ? cuda_fail(e, "cudaMemsetAsync(out_norms)") : APC_OK;
+  }
+  const int e = (int)cudaMemsetAsync(work, 0, (1 + (size_t)num_slots * kNormWords) * 8, (cudaStream_t)stream);
+  if (e) return cuda_fail(e, "cudaMemsetAsync(workspace)");
+  for (DigestEntry &en : entries) {
+    en.head = 0;
+    en.tile_begin = en.n;
+  }
+  return with_plan<kDigestSmall, kDigestMid, kDigestLarge>(entries.size(), [&](auto size) {
+    return run_digest_batches<size.value>(
+        entries, grid_for(d.sms, 1), stream, [](uint64_t n, uint64_t es) { return ceil_div(n * es, kNormTileBytes); },
+        [&](const auto &plan, unsigned grid) {
+          return launch(&plan, size.value, grid, stream, static_cast<unsigned long long *>(work), out, (unsigned)num_slots);
+        },
+        "norm kernel launch");
+  });
 }
 
 }  // namespace apc

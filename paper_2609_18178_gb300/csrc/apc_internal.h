@@ -126,7 +126,8 @@ struct CommitPlan {
   float h[8];            // b1, 1-b1, b2, 1-b2, eps, 1-lr*wd, lr/bc1, 1/sqrt(bc2)
   uint64_t pair[kPairs];
   float limit;           // adamw_group's bound, -1 where its form does not apply
-  uint32_t pad_;
+  float clip_max;        // the largest norm allowed
+  const float *clip_norm;  // the gradients' norm, on the device; null: no clipping
   uint64_t total_tiles;
   uint32_t count;
   uint32_t one;          // 1: the FMA-pipe carry-add multiplier of the digest
@@ -178,6 +179,20 @@ constexpr uint64_t digest_tile(int u) { return (uint64_t)32 * kVec * u; }  // el
 constexpr int kCountThreads = APC_COUNT_THREADS;
 constexpr int kCountGroups = APC_COUNT_GROUPS;                   // 16-byte loads per lane per tile
 constexpr uint32_t kCountTileBytes = 32 * 16 * kCountGroups;     // one warp's tile
+
+// Norm kernel (apc_gradnorm.cu): the count kernel's walk with tiles that are
+// counted from a buffer's first element, whatever its alignment.
+#ifndef APC_NORM_THREADS
+#define APC_NORM_THREADS 1024
+#endif
+#ifndef APC_NORM_GROUPS
+#define APC_NORM_GROUPS 6
+#endif
+constexpr int kNormThreads = APC_NORM_THREADS;
+constexpr int kNormGroups = APC_NORM_GROUPS;                  // 16-byte chunks per lane per tile
+constexpr uint32_t kNormTileBytes = 32 * 16 * kNormGroups;    // one warp's tile
+constexpr int kNormWords = 32;  // 64-bit words of a slot in the workspace, behind one of all slots
+
 // Minimum resident CTAs per SM the digest kernel is compiled for (its
 // register cap: 65,536 / (threads x this)), and extra dynamic shared memory
 // per CTA beyond its stages (0 by default; a larger CTA footprint keeps two
@@ -193,14 +208,15 @@ constexpr uint32_t kCountTileBytes = 32 * 16 * kCountGroups;     // one warp's t
 //   head: scalar elements before the first 16-byte boundary (<= 7); then
 //         8-element vectors, the whole tiles of which (digest_tile(U) elements
 //         for the digest kernel, kCountTileBytes for the count kernel) are
-//         counted in tile_begin; then a scalar tail.
+//         counted in tile_begin; then a scalar tail.  The norm kernel's tiles
+//         begin at the first element and the last one may be short.
 struct DigestEntry {
   const void *data;
   uint64_t n;
   uint64_t tile_begin;
   uint32_t key_base;
   uint8_t head;
-  uint8_t dtype;        // 0 fp32, 1 bf16
+  uint8_t dtype;        // 0 fp32, 1 bf16, 2 fp16 (norm kernel)
   uint8_t slot;
   uint8_t pad_;
 };
@@ -213,7 +229,7 @@ struct DigestPlan {
   uint32_t one;          // 1: the FMA-pipe carry-add multiplier of the digest
   uint16_t more;         // another launch of the same call follows, chained to this one
   uint16_t chained;      // this one is chained to another of the same call before it
-  uint32_t pad_;
+  uint32_t last;         // the call's last launch
   DigestEntry e[MAXE];
 };
 

@@ -33,6 +33,14 @@ apc_status op_ranges(const OpRange *r, int n);
 // apc_set_reserved_sms and APC_GRID_LIMIT.
 apc_status op_grid(int per_sm, unsigned *cap, unsigned *sms = nullptr);
 
+// ---- the gradients' norm: planned by apc_host.cpp like the other buffer lists,
+// launched by apc_gradnorm.cu.  plan: a DigestPlan of so many entries.
+typedef int (*NormLaunch)(const void *plan, int size, unsigned grid, void *stream, unsigned long long *work, float *out,
+                          unsigned slots);
+int launch_norm(const void *plan, int size, unsigned grid, void *stream, unsigned long long *work, float *out, unsigned slots);
+apc_status grad_norm(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots, void *work, apc_stream_t stream, float *out,
+                     NormLaunch launch);
+
 constexpr int kBlock = 128;  // columns (and, in square blocks, rows) that share a scale
 
 // ---- quantization
@@ -54,6 +62,34 @@ struct QuantArgs {
 
 int launch_quantize(const QuantArgs &a, unsigned cap, void *stream);
 int quantize_per_sm(const QuantArgs &a);
+
+// ---- root-mean-square norm
+struct NormArgs {
+  const void *x, *residual, *weight;  // residual null: none, and no sum
+  void *sum;
+  void *out;        // null: y in 8 bits
+  QuantOut q, qt;   // qt.data null: no transpose
+  float *rstd;
+  int64_t pitch, residual_pitch, sum_pitch, out_pitch;
+  uint32_t rows, cols, dtype, wdtype;
+  double eps;
+};
+
+int launch_rms_norm(const NormArgs &a, unsigned sms, void *stream);
+
+struct NormGradArgs {
+  const void *dout, *x, *weight, *dresidual;  // dresidual null: none
+  const float *rstd;
+  void *dx;
+  void *dweight;    // null: not wanted
+  float *work;      // rms_norm_parts(rows, cols) x cols
+  int64_t dout_pitch, pitch, dresidual_pitch, dx_pitch;
+  uint32_t rows, cols, dtype, wdtype, dwdtype;
+};
+
+// Runs of rows whose sums of the weight's gradient are kept apart.
+uint32_t rms_norm_parts(uint32_t rows, uint32_t cols);
+int launch_rms_norm_grad(const NormGradArgs &a, void *stream);
 
 // ---- product
 struct MatmulArgs {

@@ -108,6 +108,163 @@ APC_EXPORT apc_status apc_quantize_fp8(const void *x, int64_t rows, int64_t cols
   return e ? apc::op_cuda_fail(e, "quantize kernel launch") : APC_OK;
 }
 
+namespace {
+
+// Sizes, types and inputs of a norm, and its sum.
+apc_status check_norm(const apc_norm *d, Ranges *rs, apc::NormArgs *a) {
+  apc_status st;
+  if (!d) return op_fail(APC_EINVAL, "descriptor pointer is null");
+  if ((st = check_size("rows", d->rows)) != APC_OK || (st = check_size("cols", d->cols)) != APC_OK) return st;
+  if (d->dtype > APC_F16 || d->weight_dtype > APC_F16)
+    return op_fail(APC_EINVAL, "unknown dtype %u or weight_dtype %u", d->dtype, d->weight_dtype);
+  if (!((float)d->eps >= 1e-20f) || !std::isfinite((float)d->eps))
+    return op_fail(APC_EINVAL, "eps %g is not a binary32 number from 1e-20 on", d->eps);
+  const int64_t es = size_of(d->dtype), ws = size_of(d->weight_dtype), r = d->rows, c = d->cols;
+  const bool adds = d->residual != nullptr;
+  if (d->sum && !adds) return op_fail(APC_EINVAL, "sum without a residual");
+  if ((st = check_matrix("x", d->x, r, c, d->pitch, es)) != APC_OK) return st;
+  if (adds && (st = check_matrix("residual", d->residual, r, c, d->residual_pitch, es)) != APC_OK) return st;
+  if (adds && (st = check_matrix("sum", d->sum, r, c, d->sum_pitch, es)) != APC_OK) return st;
+  if ((st = check_matrix("weight", d->weight, r ? 1 : 0, c, c, ws)) != APC_OK) return st;
+  // the sum may take the place of either of its terms
+  const auto place = [&](const void *p, int64_t pitch) { return adds && p == d->sum && (pitch == d->sum_pitch || r <= 1); };
+  if (!place(d->x, d->pitch)) rs->add("x", d->x, r, c * es, d->pitch * es, false);
+  if (adds && !place(d->residual, d->residual_pitch))
+    rs->add("residual", d->residual, r, c * es, d->residual_pitch * es, false);
+  if (adds) rs->add("sum", d->sum, r, c * es, d->sum_pitch * es, true);
+  rs->add("weight", d->weight, r ? 1 : 0, c * ws, 0, false);
+  a->x = d->x;
+  a->residual = d->residual;
+  a->weight = d->weight;
+  a->sum = d->sum;
+  a->pitch = pitch_of(r, c, d->pitch);
+  a->residual_pitch = pitch_of(r, c, d->residual_pitch);
+  a->sum_pitch = pitch_of(r, c, d->sum_pitch);
+  a->rows = (uint32_t)r;
+  a->cols = (uint32_t)c;
+  a->dtype = d->dtype;
+  a->wdtype = d->weight_dtype;
+  a->eps = d->eps;
+  return APC_OK;
+}
+
+apc_status run_norm(const apc::NormArgs &a, const Ranges &rs, apc_stream_t stream) {
+  apc_status st = apc::op_ranges(rs.r, rs.n);
+  unsigned cap = 0, sms = 0;
+  if (st != APC_OK || (st = apc::op_grid(1, &cap, &sms)) != APC_OK) return st;
+  const int e = apc::launch_rms_norm(a, sms, stream);
+  return e ? apc::op_cuda_fail(e, "norm kernel launch") : APC_OK;
+}
+
+apc_status check_rstd(const float *rstd, int64_t rows, int64_t cols, bool written, Ranges *rs) {
+  const apc_status st = check_matrix("rstd", rstd, cols ? 1 : 0, rows, rows, 4);
+  if (st == APC_OK) rs->add("rstd", rstd, cols ? 1 : 0, rows * 4, 0, written);
+  return st;
+}
+
+}  // namespace
+
+APC_EXPORT apc_status apc_rms_norm(const apc_norm *d, void *out, int64_t out_pitch, float *rstd, apc_stream_t stream) {
+  apc::op_begin();
+  Ranges rs;
+  apc::NormArgs a = {};
+  apc_status st = check_norm(d, &rs, &a);
+  if (st != APC_OK) return st;
+  const int64_t es = size_of(d->dtype);
+  if ((st = check_matrix("out", out, d->rows, d->cols, out_pitch, es)) != APC_OK) return st;
+  rs.add("out", out, d->rows, d->cols * es, out_pitch * es, true);
+  if ((st = check_rstd(rstd, d->rows, d->cols, true, &rs)) != APC_OK) return st;
+  if (d->rows == 0 || d->cols == 0) return APC_OK;
+  a.out = out;
+  a.out_pitch = pitch_of(d->rows, d->cols, out_pitch);
+  a.rstd = rstd;
+  return run_norm(a, rs, stream);
+}
+
+APC_EXPORT apc_status apc_rms_norm_fp8(const apc_norm *d, const apc_fp8_matrix *q, const apc_fp8_matrix *qt, float *rstd,
+                                       apc_stream_t stream) {
+  apc::op_begin();
+  Ranges rs;
+  apc::NormArgs a = {};
+  apc_status st = check_norm(d, &rs, &a);
+  if (st != APC_OK) return st;
+  if ((st = check_fp8("q", q, d->rows, d->cols, true, &rs)) != APC_OK) return st;
+  if (q->block_rows != 1) return op_fail(APC_EINVAL, "q: block_rows %u is not 1", q->block_rows);
+  if (qt) {
+    if ((st = check_fp8("qt", qt, d->cols, d->rows, true, &rs)) != APC_OK) return st;
+    if (qt->block_rows != 1 || qt->format != q->format)
+      return op_fail(APC_EINVAL, "qt: block_rows %u is not 1 or its format (%u) is not q's (%u)", qt->block_rows, qt->format, q->format);
+  }
+  if ((st = check_rstd(rstd, d->rows, d->cols, true, &rs)) != APC_OK) return st;
+  if (d->rows == 0 || d->cols == 0) return APC_OK;
+  a.q = quant_out(q);
+  if (qt) a.qt = quant_out(qt);
+  a.rstd = rstd;
+  return run_norm(a, rs, stream);
+}
+
+APC_EXPORT int64_t apc_rms_norm_grad_workspace(int64_t rows, int64_t cols) {
+  if (rows < 0 || cols < 0 || rows > kMaxSize || cols > kMaxSize) return 0;
+  return (int64_t)apc::rms_norm_parts((uint32_t)rows, (uint32_t)cols) * cols * 4;
+}
+
+APC_EXPORT apc_status apc_rms_norm_grad(const apc_norm_grad *d, void *dx, int64_t dx_pitch, void *dweight, uint32_t dweight_dtype,
+                                        float *workspace, apc_stream_t stream) {
+  apc::op_begin();
+  apc_status st;
+  if (!d) return op_fail(APC_EINVAL, "descriptor pointer is null");
+  if ((st = check_size("rows", d->rows)) != APC_OK || (st = check_size("cols", d->cols)) != APC_OK) return st;
+  if (d->dtype > APC_F16 || d->weight_dtype > APC_F16 || (dweight && dweight_dtype > APC_F16))
+    return op_fail(APC_EINVAL, "unknown dtype %u, weight_dtype %u or dweight_dtype %u", d->dtype, d->weight_dtype, dweight_dtype);
+  const int64_t es = size_of(d->dtype), ws = size_of(d->weight_dtype), r = d->rows, c = d->cols;
+  Ranges rs;
+  // dx may take the place of dout or of dresidual
+  const auto place = [&](const void *p, int64_t pitch) { return p == dx && (pitch == dx_pitch || r <= 1); };
+  if ((st = check_matrix("dout", d->dout, r, c, d->dout_pitch, es)) != APC_OK) return st;
+  if (!place(d->dout, d->dout_pitch)) rs.add("dout", d->dout, r, c * es, d->dout_pitch * es, false);
+  if ((st = check_matrix("x", d->x, r, c, d->pitch, es)) != APC_OK) return st;
+  rs.add("x", d->x, r, c * es, d->pitch * es, false);
+  if (d->dresidual) {
+    if ((st = check_matrix("dresidual", d->dresidual, r, c, d->dresidual_pitch, es)) != APC_OK) return st;
+    if (!place(d->dresidual, d->dresidual_pitch)) rs.add("dresidual", d->dresidual, r, c * es, d->dresidual_pitch * es, false);
+  }
+  if ((st = check_matrix("weight", d->weight, r ? 1 : 0, c, c, ws)) != APC_OK) return st;
+  rs.add("weight", d->weight, r ? 1 : 0, c * ws, 0, false);
+  if ((st = check_rstd(d->rstd, r, c, false, &rs)) != APC_OK) return st;
+  if ((st = check_matrix("dx", dx, r, c, dx_pitch, es)) != APC_OK) return st;
+  rs.add("dx", dx, r, c * es, dx_pitch * es, true);
+  if (dweight) {
+    const int64_t dws = size_of(dweight_dtype), work = apc_rms_norm_grad_workspace(r, c);
+    if ((st = check_matrix("dweight", dweight, 1, c, c, dws)) != APC_OK) return st;
+    rs.add("dweight", dweight, 1, c * dws, 0, true);
+    if ((st = check_matrix("workspace", workspace, 1, work / 4, work / 4, 4)) != APC_OK) return st;
+    rs.add("workspace", workspace, 1, work, 0, true);
+  }
+  if (c == 0 || (r == 0 && !dweight)) return APC_OK;
+  unsigned cap = 0;
+  if ((st = apc::op_ranges(rs.r, rs.n)) != APC_OK || (st = apc::op_grid(1, &cap)) != APC_OK) return st;
+  apc::NormGradArgs a = {};
+  a.dout = d->dout;
+  a.x = d->x;
+  a.weight = d->weight;
+  a.dresidual = d->dresidual;
+  a.rstd = d->rstd;
+  a.dx = dx;
+  a.dweight = dweight;
+  a.work = workspace;
+  a.dout_pitch = pitch_of(r, c, d->dout_pitch);
+  a.pitch = pitch_of(r, c, d->pitch);
+  a.dresidual_pitch = pitch_of(r, c, d->dresidual_pitch);
+  a.dx_pitch = pitch_of(r, c, dx_pitch);
+  a.rows = (uint32_t)r;
+  a.cols = (uint32_t)c;
+  a.dtype = d->dtype;
+  a.wdtype = d->weight_dtype;
+  a.dwdtype = dweight_dtype;
+  const int e = apc::launch_rms_norm_grad(a, stream);
+  return e ? apc::op_cuda_fail(e, "norm gradient kernel launch") : APC_OK;
+}
+
 APC_EXPORT apc_status apc_matmul_fp8(const apc_fp8_matrix *a, const apc_fp8_matrix *b, int64_t m, int64_t n, int64_t k,
                                      void *out, int64_t out_pitch, uint32_t out_dtype, apc_stream_t stream) {
   apc::op_begin();
@@ -146,6 +303,12 @@ APC_EXPORT apc_status apc_matmul_fp8(const apc_fp8_matrix *a, const apc_fp8_matr
   if ((st = apc::op_grid(1, &cap, &sms)) != APC_OK) return st;
   const int e = apc::launch_matmul(p, cap, sms, stream);
   return e ? apc::op_cuda_fail(e, "product kernel launch") : APC_OK;
+}
+
+APC_EXPORT apc_status apc_grad_norm(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots, void *workspace,
+                                    apc_stream_t stream, float *out_norms) {
+  apc::op_begin();
+  return apc::grad_norm(bufs, num_bufs, num_slots, workspace, stream, out_norms, apc::launch_norm);
 }
 
 namespace {

@@ -1,8 +1,10 @@
-"""The operators around a training step's output head (include/apc.h): 8-bit
-quantization with block scales, the product of such operands, and distillation
-from a teacher's top logits.  Argument marshalling only, as in the package's
-other entry points:
+"""The operators around a training step's output head (include/apc.h): the
+root-mean-square norm in front of it with its gradient, 8-bit quantization with
+block scales, the product of such operands, and distillation from a teacher's
+top logits.  Argument marshalling only, as in the package's other entry points:
 
+* :func:`rms_norm`, :func:`rms_norm_fp8`, :func:`rms_norm_grad` ->
+  ``apc_rms_norm``, ``apc_rms_norm_fp8``, ``apc_rms_norm_grad``
 * :func:`quantize_fp8` -> ``apc_quantize_fp8``
 * :func:`matmul_fp8` -> ``apc_matmul_fp8``
 * :func:`distill_loss`, :func:`distill_grad`, :func:`distill_loss_grad` ->
@@ -22,7 +24,7 @@ import ctypes
 
 import torch
 
-__all__ = ["quantize_fp8", "matmul_fp8", "distill_loss", "distill_grad", "distill_loss_grad"]
+__all__ = ["quantize_fp8", "matmul_fp8", "rms_norm", "rms_norm_fp8", "rms_norm_grad", "distill_loss", "distill_grad", "distill_loss_grad"]
 
 BLOCK = 128
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -33,6 +35,18 @@ _INDEX = {torch.int32: 0, torch.int64: 1}
 class _Fp8Matrix(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("pitch", ctypes.c_int64),
                 ("scale_pitch", ctypes.c_int64), ("format", ctypes.c_uint32), ("block_rows", ctypes.c_uint32)]
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "residual", "weight", "sum")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "cols", "pitch", "residual_pitch", "sum_pitch")] + \
+               [("dtype", ctypes.c_uint32), ("weight_dtype", ctypes.c_uint32), ("eps", ctypes.c_double)]
+
+
+class _NormGrad(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dout", "x", "weight", "dresidual", "rstd")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "cols", "dout_pitch", "pitch", "dresidual_pitch")] + \
+               [("dtype", ctypes.c_uint32), ("weight_dtype", ctypes.c_uint32)]
 
 
 class _Distill(ctypes.Structure):
@@ -179,6 +193,133 @@ def quantize_fp8(x, block_rows: int = 1, dtype=torch.float8_e4m3fn, transposed: 
         qt = ctypes.byref(qt)
     _check(lib.apc_quantize_fp8(x.data_ptr(), r, c, pitch, kind, ctypes.byref(q), qt, _stream(stream, device)))
     return tuple(out)
+
+
+def _weight(x, name: str, device: int, n: int) -> int:
+    """Code of the type of a vector of n values (checked as by _vector)."""
+    _vector(x, name, _DTYPE, device, n)
+    return _DTYPE[x.dtype]
+
+
+def _norm(x, weight, eps, residual, sum, rstd, device, stream):
+    """The C structure of a norm, its sum (x itself without a residual) and rstd."""
+    kind, r, c, pitch = _matrix(x, "x", _DTYPE, device)
+    wkind = _weight(weight, "weight", device, c)
+    if rstd is None:
+        rstd = _empty((r,), torch.float32, x, stream)
+    else:
+        _vector(rstd, "rstd", _F32, device, r)
+    if residual is None:
+        if sum is not None:
+            raise ValueError("sum without a residual")
+        return _Norm(x.data_ptr(), None, weight.data_ptr(), None, r, c, pitch, 0, 0, kind, wkind, eps), x, rstd
+    same = {x.dtype: kind}
+    rpitch = _sized(residual, "residual", same, device, r, c)[1]
+    if sum is None:
+        sum = _empty((r, c), x.dtype, x, stream)
+    spitch = _sized(sum, "sum", same, device, r, c)[1]
+    return _Norm(x.data_ptr(), residual.data_ptr(), weight.data_ptr(), sum.data_ptr(), r, c, pitch, rpitch, spitch, kind, wkind,
+                 eps), sum, rstd
+
+
+def rms_norm(x, weight, *, eps=1e-6, residual=None, out=None, sum=None, rstd=None, stream=None):
+    """Enqueue the root-mean-square norm of the rows of ``x`` (``[rows,
+    cols]``, fp32, bf16 or fp16, any row pitch) with ``weight`` (``[cols]``, of
+    any of these types), after the addition of ``residual``.
+
+    Returns ``(out, sum, rstd)``: the normalised rows, ``x + residual`` in its
+    type (``x`` itself without a residual) and 1/rms of its rows (fp32
+    ``[rows]``), the last two for :func:`rms_norm_grad`.  ``sum`` may be ``x`` or
+    ``residual`` itself."""
+    lib = _library()
+    device = _current_device()
+    d, sum, rstd = _norm(x, weight, eps, residual, sum, rstd, device, stream)
+    if out is None:
+        out = _empty((d.rows, d.cols), x.dtype, x, stream)
+    pitch = _sized(out, "out", {x.dtype: 0}, device, d.rows, d.cols)[1]
+    _check(lib.apc_rms_norm(ctypes.byref(d), out.data_ptr(), pitch, rstd.data_ptr(), _stream(stream, device)))
+    return out, sum, rstd
+
+
+def rms_norm_fp8(x, weight, *, eps=1e-6, residual=None, dtype=torch.float8_e4m3fn, transposed: bool = False, out=None, sum=None,
+                 rstd=None, stream=None):
+    """Enqueue :func:`rms_norm` with its output in 8 bits, as
+    :func:`quantize_fp8` makes it with ``block_rows=1``, from the unrounded
+    values.
+
+    Returns ``(data, scale, sum, rstd)`` or, with ``transposed``, ``(data, scale,
+    data_t, scale_t, sum, rstd)``.  ``out`` takes the tensors in front of
+    ``sum``."""
+    lib = _library()
+    device = _current_device()
+    if dtype not in _FORMAT:
+        raise ValueError("dtype %s is not an 8-bit floating type" % dtype)
+    d, sum, rstd = _norm(x, weight, eps, residual, sum, rstd, device, stream)
+    r, c = d.rows, d.cols
+    if out is None:
+        out = _fp8_empty(r, c, 1, dtype, x, stream)
+        if transposed:
+            out += _fp8_empty(c, r, 1, dtype, x, stream)
+    elif len(out) != (4 if transposed else 2):
+        raise ValueError("out has %d tensors, expected %d" % (len(out), 4 if transposed else 2))
+    q, qr, qc = _fp8(out[0], out[1], "q", device, 1)
+    if qr != r or qc != c or q.format != _FORMAT[dtype]:
+        raise ValueError("out: q is %d x %d of %s, expected %d x %d of %s" % (qr, qc, out[0].dtype, r, c, dtype))
+    qt = None
+    if transposed:
+        qt, qr, qc = _fp8(out[2], out[3], "qt", device, 1)
+        if qr != c or qc != r or qt.format != _FORMAT[dtype]:
+            raise ValueError("out: qt is %d x %d of %s, expected %d x %d of %s" % (qr, qc, out[2].dtype, c, r, dtype))
+        qt = ctypes.byref(qt)
+    _check(lib.apc_rms_norm_fp8(ctypes.byref(d), ctypes.byref(q), qt, rstd.data_ptr(), _stream(stream, device)))
+    return *out, sum, rstd
+
+
+def rms_norm_grad(dout, x, weight, rstd, *, dresidual=None, out=None, dweight=None, weight_grad: bool = True, workspace=None,
+                  stream=None):
+    """Enqueue the gradient of :func:`rms_norm` or :func:`rms_norm_fp8`:
+    ``dout`` (``[rows, cols]`` of ``x``'s type) is the output's, ``x`` the norm's
+    ``sum``, ``rstd`` its statistics, ``dresidual`` the gradient that reaches
+    ``sum`` otherwise.
+
+    Returns ``(dx, dweight)``: the gradient of ``x`` and of the residual alike,
+    in ``x``'s type or in ``out`` (which may be ``dout`` or ``dresidual`` itself),
+    and the weight's, in its type or in ``dweight``'s; None without
+    ``weight_grad``.  ``workspace``: fp32, for a caller that keeps its own, which
+    no other call may use at the same time; ``rms_norm_grad_workspace(rows,
+    cols)`` elements."""
+    lib = _library()
+    device = _current_device()
+    kind, r, c, pitch = _matrix(x, "x", _DTYPE, device)
+    same = {x.dtype: kind}
+    dpitch = _sized(dout, "dout", same, device, r, c)[1]
+    rpitch = 0 if dresidual is None else _sized(dresidual, "dresidual", same, device, r, c)[1]
+    d = _NormGrad(dout.data_ptr(), x.data_ptr(), weight.data_ptr(), None if dresidual is None else dresidual.data_ptr(),
+                  _vector(rstd, "rstd", _F32, device, r), r, c, dpitch, pitch, rpitch, kind, _weight(weight, "weight", device, c))
+    if out is None:
+        out = _empty((r, c), x.dtype, x, stream)
+    opitch = _sized(out, "out", same, device, r, c)[1]
+    at = work = None
+    wkind = 0
+    if weight_grad:
+        if dweight is None:
+            dweight = _empty((c,), weight.dtype, weight, stream)
+        wkind, at = _weight(dweight, "dweight", device, c), dweight.data_ptr()
+        n = rms_norm_grad_workspace(r, c)
+        if workspace is None:
+            workspace = _empty((n,), torch.float32, x, stream)
+        elif workspace.numel() > n:
+            workspace = workspace.view(-1)[:n]
+        work = _vector(workspace, "workspace", _F32, device, n)
+    elif dweight is not None:
+        raise ValueError("dweight without weight_grad")
+    _check(lib.apc_rms_norm_grad(ctypes.byref(d), out.data_ptr(), opitch, at, wkind, work, _stream(stream, device)))
+    return out, dweight
+
+
+def rms_norm_grad_workspace(rows: int, cols: int) -> int:
+    """Elements of :func:`rms_norm_grad`'s workspace."""
+    return _library().apc_rms_norm_grad_workspace(rows, cols) // 4
 
 
 def matmul_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, stream=None):

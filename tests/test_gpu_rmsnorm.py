@@ -1,0 +1,292 @@
+"""The root-mean-square norm and its gradient against plain implementations in
+64 bits, on the GPU.
+
+Bounds, in units u = 2^-24 of a rounding to fp32.  A thread's sum of squares
+passes at most 8 multiply-adds and 4 additions for each 16 columns, the rest of
+the mean 2^-26: with one rounding at the end rstd is off by (12 / 2 + 2) u for
+rows that a group holds.  Everything behind rstd has a fixed order of fp32
+operations, which the same operations in torch repeat bit for bit."""
+import math
+
+import pytest
+import torch
+
+import paper_2609_18178_gb300 as apc
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+UNIT = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+TINY = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -133, torch.float16: 2.0 ** -24}
+TYPES = [torch.bfloat16, torch.float16, torch.float32]
+SIZES = [(1, 1), (1, 8), (3, 7), (5, 128), (2, 129), (7, 255), (9, 1000), (1, 4096), (33, 4096), (2, 4099), (1, 8192), (160, 2048),
+         (200, 5003), (300, 64), (700, 264), (5, 16384), (3, 16385), (2, 40001)]
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def strided(x, extra=0, offset=0):
+    """x in memory with rows `extra` elements further apart, `offset` elements
+    behind an allocation's start; what surrounds it is NaN."""
+    r, c = x.shape
+    room = torch.full((offset + r * (c + extra) + 64,), math.nan, device="cuda").to(x.dtype)
+    v = room[offset:offset + r * (c + extra)].view(r, c + extra)[:, :c]
+    v.copy_(x)
+    return v
+
+
+def inputs(r, c, dtype, wdtype, seed=0):
+    g = gen(r * 100_003 + c + seed)
+    x = torch.randn(r, c, generator=g, device="cuda")
+    x[:, ::37] *= 20
+    w = torch.randn(c, generator=g, device="cuda") * 0.2 + 1
+    return x.to(dtype), torch.randn(r, c, generator=g, device="cuda").mul_(3).to(dtype), w.to(wdtype)
+
+
+def check_rstd(h, eps, rstd):
+    want = 1 / (h.double().square().mean(1) + eps).sqrt()
+    lanes = max(1, h.shape[1] / 16384)
+    assert ((rstd.double() - want).abs() <= (8 + 8 * lanes) * U * want).all()
+
+
+def y_of(h, rstd, w):
+    return h.float() * rstd[:, None] * w.float()
+
+
+@pytest.mark.parametrize("r,c", SIZES)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("residual", [False, True])
+def test_norm(r, c, dtype, residual):
+    for k, wdtype in enumerate(dict.fromkeys([dtype, torch.float32])):
+        x, res, w = inputs(r, c, dtype, wdtype)
+        extra, offset = ((0, 0), (5, 3))[k] if c % 2 else ((0, 0), (8, 8))[k]
+        x, res = strided(x, extra, offset), strided(res, 2 * extra, offset) if residual else None
+        total = strided(torch.zeros_like(x), extra, 0) if residual else None
+        out = strided(torch.zeros_like(x), 3 * extra, offset)
+        y, h, rstd = apc.rms_norm(x, w, eps=1e-5, residual=res, out=out, sum=total)
+        assert y is out and rstd.shape == (r,) and rstd.dtype == torch.float32
+        want = (x.float() + res.float()).to(dtype) if residual else x
+        assert h is (total if residual else x) and torch.equal(h, want)
+        check_rstd(h, 1e-5, rstd)
+        assert torch.equal(y, y_of(h, rstd, w).to(dtype))
+        surround = y.as_strided((r, c + 3 * extra), (c + 3 * extra, 1), y.storage_offset())[:, c:]
+        assert surround.isnan().all()  # what lies behind the columns is left as it was
+
+
+@pytest.mark.parametrize("r,c", SIZES)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("fmt", [torch.float8_e4m3fn, torch.float8_e5m2])
+@pytest.mark.parametrize("transposed", [False, True])
+def test_norm_to_8_bits(r, c, dtype, fmt, transposed):
+    x, res, w = inputs(r, c, dtype, torch.float32 if transposed else dtype, 1)
+    res = res if r % 2 else None
+    if c % 3 == 0:
+        x = strided(x, 3, 1)
+    *got, h, rstd = apc.rms_norm_fp8(x, w, eps=1e-6, residual=res, dtype=fmt, transposed=transposed)
+    check_rstd(h, 1e-6, rstd)
+    want = apc.quantize_fp8(y_of(h, rstd, w), dtype=fmt, transposed=transposed)
+    assert len(got) == len(want)
+    for a, b in zip(got, want):
+        assert a.dtype == b.dtype and torch.equal(a.float(), b.float())
+    if r <= 9 and c <= 1000:  # and the definition itself
+        y = y_of(h, rstd, w).double()
+        top = {torch.float8_e4m3fn: 448.0, torch.float8_e5m2: 57344.0}[fmt]
+        for i in range(-(-c // 128)):
+            m = y[:, 128 * i:128 * i + 128].abs().amax(1)
+            s = got[1][i].double()
+            assert ((m <= s * top) & ((m > s * top / 2) | (m == 0))).all()
+
+
+def test_same_bits_however_rows_lie():
+    """Few rows, many rows, aligned or not: rstd is rounded once, so the bits agree but for a rare last one."""
+    x, res, w = inputs(400, 3000, torch.bfloat16, torch.bfloat16)
+    a = apc.rms_norm(x, w, residual=res)
+    b = apc.rms_norm(strided(x, 1, 1), w, residual=strided(res, 1, 0))
+    c = [apc.rms_norm(x[i:i + 1], w, residual=res[i:i + 1]) for i in range(100)]
+    assert (a[2] != b[2]).float().mean() < 0.2 and (a[2][:100] != torch.cat([t[2] for t in c])).float().mean() < 0.2
+    assert ((a[2] - b[2]).abs() <= 2 * 2 * U * a[2]).all()
+
+
+def test_norm_does_not_depend_on_the_grid(monkeypatch):
+    x, res, w = inputs(700, 1000, torch.bfloat16, torch.float32)
+    a = apc.rms_norm_fp8(x, w, residual=res, transposed=True)
+    d = apc.rms_norm_grad(res, x, w, a[-1])
+    for limit in ("1", "7"):
+        monkeypatch.setenv("APC_GRID_LIMIT", limit)
+        for p, q in zip(a, apc.rms_norm_fp8(x, w, residual=res, transposed=True)):
+            assert torch.equal(p.float(), q.float())
+        for p, q in zip(d, apc.rms_norm_grad(res, x, w, a[-1])):
+            assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("place", ["x", "residual"])
+def test_sum_in_place(place):
+    for c in (1000, 40_000):
+        x, res, w = inputs(9, c, torch.bfloat16, torch.bfloat16)
+        want = apc.rms_norm(x, w, residual=res)
+        a, b = x.clone(), res.clone()
+        got = apc.rms_norm(a, w, residual=b, sum=a if place == "x" else b)
+        for p, q in zip(got, want):
+            assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("c", [100, 1000, 4096, 20_000])
+def test_rows_of_huge_values(c):
+    """Squares that overflow binary32 are taken scaled; beside them ordinary rows, and tiny ones that eps rules."""
+    x, _, w = inputs(6, c, torch.float32, torch.float32)
+    x[0] *= 1e25
+    x[1] *= 1e-25
+    x[2] = 0
+    x[3, ::3] = 3e38 * torch.sign(x[3, ::3])
+    x[4, 0] = 1e20
+    for dtype in (torch.float32, torch.bfloat16):
+        h = x.to(dtype)
+        y, _, rstd = apc.rms_norm(h, w, eps=1e-6)
+        check_rstd(h, 1e-6, rstd)
+        want = h.double() * rstd.double()[:, None] * w.double()
+        assert ((y.double() - want).abs() <= (UNIT[dtype] + 3 * U) * want.abs() + TINY[dtype] * 2).all()
+
+
+@pytest.mark.parametrize("c", [100, 4096, 5003, 20_000])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_that_are_not_finite(c, dtype):
+    x, res, w = inputs(8, c, dtype, dtype)
+    x[1, c // 2] = math.inf
+    x[3, 7] = math.nan
+    x[5, c - 1] = -math.inf
+    x[6, 3] = math.inf
+    res[6, 3] = -math.inf  # their sum is a NaN
+    y, h, rstd = apc.rms_norm(x, w, residual=res)
+    assert rstd[[1, 5]].eq(0).all() and rstd[[3, 6]].isnan().all()
+    fine = [0, 2, 4, 7]
+    check_rstd(h[fine], 1e-6, rstd[fine])
+    want = y_of(h, rstd, w).to(dtype)
+    assert torch.equal(y.isnan(), want.isnan()) and torch.equal(y.nan_to_num(), want.nan_to_num())
+    assert y[1].isnan().sum() == 1 and (y[1].nan_to_num() == 0).all() and y[3].isnan().all()
+    for fmt in (torch.float8_e4m3fn, torch.float8_e5m2):
+        *got, _, _ = apc.rms_norm_fp8(x, w, residual=res, dtype=fmt, transposed=True)
+        ref = apc.quantize_fp8(y_of(h, rstd, w), dtype=fmt, transposed=True)
+        for a, b in zip(got, ref):
+            assert torch.equal(a.float().isnan(), b.float().isnan())
+            assert torch.equal(a.float().nan_to_num(), b.float().nan_to_num())
+    w[5] = math.inf  # in a weight
+    got = apc.rms_norm_fp8(res, w)
+    ref = apc.quantize_fp8(y_of(res, got[-1], w))
+    for a, b in zip(got, ref):
+        assert torch.equal(a.float().nan_to_num(7.0), b.float().nan_to_num(7.0))
+
+
+def test_nothing():
+    w = torch.ones(16, device="cuda")
+    x = torch.ones(0, 16, device="cuda")
+    y, h, rstd = apc.rms_norm(x, w)
+    assert y.shape == (0, 16) and rstd.shape == (0,)
+    dw = torch.full((16,), 7.0, device="cuda")
+    dx, dw = apc.rms_norm_grad(x, x, w, rstd, dweight=dw)
+    assert dx.shape == (0, 16) and (dw == 0).all()  # a sum over no rows
+    e = torch.ones(5, 0, device="cuda")
+    assert apc.rms_norm(e, w[:0])[0].shape == (5, 0)
+    assert apc.rms_norm_grad(e, e, w[:0], torch.ones(5, device="cuda"))[1].shape == (0,)
+
+
+# ---- gradient
+
+def check_grad(d, x, w, rstd, dres, dx, dw, eps_rows):
+    r, c = x.shape
+    z, g = x.double() * rstd.double()[:, None], d.double() * w.double()
+    mean = (g * z).mean(1, keepdim=True)
+    want = (g - z * mean) * rstd.double()[:, None]
+    # 16 products a thread for each 16,384 columns, 12 additions between threads, 8 roundings more
+    k = 16 * max(1, c / 16384) + 20
+    size = (g.abs() + z.abs() * (g * z).abs().mean(1, keepdim=True)) * rstd.double()[:, None]
+    if dres is not None:
+        want, size = want + dres.double(), size + dres.double().abs()
+    assert ((dx.double() - want).abs() <= k * U * size + UNIT[x.dtype] * want.abs() + TINY[x.dtype]).all()
+    if dw is not None:
+        want, size = (d.double() * z).sum(0), (d.double() * z).abs().sum(0)
+        # a run's rows, the runs of a warp, the warps
+        k = r / eps_rows + eps_rows / 8 + 8
+        assert ((dw.double() - want).abs() <= k * U * size + UNIT[dw.dtype] * want.abs() + TINY[dw.dtype]).all()
+
+
+@pytest.mark.parametrize("r,c", SIZES + [(3000, 200), (1500, 4096)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_grad(r, c, dtype):
+    for k, wdtype in enumerate(dict.fromkeys([dtype, torch.float32])):
+        x, d, w = inputs(r, c, dtype, wdtype, 2)
+        d = (d * 1e-2).to(dtype)
+        if r > 2:
+            d[1] = 0  # a position that does not count
+        dres = None if k == 0 else torch.randn(r, c, generator=gen(5), device="cuda").mul_(1e-2).to(dtype)
+        rstd = apc.rms_norm(x, w)[2]
+        extra, offset = ((0, 0), (5, 3))[k]
+        dx, dw = apc.rms_norm_grad(strided(d, extra, offset), strided(x, 2 * extra, 0), w, rstd, dresidual=dres)
+        assert dx.dtype == dtype and dw.dtype == wdtype
+        parts = apc.operators.rms_norm_grad_workspace(r, c) // c
+        check_grad(d, x, w, rstd, dres, dx, dw, parts)
+        if r > 2 and dres is None:
+            assert (dx[1] == 0).all()
+        only, none = apc.rms_norm_grad(d, x, w, rstd, dresidual=dres, weight_grad=False)
+        assert none is None
+        check_grad(d, x, w, rstd, dres, only, None, parts)
+
+
+def test_grad_in_place_and_types():
+    x, d, w = inputs(300, 1000, torch.bfloat16, torch.bfloat16)
+    rstd = apc.rms_norm(x, w)[2]
+    dres = d * 0.5
+    want = apc.rms_norm_grad(d, x, w, rstd, dresidual=dres, dweight=torch.empty(1000, device="cuda"))
+    for place in ("dout", "dresidual"):
+        a, b = d.clone(), dres.clone()
+        got = apc.rms_norm_grad(a, x, w, rstd, dresidual=b, out=a if place == "dout" else b,
+                                dweight=torch.empty(1000, dtype=torch.half, device="cuda"))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1].half())
+
+
+def test_grad_against_differences():
+    """The formula is the derivative of the forward definition, in 64 bits; the kernel follows the formula."""
+    x, d, w = inputs(4, 96, torch.float32, torch.float32)
+    eps = 1e-3
+    _, h, rstd = apc.rms_norm(x, w, eps=eps)
+    dx, dw = apc.rms_norm_grad(d, x, w, rstd)
+
+    def loss(x, w):
+        return (x / (x.square().mean(1, keepdim=True) + eps).sqrt() * w * d.double()).sum()
+
+    x, w = x.double(), w.double()
+    step = 1e-6
+    for at, grad in ((x, dx), (w, dw)):
+        for i in range(0, at.numel(), 17):
+            e = torch.zeros_like(at).view(-1)
+            e[i] = step
+            e = e.view_as(at)
+            up, down = (loss(x + s * e, w) if at is x else loss(x, w + s * e) for s in (1, -1))
+            # differences: truncation step^2, cancellation 2^-53 |loss| / step; the kernel: a few hundred u
+            assert abs((up - down) / (2 * step) - grad.view(-1)[i].double()) <= 1e-4 * (1 + abs(grad.view(-1)[i].item()))
+
+
+def test_on_another_stream_and_in_a_graph():
+    x, res, w = inputs(300, 4096, torch.bfloat16, torch.bfloat16)
+
+    def step(**kw):
+        *q, h, rstd = apc.rms_norm_fp8(x, w, residual=res, transposed=True, **kw)
+        return [*q, h, rstd, *apc.rms_norm_grad(res, h, w, rstd, dresidual=x, **kw)]
+
+    want = step()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = step(stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    for a, b in zip(got, want):
+        assert torch.equal(a.float(), b.float())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step()
+    x.copy_(res.flip(0))
+    res.mul_(0.5)
+    want = step()
+    for _ in range(2):
+        g.replay()
+    for a, b in zip(got, want):
+        assert torch.equal(a.float(), b.float())
