@@ -89,7 +89,7 @@ struct NormGradArgs {
 
 // Runs of rows whose sums of the weight's gradient are kept apart.
 uint32_t rms_norm_parts(uint32_t rows, uint32_t cols);
-int launch_rms_norm_grad(const NormGradArgs &a, void *stream);
+int launch_rms_norm_grad(const NormGradArgs &a, unsigned sms, void *stream);
 
 // ---- product
 struct MatmulArgs {

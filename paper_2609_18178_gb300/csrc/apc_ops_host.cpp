@@ -241,8 +241,8 @@ APC_EXPORT apc_status apc_rms_norm_grad(const apc_norm_grad *d, void *dx, int64_
     rs.add("workspace", workspace, 1, work, 0, true);
   }
   if (c == 0 || (r == 0 && !dweight)) return APC_OK;
-  unsigned cap = 0;
-  if ((st = apc::op_ranges(rs.r, rs.n)) != APC_OK || (st = apc::op_grid(1, &cap)) != APC_OK) return st;
+  unsigned cap = 0, sms = 0;
+  if ((st = apc::op_ranges(rs.r, rs.n)) != APC_OK || (st = apc::op_grid(1, &cap, &sms)) != APC_OK) return st;
   apc::NormGradArgs a = {};
   a.dout = d->dout;
   a.x = d->x;
@@ -261,7 +261,7 @@ APC_EXPORT apc_status apc_rms_norm_grad(const apc_norm_grad *d, void *dx, int64_
   a.dtype = d->dtype;
   a.wdtype = d->weight_dtype;
   a.dwdtype = dweight_dtype;
-  const int e = apc::launch_rms_norm_grad(a, stream);
+  const int e = apc::launch_rms_norm_grad(a, sms, stream);
   return e ? apc::op_cuda_fail(e, "norm gradient kernel launch") : APC_OK;
 }
 

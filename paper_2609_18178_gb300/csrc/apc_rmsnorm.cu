@@ -90,6 +90,23 @@ __device__ __forceinline__ void round_pair<__half>(uint32_t *w, int pair, float 
   w[pair] = *reinterpret_cast<const uint32_t *>(&v);
 }
 
+// w + x, rounded to T.  The packed 16-bit addition rounds once, and so does one in fp32
+// that is rounded again: a sum that 24 bits do not hold has a term below half a last place
+// of the other.
+template <typename T>
+__device__ __forceinline__ void add_rounded(uint32_t (&w)[8 / Word<T>::kPer], const uint32_t (&x)[8 / Word<T>::kPer]) {
+#pragma unroll
+  for (int i = 0; i < 8 / Word<T>::kPer; ++i) {
+    if (sizeof(T) == 4) {
+      w[i] = __float_as_uint(__uint_as_float(w[i]) + __uint_as_float(x[i]));
+    } else if (inf_bits<T>() == 0x7f80u) {
+      asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(w[i]) : "r"(x[i]));
+    } else {
+      asm("add.rn.f16x2 %0, %0, %1;" : "+r"(w[i]) : "r"(x[i]));
+    }
+  }
+}
+
 // The weights of eight columns, of any type.
 template <bool WIDE>
 __device__ __forceinline__ void weights(uint64_t (&v)[4], const void *weight, uint32_t dtype, bool aligned, uint32_t first, int n) {
@@ -224,14 +241,15 @@ __device__ __forceinline__ uint32_t group_max(uint32_t m, const Group &g, Stat *
   return m;
 }
 
-template <typename T>
-__device__ __forceinline__ float squares(const uint32_t (&w)[8 / Word<T>::kPer], float scale) {
-  uint64_t acc[2] = {0, 0};
-  const uint64_t both = pack2(scale, scale);
+// The squares of eight elements, each times `scale`.
+template <typename T, bool SCALED = false>
+__device__ __forceinline__ float squares(const uint32_t (&w)[8 / Word<T>::kPer], float scale = 1.0f) {
+  uint64_t acc[2];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint64_t v = mul2(pack2(element<T>(w, 2 * i), element<T>(w, 2 * i + 1)), both);
-    acc[i % 2] = fma2(v, v, acc[i % 2]);
+    uint64_t v = pack2(element<T>(w, 2 * i), element<T>(w, 2 * i + 1));
+    if (SCALED) v = mul2(v, pack2(scale, scale));
+    acc[i % 2] = i < 2 ? mul2(v, v) : fma2(v, v, acc[i % 2]);
   }
   const float2 a = unpack2(acc[0]), b = unpack2(acc[1]);
   return (a.x + a.y) + (b.x + b.y);
@@ -243,6 +261,24 @@ __device__ __forceinline__ uint32_t largest(const uint32_t (&w)[8 / Word<T>::kPe
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(element<T>(w, i)) & 0x7fffffffu);
   return m;
+}
+
+// rstd of a row some of whose threads' sums are not finite: infinities and NaNs, or
+// squares beyond the largest number, which are taken scaled (eps is nothing beside them).
+template <typename T, int V>
+__device__ __forceinline__ float wild_rstd(const uint32_t (&w)[V][8 / Word<T>::kPer], const Group &g, Stat *room, const NormConst &c) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int v = 0; v < V; ++v) m = max(m, largest<T>(w[v]));
+  m = group_max(m, g, room);
+  if (m >= 0x7f800000u) return m > 0x7f800000u ? __uint_as_float(0x7fffffffu) : 0.0f;
+  const float scale = __uint_as_float(max(254u - (m >> 23), 1u) << 23);
+  float p = 0.0f, rstd;
+#pragma unroll
+  for (int v = 0; v < V; ++v) p += squares<T, true>(w[v], scale);
+  row_rstd(p, g, room, c, false, &rstd);
+  g.sync();
+  return rstd * scale;
 }
 
 // ---------------------------------------------------------------------------
@@ -261,23 +297,29 @@ struct ForwardArgs {
   NormConst c;
 };
 
+// The largest magnitude of three values, a NaN's bits above all.
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+  float y;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+
 // Eight values of y to 8 bits; bits: their largest magnitude over the block of 128.
 template <bool E5M2, bool WIDE>
 __device__ __forceinline__ void quantize8(const ForwardArgs &a, uint32_t row, uint32_t first, int n, const uint64_t (&y)[4],
                                           uint32_t lane) {
   uint8_t *at = a.q.data + (int64_t)row * a.q.pitch + first;
-  uint32_t m[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 v = unpack2(y[i]);
-    m[2 * i] = __float_as_uint(v.x) & 0x7fffffffu, m[2 * i + 1] = __float_as_uint(v.y) & 0x7fffffffu;
-  }
+  const auto value = [&](int i) {
+    const float2 v = unpack2(y[i / 2]);
+    return i % 2 ? v.y : v.x;
+  };
 #pragma unroll
   for (int part = 0; part < (WIDE ? 1 : 2); ++part) {  // blocks: half a warp's 8 values each, or 4 of a whole warp's
     const int from = WIDE ? 0 : 4 * part, to = WIDE ? 8 : from + 4;
-    uint32_t top = 0;
+    float high = 0.0f;
 #pragma unroll
-    for (int i = from; i < to; ++i) top = max(top, m[i]);
+    for (int i = from; i < to; i += 2) high = max_abs(high, value(i), value(i + 1));
+    uint32_t top = __float_as_uint(high);
     const auto over_block = [&](uint32_t v) {
       if (!WIDE) return __reduce_max_sync(~0u, v);
 #pragma unroll
@@ -289,7 +331,10 @@ __device__ __forceinline__ void quantize8(const ForwardArgs &a, uint32_t row, ui
     if (awkward) {  // something is not finite
       top = 0;
 #pragma unroll
-      for (int i = from; i < to; ++i) top = max(top, m[i] < 0x7f800000u ? m[i] : 0u);
+      for (int i = from; i < to; ++i) {
+        const uint32_t m = __float_as_uint(value(i)) & 0x7fffffffu;
+        top = max(top, m < 0x7f800000u ? m : 0u);
+      }
       top = over_block(top);
     }
     const uint32_t e = scale_exponent<E5M2>(__uint_as_float(top));
@@ -302,8 +347,7 @@ __device__ __forceinline__ void quantize8(const ForwardArgs &a, uint32_t row, ui
     } else {
 #pragma unroll
       for (int i = from; i < to; ++i) {
-        const float2 v = unpack2(y[i / 2]);
-        if (i < n) at[WIDE ? i : 32 * i] = any_to_fp8<E5M2>(i % 2 ? v.y : v.x, inv);
+        if (i < n) at[WIDE ? i : 32 * i] = any_to_fp8<E5M2>(value(i), inv);
       }
     }
   }
@@ -347,9 +391,7 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
         if (a.residual) {
           uint32_t o[kWords];
           load<T, WIDE>(o, res + c, n);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            round_pair<T>(w[v], i, element<T>(w[v], 2 * i) + element<T>(o, 2 * i), element<T>(w[v], 2 * i + 1) + element<T>(o, 2 * i + 1));
+          add_rounded<T>(w[v], o);
           store<T, WIDE>(sum + c, w[v], n);
         }
       }
@@ -365,7 +407,7 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
     float p = 0.0f, rstd;
     over_row(false, [&](uint32_t) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) p += squares<T>(w[v], 1.0f);
+      for (int v = 0; v < V; ++v) p += squares<T>(w[v]);
     });
     if (!row_rstd(p, g, room, a.c, true, &rstd)) {
       uint32_t m = 0;
@@ -381,7 +423,7 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
         p = 0.0f;
         over_row(true, [&](uint32_t) {
 #pragma unroll
-          for (int v = 0; v < V; ++v) p += squares<T>(w[v], scale);
+          for (int v = 0; v < V; ++v) p += squares<T, true>(w[v], scale);
         });
         row_rstd(p, g, room, a.c, false, &rstd);
         rstd *= scale;
@@ -421,8 +463,10 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
 }
 
 // The transpose in 8 bits, from the sum and rstd that the forward kernel left.  A CTA walks
-// tiles of 128 x 128, as the quantization's tile kernel does: thread (tx, ty) holds rows 8
-// ty + 0..7 of columns 8 tx + 0..7.
+// tiles of 128 x 128, the last rows first: those are what the forward kernel left in L2.  The
+// next tile comes into shared memory while the one before is stored; four CTAs on an SM
+// cover for each other otherwise.  Thread (tx, ty) takes rows 8 ty + 0..7 of columns 8 tx +
+// 0..7; the transpose goes through shared memory in 8-byte pieces, swizzled.
 struct TurnArgs {
   const void *h, *weight;
   const float *rstd;
@@ -437,61 +481,119 @@ struct TurnShared {
   float inv[128], rstd[128];
 };
 
+// 16 bytes, of which the first n are copied and the others zeros.
+__device__ __forceinline__ void copy_block(uint32_t dst, const void *src, uint32_t n) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+
 template <typename T, bool E5M2>
-__global__ void __launch_bounds__(256, 2) turn_kernel(const __grid_constant__ TurnArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) turn_kernel(const __grid_constant__ TurnArgs a) {
   constexpr int kWords = 8 / Word<T>::kPer;
+  constexpr uint32_t kPitch = 128 * sizeof(T);
+  extern __shared__ __align__(128) uint8_t s_tile[];
   __shared__ __align__(16) TurnShared sh;
   const uint32_t tx = threadIdx.x % 16, ty = threadIdx.x / 16, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t across = (a.cols + kBlock - 1) / kBlock, down = (a.rows + kBlock - 1) / kBlock;
-  for (uint64_t t = blockIdx.x; t < (uint64_t)across * down; t += gridDim.x) {
-    const uint32_t tr = (uint32_t)(t / across), tc = (uint32_t)(t % across), r0 = tr * kBlock, c0 = tc * kBlock;
-    const uint32_t r = r0 + 8 * ty, c = c0 + 8 * tx;
-    const int nc = c < a.cols ? (int)min(8u, a.cols - c) : 0;
-    uint32_t w[8][kWords];
-    {
-      const T *h = static_cast<const T *>(a.h) + (int64_t)r * a.pitch + c;
+  const uint64_t tiles = (uint64_t)across * down;
+  // thread (tx, ty) brings columns 8 tx + 0..7 of rows ty, ty + 16, ...
+  const auto fetch = [&](uint64_t t) {
+    const uint32_t tr = (uint32_t)(t / across), tc = (uint32_t)(t % across), c = tc * kBlock + 8 * tx;
+    const int n = c < a.cols ? (int)min(8u, a.cols - c) : 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i, h += a.pitch) load8<T>(w[i], h, r + i < a.rows ? nc : 0, a.wide);
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t k = ty + 16 * i, r = tr * kBlock + k;
+      const int here = r < a.rows ? n : 0;
+      const T *h = static_cast<const T *>(a.h) + (here ? (int64_t)r * a.pitch + c : 0);
+      uint8_t *to = s_tile + k * kPitch + tx * (8 * sizeof(T));
+      if (a.wide) {
+#pragma unroll
+        for (int j = 0; j < kWords; j += 4) {
+          const int bytes = min(max(here * (int)sizeof(T) - 4 * j, 0), 16);
+          copy_block(smem_addr(to + 4 * j), reinterpret_cast<const uint8_t *>(h) + (bytes ? 4 * j : 0), bytes);
+        }
+      } else {
+        uint32_t w[kWords];
+        load8<T>(w, h, here, false);
+#pragma unroll
+        for (int j = 0; j < kWords; j += 4) *reinterpret_cast<uint4 *>(to + 4 * j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+      }
     }
+    if (threadIdx.x < 128) {
+      const uint32_t r = tr * kBlock + threadIdx.x;
+      sh.rstd[threadIdx.x] = r < a.rows ? __ldg(a.rstd + r) : 0.0f;
+    }
+  };
+  if (blockIdx.x < tiles) fetch(tiles - 1 - blockIdx.x);
+  for (uint64_t s = blockIdx.x; s < tiles; s += gridDim.x) {
+    const uint64_t t = tiles - 1 - s;
+    const uint32_t tr = (uint32_t)(t / across), tc = (uint32_t)(t % across), r0 = tr * kBlock, c0 = tc * kBlock;
     uint64_t wt[4];
-    weights<true>(wt, a.weight, a.wdtype, a.weight_aligned, c, nc);
-    if (threadIdx.x < 128) sh.rstd[threadIdx.x] = r0 + threadIdx.x < a.rows ? __ldg(a.rstd + r0 + threadIdx.x) : 0.0f;
+    {
+      const uint32_t c = c0 + 8 * tx;
+      weights<true>(wt, a.weight, a.wdtype, a.weight_aligned, c, c < a.cols ? (int)min(8u, a.cols - c) : 0);
+    }
+    words_landed();
     __syncthreads();
-    const auto value = [&](int i, int j) {  // columns 2j and 2j + 1 of row i
-      const float s = sh.rstd[8 * ty + i];
-      return mul2(mul2(pack2(element<T>(w[i], 2 * j), element<T>(w[i], 2 * j + 1)), pack2(s, s)), wt[j]);
+    // h * rstd of columns 2j and 2j + 1 of row 8 ty + i
+    const auto scaled = [&](const uint32_t (&w)[kWords], int i, int j) {
+      const float r = sh.rstd[8 * ty + i];
+      return mul2(pack2(element<T>(w, 2 * j), element<T>(w, 2 * j + 1)), pack2(r, r));
     };
-    uint32_t col[8], any = 0;
+    const auto row_words = [&](uint32_t (&w)[kWords], int i) {
 #pragma unroll
-    for (int pass = 0; pass < 2; ++pass) {
+      for (int j = 0; j < kWords; j += 4) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(s_tile + (8 * ty + i) * kPitch + tx * (8 * sizeof(T)) + 4 * j);
+        w[j] = v.x, w[j + 1] = v.y, w[j + 2] = v.z, w[j + 3] = v.w;
+      }
+    };
+    // The largest |y| of a column is the largest |h * rstd| times |weight|: rounding keeps the order.
+    float top[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top[j] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      uint32_t w[2][kWords];
+      row_words(w[0], i);
+      row_words(w[1], i + 1);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        uint32_t lo = 0, hi = 0;
+        const float2 p = unpack2(scaled(w[0], i, j)), q = unpack2(scaled(w[1], i + 1, j));
+        top[2 * j] = max_abs(top[2 * j], p.x, q.x);
+        top[2 * j + 1] = max_abs(top[2 * j + 1], p.y, q.y);
+      }
+    }
+    uint32_t col[8], any = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (r + i >= a.rows) continue;
-          const uint64_t y = value(i, j);
-          uint32_t u = (uint32_t)y & 0x7fffffffu, v = (uint32_t)(y >> 32) & 0x7fffffffu;
-          if (pass) u = u < 0x7f800000u ? u : 0, v = v < 0x7f800000u ? v : 0;
-          lo = max(lo, u), hi = max(hi, v);
+    for (int j = 0; j < 4; ++j) {
+      const float2 p = unpack2(mul2(pack2(top[2 * j], top[2 * j + 1]), wt[j]));
+      col[2 * j] = __float_as_uint(p.x) & 0x7fffffffu, col[2 * j + 1] = __float_as_uint(p.y) & 0x7fffffffu;
+    }
+    const auto share = [&]() {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) col[j] = max(col[j], __shfl_xor_sync(~0u, col[j], 16)), any = max(any, col[j]);
+      if (lane < 16) {
+        *reinterpret_cast<uint4 *>(&sh.col[warp][tx * 8]) = make_uint4(col[0], col[1], col[2], col[3]);
+        *reinterpret_cast<uint4 *>(&sh.col[warp][tx * 8 + 4]) = make_uint4(col[4], col[5], col[6], col[7]);
+      }
+    };
+    share();
+    any = __syncthreads_or(any >= 0x7f800000u);
+    if (any) {  // something is not finite: the largest of what is
+#pragma unroll
+      for (int j = 0; j < 8; ++j) col[j] = 0;
+      for (int i = 0; i < 8; ++i) {
+        uint32_t w[kWords];
+        row_words(w, i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint64_t y = mul2(scaled(w, i, j), wt[j]);
+          const uint32_t u = (uint32_t)y & 0x7fffffffu, v = (uint32_t)(y >> 32) & 0x7fffffffu;
+          col[2 * j] = max(col[2 * j], u < 0x7f800000u ? u : 0), col[2 * j + 1] = max(col[2 * j + 1], v < 0x7f800000u ? v : 0);
         }
-        col[2 * j] = lo, col[2 * j + 1] = hi;
       }
-      if (pass == 0) {
-        any = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) any = max(any, j < nc ? col[j] : 0u);
-        any = __syncthreads_or(any >= 0x7f800000u);
-        if (!any) break;
-      }
+      share();
+      __syncthreads();
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) col[j] = max(col[j], __shfl_xor_sync(~0u, col[j], 16));
-    if (lane < 16) {
-      *reinterpret_cast<uint4 *>(&sh.col[warp][tx * 8]) = make_uint4(col[0], col[1], col[2], col[3]);
-      *reinterpret_cast<uint4 *>(&sh.col[warp][tx * 8 + 4]) = make_uint4(col[4], col[5], col[6], col[7]);
-    }
-    __syncthreads();
     if (threadIdx.x < 128) {
       uint32_t m = 0;
 #pragma unroll
@@ -501,34 +603,49 @@ __global__ void __launch_bounds__(256, 2) turn_kernel(const __grid_constant__ Tu
       if (c0 + threadIdx.x < a.cols) a.qt.scale[(int64_t)tr * a.qt.scale_pitch + c0 + threadIdx.x] = power(e);
     }
     __syncthreads();
+    if (!any) {
+      uint32_t half[8][2];  // of a column: rows 0-3 and 4-7
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint64_t lo[4], hi[4];  // pairs of rows, of columns 2j and 2j + 1
+      for (int i = 0; i < 8; i += 4) {
+        uint32_t pair[8][2];  // rows i and i + 1, i + 2 and i + 3
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 p = unpack2(value(2 * i, j)), q = unpack2(value(2 * i + 1, j));
-        lo[i] = pack2(p.x, q.x), hi[i] = pack2(p.y, q.y);
-      }
+        for (int k = 0; k < 4; k += 2) {
+          uint32_t w[2][kWords];
+          row_words(w[0], i + k);
+          row_words(w[1], i + k + 1);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint64_t(&v)[4] = k ? hi : lo;
-        const float inv = sh.inv[8 * tx + 2 * j + k];
-        uint2 o;
-        if (!any) {
-          o = to_fp8x8<E5M2>(v, pack2(inv, inv));
-        } else {
-          uint32_t b[2] = {0, 0};
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float2 f = unpack2(v[i / 2]);
-            b[i / 4] |= (uint32_t)any_to_fp8<E5M2>(i % 2 ? f.y : f.x, inv) << (i % 4 * 8);
+          for (int j = 0; j < 4; ++j) {
+            const float2 f = *reinterpret_cast<const float2 *>(&sh.inv[8 * tx + 2 * j]);
+            const uint64_t inv = pack2(f.x, f.y);
+            const float2 p = unpack2(mul2(mul2(scaled(w[0], i + k, j), wt[j]), inv));
+            const float2 q = unpack2(mul2(mul2(scaled(w[1], i + k + 1, j), wt[j]), inv));
+            pair[2 * j][k / 2] = to_fp8x2<E5M2>(p.x, q.x);
+            pair[2 * j + 1][k / 2] = to_fp8x2<E5M2>(p.y, q.y);
           }
-          o = make_uint2(b[0], b[1]);
         }
-        sh.turn[(8 * tx + 2 * j + k) * 16 + (ty ^ tx)] = o;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) half[j][i / 4] = __byte_perm(pair[j][0], pair[j][1], 0x5410);
       }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sh.turn[(8 * tx + j) * 16 + (ty ^ tx)] = make_uint2(half[j][0], half[j][1]);
+    } else {
+      uint32_t b[8][2] = {};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint32_t w[kWords];
+        row_words(w, i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 f = unpack2(mul2(scaled(w, i, j), wt[j]));
+          b[2 * j][i / 4] |= (uint32_t)any_to_fp8<E5M2>(f.x, sh.inv[8 * tx + 2 * j]) << (i % 4 * 8);
+          b[2 * j + 1][i / 4] |= (uint32_t)any_to_fp8<E5M2>(f.y, sh.inv[8 * tx + 2 * j + 1]) << (i % 4 * 8);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sh.turn[(8 * tx + j) * 16 + (ty ^ tx)] = make_uint2(b[j][0], b[j][1]);
     }
     __syncthreads();
+    if (s + gridDim.x < tiles) fetch(tiles - 1 - s - gridDim.x);
     const uint32_t rr = r0 + 8 * tx;  // now tx counts pieces down a column
     const int nr = rr < a.rows ? (int)min(8u, a.rows - rr) : 0;
     uint8_t *to = a.qt.data + (int64_t)(c0 + ty) * a.qt.pitch + rr;
@@ -537,14 +654,14 @@ __global__ void __launch_bounds__(256, 2) turn_kernel(const __grid_constant__ Tu
       const uint32_t k = 16 * i + ty;
       if (c0 + k < a.cols && nr) store8(to, sh.turn[k * 16 + (tx ^ k / 8)], nr);
     }
-    __syncthreads();
   }
 }
 
 // ---------------------------------------------------------------------------
-// Gradient.  The rows are cut into `parts` runs whose number follows the sizes alone
-// (rms_norm_parts); a group walks a run and keeps its columns' sums of dout * z in
-// registers, which go to the workspace, from where a second kernel adds them in order.
+// Gradient.  The rows are dealt out to `parts` parts whose number follows the sizes alone
+// (rms_norm_parts): part p has rows p, p + parts, ....  A group walks a part and keeps its
+// columns' sums of dout * z in registers, which go to the workspace, from where a second
+// kernel adds them in order.
 
 struct GradArgs {
   const void *dout, *x, *weight, *dresidual;
@@ -555,10 +672,6 @@ struct GradArgs {
   uint32_t rows, cols, parts, wdtype, weight_aligned;
   float inv_cols;
 };
-
-__device__ __forceinline__ uint32_t part_begin(uint32_t rows, uint32_t parts, uint32_t p) {
-  return (uint32_t)((uint64_t)rows * p / parts);
-}
 
 // The sum of p over a group, in an order of its own, in every thread.
 __device__ __forceinline__ float group_sum(float p, const Group &g, float *room) {
@@ -583,7 +696,7 @@ __device__ __forceinline__ void z_and_g(const uint32_t (&x)[8 / Word<T>::kPer], 
 }
 
 template <typename T, int V, bool WIDE>
-__global__ void __launch_bounds__(1024, 1) grad_kernel(const __grid_constant__ GradArgs a) {
+__global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ GradArgs a) {
   constexpr int kWords = 8 / Word<T>::kPer;
   extern __shared__ float s_sums[];  // [2][groups][warps]
   const Group g{blockDim.x / 32, 1 + threadIdx.y, threadIdx.x / 32, threadIdx.x % 32};
@@ -599,8 +712,8 @@ __global__ void __launch_bounds__(1024, 1) grad_kernel(const __grid_constant__ G
   }
   for (uint32_t part = blockIdx.x * blockDim.y + threadIdx.y; part < a.parts; part += gridDim.x * blockDim.y) {
     uint64_t acc[V][4] = {};
-    const uint32_t end = part_begin(a.rows, a.parts, part + 1);
-    for (uint32_t row = part_begin(a.rows, a.parts, part); row < end; ++row) {
+    for (uint64_t at_row = part; at_row < a.rows; at_row += a.parts) {
+      const uint32_t row = (uint32_t)at_row;
       float *room = s_sums + (turn ^= 1) * blockDim.y * g.warps + threadIdx.y * g.warps;
       const float rstd = __ldg(a.rstd + row);
       uint32_t x[V][kWords], d[V][kWords], r[V][kWords];
@@ -681,10 +794,10 @@ template <typename T>
 __global__ void __launch_bounds__(256) grad_long_parts_kernel(const __grid_constant__ GradArgs a) {
   const uint64_t per = (a.cols + 255) / 256;
   for (uint64_t t = blockIdx.x; t < per * a.parts; t += gridDim.x) {
-    const uint32_t part = (uint32_t)(t / per), c = (uint32_t)(t % per) * 256 + threadIdx.x, end = part_begin(a.rows, a.parts, part + 1);
+    const uint32_t part = (uint32_t)(t / per), c = (uint32_t)(t % per) * 256 + threadIdx.x;
     if (c >= a.cols) continue;
     float acc = 0.0f;
-    for (uint32_t row = part_begin(a.rows, a.parts, part); row < end; ++row)
+    for (uint64_t row = part; row < a.rows; row += a.parts)
       acc = __fmaf_rn(to_float(static_cast<const T *>(a.dout)[(int64_t)row * a.dout_pitch + c]),
                       to_float(static_cast<const T *>(a.x)[(int64_t)row * a.pitch + c]) * __ldg(a.rstd + row), acc);
     a.partial[(uint64_t)part * a.cols + c] = acc;
@@ -714,6 +827,387 @@ __global__ void __launch_bounds__(256) parts_kernel(const float *partial, uint32
 }
 
 // ---------------------------------------------------------------------------
+// Many rows: a CTA walks rows, which bulk copies bring into a ring of shared memory, one or
+// two rows ahead of the one at work, so that memory is never waited for row by row.
+//
+// A row's copy takes the 16-byte blocks that hold it, wherever it begins, and a thread works
+// on units of eight elements that begin at a block's boundary, not at a multiple of eight
+// columns: loads and stores stay wide for rows at any boundary, as long as all matrices lie
+// alike within 16 bytes.  What a unit holds beside the row is masked.  Blocks that would
+// leave the matrix are not copied: their elements are put in place one by one.  The
+// barrier of a row's sum is also what frees the stage of the row before.
+//
+// The weights lie in shared memory as fp32, as the threads' elements do; rows that a CTA
+// walks begin alike where the grid allows it, else the weights are laid out again for each.
+
+constexpr uint32_t kRingThreads = 512, kStagesMost = 3;
+
+struct Ring {
+  uint32_t stages, region, mats;  // region: bytes of a matrix's part of a stage
+  uint32_t weights;               // bytes of the weights
+  uint32_t edges;                 // 1: the first row's first block begins in front of the matrix, 2: the last one's last ends behind
+  unsigned *status;
+
+  __host__ __device__ uint32_t stage() const { return region * mats; }
+  __host__ __device__ uint32_t bytes() const { return stages * stage() + weights; }
+};
+
+struct RingShared {
+  uint64_t full[kStagesMost];
+  Stat stats[2][32];
+  float sums[2][32];
+  int dead;
+};
+
+__device__ __forceinline__ void ring_begin(RingShared &sh, uint32_t stages) {
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < stages; ++s) mbar_init(&sh.full[s], 1);
+    sh.dead = 0;
+    mbar_init_fence();
+  }
+  __syncthreads();
+}
+
+// The bounded wait for a stage.  After one that gave up nothing more is copied and nothing
+// waited for; what follows is not to be used, as the status word says.
+__device__ __noinline__ void ring_wait_on(RingShared &sh, uint32_t stage, uint32_t parity, unsigned *status) {
+  if (*(volatile int *)&sh.dead || mbar_wait(&sh.full[stage], parity)) return;
+  atomicOr(status, (unsigned)APC_ETIMEOUT);
+  *(volatile int *)&sh.dead = 1;
+}
+__device__ __forceinline__ void ring_wait(RingShared &sh, uint32_t stage, uint32_t parity, unsigned *status) {
+  if (!mbar_try_wait(smem_addr(&sh.full[stage]), parity)) ring_wait_on(sh, stage, parity, status);
+}
+
+// Bytes of a row's first block in front of the row.
+__device__ __forceinline__ uint32_t skip_of(const void *base, int64_t pitch, uint32_t row, uint32_t size) {
+  return ((uint32_t)(uintptr_t)base + row * (uint32_t)pitch * size) & 15;
+}
+
+struct Source {
+  const void *base;
+  int64_t pitch;
+};
+
+// One thread: copy a row of each matrix into a stage.
+template <int M>
+__device__ __forceinline__ void ring_issue(RingShared &sh, const Source (&src)[M], const Ring &ring, uint8_t *stage, uint64_t *full,
+                                           uint32_t row, uint32_t rows, uint32_t cols, uint32_t size, uint64_t policy) {
+  if (*(volatile int *)&sh.dead) return;
+  const uint32_t skip = skip_of(src[0].base, src[0].pitch, row, size);
+  const uint32_t from = row == 0 && ring.edges & 1 ? 16 : 0;
+  const uint32_t bytes = ((skip + cols * size + 15) & ~15u) - from - (row == rows - 1 && ring.edges & 2 ? 16 : 0);
+  mbar_arrive_expect_tx(full, bytes * ring.mats);
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    if (m >= ring.mats) break;
+    const uint8_t *at = static_cast<const uint8_t *>(src[m].base) + (int64_t)row * src[m].pitch * size - skip + from;
+    bulk_g2s(stage + m * ring.region + from, at, bytes, full, policy);
+  }
+}
+
+// The elements of the blocks that ring_issue left out, in the first and the last row alone.
+template <typename T, int M>
+__device__ __forceinline__ void ring_edges(const Source (&src)[M], const Ring &ring, uint8_t *stage, uint32_t row, uint32_t rows,
+                                           uint32_t cols) {
+  const bool front = row == 0 && ring.edges & 1, back = row == rows - 1 && ring.edges & 2;
+  if (!front && !back) return;
+  const uint32_t skip = skip_of(src[0].base, src[0].pitch, row, sizeof(T)), i = threadIdx.x % 16;
+  const uint32_t per = 16 / sizeof(T), first = skip / sizeof(T), last = (first + cols) & ~(per - 1);  // the first element of the last block
+  const uint32_t e = threadIdx.x < 16 ? i : last + i;                                                 // counted from the first block
+  if (threadIdx.x < 32 && i < per && (threadIdx.x < 16 ? front : back) && e >= first && e < first + cols)
+    for (int m = 0; m < M; ++m)
+      if (m < ring.mats)
+        reinterpret_cast<T *>(stage + m * ring.region)[e] =
+            *(static_cast<const T *>(src[m].base) + (int64_t)row * src[m].pitch + (e - first));
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // copies come here again
+  __syncthreads();
+}
+
+// Unit u of a row: eight elements from column `first` on (below 0 in front of the row).
+// WHOLE: rows begin at blocks and are units and nothing else.
+template <bool WHOLE>
+struct Unit {
+  int32_t first;
+  bool any, full;
+
+  __device__ Unit(uint32_t u, uint32_t shift, uint32_t cols) {
+    first = (int32_t)(8 * u - (WHOLE ? 0 : shift));
+    any = first < (int32_t)cols;
+    full = WHOLE ? any : first >= 0 && first + 8 <= (int32_t)cols;
+  }
+};
+
+// Its elements, zeros where there are none.
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void ring_load(uint32_t (&w)[8 / Word<T>::kPer], const uint8_t *region, uint32_t k, const Unit<WHOLE> &u,
+                                          uint32_t cols) {
+  constexpr int kWords = 8 / Word<T>::kPer;
+  if (u.any) {
+#pragma unroll
+    for (int i = 0; i < kWords; i += 4) {
+      const uint4 v = *reinterpret_cast<const uint4 *>(region + k * (8 * sizeof(T)) + 4 * i);
+      w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+    }
+    if (!WHOLE && !u.full) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool there = u.first + i >= 0 && u.first + i < (int32_t)cols;
+        if (sizeof(T) == 4) w[i] = there ? w[i] : 0;
+        else w[i / 2] &= there ? ~0u : i % 2 ? 0xffffu : 0xffff0000u;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
+  }
+}
+
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void ring_store(T *row, const uint32_t (&w)[8 / Word<T>::kPer], const Unit<WHOLE> &u, uint32_t cols) {
+  if (u.full) {
+#pragma unroll
+    for (int i = 0; i < 8 / Word<T>::kPer; i += 4)
+      *(reinterpret_cast<uint4 *>(row + u.first) + i / 4) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+  } else if (!WHOLE && u.any) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int32_t c = u.first + i;
+      if (c < 0 || c >= (int32_t)cols) continue;
+      if (sizeof(T) == 4) reinterpret_cast<uint32_t *>(row)[c] = w[i];
+      else reinterpret_cast<uint16_t *>(row)[c] = (uint16_t)element_bits<T>(w, i);
+    }
+  }
+}
+
+// The weights of all units, the first of which begins `shift` columns in front of the row.
+__device__ __forceinline__ void lay_weights(float *to, const void *weight, uint32_t dtype, uint32_t units, uint32_t shift, uint32_t cols) {
+  for (uint32_t i = threadIdx.x; i < 8 * units; i += blockDim.x) {
+    const uint32_t c = i - shift;
+    float v = 0.0f;
+    if (i >= shift && c < cols)
+      v = dtype == APC_F32    ? __ldg(static_cast<const float *>(weight) + c)
+          : dtype == APC_BF16 ? to_float(static_cast<const __nv_bfloat16 *>(weight)[c])
+                              : to_float(static_cast<const __half *>(weight)[c]);
+    // a unit's halves lie apart, so that a warp's 16-byte loads meet no bank twice
+    to[(i / 8 * 4) + (i % 8 / 4) * 4 * units + i % 4] = v;
+  }
+}
+
+__device__ __forceinline__ void unit_weights(uint64_t (&v)[4], const float *laid, uint32_t units, uint32_t k) {
+  const ulonglong2 a = *reinterpret_cast<const ulonglong2 *>(laid + 4 * k), b = *reinterpret_cast<const ulonglong2 *>(laid + 4 * units + 4 * k);
+  v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+}
+
+// Eight elements from `skip` bytes behind a unit's first block on.
+template <typename T>
+__device__ __forceinline__ void ring_shifted(uint32_t (&w)[8 / Word<T>::kPer], const uint8_t *unit, uint32_t skip) {
+  constexpr int kWords = 8 / Word<T>::kPer;
+  uint32_t v[kWords + 4];
+#pragma unroll
+  for (int i = 0; i < kWords + 4; i += 4) {
+    const uint4 b = *reinterpret_cast<const uint4 *>(unit + 4 * i);
+    v[i] = b.x, v[i + 1] = b.y, v[i + 2] = b.z, v[i + 3] = b.w;
+  }
+  if (skip & 8) {
+#pragma unroll
+    for (int i = 0; i < kWords + 2; ++i) v[i] = v[i + 2];
+  }
+  if (skip & 4) {
+#pragma unroll
+    for (int i = 0; i < kWords + 1; ++i) v[i] = v[i + 1];
+  }
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) w[i] = sizeof(T) == 4 ? v[i] : __funnelshift_r(v[i], v[i + 1], (skip & 3) * 8);
+}
+
+// 8-bit outputs have rows at multiples of 16 bytes: their threads take units that begin at
+// multiples of eight columns.  For rows that begin elsewhere the sum goes through the stage.
+template <typename T, int OUT, int V, bool WHOLE>
+__global__ void __launch_bounds__(kRingThreads, V == 2 ? 2 : 1) ring_forward_kernel(const __grid_constant__ ForwardArgs a,
+                                                                                    const __grid_constant__ Ring ring) {
+  constexpr int kWords = 8 / Word<T>::kPer;
+  extern __shared__ __align__(128) uint8_t s_ring[];
+  __shared__ RingShared sh;
+  const Group g{blockDim.x / 32, 0, threadIdx.x / 32, threadIdx.x % 32};
+  const uint32_t units = V * blockDim.x;
+  float *const laid = reinterpret_cast<float *>(s_ring + ring.stages * ring.stage());
+  ring_begin(sh, ring.stages);
+  const Source src[2] = {{a.x, a.pitch}, {a.residual, a.residual_pitch}};
+  uint32_t next = blockIdx.x, into = 0;  // the row to copy next, its stage
+  const auto issue = [&]() {
+    if (next < a.rows) {
+      ring_issue<2>(sh, src, ring, s_ring + into * ring.stage(), &sh.full[into], next, a.rows, a.cols, sizeof(T), l2_evict_first());
+      next += gridDim.x;
+    }
+    if (++into == ring.stages) into = 0;
+  };
+  if (threadIdx.x == 0)
+    for (uint32_t s = 0; s + 1 < ring.stages; ++s) issue();
+  uint32_t shift = ~0u, stage = 0, parity = 0, turn = 0;
+  if (OUT != kSame) {
+    lay_weights(laid, a.weight, a.wdtype, units, 0, a.cols);
+    __syncthreads();
+  }
+  for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const uint32_t skip = WHOLE ? 0 : skip_of(a.x, a.pitch, row, sizeof(T));
+    if (OUT == kSame && skip != shift) {
+      __syncthreads();
+      lay_weights(laid, a.weight, a.wdtype, units, skip / sizeof(T), a.cols);
+      __syncthreads();
+      shift = skip;
+    }
+    uint8_t *const at = s_ring + stage * ring.stage();
+    ring_wait(sh, stage, parity, ring.status);
+    if (!WHOLE && ring.edges) ring_edges<T, 2>(src, ring, at, row, a.rows, a.cols);
+    uint32_t w[V][kWords];
+    float p = 0.0f, rstd;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const uint32_t k = threadIdx.x + v * blockDim.x;
+      const Unit<WHOLE> u(k, skip / sizeof(T), a.cols);
+      ring_load<T, WHOLE>(w[v], at, k, u, a.cols);
+      if (a.residual) {
+        uint32_t x[kWords];
+        ring_load<T, WHOLE>(x, at + ring.region, k, u, a.cols);
+        add_rounded<T>(w[v], x);
+        ring_store<T, WHOLE>(static_cast<T *>(a.sum) + (int64_t)row * a.sum_pitch, w[v], u, a.cols);
+      }
+      if (OUT != kSame && skip && u.any) {
+#pragma unroll
+        for (int i = 0; i < kWords; i += 4)
+          *reinterpret_cast<uint4 *>(at + k * (8 * sizeof(T)) + 4 * i) = make_uint4(w[v][i], w[v][i + 1], w[v][i + 2], w[v][i + 3]);
+      }
+      p += squares<T>(w[v]);
+    }
+    // before the next copy into a stage that was written here
+    if (OUT != kSame && skip) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    const bool fine = row_rstd(p, g, sh.stats[turn ^= 1], a.c, true, &rstd);
+    if (threadIdx.x == 0) issue();  // into the stage of the row before, which all have left
+    if (!fine) rstd = wild_rstd<T, V>(w, g, sh.stats[turn], a.c);
+    if (threadIdx.x == 0) a.rstd[row] = rstd;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const uint32_t k = threadIdx.x + v * blockDim.x;
+      const Unit<WHOLE> u(k, OUT == kSame ? skip / sizeof(T) : 0, a.cols);
+      if (OUT != kSame && skip && u.any) ring_shifted<T>(w[v], at + k * (8 * sizeof(T)), skip);
+      uint64_t wt[4], y[4];
+      unit_weights(wt, laid, units, k);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = mul2(mul2(pack2(element<T>(w[v], 2 * i), element<T>(w[v], 2 * i + 1)), pack2(rstd, rstd)), wt[i]);
+      if (OUT == kSame) {
+        uint32_t o[kWords];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 f = unpack2(y[i]);
+          round_pair<T>(o, i, f.x, f.y);
+        }
+        ring_store<T, WHOLE>(static_cast<T *>(a.out) + (int64_t)row * a.out_pitch, o, u, a.cols);
+      } else {
+        const int n = u.full ? 8 : u.any ? (int)a.cols - u.first : 0;
+        if (!u.full)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack2(y[i]);
+            y[i] = pack2(2 * i < n ? f.x : 0.0f, 2 * i + 1 < n ? f.y : 0.0f);
+          }
+        quantize8<OUT == kE5M2, true>(a, row, 8 * k, n, y, g.lane);
+      }
+    }
+    if (++stage == ring.stages) stage = 0, parity ^= 1;
+  }
+}
+
+// The gradient's rows through a ring of x, dout and dresidual.  Part p is rows p, p + parts,
+// ...: rows of a part begin alike.
+template <typename T, int V, bool WHOLE>
+__global__ void __launch_bounds__(kRingThreads, 1) ring_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ Ring ring) {
+  constexpr int kWords = 8 / Word<T>::kPer;
+  extern __shared__ __align__(128) uint8_t s_ring[];
+  __shared__ RingShared sh;
+  const Group g{blockDim.x / 32, 0, threadIdx.x / 32, threadIdx.x % 32};
+  const uint32_t units = V * blockDim.x;
+  float *const laid = reinterpret_cast<float *>(s_ring + ring.stages * ring.stage());
+  ring_begin(sh, ring.stages);
+  const Source src[3] = {{a.x, a.pitch}, {a.dout, a.dout_pitch}, {a.dresidual, a.dresidual_pitch}};
+  uint32_t next_part = blockIdx.x, next = next_part, into = 0;
+  const auto issue = [&]() {
+    if (next_part < a.parts) {
+      ring_issue<3>(sh, src, ring, s_ring + into * ring.stage(), &sh.full[into], next, a.rows, a.cols, sizeof(T), l2_evict_first());
+      next += a.parts;
+      if (next >= a.rows) next = next_part += gridDim.x;
+    }
+    if (++into == ring.stages) into = 0;
+  };
+  if (threadIdx.x == 0)
+    for (uint32_t s = 0; s + 1 < ring.stages; ++s) issue();
+  uint32_t shift = ~0u, stage = 0, parity = 0, turn = 0;
+  for (uint32_t part = blockIdx.x; part < a.parts; part += gridDim.x) {
+    uint64_t acc[V][4] = {};
+    const uint32_t skip = WHOLE ? 0 : skip_of(a.x, a.pitch, part, sizeof(T));
+    if (skip != shift) {
+      __syncthreads();
+      lay_weights(laid, a.weight, a.wdtype, units, skip / sizeof(T), a.cols);
+      __syncthreads();
+      shift = skip;
+    }
+    for (uint32_t row = part; row < a.rows; row += a.parts) {
+      const float rstd = __ldg(a.rstd + row);
+      uint8_t *const at = s_ring + stage * ring.stage();
+      ring_wait(sh, stage, parity, ring.status);
+      if (!WHOLE && ring.edges) ring_edges<T, 3>(src, ring, at, row, a.rows, a.cols);
+      uint64_t z[V][4], gg[V][4], dot = 0;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const uint32_t k = threadIdx.x + v * blockDim.x;
+        const Unit<WHOLE> u(k, skip / sizeof(T), a.cols);
+        uint32_t x[kWords], d[kWords];
+        ring_load<T, WHOLE>(x, at, k, u, a.cols);
+        ring_load<T, WHOLE>(d, at + ring.region, k, u, a.cols);
+        uint64_t wt[4];
+        unit_weights(wt, laid, units, k);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint64_t dd;
+          z_and_g<T>(x, d, rstd, wt, i, &z[v][i], &gg[v][i], &dd);
+          dot = fma2(gg[v][i], z[v][i], dot);
+          acc[v][i] = fma2(dd, z[v][i], acc[v][i]);
+        }
+      }
+      const float2 both = unpack2(dot);
+      const float mean = group_sum(both.x + both.y, g, sh.sums[turn ^= 1]) * a.inv_cols;
+      if (threadIdx.x == 0) issue();  // into the stage of the row before, which all have left
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const uint32_t k = threadIdx.x + v * blockDim.x;
+        const Unit<WHOLE> u(k, skip / sizeof(T), a.cols);
+        uint32_t o[kWords];
+        if (a.dresidual) ring_load<T, WHOLE>(o, at + 2 * ring.region, k, u, a.cols);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float2 f = unpack2(mul2(fma2(z[v][i], pack2(-mean, -mean), gg[v][i]), pack2(rstd, rstd)));
+          if (a.dresidual) f.x += element<T>(o, 2 * i), f.y += element<T>(o, 2 * i + 1);
+          round_pair<T>(o, i, f.x, f.y);
+        }
+        ring_store<T, WHOLE>(static_cast<T *>(a.dx) + (int64_t)row * a.dx_pitch, o, u, a.cols);
+      }
+      if (++stage == ring.stages) stage = 0, parity ^= 1;
+    }
+    if (!a.partial) continue;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const Unit<WHOLE> u(threadIdx.x + v * blockDim.x, skip / sizeof(T), a.cols);
+      float *to = a.partial + (uint64_t)part * a.cols + u.first;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 f = unpack2(acc[v][i / 2]);
+        if (u.first + i >= 0 && u.first + i < (int32_t)a.cols) to[i] = i % 2 ? f.y : f.x;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
 // How a row lies over threads.
 
 struct Shape {
@@ -722,11 +1216,11 @@ struct Shape {
   bool fits;                 // a group holds the row
 };
 
-Shape shape_of(uint32_t cols, bool few) {
+Shape shape_of(uint32_t cols, int v) {
   Shape s;
-  s.v = few && cols <= 8192 ? 1 : 2;
+  s.v = v;
   const uint32_t per = 256 * s.v, warps = (cols + per - 1) / per;
-  s.fits = warps <= 32;
+  s.fits = warps <= (v == 4 ? 16u : 32u);
   s.threads = 32 * (s.fits ? warps : 32);
   s.groups = s.threads >= 256 ? 1 : 256 / s.threads;
   return s;
@@ -741,6 +1235,57 @@ unsigned grid_of(uint64_t want, uint32_t per_sm) {
 
 bool aligned(const void *p, int64_t pitch_bytes) { return (uintptr_t)p % 16 == 0 && pitch_bytes % 16 == 0; }
 
+// Rows that many, and alike within 16 bytes: the ring's shape, or none (threads 0).
+struct RingShape {
+  uint32_t threads;
+  int v;
+  bool whole;
+  Ring ring;
+};
+
+RingShape ring_shape(const void *x, int64_t pitch, uint32_t rows, uint32_t cols, uint32_t size, uint32_t mats, unsigned sms, bool alike) {
+  RingShape s = {};
+  const bool begins = aligned(x, pitch * size);  // rows begin at blocks
+  const uint32_t units = (cols + (begins ? 0 : 7) + 7) / 8;
+  s.whole = begins && cols % 8 == 0;
+  if (!alike || rows <= 2 * sms || cols <= 512 || units > 4 * kRingThreads) return s;
+  s.v = units <= 2 * kRingThreads ? 2 : 4;
+  s.threads = 32 * ((units + 32 * s.v - 1) / (32 * s.v));
+  s.ring.region = (cols * size + 15 + 15) / 16 * 16 + 16;
+  s.ring.mats = mats;
+  s.ring.weights = s.threads * s.v * 32;
+  s.ring.edges = ((uintptr_t)x % 16 != 0) | (((uintptr_t)x + ((int64_t)(rows - 1) * pitch + cols) * size) % 16 != 0) << 1;
+  for (s.ring.stages = 3; s.ring.stages > 1 && s.ring.bytes() > 220 * 1024; --s.ring.stages) {}
+  if (s.ring.stages < 2) s.threads = 0;
+  return s;
+}
+
+// The launch of a ring kernel: persistent, in so many CTAs as an SM holds, rows of a CTA
+// beginning alike where the grid allows.
+template <typename K, typename A>
+int ring_launch(K kernel, const A &a, RingShape s, uint32_t work, uint32_t period, void *stream) {
+  const uint32_t bytes = s.ring.bytes();
+  int e = commit_status_word(&s.ring.status), per_sm = 1;
+  if (!e) e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (!e) e = (int)cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, (int)s.threads, bytes);
+  if (e) return e;
+  unsigned grid = grid_of(work, (uint32_t)per_sm);
+  if (grid < work && grid > period) grid -= grid % period;
+  kernel<<<grid, s.threads, bytes, (cudaStream_t)stream>>>(a, s.ring);
+  return (int)cudaGetLastError();
+}
+
+// Rows after which a matrix's place within 16 bytes repeats.
+uint32_t period_of(int64_t pitch_bytes) {
+  uint32_t n = 1;
+  while (n < 16 && pitch_bytes * n % 16) n *= 2;
+  return n;
+}
+
+bool same_place(const void *p, int64_t pitch_bytes, const void *q, int64_t q_pitch_bytes) {
+  return !q || (((uintptr_t)p ^ (uintptr_t)q) % 16 == 0 && (pitch_bytes - q_pitch_bytes) % 16 == 0);
+}
+
 template <typename T, int OUT, int V, bool WIDE, bool LONG>
 int forward_launch(const ForwardArgs &a, const Shape &s, void *stream) {
   const uint32_t per = s.threads * s.groups;
@@ -751,7 +1296,15 @@ int forward_launch(const ForwardArgs &a, const Shape &s, void *stream) {
 }
 
 template <typename T, int OUT>
-int forward(const ForwardArgs &a, const Shape &s, bool wide, void *stream) {
+int forward(const ForwardArgs &a, const Shape &s, const RingShape &ring, bool wide, void *stream) {
+  if (ring.threads) {
+    const uint32_t period = period_of(a.pitch * (int64_t)sizeof(T));
+    if (ring.whole)
+      return ring.v == 2 ? ring_launch(ring_forward_kernel<T, OUT, 2, true>, a, ring, a.rows, period, stream)
+                         : ring_launch(ring_forward_kernel<T, OUT, 4, true>, a, ring, a.rows, period, stream);
+    return ring.v == 2 ? ring_launch(ring_forward_kernel<T, OUT, 2, false>, a, ring, a.rows, period, stream)
+                       : ring_launch(ring_forward_kernel<T, OUT, 4, false>, a, ring, a.rows, period, stream);
+  }
   if (!s.fits) return wide ? forward_launch<T, OUT, 2, true, true>(a, s, stream) : forward_launch<T, OUT, 2, false, true>(a, s, stream);
   if (s.v == 1) return wide ? forward_launch<T, OUT, 1, true, false>(a, s, stream) : forward_launch<T, OUT, 1, false, false>(a, s, stream);
   return wide ? forward_launch<T, OUT, 2, true, false>(a, s, stream) : forward_launch<T, OUT, 2, false, false>(a, s, stream);
@@ -774,14 +1327,19 @@ int launch_rms_norm(const NormArgs &n, unsigned sms, void *stream) {
   a.weight_aligned = (uintptr_t)n.weight % 16 == 0;
   two_parts(1.0 / n.cols, &a.c.inv_hi, &a.c.inv_lo);
   two_parts(n.eps, &a.c.eps_hi, &a.c.eps_lo);
-  const Shape s = shape_of(n.cols, n.rows <= sms);
+  const Shape s = shape_of(n.cols, n.rows <= sms && n.cols <= 8192 ? 1 : 2);
   return with_dtype(n.dtype, [&](auto t) {
     using T = decltype(t);
     const auto at = [](const void *p, int64_t pitch) { return aligned(p, pitch * (int64_t)sizeof(T)); };
     const bool wide = at(n.x, n.pitch) && at(n.residual, n.residual_pitch) && at(n.sum, n.sum_pitch) && at(n.out, n.out_pitch);
+    const auto alike = [&](const void *p, int64_t pitch) {
+      return same_place(n.x, n.pitch * (int64_t)sizeof(T), p, pitch * (int64_t)sizeof(T));
+    };
+    const RingShape ring = ring_shape(n.x, n.pitch, n.rows, n.cols, sizeof(T), n.residual ? 2 : 1, sms,
+                                      alike(n.residual, n.residual_pitch) && alike(n.sum, n.sum_pitch) && alike(n.out, n.out_pitch));
     int e;
-    if (n.out) e = forward<T, kSame>(a, s, wide, stream);
-    else e = n.q.e5m2 ? forward<T, kE5M2>(a, s, wide, stream) : forward<T, kE4M3>(a, s, wide, stream);
+    if (n.out) e = forward<T, kSame>(a, s, ring, wide, stream);
+    else e = n.q.e5m2 ? forward<T, kE5M2>(a, s, ring, wide, stream) : forward<T, kE4M3>(a, s, ring, wide, stream);
     if (e || !n.qt.data) return e;
     TurnArgs r = {};
     r.h = n.residual ? n.sum : n.x, r.weight = n.weight, r.rstd = n.rstd;
@@ -790,9 +1348,11 @@ int launch_rms_norm(const NormArgs &n, unsigned sms, void *stream) {
     r.rows = n.rows, r.cols = n.cols, r.wdtype = n.wdtype;
     r.weight_aligned = a.weight_aligned;
     r.wide = at(r.h, r.pitch);
-    const unsigned grid = grid_of((uint64_t)((n.cols + kBlock - 1) / kBlock) * ((n.rows + kBlock - 1) / kBlock), 2);
-    if (n.qt.e5m2) turn_kernel<T, true><<<grid, 256, 0, (cudaStream_t)stream>>>(r);
-    else turn_kernel<T, false><<<grid, 256, 0, (cudaStream_t)stream>>>(r);
+    const auto turn = n.qt.e5m2 ? turn_kernel<T, true> : turn_kernel<T, false>;
+    constexpr uint32_t bytes = 128 * 128 * sizeof(T);
+    if ((e = (int)cudaFuncSetAttribute(turn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes))) return e;
+    turn<<<grid_of((uint64_t)((n.cols + kBlock - 1) / kBlock) * ((n.rows + kBlock - 1) / kBlock), sizeof(T) == 4 ? 2 : 4), 256, bytes,
+           (cudaStream_t)stream>>>(r);
     return (int)cudaGetLastError();
   });
 }
@@ -803,7 +1363,7 @@ uint32_t rms_norm_parts(uint32_t rows, uint32_t cols) {
   return rows < parts ? rows : parts;
 }
 
-int launch_rms_norm_grad(const NormGradArgs &n, void *stream) {
+int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
   GradArgs a = {};
   a.dout = n.dout, a.x = n.x, a.weight = n.weight, a.dresidual = n.dresidual, a.rstd = n.rstd, a.dx = n.dx;
   a.partial = n.dweight ? n.work : nullptr;
@@ -813,7 +1373,7 @@ int launch_rms_norm_grad(const NormGradArgs &n, void *stream) {
   a.weight_aligned = (uintptr_t)n.weight % 16 == 0;
   a.inv_cols = (float)(1.0 / n.cols);
   cudaStream_t s = (cudaStream_t)stream;
-  const Shape sh = shape_of(n.cols, false);
+  const Shape sh = shape_of(n.cols, n.cols <= 8192 ? 2 : 4);
   const int e = !n.rows ? 0 : with_dtype(n.dtype, [&](auto t) {
     using T = decltype(t);
     const auto at = [](const void *p, int64_t pitch) { return aligned(p, pitch * (int64_t)sizeof(T)); };
@@ -822,12 +1382,31 @@ int launch_rms_norm_grad(const NormGradArgs &n, void *stream) {
       if (a.partial) grad_long_parts_kernel<T><<<grid_of((uint64_t)((n.cols + 255) / 256) * a.parts, 8), 256, 0, s>>>(a);
       return (int)cudaGetLastError();
     }
+    const auto alike = [&](const void *p, int64_t pitch) {
+      return same_place(n.x, n.pitch * (int64_t)sizeof(T), p, pitch * (int64_t)sizeof(T));
+    };
+    const RingShape ring = ring_shape(n.x, n.pitch, n.rows, n.cols, sizeof(T), n.dresidual ? 3 : 2, sms,
+                                      alike(n.dout, n.dout_pitch) && alike(n.dresidual, n.dresidual_pitch) && alike(n.dx, n.dx_pitch));
+    if (ring.threads) {
+      const uint32_t period = period_of(n.pitch * (int64_t)sizeof(T));
+      if (ring.whole)
+        return ring.v == 2 ? ring_launch(ring_grad_kernel<T, 2, true>, a, ring, a.parts, period, stream)
+                           : ring_launch(ring_grad_kernel<T, 4, true>, a, ring, a.parts, period, stream);
+      return ring.v == 2 ? ring_launch(ring_grad_kernel<T, 2, false>, a, ring, a.parts, period, stream)
+                         : ring_launch(ring_grad_kernel<T, 4, false>, a, ring, a.parts, period, stream);
+    }
     const bool wide = at(n.x, n.pitch) && at(n.dout, n.dout_pitch) && at(n.dresidual, n.dresidual_pitch) && at(n.dx, n.dx_pitch);
     const uint32_t per = sh.threads * sh.groups;
     const unsigned grid = grid_of((a.parts + sh.groups - 1) / sh.groups, 1024 / per);
     const size_t room = sizeof(float) * 2 * per / 32;
-    if (wide) grad_kernel<T, 2, true><<<grid, dim3(sh.threads, sh.groups), room, s>>>(a);
-    else grad_kernel<T, 2, false><<<grid, dim3(sh.threads, sh.groups), room, s>>>(a);
+    const dim3 block(sh.threads, sh.groups);
+    if (sh.v == 2) {
+      if (wide) grad_kernel<T, 2, true><<<grid, block, room, s>>>(a);
+      else grad_kernel<T, 2, false><<<grid, block, room, s>>>(a);
+    } else {
+      if (wide) grad_kernel<T, 4, true><<<grid, block, room, s>>>(a);
+      else grad_kernel<T, 4, false><<<grid, block, room, s>>>(a);
+    }
     return (int)cudaGetLastError();
   });
   if (e || !n.dweight) return e;

@@ -20,6 +20,8 @@ TINY = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -133, torch.float16: 
 TYPES = [torch.bfloat16, torch.float16, torch.float32]
 SIZES = [(1, 1), (1, 8), (3, 7), (5, 128), (2, 129), (7, 255), (9, 1000), (1, 4096), (33, 4096), (2, 4099), (1, 8192), (160, 2048),
          (200, 5003), (300, 64), (700, 264), (5, 16384), (3, 16385), (2, 40001)]
+# enough rows to walk them: (rows, columns)
+MANY = [(305, 513), (700, 1000), (400, 1024), (333, 4096), (1000, 2047), (350, 5003), (306, 9001), (310, 16384), (320, 16377)]
 
 
 def gen(seed):
@@ -54,15 +56,15 @@ def y_of(h, rstd, w):
     return h.float() * rstd[:, None] * w.float()
 
 
-@pytest.mark.parametrize("r,c", SIZES)
+@pytest.mark.parametrize("r,c", SIZES + MANY)
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("residual", [False, True])
 def test_norm(r, c, dtype, residual):
-    for k, wdtype in enumerate(dict.fromkeys([dtype, torch.float32])):
+    # packed; at odds with each other; alike within 16 bytes, but at no boundary
+    for extra, offset, wdtype in ((0, 0, dtype), (5 if c % 2 else 8, 3 if c % 2 else 8, torch.float32), (8, 3, dtype)):
         x, res, w = inputs(r, c, dtype, wdtype)
-        extra, offset = ((0, 0), (5, 3))[k] if c % 2 else ((0, 0), (8, 8))[k]
         x, res = strided(x, extra, offset), strided(res, 2 * extra, offset) if residual else None
-        total = strided(torch.zeros_like(x), extra, 0) if residual else None
+        total = strided(torch.zeros_like(x), extra, offset if extra == 8 else 0) if residual else None
         out = strided(torch.zeros_like(x), 3 * extra, offset)
         y, h, rstd = apc.rms_norm(x, w, eps=1e-5, residual=res, out=out, sum=total)
         assert y is out and rstd.shape == (r,) and rstd.dtype == torch.float32
@@ -74,7 +76,7 @@ def test_norm(r, c, dtype, residual):
         assert surround.isnan().all()  # what lies behind the columns is left as it was
 
 
-@pytest.mark.parametrize("r,c", SIZES)
+@pytest.mark.parametrize("r,c", SIZES + MANY)
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("fmt", [torch.float8_e4m3fn, torch.float8_e5m2])
 @pytest.mark.parametrize("transposed", [False, True])
@@ -83,7 +85,11 @@ def test_norm_to_8_bits(r, c, dtype, fmt, transposed):
     res = res if r % 2 else None
     if c % 3 == 0:
         x = strided(x, 3, 1)
-    *got, h, rstd = apc.rms_norm_fp8(x, w, eps=1e-6, residual=res, dtype=fmt, transposed=transposed)
+    elif c % 3 == 1:  # alike, at no boundary
+        x, res = strided(x, 8, 5), None if res is None else strided(res, 16, 5)
+    total = None if res is None else strided(torch.zeros_like(x), 0, x.storage_offset()) if c % 3 == 1 else torch.empty_like(res)
+    *got, h, rstd = apc.rms_norm_fp8(x, w, eps=1e-6, residual=res, sum=total, dtype=fmt, transposed=transposed)
+    assert torch.equal(h, x if res is None else (x.float() + res.float()).to(dtype))
     check_rstd(h, 1e-6, rstd)
     want = apc.quantize_fp8(y_of(h, rstd, w), dtype=fmt, transposed=transposed)
     assert len(got) == len(want)
@@ -108,11 +114,12 @@ def test_same_bits_however_rows_lie():
     assert ((a[2] - b[2]).abs() <= 2 * 2 * U * a[2]).all()
 
 
-def test_norm_does_not_depend_on_the_grid(monkeypatch):
-    x, res, w = inputs(700, 1000, torch.bfloat16, torch.float32)
+@pytest.mark.parametrize("c", [264, 1000, 1003])
+def test_norm_does_not_depend_on_the_grid(monkeypatch, c):
+    x, res, w = inputs(1500, c, torch.bfloat16, torch.float32)
     a = apc.rms_norm_fp8(x, w, residual=res, transposed=True)
     d = apc.rms_norm_grad(res, x, w, a[-1])
-    for limit in ("1", "7"):
+    for limit in ("1", "7", "100"):
         monkeypatch.setenv("APC_GRID_LIMIT", limit)
         for p, q in zip(a, apc.rms_norm_fp8(x, w, residual=res, transposed=True)):
             assert torch.equal(p.float(), q.float())
@@ -122,8 +129,8 @@ def test_norm_does_not_depend_on_the_grid(monkeypatch):
 
 @pytest.mark.parametrize("place", ["x", "residual"])
 def test_sum_in_place(place):
-    for c in (1000, 40_000):
-        x, res, w = inputs(9, c, torch.bfloat16, torch.bfloat16)
+    for r, c in ((9, 1000), (9, 40_000), (400, 1000), (400, 1003)):
+        x, res, w = inputs(r, c, torch.bfloat16, torch.bfloat16)
         want = apc.rms_norm(x, w, residual=res)
         a, b = x.clone(), res.clone()
         got = apc.rms_norm(a, w, residual=b, sum=a if place == "x" else b)
@@ -131,10 +138,11 @@ def test_sum_in_place(place):
             assert torch.equal(p, q)
 
 
-@pytest.mark.parametrize("c", [100, 1000, 4096, 20_000])
-def test_rows_of_huge_values(c):
+@pytest.mark.parametrize("r", [6, 400])
+@pytest.mark.parametrize("c", [100, 1000, 4096, 5003, 20_000])
+def test_rows_of_huge_values(r, c):
     """Squares that overflow binary32 are taken scaled; beside them ordinary rows, and tiny ones that eps rules."""
-    x, _, w = inputs(6, c, torch.float32, torch.float32)
+    x, _, w = inputs(r, c, torch.float32, torch.float32)
     x[0] *= 1e25
     x[1] *= 1e-25
     x[2] = 0
@@ -148,10 +156,11 @@ def test_rows_of_huge_values(c):
         assert ((y.double() - want).abs() <= (UNIT[dtype] + 3 * U) * want.abs() + TINY[dtype] * 2).all()
 
 
+@pytest.mark.parametrize("r", [8, 400])
 @pytest.mark.parametrize("c", [100, 4096, 5003, 20_000])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-def test_rows_that_are_not_finite(c, dtype):
-    x, res, w = inputs(8, c, dtype, dtype)
+def test_rows_that_are_not_finite(r, c, dtype):
+    x, res, w = inputs(r, c, dtype, dtype)
     x[1, c // 2] = math.inf
     x[3, 7] = math.nan
     x[5, c - 1] = -math.inf
@@ -159,7 +168,7 @@ def test_rows_that_are_not_finite(c, dtype):
     res[6, 3] = -math.inf  # their sum is a NaN
     y, h, rstd = apc.rms_norm(x, w, residual=res)
     assert rstd[[1, 5]].eq(0).all() and rstd[[3, 6]].isnan().all()
-    fine = [0, 2, 4, 7]
+    fine = [0, 2, 4, 7, r - 1]
     check_rstd(h[fine], 1e-6, rstd[fine])
     want = y_of(h, rstd, w).to(dtype)
     assert torch.equal(y.isnan(), want.isnan()) and torch.equal(y.nan_to_num(), want.nan_to_num())
@@ -210,18 +219,22 @@ def check_grad(d, x, w, rstd, dres, dx, dw, eps_rows):
         assert ((dw.double() - want).abs() <= k * U * size + UNIT[dw.dtype] * want.abs() + TINY[dw.dtype]).all()
 
 
-@pytest.mark.parametrize("r,c", SIZES + [(3000, 200), (1500, 4096)])
+@pytest.mark.parametrize("r,c", SIZES + MANY + [(3000, 200), (1500, 4096), (3000, 999)])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_grad(r, c, dtype):
-    for k, wdtype in enumerate(dict.fromkeys([dtype, torch.float32])):
+    for k, wdtype in enumerate((dtype, torch.float32, dtype)):
         x, d, w = inputs(r, c, dtype, wdtype, 2)
         d = (d * 1e-2).to(dtype)
         if r > 2:
             d[1] = 0  # a position that does not count
         dres = None if k == 0 else torch.randn(r, c, generator=gen(5), device="cuda").mul_(1e-2).to(dtype)
         rstd = apc.rms_norm(x, w)[2]
-        extra, offset = ((0, 0), (5, 3))[k]
-        dx, dw = apc.rms_norm_grad(strided(d, extra, offset), strided(x, 2 * extra, 0), w, rstd, dresidual=dres)
+        # packed; at odds with each other; alike within 16 bytes, but at no boundary
+        extra, offset, at = ((0, 0, 0), (5, 3, 0), (8, 5, 5))[k]
+        out = strided(torch.zeros_like(x), extra, at)
+        dx, dw = apc.rms_norm_grad(strided(d, extra, offset), strided(x, 2 * extra, at), w, rstd, out=out,
+                                   dresidual=None if dres is None else strided(dres, extra, offset))
+        assert out.as_strided((r, c + extra), (c + extra, 1), out.storage_offset())[:, c:].isnan().all()
         assert dx.dtype == dtype and dw.dtype == wdtype
         parts = apc.operators.rms_norm_grad_workspace(r, c) // c
         check_grad(d, x, w, rstd, dres, dx, dw, parts)
@@ -232,15 +245,16 @@ def test_grad(r, c, dtype):
         check_grad(d, x, w, rstd, dres, only, None, parts)
 
 
-def test_grad_in_place_and_types():
-    x, d, w = inputs(300, 1000, torch.bfloat16, torch.bfloat16)
+@pytest.mark.parametrize("r,c", [(9, 1000), (300, 1000), (700, 1003), (400, 9000)])
+def test_grad_in_place_and_types(r, c):
+    x, d, w = inputs(r, c, torch.bfloat16, torch.bfloat16)
     rstd = apc.rms_norm(x, w)[2]
     dres = d * 0.5
-    want = apc.rms_norm_grad(d, x, w, rstd, dresidual=dres, dweight=torch.empty(1000, device="cuda"))
+    want = apc.rms_norm_grad(d, x, w, rstd, dresidual=dres, dweight=torch.empty(c, device="cuda"))
     for place in ("dout", "dresidual"):
         a, b = d.clone(), dres.clone()
         got = apc.rms_norm_grad(a, x, w, rstd, dresidual=b, out=a if place == "dout" else b,
-                                dweight=torch.empty(1000, dtype=torch.half, device="cuda"))
+                                dweight=torch.empty(c, dtype=torch.half, device="cuda"))
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1].half())
 
 
