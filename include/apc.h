@@ -217,7 +217,11 @@ apc_status apc_digest(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slot
 apc_status apc_count_nonzero(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots, apc_stream_t stream,
                              uint64_t *out_counts);
 
-#define APC_GRAD_NORM_WORKSPACE 2056 /* bytes */
+#define APC_GRAD_NORM_WORKSPACE 2056 /* bytes, at most */
+
+/* Bytes that apc_grad_norm's workspace takes for such a list: 0 (a small list, up to some
+ * 6 million 16-bit elements) or APC_GRAD_NORM_WORKSPACE.  Host only, no CUDA call. */
+int64_t apc_grad_norm_workspace(const apc_buffer *bufs, int32_t num_bufs);
 
 /* The 2-norm of the elements of a list of buffers, read only: the norm of a
  * step's gradients, by which apc_commit_step_clipped clips them.
@@ -229,11 +233,13 @@ apc_status apc_count_nonzero(const apc_buffer *bufs, int32_t num_bufs, int32_t n
  * overflow or vanish.  A slot with a NaN gives NaN, one with an infinity infinity; one
  * without elements 0.
  *   bufs       as for apc_digest, of any apc_dtype, any alignment to their elements
- *              (global_offset is ignored)
+ *              (global_offset is ignored); n at most 2^40
  *   workspace  device, 8-byte aligned, APC_GRAD_NORM_WORKSPACE bytes that no other
- *              call uses before this one has completed; need not be initialised
+ *              call uses before this one has completed; need not be initialised.  NULL
+ *              where apc_grad_norm_workspace gives 0
  *   out_norms  device, fp32, num_slots of them
- * Errors as apc_digest. */
+ * Errors as apc_digest.  A small list runs on one cluster of up to 16 CTAs, whatever
+ * APC_GRID_LIMIT and apc_set_reserved_sms say. */
 apc_status apc_grad_norm(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots, void *workspace, apc_stream_t stream,
                          float *out_norms);
 
@@ -368,14 +374,16 @@ typedef struct apc_norm_grad {
   uint32_t dtype, weight_dtype;
 } apc_norm_grad;
 
-/* Bytes of the workspace: host only, no CUDA call; 0 for sizes out of range. */
+/* Bytes of the workspace: host only, no CUDA call; 0 for few rows, which take none, and for
+ * sizes out of range. */
 int64_t apc_rms_norm_grad_workspace(int64_t rows, int64_t cols);
 
 /* dx (rows x cols, x's type) may be dout's or dresidual's own memory with the same pitch.
  * dweight: cols values of dweight_dtype, or NULL with workspace NULL: not wanted; without
  * rows it is zeros.  workspace: device, 4-byte aligned, apc_rms_norm_grad_workspace bytes
- * that no other call uses before this one has completed; need not be initialised.
- * Errors as apc_quantize_fp8. */
+ * that no other call uses before this one has completed; need not be initialised; NULL where
+ * those are 0.  Few rows with dweight run on one cluster of up to 16 CTAs, whatever
+ * APC_GRID_LIMIT and apc_set_reserved_sms say.  Errors as apc_quantize_fp8. */
 apc_status apc_rms_norm_grad(const apc_norm_grad *d, void *dx, int64_t dx_pitch, void *dweight, uint32_t dweight_dtype,
                              float *workspace, apc_stream_t stream);
 

@@ -129,6 +129,8 @@ def library():
         lib.apc_commit_step_clipped.restype = ctypes.c_int
         lib.apc_commit_step_bf16_clipped.argtypes = [vp, i32, vp, i64, u32, vp, ctypes.c_double, vp, vp]
         lib.apc_commit_step_bf16_clipped.restype = ctypes.c_int
+        lib.apc_grad_norm_workspace.argtypes = [vp, i32]
+        lib.apc_grad_norm_workspace.restype = i64
         lib.apc_grad_norm.argtypes = [vp, i32, i32, vp, vp, vp]
         lib.apc_grad_norm.restype = ctypes.c_int
         lib.apc_quantize_fp8.argtypes = [vp, i64, i64, i64, u32, vp, vp, vp]
@@ -280,7 +282,8 @@ class PreparedTable:
 
     def __init__(self, kind: str, arr, count: int, first, keep: list):
         self.kind, self.arr, self.count, self.first, self._keep = kind, arr, count, first, keep
-        self.grads = None  # a commit table's gradients as a buffer list, once grad_norm has asked for it
+        # for grad_norm: a commit table's gradients as a buffer list, once asked for; the bytes of its workspace
+        self.grads = self.work = None
 
     def __len__(self) -> int:
         return self.count
@@ -401,6 +404,7 @@ def _grads(grads):
             for i in range(grads.count):
                 arr[i] = _Buffer(grads.arr[i].g, grads.arr[i].n, 0, BF16, 0)
             grads.grads = arr
+            grads.work = library().apc_grad_norm_workspace(ctypes.addressof(arr), grads.count)
         return grads.grads, grads.count, grads.first
     grads = list(grads)
     arr = (_Buffer * max(1, len(grads)))()
@@ -435,7 +439,9 @@ def prepare_grads(grads) -> PreparedTable:
     """Marshal a gradient list once for :func:`grad_norm`."""
     grads = list(grads)
     arr, n, first = _grads(grads)
-    return PreparedTable("grads", arr, n, first, grads)
+    out = PreparedTable("grads", arr, n, first, grads)
+    out.work = library().apc_grad_norm_workspace(ctypes.addressof(arr), n)
+    return out
 
 
 def grad_norm(grads, num_slots: int = 1, stream=None, out=None, workspace=None):
@@ -447,16 +453,18 @@ def grad_norm(grads, num_slots: int = 1, stream=None, out=None, workspace=None):
 
     Returns the device float32[num_slots] tensor of norms.  ``workspace``:
     ``GRAD_NORM_WORKSPACE`` bytes for a caller that keeps its own, which no
-    other call may use at the same time."""
-    arr, n, first = _grads(grads)
+    other call may use at the same time; short lists take none."""
     import torch
-    dev = first.device if hasattr(first, "device") else torch.device("cuda", torch.cuda.current_device())
+    arr, n, first = _grads(grads)
+    if out is None or workspace is None:
+        dev = first.device if hasattr(first, "device") else torch.device("cuda", torch.cuda.current_device())
     if out is None:
         out = _empty(num_slots, torch.float32, dev, stream)
     elif not isinstance(out, int) and (out.dtype != torch.float32 or out.numel() < num_slots):
         raise ValueError("out: expected %d float32 values, got %s of %s" % (num_slots, tuple(out.shape), out.dtype))
     if workspace is None:
-        workspace = _empty(GRAD_NORM_WORKSPACE // 8, torch.int64, dev, stream)
+        bytes = grads.work if isinstance(grads, PreparedTable) else library().apc_grad_norm_workspace(ctypes.addressof(arr), n)
+        workspace = _empty(bytes // 8, torch.int64, dev, stream) if bytes else None
     elif not isinstance(workspace, int) and workspace.numel() * workspace.element_size() < GRAD_NORM_WORKSPACE:
         raise ValueError("workspace holds fewer than %d bytes" % GRAD_NORM_WORKSPACE)
     _check(library().apc_grad_norm(ctypes.addressof(arr), n, int(num_slots), _ptr(workspace), _stream(stream), _ptr(out)))

@@ -20,9 +20,10 @@
 #include <cuda_runtime.h>
 
 #include "../../include/apc.h"
+#include "apc_cluster.cuh"
 #include "apc_device.cuh"
 #include "apc_internal.h"
-#include "apc_launch.cuh"
+#include "apc_tma.cuh"
 
 namespace apc {
 namespace {
@@ -124,16 +125,14 @@ __device__ __forceinline__ void add_tile(const uint4 (&x)[kNormGroups], uint64_t
 }
 
 // The aligned 16-byte block at p, with what lies outside [lo, hi) as zeros.
-__device__ __noinline__ uint4 edge_block(const uint8_t *p, const uint8_t *lo, const uint8_t *hi) {
-  uint32_t w[4] = {0, 0, 0, 0};
-  for (int i = 0; i < 16; i += 2)
-    if (p + i >= lo && p + i < hi) w[i / 4] |= (uint32_t)*reinterpret_cast<const uint16_t *>(p + i) << (i % 4 * 8);
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
 __device__ __forceinline__ uint4 block(const uint8_t *p, const uint8_t *lo, const uint8_t *hi) {
+  if (p + 16 <= lo || p >= hi) return make_uint4(0, 0, 0, 0);
   if (p >= lo && p + 16 <= hi) return __ldcs(reinterpret_cast<const uint4 *>(p));
-  return p + 16 > lo && p < hi ? edge_block(p, lo, hi) : make_uint4(0, 0, 0, 0);
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (p + 2 * i >= lo && p + 2 * i < hi) w[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t *>(p + 2 * i) << (i % 2 * 16);
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // 16 bytes from byte `off` (1 to 15, even) of two neighbouring blocks.
@@ -152,30 +151,63 @@ __device__ __forceinline__ uint4 cut(uint4 a, uint4 b, uint32_t off) {
                     __funnelshift_r(w[3], w[4], bits));
 }
 
-// A warp's tile that begins at `at` in a buffer that ends at `end`: zeros behind the end.
-__device__ __forceinline__ void load_tile(uint4 (&x)[kNormGroups], const uint8_t *at, const uint8_t *lo, const uint8_t *end,
-                                          uint32_t lane) {
+// A tile that begins at no 16-byte boundary or ends with its buffer: the blocks that hold it,
+// and a lane's chunk cut from its own and the next lane's, four shuffles each (60 M in 291 odd
+// entries 32 us; 45 with the second block loaded again).  Zeros behind the end.
+template <uint32_t DTYPE>
+__device__ __noinline__ uint64_t other_tile(const uint8_t *at, const uint8_t *lo, const uint8_t *end, uint64_t word, uint32_t lane) {
   const uint32_t off = (uint32_t)((uintptr_t)at & 15);
-  if (off == 0 && at + kNormTileBytes <= end) {
+  const uint8_t *p = at - off + 16 * lane;
+  uint4 x[kNormGroups], more = make_uint4(0, 0, 0, 0);  // more: lane 0's block behind lane 31's last
+  if (at - off >= lo && at - off + kNormTileBytes + 16 <= end) {
+#pragma unroll
+    for (int j = 0; j < kNormGroups; ++j) x[j] = __ldcs(reinterpret_cast<const uint4 *>(p) + j * 32);
+    if (lane == 0) more = __ldcs(reinterpret_cast<const uint4 *>(p + kNormTileBytes));
+  } else {
+#pragma unroll
+    for (int j = 0; j < kNormGroups; ++j) x[j] = block(p + j * 512, lo, end);
+    if (lane == 0 && off) more = block(p + kNormTileBytes, lo, end);
+  }
+  if (off) {
+    const int next = (int)(lane + 1) & 31;
+#pragma unroll
+    for (int j = 0; j < kNormGroups; ++j) {
+      const uint4 from = lane ? x[j] : j + 1 < kNormGroups ? x[(j + 1) % kNormGroups] : more;
+      x[j] = cut(x[j], make_uint4(__shfl_sync(~0u, from.x, next), __shfl_sync(~0u, from.y, next), __shfl_sync(~0u, from.z, next),
+                                  __shfl_sync(~0u, from.w, next)), off);
+    }
+  }
+  add_tile<DTYPE>(x, word, lane);
+  return word;
+}
+
+template <uint32_t DTYPE>
+__device__ __noinline__ uint64_t awkward_tile(const uint8_t *at, uint64_t word, uint32_t lane) {
+  uint4 x[kNormGroups];
+#pragma unroll
+  for (int j = 0; j < kNormGroups; ++j) x[j] = __ldcs(reinterpret_cast<const uint4 *>(at) + j * 32 + lane);
+  awkward<DTYPE>(x, word, lane);
+  return word;
+}
+
+// The tiles at `at`, `at` + step, ... of a buffer, `count` of them, into the lanes' words.
+template <uint32_t DTYPE>
+__device__ __forceinline__ uint64_t add_tiles(const uint8_t *at, const uint8_t *lo, const uint8_t *end, uint32_t count, uint32_t step,
+                                              uint64_t word, uint32_t lane) {
+  const bool aligned = ((uintptr_t)at & 15) == 0;
+  for (; count; --count, at += step) {
+    if (!aligned || at + kNormTileBytes > end) {
+      word = other_tile<DTYPE>(at, lo, end, word, lane);
+      continue;
+    }
+    uint4 x[kNormGroups];
 #pragma unroll
     for (int j = 0; j < kNormGroups; ++j) x[j] = __ldcs(reinterpret_cast<const uint4 *>(at) + j * 32 + lane);
-    return;
+    const float s = warp_squares<DTYPE, false>(x, 1.0f);
+    if (s >= 0x1p-90f && s <= 3.402823466e38f) add_exact(word, s, 0, lane);
+    else word = awkward_tile<DTYPE>(at, word, lane);
   }
-  // lane 0 holds one block more: the one behind lane 31's last
-  const uint8_t *p = at - off + 16 * lane;
-#pragma unroll
-  for (int j = 0; j < kNormGroups; ++j) x[j] = block(p + j * 512, lo, end);
-  if (off == 0) return;
-  uint4 more = make_uint4(0, 0, 0, 0);
-  if (lane == 0) more = block(p + kNormTileBytes, lo, end);
-#pragma unroll
-  for (int j = 0; j < kNormGroups; ++j) {
-    const uint4 from = lane ? x[j] : j + 1 < kNormGroups ? x[j + 1] : more;
-    const int next = (int)(lane + 1) & 31;
-    const uint4 b = make_uint4(__shfl_sync(~0u, from.x, next), __shfl_sync(~0u, from.y, next), __shfl_sync(~0u, from.z, next),
-                               __shfl_sync(~0u, from.w, next));
-    x[j] = cut(x[j], b, off);
-  }
+  return word;
 }
 
 // A slot's number as a norm: its words, highest first, in double; one rounding to fp32.
@@ -187,49 +219,82 @@ __device__ __forceinline__ float norm_of(unsigned long long word, uint32_t lane)
   return nan ? __uint_as_float(0x7fffffffu) : inf ? __uint_as_float(0x7f800000u) : (float)sqrt(v);
 }
 
+// The entry whose tiles hold `tile`, at or after entry `lo`.
 template <int MAXE>
-__global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const __grid_constant__ DigestPlan<MAXE> plan,
-                                                               unsigned long long *work, float *out, uint32_t slots) {
-  __shared__ unsigned long long s_bins[APC_MAX_SLOTS][kBins];
+__device__ __forceinline__ uint32_t norm_entry(const NormPlan<MAXE> &plan, uint32_t lo, uint32_t tile) {
+  uint32_t hi = plan.count;
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) >> 1;
+    if (plan.tile_begin[mid] <= tile) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// CLUSTER: all CTAs are one cluster, which joins its numbers in shared memory; no workspace.
+// A small list then takes one launch and nothing else.
+template <int MAXE, bool CLUSTER>
+__global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const __grid_constant__ NormPlan<MAXE> plan, unsigned long long *work,
+                                                               float *out, uint32_t slots) {
+  __shared__ unsigned long long s_bins[APC_MAX_SLOTS * kBins];
   __shared__ bool s_last;
-  if (plan.more) chain_start_next();
+  if (!CLUSTER && plan.more) chain_start_next();
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (threadIdx.x < APC_MAX_SLOTS * kBins) s_bins[threadIdx.x / kBins][threadIdx.x % kBins] = 0;
-  __syncthreads();
-  // this CTA's run of tiles, walked by its warps
-  const uint64_t per = plan.total_tiles / gridDim.x, rem = plan.total_tiles % gridDim.x;
-  const uint64_t t_begin = blockIdx.x * per + (blockIdx.x < rem ? blockIdx.x : rem);
-  const uint32_t len = (uint32_t)(per + (blockIdx.x < rem ? 1 : 0));
-  uint32_t cur = 0, r = warp;
+  if (threadIdx.x < APC_MAX_SLOTS * kBins) s_bins[threadIdx.x] = 0;
+  if (CLUSTER) cluster_arrive();
+  else __syncthreads();
+  // this CTA's run of tiles: its warps walk it interleaved or, where each has few of them, in
+  // runs of their own, over entries that follow one another
+  const uint32_t per = plan.total_tiles / gridDim.x, rem = plan.total_tiles % gridDim.x;
+  const uint32_t t_begin = blockIdx.x * per + min(blockIdx.x, rem), run = per + (blockIdx.x < rem ? 1 : 0);
+  const bool short_run = run < 16 * kWarps;
+  const uint32_t step = short_run ? 1 : kWarps, len = short_run ? run * (warp + 1) / kWarps : run;
+  uint32_t cur = 0, r = short_run ? run * warp / kWarps : warp;
   int slot = -1;
   uint64_t word = 0;
+  bool waited = !CLUSTER;
+  const auto flush_word = [&]() {
+    if (!waited) {
+      cluster_wait();
+      waited = true;
+    }
+    if (slot >= 0 && word) atomicAdd(&s_bins[slot * kBins + lane], (unsigned long long)word);
+    word = 0;
+  };
   while (r < len) {
-    cur = entry_of(plan, cur, t_begin + r);
-    const DigestEntry &E = plan.e[cur];
-    const uint64_t left = (cur + 1 < plan.count ? plan.e[cur + 1].tile_begin : plan.total_tiles) - t_begin;
-    const uint32_t stop = left < len ? (uint32_t)left : len;
-    if ((int)E.slot != slot) {
-      if (slot >= 0 && word) atomicAdd(&s_bins[slot][lane], (unsigned long long)word);
-      word = 0;
-      slot = E.slot;
+    if (slot < 0 || !short_run) cur = norm_entry(plan, cur, t_begin + r);
+    const uint64_t kind = plan.kind[cur];
+    const uint32_t dtype = (uint32_t)(kind & 3), begin = plan.tile_begin[cur];
+    const uint32_t stop = min(len, (cur + 1 < plan.count ? plan.tile_begin[cur + 1] : plan.total_tiles) - t_begin);
+    if ((int)(kind >> 2 & 7) != slot) {
+      flush_word();
+      slot = (int)(kind >> 2 & 7);
     }
-    const uint8_t *lo = static_cast<const uint8_t *>(E.data), *end = lo + E.n * (E.dtype == APC_F32 ? 4 : 2);
-    const uint8_t *at = lo + (t_begin + r - E.tile_begin) * kNormTileBytes;
-    for (; r < stop; r += kWarps, at += kWarps * kNormTileBytes) {
-      uint4 x[kNormGroups];
-      load_tile(x, at, lo, end, lane);
-      if (E.dtype == APC_BF16) add_tile<APC_BF16>(x, word, lane);
-      else if (E.dtype == APC_F32) add_tile<APC_F32>(x, word, lane);
-      else add_tile<APC_F16>(x, word, lane);
-    }
+    const uint8_t *lo = static_cast<const uint8_t *>(plan.data[cur]), *end = lo + (kind >> 5) * (dtype == APC_F32 ? 4 : 2);
+    const uint8_t *at = lo + (uint64_t)(t_begin + r - begin) * kNormTileBytes;
+    const uint32_t count = (stop - r + step - 1) / step;
+    if (dtype == APC_BF16) word = add_tiles<APC_BF16>(at, lo, end, count, step * kNormTileBytes, word, lane);
+    else if (dtype == APC_F32) word = add_tiles<APC_F32>(at, lo, end, count, step * kNormTileBytes, word, lane);
+    else word = add_tiles<APC_F16>(at, lo, end, count, step * kNormTileBytes, word, lane);
+    r += count * step;
+    cur += short_run;
   }
-  if (slot >= 0 && word) atomicAdd(&s_bins[slot][lane], (unsigned long long)word);
+  flush_word();
   __syncthreads();
-  chain_wait();
-  if (threadIdx.x < slots * kBins) {
-    const unsigned long long b = s_bins[threadIdx.x / kBins][threadIdx.x % kBins];
-    if (b) atomicAdd(&work[1 + threadIdx.x], b);
+  if (CLUSTER) {
+    if (cluster_rank() && threadIdx.x < slots * kBins && s_bins[threadIdx.x])
+      asm volatile("red.relaxed.cluster.shared::cluster.add.u64 [%0], %1;" ::"r"(map_rank(smem_addr(&s_bins[threadIdx.x]), 0)),
+                   "l"(s_bins[threadIdx.x])
+                   : "memory");
+    cluster_arrive();
+    cluster_wait();
+    if (cluster_rank() || warp >= slots) return;
+    const float n = norm_of(s_bins[warp * kBins + lane], lane);
+    if (lane == 0) out[warp] = n;
+    return;
   }
+  chain_wait();
+  if (threadIdx.x < slots * kBins && s_bins[threadIdx.x]) atomicAdd(&work[1 + threadIdx.x], s_bins[threadIdx.x]);
   if (!plan.last) return;
   // the last CTA of the last launch: what the others added is behind their tickets
   __threadfence();
@@ -246,25 +311,33 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const __grid_cons
 
 template <int MAXE>
 int launch_n(const void *plan, unsigned grid, void *stream, unsigned long long *work, float *out, unsigned slots) {
-  const DigestPlan<MAXE> &p = *static_cast<const DigestPlan<MAXE> *>(plan);
+  const NormPlan<MAXE> &p = *static_cast<const NormPlan<MAXE> *>(plan);
   cudaLaunchAttribute attr = {};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(kNormThreads);
   cfg.stream = (cudaStream_t)stream;
   cfg.attrs = &attr;
+  if (!work) {
+    cfg.gridDim = dim3(norm_cluster(p.total_tiles));
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim = {cfg.gridDim.x, 1, 1};
+    cfg.numAttrs = 1;
+    const int e = (int)cudaFuncSetAttribute(norm_kernel<MAXE, true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return e ? e : (int)cudaLaunchKernelEx(&cfg, norm_kernel<MAXE, true>, p, work, out, slots);
+  }
+  cfg.gridDim = dim3(grid);
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.numAttrs = p.chained ? 1 : 0;
-  return (int)cudaLaunchKernelEx(&cfg, norm_kernel<MAXE>, p, work, out, slots);
+  return (int)cudaLaunchKernelEx(&cfg, norm_kernel<MAXE, false>, p, work, out, slots);
 }
 
 }  // namespace
 
 int launch_norm(const void *plan, int size, unsigned grid, void *stream, unsigned long long *work, float *out, unsigned slots) {
-  return size == kDigestSmall ? launch_n<kDigestSmall>(plan, grid, stream, work, out, slots)
-         : size == kDigestMid ? launch_n<kDigestMid>(plan, grid, stream, work, out, slots)
-                              : launch_n<kDigestLarge>(plan, grid, stream, work, out, slots);
+  return size == kNormSmall ? launch_n<kNormSmall>(plan, grid, stream, work, out, slots)
+         : size == kNormMid ? launch_n<kNormMid>(plan, grid, stream, work, out, slots)
+                            : launch_n<kNormLarge>(plan, grid, stream, work, out, slots);
 }
 
 }  // namespace apc

@@ -439,7 +439,6 @@ apc_status run_digest_batches(const std::vector<apc::DigestEntry> &entries, Grid
     plan->tiles32 = tiles32;
     plan->more = chain && i + k < entries.size();
     plan->chained = chain && i > 0;
-    plan->last = i + k == entries.size();
     const unsigned grid = (unsigned)std::max<uint64_t>(1, std::min<uint64_t>(std::max<uint64_t>(tiles, k), grid_max.cap));
     int e = launch(*plan, grid);
     if (e) return cuda_fail(e, what);
@@ -916,34 +915,84 @@ apc_status op_grid(int per_sm, unsigned *cap, unsigned *sms) {
   return st;
 }
 
-// The norm kernel's tiles begin at a buffer's first element; the last one may be short.
+namespace {
+
+uint64_t norm_tiles(uint64_t n, uint32_t dtype) { return ceil_div(n * (dtype == APC_F32 ? 4 : 2), kNormTileBytes); }
+
+// Tiles begin at a buffer's first element; the last one may be short.
+template <int MAXE>
+apc_status run_norm_batches(const std::vector<DigestEntry> &entries, Grid grid_max, unsigned long long *work, void *stream, float *out,
+                            unsigned slots, NormLaunch launch) {
+  std::unique_ptr<NormPlan<MAXE>> plan(new NormPlan<MAXE>);  // not cleared: the kernel reads what is filled
+  const bool chain = grid_max.whole && entries.size() > (size_t)MAXE;
+  std::unique_lock<std::mutex> lock;
+  if (chain) lock = std::unique_lock<std::mutex>(chain_lock(stream));
+  for (size_t i = 0, k; i < entries.size(); i += k) {
+    k = std::min(entries.size() - i, (size_t)MAXE);
+    uint64_t tiles = 0;
+    for (size_t j = 0; j < k; ++j) {
+      const DigestEntry &e = entries[i + j];
+      plan->data[j] = e.data;
+      plan->kind[j] = e.n << 5 | (uint64_t)e.slot << 2 | e.dtype;
+      plan->tile_begin[j] = (uint32_t)tiles;
+      tiles += norm_tiles(e.n, e.dtype);
+    }
+    plan->count = (uint32_t)k;
+    plan->total_tiles = (uint32_t)tiles;
+    plan->more = chain && i + k < entries.size();
+    plan->chained = chain && i > 0;
+    plan->last = i + k == entries.size();
+    const unsigned grid = (unsigned)std::max<uint64_t>(1, std::min<uint64_t>(tiles, grid_max.cap));
+    const int e = launch(plan.get(), MAXE, grid, stream, work, out, slots);
+    if (e) return cuda_fail(e, "norm kernel launch");
+  }
+  return APC_OK;
+}
+
+}  // namespace
+
+// Whether the norm of so many buffers of so many tiles takes one launch of a cluster, and no workspace.
+bool norm_is_small(uint64_t count, uint64_t tiles) { return count <= (uint64_t)kNormLarge && tiles <= kNormFewTiles; }
+
 apc_status grad_norm(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots, void *work, apc_stream_t stream, float *out,
                      NormLaunch launch) {
-  if (!work) return fail(APC_EINVAL, "workspace pointer is null");
   if ((uintptr_t)work % 8) return fail(APC_EALIGN, "workspace not 8-byte aligned");
   std::vector<DigestEntry> entries;
   apc_status st = buffer_entries(bufs, num_bufs, num_slots, out, 4, 3, work, APC_GRAD_NORM_WORKSPACE, &entries);
   if (st != APC_OK) return st;
-  Device d;
-  if (!entries.empty() && (st = device_info(&d)) != APC_OK) return st;
   if (entries.empty()) {
     const int e = (int)cudaMemsetAsync(out, 0, (size_t)num_slots * sizeof(float), (cudaStream_t)stream);
     return e ? cuda_fail(e, "cudaMemsetAsync(out_norms)") : APC_OK;
   }
-  const int e = (int)cudaMemsetAsync(work, 0, (1 + (size_t)num_slots * kNormWords) * 8, (cudaStream_t)stream);
-  if (e) return cuda_fail(e, "cudaMemsetAsync(workspace)");
-  for (DigestEntry &en : entries) {
-    en.head = 0;
-    en.tile_begin = en.n;
+  uint64_t tiles = 0;
+  for (size_t k = 0; k < entries.size(); ++k) {
+    if (entries[k].n > (uint64_t)1 << 40) return fail(APC_ERANGE, "a buffer of more than 2^40 elements");
+    tiles += norm_tiles(entries[k].n, entries[k].dtype);
   }
-  return with_plan<kDigestSmall, kDigestMid, kDigestLarge>(entries.size(), [&](auto size) {
-    return run_digest_batches<size.value>(
-        entries, grid_for(d.sms, 1), stream, [](uint64_t n, uint64_t es) { return ceil_div(n * es, kNormTileBytes); },
-        [&](const auto &plan, unsigned grid) {
-          return launch(&plan, size.value, grid, stream, static_cast<unsigned long long *>(work), out, (unsigned)num_slots);
-        },
-        "norm kernel launch");
+  Grid grid{1, false};
+  if (norm_is_small(entries.size(), tiles)) {
+    work = nullptr;
+  } else {
+    if (!work) return fail(APC_EINVAL, "workspace pointer is null");
+    Device d;
+    if ((st = device_info(&d)) != APC_OK) return st;
+    grid = grid_for(d.sms, 1);
+    const int e = (int)cudaMemsetAsync(work, 0, (1 + (size_t)num_slots * kNormWords) * 8, (cudaStream_t)stream);
+    if (e) return cuda_fail(e, "cudaMemsetAsync(workspace)");
+  }
+  return with_plan<kNormSmall, kNormMid, kNormLarge>(entries.size(), [&](auto size) {
+    return run_norm_batches<size.value>(entries, grid, static_cast<unsigned long long *>(work), stream, out, (unsigned)num_slots, launch);
   });
+}
+
+int64_t grad_norm_workspace(const apc_buffer *bufs, int32_t num_bufs) {
+  uint64_t tiles = 0, count = 0;
+  for (int32_t k = 0; bufs && k < num_bufs; ++k) {
+    if (bufs[k].n > (uint64_t)1 << 40) return APC_GRAD_NORM_WORKSPACE;
+    tiles += norm_tiles(bufs[k].n, bufs[k].dtype);
+    count += bufs[k].n != 0;
+  }
+  return norm_is_small(count, tiles) ? 0 : APC_GRAD_NORM_WORKSPACE;
 }
 
 }  // namespace apc

@@ -181,16 +181,26 @@ constexpr int kCountGroups = APC_COUNT_GROUPS;                   // 16-byte load
 constexpr uint32_t kCountTileBytes = 32 * 16 * kCountGroups;     // one warp's tile
 
 // Norm kernel (apc_gradnorm.cu): the count kernel's walk with tiles that are
-// counted from a buffer's first element, whatever its alignment.
+// counted from a buffer's first element, whatever its alignment.  With 128 registers a
+// thread nothing spills and 8 loads a lane are in flight: 152 M bf16 gradients in 146
+// tensors 53 us (59 with 768 threads and 6 loads, 61 with 1024 and 6, 58 with 768 and 8).
 #ifndef APC_NORM_THREADS
-#define APC_NORM_THREADS 1024
+#define APC_NORM_THREADS 512
 #endif
 #ifndef APC_NORM_GROUPS
-#define APC_NORM_GROUPS 6
+#define APC_NORM_GROUPS 8
 #endif
 constexpr int kNormThreads = APC_NORM_THREADS;
 constexpr int kNormGroups = APC_NORM_GROUPS;                  // 16-byte chunks per lane per tile
 constexpr uint32_t kNormTileBytes = 32 * 16 * kNormGroups;    // one warp's tile
+// A small list is one launch of one cluster, a CTA for each kNormClusterTiles tiles: it needs
+// no workspace, and no memset in front of it.
+constexpr uint32_t kNormClusterTiles = 64, kNormClusterMost = 16, kNormFewTiles = 4096;
+inline unsigned norm_cluster(uint64_t tiles) {
+  unsigned n = 1;
+  while (n < kNormClusterMost && n * kNormClusterTiles < tiles) n *= 2;
+  return n;
+}
 constexpr int kNormWords = 32;  // 64-bit words of a slot in the workspace, behind one of all slots
 
 // Minimum resident CTAs per SM the digest kernel is compiled for (its
@@ -208,15 +218,14 @@ constexpr int kNormWords = 32;  // 64-bit words of a slot in the workspace, behi
 //   head: scalar elements before the first 16-byte boundary (<= 7); then
 //         8-element vectors, the whole tiles of which (digest_tile(U) elements
 //         for the digest kernel, kCountTileBytes for the count kernel) are
-//         counted in tile_begin; then a scalar tail.  The norm kernel's tiles
-//         begin at the first element and the last one may be short.
+//         counted in tile_begin; then a scalar tail.
 struct DigestEntry {
   const void *data;
   uint64_t n;
   uint64_t tile_begin;
   uint32_t key_base;
   uint8_t head;
-  uint8_t dtype;        // 0 fp32, 1 bf16, 2 fp16 (norm kernel)
+  uint8_t dtype;        // 0 fp32, 1 bf16
   uint8_t slot;
   uint8_t pad_;
 };
@@ -229,13 +238,28 @@ struct DigestPlan {
   uint32_t one;          // 1: the FMA-pipe carry-add multiplier of the digest
   uint16_t more;         // another launch of the same call follows, chained to this one
   uint16_t chained;      // this one is chained to another of the same call before it
-  uint32_t last;         // the call's last launch
+  uint32_t pad_;
   DigestEntry e[MAXE];
 };
 
 constexpr int kDigestSmall = 16, kDigestMid = 200, kDigestLarge = 1000;
 static_assert(sizeof(DigestEntry) == 32, "entry layout");
 static_assert(sizeof(DigestPlan<kDigestLarge>) <= 32764, "kernel parameter limit");
+
+// Buffers of the norm kernel, 20 bytes each.  kind: apc_dtype, slot << 2, elements << 5.
+template <int MAXE>
+struct NormPlan {
+  uint32_t total_tiles;  // 2^32 are 13 TB
+  uint32_t count;
+  uint16_t more, chained;  // as in DigestPlan
+  uint32_t last;           // the call's last launch
+  const void *data[MAXE];
+  uint64_t kind[MAXE];
+  uint32_t tile_begin[MAXE];
+};
+
+constexpr int kNormSmall = 24, kNormMid = 240, kNormLarge = 1600;
+static_assert(sizeof(NormPlan<kNormLarge>) <= 32764, "kernel parameter limit");
 
 // One segment of the upload kernel (48 bytes): bytes [head, head + body) in
 // 16-byte words of the destination (dst + head is 16-byte aligned, body a

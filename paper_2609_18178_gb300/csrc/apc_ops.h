@@ -34,12 +34,13 @@ apc_status op_ranges(const OpRange *r, int n);
 apc_status op_grid(int per_sm, unsigned *cap, unsigned *sms = nullptr);
 
 // ---- the gradients' norm: planned by apc_host.cpp like the other buffer lists,
-// launched by apc_gradnorm.cu.  plan: a DigestPlan of so many entries.
+// launched by apc_gradnorm.cu.  plan: a NormPlan of so many entries; work null: a small list.
 typedef int (*NormLaunch)(const void *plan, int size, unsigned grid, void *stream, unsigned long long *work, float *out,
                           unsigned slots);
 int launch_norm(const void *plan, int size, unsigned grid, void *stream, unsigned long long *work, float *out, unsigned slots);
 apc_status grad_norm(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots, void *work, apc_stream_t stream, float *out,
                      NormLaunch launch);
+int64_t grad_norm_workspace(const apc_buffer *bufs, int32_t num_bufs);
 
 constexpr int kBlock = 128;  // columns (and, in square blocks, rows) that share a scale
 
@@ -82,7 +83,7 @@ struct NormGradArgs {
   const float *rstd;
   void *dx;
   void *dweight;    // null: not wanted
-  float *work;      // rms_norm_parts(rows, cols) x cols
+  float *work;      // rms_norm_parts(rows, cols) x cols; null where that is none
   int64_t dout_pitch, pitch, dresidual_pitch, dx_pitch;
   uint32_t rows, cols, dtype, wdtype, dwdtype;
 };

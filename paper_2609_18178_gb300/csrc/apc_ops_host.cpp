@@ -305,6 +305,10 @@ APC_EXPORT apc_status apc_matmul_fp8(const apc_fp8_matrix *a, const apc_fp8_matr
   return e ? apc::op_cuda_fail(e, "product kernel launch") : APC_OK;
 }
 
+APC_EXPORT int64_t apc_grad_norm_workspace(const apc_buffer *bufs, int32_t num_bufs) {
+  return apc::grad_norm_workspace(bufs, num_bufs);
+}
+
 APC_EXPORT apc_status apc_grad_norm(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots, void *workspace,
                                     apc_stream_t stream, float *out_norms) {
   apc::op_begin();

@@ -15,6 +15,7 @@
 // places, and stays in registers between its statistics and its output.
 #include <cuda_runtime.h>
 
+#include "apc_cluster.cuh"
 #include "apc_fp8.cuh"
 
 namespace apc {
@@ -659,7 +660,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) turn_kernel(const
 
 // ---------------------------------------------------------------------------
 // Gradient.  The rows are dealt out to `parts` parts whose number follows the sizes alone
-// (rms_norm_parts): part p has rows p, p + parts, ....  A group walks a part and keeps its
+// (few_of, rms_norm_parts): part p has rows p, p + parts, ....  A group walks a part and keeps its
 // columns' sums of dout * z in registers, which go to the workspace, from where a second
 // kernel adds them in order.
 
@@ -667,9 +668,10 @@ struct GradArgs {
   const void *dout, *x, *weight, *dresidual;
   const float *rstd;
   void *dx;
-  float *partial;  // [parts][cols]; null: no dweight
+  float *partial;  // [parts][cols]; null: no dweight, or a cluster's
+  void *dweight;   // written by the cluster kernel
   int64_t dout_pitch, pitch, dresidual_pitch, dx_pitch;
-  uint32_t rows, cols, parts, wdtype, weight_aligned;
+  uint32_t rows, cols, parts, wdtype, weight_aligned, dwdtype;
   float inv_cols;
 };
 
@@ -695,7 +697,21 @@ __device__ __forceinline__ void z_and_g(const uint32_t (&x)[8 / Word<T>::kPer], 
   *g = mul2(*dd, wt[i]);
 }
 
-template <typename T, int V, bool WIDE>
+__device__ __forceinline__ void store_weight(void *to, uint32_t dtype, uint32_t c, float y) {
+  if (dtype == APC_F32) static_cast<float *>(to)[c] = y;
+  else if (dtype == APC_BF16) static_cast<__nv_bfloat16 *>(to)[c] = from_float<__nv_bfloat16>(y);
+  else static_cast<__half *>(to)[c] = from_float<__half>(y);
+}
+
+__device__ __forceinline__ float load_remote(uint32_t mapped) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(mapped) : "memory");
+  return v;
+}
+
+// CLUSTER, for few rows: the grid is one cluster with a part for each group, and the parts'
+// sums meet in its shared memory: one launch, no workspace.
+template <typename T, int V, bool WIDE, bool CLUSTER>
 __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ GradArgs a) {
   constexpr int kWords = 8 / Word<T>::kPer;
   extern __shared__ float s_sums[];  // [2][groups][warps]
@@ -710,10 +726,9 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
     n[v] = count_of<WIDE>(c[v], a.cols);
     weights<WIDE>(wt[v], a.weight, a.wdtype, a.weight_aligned, c[v], n[v]);
   }
+  uint64_t acc[V][4] = {};
   for (uint32_t part = blockIdx.x * blockDim.y + threadIdx.y; part < a.parts; part += gridDim.x * blockDim.y) {
-    uint64_t acc[V][4] = {};
-    for (uint64_t at_row = part; at_row < a.rows; at_row += a.parts) {
-      const uint32_t row = (uint32_t)at_row;
+    for (uint32_t row = part; row < a.rows; row += a.parts) {
       float *room = s_sums + (turn ^= 1) * blockDim.y * g.warps + threadIdx.y * g.warps;
       const float rstd = __ldg(a.rstd + row);
       uint32_t x[V][kWords], d[V][kWords], r[V][kWords];
@@ -750,7 +765,7 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
         store<T, WIDE>(static_cast<T *>(a.dx) + (int64_t)row * a.dx_pitch + c[v], o, n[v]);
       }
     }
-    if (!a.partial) continue;
+    if (CLUSTER || !a.partial) continue;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       float *to = a.partial + (uint64_t)part * a.cols + c[v];
@@ -758,9 +773,40 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
       for (int i = 0; i < 8; ++i) {
         const float2 f = unpack2(acc[v][i / 2]);
         if (i < n[v]) to[WIDE ? i : 32 * i] = i % 2 ? f.y : f.x;
+        acc[v][i / 2] = i % 2 ? 0 : acc[v][i / 2];
       }
     }
   }
+  if (!CLUSTER) return;
+  float *const part_sums = s_sums + 2 * blockDim.y * g.warps;  // [groups][cols]
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    float *to = part_sums + threadIdx.y * a.cols + c[v];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 f = unpack2(acc[v][i / 2]);
+      if (i < n[v]) to[WIDE ? i : 32 * i] = i % 2 ? f.y : f.x;
+    }
+  }
+  cluster_arrive();
+  cluster_wait();
+  // a slice of the columns for each CTA
+  const uint32_t per = (a.cols + gridDim.x - 1) / gridDim.x, begin = blockIdx.x * per, end = min(a.cols, begin + per);
+  for (uint32_t k = begin + threadIdx.y * blockDim.x + threadIdx.x; k < end; k += blockDim.x * blockDim.y) {
+    float s = 0.0f;
+    for (uint32_t r = 0; r < blockDim.y; ++r) {
+      const uint32_t at = smem_addr(part_sums + r * a.cols + k);
+      for (uint32_t q = 0; q < gridDim.x; q += 8) {  // a power of two of CTAs
+        float f[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) f[i] = q + i < gridDim.x ? load_remote(map_rank(at, q + i)) : 0.0f;
+        s += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+      }
+    }
+    store_weight(a.dweight, a.dwdtype, k, s);
+  }
+  cluster_arrive();
+  cluster_wait();  // the others' reads of this CTA's sums
 }
 
 // Rows that a group does not hold: twice over each, element by element.
@@ -820,9 +866,7 @@ __global__ void __launch_bounds__(256) parts_kernel(const float *partial, uint32
     if (warp || c >= cols) continue;
     const float y = ((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane])) +
                     ((sums[4][lane] + sums[5][lane]) + (sums[6][lane] + sums[7][lane]));
-    if (dtype == APC_F32) static_cast<float *>(dweight)[c] = y;
-    else if (dtype == APC_BF16) static_cast<__nv_bfloat16 *>(dweight)[c] = from_float<__nv_bfloat16>(y);
-    else static_cast<__half *>(dweight)[c] = from_float<__half>(y);
+    store_weight(dweight, dtype, c, y);
   }
 }
 
@@ -1235,7 +1279,12 @@ unsigned grid_of(uint64_t want, uint32_t per_sm) {
 
 bool aligned(const void *p, int64_t pitch_bytes) { return (uintptr_t)p % 16 == 0 && pitch_bytes % 16 == 0; }
 
-// Rows that many, and alike within 16 bytes: the ring's shape, or none (threads 0).
+// More rows than `least`, of 16 bits, alike within 16 bytes: the ring's shape, or none (threads
+// 0).  Where rows begin at blocks and end with them, plain loads by more warps keep up for most: the ring pays
+// where a row's work is long, for 8-bit outputs (8192 x 4096 46 us, 50 by plain loads; to 16 bits
+// 51 and 48, 4883 x 4096 of fp32 60 and 52) and for gradients of middling rows (8192 x 4096 59
+// and 63, 16384 x 1024 41 and 38, 4883 x 4096 of fp32 65 and 59).  Elsewhere in the
+// matrix it always does: 4001 x 5001 to 16 bits 35 us (46), its gradient 57 (100).
 struct RingShape {
   uint32_t threads;
   int v;
@@ -1243,12 +1292,13 @@ struct RingShape {
   Ring ring;
 };
 
-RingShape ring_shape(const void *x, int64_t pitch, uint32_t rows, uint32_t cols, uint32_t size, uint32_t mats, unsigned sms, bool alike) {
+RingShape ring_shape(const void *x, int64_t pitch, uint32_t rows, uint32_t cols, uint32_t size, uint32_t mats, uint32_t least, bool alike,
+                     bool pays) {
   RingShape s = {};
   const bool begins = aligned(x, pitch * size);  // rows begin at blocks
   const uint32_t units = (cols + (begins ? 0 : 7) + 7) / 8;
   s.whole = begins && cols % 8 == 0;
-  if (!alike || rows <= 2 * sms || cols <= 512 || units > 4 * kRingThreads) return s;
+  if (size != 2 || (s.whole && !pays) || !alike || rows <= least || cols <= 512 || units > 4 * kRingThreads) return s;
   s.v = units <= 2 * kRingThreads ? 2 : 4;
   s.threads = 32 * ((units + 32 * s.v - 1) / (32 * s.v));
   s.ring.region = (cols * size + 15 + 15) / 16 * 16 + 16;
@@ -1335,8 +1385,9 @@ int launch_rms_norm(const NormArgs &n, unsigned sms, void *stream) {
     const auto alike = [&](const void *p, int64_t pitch) {
       return same_place(n.x, n.pitch * (int64_t)sizeof(T), p, pitch * (int64_t)sizeof(T));
     };
-    const RingShape ring = ring_shape(n.x, n.pitch, n.rows, n.cols, sizeof(T), n.residual ? 2 : 1, sms,
-                                      alike(n.residual, n.residual_pitch) && alike(n.sum, n.sum_pitch) && alike(n.out, n.out_pitch));
+    const RingShape ring = ring_shape(n.x, n.pitch, n.rows, n.cols, sizeof(T), n.residual ? 2 : 1, 8 * sms,
+                                      alike(n.residual, n.residual_pitch) && alike(n.sum, n.sum_pitch) && alike(n.out, n.out_pitch),
+                                      !n.out);
     int e;
     if (n.out) e = forward<T, kSame>(a, s, ring, wide, stream);
     else e = n.q.e5m2 ? forward<T, kE5M2>(a, s, ring, wide, stream) : forward<T, kE4M3>(a, s, ring, wide, stream);
@@ -1357,11 +1408,54 @@ int launch_rms_norm(const NormArgs &n, unsigned sms, void *stream) {
   });
 }
 
-// Enough runs for every SM, more of them where a group is small.
+namespace {
+
+// Few rows: a cluster of so many CTAs (0: none) of so many groups, up to 8 rows for each.
+struct Few {
+  uint32_t ctas, groups;
+};
+
+Few few_of(uint32_t rows, uint32_t cols) {
+  const Shape s = shape_of(cols, cols <= 8192 ? 2 : 4);
+  if (!rows || !s.fits || (uint64_t)rows * cols > 1u << 20) return {0, 0};
+  Few f = {1, 1};
+  while (f.ctas < 16 && f.ctas < rows) f.ctas *= 2;
+  const uint32_t most = s.threads >= 512 ? 1 : 512 / s.threads, want = (rows + 15) / 16;
+  if (rows > 16) f.groups = want < most ? want : most;
+  return rows > 8 * f.ctas * f.groups ? Few{0, 0} : f;
+}
+
+}  // namespace
+
+// Enough parts for every SM, more of them where a group is small; none where a cluster does it.
 uint32_t rms_norm_parts(uint32_t rows, uint32_t cols) {
+  if (few_of(rows, cols).ctas) return 0;
   const uint32_t parts = 304 * (cols <= 512 ? 8 : cols <= 1024 ? 4 : cols <= 2048 ? 2 : 1);
   return rows < parts ? rows : parts;
 }
+
+namespace {
+
+template <typename K>
+int grad_few(K kernel, const GradArgs &a, const Shape &s, const Few &few, cudaStream_t stream) {
+  const uint32_t bytes = (2 * few.groups * (s.threads / 32) + few.groups * a.cols) * sizeof(float);
+  int e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (!e && few.ctas > 8) e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e) return e;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim = {few.ctas, 1, 1};
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(few.ctas);
+  cfg.blockDim = dim3(s.threads, few.groups);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return (int)cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+}  // namespace
 
 int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
   GradArgs a = {};
@@ -1369,7 +1463,10 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
   a.partial = n.dweight ? n.work : nullptr;
   a.dout_pitch = n.dout_pitch, a.pitch = n.pitch, a.dresidual_pitch = n.dresidual_pitch, a.dx_pitch = n.dx_pitch;
   a.rows = n.rows, a.cols = n.cols, a.wdtype = n.wdtype;
-  a.parts = rms_norm_parts(n.rows, n.cols);
+  const Few few = n.dweight ? few_of(n.rows, n.cols) : Few{0, 0};
+  a.parts = few.ctas ? few.ctas * few.groups : rms_norm_parts(n.rows, n.cols);
+  if (!a.parts) a.parts = n.rows < 304 ? n.rows : 304;  // without dweight
+  if (few.ctas) a.partial = nullptr, a.dweight = n.dweight, a.dwdtype = n.dwdtype;
   a.weight_aligned = (uintptr_t)n.weight % 16 == 0;
   a.inv_cols = (float)(1.0 / n.cols);
   cudaStream_t s = (cudaStream_t)stream;
@@ -1385,9 +1482,10 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
     const auto alike = [&](const void *p, int64_t pitch) {
       return same_place(n.x, n.pitch * (int64_t)sizeof(T), p, pitch * (int64_t)sizeof(T));
     };
-    const RingShape ring = ring_shape(n.x, n.pitch, n.rows, n.cols, sizeof(T), n.dresidual ? 3 : 2, sms,
-                                      alike(n.dout, n.dout_pitch) && alike(n.dresidual, n.dresidual_pitch) && alike(n.dx, n.dx_pitch));
-    if (ring.threads) {
+    const RingShape ring = ring_shape(n.x, n.pitch, n.rows, n.cols, sizeof(T), n.dresidual ? 3 : 2, 2 * sms,
+                                      alike(n.dout, n.dout_pitch) && alike(n.dresidual, n.dresidual_pitch) && alike(n.dx, n.dx_pitch),
+                                      n.cols >= 2048 && n.cols <= 8192);
+    if (ring.threads && !few.ctas) {
       const uint32_t period = period_of(n.pitch * (int64_t)sizeof(T));
       if (ring.whole)
         return ring.v == 2 ? ring_launch(ring_grad_kernel<T, 2, true>, a, ring, a.parts, period, stream)
@@ -1396,20 +1494,24 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
                          : ring_launch(ring_grad_kernel<T, 4, false>, a, ring, a.parts, period, stream);
     }
     const bool wide = at(n.x, n.pitch) && at(n.dout, n.dout_pitch) && at(n.dresidual, n.dresidual_pitch) && at(n.dx, n.dx_pitch);
+    if (few.ctas) {
+      if (sh.v == 2) return wide ? grad_few(grad_kernel<T, 2, true, true>, a, sh, few, s) : grad_few(grad_kernel<T, 2, false, true>, a, sh, few, s);
+      return wide ? grad_few(grad_kernel<T, 4, true, true>, a, sh, few, s) : grad_few(grad_kernel<T, 4, false, true>, a, sh, few, s);
+    }
     const uint32_t per = sh.threads * sh.groups;
     const unsigned grid = grid_of((a.parts + sh.groups - 1) / sh.groups, 1024 / per);
     const size_t room = sizeof(float) * 2 * per / 32;
     const dim3 block(sh.threads, sh.groups);
     if (sh.v == 2) {
-      if (wide) grad_kernel<T, 2, true><<<grid, block, room, s>>>(a);
-      else grad_kernel<T, 2, false><<<grid, block, room, s>>>(a);
+      if (wide) grad_kernel<T, 2, true, false><<<grid, block, room, s>>>(a);
+      else grad_kernel<T, 2, false, false><<<grid, block, room, s>>>(a);
     } else {
-      if (wide) grad_kernel<T, 4, true><<<grid, block, room, s>>>(a);
-      else grad_kernel<T, 4, false><<<grid, block, room, s>>>(a);
+      if (wide) grad_kernel<T, 4, true, false><<<grid, block, room, s>>>(a);
+      else grad_kernel<T, 4, false, false><<<grid, block, room, s>>>(a);
     }
     return (int)cudaGetLastError();
   });
-  if (e || !n.dweight) return e;
+  if (e || !n.dweight || few.ctas) return e;
   parts_kernel<<<grid_of((n.cols + 31) / 32, 8), 256, 0, s>>>(n.work, a.parts, n.cols, n.dweight, n.dwdtype);
   return (int)cudaGetLastError();
 }

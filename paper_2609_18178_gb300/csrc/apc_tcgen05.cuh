@@ -5,6 +5,7 @@
 #include <cuda.h>
 #include <stdint.h>
 
+#include "apc_cluster.cuh"
 #include "apc_tma.cuh"
 
 namespace apc {
@@ -14,23 +15,7 @@ namespace apc {
 // themselves are elected (elect.sync): with a loop in one lane the issue of
 // four products took 600 cycles, more than the products.
 
-// ---- clusters
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-
-// The address in the cluster's window of shared address `a` in CTA `rank`.
-__device__ __forceinline__ uint32_t map_rank(uint32_t a, uint32_t rank) {
-  uint32_t r;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
-  return r;
-}
-
+// ---- arrivals and copies across a cluster
 __device__ __forceinline__ void arrive_remote(uint32_t mapped) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(mapped) : "memory");
 }

@@ -287,7 +287,7 @@ def rms_norm_grad(dout, x, weight, rstd, *, dresidual=None, out=None, dweight=No
     and the weight's, in its type or in ``dweight``'s; None without
     ``weight_grad``.  ``workspace``: fp32, for a caller that keeps its own, which
     no other call may use at the same time; ``rms_norm_grad_workspace(rows,
-    cols)`` elements."""
+    cols)`` elements, none for few rows."""
     lib = _library()
     device = _current_device()
     kind, r, c, pitch = _matrix(x, "x", _DTYPE, device)
@@ -305,12 +305,13 @@ def rms_norm_grad(dout, x, weight, rstd, *, dresidual=None, out=None, dweight=No
         if dweight is None:
             dweight = _empty((c,), weight.dtype, weight, stream)
         wkind, at = _weight(dweight, "dweight", device, c), dweight.data_ptr()
-        n = rms_norm_grad_workspace(r, c)
-        if workspace is None:
-            workspace = _empty((n,), torch.float32, x, stream)
-        elif workspace.numel() > n:
-            workspace = workspace.view(-1)[:n]
-        work = _vector(workspace, "workspace", _F32, device, n)
+        n = lib.apc_rms_norm_grad_workspace(r, c) // 4
+        if n:
+            if workspace is None:
+                workspace = _empty((n,), torch.float32, x, stream)
+            elif workspace.numel() > n:
+                workspace = workspace.view(-1)[:n]
+            work = _vector(workspace, "workspace", _F32, device, n)
     elif dweight is not None:
         raise ValueError("dweight without weight_grad")
     _check(lib.apc_rms_norm_grad(ctypes.byref(d), out.data_ptr(), opitch, at, wkind, work, _stream(stream, device)))

@@ -1,9 +1,9 @@
 """The gradients' norm against 64-bit sums, and the clipped step against the
 step's fixed order of binary32 operations, on the GPU.
 
-Bounds: a tile's sum of squares passes at most 12 multiply-adds, 2 additions and
+Bounds: a tile's sum of squares passes at most 16 multiply-adds, 2 additions and
 5 more between lanes, each off by 2^-24 of a partial sum of non-negative terms,
-and tiles add exactly: 19 * 2^-24, of which a square root leaves half, and one
+and tiles add exactly: 23 * 2^-24, of which a square root leaves half, and one
 rounding: below 2^-20 in all."""
 import math
 import os
@@ -38,7 +38,7 @@ def placed(x, off):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("n", [1, 2, 7, 8, 9, 255, 767, 768, 769, 1535, 1536, 1537, 3071, 4097, 100_003])
+@pytest.mark.parametrize("n", [1, 2, 7, 8, 9, 255, 1023, 1024, 1025, 2047, 2048, 2049, 4097, 100_003, 9_000_001])
 def test_norm_at_every_alignment(dtype, n):
     x = torch.randn(n, generator=gen(n), device="cuda").to(dtype)
     want = exact([x])
@@ -51,9 +51,10 @@ def test_norm_at_every_alignment(dtype, n):
     assert abs(bits.pop() - want) <= REL * want
 
 
-@pytest.mark.parametrize("count", [1, 16, 17, 200, 201, 1000, 1001, 2303])
-def test_norm_of_many_buffers(count):
-    sizes = torch.randint(1, 6000, (count,), generator=torch.Generator().manual_seed(count)).tolist()
+@pytest.mark.parametrize("count", [1, 24, 25, 240, 241, 1100, 1600, 1601, 3333])
+@pytest.mark.parametrize("size", [300, 6000, 60_000])
+def test_norm_of_many_buffers(count, size):
+    sizes = torch.randint(1, size, (count,), generator=torch.Generator().manual_seed(count)).tolist()
     whole = torch.randn(sum(sizes), generator=gen(3), device="cuda").mul_(1e-3).bfloat16()
     parts = list(whole.split(sizes))
     a = apc.grad_norm(parts)
@@ -118,7 +119,7 @@ def test_norm_of_half_at_its_ends():
 @pytest.mark.parametrize("dtype", TYPES)
 def test_norm_of_values_that_are_not_finite(dtype):
     x = torch.randn(9001, generator=gen(4), device="cuda").to(dtype)
-    for at in (0, 1535, 9000):
+    for at in (0, 2047, 9000):
         y = x.clone()
         y[at] = -math.inf
         assert apc.grad_norm([x, y]).item() == math.inf

@@ -201,7 +201,7 @@ def test_nothing():
 
 # ---- gradient
 
-def check_grad(d, x, w, rstd, dres, dx, dw, eps_rows):
+def check_grad(d, x, w, rstd, dres, dx, dw, parts):
     r, c = x.shape
     z, g = x.double() * rstd.double()[:, None], d.double() * w.double()
     mean = (g * z).mean(1, keepdim=True)
@@ -214,8 +214,8 @@ def check_grad(d, x, w, rstd, dres, dx, dw, eps_rows):
     assert ((dx.double() - want).abs() <= k * U * size + UNIT[x.dtype] * want.abs() + TINY[x.dtype]).all()
     if dw is not None:
         want, size = (d.double() * z).sum(0), (d.double() * z).abs().sum(0)
-        # a run's rows, the runs of a warp, the warps
-        k = r / eps_rows + eps_rows / 8 + 8
+        # a part's rows, the parts of a warp, the warps; of few rows up to 8 a part, 256 parts
+        k = r / parts + parts / 8 + 8 if parts else 8 + 256 + 4
         assert ((dw.double() - want).abs() <= k * U * size + UNIT[dw.dtype] * want.abs() + TINY[dw.dtype]).all()
 
 
