@@ -463,6 +463,91 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
   }
 }
 
+// Many rows that a warp holds: U rows at a time, so that one's latencies lie beside the others'
+// (16384 x 128: 10.4 us a row at a time).
+template <typename T, int OUT, int V, int U, bool WIDE>
+__global__ void __launch_bounds__(256) narrow_kernel(const __grid_constant__ ForwardArgs a) {
+  constexpr int kWords = 8 / Word<T>::kPer;
+  const Group g{1, 0, 0, threadIdx.x % 32};
+  const uint64_t step = (uint64_t)gridDim.x * (blockDim.x / 32) * U;
+  uint32_t c[V];
+  int n[V];
+  uint64_t wt[V][4];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    c[v] = first_of<WIDE>(v, g.lane);
+    n[v] = count_of<WIDE>(c[v], a.cols);
+    weights<WIDE>(wt[v], a.weight, a.wdtype, a.weight_aligned, c[v], n[v]);
+  }
+  for (uint64_t first = ((uint64_t)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32) * U; first < a.rows; first += step) {
+    uint32_t w[U][V][kWords];
+    float rstd[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool there = first + u < a.rows;
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        load<T, WIDE>(w[u][v], static_cast<const T *>(a.x) + (int64_t)(first + u) * a.pitch + c[v], there ? n[v] : 0);
+    }
+    if (a.residual) {
+      uint32_t o[U][V][kWords];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool there = first + u < a.rows;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          load<T, WIDE>(o[u][v], static_cast<const T *>(a.residual) + (int64_t)(first + u) * a.residual_pitch + c[v], there ? n[v] : 0);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool there = first + u < a.rows;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          add_rounded<T>(w[u][v], o[u][v]);
+          store<T, WIDE>(static_cast<T *>(a.sum) + (int64_t)(first + u) * a.sum_pitch + c[v], w[u][v], there ? n[v] : 0);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float p = 0.0f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) p += squares<T>(w[u][v]);
+      if (!row_rstd(p, g, nullptr, a.c, true, &rstd[u])) rstd[u] = wild_rstd<T, V>(w[u], g, nullptr, a.c);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (first + u >= a.rows) break;
+      const uint32_t row = (uint32_t)first + u;
+      if (g.lane == 0) a.rstd[row] = rstd[u];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        uint64_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          y[i] = mul2(mul2(pack2(element<T>(w[u][v], 2 * i), element<T>(w[u][v], 2 * i + 1)), pack2(rstd[u], rstd[u])), wt[v][i]);
+        if (OUT == kSame) {
+          uint32_t o[kWords];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack2(y[i]);
+            round_pair<T>(o, i, f.x, f.y);
+          }
+          store<T, WIDE>(static_cast<T *>(a.out) + (int64_t)row * a.out_pitch + c[v], o, n[v]);
+        } else {
+          if (n[v] < 8)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 f = unpack2(y[i]);
+              y[i] = pack2(2 * i < n[v] ? f.x : 0.0f, 2 * i + 1 < n[v] ? f.y : 0.0f);
+            }
+          quantize8<OUT == kE5M2, WIDE>(a, row, c[v], n[v], y, g.lane);
+        }
+      }
+    }
+  }
+}
+
 // The transpose in 8 bits, from the sum and rstd that the forward kernel left.  A CTA walks
 // tiles of 128 x 128, the last rows first: those are what the forward kernel left in L2.  The
 // next tile comes into shared memory while the one before is stored; four CTAs on an SM
@@ -675,17 +760,25 @@ struct GradArgs {
   float inv_cols;
 };
 
-// The sum of p over a group, in an order of its own, in every thread.
-__device__ __forceinline__ float group_sum(float p, const Group &g, float *room) {
+// The sums of p over a group, in an order of its own, in every thread.
+template <int U>
+__device__ __forceinline__ void group_sums(float (&p)[U], const Group &g, float *room) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) p += __shfl_xor_sync(~0u, p, o);
-  if (g.warps == 1) return p;
-  if (g.lane == 0) room[g.warp] = p;
+  for (int o = 16; o; o >>= 1)
+#pragma unroll
+    for (int u = 0; u < U; ++u) p[u] += __shfl_xor_sync(~0u, p[u], o);
+  if (U > 1 || g.warps == 1) return;  // several rows at a time: groups of one warp
+  if (g.lane == 0) room[g.warp] = p[0];
   g.sync();
-  p = g.lane < g.warps ? room[g.lane] : 0.0f;
+  p[0] = g.lane < g.warps ? room[g.lane] : 0.0f;
 #pragma unroll
-  for (int o = 16; o; o >>= 1) p += __shfl_xor_sync(~0u, p, o);
-  return p;
+  for (int o = 16; o; o >>= 1) p[0] += __shfl_xor_sync(~0u, p[0], o);
+}
+
+__device__ __forceinline__ float group_sum(float p, const Group &g, float *room) {
+  float s[1] = {p};
+  group_sums<1>(s, g, room);
+  return s[0];
 }
 
 // One run of 8 columns a thread: z and g = dout * weight of a row.
@@ -709,13 +802,16 @@ __device__ __forceinline__ float load_remote(uint32_t mapped) {
   return v;
 }
 
-// CLUSTER, for few rows: the grid is one cluster with a part for each group, and the parts'
-// sums meet in its shared memory: one launch, no workspace.
-template <typename T, int V, bool WIDE, bool CLUSTER>
+// The groups of a CTA join their sums in shared memory, and their part of the workspace is
+// the CTA's.  CLUSTER, for few rows: the grid is one cluster with a part for each group, and all
+// sums meet in its shared memory: one launch, no workspace.  U rows at a time where a group is
+// a warp, so that one's latencies lie beside the others'.
+template <typename T, int V, int U, bool WIDE, bool CLUSTER>
 __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ GradArgs a) {
   constexpr int kWords = 8 / Word<T>::kPer;
-  extern __shared__ float s_sums[];  // [2][groups][warps]
+  extern __shared__ float s_sums[];  // [2][groups][warps], [groups][cols]
   const Group g{blockDim.x / 32, 1 + threadIdx.y, threadIdx.x / 32, threadIdx.x % 32};
+  float *const part_sums = s_sums + 2 * blockDim.y * g.warps;
   uint32_t turn = 0;
   uint32_t c[V];
   int n[V];
@@ -726,68 +822,84 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
     n[v] = count_of<WIDE>(c[v], a.cols);
     weights<WIDE>(wt[v], a.weight, a.wdtype, a.weight_aligned, c[v], n[v]);
   }
-  uint64_t acc[V][4] = {};
-  for (uint32_t part = blockIdx.x * blockDim.y + threadIdx.y; part < a.parts; part += gridDim.x * blockDim.y) {
-    for (uint32_t row = part; row < a.rows; row += a.parts) {
+  const uint32_t step = a.parts * blockDim.y;  // parts: of CTAs
+  for (uint32_t part = blockIdx.x; part < a.parts; part += gridDim.x) {
+    uint64_t acc[V][4] = {};
+    for (uint64_t first = part * blockDim.y + threadIdx.y; first < a.rows; first += (uint64_t)step * U) {
       float *room = s_sums + (turn ^= 1) * blockDim.y * g.warps + threadIdx.y * g.warps;
-      const float rstd = __ldg(a.rstd + row);
-      uint32_t x[V][kWords], d[V][kWords], r[V][kWords];
+      uint32_t x[U][V][kWords], d[U][V][kWords], r[U][V][kWords];
+      float rstd[U], dot[U];
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        load<T, WIDE>(x[v], static_cast<const T *>(a.x) + (int64_t)row * a.pitch + c[v], n[v]);
-        load<T, WIDE>(d[v], static_cast<const T *>(a.dout) + (int64_t)row * a.dout_pitch + c[v], n[v]);
-        if (a.dresidual) load<T, WIDE>(r[v], static_cast<const T *>(a.dresidual) + (int64_t)row * a.dresidual_pitch + c[v], n[v]);
+      for (int u = 0; u < U; ++u) {
+        const uint64_t at = first + (uint64_t)u * step;
+        const bool there = u == 0 || at < a.rows;
+        const int64_t row = there ? (int64_t)at : 0;
+        rstd[u] = __ldg(a.rstd + row);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int m = there ? n[v] : 0;
+          load<T, WIDE>(x[u][v], static_cast<const T *>(a.x) + row * a.pitch + c[v], m);
+          load<T, WIDE>(d[u][v], static_cast<const T *>(a.dout) + row * a.dout_pitch + c[v], m);
+          if (a.dresidual) load<T, WIDE>(r[u][v], static_cast<const T *>(a.dresidual) + row * a.dresidual_pitch + c[v], m);
+        }
       }
-      uint64_t dot = 0;
 #pragma unroll
-      for (int v = 0; v < V; ++v)
+      for (int u = 0; u < U; ++u) {
+        if (u && first + (uint64_t)u * step >= a.rows) rstd[u] = 0.0f;  // nothing is added for a row that is not there
+        uint64_t sum = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint64_t z, gg, dd;
-          z_and_g<T>(x[v], d[v], rstd, wt[v], i, &z, &gg, &dd);
-          dot = fma2(gg, z, dot);
-          acc[v][i] = fma2(dd, z, acc[v][i]);
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint64_t z, gg, dd;
+            z_and_g<T>(x[u][v], d[u][v], rstd[u], wt[v], i, &z, &gg, &dd);
+            sum = fma2(gg, z, sum);
+            acc[v][i] = fma2(dd, z, acc[v][i]);
+          }
+        const float2 both = unpack2(sum);
+        dot[u] = both.x + both.y;
+      }
+      group_sums<U>(dot, g, room);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint64_t row = first + (uint64_t)u * step;
+        if (u && row >= a.rows) break;
+        const float mean = dot[u] * a.inv_cols;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          uint32_t o[kWords];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint64_t z, gg, dd;
+            z_and_g<T>(x[u][v], d[u][v], rstd[u], wt[v], i, &z, &gg, &dd);
+            float2 f = unpack2(mul2(fma2(z, pack2(-mean, -mean), gg), pack2(rstd[u], rstd[u])));
+            if (a.dresidual) f.x += element<T>(r[u][v], 2 * i), f.y += element<T>(r[u][v], 2 * i + 1);
+            round_pair<T>(o, i, f.x, f.y);
+          }
+          store<T, WIDE>(static_cast<T *>(a.dx) + (int64_t)row * a.dx_pitch + c[v], o, n[v]);
         }
-      const float2 both = unpack2(dot);
-      const float mean = group_sum(both.x + both.y, g, room) * a.inv_cols;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        uint32_t o[kWords];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint64_t z, gg, dd;
-          z_and_g<T>(x[v], d[v], rstd, wt[v], i, &z, &gg, &dd);
-          uint64_t y = mul2(fma2(z, pack2(-mean, -mean), gg), pack2(rstd, rstd));
-          float2 f = unpack2(y);
-          if (a.dresidual) f.x += element<T>(r[v], 2 * i), f.y += element<T>(r[v], 2 * i + 1);
-          round_pair<T>(o, i, f.x, f.y);
-        }
-        store<T, WIDE>(static_cast<T *>(a.dx) + (int64_t)row * a.dx_pitch + c[v], o, n[v]);
       }
     }
-    if (CLUSTER || !a.partial) continue;
+    if (!CLUSTER && !a.partial) continue;
+    const bool alone = !CLUSTER && blockDim.y == 1;
+    float *const sums = alone ? a.partial + (uint64_t)part * a.cols : part_sums + threadIdx.y * a.cols;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      float *to = a.partial + (uint64_t)part * a.cols + c[v];
+    for (int v = 0; v < V; ++v)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float2 f = unpack2(acc[v][i / 2]);
-        if (i < n[v]) to[WIDE ? i : 32 * i] = i % 2 ? f.y : f.x;
-        acc[v][i / 2] = i % 2 ? 0 : acc[v][i / 2];
+        if (i < n[v]) sums[c[v] + (WIDE ? i : 32 * i)] = i % 2 ? f.y : f.x;
       }
+    if (CLUSTER || alone) continue;
+    __syncthreads();
+    for (uint32_t k = threadIdx.y * blockDim.x + threadIdx.x; k < a.cols; k += blockDim.x * blockDim.y) {
+      float s = 0.0f;
+      for (uint32_t q = 0; q < blockDim.y; ++q) s += part_sums[q * a.cols + k];
+      a.partial[(uint64_t)part * a.cols + k] = s;
     }
+    __syncthreads();
   }
   if (!CLUSTER) return;
-  float *const part_sums = s_sums + 2 * blockDim.y * g.warps;  // [groups][cols]
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    float *to = part_sums + threadIdx.y * a.cols + c[v];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float2 f = unpack2(acc[v][i / 2]);
-      if (i < n[v]) to[WIDE ? i : 32 * i] = i % 2 ? f.y : f.x;
-    }
-  }
   cluster_arrive();
   cluster_wait();
   // a slice of the columns for each CTA
@@ -850,22 +962,24 @@ __global__ void __launch_bounds__(256) grad_long_parts_kernel(const __grid_const
   }
 }
 
-// dweight: the parts' sums, warp k of a CTA those of parts k, k + 8, ..., then the warps'.
-__global__ void __launch_bounds__(256) parts_kernel(const float *partial, uint32_t parts, uint32_t cols, void *dweight, uint32_t dtype) {
-  __shared__ float sums[8][32];
+// dweight: the parts' sums, 32 columns a CTA, warp k those of parts k, k + 16, ..., then the warps'.
+__global__ void __launch_bounds__(512) parts_kernel(const float *partial, uint32_t parts, uint32_t cols, void *dweight, uint32_t dtype) {
+  __shared__ float sums[16][32];
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const uint32_t runs = (cols + 31) / 32;
   for (uint32_t run = blockIdx.x; run < runs; run += gridDim.x) {
     const uint32_t c = run * 32 + lane;
     float s = 0.0f;
     if (c < cols)
-      for (uint32_t p = warp; p < parts; p += 8) s += __ldcg(partial + (uint64_t)p * cols + c);
+#pragma unroll 8
+      for (uint32_t p = warp; p < parts; p += 16) s += __ldcg(partial + (uint64_t)p * cols + c);
     __syncthreads();
     sums[warp][lane] = s;
     __syncthreads();
     if (warp || c >= cols) continue;
-    const float y = ((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane])) +
-                    ((sums[4][lane] + sums[5][lane]) + (sums[6][lane] + sums[7][lane]));
+    float y = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; k += 4) y += (sums[k][lane] + sums[k + 1][lane]) + (sums[k + 2][lane] + sums[k + 3][lane]);
     store_weight(dweight, dtype, c, y);
   }
 }
@@ -1277,6 +1391,9 @@ unsigned grid_of(uint64_t want, uint32_t per_sm) {
   return (unsigned)(want < cap ? want : cap);
 }
 
+// From so many rows on a warp takes several at a time.
+constexpr uint32_t kNarrowRows = 1024;
+
 bool aligned(const void *p, int64_t pitch_bytes) { return (uintptr_t)p % 16 == 0 && pitch_bytes % 16 == 0; }
 
 // More rows than `least`, of 16 bits, alike within 16 bytes: the ring's shape, or none (threads
@@ -1355,6 +1472,18 @@ int forward(const ForwardArgs &a, const Shape &s, const RingShape &ring, bool wi
     return ring.v == 2 ? ring_launch(ring_forward_kernel<T, OUT, 2, false>, a, ring, a.rows, period, stream)
                        : ring_launch(ring_forward_kernel<T, OUT, 4, false>, a, ring, a.rows, period, stream);
   }
+  if (a.cols <= 512 && a.rows > kNarrowRows) {
+    const unsigned grid = grid_of((a.rows + 31) / 32, 4);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (a.cols <= 256) {
+      if (wide) narrow_kernel<T, OUT, 1, 4, true><<<grid, 256, 0, st>>>(a);
+      else narrow_kernel<T, OUT, 1, 4, false><<<grid, 256, 0, st>>>(a);
+    } else {
+      if (wide) narrow_kernel<T, OUT, 2, 2, true><<<grid, 256, 0, st>>>(a);
+      else narrow_kernel<T, OUT, 2, 2, false><<<grid, 256, 0, st>>>(a);
+    }
+    return (int)cudaGetLastError();
+  }
   if (!s.fits) return wide ? forward_launch<T, OUT, 2, true, true>(a, s, stream) : forward_launch<T, OUT, 2, false, true>(a, s, stream);
   if (s.v == 1) return wide ? forward_launch<T, OUT, 1, true, false>(a, s, stream) : forward_launch<T, OUT, 1, false, false>(a, s, stream);
   return wide ? forward_launch<T, OUT, 2, true, false>(a, s, stream) : forward_launch<T, OUT, 2, false, false>(a, s, stream);
@@ -1415,8 +1544,12 @@ struct Few {
   uint32_t ctas, groups;
 };
 
+constexpr uint32_t kGradParts = 304;
+
+Shape grad_shape(uint32_t cols) { return shape_of(cols, cols <= 256 ? 1 : cols <= 8192 ? 2 : 4); }
+
 Few few_of(uint32_t rows, uint32_t cols) {
-  const Shape s = shape_of(cols, cols <= 8192 ? 2 : 4);
+  const Shape s = grad_shape(cols);
   if (!rows || !s.fits || (uint64_t)rows * cols > 1u << 20) return {0, 0};
   Few f = {1, 1};
   while (f.ctas < 16 && f.ctas < rows) f.ctas *= 2;
@@ -1427,11 +1560,10 @@ Few few_of(uint32_t rows, uint32_t cols) {
 
 }  // namespace
 
-// Enough parts for every SM, more of them where a group is small; none where a cluster does it.
+// Parts, of a CTA each: two for every SM; none where a cluster does it.
 uint32_t rms_norm_parts(uint32_t rows, uint32_t cols) {
   if (few_of(rows, cols).ctas) return 0;
-  const uint32_t parts = 304 * (cols <= 512 ? 8 : cols <= 1024 ? 4 : cols <= 2048 ? 2 : 1);
-  return rows < parts ? rows : parts;
+  return rows < kGradParts ? rows : kGradParts;
 }
 
 namespace {
@@ -1464,13 +1596,12 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
   a.dout_pitch = n.dout_pitch, a.pitch = n.pitch, a.dresidual_pitch = n.dresidual_pitch, a.dx_pitch = n.dx_pitch;
   a.rows = n.rows, a.cols = n.cols, a.wdtype = n.wdtype;
   const Few few = n.dweight ? few_of(n.rows, n.cols) : Few{0, 0};
-  a.parts = few.ctas ? few.ctas * few.groups : rms_norm_parts(n.rows, n.cols);
-  if (!a.parts) a.parts = n.rows < 304 ? n.rows : 304;  // without dweight
+  a.parts = few.ctas ? few.ctas : n.rows < kGradParts ? n.rows : kGradParts;
   if (few.ctas) a.partial = nullptr, a.dweight = n.dweight, a.dwdtype = n.dwdtype;
   a.weight_aligned = (uintptr_t)n.weight % 16 == 0;
   a.inv_cols = (float)(1.0 / n.cols);
   cudaStream_t s = (cudaStream_t)stream;
-  const Shape sh = shape_of(n.cols, n.cols <= 8192 ? 2 : 4);
+  const Shape sh = grad_shape(n.cols);
   const int e = !n.rows ? 0 : with_dtype(n.dtype, [&](auto t) {
     using T = decltype(t);
     const auto at = [](const void *p, int64_t pitch) { return aligned(p, pitch * (int64_t)sizeof(T)); };
@@ -1494,25 +1625,25 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
                          : ring_launch(ring_grad_kernel<T, 4, false>, a, ring, a.parts, period, stream);
     }
     const bool wide = at(n.x, n.pitch) && at(n.dout, n.dout_pitch) && at(n.dresidual, n.dresidual_pitch) && at(n.dx, n.dx_pitch);
-    if (few.ctas) {
-      if (sh.v == 2) return wide ? grad_few(grad_kernel<T, 2, true, true>, a, sh, few, s) : grad_few(grad_kernel<T, 2, false, true>, a, sh, few, s);
-      return wide ? grad_few(grad_kernel<T, 4, true, true>, a, sh, few, s) : grad_few(grad_kernel<T, 4, false, true>, a, sh, few, s);
-    }
-    const uint32_t per = sh.threads * sh.groups;
-    const unsigned grid = grid_of((a.parts + sh.groups - 1) / sh.groups, 1024 / per);
-    const size_t room = sizeof(float) * 2 * per / 32;
-    const dim3 block(sh.threads, sh.groups);
-    if (sh.v == 2) {
-      if (wide) grad_kernel<T, 2, true, false><<<grid, block, room, s>>>(a);
-      else grad_kernel<T, 2, false, false><<<grid, block, room, s>>>(a);
-    } else {
-      if (wide) grad_kernel<T, 4, true, false><<<grid, block, room, s>>>(a);
-      else grad_kernel<T, 4, false, false><<<grid, block, room, s>>>(a);
-    }
-    return (int)cudaGetLastError();
+    const auto with_shape = [&](auto f) {
+      if (sh.v == 1) return wide ? f(grad_kernel<T, 1, 4, true, false>, grad_kernel<T, 1, 4, true, true>)
+                                 : f(grad_kernel<T, 1, 4, false, false>, grad_kernel<T, 1, 4, false, true>);
+      if (sh.threads == 32) return wide ? f(grad_kernel<T, 2, 2, true, false>, grad_kernel<T, 2, 2, true, true>)
+                                        : f(grad_kernel<T, 2, 2, false, false>, grad_kernel<T, 2, 2, false, true>);
+      if (sh.v == 2) return wide ? f(grad_kernel<T, 2, 1, true, false>, grad_kernel<T, 2, 1, true, true>)
+                                 : f(grad_kernel<T, 2, 1, false, false>, grad_kernel<T, 2, 1, false, true>);
+      return wide ? f(grad_kernel<T, 4, 1, true, false>, grad_kernel<T, 4, 1, true, true>)
+                  : f(grad_kernel<T, 4, 1, false, false>, grad_kernel<T, 4, 1, false, true>);
+    };
+    if (few.ctas) return with_shape([&](auto, auto kernel) { return grad_few(kernel, a, sh, few, s); });
+    const uint32_t room = (2 * sh.groups * (sh.threads / 32) + (sh.groups > 1 ? sh.groups * n.cols : 0)) * sizeof(float);
+    return with_shape([&](auto kernel, auto) {
+      kernel<<<grid_of(a.parts, 2), dim3(sh.threads, sh.groups), room, s>>>(a);
+      return (int)cudaGetLastError();
+    });
   });
   if (e || !n.dweight || few.ctas) return e;
-  parts_kernel<<<grid_of((n.cols + 31) / 32, 8), 256, 0, s>>>(n.work, a.parts, n.cols, n.dweight, n.dwdtype);
+  parts_kernel<<<grid_of((n.cols + 31) / 32, 4), 512, 0, s>>>(n.work, a.parts, n.cols, n.dweight, n.dwdtype);
   return (int)cudaGetLastError();
 }
 
