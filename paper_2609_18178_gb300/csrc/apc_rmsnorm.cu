@@ -22,6 +22,26 @@ namespace apc {
 
 namespace {
 
+// A call's second kernel may start while its first one drains (launch_after), and waits
+// for it to have completed before it does anything.
+__device__ __forceinline__ void start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_first() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... P, typename... A>
+int launch_after(void (*kernel)(P...), unsigned grid, unsigned threads, uint32_t bytes, void *stream, const A &...args) {
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = (cudaStream_t)stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return (int)cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // ---------------------------------------------------------------------------
 // Eight elements of a row.  WIDE: neighbours, in 16-byte accesses.  Otherwise (rows
 // at any boundary) every 32nd element, so that a warp's accesses stay dense.  n: how
@@ -295,6 +315,7 @@ struct ForwardArgs {
   int64_t pitch, residual_pitch, sum_pitch, out_pitch;
   uint32_t rows, cols, wdtype;
   uint32_t weight_aligned;
+  uint32_t then;  // the transpose's kernel follows
   NormConst c;
 };
 
@@ -361,6 +382,7 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
   constexpr int kWords = 8 / Word<T>::kPer;
   extern __shared__ Stat s_room[];  // [2][groups][warps]
   const Group g{blockDim.x / 32, 1 + threadIdx.y, threadIdx.x / 32, threadIdx.x % 32};
+  if (a.then) start_next();
   const uint32_t groups = (LONG ? (a.cols + 255) / 256 : V * g.warps);  // runs of 256 columns
   uint32_t turn = 0;
   for (uint64_t row = (uint64_t)blockIdx.x * blockDim.y + threadIdx.y; row < a.rows; row += (uint64_t)gridDim.x * blockDim.y) {
@@ -470,6 +492,7 @@ __global__ void __launch_bounds__(256) narrow_kernel(const __grid_constant__ For
   constexpr int kWords = 8 / Word<T>::kPer;
   const Group g{1, 0, 0, threadIdx.x % 32};
   const uint64_t step = (uint64_t)gridDim.x * (blockDim.x / 32) * U;
+  if (a.then) start_next();
   uint32_t c[V];
   int n[V];
   uint64_t wt[V][4];
@@ -581,38 +604,46 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) turn_kernel(const
   const uint32_t tx = threadIdx.x % 16, ty = threadIdx.x / 16, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t across = (a.cols + kBlock - 1) / kBlock, down = (a.rows + kBlock - 1) / kBlock;
   const uint64_t tiles = (uint64_t)across * down;
+  wait_for_first();
+  // tiles from the last one on: each step goes back gridDim.x of them
+  const uint32_t back_r = gridDim.x / across, back_c = gridDim.x % across;
+  const auto step_back = [&](uint32_t &tr, uint32_t &tc) {
+    tr -= back_r + (tc < back_c);
+    tc = tc < back_c ? tc + across - back_c : tc - back_c;
+  };
   // thread (tx, ty) brings columns 8 tx + 0..7 of rows ty, ty + 16, ...
-  const auto fetch = [&](uint64_t t) {
-    const uint32_t tr = (uint32_t)(t / across), tc = (uint32_t)(t % across), c = tc * kBlock + 8 * tx;
-    const int n = c < a.cols ? (int)min(8u, a.cols - c) : 0;
+  const auto fetch = [&](uint32_t tr, uint32_t tc) {
+    const uint32_t c = tc * kBlock + 8 * tx, r = tr * kBlock + ty;
+    uint8_t *to = s_tile + ty * kPitch + tx * (8 * sizeof(T));
+    const T *h = static_cast<const T *>(a.h) + (int64_t)r * a.pitch + c;
+    if (a.wide && (tr + 1) * kBlock <= a.rows && (tc + 1) * kBlock <= a.cols) {
+      uint32_t at = smem_addr(to);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t k = ty + 16 * i, r = tr * kBlock + k;
-      const int here = r < a.rows ? n : 0;
-      const T *h = static_cast<const T *>(a.h) + (here ? (int64_t)r * a.pitch + c : 0);
-      uint8_t *to = s_tile + k * kPitch + tx * (8 * sizeof(T));
-      if (a.wide) {
+      for (int i = 0; i < 8; ++i, h += 16 * a.pitch)
 #pragma unroll
-        for (int j = 0; j < kWords; j += 4) {
-          const int bytes = min(max(here * (int)sizeof(T) - 4 * j, 0), 16);
-          copy_block(smem_addr(to + 4 * j), reinterpret_cast<const uint8_t *>(h) + (bytes ? 4 * j : 0), bytes);
-        }
-      } else {
+        for (int j = 0; j < kWords; j += 4) copy_block(at + i * 16 * kPitch + 4 * j, reinterpret_cast<const uint8_t *>(h) + 4 * j, 16);
+    } else {
+      const int n = c < a.cols ? (int)min(8u, a.cols - c) : 0;
+      for (int i = 0; i < 8; ++i, h += 16 * a.pitch, to += 16 * kPitch) {
         uint32_t w[kWords];
-        load8<T>(w, h, here, false);
+        load8<T>(w, h, r + 16 * i < a.rows ? n : 0, a.wide);
 #pragma unroll
         for (int j = 0; j < kWords; j += 4) *reinterpret_cast<uint4 *>(to + 4 * j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
       }
     }
     if (threadIdx.x < 128) {
-      const uint32_t r = tr * kBlock + threadIdx.x;
-      sh.rstd[threadIdx.x] = r < a.rows ? __ldg(a.rstd + r) : 0.0f;
+      const uint32_t k = tr * kBlock + threadIdx.x;
+      sh.rstd[threadIdx.x] = k < a.rows ? __ldg(a.rstd + k) : 0.0f;
     }
   };
-  if (blockIdx.x < tiles) fetch(tiles - 1 - blockIdx.x);
+  uint32_t tr = 0, tc = 0;
+  if (blockIdx.x < tiles) {
+    const uint64_t t = tiles - 1 - blockIdx.x;
+    tr = (uint32_t)(t / across), tc = (uint32_t)(t % across);
+    fetch(tr, tc);
+  }
   for (uint64_t s = blockIdx.x; s < tiles; s += gridDim.x) {
-    const uint64_t t = tiles - 1 - s;
-    const uint32_t tr = (uint32_t)(t / across), tc = (uint32_t)(t % across), r0 = tr * kBlock, c0 = tc * kBlock;
+    const uint32_t r0 = tr * kBlock, c0 = tc * kBlock;
     uint64_t wt[4];
     {
       const uint32_t c = c0 + 8 * tx;
@@ -731,14 +762,25 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) turn_kernel(const
       for (int j = 0; j < 8; ++j) sh.turn[(8 * tx + j) * 16 + (ty ^ tx)] = make_uint2(b[j][0], b[j][1]);
     }
     __syncthreads();
-    if (s + gridDim.x < tiles) fetch(tiles - 1 - s - gridDim.x);
     const uint32_t rr = r0 + 8 * tx;  // now tx counts pieces down a column
-    const int nr = rr < a.rows ? (int)min(8u, a.rows - rr) : 0;
+    const bool whole = r0 + kBlock <= a.rows && c0 + kBlock <= a.cols;
+    if (s + gridDim.x < tiles) {
+      step_back(tr, tc);
+      fetch(tr, tc);
+    }
     uint8_t *to = a.qt.data + (int64_t)(c0 + ty) * a.qt.pitch + rr;
+    if (whole) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i, to += 16 * a.qt.pitch) {
-      const uint32_t k = 16 * i + ty;
-      if (c0 + k < a.cols && nr) store8(to, sh.turn[k * 16 + (tx ^ k / 8)], nr);
+      for (int i = 0; i < 8; ++i, to += 16 * a.qt.pitch) {
+        const uint32_t k = 16 * i + ty;
+        *reinterpret_cast<uint2 *>(to) = sh.turn[k * 16 + (tx ^ k / 8)];
+      }
+    } else {
+      const int nr = rr < a.rows ? (int)min(8u, a.rows - rr) : 0;
+      for (int i = 0; i < 8; ++i, to += 16 * a.qt.pitch) {
+        const uint32_t k = 16 * i + ty;
+        if (c0 + k < a.cols && nr) store8(to, sh.turn[k * 16 + (tx ^ k / 8)], nr);
+      }
     }
   }
 }
@@ -810,24 +852,26 @@ template <typename T, int V, int U, bool WIDE, bool CLUSTER>
 __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ GradArgs a) {
   constexpr int kWords = 8 / Word<T>::kPer;
   extern __shared__ float s_sums[];  // [2][groups][warps], [groups][cols]
+  if (!CLUSTER && a.partial) start_next();
   const Group g{blockDim.x / 32, 1 + threadIdx.y, threadIdx.x / 32, threadIdx.x % 32};
   float *const part_sums = s_sums + 2 * blockDim.y * g.warps;
   uint32_t turn = 0;
   uint32_t c[V];
   int n[V];
-  uint64_t wt[V][4];
+  constexpr bool kAgain = V == 4;  // registers are short: weights come from L1 for each row, dresidual after the sum
+  uint64_t wt[kAgain ? 1 : V][4];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     c[v] = first_of<WIDE>(g.warp + v * g.warps, g.lane);
     n[v] = count_of<WIDE>(c[v], a.cols);
-    weights<WIDE>(wt[v], a.weight, a.wdtype, a.weight_aligned, c[v], n[v]);
+    if (!kAgain) weights<WIDE>(wt[v], a.weight, a.wdtype, a.weight_aligned, c[v], n[v]);
   }
   const uint32_t step = a.parts * blockDim.y;  // parts: of CTAs
   for (uint32_t part = blockIdx.x; part < a.parts; part += gridDim.x) {
     uint64_t acc[V][4] = {};
     for (uint64_t first = part * blockDim.y + threadIdx.y; first < a.rows; first += (uint64_t)step * U) {
       float *room = s_sums + (turn ^= 1) * blockDim.y * g.warps + threadIdx.y * g.warps;
-      uint32_t x[U][V][kWords], d[U][V][kWords], r[U][V][kWords];
+      uint32_t x[U][V][kWords], d[U][V][kWords], r[U][kAgain ? 1 : V][kWords];
       float rstd[U], dot[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -840,7 +884,7 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
           const int m = there ? n[v] : 0;
           load<T, WIDE>(x[u][v], static_cast<const T *>(a.x) + row * a.pitch + c[v], m);
           load<T, WIDE>(d[u][v], static_cast<const T *>(a.dout) + row * a.dout_pitch + c[v], m);
-          if (a.dresidual) load<T, WIDE>(r[u][v], static_cast<const T *>(a.dresidual) + row * a.dresidual_pitch + c[v], m);
+          if (!kAgain && a.dresidual) load<T, WIDE>(r[u][v], static_cast<const T *>(a.dresidual) + row * a.dresidual_pitch + c[v], m);
         }
       }
 #pragma unroll
@@ -848,14 +892,17 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
         if (u && first + (uint64_t)u * step >= a.rows) rstd[u] = 0.0f;  // nothing is added for a row that is not there
         uint64_t sum = 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
+        for (int v = 0; v < V; ++v) {
+          uint64_t(&w)[4] = wt[kAgain ? 0 : v];
+          if (kAgain) weights<WIDE>(w, a.weight, a.wdtype, a.weight_aligned, c[v], n[v]);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint64_t z, gg, dd;
-            z_and_g<T>(x[u][v], d[u][v], rstd[u], wt[v], i, &z, &gg, &dd);
+            z_and_g<T>(x[u][v], d[u][v], rstd[u], w, i, &z, &gg, &dd);
             sum = fma2(gg, z, sum);
             acc[v][i] = fma2(dd, z, acc[v][i]);
           }
+        }
         const float2 both = unpack2(sum);
         dot[u] = both.x + both.y;
       }
@@ -867,13 +914,18 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
         const float mean = dot[u] * a.inv_cols;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          uint32_t o[kWords];
+          uint32_t o[kWords], (&res)[kWords] = r[u][kAgain ? 0 : v];
+          uint64_t(&w)[4] = wt[kAgain ? 0 : v];
+          if (kAgain) {
+            weights<WIDE>(w, a.weight, a.wdtype, a.weight_aligned, c[v], n[v]);
+            if (a.dresidual) load<T, WIDE>(res, static_cast<const T *>(a.dresidual) + (int64_t)row * a.dresidual_pitch + c[v], n[v]);
+          }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint64_t z, gg, dd;
-            z_and_g<T>(x[u][v], d[u][v], rstd[u], wt[v], i, &z, &gg, &dd);
+            z_and_g<T>(x[u][v], d[u][v], rstd[u], w, i, &z, &gg, &dd);
             float2 f = unpack2(mul2(fma2(z, pack2(-mean, -mean), gg), pack2(rstd[u], rstd[u])));
-            if (a.dresidual) f.x += element<T>(r[u][v], 2 * i), f.y += element<T>(r[u][v], 2 * i + 1);
+            if (a.dresidual) f.x += element<T>(res, 2 * i), f.y += element<T>(res, 2 * i + 1);
             round_pair<T>(o, i, f.x, f.y);
           }
           store<T, WIDE>(static_cast<T *>(a.dx) + (int64_t)row * a.dx_pitch + c[v], o, n[v]);
@@ -925,6 +977,7 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
 template <typename T>
 __global__ void __launch_bounds__(1024, 1) grad_long_kernel(const __grid_constant__ GradArgs a) {
   __shared__ float room[2][32];
+  if (a.partial) start_next();
   const Group g{32, 0, threadIdx.x / 32, threadIdx.x % 32};
   uint32_t turn = 0;
   const auto weight = [&](uint32_t c) {
@@ -951,6 +1004,8 @@ __global__ void __launch_bounds__(1024, 1) grad_long_kernel(const __grid_constan
 template <typename T>
 __global__ void __launch_bounds__(256) grad_long_parts_kernel(const __grid_constant__ GradArgs a) {
   const uint64_t per = (a.cols + 255) / 256;
+  wait_for_first();
+  start_next();
   for (uint64_t t = blockIdx.x; t < per * a.parts; t += gridDim.x) {
     const uint32_t part = (uint32_t)(t / per), c = (uint32_t)(t % per) * 256 + threadIdx.x;
     if (c >= a.cols) continue;
@@ -967,6 +1022,7 @@ __global__ void __launch_bounds__(512) parts_kernel(const float *partial, uint32
   __shared__ float sums[16][32];
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const uint32_t runs = (cols + 31) / 32;
+  wait_for_first();
   for (uint32_t run = blockIdx.x; run < runs; run += gridDim.x) {
     const uint32_t c = run * 32 + lane;
     float s = 0.0f;
@@ -998,7 +1054,7 @@ __global__ void __launch_bounds__(512) parts_kernel(const float *partial, uint32
 // The weights lie in shared memory as fp32, as the threads' elements do; rows that a CTA
 // walks begin alike where the grid allows it, else the weights are laid out again for each.
 
-constexpr uint32_t kRingThreads = 512, kStagesMost = 3;
+constexpr uint32_t kStagesMost = 3;
 
 struct Ring {
   uint32_t stages, region, mats;  // region: bytes of a matrix's part of a stage
@@ -1017,13 +1073,14 @@ struct RingShared {
   int dead;
 };
 
-__device__ __forceinline__ void ring_begin(RingShared &sh, uint32_t stages) {
-  if (threadIdx.x == 0) {
-    for (uint32_t s = 0; s < stages; ++s) mbar_init(&sh.full[s], 1);
-    sh.dead = 0;
-    mbar_init_fence();
-  }
-  __syncthreads();
+// The barriers, and the first copies by `issue`: one thread.  A __syncthreads has to follow.
+template <typename F>
+__device__ __forceinline__ void ring_begin(RingShared &sh, uint32_t stages, F issue) {
+  if (threadIdx.x) return;
+  for (uint32_t s = 0; s < stages; ++s) mbar_init(&sh.full[s], 1);
+  sh.dead = 0;
+  mbar_init_fence();
+  for (uint32_t s = 0; s + 1 < stages; ++s) issue();
 }
 
 // The bounded wait for a stage.  After one that gave up nothing more is copied and nothing
@@ -1182,7 +1239,7 @@ __device__ __forceinline__ void ring_shifted(uint32_t (&w)[8 / Word<T>::kPer], c
 // 8-bit outputs have rows at multiples of 16 bytes: their threads take units that begin at
 // multiples of eight columns.  For rows that begin elsewhere the sum goes through the stage.
 template <typename T, int OUT, int V, bool WHOLE>
-__global__ void __launch_bounds__(kRingThreads, V == 2 ? 2 : 1) ring_forward_kernel(const __grid_constant__ ForwardArgs a,
+__global__ void __launch_bounds__(V == 1 ? 512 : 1024, V == 1 ? 2 : 1) ring_forward_kernel(const __grid_constant__ ForwardArgs a,
                                                                                     const __grid_constant__ Ring ring) {
   constexpr int kWords = 8 / Word<T>::kPer;
   extern __shared__ __align__(128) uint8_t s_ring[];
@@ -1190,7 +1247,7 @@ __global__ void __launch_bounds__(kRingThreads, V == 2 ? 2 : 1) ring_forward_ker
   const Group g{blockDim.x / 32, 0, threadIdx.x / 32, threadIdx.x % 32};
   const uint32_t units = V * blockDim.x;
   float *const laid = reinterpret_cast<float *>(s_ring + ring.stages * ring.stage());
-  ring_begin(sh, ring.stages);
+  if (a.then) start_next();
   const Source src[2] = {{a.x, a.pitch}, {a.residual, a.residual_pitch}};
   uint32_t next = blockIdx.x, into = 0;  // the row to copy next, its stage
   const auto issue = [&]() {
@@ -1200,13 +1257,10 @@ __global__ void __launch_bounds__(kRingThreads, V == 2 ? 2 : 1) ring_forward_ker
     }
     if (++into == ring.stages) into = 0;
   };
-  if (threadIdx.x == 0)
-    for (uint32_t s = 0; s + 1 < ring.stages; ++s) issue();
+  ring_begin(sh, ring.stages, issue);
   uint32_t shift = ~0u, stage = 0, parity = 0, turn = 0;
-  if (OUT != kSame) {
-    lay_weights(laid, a.weight, a.wdtype, units, 0, a.cols);
-    __syncthreads();
-  }
+  if (OUT != kSame) lay_weights(laid, a.weight, a.wdtype, units, 0, a.cols);
+  __syncthreads();
   for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const uint32_t skip = WHOLE ? 0 : skip_of(a.x, a.pitch, row, sizeof(T));
     if (OUT == kSame && skip != shift) {
@@ -1279,14 +1333,14 @@ __global__ void __launch_bounds__(kRingThreads, V == 2 ? 2 : 1) ring_forward_ker
 // The gradient's rows through a ring of x, dout and dresidual.  Part p is rows p, p + parts,
 // ...: rows of a part begin alike.
 template <typename T, int V, bool WHOLE>
-__global__ void __launch_bounds__(kRingThreads, 1) ring_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ Ring ring) {
+__global__ void __launch_bounds__(V == 1 ? 1024 : 512, 1) ring_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ Ring ring) {
   constexpr int kWords = 8 / Word<T>::kPer;
   extern __shared__ __align__(128) uint8_t s_ring[];
   __shared__ RingShared sh;
   const Group g{blockDim.x / 32, 0, threadIdx.x / 32, threadIdx.x % 32};
   const uint32_t units = V * blockDim.x;
   float *const laid = reinterpret_cast<float *>(s_ring + ring.stages * ring.stage());
-  ring_begin(sh, ring.stages);
+  if (a.partial) start_next();
   const Source src[3] = {{a.x, a.pitch}, {a.dout, a.dout_pitch}, {a.dresidual, a.dresidual_pitch}};
   uint32_t next_part = blockIdx.x, next = next_part, into = 0;
   const auto issue = [&]() {
@@ -1297,9 +1351,9 @@ __global__ void __launch_bounds__(kRingThreads, 1) ring_grad_kernel(const __grid
     }
     if (++into == ring.stages) into = 0;
   };
-  if (threadIdx.x == 0)
-    for (uint32_t s = 0; s + 1 < ring.stages; ++s) issue();
+  ring_begin(sh, ring.stages, issue);
   uint32_t shift = ~0u, stage = 0, parity = 0, turn = 0;
+  __syncthreads();
   for (uint32_t part = blockIdx.x; part < a.parts; part += gridDim.x) {
     uint64_t acc[V][4] = {};
     const uint32_t skip = WHOLE ? 0 : skip_of(a.x, a.pitch, part, sizeof(T));
@@ -1409,14 +1463,14 @@ struct RingShape {
   Ring ring;
 };
 
-RingShape ring_shape(const void *x, int64_t pitch, uint32_t rows, uint32_t cols, uint32_t size, uint32_t mats, uint32_t least, bool alike,
-                     bool pays) {
+RingShape ring_shape(const void *x, int64_t pitch, uint32_t rows, uint32_t cols, uint32_t size, uint32_t mats, uint32_t least, bool grad,
+                     bool alike, bool pays) {
   RingShape s = {};
   const bool begins = aligned(x, pitch * size);  // rows begin at blocks
   const uint32_t units = (cols + (begins ? 0 : 7) + 7) / 8;
   s.whole = begins && cols % 8 == 0;
-  if (size != 2 || (s.whole && !pays) || !alike || rows <= least || cols <= 512 || units > 4 * kRingThreads) return s;
-  s.v = units <= 2 * kRingThreads ? 2 : 4;
+  if (size != 2 || (s.whole && !pays) || !alike || rows <= least || cols <= 512 || units > 2048) return s;
+  s.v = grad ? units <= 1024 ? 1 : 4 : units <= 512 ? 1 : 2;
   s.threads = 32 * ((units + 32 * s.v - 1) / (32 * s.v));
   s.ring.region = (cols * size + 15 + 15) / 16 * 16 + 16;
   s.ring.mats = mats;
@@ -1464,13 +1518,13 @@ int forward_launch(const ForwardArgs &a, const Shape &s, void *stream) {
 
 template <typename T, int OUT>
 int forward(const ForwardArgs &a, const Shape &s, const RingShape &ring, bool wide, void *stream) {
-  if (ring.threads) {
+  if constexpr (sizeof(T) == 2) if (ring.threads) {
     const uint32_t period = period_of(a.pitch * (int64_t)sizeof(T));
     if (ring.whole)
-      return ring.v == 2 ? ring_launch(ring_forward_kernel<T, OUT, 2, true>, a, ring, a.rows, period, stream)
-                         : ring_launch(ring_forward_kernel<T, OUT, 4, true>, a, ring, a.rows, period, stream);
-    return ring.v == 2 ? ring_launch(ring_forward_kernel<T, OUT, 2, false>, a, ring, a.rows, period, stream)
-                       : ring_launch(ring_forward_kernel<T, OUT, 4, false>, a, ring, a.rows, period, stream);
+      return ring.v == 1 ? ring_launch(ring_forward_kernel<T, OUT, 1, true>, a, ring, a.rows, period, stream)
+                         : ring_launch(ring_forward_kernel<T, OUT, 2, true>, a, ring, a.rows, period, stream);
+    return ring.v == 1 ? ring_launch(ring_forward_kernel<T, OUT, 1, false>, a, ring, a.rows, period, stream)
+                       : ring_launch(ring_forward_kernel<T, OUT, 2, false>, a, ring, a.rows, period, stream);
   }
   if (a.cols <= 512 && a.rows > kNarrowRows) {
     const unsigned grid = grid_of((a.rows + 31) / 32, 4);
@@ -1506,6 +1560,8 @@ int launch_rms_norm(const NormArgs &n, unsigned sms, void *stream) {
   a.weight_aligned = (uintptr_t)n.weight % 16 == 0;
   two_parts(1.0 / n.cols, &a.c.inv_hi, &a.c.inv_lo);
   two_parts(n.eps, &a.c.eps_hi, &a.c.eps_lo);
+  // with much to transpose its CTAs would be in the way (8192 x 4096 72 us, 67 one after the other)
+  a.then = n.qt.data && (uint64_t)n.rows * n.cols <= 1u << 21;
   const Shape s = shape_of(n.cols, n.rows <= sms && n.cols <= 8192 ? 1 : 2);
   return with_dtype(n.dtype, [&](auto t) {
     using T = decltype(t);
@@ -1514,7 +1570,7 @@ int launch_rms_norm(const NormArgs &n, unsigned sms, void *stream) {
     const auto alike = [&](const void *p, int64_t pitch) {
       return same_place(n.x, n.pitch * (int64_t)sizeof(T), p, pitch * (int64_t)sizeof(T));
     };
-    const RingShape ring = ring_shape(n.x, n.pitch, n.rows, n.cols, sizeof(T), n.residual ? 2 : 1, 8 * sms,
+    const RingShape ring = ring_shape(n.x, n.pitch, n.rows, n.cols, sizeof(T), n.residual ? 2 : 1, 8 * sms, false,
                                       alike(n.residual, n.residual_pitch) && alike(n.sum, n.sum_pitch) && alike(n.out, n.out_pitch),
                                       !n.out);
     int e;
@@ -1531,8 +1587,9 @@ int launch_rms_norm(const NormArgs &n, unsigned sms, void *stream) {
     const auto turn = n.qt.e5m2 ? turn_kernel<T, true> : turn_kernel<T, false>;
     constexpr uint32_t bytes = 128 * 128 * sizeof(T);
     if ((e = (int)cudaFuncSetAttribute(turn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes))) return e;
-    turn<<<grid_of((uint64_t)((n.cols + kBlock - 1) / kBlock) * ((n.rows + kBlock - 1) / kBlock), sizeof(T) == 4 ? 2 : 4), 256, bytes,
-           (cudaStream_t)stream>>>(r);
+    const unsigned grid = grid_of((uint64_t)((n.cols + kBlock - 1) / kBlock) * ((n.rows + kBlock - 1) / kBlock), sizeof(T) == 4 ? 2 : 4);
+    if (a.then) return launch_after(turn, grid, 256, bytes, stream, r);
+    turn<<<grid, 256, bytes, (cudaStream_t)stream>>>(r);
     return (int)cudaGetLastError();
   });
 }
@@ -1560,10 +1617,11 @@ Few few_of(uint32_t rows, uint32_t cols) {
 
 }  // namespace
 
-// Parts, of a CTA each: two for every SM; none where a cluster does it.
+// Parts: two CTAs for every SM, or as many groups (the ring's CTAs are one); none where a cluster does it.
 uint32_t rms_norm_parts(uint32_t rows, uint32_t cols) {
   if (few_of(rows, cols).ctas) return 0;
-  return rows < kGradParts ? rows : kGradParts;
+  const uint32_t parts = kGradParts * grad_shape(cols).groups;
+  return rows < parts ? rows : parts;
 }
 
 namespace {
@@ -1607,21 +1665,23 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
     const auto at = [](const void *p, int64_t pitch) { return aligned(p, pitch * (int64_t)sizeof(T)); };
     if (!sh.fits) {
       grad_long_kernel<T><<<grid_of(n.rows, 1), 1024, 0, s>>>(a);
-      if (a.partial) grad_long_parts_kernel<T><<<grid_of((uint64_t)((n.cols + 255) / 256) * a.parts, 8), 256, 0, s>>>(a);
-      return (int)cudaGetLastError();
+      const int e = (int)cudaGetLastError();
+      if (e || !a.partial) return e;
+      return launch_after(grad_long_parts_kernel<T>, grid_of((uint64_t)((n.cols + 255) / 256) * a.parts, 8), 256, 0, s, a);
     }
     const auto alike = [&](const void *p, int64_t pitch) {
       return same_place(n.x, n.pitch * (int64_t)sizeof(T), p, pitch * (int64_t)sizeof(T));
     };
-    const RingShape ring = ring_shape(n.x, n.pitch, n.rows, n.cols, sizeof(T), n.dresidual ? 3 : 2, 2 * sms,
+    const RingShape ring = ring_shape(n.x, n.pitch, n.rows, n.cols, sizeof(T), n.dresidual ? 3 : 2, 2 * sms, true,
                                       alike(n.dout, n.dout_pitch) && alike(n.dresidual, n.dresidual_pitch) && alike(n.dx, n.dx_pitch),
                                       n.cols >= 2048 && n.cols <= 8192);
-    if (ring.threads && !few.ctas) {
+    if constexpr (sizeof(T) == 2) if (ring.threads && !few.ctas) {
+      a.parts = n.dweight ? rms_norm_parts(n.rows, n.cols) : n.rows;
       const uint32_t period = period_of(n.pitch * (int64_t)sizeof(T));
       if (ring.whole)
-        return ring.v == 2 ? ring_launch(ring_grad_kernel<T, 2, true>, a, ring, a.parts, period, stream)
+        return ring.v == 1 ? ring_launch(ring_grad_kernel<T, 1, true>, a, ring, a.parts, period, stream)
                            : ring_launch(ring_grad_kernel<T, 4, true>, a, ring, a.parts, period, stream);
-      return ring.v == 2 ? ring_launch(ring_grad_kernel<T, 2, false>, a, ring, a.parts, period, stream)
+      return ring.v == 1 ? ring_launch(ring_grad_kernel<T, 1, false>, a, ring, a.parts, period, stream)
                          : ring_launch(ring_grad_kernel<T, 4, false>, a, ring, a.parts, period, stream);
     }
     const bool wide = at(n.x, n.pitch) && at(n.dout, n.dout_pitch) && at(n.dresidual, n.dresidual_pitch) && at(n.dx, n.dx_pitch);
@@ -1643,7 +1703,10 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
     });
   });
   if (e || !n.dweight || few.ctas) return e;
-  parts_kernel<<<grid_of((n.cols + 31) / 32, 4), 512, 0, s>>>(n.work, a.parts, n.cols, n.dweight, n.dwdtype);
+  const unsigned grid = grid_of((n.cols + 31) / 32, 4);
+  const float *work = n.work;
+  if (n.rows) return launch_after(parts_kernel, grid, 512, 0, s, work, a.parts, n.cols, n.dweight, n.dwdtype);
+  parts_kernel<<<grid, 512, 0, s>>>(work, a.parts, n.cols, n.dweight, n.dwdtype);
   return (int)cudaGetLastError();
 }
 
