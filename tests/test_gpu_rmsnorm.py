@@ -304,3 +304,52 @@ def test_on_another_stream_and_in_a_graph():
         g.replay()
     for a, b in zip(got, want):
         assert torch.equal(a.float(), b.float())
+
+
+def test_a_whole_step_of_two_replicas(monkeypatch):
+    """Norm, product, distillation, products, the norm's gradient, the gradients' norm and the clipped step on one
+    stream: the gradients against 64 bits of what each operator was given, and equal digests on any grid."""
+    tokens, vocab, hidden, k, eps, most = 500, 1003, 272, 12, 1e-5, 1e-3
+    x, res, _ = inputs(tokens, hidden, torch.bfloat16, torch.bfloat16, 9)
+    head = torch.randn(vocab, hidden, generator=gen(2), device="cuda").mul_(0.05)
+    u, ids = torch.randn(tokens, vocab, generator=gen(3), device="cuda").mul_(3).topk(k, 1)
+    weights = torch.full((tokens,), 1.0 / tokens, device="cuda")
+
+    def run():
+        p = [head.clone(), torch.ones(hidden, device="cuda")]
+        w = [t.bfloat16() for t in p]
+        g = [torch.empty_like(t) for t in w]
+        m, v = [torch.zeros_like(t) for t in p], [torch.zeros_like(t) for t in p]
+        table = apc.prepare_table([apc.TensorEntry(*t, 1000 * i) for i, t in enumerate(zip(p, m, v, g, w))])
+        kept = []
+        for step in (1, 2):
+            x8, xs, x8t, xst, h, rstd = apc.rms_norm_fp8(x, w[1], eps=eps, residual=res, transposed=True)
+            w8, ws, w8t, wst = apc.quantize_fp8(w[0], block_rows=128, transposed=True)
+            logits = apc.matmul_fp8(x8, xs, w8, ws)
+            loss, _, d = apc.distill_loss_grad(logits, ids, u, weights, out=logits)
+            d8, ds, d8t, dst = apc.quantize_fp8(d, transposed=True)
+            dy = apc.matmul_fp8(d8, ds, w8t, wst)
+            apc.matmul_fp8(d8t, dst, x8t, xst, out=g[0])
+            dx, _ = apc.rms_norm_grad(dy, h, w[1], rstd, dweight=g[1])
+            norm = apc.grad_norm(table)
+            old = [t.clone() for t in p]
+            digests = apc.commit_step(table, step, grad_norm=norm, max_norm=most)
+            kept += [loss, dx, g[0].clone(), g[1].clone(), norm, digests] + [t.clone() for t in p + w]
+            if step == 1:
+                parts = apc.operators.rms_norm_grad_workspace(tokens, hidden) // hidden
+                check_grad(dy, h, w[1], rstd, None, dx, g[1], parts)
+                want = torch.cat([t.double().view(-1) for t in g]).norm()
+                assert norm.item() > most and abs(norm.item() - want.item()) <= 2.0 ** -20 * want.item()
+                # AdamW's first step from zero moments: every parameter moves by lr at most, and by nothing without a gradient
+                for a, b, q in zip(old, p, g):
+                    moved = (b - a * (1 - 3e-4 * 0.1)).abs()
+                    assert (moved <= 3e-4 * 1.001 + a.abs() * 2.0 ** -22).all() and (moved[q != 0] > 0).float().mean() > 0.9
+        return kept
+
+    a = run()
+    for limit in ("3", "50"):
+        monkeypatch.setenv("APC_GRID_LIMIT", limit)
+        for s, t in zip(a, run()):
+            assert torch.equal(s, t)
+    monkeypatch.delenv("APC_GRID_LIMIT")
+    assert apc.device_status() == 0
