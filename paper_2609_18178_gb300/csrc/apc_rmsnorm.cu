@@ -17,19 +17,66 @@ namespace {
 
 // ---------------------------------------------------------------------------
 // A row's sum of squares and its rstd.  Blocks are quantized by their largest value,
-// so a last bit of rstd can turn a scale: it is rounded once from a sum that does not
-// depend on how the row lies over the threads, up to the threads' own sums of 8 or 16
-// squares.  Those are added as integers: of 26 bits under the largest of a warp, warps'
-// sums with 20 bits more.  Integer additions across a warp are one instruction where
-// five shuffles and additions of pairs of floats took 35.
+// so a last bit of rstd can turn a scale, and the roundings of a whole row with it: rstd is
+// rounded once, from a sum that is exact but for 2^-40 of itself and so does not depend
+// on how the row lies over the threads.  A thread adds its squares in pairs of floats, the
+// second of which holds what the first one's additions lost (D. Knuth's sum, The Art of
+// Computer Programming 2, 4.2.2): 30 instructions for 8 squares, 7 without.  Threads' sums
+// are added as integers, of 26 bits under the largest of a warp and 20 behind: integer
+// additions across a warp are one instruction where five shuffles and additions of such
+// pairs took 50.
 
 constexpr uint32_t kLeast = 32;  // least e: 2^-120 of the sum, far below eps
 
-__device__ __forceinline__ Stat warp_stat(float p) {
-  const uint32_t top = __reduce_max_sync(~0u, __float_as_uint(p) & 0x7fffffffu);
+struct Two {
+  float hi, lo;
+};
+
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+  const float s = __fadd_rn(a.hi, b.hi), t = __fsub_rn(s, a.hi);
+  return {s, __fadd_rn(__fadd_rn(a.lo, b.lo), __fadd_rn(__fsub_rn(a.hi, __fsub_rn(s, t)), __fsub_rn(b.hi, t)))};
+}
+
+__device__ __forceinline__ uint64_t sub2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// The sum of two pairs, lane by lane; err: what it lost.
+__device__ __forceinline__ uint64_t two_sum2(uint64_t a, uint64_t b, uint64_t *err) {
+  const uint64_t s = add2(a, b), t = sub2(s, a);
+  *err = add2(sub2(a, sub2(s, t)), sub2(b, t));
+  return s;
+}
+
+// The squares of eight elements, each times `scale`.
+template <typename T, bool SCALED = false>
+__device__ __forceinline__ Two squares(const uint32_t (&w)[8 / Word<T>::kPer], float scale = 1.0f) {
+  uint64_t p[4], lost = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint64_t v = pack2(element<T>(w, 2 * i), element<T>(w, 2 * i + 1));
+    if (SCALED) v = mul2(v, pack2(scale, scale));
+    p[i] = mul2(v, v);  // exact for 16 bits
+    if (sizeof(T) == 4) lost = add2(lost, fma2(v, v, p[i] ^ 0x8000000080000000ull));
+  }
+  uint64_t e[3];
+  const uint64_t s = two_sum2(two_sum2(p[0], p[1], &e[0]), two_sum2(p[2], p[3], &e[1]), &e[2]);
+  lost = add2(add2(e[0], e[1]), sizeof(T) == 4 ? add2(e[2], lost) : e[2]);
+  const float2 a = unpack2(s), b = unpack2(lost);
+  return Two{a.x, b.x} + Two{a.y, b.y};
+}
+
+// A warp's sum of its threads' sums.
+__device__ __forceinline__ Stat warp_stat(Two p) {
+  const uint32_t top = __reduce_max_sync(~0u, __float_as_uint(p.hi) & 0x7fffffffu);
   const uint32_t e = max(top >> 23, kLeast);
-  const uint32_t i = e == 255 ? 0 : __float2uint_rn(p * __uint_as_float((279 - e) << 23));
-  return {__reduce_add_sync(~0u, i), e};
+  if (e == 255) return {0, 255, 0};
+  const float f = __uint_as_float((279 - e) << 23), t = p.hi * f;  // below 2^26
+  const uint32_t i = __float2uint_rn(t);
+  const int32_t low = __float2int_rn((__fsub_rn(t, (float)i) + p.lo * f) * 0x1p20f);
+  return {__reduce_add_sync(~0u, i), e, (int32_t)__reduce_add_sync(~0u, (uint32_t)low)};
 }
 
 struct NormConst {
@@ -64,22 +111,22 @@ __device__ __forceinline__ void split_sum(uint32_t s, float &hi, float &lo) {
 }
 
 // rstd of a row whose threads' sums of squares are p; false: a sum is not finite.
-__device__ __forceinline__ bool row_rstd(float p, const Group &g, Stat *room, const NormConst &c, bool with_eps, float *rstd) {
+__device__ __forceinline__ bool row_rstd(Two p, const Group &g, Stat *room, const NormConst &c, bool with_eps, float *rstd) {
   Stat s = warp_stat(p);
   float hi, lo;
   if (g.warps == 1) {
     if (s.e == 255) return false;
     split_sum(s.sum, hi, lo);
+    lo += (float)s.low * 0x1p-20f;
     *rstd = rstd_of(hi, lo, (int)s.e - 152, c, with_eps);
     return true;
   }
   if (g.lane == 0) room[g.warp] = s;
   g.sync();
-  s = g.lane < g.warps ? room[g.lane] : Stat{0, kLeast};
+  s = g.lane < g.warps ? room[g.lane] : Stat{0, kLeast, 0};
   const uint32_t e = __reduce_max_sync(~0u, s.e);
   if (e == 255) return false;
-  const uint32_t down = e - s.e;
-  const uint64_t v = down < 64 ? ((uint64_t)s.sum << 20) >> down : 0;
+  const int64_t v = (((int64_t)s.sum << 20) + s.low) >> min(e - s.e, 63u);
   const uint32_t high = __reduce_add_sync(~0u, (uint32_t)(v >> 26)), low = __reduce_add_sync(~0u, (uint32_t)v & 0x3ffffffu);
   split_sum(high, hi, lo);
   lo += (float)low * 0x1p-26f;
@@ -97,20 +144,6 @@ __device__ __forceinline__ uint32_t group_max(uint32_t m, const Group &g, Stat *
   m = __reduce_max_sync(~0u, g.lane < g.warps ? room[g.lane].sum : 0u);
   g.sync();
   return m;
-}
-
-// The squares of eight elements, each times `scale`.
-template <typename T, bool SCALED = false>
-__device__ __forceinline__ float squares(const uint32_t (&w)[8 / Word<T>::kPer], float scale = 1.0f) {
-  uint64_t acc[2];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint64_t v = pack2(element<T>(w, 2 * i), element<T>(w, 2 * i + 1));
-    if (SCALED) v = mul2(v, pack2(scale, scale));
-    acc[i % 2] = i < 2 ? mul2(v, v) : fma2(v, v, acc[i % 2]);
-  }
-  const float2 a = unpack2(acc[0]), b = unpack2(acc[1]);
-  return (a.x + a.y) + (b.x + b.y);
 }
 
 template <typename T>
@@ -131,9 +164,10 @@ __device__ __forceinline__ float wild_rstd(const uint32_t (&w)[V][8 / Word<T>::k
   m = group_max(m, g, room);
   if (m >= 0x7f800000u) return m > 0x7f800000u ? __uint_as_float(0x7fffffffu) : 0.0f;
   const float scale = __uint_as_float(max(254u - (m >> 23), 1u) << 23);
-  float p = 0.0f, rstd;
+  Two p = {0.0f, 0.0f};
+  float rstd;
 #pragma unroll
-  for (int v = 0; v < V; ++v) p += squares<T, true>(w[v], scale);
+  for (int v = 0; v < V; ++v) p = p + squares<T, true>(w[v], scale);
   row_rstd(p, g, room, c, false, &rstd);
   g.sync();
   return rstd * scale;
@@ -270,10 +304,11 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
       }
     };
     if (!LONG) fetch(g.warp, false);
-    float p = 0.0f, rstd;
+    Two p = {0.0f, 0.0f};
+    float rstd;
     over_row(false, [&](uint32_t) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) p += squares<T>(w[v]);
+      for (int v = 0; v < V; ++v) p = v || LONG ? p + squares<T>(w[v]) : squares<T>(w[v]);
     });
     if (!row_rstd(p, g, room, a.c, true, &rstd)) {
       uint32_t m = 0;
@@ -286,10 +321,10 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
         rstd = m > 0x7f800000u ? __uint_as_float(0x7fffffffu) : 0.0f;
       } else {  // squares beyond the largest number: eps is nothing beside them
         const float scale = __uint_as_float(max(254u - (m >> 23), 1u) << 23);
-        p = 0.0f;
+        p = {0.0f, 0.0f};
         over_row(true, [&](uint32_t) {
 #pragma unroll
-          for (int v = 0; v < V; ++v) p += squares<T, true>(w[v], scale);
+          for (int v = 0; v < V; ++v) p = p + squares<T, true>(w[v], scale);
         });
         row_rstd(p, g, room, a.c, false, &rstd);
         rstd *= scale;
@@ -376,9 +411,9 @@ __global__ void __launch_bounds__(256) narrow_kernel(const __grid_constant__ For
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float p = 0.0f;
+      Two p;
 #pragma unroll
-      for (int v = 0; v < V; ++v) p += squares<T>(w[u][v]);
+      for (int v = 0; v < V; ++v) p = v ? p + squares<T>(w[u][v]) : squares<T>(w[u][v]);
       if (!row_rstd(p, g, nullptr, a.c, true, &rstd[u])) rstd[u] = wild_rstd<T, V>(w[u], g, nullptr, a.c);
     }
 #pragma unroll
@@ -687,7 +722,8 @@ __global__ void __launch_bounds__(V == 1 ? 512 : 1024, V == 1 ? 2 : 1) ring_forw
     ring_wait(sh, stage, parity, ring.status);
     if (!WHOLE && ring.edges) ring_edges<T, 2>(src, ring, at, row, a.rows, a.cols);
     uint32_t w[V][kWords];
-    float p = 0.0f, rstd;
+    Two p;
+    float rstd;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const uint32_t k = threadIdx.x + v * blockDim.x;
@@ -704,7 +740,7 @@ __global__ void __launch_bounds__(V == 1 ? 512 : 1024, V == 1 ? 2 : 1) ring_forw
         for (int i = 0; i < kWords; i += 4)
           *reinterpret_cast<uint4 *>(at + k * (8 * sizeof(T)) + 4 * i) = make_uint4(w[v][i], w[v][i + 1], w[v][i + 2], w[v][i + 3]);
       }
-      p += squares<T>(w[v]);
+      p = v ? p + squares<T>(w[v]) : squares<T>(w[v]);
     }
     // before the next copy into a stage that was written here
     if (OUT != kSame && skip) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

@@ -190,9 +190,10 @@ struct Ring {
   __host__ __device__ uint32_t bytes() const { return stages * stage() + weights; }
 };
 
-// A warp's sum of squares: sum * 2^(e - 152).
-struct Stat {
+// A warp's sum of squares: (sum + low * 2^-20) * 2^(e - 152).
+struct __align__(16) Stat {
   uint32_t sum, e;
+  int32_t low;
 };
 
 struct RingShared {
