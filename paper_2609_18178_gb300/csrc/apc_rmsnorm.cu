@@ -122,16 +122,23 @@ __device__ __forceinline__ bool row_rstd(Two p, const Group &g, Stat *room, cons
     return true;
   }
   if (g.lane == 0) room[g.warp] = s;
-  g.sync();
-  s = g.lane < g.warps ? room[g.lane] : Stat{0, kLeast, 0};
-  const uint32_t e = __reduce_max_sync(~0u, s.e);
-  if (e == 255) return false;
-  const int64_t v = (((int64_t)s.sum << 20) + s.low) >> min(e - s.e, 63u);
-  const uint32_t high = __reduce_add_sync(~0u, (uint32_t)(v >> 26)), low = __reduce_add_sync(~0u, (uint32_t)v & 0x3ffffffu);
-  split_sum(high, hi, lo);
-  lo += (float)low * 0x1p-26f;
-  *rstd = rstd_of(hi, lo, (int)e - 146, c, with_eps);
-  return true;
+  if (g.warp == 0) {  // the others wait for one warp's work instead of doing it too
+    g.sync();
+    s = g.lane < g.warps ? room[g.lane] : Stat{0, kLeast, 0};
+    const uint32_t e = __reduce_max_sync(~0u, s.e);
+    const int64_t v = (((int64_t)s.sum << 20) + s.low) >> min(e - s.e, 63u);
+    const uint32_t high = __reduce_add_sync(~0u, (uint32_t)(v >> 26)), low = __reduce_add_sync(~0u, (uint32_t)v & 0x3ffffffu);
+    split_sum(high, hi, lo);
+    lo += (float)low * 0x1p-26f;
+    const float r = rstd_of(hi, lo, (int)min(e, 254u) - 146, c, with_eps);
+    if (g.lane == 0) room[g.warps] = {__float_as_uint(r), e, 0};
+  } else {
+    g.arrive();
+  }
+  g.sync_again();
+  s = room[g.warps];
+  *rstd = __uint_as_float(s.sum);
+  return s.e != 255;
 }
 
 // The largest magnitude's bits over a group.
@@ -254,7 +261,7 @@ __device__ __forceinline__ void quantize8(const ForwardArgs &a, uint32_t row, ui
 template <typename T, int OUT, int V, bool WIDE, bool LONG>
 __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant__ ForwardArgs a) {
   constexpr int kWords = 8 / Word<T>::kPer;
-  extern __shared__ Stat s_room[];  // [2][groups][warps]
+  extern __shared__ Stat s_room[];  // [2][groups][warps + 1]
   const Group g{blockDim.x / 32, 1 + threadIdx.y, threadIdx.x / 32, threadIdx.x % 32};
   if (a.then) start_next();
   const uint32_t groups = (LONG ? (a.cols + 255) / 256 : V * g.warps);  // runs of 256 columns
@@ -263,7 +270,7 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
     const T *x = static_cast<const T *>(a.x) + (int64_t)row * a.pitch;
     const T *res = static_cast<const T *>(a.residual) + (int64_t)row * a.residual_pitch;
     T *sum = static_cast<T *>(a.sum) + (int64_t)row * a.sum_pitch;
-    Stat *room = s_room + (turn ^= 1) * blockDim.y * g.warps + threadIdx.y * g.warps;
+    Stat *room = s_room + ((turn ^= 1) * blockDim.y + threadIdx.y) * (g.warps + 1);
     uint32_t w[V][kWords];
     // the sum's elements of V runs from `run` on, as they are stored
     const auto fetch = [&](uint32_t run, bool again) {
@@ -500,11 +507,21 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) turn_kernel(const
       for (int i = 0; i < 8; ++i, h += 16 * a.pitch)
 #pragma unroll
         for (int j = 0; j < kWords; j += 4) copy_block(at + i * 16 * kPitch + 4 * j, reinterpret_cast<const uint8_t *>(h) + 4 * j, 16);
+    } else if (a.wide) {  // zeros where there is nothing
+      const int n = c < a.cols ? (int)min(8u, a.cols - c) * (int)sizeof(T) : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i, h += 16 * a.pitch)
+#pragma unroll
+        for (int j = 0; j < kWords; j += 4) {
+          const int bytes = r + 16 * i < a.rows ? min(max(n - 4 * j, 0), 16) : 0;
+          copy_block(smem_addr(to) + i * 16 * kPitch + 4 * j, bytes ? reinterpret_cast<const uint8_t *>(h) + 4 * j : a.h, bytes);
+        }
     } else {
       const int n = c < a.cols ? (int)min(8u, a.cols - c) : 0;
+#pragma unroll 4
       for (int i = 0; i < 8; ++i, h += 16 * a.pitch, to += 16 * kPitch) {
         uint32_t w[kWords];
-        load8<T>(w, h, r + 16 * i < a.rows ? n : 0, a.wide);
+        load8<T>(w, h, r + 16 * i < a.rows ? n : 0, false);
 #pragma unroll
         for (int j = 0; j < kWords; j += 4) *reinterpret_cast<uint4 *>(to + 4 * j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
       }
@@ -787,7 +804,7 @@ template <typename T, int OUT, int V, bool WIDE, bool LONG>
 int forward_launch(const ForwardArgs &a, const Shape &s, void *stream) {
   const uint32_t per = s.threads * s.groups;
   const unsigned grid = grid_of((a.rows + s.groups - 1) / s.groups, 2048 / per);
-  const size_t room = sizeof(Stat) * 2 * per / 32;
+  const size_t room = sizeof(Stat) * 2 * (per / 32 + s.groups);
   forward_kernel<T, OUT, V, WIDE, LONG><<<grid, dim3(s.threads, s.groups), room, (cudaStream_t)stream>>>(a);
   return (int)cudaGetLastError();
 }
@@ -848,7 +865,7 @@ int launch_rms_norm(const NormArgs &n, unsigned sms, void *stream) {
     };
     const RingShape ring = ring_shape(n.x, n.pitch, n.rows, n.cols, sizeof(T), n.residual ? 2 : 1, 8 * sms, false,
                                       alike(n.residual, n.residual_pitch) && alike(n.sum, n.sum_pitch) && alike(n.out, n.out_pitch),
-                                      !n.out);
+                                      true);
     int e;
     if (n.out) e = forward<T, kSame>(a, s, ring, wide, stream);
     else e = n.q.e5m2 ? forward<T, kE5M2>(a, s, ring, wide, stream) : forward<T, kE4M3>(a, s, ring, wide, stream);

@@ -162,6 +162,9 @@ struct Group {
   __device__ void sync() const {
     if (warps > 1) group_sync(id, warps * 32);
   }
+  // for those who do not wait in a sync() of the others, and a barrier of its own behind it
+  __device__ void arrive() const { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(warps * 32) : "memory"); }
+  __device__ void sync_again() const { group_sync(id + 8, warps * 32); }
 };
 
 // ---------------------------------------------------------------------------
@@ -198,7 +201,7 @@ struct __align__(16) Stat {
 
 struct RingShared {
   uint64_t full[kStagesMost];
-  Stat stats[2][32];
+  Stat stats[2][33];
   float sums[2][32];
   int dead;
 };
@@ -373,11 +376,11 @@ unsigned grid_of(uint64_t want, uint32_t per_sm) {
 bool aligned(const void *p, int64_t pitch_bytes) { return (uintptr_t)p % 16 == 0 && pitch_bytes % 16 == 0; }
 
 // More rows than `least`, of 16 bits, alike within 16 bytes: the ring's shape, or none (threads
-// 0).  Where rows begin at blocks and end with them, plain loads by more warps keep up for most: the ring pays
-// where a row's work is long, for 8-bit outputs (8192 x 4096 46 us, 50 by plain loads; to 16 bits
-// 51 and 48, 4883 x 4096 of fp32 60 and 52) and for gradients of middling rows (8192 x 4096 59
-// and 63, 16384 x 1024 41 and 38, 4883 x 4096 of fp32 65 and 59).  Elsewhere in the
-// matrix it always does: 4001 x 5001 to 16 bits 35 us (46), its gradient 57 (100).
+// 0).  Where rows begin at blocks and end with them, plain loads by more warps keep up with it
+// for some (pays): 8192 x 4096 to 8 bits takes 45 us (50 by plain loads), to 16 bits 48 (51), its
+// gradient 53 (63), but the gradient of 16384 x 1024 33 (31).  fp32 rows do better without it
+// too: 4883 x 4096 52 us (60).  Elsewhere in the matrix 16-bit rows need it: 4001 x 5001 to 16
+// bits 35 us (46), its gradient 49 (100).
 struct RingShape {
   uint32_t threads;
   int v;
@@ -392,7 +395,8 @@ RingShape ring_shape(const void *x, int64_t pitch, uint32_t rows, uint32_t cols,
   const uint32_t units = (cols + (begins ? 0 : 7) + 7) / 8;
   s.whole = begins && cols % 8 == 0;
   if (size != 2 || (s.whole && !pays) || !alike || rows <= least || cols <= 512 || units > 2048) return s;
-  s.v = grad ? units <= 1024 ? 1 : 4 : units <= 512 ? 1 : 2;
+  // units a thread: with more than registers have room for, or barriers to wait for, fewer threads do more
+  s.v = grad ? units <= 1024 ? 1 : 4 : units <= 512 && mats == 2 ? 1 : 2;
   s.threads = 32 * ((units + 32 * s.v - 1) / (32 * s.v));
   s.ring.region = (cols * size + 15 + 15) / 16 * 16 + 16;
   s.ring.mats = mats;
