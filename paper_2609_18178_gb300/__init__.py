@@ -403,8 +403,8 @@ def _grads(grads):
             arr = (_Buffer * max(1, grads.count))()
             for i in range(grads.count):
                 arr[i] = _Buffer(grads.arr[i].g, grads.arr[i].n, 0, BF16, 0)
-            grads.grads = arr
             grads.work = library().apc_grad_norm_workspace(ctypes.addressof(arr), grads.count)
+            grads.grads = arr  # last: another thread may look
         return grads.grads, grads.count, grads.first
     grads = list(grads)
     arr = (_Buffer * max(1, len(grads)))()

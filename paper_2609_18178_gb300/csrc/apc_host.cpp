@@ -969,6 +969,7 @@ apc_status grad_norm(const apc_buffer *bufs, int32_t num_bufs, int32_t num_slots
     if (entries[k].n > (uint64_t)1 << 40) return fail(APC_ERANGE, "a buffer of more than 2^40 elements");
     tiles += norm_tiles(entries[k].n, entries[k].dtype);
   }
+  if (tiles > UINT32_MAX) return fail(APC_ERANGE, "buffers of more than 2^32 tiles");
   Grid grid{1, false};
   if (norm_is_small(entries.size(), tiles)) {
     work = nullptr;

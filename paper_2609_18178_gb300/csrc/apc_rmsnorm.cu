@@ -193,7 +193,7 @@ struct ForwardArgs {
   int64_t pitch, residual_pitch, sum_pitch, out_pitch;
   uint32_t rows, cols, wdtype;
   uint32_t weight_aligned;
-  uint32_t then;  // the transpose's kernel follows
+  uint32_t then;  // the transpose's kernel follows, and may start: 1 at once, 2 as CTAs end
   NormConst c;
 };
 
@@ -246,7 +246,8 @@ __device__ __forceinline__ void quantize8(const ForwardArgs &a, uint32_t row, ui
     const uint32_t c = first + (WIDE ? 0 : 32 * from);
     if (c % kBlock == 0 && here > 0) a.q.scale[(int64_t)(c / kBlock) * a.q.scale_pitch + row] = power(e);
     if (WIDE && !awkward) {
-      if (n) store8(at, to_fp8x8<E5M2>(y, pack2(inv, inv)), n);
+      if (n == 8) __stcs(reinterpret_cast<uint2 *>(at), to_fp8x8<E5M2>(y, pack2(inv, inv)));
+      else if (n) store8(at, to_fp8x8<E5M2>(y, pack2(inv, inv)), n);
     } else {
 #pragma unroll
       for (int i = from; i < to; ++i) {
@@ -263,7 +264,7 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
   constexpr int kWords = 8 / Word<T>::kPer;
   extern __shared__ Stat s_room[];  // [2][groups][warps + 1]
   const Group g{blockDim.x / 32, 1 + threadIdx.y, threadIdx.x / 32, threadIdx.x % 32};
-  if (a.then) start_next();
+  if (a.then == 1) start_next();
   const uint32_t groups = (LONG ? (a.cols + 255) / 256 : V * g.warps);  // runs of 256 columns
   uint32_t turn = 0;
   for (uint64_t row = (uint64_t)blockIdx.x * blockDim.y + threadIdx.y; row < a.rows; row += (uint64_t)gridDim.x * blockDim.y) {
@@ -377,7 +378,7 @@ __global__ void __launch_bounds__(256) narrow_kernel(const __grid_constant__ For
   constexpr int kWords = 8 / Word<T>::kPer;
   const Group g{1, 0, 0, threadIdx.x % 32};
   const uint64_t step = (uint64_t)gridDim.x * (blockDim.x / 32) * U;
-  if (a.then) start_next();
+  if (a.then == 1) start_next();
   uint32_t c[V];
   int n[V];
   uint64_t wt[V][4];
@@ -668,7 +669,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) turn_kernel(const
 #pragma unroll
       for (int i = 0; i < 8; ++i, to += 16 * a.qt.pitch) {
         const uint32_t k = 16 * i + ty;
-        *reinterpret_cast<uint2 *>(to) = sh.turn[k * 16 + (tx ^ k / 8)];
+        __stcs(reinterpret_cast<uint2 *>(to), sh.turn[k * 16 + (tx ^ k / 8)]);
       }
     } else {
       const int nr = rr < a.rows ? (int)min(8u, a.rows - rr) : 0;
@@ -713,7 +714,7 @@ __global__ void __launch_bounds__(V == 1 ? 512 : 1024, V == 1 ? 2 : 1) ring_forw
   const Group g{blockDim.x / 32, 0, threadIdx.x / 32, threadIdx.x % 32};
   const uint32_t units = V * blockDim.x;
   float *const laid = reinterpret_cast<float *>(s_ring + ring.stages * ring.stage());
-  if (a.then) start_next();
+  if (a.then == 1) start_next();
   const Source src[2] = {{a.x, a.pitch}, {a.residual, a.residual_pitch}};
   uint32_t next = blockIdx.x, into = 0;  // the row to copy next, its stage
   const auto issue = [&]() {
@@ -795,6 +796,7 @@ __global__ void __launch_bounds__(V == 1 ? 512 : 1024, V == 1 ? 2 : 1) ring_forw
     }
     if (++stage == ring.stages) stage = 0, parity ^= 1;
   }
+  if (a.then == 2) start_next();
 }
 
 // From so many rows on a warp takes several at a time.
@@ -853,8 +855,8 @@ int launch_rms_norm(const NormArgs &n, unsigned sms, void *stream) {
   a.weight_aligned = (uintptr_t)n.weight % 16 == 0;
   two_parts(1.0 / n.cols, &a.c.inv_hi, &a.c.inv_lo);
   two_parts(n.eps, &a.c.eps_hi, &a.c.eps_lo);
-  // with much to transpose its CTAs would be in the way (8192 x 4096 72 us, 67 one after the other)
-  a.then = n.qt.data && (uint64_t)n.rows * n.cols <= 1u << 21;
+  // with much to transpose CTAs that wait would be in the way (8192 x 4096: 72 us, 64 so)
+  a.then = !n.qt.data ? 0 : (uint64_t)n.rows * n.cols <= 1u << 21 ? 1 : 2;
   const Shape s = shape_of(n.cols, n.rows <= sms && n.cols <= 8192 ? 1 : 2);
   return with_dtype(n.dtype, [&](auto t) {
     using T = decltype(t);

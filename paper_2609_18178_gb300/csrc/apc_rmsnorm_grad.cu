@@ -204,7 +204,10 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
 template <typename T>
 __global__ void __launch_bounds__(1024, 1) grad_long_kernel(const __grid_constant__ GradArgs a) {
   __shared__ float room[2][32];
-  if (a.partial) start_next();
+  if (a.partial) {
+    wait_for_first();
+    start_next();
+  }
   const Group g{32, 0, threadIdx.x / 32, threadIdx.x % 32};
   uint32_t turn = 0;
   const auto weight = [&](uint32_t c) {
@@ -231,7 +234,6 @@ __global__ void __launch_bounds__(1024, 1) grad_long_kernel(const __grid_constan
 template <typename T>
 __global__ void __launch_bounds__(256) grad_long_parts_kernel(const __grid_constant__ GradArgs a) {
   const uint64_t per = (a.cols + 255) / 256;
-  wait_for_first();
   start_next();
   for (uint64_t t = blockIdx.x; t < per * a.parts; t += gridDim.x) {
     const uint32_t part = (uint32_t)(t / per), c = (uint32_t)(t % per) * 256 + threadIdx.x;
@@ -423,11 +425,15 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
   const int e = !n.rows ? 0 : with_dtype(n.dtype, [&](auto t) {
     using T = decltype(t);
     const auto at = [](const void *p, int64_t pitch) { return aligned(p, pitch * (int64_t)sizeof(T)); };
-    if (!sh.fits) {
-      grad_long_kernel<T><<<grid_of(n.rows, 1), 1024, 0, s>>>(a);
+    if (!sh.fits) {  // dweight's sums first: dx may take dout's place
+      const unsigned grid = grid_of(n.rows, 1);
+      if (!a.partial) {
+        grad_long_kernel<T><<<grid, 1024, 0, s>>>(a);
+        return (int)cudaGetLastError();
+      }
+      grad_long_parts_kernel<T><<<grid_of((uint64_t)((n.cols + 255) / 256) * a.parts, 8), 256, 0, s>>>(a);
       const int e = (int)cudaGetLastError();
-      if (e || !a.partial) return e;
-      return launch_after(grad_long_parts_kernel<T>, grid_of((uint64_t)((n.cols + 255) / 256) * a.parts, 8), 256, 0, s, a);
+      return e ? e : launch_after(grad_long_kernel<T>, grid, 1024, 0, s, a);
     }
     const auto alike = [&](const void *p, int64_t pitch) {
       return same_place(n.x, n.pitch * (int64_t)sizeof(T), p, pitch * (int64_t)sizeof(T));
