@@ -261,19 +261,20 @@ apc_status apc_commit_step_bf16_clipped(const apc_tensor_bf16 *table, int32_t nu
 /* ---- The operators around a training step's output head -----------------
  *
  * What makes the gradient that apc_commit_step consumes, for a model whose
- * head is distilled in 8 bits: quantization with a scale per block of 128, the
- * matrix product of such operands, and the distillation loss with its
- * gradient.  Every sum has a fixed order that follows the call's arguments and the
+ * head is distilled in 8 bits: the norm in front of the head, quantization with a
+ * scale per block of 128, the matrix product of such operands, the distillation
+ * loss with its gradient, and the norm's gradient.  Every sum has a fixed order that follows the call's arguments and the
  * number of the GPU's SMs, not the grid or the order of atomics, so replicas that run
  * the same step on the same kind of GPU commit identical bits and their digests agree.
- * One argument's address counts: sums over a row of logits follow the row's place
- * within 16 bytes, so equal bits need rows that are aligned alike.
+ * Some arguments' addresses count: sums over a row of logits, and those of the norm's
+ * gradient, follow the rows' place within 16 bytes, so equal bits need rows that are aligned
+ * alike.
  *
  * Matrices are row-major: element (i, j) of a matrix with pitch P sits at
  * i*P + j, and columns behind the last are neither read nor written.  A matrix
  * without rows or columns is valid and its pointers may be NULL.  Sizes are at
  * most 2^31 - 1 rows and columns.  Outputs must not overlap each other or any
- * input, but for the one aliasing that apc_distill_grad allows.  The
+ * input, but for what apc_distill_grad, apc_rms_norm and apc_rms_norm_grad allow.  The
  * conventions at the head of this file hold (device memory of the caller, no
  * synchronization, statuses); APC_GRID_LIMIT and apc_set_reserved_sms apply. */
 
@@ -330,8 +331,8 @@ apc_status apc_matmul_fp8(const apc_fp8_matrix *a, const apc_fp8_matrix *b, int6
 /* The root-mean-square norm of each row, after the residual's addition: what
  * stands in front of the head, whose operand it can write.
  *   h    = x + residual, rounded to x's type and kept in sum; x without a residual
- *   rstd = 1 / sqrt(mean of h^2 + eps), fp32: the mean of the stored h, rounded once
- *          from a sum that no thread layout changes beyond 2^-26 of itself
+ *   rstd = 1 / sqrt(mean of h^2 + eps), fp32: of the stored h, rounded once from a sum
+ *          that is exact to 2^-40 of itself, so that its bits do not follow the rows' layout
  *   y    = (h * rstd) * weight in fp32
  * Squares that overflow binary32 are taken scaled.  A row with a NaN has rstd NaN, one
  * with an infinity 0 (and NaNs where the infinities are).
@@ -361,8 +362,8 @@ apc_status apc_rms_norm_fp8(const apc_norm *d, const apc_fp8_matrix *q, const ap
 /* The gradient of the norm: with z = h * rstd and g = dout * weight,
  *   dx      = (g - z * mean of g z) * rstd + dresidual   (x's gradient and residual's)
  *   dweight = sum over rows of dout * z
- * in fp32, each rounded once.  The rows are summed in runs whose number follows rows and
- * cols alone, and the runs in order.
+ * in fp32, each rounded once.  The sums' orders follow the sizes, the types and how the
+ * matrices lie within 16 bytes, not the grid.
  *   x          h: the norm's sum, or its x where there was no residual
  *   dresidual  the gradient that reaches sum otherwise, or NULL
  *   rstd       as the norm left it */
