@@ -181,7 +181,7 @@ struct Group {
 // The weights lie in shared memory as fp32, as the threads' elements do; rows that a CTA
 // walks begin alike where the grid allows it, else the weights are laid out again for each.
 
-constexpr uint32_t kStagesMost = 3;
+constexpr uint32_t kStagesMost = 3, kRingBytes = 220 * 1024;
 
 struct Ring {
   uint32_t stages, region, mats;  // region: bytes of a matrix's part of a stage
@@ -402,7 +402,7 @@ RingShape ring_shape(const void *x, int64_t pitch, uint32_t rows, uint32_t cols,
   s.ring.mats = mats;
   s.ring.weights = s.threads * s.v * 32;
   s.ring.edges = ((uintptr_t)x % 16 != 0) | (((uintptr_t)x + ((int64_t)(rows - 1) * pitch + cols) * size) % 16 != 0) << 1;
-  for (s.ring.stages = 3; s.ring.stages > 1 && s.ring.bytes() > 220 * 1024; --s.ring.stages) {}
+  for (s.ring.stages = 3; s.ring.stages > 1 && s.ring.bytes() > kRingBytes; --s.ring.stages) {}
   if (s.ring.stages < 2) s.threads = 0;
   return s;
 }
@@ -413,7 +413,8 @@ template <typename K, typename A>
 int ring_launch(K kernel, const A &a, RingShape s, uint32_t work, uint32_t period, void *stream) {
   const uint32_t bytes = s.ring.bytes();
   int e = commit_status_word(&s.ring.status), per_sm = 1;
-  if (!e) e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  // the limit is what any launch takes: a call of another thread sets it too
+  if (!e) e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
   if (!e) e = (int)cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, (int)s.threads, bytes);
   if (e) return e;
   unsigned grid = grid_of(work, (uint32_t)per_sm);

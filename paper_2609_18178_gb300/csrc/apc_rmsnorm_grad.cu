@@ -391,7 +391,8 @@ namespace {
 template <typename K>
 int grad_few(K kernel, const GradArgs &a, const Shape &s, const Few &few, cudaStream_t stream) {
   const uint32_t bytes = (2 * few.groups * (s.threads / 32) + few.groups * a.cols) * sizeof(float);
-  int e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  constexpr int kMost = 72 * 1024;  // of any such launch: 16,384 columns in one group
+  int e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
   if (!e && few.ctas > 8) e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e) return e;
   cudaLaunchAttribute attr = {};

@@ -21,6 +21,7 @@ given; outputs that a call allocates are memory of that stream.
 from __future__ import annotations
 
 import ctypes
+from struct import Struct
 
 import torch
 
@@ -37,24 +38,15 @@ class _Fp8Matrix(ctypes.Structure):
                 ("scale_pitch", ctypes.c_int64), ("format", ctypes.c_uint32), ("block_rows", ctypes.c_uint32)]
 
 
-class _Norm(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "residual", "weight", "sum")] + \
-               [(n, ctypes.c_int64) for n in ("rows", "cols", "pitch", "residual_pitch", "sum_pitch")] + \
-               [("dtype", ctypes.c_uint32), ("weight_dtype", ctypes.c_uint32), ("eps", ctypes.c_double)]
-
-
-class _NormGrad(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_void_p) for n in ("dout", "x", "weight", "dresidual", "rstd")] + \
-               [(n, ctypes.c_int64) for n in ("rows", "cols", "dout_pitch", "pitch", "dresidual_pitch")] + \
-               [("dtype", ctypes.c_uint32), ("weight_dtype", ctypes.c_uint32)]
-
-
 class _Distill(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("logits", "ids", "teacher", "teacher_lse", "labels")] + \
                [(n, ctypes.c_int64) for n in ("rows", "vocab", "k", "pitch", "ids_pitch", "teacher_pitch")] + \
                [(n, ctypes.c_uint32) for n in ("dtype", "ids_dtype", "teacher_dtype", "labels_dtype")] + \
                [(n, ctypes.c_double) for n in ("temperature", "kd_weight", "label_weight")]
 
+
+# The structures of a call as bytes, packed in one step (a ctypes structure takes 0.4 us more)
+_pack_fp8, _pack_norm, _pack_norm_grad = (Struct(f).pack for f in ("2P2q2I", "4P5q2Id", "5P5q2I"))
 
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # the handle without a Stream object around it
@@ -131,8 +123,8 @@ def _blocks(n: int) -> int:
 
 
 def _fp8(data, scale, name: str, device: int, block=None):
-    """The C structure of an 8-bit matrix, its rows and columns; block: its rows
-    per scale, found from the scale's shape if not given."""
+    """The C structure of an 8-bit matrix, its rows, columns and format; block: its
+    rows per scale, found from the scale's shape if not given."""
     kind, r, c, pitch = _matrix(data, name, _FORMAT, device)
     _, lines, width, scale_pitch = _matrix(scale, name + "_scale", _F32, device)
     if block is None:
@@ -140,7 +132,7 @@ def _fp8(data, scale, name: str, device: int, block=None):
     if lines != (c + BLOCK - 1) // BLOCK or width != (r if block == 1 else -(-r // block)):
         raise ValueError("%s_scale is %d x %d: expected %d x %d, or %d columns for square blocks"
                          % (name, lines, width, _blocks(c), r, _blocks(r)))
-    return _Fp8Matrix(data.data_ptr(), scale.data_ptr(), pitch, scale_pitch, kind, block), r, c
+    return _pack_fp8(data.data_ptr(), scale.data_ptr(), pitch, scale_pitch, kind, block), r, c, kind
 
 
 def _empty(shape, dtype, like, stream):
@@ -182,16 +174,15 @@ def quantize_fp8(x, block_rows: int = 1, dtype=torch.float8_e4m3fn, transposed: 
             out += _fp8_empty(c, r, block_rows, dtype, x, stream)
     elif len(out) != (4 if transposed else 2):
         raise ValueError("out has %d tensors, expected %d" % (len(out), 4 if transposed else 2))
-    q, qr, qc = _fp8(out[0], out[1], "q", device, block_rows)
-    if qr != r or qc != c or q.format != _FORMAT[dtype]:
+    q, qr, qc, fmt = _fp8(out[0], out[1], "q", device, block_rows)
+    if qr != r or qc != c or fmt != _FORMAT[dtype]:
         raise ValueError("out: q is %d x %d of %s, expected %d x %d of %s" % (qr, qc, out[0].dtype, r, c, dtype))
     qt = None
     if transposed:
-        qt, qr, qc = _fp8(out[2], out[3], "qt", device, block_rows)
-        if qr != c or qc != r or qt.format != _FORMAT[dtype]:
+        qt, qr, qc, fmt = _fp8(out[2], out[3], "qt", device, block_rows)
+        if qr != c or qc != r or fmt != _FORMAT[dtype]:
             raise ValueError("out: qt is %d x %d of %s, expected %d x %d of %s" % (qr, qc, out[2].dtype, c, r, dtype))
-        qt = ctypes.byref(qt)
-    _check(lib.apc_quantize_fp8(x.data_ptr(), r, c, pitch, kind, ctypes.byref(q), qt, _stream(stream, device)))
+    _check(lib.apc_quantize_fp8(x.data_ptr(), r, c, pitch, kind, q, qt, _stream(stream, device)))
     return tuple(out)
 
 
@@ -202,7 +193,8 @@ def _weight(x, name: str, device: int, n: int) -> int:
 
 
 def _norm(x, weight, eps, residual, sum, rstd, device, stream):
-    """The C structure of a norm, its sum (x itself without a residual) and rstd."""
+    """The C structure of a norm, its rows and columns, its sum (x itself
+    without a residual) and rstd."""
     kind, r, c, pitch = _matrix(x, "x", _DTYPE, device)
     wkind = _weight(weight, "weight", device, c)
     if rstd is None:
@@ -212,14 +204,14 @@ def _norm(x, weight, eps, residual, sum, rstd, device, stream):
     if residual is None:
         if sum is not None:
             raise ValueError("sum without a residual")
-        return _Norm(x.data_ptr(), None, weight.data_ptr(), None, r, c, pitch, 0, 0, kind, wkind, eps), x, rstd
+        return _pack_norm(x.data_ptr(), 0, weight.data_ptr(), 0, r, c, pitch, 0, 0, kind, wkind, eps), r, c, x, rstd
     same = {x.dtype: kind}
     rpitch = _sized(residual, "residual", same, device, r, c)[1]
     if sum is None:
         sum = _empty((r, c), x.dtype, x, stream)
     spitch = _sized(sum, "sum", same, device, r, c)[1]
-    return _Norm(x.data_ptr(), residual.data_ptr(), weight.data_ptr(), sum.data_ptr(), r, c, pitch, rpitch, spitch, kind, wkind,
-                 eps), sum, rstd
+    return _pack_norm(x.data_ptr(), residual.data_ptr(), weight.data_ptr(), sum.data_ptr(), r, c, pitch, rpitch, spitch, kind,
+                      wkind, eps), r, c, sum, rstd
 
 
 def rms_norm(x, weight, *, eps=1e-6, residual=None, out=None, sum=None, rstd=None, stream=None):
@@ -233,11 +225,11 @@ def rms_norm(x, weight, *, eps=1e-6, residual=None, out=None, sum=None, rstd=Non
     ``residual`` itself."""
     lib = _library()
     device = _current_device()
-    d, sum, rstd = _norm(x, weight, eps, residual, sum, rstd, device, stream)
+    d, r, c, sum, rstd = _norm(x, weight, eps, residual, sum, rstd, device, stream)
     if out is None:
-        out = _empty((d.rows, d.cols), x.dtype, x, stream)
-    pitch = _sized(out, "out", {x.dtype: 0}, device, d.rows, d.cols)[1]
-    _check(lib.apc_rms_norm(ctypes.byref(d), out.data_ptr(), pitch, rstd.data_ptr(), _stream(stream, device)))
+        out = _empty((r, c), x.dtype, x, stream)
+    pitch = _sized(out, "out", {x.dtype: 0}, device, r, c)[1]
+    _check(lib.apc_rms_norm(d, out.data_ptr(), pitch, rstd.data_ptr(), _stream(stream, device)))
     return out, sum, rstd
 
 
@@ -254,24 +246,22 @@ def rms_norm_fp8(x, weight, *, eps=1e-6, residual=None, dtype=torch.float8_e4m3f
     device = _current_device()
     if dtype not in _FORMAT:
         raise ValueError("dtype %s is not an 8-bit floating type" % dtype)
-    d, sum, rstd = _norm(x, weight, eps, residual, sum, rstd, device, stream)
-    r, c = d.rows, d.cols
+    d, r, c, sum, rstd = _norm(x, weight, eps, residual, sum, rstd, device, stream)
     if out is None:
         out = _fp8_empty(r, c, 1, dtype, x, stream)
         if transposed:
             out += _fp8_empty(c, r, 1, dtype, x, stream)
     elif len(out) != (4 if transposed else 2):
         raise ValueError("out has %d tensors, expected %d" % (len(out), 4 if transposed else 2))
-    q, qr, qc = _fp8(out[0], out[1], "q", device, 1)
-    if qr != r or qc != c or q.format != _FORMAT[dtype]:
+    q, qr, qc, fmt = _fp8(out[0], out[1], "q", device, 1)
+    if qr != r or qc != c or fmt != _FORMAT[dtype]:
         raise ValueError("out: q is %d x %d of %s, expected %d x %d of %s" % (qr, qc, out[0].dtype, r, c, dtype))
     qt = None
     if transposed:
-        qt, qr, qc = _fp8(out[2], out[3], "qt", device, 1)
-        if qr != c or qc != r or qt.format != _FORMAT[dtype]:
+        qt, qr, qc, fmt = _fp8(out[2], out[3], "qt", device, 1)
+        if qr != c or qc != r or fmt != _FORMAT[dtype]:
             raise ValueError("out: qt is %d x %d of %s, expected %d x %d of %s" % (qr, qc, out[2].dtype, c, r, dtype))
-        qt = ctypes.byref(qt)
-    _check(lib.apc_rms_norm_fp8(ctypes.byref(d), ctypes.byref(q), qt, rstd.data_ptr(), _stream(stream, device)))
+    _check(lib.apc_rms_norm_fp8(d, q, qt, rstd.data_ptr(), _stream(stream, device)))
     return *out, sum, rstd
 
 
@@ -294,8 +284,8 @@ def rms_norm_grad(dout, x, weight, rstd, *, dresidual=None, out=None, dweight=No
     same = {x.dtype: kind}
     dpitch = _sized(dout, "dout", same, device, r, c)[1]
     rpitch = 0 if dresidual is None else _sized(dresidual, "dresidual", same, device, r, c)[1]
-    d = _NormGrad(dout.data_ptr(), x.data_ptr(), weight.data_ptr(), None if dresidual is None else dresidual.data_ptr(),
-                  _vector(rstd, "rstd", _F32, device, r), r, c, dpitch, pitch, rpitch, kind, _weight(weight, "weight", device, c))
+    d = _pack_norm_grad(dout.data_ptr(), x.data_ptr(), weight.data_ptr(), 0 if dresidual is None else dresidual.data_ptr(),
+                        _vector(rstd, "rstd", _F32, device, r), r, c, dpitch, pitch, rpitch, kind, _weight(weight, "weight", device, c))
     if out is None:
         out = _empty((r, c), x.dtype, x, stream)
     opitch = _sized(out, "out", same, device, r, c)[1]
@@ -314,7 +304,7 @@ def rms_norm_grad(dout, x, weight, rstd, *, dresidual=None, out=None, dweight=No
             work = _vector(workspace, "workspace", _F32, device, n)
     elif dweight is not None:
         raise ValueError("dweight without weight_grad")
-    _check(lib.apc_rms_norm_grad(ctypes.byref(d), out.data_ptr(), opitch, at, wkind, work, _stream(stream, device)))
+    _check(lib.apc_rms_norm_grad(d, out.data_ptr(), opitch, at, wkind, work, _stream(stream, device)))
     return out, dweight
 
 
@@ -329,14 +319,14 @@ def matmul_fp8(a, a_scale, b, b_scale, out=None, out_dtype=torch.bfloat16, strea
     fp32, bf16 or fp16), or fills the one given, of any row pitch."""
     lib = _library()
     device = _current_device()
-    p, m, k = _fp8(a, a_scale, "a", device)
-    q, n, kb = _fp8(b, b_scale, "b", device)
+    p, m, k, _ = _fp8(a, a_scale, "a", device)
+    q, n, kb, _ = _fp8(b, b_scale, "b", device)
     if kb != k:
         raise ValueError("a has %d columns and b has %d" % (k, kb))
     if out is None:
         out = _empty((m, n), out_dtype, a, stream)
     kind, pitch = _sized(out, "out", _DTYPE, device, m, n)
-    _check(lib.apc_matmul_fp8(ctypes.byref(p), ctypes.byref(q), m, n, k, out.data_ptr(), pitch, kind, _stream(stream, device)))
+    _check(lib.apc_matmul_fp8(p, q, m, n, k, out.data_ptr(), pitch, kind, _stream(stream, device)))
     return out
 
 

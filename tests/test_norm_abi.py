@@ -6,7 +6,24 @@ import ctypes
 import pytest
 
 import paper_2609_18178_gb300 as apc
-from paper_2609_18178_gb300.operators import _Fp8Matrix, _Norm, _NormGrad
+from paper_2609_18178_gb300 import operators
+from paper_2609_18178_gb300.operators import _Fp8Matrix
+
+
+
+class _Norm(ctypes.Structure):
+    """apc_norm, field by field."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "residual", "weight", "sum")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "cols", "pitch", "residual_pitch", "sum_pitch")] + \
+               [("dtype", ctypes.c_uint32), ("weight_dtype", ctypes.c_uint32), ("eps", ctypes.c_double)]
+
+
+class _NormGrad(ctypes.Structure):
+    """apc_norm_grad, field by field."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dout", "x", "weight", "dresidual", "rstd")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "cols", "dout_pitch", "pitch", "dresidual_pitch")] + \
+               [("dtype", ctypes.c_uint32), ("weight_dtype", ctypes.c_uint32)]
+
 
 EINVAL, EALIGN, ERANGE, ECUDA = 1, 2, 3, 4
 AT = 1 << 40  # an address that nothing dereferences
@@ -226,9 +243,12 @@ def test_clipped_commit_refuses(bf16, want, kw):
     assert apc.library().apc_last_error()
 
 
-def test_struct_layout():
-    assert ctypes.sizeof(_Norm) == 4 * 8 + 5 * 8 + 2 * 4 + 8
-    assert ctypes.sizeof(_NormGrad) == 5 * 8 + 5 * 8 + 2 * 4
+def test_packed_structures_are_the_header_s():
+    """What the binding packs has the fields' places of the structures."""
+    for pack, like, values in ((operators._pack_norm, _Norm, list(range(1, 12)) + [0.5]),
+                               (operators._pack_norm_grad, _NormGrad, list(range(1, 13))),
+                               (operators._pack_fp8, _Fp8Matrix, list(range(1, 7)))):
+        assert pack(*values) == bytes(like(*values)) and len(pack(*values)) == ctypes.sizeof(like)
 
 
 # ---- the binding
@@ -236,7 +256,6 @@ def test_struct_layout():
 @pytest.fixture
 def on_cpu(monkeypatch):
     """The binding with the CPU for the current device and a library that takes everything."""
-    from paper_2609_18178_gb300 import operators
     real = apc.library()
 
     class Library:
