@@ -456,18 +456,24 @@ def grad_norm(grads, num_slots: int = 1, stream=None, out=None, workspace=None):
     other call may use at the same time; short lists take none."""
     import torch
     arr, n, first = _grads(grads)
-    if out is None or workspace is None:
-        dev = first.device if hasattr(first, "device") else torch.device("cuda", torch.cuda.current_device())
     if out is None:
+        dev = first.device if hasattr(first, "device") else torch.device("cuda", torch.cuda.current_device())
         out = _empty(num_slots, torch.float32, dev, stream)
     elif not isinstance(out, int) and (out.dtype != torch.float32 or out.numel() < num_slots):
         raise ValueError("out: expected %d float32 values, got %s of %s" % (num_slots, tuple(out.shape), out.dtype))
-    if workspace is None:
-        bytes = grads.work if isinstance(grads, PreparedTable) else library().apc_grad_norm_workspace(ctypes.addressof(arr), n)
-        workspace = _empty(bytes // 8, torch.int64, dev, stream) if bytes else None
-    elif not isinstance(workspace, int) and workspace.numel() * workspace.element_size() < GRAD_NORM_WORKSPACE:
+    if workspace is not None and not isinstance(workspace, int) and workspace.numel() * workspace.element_size() < GRAD_NORM_WORKSPACE:
         raise ValueError("workspace holds fewer than %d bytes" % GRAD_NORM_WORKSPACE)
-    _check(library().apc_grad_norm(ctypes.addressof(arr), n, int(num_slots), _ptr(workspace), _stream(stream), _ptr(out)))
+    handle = _stream(stream)
+    given = ctypes.addressof(arr), n, int(num_slots)
+    size = 0
+    if workspace is None:
+        size = grads.work if isinstance(grads, PreparedTable) else library().apc_grad_norm_workspace(ctypes.addressof(arr), n)
+    if size:
+        from .operators import _Workspace
+        with _Workspace(size, stream, handle) as work:
+            _check(library().apc_grad_norm(*given, work, handle, _ptr(out)))
+    else:
+        _check(library().apc_grad_norm(*given, _ptr(workspace), handle, _ptr(out)))
     return out
 
 

@@ -316,6 +316,9 @@ def test_allocated_outputs_are_memory_of_the_stream_given(on_cpu, monkeypatch):
         current.pop()
 
     empty = torch.empty
+    held = []
+    monkeypatch.setattr(operators, "_raw_alloc", lambda size, stream: asked.append([stream]) or held.append(size) or 1 << 40)
+    monkeypatch.setattr(operators, "_raw_free", lambda at: held.pop())
     monkeypatch.setattr(torch.cuda, "Stream", Stream)
     monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
     monkeypatch.setattr(torch.cuda, "stream", use)
@@ -331,7 +334,12 @@ def test_allocated_outputs_are_memory_of_the_stream_given(on_cpu, monkeypatch):
                               (lambda: apc.grad_norm([x] * 1700, stream=s), 2)):
             del asked[:]
             call()
-            assert asked == [[0x1230]] * outputs
+            assert asked == [[0x1230]] * outputs and not held
+    # a call that is refused gives its workspace back
+    monkeypatch.setattr(operators, "_check", lambda status: 1 / 0)
+    with pytest.raises(ZeroDivisionError):
+        apc.rms_norm_grad(big, big, torch.ones(400), torch.ones(3000), stream=0x1230)
+    assert not held
 
 
 def test_a_commit_table_gives_its_gradients(on_cpu):
