@@ -160,16 +160,16 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
       }
     }
     if (!CLUSTER && !a.partial) continue;
-    const bool alone = !CLUSTER && blockDim.y == 1;
-    float *const sums = alone ? a.partial + (uint64_t)part * a.cols : part_sums + threadIdx.y * a.cols;
+    // by way of shared memory, a warp's stores to the workspace being neighbours: 4-byte stores 32
+    // bytes apart took 5 us more for 304 parts of 4,096 columns
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float2 f = unpack2(acc[v][i / 2]);
-        if (i < n[v]) sums[c[v] + (WIDE ? i : 32 * i)] = i % 2 ? f.y : f.x;
+        if (i < n[v]) part_sums[threadIdx.y * a.cols + c[v] + (WIDE ? i : 32 * i)] = i % 2 ? f.y : f.x;
       }
-    if (CLUSTER || alone) continue;
+    if (CLUSTER) continue;
     __syncthreads();
     for (uint32_t k = threadIdx.y * blockDim.x + threadIdx.x; k < a.cols; k += blockDim.x * blockDim.y) {
       float s = 0.0f;
@@ -252,9 +252,10 @@ __global__ void __launch_bounds__(256) grad_long_parts_kernel(const __grid_const
   }
 }
 
-// dweight: the parts' sums, 32 columns a CTA, warp k those of parts k, k + 16, ..., then the warps'.
-__global__ void __launch_bounds__(512) parts_kernel(const float *partial, uint32_t parts, uint32_t cols, void *dweight, uint32_t dtype) {
-  __shared__ float sums[16][32];
+// dweight: the parts' sums, 32 columns a CTA, warp k those of parts k, k + 32, ..., ten loads of a
+// lane under way, then the warps'.
+__global__ void __launch_bounds__(1024) parts_kernel(const float *partial, uint32_t parts, uint32_t cols, void *dweight, uint32_t dtype) {
+  __shared__ float sums[32][33];
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const uint32_t runs = (cols + 31) / 32;
   wait_for_first();
@@ -262,16 +263,19 @@ __global__ void __launch_bounds__(512) parts_kernel(const float *partial, uint32
     const uint32_t c = run * 32 + lane;
     float s = 0.0f;
     if (c < cols)
-#pragma unroll 8
-      for (uint32_t p = warp; p < parts; p += 16) s += __ldcg(partial + (uint64_t)p * cols + c);
+      for (uint32_t p = warp; p < parts; p += 320) {
+        float f[10];
+#pragma unroll
+        for (uint32_t i = 0; i < 10; ++i) f[i] = p + 32 * i < parts ? __ldcg(partial + (uint64_t)(p + 32 * i) * cols + c) : 0.0f;
+        s += (((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]))) + (f[8] + f[9]);
+      }
     __syncthreads();
     sums[warp][lane] = s;
     __syncthreads();
-    if (warp || c >= cols) continue;
-    float y = 0.0f;
+    float y = sums[lane][warp];  // column `warp`, a part of it in each lane
 #pragma unroll
-    for (int k = 0; k < 16; k += 4) y += (sums[k][lane] + sums[k + 1][lane]) + (sums[k + 2][lane] + sums[k + 3][lane]);
-    store_weight(dweight, dtype, c, y);
+    for (int o = 16; o; o >>= 1) y += __shfl_xor_sync(~0u, y, o);
+    if (lane == 0 && run * 32 + warp < cols) store_weight(dweight, dtype, run * 32 + warp, y);
   }
 }
 
@@ -351,33 +355,39 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512, 1) ring_grad_kernel(const
       if (++stage == ring.stages) stage = 0, parity ^= 1;
     }
     if (!a.partial) continue;
+    // by way of the stage that the last row has left, as in grad_kernel
+    float *const sums = reinterpret_cast<float *>(s_ring + (stage ? stage - 1 : ring.stages - 1) * ring.stage());
+    __syncthreads();
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const Unit<WHOLE> u(threadIdx.x + v * blockDim.x, skip / sizeof(T), a.cols);
-      float *to = a.partial + (uint64_t)part * a.cols + u.first;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float2 f = unpack2(acc[v][i / 2]);
-        if (u.first + i >= 0 && u.first + i < (int32_t)a.cols) to[i] = i % 2 ? f.y : f.x;
+        if (u.first + i >= 0 && u.first + i < (int32_t)a.cols) sums[u.first + i] = i % 2 ? f.y : f.x;
       }
     }
+    __syncthreads();
+    for (uint32_t k = threadIdx.x; k < a.cols; k += blockDim.x) a.partial[(uint64_t)part * a.cols + k] = sums[k];
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the next copy comes behind a barrier
   }
 }
 
 // Few rows: a cluster of so many CTAs (0: none) of so many groups, up to 8 rows for each.  It
-// saves 2.4 us of host time: 64 x 1024 takes 4.6 us of kernel time (5.4 by two kernels), 128 x
-// 4096 10.4 (7.2), 256 x 4096 would take 15.0 (10.3).
+// saves 2.4 us of host time: 64 x 1024 takes 4.6 us of kernel time (5.1 by two kernels), 64 x
+// 4096 7.8 (6.4), 128 x 4096 would take 10.4 (6.5) and 1000 x 500 11.8 (7.3).
 struct Few {
   uint32_t ctas, groups;
 };
 
 constexpr uint32_t kGradParts = 304;
+constexpr int kSumsBytes = 72 * 1024;  // shared memory of any launch of grad_kernel: 16,384 columns in one group
 
 Shape grad_shape(uint32_t cols) { return shape_of(cols, cols <= 256 ? 1 : cols <= 8192 ? 2 : 4); }
 
 Few few_of(uint32_t rows, uint32_t cols) {
   const Shape s = grad_shape(cols);
-  if (!rows || !s.fits || (uint64_t)rows * cols > 1u << 19) return {0, 0};
+  if (!rows || !s.fits || (uint64_t)rows * cols > 1u << 18) return {0, 0};
   Few f = {1, 1};
   while (f.ctas < 16 && f.ctas < rows) f.ctas *= 2;
   const uint32_t most = s.threads >= 512 ? 1 : 512 / s.threads, want = (rows + 15) / 16;
@@ -399,8 +409,7 @@ namespace {
 template <typename K>
 int grad_few(K kernel, const GradArgs &a, const Shape &s, const Few &few, cudaStream_t stream) {
   const uint32_t bytes = (2 * few.groups * (s.threads / 32) + few.groups * a.cols) * sizeof(float);
-  constexpr int kMost = 72 * 1024;  // of any such launch: 16,384 columns in one group
-  int e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+  int e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSumsBytes);
   if (!e && few.ctas > 8) e = (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e) return e;
   cudaLaunchAttribute attr = {};
@@ -471,17 +480,19 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
                   : f(grad_kernel<T, 4, 1, false, false>, grad_kernel<T, 4, 1, false, true>);
     };
     if (few.ctas) return with_shape([&](auto, auto kernel) { return grad_few(kernel, a, sh, few, s); });
-    const uint32_t room = (2 * sh.groups * (sh.threads / 32) + (sh.groups > 1 ? sh.groups * n.cols : 0)) * sizeof(float);
     return with_shape([&](auto kernel, auto) {
+      const uint32_t room = (2 * sh.groups * (sh.threads / 32) + (a.partial ? sh.groups * n.cols : 0)) * sizeof(float);
+      const int e = room <= 48 * 1024 ? 0 : (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSumsBytes);
+      if (e) return e;
       kernel<<<grid_of(a.parts, 2), dim3(sh.threads, sh.groups), room, s>>>(a);
       return (int)cudaGetLastError();
     });
   });
   if (e || !n.dweight || few.ctas) return e;
-  const unsigned grid = grid_of((n.cols + 31) / 32, 4);
+  const unsigned grid = grid_of((n.cols + 31) / 32, 2);
   const float *work = n.work;
-  if (n.rows) return launch_after(parts_kernel, grid, 512, 0, s, work, a.parts, n.cols, n.dweight, n.dwdtype);
-  parts_kernel<<<grid, 512, 0, s>>>(work, a.parts, n.cols, n.dweight, n.dwdtype);
+  if (n.rows) return launch_after(parts_kernel, grid, 1024, 0, s, work, a.parts, n.cols, n.dweight, n.dwdtype);
+  parts_kernel<<<grid, 1024, 0, s>>>(work, a.parts, n.cols, n.dweight, n.dwdtype);
   return (int)cudaGetLastError();
 }
 

@@ -156,8 +156,8 @@ def test_empty_calls_need_no_device():
 
 def test_grad_workspace():
     f = apc.library().apc_rms_norm_grad_workspace
-    assert f(0, 4096) == f(4, 4096) == f(128, 4096) == f(-1, 5) == f(5, 1 << 31) == 0
-    assert f(129, 4096) == 129 * 4096 * 4 and f(8192, 4096) == 304 * 4096 * 4
+    assert f(0, 4096) == f(4, 4096) == f(64, 4096) == f(-1, 5) == f(5, 1 << 31) == 0
+    assert f(65, 4096) == 65 * 4096 * 4 and f(8192, 4096) == 304 * 4096 * 4
     assert f(9000, 256) == 8 * 304 * 256 * 4
 
 
