@@ -160,16 +160,18 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
       }
     }
     if (!CLUSTER && !a.partial) continue;
-    // by way of shared memory, a warp's stores to the workspace being neighbours: 4-byte stores 32
-    // bytes apart took 5 us more for 304 parts of 4,096 columns
+    // wide units go by way of shared memory, a warp's stores to the workspace being neighbours: 4-byte
+    // stores 32 bytes apart took 5 us more for 304 parts of 4,096 columns; but long rows' weights need L1
+    const bool alone = !CLUSTER && (!WIDE || kAgain) && blockDim.y == 1;
+    float *const sums = alone ? a.partial + (uint64_t)part * a.cols : part_sums + threadIdx.y * a.cols;
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float2 f = unpack2(acc[v][i / 2]);
-        if (i < n[v]) part_sums[threadIdx.y * a.cols + c[v] + (WIDE ? i : 32 * i)] = i % 2 ? f.y : f.x;
+        if (i < n[v]) sums[c[v] + (WIDE ? i : 32 * i)] = i % 2 ? f.y : f.x;
       }
-    if (CLUSTER) continue;
+    if (CLUSTER || alone) continue;
     __syncthreads();
     for (uint32_t k = threadIdx.y * blockDim.x + threadIdx.x; k < a.cols; k += blockDim.x * blockDim.y) {
       float s = 0.0f;
@@ -253,8 +255,10 @@ __global__ void __launch_bounds__(256) grad_long_parts_kernel(const __grid_const
 }
 
 // dweight: the parts' sums, 32 columns a CTA, warp k those of parts k, k + 32, ..., ten loads of a
-// lane under way, then the warps'.
-__global__ void __launch_bounds__(1024) parts_kernel(const float *partial, uint32_t parts, uint32_t cols, void *dweight, uint32_t dtype) {
+// lane under way, then the warps'.  Two CTAs on an SM pay once there are more than SMs: 300 x 4096
+// took 8.5 us with both in place of 7.7, 1221 x 16384 69.9 in place of 73.3.
+template <int PER_SM>
+__global__ void __launch_bounds__(1024, PER_SM) parts_kernel(const float *partial, uint32_t parts, uint32_t cols, void *dweight, uint32_t dtype) {
   __shared__ float sums[32][33];
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const uint32_t runs = (cols + 31) / 32;
@@ -481,7 +485,7 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
     };
     if (few.ctas) return with_shape([&](auto, auto kernel) { return grad_few(kernel, a, sh, few, s); });
     return with_shape([&](auto kernel, auto) {
-      const uint32_t room = (2 * sh.groups * (sh.threads / 32) + (a.partial ? sh.groups * n.cols : 0)) * sizeof(float);
+      const uint32_t room = (2 * sh.groups * (sh.threads / 32) + (a.partial && (sh.groups > 1 || (wide && sh.v < 4)) ? sh.groups * n.cols : 0)) * sizeof(float);
       const int e = room <= 48 * 1024 ? 0 : (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSumsBytes);
       if (e) return e;
       kernel<<<grid_of(a.parts, 2), dim3(sh.threads, sh.groups), room, s>>>(a);
@@ -489,10 +493,12 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
     });
   });
   if (e || !n.dweight || few.ctas) return e;
-  const unsigned grid = grid_of((n.cols + 31) / 32, 2);
+  const uint32_t runs = (n.cols + 31) / 32;
+  const auto kernel = runs <= sms ? parts_kernel<1> : parts_kernel<2>;
+  const unsigned grid = grid_of(runs, 2);
   const float *work = n.work;
-  if (n.rows) return launch_after(parts_kernel, grid, 1024, 0, s, work, a.parts, n.cols, n.dweight, n.dwdtype);
-  parts_kernel<<<grid, 1024, 0, s>>>(work, a.parts, n.cols, n.dweight, n.dwdtype);
+  if (n.rows) return launch_after(kernel, grid, 1024, 0, s, work, a.parts, n.cols, n.dweight, n.dwdtype);
+  kernel<<<grid, 1024, 0, s>>>(work, a.parts, n.cols, n.dweight, n.dwdtype);
   return (int)cudaGetLastError();
 }
 
