@@ -396,7 +396,8 @@ RingShape ring_shape(const void *x, int64_t pitch, uint32_t rows, uint32_t cols,
   s.whole = begins && cols % 8 == 0;
   if (size != 2 || (s.whole && !pays) || !alike || rows <= least || cols <= 512 || units > 2048) return s;
   // units a thread: with more than registers have room for, or barriers to wait for, fewer threads do more
-  s.v = grad ? units <= 1024 ? 1 : 4 : units <= 512 && mats == 2 ? 1 : 2;
+  s.v = grad ? units <= 1024 ? 1 : 2 : units <= 512 && mats == 2 ? 1 : 2;
+  if (grad && s.v == 2) mats = 2;
   s.threads = 32 * ((units + 32 * s.v - 1) / (32 * s.v));
   s.ring.region = (cols * size + 15 + 15) / 16 * 16 + 16;
   s.ring.mats = mats;

@@ -283,22 +283,45 @@ __global__ void __launch_bounds__(1024, PER_SM) parts_kernel(const float *partia
   }
 }
 
+// A unit's elements from global memory.
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void unit_load(uint32_t (&w)[8 / Word<T>::kPer], const T *row, const Unit<WHOLE> &u, uint32_t cols) {
+  static_assert(sizeof(T) == 2, "");
+  if (u.full) {
+    const uint4 v = *reinterpret_cast<const uint4 *>(row + u.first);
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = 0;
+  if (WHOLE || !u.any) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int32_t c = u.first + i;
+    if (c >= 0 && c < (int32_t)cols) w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[c] << (i % 2 * 16);
+  }
+}
+
 // The gradient's rows through a ring of x, dout and dresidual.  Part p is rows p, p + parts,
-// ...: rows of a part begin alike.
+// ...: rows of a part begin alike.  Rows of more than 1,024 units, two a thread (V): two stages of x
+// and dout are what fits, dresidual comes into registers, and z and g are formed twice.
 template <typename T, int V, bool WHOLE>
-__global__ void __launch_bounds__(V == 1 ? 1024 : 512, 1) ring_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ Ring ring) {
+__global__ void __launch_bounds__(1024, 1) ring_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ Ring ring) {
   constexpr int kWords = 8 / Word<T>::kPer;
+  constexpr bool kAgain = V > 1;
   extern __shared__ __align__(128) uint8_t s_ring[];
   __shared__ RingShared sh;
   const Group g{blockDim.x / 32, 0, threadIdx.x / 32, threadIdx.x % 32};
   const uint32_t units = V * blockDim.x;
   float *const laid = reinterpret_cast<float *>(s_ring + ring.stages * ring.stage());
   if (a.partial) start_next();
-  const Source src[3] = {{a.x, a.pitch}, {a.dout, a.dout_pitch}, {a.dresidual, a.dresidual_pitch}};
+  constexpr int kMats = kAgain ? 2 : 3;
+  Source src[kMats] = {{a.x, a.pitch}, {a.dout, a.dout_pitch}};
+  if constexpr (!kAgain) src[2] = {a.dresidual, a.dresidual_pitch};
   uint32_t next_part = blockIdx.x, next = next_part, into = 0;
   const auto issue = [&]() {
     if (next_part < a.parts) {
-      ring_issue<3>(sh, src, ring, s_ring + into * ring.stage(), &sh.full[into], next, a.rows, a.cols, sizeof(T), l2_evict_first());
+      ring_issue<kMats>(sh, src, ring, s_ring + into * ring.stage(), &sh.full[into], next, a.rows, a.cols, sizeof(T), l2_evict_first());
       next += a.parts;
       if (next >= a.rows) next = next_part += gridDim.x;
     }
@@ -320,10 +343,9 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512, 1) ring_grad_kernel(const
       const float rstd = __ldg(a.rstd + row);
       uint8_t *const at = s_ring + stage * ring.stage();
       ring_wait(sh, stage, parity, ring.status);
-      if (!WHOLE && ring.edges) ring_edges<T, 3>(src, ring, at, row, a.rows, a.cols);
-      uint64_t z[V][4], gg[V][4], dot = 0;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
+      if (!WHOLE && ring.edges) ring_edges<T, kMats>(src, ring, at, row, a.rows, a.cols);
+      uint64_t z[kAgain ? 1 : V][4], gg[kAgain ? 1 : V][4], dot = 0;
+      const auto form = [&](int v, auto each) {
         const uint32_t k = threadIdx.x + v * blockDim.x;
         const Unit<WHOLE> u(k, skip / sizeof(T), a.cols);
         uint32_t x[kWords], d[kWords];
@@ -334,11 +356,22 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512, 1) ring_grad_kernel(const
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint64_t dd;
-          z_and_g<T>(x, d, rstd, wt, i, &z[v][i], &gg[v][i], &dd);
-          dot = fma2(gg[v][i], z[v][i], dot);
-          acc[v][i] = fma2(dd, z[v][i], acc[v][i]);
+          z_and_g<T>(x, d, rstd, wt, i, &z[kAgain ? 0 : v][i], &gg[kAgain ? 0 : v][i], &dd);
+          each(i, dd);
         }
-      }
+      };
+      uint32_t res[kAgain ? V : 1][kWords];
+      if (kAgain && a.dresidual)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          unit_load<T, WHOLE>(res[kAgain ? v : 0], static_cast<const T *>(a.dresidual) + (int64_t)row * a.dresidual_pitch,
+                              Unit<WHOLE>(threadIdx.x + v * blockDim.x, skip / sizeof(T), a.cols), a.cols);
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        form(v, [&](int i, uint64_t dd) {
+          dot = fma2(gg[kAgain ? 0 : v][i], z[kAgain ? 0 : v][i], dot);
+          acc[v][i] = fma2(dd, z[kAgain ? 0 : v][i], acc[v][i]);
+        });
       const float2 both = unpack2(dot);
       const float mean = group_sum(both.x + both.y, g, sh.sums[turn ^= 1]) * a.inv_cols;
       if (threadIdx.x == 0) issue();  // into the stage of the row before, which all have left
@@ -346,12 +379,15 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512, 1) ring_grad_kernel(const
       for (int v = 0; v < V; ++v) {
         const uint32_t k = threadIdx.x + v * blockDim.x;
         const Unit<WHOLE> u(k, skip / sizeof(T), a.cols);
+        if (kAgain) form(v, [](int, uint64_t) {});
         uint32_t o[kWords];
-        if (a.dresidual) ring_load<T, WHOLE>(o, at + 2 * ring.region, k, u, a.cols);
+        uint32_t(&r)[kWords] = kAgain ? res[kAgain ? v : 0] : o;
+        if (!kAgain && a.dresidual) ring_load<T, WHOLE>(o, at + 2 * ring.region, k, u, a.cols);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float2 f = unpack2(mul2(fma2(z[v][i], pack2(-mean, -mean), gg[v][i]), pack2(rstd, rstd)));
-          if (a.dresidual) f.x += element<T>(o, 2 * i), f.y += element<T>(o, 2 * i + 1);
+          const uint64_t(&zv)[4] = z[kAgain ? 0 : v], (&gv)[4] = gg[kAgain ? 0 : v];
+          float2 f = unpack2(mul2(fma2(zv[i], pack2(-mean, -mean), gv[i]), pack2(rstd, rstd)));
+          if (a.dresidual) f.x += element<T>(r, 2 * i), f.y += element<T>(r, 2 * i + 1);
           round_pair<T>(o, i, f.x, f.y);
         }
         ring_store<T, WHOLE>(static_cast<T *>(a.dx) + (int64_t)row * a.dx_pitch, o, u, a.cols);
@@ -384,10 +420,11 @@ struct Few {
   uint32_t ctas, groups;
 };
 
-constexpr uint32_t kGradParts = 304;
 constexpr int kSumsBytes = 72 * 1024;  // shared memory of any launch of grad_kernel: 16,384 columns in one group
 
 Shape grad_shape(uint32_t cols) { return shape_of(cols, cols <= 256 ? 1 : cols <= 8192 ? 2 : 4); }
+
+uint32_t grad_ctas(uint32_t cols) { return cols <= 4096 ? 304 : 152; }
 
 Few few_of(uint32_t rows, uint32_t cols) {
   const Shape s = grad_shape(cols);
@@ -401,10 +438,11 @@ Few few_of(uint32_t rows, uint32_t cols) {
 
 }  // namespace
 
-// Parts: two CTAs for every SM, or as many groups (the ring's CTAs are one); none where a cluster does it.
+// Parts: two CTAs for every SM, above 4,096 columns one, which is what an SM then holds, or as
+// many groups (the ring's CTAs are one); none where a cluster does it.
 uint32_t rms_norm_parts(uint32_t rows, uint32_t cols) {
   if (few_of(rows, cols).ctas) return 0;
-  const uint32_t parts = kGradParts * grad_shape(cols).groups;
+  const uint32_t parts = grad_ctas(cols) * grad_shape(cols).groups;
   return rows < parts ? rows : parts;
 }
 
@@ -438,7 +476,7 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
   a.dout_pitch = n.dout_pitch, a.pitch = n.pitch, a.dresidual_pitch = n.dresidual_pitch, a.dx_pitch = n.dx_pitch;
   a.rows = n.rows, a.cols = n.cols, a.wdtype = n.wdtype;
   const Few few = n.dweight ? few_of(n.rows, n.cols) : Few{0, 0};
-  a.parts = few.ctas ? few.ctas : n.rows < kGradParts ? n.rows : kGradParts;
+  a.parts = few.ctas ? few.ctas : n.rows < grad_ctas(n.cols) ? n.rows : grad_ctas(n.cols);
   if (few.ctas) a.partial = nullptr, a.dweight = n.dweight, a.dwdtype = n.dwdtype;
   a.weight_aligned = (uintptr_t)n.weight % 16 == 0;
   a.inv_cols = (float)(1.0 / n.cols);
@@ -462,15 +500,15 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
     };
     const RingShape ring = ring_shape(n.x, n.pitch, n.rows, n.cols, sizeof(T), n.dresidual ? 3 : 2, 2 * sms, true,
                                       alike(n.dout, n.dout_pitch) && alike(n.dresidual, n.dresidual_pitch) && alike(n.dx, n.dx_pitch),
-                                      n.cols >= 2048 && n.cols <= 8192);
+                                      n.cols >= 2048);
     if constexpr (sizeof(T) == 2) if (ring.threads && !few.ctas) {
       a.parts = n.dweight ? rms_norm_parts(n.rows, n.cols) : n.rows;
       const uint32_t period = period_of(n.pitch * (int64_t)sizeof(T));
       if (ring.whole)
         return ring.v == 1 ? ring_launch(ring_grad_kernel<T, 1, true>, a, ring, a.parts, period, stream)
-                           : ring_launch(ring_grad_kernel<T, 4, true>, a, ring, a.parts, period, stream);
+                           : ring_launch(ring_grad_kernel<T, 2, true>, a, ring, a.parts, period, stream);
       return ring.v == 1 ? ring_launch(ring_grad_kernel<T, 1, false>, a, ring, a.parts, period, stream)
-                         : ring_launch(ring_grad_kernel<T, 4, false>, a, ring, a.parts, period, stream);
+                         : ring_launch(ring_grad_kernel<T, 2, false>, a, ring, a.parts, period, stream);
     }
     const bool wide = at(n.x, n.pitch) && at(n.dout, n.dout_pitch) && at(n.dresidual, n.dresidual_pitch) && at(n.dx, n.dx_pitch);
     const auto with_shape = [&](auto f) {
