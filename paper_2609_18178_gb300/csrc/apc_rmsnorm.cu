@@ -43,6 +43,32 @@ __device__ __forceinline__ uint64_t sub2(uint64_t a, uint64_t b) {
   return r;
 }
 
+// a + b rounded; err: what that lost.
+__device__ __forceinline__ float two_sum(float a, float b, float *err) {
+  const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+  *err = __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t));
+  return s;
+}
+
+// A thread's sum over the many parts of a long row.  The second float of a pair that is only
+// added to grows with every addition: where the values are alike it passed what warp_stat's
+// integers hold, from 600,000 columns on.  So it goes back into the first after each addition,
+// and what the second one's additions lose is kept too: a sum of 2^17 parts (2^31 columns) is
+// then off by 2^-39 of itself at most, and by 2^-46 of 2^10 parts of one value.
+struct LongSum {
+  float hi = 0.0f, lo = 0.0f, rest = 0.0f;
+
+  __device__ __forceinline__ void add(Two b) {
+    float e[3];
+    const float s = two_sum(hi, b.hi, &e[0]);
+    const float l = two_sum(two_sum(lo, e[0], &e[1]), b.lo, &e[2]);
+    rest = __fadd_rn(rest, __fadd_rn(e[1], e[2]));
+    hi = __fadd_rn(s, l);
+    lo = __fsub_rn(l, __fsub_rn(hi, s));
+  }
+  __device__ __forceinline__ Two sum() const { return {hi, __fadd_rn(lo, rest)}; }
+};
+
 // The sum of two pairs, lane by lane; err: what it lost.
 __device__ __forceinline__ uint64_t two_sum2(uint64_t a, uint64_t b, uint64_t *err) {
   const uint64_t s = add2(a, b), t = sub2(s, a);
@@ -312,13 +338,19 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
       }
     };
     if (!LONG) fetch(g.warp, false);
-    Two p = {0.0f, 0.0f};
-    float rstd;
-    over_row(false, [&](uint32_t) {
+    // the sum of squares over the row
+    const auto sum_of = [&](bool again, auto square) {
+      LongSum all;
+      Two p;
+      over_row(again, [&](uint32_t) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) p = v || LONG ? p + squares<T>(w[v]) : squares<T>(w[v]);
-    });
-    if (!row_rstd(p, g, room, a.c, true, &rstd)) {
+        for (int v = 0; v < V; ++v) p = v ? p + square(w[v]) : square(w[v]);
+        if (LONG) all.add(p);
+      });
+      return LONG ? all.sum() : p;
+    };
+    float rstd;
+    if (!row_rstd(sum_of(false, [](const auto &x) { return squares<T>(x); }), g, room, a.c, true, &rstd)) {
       uint32_t m = 0;
       over_row(true, [&](uint32_t) {
 #pragma unroll
@@ -329,12 +361,7 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
         rstd = m > 0x7f800000u ? __uint_as_float(0x7fffffffu) : 0.0f;
       } else {  // squares beyond the largest number: eps is nothing beside them
         const float scale = __uint_as_float(max(254u - (m >> 23), 1u) << 23);
-        p = {0.0f, 0.0f};
-        over_row(true, [&](uint32_t) {
-#pragma unroll
-          for (int v = 0; v < V; ++v) p = p + squares<T, true>(w[v], scale);
-        });
-        row_rstd(p, g, room, a.c, false, &rstd);
+        row_rstd(sum_of(true, [&](const auto &x) { return squares<T, true>(x, scale); }), g, room, a.c, false, &rstd);
         rstd *= scale;
         g.sync();
       }

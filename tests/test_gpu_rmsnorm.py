@@ -141,6 +141,20 @@ def test_sum_in_place(place):
             assert torch.equal(p, q)
 
 
+@pytest.mark.parametrize("c", [1 << 19, 655_360, (1 << 20) + 3, 1 << 22])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_long_rows_of_one_value(dtype, c):
+    """What the additions of equal squares lose has one sign, and adds up over a row; huge values are summed scaled."""
+    values = (torch.rand(24, generator=gen(c), device="cuda") * 1.5 + 0.5).to(dtype)
+    if dtype != torch.float16:
+        values[20:] *= 1e25
+    x = values[:, None].expand(24, c).contiguous()
+    rstd = apc.rms_norm(x, torch.ones(c, device="cuda", dtype=dtype))[2]
+    # the mean of equal squares is the square: bounds as above
+    want = 1 / (values.double().square() + 1e-6).sqrt()
+    assert ((rstd.double() - want).abs() <= (1 + 2.0 ** -8) * U * want).all()
+
+
 @pytest.mark.parametrize("r", [6, 400])
 @pytest.mark.parametrize("c", [100, 1000, 4096, 5003, 20_000])
 def test_rows_of_huge_values(r, c):
