@@ -99,24 +99,36 @@ __device__ __forceinline__ uint2 to_fp8x8(const uint64_t (&v)[4], uint64_t inv) 
   return {__byte_perm(h[0], h[1], 0x5410), __byte_perm(h[2], h[3], 0x5410)};
 }
 
+// How memory is read.  The read-only path is for what nothing writes while the kernel runs;
+// a matrix that an output may replace is read plainly; and what a kernel that is still running
+// when this one starts has written, from L2, behind the wait for that kernel.
+enum class Read { kOnly, kPlain, kL2 };
+
+template <Read HOW, typename U>
+__device__ __forceinline__ U read(const U *p) {
+  if (HOW == Read::kOnly) return __ldg(p);
+  if (HOW == Read::kL2) return __ldcg(p);
+  return *p;
+}
+
 // 8 elements from x, of which the first n exist, as words; `wide`: x is 16-byte aligned.
-template <typename T>
+template <typename T, Read HOW = Read::kOnly>
 __device__ __forceinline__ void load8(uint32_t *w, const T *x, int n, bool wide) {
   constexpr int kWords = 8 / Word<T>::kPer;
   if (wide && n >= 8) {
 #pragma unroll
     for (int i = 0; i < kWords; i += 4) {
-      const uint4 v = __ldg(reinterpret_cast<const uint4 *>(x) + i / 4);
+      const uint4 v = read<HOW>(reinterpret_cast<const uint4 *>(x) + i / 4);
       w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
     }
   } else {
 #pragma unroll
     for (int i = 0; i < kWords; ++i) {
       if (sizeof(T) == 4) {
-        w[i] = i < n ? __ldg(reinterpret_cast<const uint32_t *>(x) + i) : 0;
+        w[i] = i < n ? read<HOW>(reinterpret_cast<const uint32_t *>(x) + i) : 0;
       } else {
-        const uint32_t lo = 2 * i < n ? __ldg(reinterpret_cast<const uint16_t *>(x) + 2 * i) : 0;
-        const uint32_t hi = 2 * i + 1 < n ? __ldg(reinterpret_cast<const uint16_t *>(x) + 2 * i + 1) : 0;
+        const uint32_t lo = 2 * i < n ? read<HOW>(reinterpret_cast<const uint16_t *>(x) + 2 * i) : 0;
+        const uint32_t hi = 2 * i + 1 < n ? read<HOW>(reinterpret_cast<const uint16_t *>(x) + 2 * i + 1) : 0;
         w[i] = hi << 16 | lo;
       }
     }

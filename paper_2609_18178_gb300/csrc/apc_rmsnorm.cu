@@ -299,33 +299,33 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
     T *sum = static_cast<T *>(a.sum) + (int64_t)row * a.sum_pitch;
     Stat *room = s_room + ((turn ^= 1) * blockDim.y + threadIdx.y) * (g.warps + 1);
     uint32_t w[V][kWords];
-    // the sum's elements of V runs from `run` on, as they are stored
+    // the sum's elements of V runs from `run` on, as they are stored.  All loads stand in front
+    // of the stores, which they might not pass (1200 x 16384 bf16 32.4 us, 36.9 in turns), but for
+    // aligned fp32 rows to fp32, which do as well or better with fewer under way: 8192 x 4096 82.3 us
+    // (92.7), though 2441 x 8192 56.5 (52.7).
+    constexpr bool kTurns = sizeof(T) == 4 && OUT == kSame && WIDE && !LONG;
     const auto fetch = [&](uint32_t run, bool again) {
+      const bool adds = !again && a.residual;
+      uint32_t c[V], o[V][kWords];
+      int n[V];
+      const auto add = [&](int v) {
+        add_rounded<T>(w[v], o[v]);
+        store<T, WIDE>(sum + c[v], w[v], n[v]);
+      };
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const uint32_t c = first_of<WIDE>(run + v * g.warps, g.lane);
-        const int n = count_of<WIDE>(c, a.cols);
-        if (again && a.residual) {
-          load<T, WIDE>(w[v], const_cast<const T *>(sum) + c, 0);
-          if (n) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              if (i >= n) continue;
-              const uint32_t at = c + (WIDE ? i : 32 * i);
-              if (sizeof(T) == 4) w[v][i] = reinterpret_cast<volatile uint32_t *>(sum)[at];
-              else w[v][i / 2] |= (uint32_t)reinterpret_cast<volatile uint16_t *>(sum)[at] << (i % 2 * 16);
-            }
-          }
-          continue;
-        }
-        load<T, WIDE>(w[v], x + c, n);
-        if (a.residual) {
-          uint32_t o[kWords];
-          load<T, WIDE>(o, res + c, n);
-          add_rounded<T>(w[v], o);
-          store<T, WIDE>(sum + c, w[v], n);
-        }
+        c[v] = first_of<WIDE>(run + v * g.warps, g.lane);
+        n[v] = count_of<WIDE>(c[v], a.cols);
+        load<T, WIDE>(w[v], (again && a.residual ? sum : x) + c[v], n[v]);
+        if (!kTurns || !adds) continue;
+        load<T, WIDE>(o[v], res + c[v], n[v]);
+        add(v);
       }
+      if (kTurns || !adds) return;
+#pragma unroll
+      for (int v = 0; v < V; ++v) load<T, WIDE>(o[v], res + c[v], n[v]);
+#pragma unroll
+      for (int v = 0; v < V; ++v) add(v);
     };
     const auto over_row = [&](bool again, auto f) {  // f() for each part that the registers hold
       if constexpr (LONG) {
@@ -484,7 +484,8 @@ __global__ void __launch_bounds__(256) narrow_kernel(const __grid_constant__ For
   }
 }
 
-// The transpose in 8 bits, from the sum and rstd that the forward kernel left.  A CTA walks
+// The transpose in 8 bits, from the sum and rstd that the forward kernel left: that one may still
+// run when this one starts, so they are read from L2 (cp.async.cg, ld.cg), behind the wait.  A CTA walks
 // tiles of 128 x 128, the last rows first: those are what the forward kernel left in L2.  The
 // next tile comes into shared memory while the one before is stored; four CTAs on an SM
 // cover for each other otherwise.  Thread (tx, ty) takes rows 8 ty + 0..7 of columns 8 tx +
@@ -549,14 +550,14 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) turn_kernel(const
 #pragma unroll 4
       for (int i = 0; i < 8; ++i, h += 16 * a.pitch, to += 16 * kPitch) {
         uint32_t w[kWords];
-        load8<T>(w, h, r + 16 * i < a.rows ? n : 0, false);
+        load8<T, Read::kL2>(w, h, r + 16 * i < a.rows ? n : 0, false);
 #pragma unroll
         for (int j = 0; j < kWords; j += 4) *reinterpret_cast<uint4 *>(to + 4 * j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
       }
     }
     if (threadIdx.x < 128) {
       const uint32_t k = tr * kBlock + threadIdx.x;
-      sh.rstd[threadIdx.x] = k < a.rows ? __ldg(a.rstd + k) : 0.0f;
+      sh.rstd[threadIdx.x] = k < a.rows ? __ldcg(a.rstd + k) : 0.0f;
     }
   };
   uint32_t tr = 0, tc = 0;

@@ -45,10 +45,11 @@ __device__ __forceinline__ int count_of(uint32_t first, uint32_t cols) {
   return (int)min(8u, WIDE ? cols - first : (cols - first + 31) / 32);
 }
 
+// Plain loads: outputs may take the place of what is read.
 template <typename T, bool WIDE>
 __device__ __forceinline__ void load(uint32_t (&w)[8 / Word<T>::kPer], const T *x, int n) {
   if (WIDE) {
-    load8<T>(w, x, n, true);
+    load8<T, Read::kPlain>(w, x, n, true);
   } else if (sizeof(T) == 4) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = i < n ? reinterpret_cast<const uint32_t *>(x)[32 * i] : 0;

@@ -86,6 +86,7 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
   uint32_t c[V];
   int n[V];
   constexpr bool kAgain = V == 4;  // registers are short: weights come from L1 for each row, dresidual after the sum
+  constexpr int kRes = kAgain ? 2 : V;
   uint64_t wt[kAgain ? 1 : V][4];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
@@ -98,7 +99,7 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
     uint64_t acc[V][4] = {};
     for (uint64_t first = part * blockDim.y + threadIdx.y; first < a.rows; first += (uint64_t)step * U) {
       float *room = s_sums + (turn ^= 1) * blockDim.y * g.warps + threadIdx.y * g.warps;
-      uint32_t x[U][V][kWords], d[U][V][kWords], r[U][kAgain ? 1 : V][kWords];
+      uint32_t x[U][V][kWords], d[U][V][kWords], r[U][kRes][kWords];
       float rstd[U], dot[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -139,14 +140,17 @@ __global__ void __launch_bounds__(512, 1) grad_kernel(const __grid_constant__ Gr
         const uint64_t row = first + (uint64_t)u * step;
         if (u && row >= a.rows) break;
         const float mean = dot[u] * a.inv_cols;
+        const auto late = [&](int v) {  // one ahead of the stores, which it might not pass
+          if (kAgain && a.dresidual)
+            load<T, WIDE>(r[u][v % kRes], static_cast<const T *>(a.dresidual) + (int64_t)row * a.dresidual_pitch + c[v], n[v]);
+        };
+        late(0);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          uint32_t o[kWords], (&res)[kWords] = r[u][kAgain ? 0 : v];
+          uint32_t o[kWords], (&res)[kWords] = r[u][v % kRes];
           uint64_t(&w)[4] = wt[kAgain ? 0 : v];
-          if (kAgain) {
-            weights<WIDE>(w, a.weight, a.wdtype, a.weight_aligned, c[v], n[v]);
-            if (a.dresidual) load<T, WIDE>(res, static_cast<const T *>(a.dresidual) + (int64_t)row * a.dresidual_pitch + c[v], n[v]);
-          }
+          if (kAgain) weights<WIDE>(w, a.weight, a.wdtype, a.weight_aligned, c[v], n[v]);
+          if (v + 1 < V) late(v + 1);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint64_t z, gg, dd;

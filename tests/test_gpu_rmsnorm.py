@@ -141,6 +141,28 @@ def test_sum_in_place(place):
             assert torch.equal(p, q)
 
 
+@pytest.mark.parametrize("place", ["x", "residual"])
+@pytest.mark.parametrize("r,c", [(9, 1003), (200, 1003), (300, 131), (1500, 203), (2000, 1200), (2100, 1003), (40, 20_003), (110, 20_003)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sum_in_place_and_transposed(place, r, c, dtype):
+    """The transpose is made of sums that a kernel still running stored where its input was, in sectors that rows share;
+    below 2^21 elements the second kernel waits beside the first, above it starts as that one ends."""
+    for extra, offset in ((0, 0), (1, 3), (8, 1)):
+        x, res, w = inputs(r, c, dtype, dtype, 7)
+        want = apc.rms_norm_fp8(x, w, residual=res, transposed=True)
+        check_rstd(want[4], 1e-6, want[5])
+        a, b = strided(x, extra, offset), strided(res, extra, offset)
+        for _ in range(3):
+            a.copy_(x), b.copy_(res)
+            *got, rstd = apc.rms_norm_fp8(a, w, residual=b, sum=a if place == "x" else b, transposed=True)
+            assert torch.equal(got[4], want[4])
+            # rstd's bits may follow the layout, in a row near a border
+            check_rstd(want[4], 1e-6, rstd)
+            ref = apc.quantize_fp8(y_of(want[4], rstd, w), transposed=True)
+            for p, q in zip(got, ref):
+                assert torch.equal(p.float(), q.float())
+
+
 @pytest.mark.parametrize("c", [1 << 19, 655_360, (1 << 20) + 3, 1 << 22])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_long_rows_of_one_value(dtype, c):
