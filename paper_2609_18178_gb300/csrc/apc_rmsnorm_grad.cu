@@ -481,7 +481,9 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
   a.partial = n.dweight ? n.work : nullptr;
   a.dout_pitch = n.dout_pitch, a.pitch = n.pitch, a.dresidual_pitch = n.dresidual_pitch, a.dx_pitch = n.dx_pitch;
   a.rows = n.rows, a.cols = n.cols, a.wdtype = n.wdtype;
-  const Few few = n.dweight ? few_of(n.rows, n.cols) : Few{0, 0};
+  // dx's bits are the same with dweight and without: few rows take the plain kernel either way
+  // (400 x 601 bf16 without dweight 2.9 us, through the ring 4.5)
+  const Few rows = few_of(n.rows, n.cols), few = n.dweight ? rows : Few{0, 0};
   a.parts = few.ctas ? few.ctas : n.rows < grad_ctas(n.cols) ? n.rows : grad_ctas(n.cols);
   if (few.ctas) a.partial = nullptr, a.dweight = n.dweight, a.dwdtype = n.dwdtype;
   a.weight_aligned = (uintptr_t)n.weight % 16 == 0;
@@ -507,7 +509,7 @@ int launch_rms_norm_grad(const NormGradArgs &n, unsigned sms, void *stream) {
     const RingShape ring = ring_shape(n.x, n.pitch, n.rows, n.cols, sizeof(T), n.dresidual ? 3 : 2, 2 * sms, true,
                                       alike(n.dout, n.dout_pitch) && alike(n.dresidual, n.dresidual_pitch) && alike(n.dx, n.dx_pitch),
                                       n.cols >= 2048);
-    if constexpr (sizeof(T) == 2) if (ring.threads && !few.ctas) {
+    if constexpr (sizeof(T) == 2) if (ring.threads && !rows.ctas) {
       a.parts = n.dweight ? rms_norm_parts(n.rows, n.cols) : n.rows;
       const uint32_t period = period_of(n.pitch * (int64_t)sizeof(T));
       if (ring.whole)

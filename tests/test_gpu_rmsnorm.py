@@ -297,6 +297,23 @@ def test_grad_in_place_and_types(r, c):
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1].half())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_dx_does_not_depend_on_dweight(dtype):
+    """A frozen weight leaves dx's bits as they are, in the ring, by plain loads and where a cluster makes both."""
+    for r, c in ((3, 40), (60, 500), (400, 601), (310, 840), (330, 784), (350, 601), (500, 513), (400, 2048), (700, 1003), (20, 12_000), (310, 9001),
+                 (4, 17_000), (9000, 90)):
+        x, d, w = inputs(r, c, dtype, dtype, 11)
+        dres = torch.randn(r, c, generator=gen(6), device="cuda").to(dtype)
+        rstd = apc.rms_norm(x, w)[2]
+        for extra, offset in ((0, 0), (8, 5)):
+            given = strided(d, extra, offset), strided(x, extra, offset), w, rstd
+            for k in (dict(), dict(dresidual=strided(dres, extra, offset))):
+                out = [strided(torch.zeros_like(x), extra, offset) for _ in range(2)]
+                apc.rms_norm_grad(*given, out=out[0], **k)
+                apc.rms_norm_grad(*given, out=out[1], weight_grad=False, **k)
+                assert torch.equal(*out)
+
+
 def test_grad_against_differences():
     """The formula is the derivative of the forward definition, in 64 bits; the kernel follows the formula."""
     x, d, w = inputs(4, 96, torch.float32, torch.float32)
