@@ -266,7 +266,7 @@ apc_status apc_commit_step_bf16_clipped(const apc_tensor_bf16 *table, int32_t nu
  * loss with its gradient, and the norm's gradient.  Every sum has a fixed order that follows the call's arguments and the
  * number of the GPU's SMs, not the grid or the order of atomics, so replicas that run
  * the same step on the same kind of GPU commit identical bits and their digests agree.
- * Some arguments' addresses count: sums over a row of logits, and those of the norm's
+ * Some arguments' addresses count: sums over a row of logits, and those of the norm and its
  * gradient, follow the rows' place within 16 bytes, so equal bits need rows that are aligned
  * alike.
  *
@@ -332,7 +332,10 @@ apc_status apc_matmul_fp8(const apc_fp8_matrix *a, const apc_fp8_matrix *b, int6
  * stands in front of the head, whose operand it can write.
  *   h    = x + residual, rounded to x's type and kept in sum; x without a residual
  *   rstd = 1 / sqrt(mean of h^2 + eps), fp32: of the stored h, rounded once from a sum
- *          that is exact to 2^-40 of itself, so that its bits do not follow the rows' layout
+ *          that is within 2^-38 of itself.  Calls with other numbers of rows, pitches or
+ *          addresses sum in other orders: they give the same bits but for a row whose value lies
+ *          within 2^-38 of the middle between two fp32 numbers.  For replicas that need all
+ *          bits equal rows have to lie alike
  *   y    = (h * rstd) * weight in fp32
  * Squares that overflow binary32 are taken scaled.  A row with a NaN has rstd NaN, one
  * with an infinity 0 (and NaNs where the infinities are).

@@ -117,6 +117,22 @@ def test_same_bits_however_rows_lie():
         assert off.sum() <= 1  # 2^-15 of the rows lie so near a border
 
 
+@pytest.mark.parametrize("r,c,dtype", [(100_000, 200, torch.float32), (100_000, 200, torch.bfloat16), (50_000, 500, torch.float16),
+                                       (10_000, 4096, torch.bfloat16), (5000, 9001, torch.float16), (5000, 4096, torch.float32),
+                                       (1000, 20_000, torch.float32)])
+def test_layouts_differ_at_borders_alone(r, c, dtype):
+    """Sums within 2^-38 of themselves, so values within 2^-39, and 2^-40 for what follows: bits turn only that near a
+    border.  (The mean in 64 bits is off by 2^-50 at most.)"""
+    x, _, w = inputs(r, c, dtype, dtype, 13)
+    some = slice(0, 120)
+    exact = torch.cat([1 / (t.double().square().mean(1) + 1e-6).sqrt() for t in x.split(8192)])
+    for got, want in ((apc.rms_norm(x, w)[2], exact), (apc.rms_norm(strided(x, 1, 1), w)[2], exact),
+                      (apc.rms_norm(x[some], w)[2], exact[some])):
+        turned = got != want.float()
+        border = (got.double() + want.float().double())[turned] / 2
+        assert ((border - want[turned]).abs() <= (2.0 ** -39 + 2.0 ** -40) * want[turned]).all()
+
+
 @pytest.mark.parametrize("c", [264, 1000, 1003])
 def test_norm_does_not_depend_on_the_grid(monkeypatch, c):
     x, res, w = inputs(1500, c, torch.bfloat16, torch.float32)
