@@ -326,7 +326,7 @@ def rms_norm_grad(dout, x, weight, rstd, *, dresidual=None, out=None, dweight=No
     if not size:
         _check(lib.apc_rms_norm_grad(*given, None, handle))
     elif workspace is not None:
-        if workspace.numel() > size // 4:
+        if workspace.numel() > size // 4 and workspace.is_contiguous():
             workspace = workspace.view(-1)[:size // 4]
         _check(lib.apc_rms_norm_grad(*given, _vector(workspace, "workspace", _F32, device, size // 4), handle))
     else:

@@ -298,6 +298,19 @@ def test_binding_checks_its_tensors(on_cpu):
     assert not on_cpu.calls
 
 
+def test_workspaces_that_are_refused_and_taken(on_cpu):
+    import torch
+    x, w = torch.zeros(3000, 400), torch.ones(400)
+    n = operators.rms_norm_grad_workspace(3000, 400)
+    for workspace in (torch.zeros(2 * n, 2)[:, 0], torch.zeros(n, 2)[:, 0], torch.zeros(n - 1), torch.zeros(n).int(), torch.zeros(n).double()):
+        with pytest.raises(ValueError):
+            apc.rms_norm_grad(x, x, w, torch.ones(3000), workspace=workspace)
+    assert not on_cpu.calls
+    for workspace in (torch.zeros(n), torch.zeros(n + 5), torch.zeros(2, n)):
+        apc.rms_norm_grad(x, x, w, torch.ones(3000), workspace=workspace)
+        assert on_cpu.calls[-1][1][5] == workspace.data_ptr()
+
+
 def test_allocated_outputs_are_memory_of_the_stream_given(on_cpu, monkeypatch):
     import torch
 
