@@ -302,7 +302,8 @@ def test_workspaces_that_are_refused_and_taken(on_cpu):
     import torch
     x, w = torch.zeros(3000, 400), torch.ones(400)
     n = operators.rms_norm_grad_workspace(3000, 400)
-    for workspace in (torch.zeros(2 * n, 2)[:, 0], torch.zeros(n, 2)[:, 0], torch.zeros(n - 1), torch.zeros(n).int(), torch.zeros(n).double()):
+    for workspace in (torch.zeros(2, n + 8)[:, :n], torch.zeros(2 * n, 2)[:, 0], torch.zeros(n, 2)[:, 0], torch.zeros(n - 1),
+                      torch.zeros(n).int(), torch.zeros(n).double()):
         with pytest.raises(ValueError):
             apc.rms_norm_grad(x, x, w, torch.ones(3000), workspace=workspace)
     assert not on_cpu.calls
