@@ -24,8 +24,9 @@ Entry points mirror the C names:
 * :mod:`.operators`: the norm in front of the output head and its gradient,
   8-bit quantization, the block-scaled 8-bit product and distillation, around
   the head of the step that makes the gradient (``rms_norm``, ``rms_norm_fp8``,
-  ``rms_norm_grad``, ``quantize_fp8``, ``matmul_fp8``, ``distill_loss``,
-  ``distill_grad``, ``distill_loss_grad``, here too).
+  ``rms_norm_grad``, ``rms_norm_grad_workspace``, ``quantize_fp8``,
+  ``matmul_fp8``, ``distill_loss``, ``distill_grad``, ``distill_loss_grad``, here
+  too).
 
 ``stream`` is a ``torch.cuda.Stream`` or a handle, the current stream if not
 given.  Outputs that a call allocates are memory of that stream: code on another
@@ -627,8 +628,8 @@ def state_buffers_bf16(p, m, v, global_offset: int = 0) -> list[BufferEntry]:
 __all__ += ["digests_to_host", "state_buffers", "device_status", "selftest_wait_timeout", "count_nonzero",
             "COMMIT_ZERO_GRAD", "GRAD_NORM_WORKSPACE", "F16", "grad_norm", "prepare_grads", "TensorEntryBF16", "commit_step_bf16", "state_buffers_bf16"]
 
-_OPERATORS = ("quantize_fp8", "matmul_fp8", "rms_norm", "rms_norm_fp8", "rms_norm_grad", "distill_loss", "distill_grad",
-              "distill_loss_grad")
+_OPERATORS = ("quantize_fp8", "matmul_fp8", "rms_norm", "rms_norm_fp8", "rms_norm_grad", "rms_norm_grad_workspace",
+              "distill_loss", "distill_grad", "distill_loss_grad")
 
 
 def __getattr__(name: str):

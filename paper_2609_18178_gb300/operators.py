@@ -25,7 +25,8 @@ from struct import Struct
 
 import torch
 
-__all__ = ["quantize_fp8", "matmul_fp8", "rms_norm", "rms_norm_fp8", "rms_norm_grad", "distill_loss", "distill_grad", "distill_loss_grad"]
+__all__ = ["quantize_fp8", "matmul_fp8", "rms_norm", "rms_norm_fp8", "rms_norm_grad", "rms_norm_grad_workspace", "distill_loss",
+           "distill_grad", "distill_loss_grad"]
 
 BLOCK = 128
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}

@@ -312,6 +312,11 @@ def test_workspaces_that_are_refused_and_taken(on_cpu):
         assert on_cpu.calls[-1][1][5] == workspace.data_ptr()
 
 
+def test_every_operator_is_the_package_s_too():
+    assert all(getattr(apc, n) is getattr(operators, n) for n in operators.__all__)
+    assert apc.rms_norm_grad_workspace(3000, 400) == 8 * 304 * 400  # as rms_norm_grad's documentation names it
+
+
 def test_allocated_outputs_are_memory_of_the_stream_given(on_cpu, monkeypatch):
     import torch
 
