@@ -746,10 +746,10 @@ __global__ void __launch_bounds__(V == 1 ? 512 : 1024, V == 1 ? 2 : 1) ring_forw
   float *const laid = reinterpret_cast<float *>(s_ring + ring.stages * ring.stage());
   if (a.then == 1) start_next();
   const Source src[2] = {{a.x, a.pitch}, {a.residual, a.residual_pitch}};
-  uint32_t next = blockIdx.x, into = 0;  // the row to copy next, its stage
+  uint32_t next = blockIdx.x, into = 0, issued = 0;  // the row to copy next, its stage; rows so far
   const auto issue = [&]() {
     if (next < a.rows) {
-      ring_issue<2>(sh, src, ring, s_ring + into * ring.stage(), &sh.full[into], next, a.rows, a.cols, sizeof(T), l2_evict_first());
+      issued += ring_issue<2>(sh, src, ring, s_ring + into * ring.stage(), &sh.full[into], next, a.rows, a.cols, sizeof(T), l2_evict_first());
       next += gridDim.x;
     }
     if (++into == ring.stages) into = 0;
@@ -826,6 +826,7 @@ __global__ void __launch_bounds__(V == 1 ? 512 : 1024, V == 1 ? 2 : 1) ring_forw
     }
     if (++stage == ring.stages) stage = 0, parity ^= 1;
   }
+  ring_end(sh, ring.stages, issued);
   if (a.then == 2) start_next();
 }
 

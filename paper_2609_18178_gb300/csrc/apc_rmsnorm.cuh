@@ -217,8 +217,9 @@ __device__ __forceinline__ void ring_begin(RingShared &sh, uint32_t stages, F is
   for (uint32_t s = 0; s + 1 < stages; ++s) issue();
 }
 
-// The bounded wait for a stage.  After one that gave up nothing more is copied and nothing
-// waited for; what follows is not to be used, as the status word says.
+// The bounded wait for a stage.  After one that gave up nothing more is copied and no stage
+// waited for; what follows is not to be used, as the status word says.  Copies that are under way
+// have to land before the CTA ends (ring_end).
 __device__ __noinline__ void ring_wait_on(RingShared &sh, uint32_t stage, uint32_t parity, unsigned *status) {
   if (*(volatile int *)&sh.dead || mbar_wait(&sh.full[stage], parity)) return;
   atomicOr(status, (unsigned)APC_ETIMEOUT);
@@ -238,11 +239,12 @@ struct Source {
   int64_t pitch;
 };
 
-// One thread: copy a row of each matrix into a stage.
+// One thread: copy a row of each matrix into a stage.  How many rows that were: 1, or 0 after a
+// wait that gave up.
 template <int M>
-__device__ __forceinline__ void ring_issue(RingShared &sh, const Source (&src)[M], const Ring &ring, uint8_t *stage, uint64_t *full,
+__device__ __forceinline__ uint32_t ring_issue(RingShared &sh, const Source (&src)[M], const Ring &ring, uint8_t *stage, uint64_t *full,
                                            uint32_t row, uint32_t rows, uint32_t cols, uint32_t size, uint64_t policy) {
-  if (*(volatile int *)&sh.dead) return;
+  if (*(volatile int *)&sh.dead) return 0;
   const uint32_t skip = skip_of(src[0].base, src[0].pitch, row, size);
   const uint32_t from = row == 0 && ring.edges & 1 ? 16 : 0;
   const uint32_t bytes = ((skip + cols * size + 15) & ~15u) - from - (row == rows - 1 && ring.edges & 2 ? 16 : 0);
@@ -253,6 +255,14 @@ __device__ __forceinline__ void ring_issue(RingShared &sh, const Source (&src)[M
     const uint8_t *at = static_cast<const uint8_t *>(src[m].base) + (int64_t)row * src[m].pitch * size - skip + from;
     bulk_g2s(stage + m * ring.region + from, at, bytes, full, policy);
   }
+  return 1;
+}
+
+// The thread that issued: after a wait that gave up, the (bounded) ones for the last copy into each
+// stage, of `issued` rows that went into the stages in turn.
+__device__ __forceinline__ void ring_end(RingShared &sh, uint32_t stages, uint32_t issued) {
+  if (threadIdx.x || !*(volatile int *)&sh.dead) return;
+  for (uint32_t u = issued > stages ? issued - stages : 0; u < issued; ++u) mbar_wait(&sh.full[u % stages], u / stages & 1);
 }
 
 // The elements of the blocks that ring_issue left out, in the first and the last row alone.

@@ -324,10 +324,10 @@ __global__ void __launch_bounds__(1024, 1) ring_grad_kernel(const __grid_constan
   constexpr int kMats = kAgain ? 2 : 3;
   Source src[kMats] = {{a.x, a.pitch}, {a.dout, a.dout_pitch}};
   if constexpr (!kAgain) src[2] = {a.dresidual, a.dresidual_pitch};
-  uint32_t next_part = blockIdx.x, next = next_part, into = 0;
+  uint32_t next_part = blockIdx.x, next = next_part, into = 0, issued = 0;
   const auto issue = [&]() {
     if (next_part < a.parts) {
-      ring_issue<kMats>(sh, src, ring, s_ring + into * ring.stage(), &sh.full[into], next, a.rows, a.cols, sizeof(T), l2_evict_first());
+      issued += ring_issue<kMats>(sh, src, ring, s_ring + into * ring.stage(), &sh.full[into], next, a.rows, a.cols, sizeof(T), l2_evict_first());
       next += a.parts;
       if (next >= a.rows) next = next_part += gridDim.x;
     }
@@ -417,6 +417,7 @@ __global__ void __launch_bounds__(1024, 1) ring_grad_kernel(const __grid_constan
     for (uint32_t k = threadIdx.x; k < a.cols; k += blockDim.x) a.partial[(uint64_t)part * a.cols + k] = sums[k];
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the next copy comes behind a barrier
   }
+  ring_end(sh, ring.stages, issued);
 }
 
 // Few rows: a cluster of so many CTAs (0: none) of so many groups, up to 8 rows for each.  It
