@@ -138,8 +138,8 @@ apc_status check_norm(const apc_norm *d, Ranges *rs, apc::NormArgs *a) {
   a->weight = d->weight;
   a->sum = d->sum;
   a->pitch = pitch_of(r, c, d->pitch);
-  a->residual_pitch = pitch_of(r, c, d->residual_pitch);
-  a->sum_pitch = pitch_of(r, c, d->sum_pitch);
+  a->residual_pitch = adds ? pitch_of(r, c, d->residual_pitch) : 0;  // else whatever the caller left there
+  a->sum_pitch = adds ? pitch_of(r, c, d->sum_pitch) : 0;
   a->rows = (uint32_t)r;
   a->cols = (uint32_t)c;
   a->dtype = d->dtype;
@@ -254,7 +254,7 @@ APC_EXPORT apc_status apc_rms_norm_grad(const apc_norm_grad *d, void *dx, int64_
   a.work = workspace;
   a.dout_pitch = pitch_of(r, c, d->dout_pitch);
   a.pitch = pitch_of(r, c, d->pitch);
-  a.dresidual_pitch = pitch_of(r, c, d->dresidual_pitch);
+  a.dresidual_pitch = d->dresidual ? pitch_of(r, c, d->dresidual_pitch) : 0;
   a.dx_pitch = pitch_of(r, c, dx_pitch);
   a.rows = (uint32_t)r;
   a.cols = (uint32_t)c;

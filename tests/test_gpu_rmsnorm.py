@@ -330,6 +330,28 @@ def test_dx_does_not_depend_on_dweight(dtype):
                 assert torch.equal(*out)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_pitches_of_what_is_not_there(dtype):
+    """Without a residual its pitch says nothing, not about which kernel runs either."""
+    r, c = 200, 1000
+    x, d, w = inputs(r, c, dtype, dtype, 17)
+    kind = apc.operators._DTYPE[dtype]
+    handle = torch.cuda.current_stream().cuda_stream
+    rstd, dw = torch.empty(r, device="cuda"), torch.empty_like(w)
+    work = torch.empty(apc.operators.rms_norm_grad_workspace(r, c), device="cuda")
+    want = None
+    for pitch in (0, c, 5, -3, 1 << 62):
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        norm = apc.operators._pack_norm(x.data_ptr(), 0, w.data_ptr(), 0, r, c, c, pitch, pitch, kind, kind, 1e-6)
+        apc._check(apc.library().apc_rms_norm(norm, y.data_ptr(), c, rstd.data_ptr(), handle))
+        grad = apc.operators._pack_norm_grad(d.data_ptr(), x.data_ptr(), w.data_ptr(), 0, rstd.data_ptr(), r, c, c, c, pitch, kind, kind)
+        apc._check(apc.library().apc_rms_norm_grad(grad, dx.data_ptr(), c, dw.data_ptr(), kind, work.data_ptr() if work.numel() else None, handle))
+        got = y, rstd.clone(), dx, dw.clone()
+        want = got if want is None else want
+        for p, q in zip(got, want):
+            assert torch.equal(p, q)
+
+
 def test_grad_against_differences():
     """The formula is the derivative of the forward definition, in 64 bits; the kernel follows the formula."""
     x, d, w = inputs(4, 96, torch.float32, torch.float32)
