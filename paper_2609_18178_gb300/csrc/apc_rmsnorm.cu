@@ -109,22 +109,26 @@ __device__ __forceinline__ Stat warp_stat(Two p) {
 
 struct NormConst {
   float inv_hi, inv_lo, eps_hi, eps_lo;  // 1/cols and eps in two parts
+
+  // for rows whose elements are taken times `scale`, a power of two
+  __device__ __forceinline__ NormConst scaled(float scale) const {
+    return {inv_hi, inv_lo, eps_hi * scale * scale, eps_lo * scale * scale};
+  }
 };
 
 // 1 / sqrt((hi + lo) * 2^k / cols + eps), rounded to nearest but for one in some 2^20.
-__device__ __forceinline__ float rstd_of(float hi, float lo, int k, const NormConst &c, bool with_eps) {
+__device__ __forceinline__ float rstd_of(float hi, float lo, int k, const NormConst &c) {
   const float two_k = __uint_as_float((uint32_t)(k + 127) << 23);
   float m = hi * c.inv_hi, rest = __fmaf_rn(hi, c.inv_hi, -m);
   rest += hi * c.inv_lo + lo * c.inv_hi;
   m *= two_k, rest *= two_k;
-  if (with_eps) {
-    const float s = m + c.eps_hi, b = s - m;
-    rest += ((m - (s - b)) + (c.eps_hi - b)) + c.eps_lo;
-    m = s;
-  }
-  const float move = m > 0x1p60f ? 0x1p-80f : m < 0x1p-60f ? 0x1p80f : 1.0f;
-  const float back = m > 0x1p60f ? 0x1p-40f : m < 0x1p-60f ? 0x1p40f : 1.0f;
+  const float top = fmaxf(m, c.eps_hi);  // mean and eps may be large enough for their sum to overflow
+  const float move = top > 0x1p60f ? 0x1p-80f : top < 0x1p-60f ? 0x1p80f : 1.0f;
+  const float back = top > 0x1p60f ? 0x1p-40f : top < 0x1p-60f ? 0x1p40f : 1.0f;
   m *= move, rest *= move;
+  const float eps = c.eps_hi * move, s = m + eps, b = s - m;
+  rest += ((m - (s - b)) + (eps - b)) + c.eps_lo * move;
+  m = s;
   float y;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(m));
   // a Newton step whose remainder 1 - (m + rest) y^2 is taken with y^2 in two parts
@@ -139,14 +143,14 @@ __device__ __forceinline__ void split_sum(uint32_t s, float &hi, float &lo) {
 }
 
 // rstd of a row whose threads' sums of squares are p; false: a sum is not finite.
-__device__ __forceinline__ bool row_rstd(Two p, const Group &g, Stat *room, const NormConst &c, bool with_eps, float *rstd) {
+__device__ __forceinline__ bool row_rstd(Two p, const Group &g, Stat *room, const NormConst &c, float *rstd) {
   Stat s = warp_stat(p);
   float hi, lo;
   if (g.warps == 1) {
     if (s.e == 255) return false;
     split_sum(s.sum, hi, lo);
     lo += (float)s.low * 0x1p-20f;
-    *rstd = rstd_of(hi, lo, (int)s.e - 152, c, with_eps);
+    *rstd = rstd_of(hi, lo, (int)s.e - 152, c);
     return true;
   }
   if (g.lane == 0) room[g.warp] = s;
@@ -158,7 +162,7 @@ __device__ __forceinline__ bool row_rstd(Two p, const Group &g, Stat *room, cons
     const uint32_t high = __reduce_add_sync(~0u, (uint32_t)(v >> 26)), low = __reduce_add_sync(~0u, (uint32_t)v & 0x3ffffffu);
     split_sum(high, hi, lo);
     lo += (float)low * 0x1p-26f;
-    const float r = rstd_of(hi, lo, (int)min(e, 254u) - 146, c, with_eps);
+    const float r = rstd_of(hi, lo, (int)min(e, 254u) - 146, c);
     if (g.lane == 0) room[g.warps] = {__float_as_uint(r), e, 0};
   } else {
     g.arrive();
@@ -190,7 +194,7 @@ __device__ __forceinline__ uint32_t largest(const uint32_t (&w)[8 / Word<T>::kPe
 }
 
 // rstd of a row some of whose threads' sums are not finite: infinities and NaNs, or
-// squares beyond the largest number, which are taken scaled (eps is nothing beside them).
+// squares beyond the largest number, which are taken scaled, and eps too.
 template <typename T, int V>
 __device__ __forceinline__ float wild_rstd(const uint32_t (&w)[V][8 / Word<T>::kPer], const Group &g, Stat *room, const NormConst &c) {
   uint32_t m = 0;
@@ -203,7 +207,7 @@ __device__ __forceinline__ float wild_rstd(const uint32_t (&w)[V][8 / Word<T>::k
   float rstd;
 #pragma unroll
   for (int v = 0; v < V; ++v) p = p + squares<T, true>(w[v], scale);
-  row_rstd(p, g, room, c, false, &rstd);
+  row_rstd(p, g, room, c.scaled(scale), &rstd);
   g.sync();
   return rstd * scale;
 }
@@ -352,7 +356,7 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
       return LONG ? all.sum() : p;
     };
     float rstd;
-    if (!row_rstd(sum_of(false, [](const auto &x) { return squares<T>(x); }), g, room, a.c, true, &rstd)) {
+    if (!row_rstd(sum_of(false, [](const auto &x) { return squares<T>(x); }), g, room, a.c, &rstd)) {
       uint32_t m = 0;
       over_row(true, [&](uint32_t) {
 #pragma unroll
@@ -361,9 +365,9 @@ __global__ void __launch_bounds__(1024, 1) forward_kernel(const __grid_constant_
       m = group_max(m, g, room);
       if (m >= 0x7f800000u) {
         rstd = m > 0x7f800000u ? __uint_as_float(0x7fffffffu) : 0.0f;
-      } else {  // squares beyond the largest number: eps is nothing beside them
+      } else {  // squares beyond the largest number
         const float scale = __uint_as_float(max(254u - (m >> 23), 1u) << 23);
-        row_rstd(sum_of(true, [&](const auto &x) { return squares<T, true>(x, scale); }), g, room, a.c, false, &rstd);
+        row_rstd(sum_of(true, [&](const auto &x) { return squares<T, true>(x, scale); }), g, room, a.c.scaled(scale), &rstd);
         rstd *= scale;
         g.sync();
       }
@@ -451,7 +455,7 @@ __global__ void __launch_bounds__(256) narrow_kernel(const __grid_constant__ For
       Two p;
 #pragma unroll
       for (int v = 0; v < V; ++v) p = v ? p + squares<T>(w[u][v]) : squares<T>(w[u][v]);
-      if (!row_rstd(p, g, nullptr, a.c, true, &rstd[u])) rstd[u] = wild_rstd<T, V>(w[u], g, nullptr, a.c);
+      if (!row_rstd(p, g, nullptr, a.c, &rstd[u])) rstd[u] = wild_rstd<T, V>(w[u], g, nullptr, a.c);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -792,7 +796,7 @@ __global__ void __launch_bounds__(V == 1 ? 512 : 1024, V == 1 ? 2 : 1) ring_forw
     }
     // before the next copy into a stage that was written here
     if (OUT != kSame && skip) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    const bool fine = row_rstd(p, g, sh.stats[turn ^= 1], a.c, true, &rstd);
+    const bool fine = row_rstd(p, g, sh.stats[turn ^= 1], a.c, &rstd);
     if (threadIdx.x == 0) issue();  // into the stage of the row before, which all have left
     if (!fine) rstd = wild_rstd<T, V>(w, g, sh.stats[turn], a.c);
     if (threadIdx.x == 0) a.rstd[row] = rstd;

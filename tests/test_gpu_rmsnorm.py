@@ -211,6 +211,23 @@ def test_rows_of_huge_values(r, c):
         assert ((y.double() - want).abs() <= (UNIT[dtype] + 3 * U) * want.abs() + TINY[dtype] * 2).all()
 
 
+@pytest.mark.parametrize("r", [8, 400, 2000])
+@pytest.mark.parametrize("c", [1, 100, 4096, 5003, 20_000])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_any_eps(r, c, dtype):
+    """eps counts beside squares that overflow, and a mean and an eps whose sum does are no infinity."""
+    if r * c > 10_000_000:
+        r = 400
+    x, _, w = inputs(r, c, dtype, dtype)
+    for i, size in enumerate((1e16, 1e19, 1.2e19, 1e20, 1e28)):
+        x[i] *= size / x[i].float().abs().max()
+    x[5], x[5, 0] = 0, 2e19  # one element whose square overflows
+    x[6], x[6, ::2] = 0, 1.8e19
+    x[7] = 1.3e19
+    for eps in (1e-20, 1e-5, 1.0, 1e10, 1e25, 1e36, 1e38, 3e38):
+        check_rstd(x, eps, apc.rms_norm(x, w, eps=eps)[2])
+
+
 @pytest.mark.parametrize("r", [8, 400])
 @pytest.mark.parametrize("c", [100, 4096, 5003, 20_000])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
