@@ -219,8 +219,9 @@ apc_status apc_count_nonzero(const apc_buffer *bufs, int32_t num_bufs, int32_t n
 
 #define APC_GRAD_NORM_WORKSPACE 2056 /* bytes, at most */
 
-/* Bytes that apc_grad_norm's workspace takes for such a list: 0 (a small list, up to some
- * 6 million 16-bit elements) or APC_GRAD_NORM_WORKSPACE.  Host only, no CUDA call. */
+/* Bytes that apc_grad_norm's workspace takes for such a list: 0 (a small list: up to 1,600
+ * buffers in 4,096 tiles of 4 KB, which are 8.4 million 16-bit elements, fewer where many buffers
+ * end inside a tile) or APC_GRAD_NORM_WORKSPACE.  Host only, no CUDA call. */
 int64_t apc_grad_norm_workspace(const apc_buffer *bufs, int32_t num_bufs);
 
 /* The 2-norm of the elements of a list of buffers, read only: the norm of a
@@ -248,7 +249,8 @@ apc_status apc_grad_norm(const apc_buffer *bufs, int32_t num_bufs, int32_t num_s
  *   g' = c * g in binary32, one rounding, takes g's place in the update; the gradient
  *        buffers are left as they are (or zeroed, by flags)
  * grad_norm (device, fp32, one value) is read when the kernel runs: apc_grad_norm's output
- * on the same stream, or that of all ranks together.  An infinite norm gives c = 0, a NaN
+ * on the same stream, or that of all ranks together: the root of the sum of their norms'
+ * squares, added in one order so that all clip alike.  An infinite norm gives c = 0, a NaN
  * c = NaN.  max_norm: > 0 and finite, as binary32 too.
  * Errors as apc_commit_step_ex; grad_norm must not overlap anything that is written. */
 apc_status apc_commit_step_clipped(const apc_tensor *table, int32_t num_tensors, const apc_adamw_hparams *hp, int64_t step,
@@ -366,7 +368,7 @@ apc_status apc_rms_norm_fp8(const apc_norm *d, const apc_fp8_matrix *q, const ap
  *   dx      = (g - z * mean of g z) * rstd + dresidual   (x's gradient and residual's)
  *   dweight = sum over rows of dout * z
  * in fp32, each rounded once.  The sums' orders follow the sizes, the types and how the
- * matrices lie within 16 bytes, not the grid.
+ * matrices lie within 16 bytes, not the grid; dx's not whether dweight is wanted.
  *   x          h: the norm's sum, or its x where there was no residual
  *   dresidual  the gradient that reaches sum otherwise, or NULL
  *   rstd       as the norm left it */

@@ -452,6 +452,9 @@ def grad_norm(grads, num_slots: int = 1, stream=None, out=None, workspace=None):
     (their gradients), a commit table prepared by :func:`prepare_table`, or a
     list prepared by :func:`prepare_grads`.
 
+    A list is packed by each call, at some 2 us of host time a tensor: prepared
+    ones are for jobs whose gradients stay where they are.
+
     Returns the device float32[num_slots] tensor of norms.  ``workspace``:
     ``GRAD_NORM_WORKSPACE`` bytes for a caller that keeps its own, which no
     other call may use at the same time; short lists take none."""

@@ -388,10 +388,11 @@ bool aligned(const void *p, int64_t pitch_bytes) { return (uintptr_t)p % 16 == 0
 
 // More rows than `least`, of 16 bits, alike within 16 bytes: the ring's shape, or none (threads
 // 0).  Where rows begin at blocks and end with them, plain loads by more warps keep up with it
-// for some (pays): 8192 x 4096 to 8 bits takes 45 us (50 by plain loads), to 16 bits 48 (51), its
-// gradient 53 (63), but the gradient of 16384 x 1024 33 (31).  fp32 rows do better without it
-// too: 4883 x 4096 52 us (60).  Elsewhere in the matrix 16-bit rows need it: 4001 x 5001 to 16
-// bits 35 us (46), its gradient 49 (100).
+// for some (pays): 8192 x 4096 to 8 bits takes 45 us (47 by plain loads), to 16 bits without a residual
+// 31 (34), its gradient 50 (60), but the gradient of 16384 x 1024 33 (30).  To 16 bits with a residual
+// plain loads are ahead, and this rule takes the ring all the same: 8192 x 4096 48 us (45), 1221 x
+// 16384 44 (34).  fp32 rows do better without it too: 4883 x 4096 52 us (60).  Elsewhere in the matrix
+// 16-bit rows need it: 4001 x 5001 to 16 bits 36 us (41), its gradient 49 (94).
 struct RingShape {
   uint32_t threads;
   int v;

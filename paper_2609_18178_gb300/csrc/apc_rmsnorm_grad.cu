@@ -310,7 +310,7 @@ __device__ __forceinline__ void unit_load(uint32_t (&w)[8 / Word<T>::kPer], cons
 // ...: rows of a part begin alike.  Rows of more than 1,024 units, two a thread (V): two stages of x
 // and dout are what fits, dresidual comes into registers, and z and g are formed twice.  Bound:
 // memory, at 5.8 TB/s for 8192 x 4096 (45.5 us of 50, then the parts); above 8,192 columns the wait
-// for the one row under way: 1221 x 16384 in 48 us, by plain loads 70.
+// for the one row under way: 1221 x 16384 in 49 us, by plain loads 67.
 template <typename T, int V, bool WHOLE>
 __global__ void __launch_bounds__(1024, 1) ring_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ Ring ring) {
   constexpr int kWords = 8 / Word<T>::kPer;
